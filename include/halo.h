@@ -408,6 +408,107 @@ halo_status halo_group_lm_head_i4(const halo_lm_shape* shape, const void* Q, con
                                   void* stream);
 
 /* ------------------------------------------------------------------------
+ * The attention block of a batched token step on a paged K/V cache: append, attention, the residual between blocks.
+ * Beside halo_mha_* (one sequence, dense cache, no position rotation, one K/V head per head) these serve many
+ * sequences of different lengths, grouped K/V heads and rotated positions.
+ *
+ * halo_paged_shape: n_heads % n_kv_heads == 0, n_heads <= HALO_MAX_GROUPS; query head h reads K/V head
+ *   h / (n_heads / n_kv_heads).  head_dim a multiple of 16, <= 256.  dtype: queries, caches and outputs.
+ *   K_cache, V_cache device [n_pages][n_kv_heads][page_size][head_dim], one page every page_stride elements (0 = dense;
+ *   else a multiple of 8, at least n_kv_heads * page_size * head_dim), so that K and V pages may lie interleaved.
+ *   block_table device int32 [n_seq][max_pages]: position p of sequence s is row p % page_size of page
+ *   block_table[s][p / page_size].  Sequences may share pages that are only read.  max_pages * page_size < 2^31.
+ *
+ * halo_paged_kv_append: for every token t with pos[t] >= 0: its keys, turned by the position, and its values are
+ *   written at position pos[t] of sequence seq_of_tok[t], its queries, turned, to q_out.
+ *   q, q_out device [n_tok] rows of n_heads * head_dim; k, v rows of n_kv_heads * head_dim; rows every *_stride elements
+ *     (a whole number of 16 bytes), so that they may lie side by side in one projection's output.  q_out may be q.
+ *     q and q_out NULL: keys and values only.
+ *   pos device int32 [n_tok]; a negative position marks a padding row: nothing of it is read or written.
+ *   seq_of_tok device int32 [n_tok], or NULL: token t belongs to sequence t (n_tok <= n_seq).
+ *   inv_freq device double [rotary_dim / 2]: pair i is turned by the angle pos * inv_freq[i] (formed in fp64, so far
+ *     positions keep their angle).  Pairs are (2i, 2i + 1) if interleaved != 0, else (i, i + rotary_dim / 2);
+ *     elements from rotary_dim (even, <= head_dim; 0 = no rotation, inv_freq may be NULL) on are copied.
+ *   One rounding to dtype.  A position behind the table, a sequence or a page out of range sets HALO_DEV_BAD_INDEX and
+ *   the token is skipped.  Two tokens of one call must not have the same place in the cache (the bytes of either may
+ *   remain).
+ *
+ * halo_paged_mha: for every sequence s and head h, over the positions p < seq_len[s]:
+ *     w = softmax(scale * <q[s][h], K_p>),  out[s][h] = sum_p w_p V_p,  lse[s][h] = log sum_p exp(scale * <q[s][h], K_p>).
+ *   q device, rows of n_heads * head_dim every q_stride elements; out device [n_seq][n_heads][head_dim]; lse device fp32
+ *     [n_seq][n_heads] or NULL; seq_len device int32 [n_seq] (0 allowed).
+ *   keep device uint8 [n_heads] or NULL: heads with 0 (what halo_select_groups lost) give zeros; K/V heads of which
+ *     every head is lost are not read.
+ *   A row without positions (length 0, a lost head, scores that are all -infinity) gives zeros and lse = -infinity.
+ *   Cache rows behind the length are never read into the result, whatever they hold.  In fp32 an infinity among the
+ *   values that are read may come out as NaN (products are formed from two parts); bf16 follows the formula.
+ *   fp32 sums and softmax; bf16 caches: weights rounded to bf16 before they meet the values.
+ *   A length that is negative or behind the table counts as 0, positions on a page out of range are left out; both set
+ *   HALO_DEV_BAD_INDEX.
+ *   workspace: halo_paged_mha_workspace_bytes(shape, n_seq) bytes, device; calls that may overlap on the GPU need one
+ *   each.  The result does not depend on timing.  n_seq <= HALO_MAX_SEQUENCES.
+ *
+ * halo_norm_glue: halo_glue with a norm behind the block, gains, a gate and a residual scale:
+ *     n(v) = v / sqrt(mean(v^2) + eps),  u = w_post ? n(y) * w_post : y,
+ *     h_out = h + res_scale * gate * u,  x_out = cast(n(h_out) * w_pre)      per token
+ *   h, h_out device fp32 [n_tok][d] (h_out may alias h); y device [n_tok][d] in ydtype, or NULL (h_out = h);
+ *   w_post, w_pre device [d], gate device rows of d every gate_stride elements (0: one row for all tokens), x_out device
+ *   [n_tok][d], all in xdtype; w_post, w_pre and gate may be NULL (absent).  d_model % 8 == 0, <= HALO_MAX_NORM_WIDTH;
+ *   eps > 0.  fp32 sums.
+ * ---------------------------------------------------------------------- */
+#define HALO_MAX_SEQUENCES 8192
+#define HALO_MAX_NORM_WIDTH 16384
+typedef struct {
+    int n_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages;
+    long long page_stride;
+    halo_dtype dtype;
+} halo_paged_shape;
+typedef struct {
+    int d_model;
+    float eps;
+    halo_dtype ydtype, xdtype;
+} halo_norm_shape;
+halo_status halo_paged_kv_append(const halo_paged_shape* shape, int n_tok, int n_seq, const void* q, long long q_stride,
+                                 const void* k, long long k_stride, const void* v, long long v_stride, const int32_t* pos,
+                                 const int32_t* seq_of_tok, const int32_t* block_table, const double* inv_freq,
+                                 int rotary_dim, int interleaved, void* q_out, long long q_out_stride, void* K_cache,
+                                 void* V_cache, uint32_t* dev_status, void* stream);
+size_t halo_paged_mha_workspace_bytes(const halo_paged_shape* shape, int n_seq);
+halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, const void* q, long long q_stride, const void* K_cache,
+                           const void* V_cache, const int32_t* block_table, const int32_t* seq_len, const uint8_t* keep,
+                           float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                           uint32_t* dev_status, void* stream);
+halo_status halo_norm_glue(const halo_norm_shape* shape, int n_tok, const float* h, const void* y, const void* w_post,
+                           const void* gate, long long gate_stride, float res_scale, const void* w_pre, float* h_out,
+                           void* x_out, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Rows in microscaled 4-bit floating point, the 4-bit form that the tensor cores multiply as it is: beside
+ * halo_quantize_rows_i4 (4-bit weights, bf16 activations) here both sides are 4-bit.
+ *   32 consecutive elements of a row share a power of two 2^e, e = max(floor(log2(amax)) - 2, -127), stored as the byte
+ *   e + 127; an element is the nearest of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} times it, ties to the even code, larger ones
+ *   become 6; code = sign * 8 + index, two codes a byte, element 2i in the low half of byte i.  A block that holds a NaN
+ *   or an infinity gets the scale byte 255 and all its values read back as NaN.
+ *   d_model % 128 == 0, <= HALO_MX4_MAX_WIDTH; n_rows <= HALO_MX4_MAX_ROWS; everything 16-byte aligned, device.
+ *   Q uint8 [n_rows][d_model / 2].  scales: halo_mx4_scale_bytes(d_model, n_rows) bytes, blocks of 512 bytes for 128 rows
+ *     x 128 elements [ceil(n_rows / 128)][d_model / 128]: byte (r % 32) * 16 + (r / 32) * 4 + j for row r of the 128 and
+ *     run j of the four runs of 32 elements; rows behind n_rows are zero.
+ *   halo_quantize_rows_mx4: W [n_rows][d_model] in wdtype -> Q, scales.  halo_dequantize_rows_mx4: back, exactly.
+ *   halo_product_mx4: y[t][r] = <x_t, w_r>, x = (Qx, Sx) of n_tok rows, w = (Qw, Sw) of n_rows rows; y [n_tok][n_rows] in
+ *     ydtype, one rounding of fp32 sums.  n_tok <= HALO_MX4_MAX_TOKENS.  The same call gives the same bits.
+ * ---------------------------------------------------------------------- */
+#define HALO_MX4_MAX_WIDTH 65536
+#define HALO_MX4_MAX_ROWS (1 << 24)
+#define HALO_MX4_MAX_TOKENS (1 << 20)
+size_t halo_mx4_scale_bytes(int d_model, long long n_rows);
+halo_status halo_quantize_rows_mx4(int d_model, long long n_rows, halo_dtype wdtype, const void* W, void* Q, void* scales,
+                                   void* stream);
+halo_status halo_dequantize_rows_mx4(int d_model, long long n_rows, halo_dtype wdtype, const void* Q, const void* scales,
+                                     void* W, void* stream);
+halo_status halo_product_mx4(int d_model, int n_tok, int n_rows, const void* Qx, const void* Sx, const void* Qw,
+                             const void* Sw, halo_dtype ydtype, void* y, uint32_t* dev_status, void* stream);
+
+/* ------------------------------------------------------------------------
  * One block, steps a1..a9 in one call (the Pred, Comp and merge of one block of the generation phase,
  * Sec. III-B.3): scores from `feat` (the input of the previous block: one layer ahead), selection and arrival
  * draw for (step, layer), FFN of `x` over the kept groups, merge of what arrived.  Same results as calling

@@ -1,0 +1,177 @@
+// halo_quantize_rows_mx4 / halo_dequantize_rows_mx4: rows in microscaled 4-bit floating point.
+//
+// 32 consecutive elements of a row share a power of two 2^e, e = floor(log2(amax)) - 2, kept as the byte e + 127
+// (0 at least; 255 = the block holds a NaN or an infinity); an element is the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6
+// times it, ties to the even code, larger ones become 6.  HBM-bound: one pass, every element read once.
+//
+// Codes: two a byte, the lower element in the low half, rows dense.  Scales: in blocks of 512 bytes for 128 rows x 128
+// elements, byte (r % 32) * 16 + (r / 32) * 4 + j for row r of the 128 and block j of the 4, the order in which the
+// tensor cores take them from tensor memory (halo_product_mx4 copies a block there as it is).
+//
+// Four lanes hold a block of 32 (8 elements each), so a warp reads 256 consecutive elements, writes 128 consecutive
+// code bytes, and 16 lanes meet for one 4-byte word of scales.
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace halo {
+namespace {
+
+constexpr int kThreads = 256;
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
+    if constexpr (sizeof(T) == 4) {
+        const uint4 a = ldg_stream16(p), b = ldg_stream16(p + 4);
+        f[0] = __uint_as_float(a.x); f[1] = __uint_as_float(a.y); f[2] = __uint_as_float(a.z); f[3] = __uint_as_float(a.w);
+        f[4] = __uint_as_float(b.x); f[5] = __uint_as_float(b.y); f[6] = __uint_as_float(b.z); f[7] = __uint_as_float(b.w);
+    } else {
+        Elem<__nv_bfloat16>::widen(ldg_stream16(p), f);
+    }
+}
+// two values -> two codes in a byte, the first in the low half (round to nearest even, 6 at most)
+__device__ __forceinline__ uint32_t e2m1x2(float lo, float hi) {
+    uint32_t r;
+    asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u32.u8 %0, t;\n\t}" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// 2^(code - 127); 255 is NaN
+__device__ __forceinline__ float scale_of(uint32_t code) {
+    return __uint_as_float(code == 0 ? 0x00400000u : code == 255u ? 0x7fc00000u : code << 23);
+}
+
+// One unit = 8 elements of a row; the rows behind n_rows up to a multiple of 128 get scales of zero.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+quantize_mx4_kernel(int d, long long n_rows, long long units, const T* __restrict__ W, uint32_t* __restrict__ Q,
+                    uint32_t* __restrict__ S) {
+    const int per_row = d / 8;
+    const int lane = threadIdx.x & 31;
+    for (long long u = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x; u < units;
+         u += static_cast<long long>(gridDim.x) * kThreads) {
+        const long long row = u / per_row;
+        const int c = static_cast<int>(u - row * per_row);
+        uint32_t top = 0, word = 0, scale = 0;
+        float f[8];
+        const bool real = row < n_rows;
+        if (real) {
+            load8(W + row * d + c * 8, f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
+        }
+        // per_row is a multiple of 16: the 16 lanes of a word of scales are always on one row, and alive together
+        const uint32_t group = 0xffffu << (lane & 16);
+        top = max(top, __shfl_xor_sync(group, top, 1));
+        top = max(top, __shfl_xor_sync(group, top, 2));
+        if (real) {
+            const uint32_t field = top >> 23;
+            scale = field == 255u ? 255u : field < 2u ? 0u : field - 2u;
+            const float inv = __uint_as_float((254u - min(scale, 252u)) << 23);   // 2^(127 - scale), exact
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) word |= e2m1x2(f[e] * inv, f[e + 1] * inv) << (e * 4);
+            if (scale == 255u) word = 0;
+            Q[(row * d + c * 8) >> 3] = word;
+        }
+        uint32_t four = scale << (((lane >> 2) & 3) * 8);
+        four |= __shfl_xor_sync(group, four, 4);
+        four |= __shfl_xor_sync(group, four, 8);
+        if ((lane & 15) == 0) {
+            const long long block = (row >> 7) * (d >> 7) + (c >> 4);
+            S[block * 128 + (row & 31) * 4 + ((row >> 5) & 3)] = four;
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+dequantize_mx4_kernel(int d, long long units, const uint32_t* __restrict__ Q, const uint8_t* __restrict__ S,
+                      T* __restrict__ W) {
+    const int per_row = d / 8;
+    for (long long u = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x; u < units;
+         u += static_cast<long long>(gridDim.x) * kThreads) {
+        const long long row = u / per_row;
+        const int c = static_cast<int>(u - row * per_row);
+        const uint32_t word = __ldg(Q + u);
+        const long long block = (row >> 7) * (d >> 7) + (c >> 4);
+        const float scale = scale_of(__ldg(S + block * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + ((c >> 2) & 3)));
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            uint32_t h;
+            asm("{\n\t.reg .b8 t;\n\tcvt.u8.u32 t, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, t;\n\t}" : "=r"(h) : "r"((word >> (e * 4)) & 0xffu));
+            const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h));
+            f[e] = v.x * scale;
+            f[e + 1] = v.y * scale;
+        }
+        T* out = W + u * 8;
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<float4*>(out) = make_float4(f[0], f[1], f[2], f[3]);
+            *reinterpret_cast<float4*>(out + 4) = make_float4(f[4], f[5], f[6], f[7]);
+        } else {
+            __nv_bfloat162 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);   // exact: two significant bits
+            *reinterpret_cast<uint4*>(out) =
+                make_uint4(*reinterpret_cast<uint32_t*>(&v[0]), *reinterpret_cast<uint32_t*>(&v[1]),
+                           *reinterpret_cast<uint32_t*>(&v[2]), *reinterpret_cast<uint32_t*>(&v[3]));
+        }
+    }
+}
+
+halo_status check_rows(int d_model, long long n_rows, halo_dtype dtype) {
+    if (dtype != HALO_F32 && dtype != HALO_BF16) return HALO_ERR_DTYPE;
+    if (d_model <= 0 || d_model % 128 != 0 || d_model > HALO_MX4_MAX_WIDTH || n_rows <= 0 || n_rows > HALO_MX4_MAX_ROWS)
+        return HALO_ERR_SHAPE;
+    return HALO_OK;
+}
+unsigned grid_for(long long units) {
+    const long long blocks = (units + kThreads - 1) / kThreads;
+    const long long most = static_cast<long long>(kSmCount) * 8 * 4;
+    return static_cast<unsigned>(blocks < most ? blocks : most);
+}
+
+}  // namespace
+}  // namespace halo
+
+using namespace halo;
+
+extern "C" size_t halo_mx4_scale_bytes(int d_model, long long n_rows) {
+    if (check_rows(d_model, n_rows, HALO_F32) != HALO_OK) return 0;
+    return static_cast<size_t>((n_rows + 127) / 128) * (d_model / 128) * 512;
+}
+
+extern "C" halo_status halo_quantize_rows_mx4(int d_model, long long n_rows, halo_dtype wdtype, const void* W, void* Q,
+                                              void* scales, void* stream) {
+    const halo_status rc = check_rows(d_model, n_rows, wdtype);
+    if (rc != HALO_OK) return rc;
+    if (!W || !Q || !scales) return HALO_ERR_ARG;
+    if (!aligned16(W) || !aligned16(Q) || !aligned16(scales)) return HALO_ERR_ALIGN;
+    const long long units = (n_rows + 127) / 128 * 128 * (d_model / 8);
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (wdtype == HALO_BF16)
+        quantize_mx4_kernel<__nv_bfloat16><<<grid_for(units), kThreads, 0, st>>>(
+            d_model, n_rows, units, static_cast<const __nv_bfloat16*>(W), static_cast<uint32_t*>(Q), static_cast<uint32_t*>(scales));
+    else
+        quantize_mx4_kernel<float><<<grid_for(units), kThreads, 0, st>>>(
+            d_model, n_rows, units, static_cast<const float*>(W), static_cast<uint32_t*>(Q), static_cast<uint32_t*>(scales));
+    HALO_CHECK_LAUNCH();
+    return HALO_OK;
+}
+
+extern "C" halo_status halo_dequantize_rows_mx4(int d_model, long long n_rows, halo_dtype wdtype, const void* Q,
+                                                const void* scales, void* W, void* stream) {
+    const halo_status rc = check_rows(d_model, n_rows, wdtype);
+    if (rc != HALO_OK) return rc;
+    if (!W || !Q || !scales) return HALO_ERR_ARG;
+    if (!aligned16(W) || !aligned16(Q) || !aligned16(scales)) return HALO_ERR_ALIGN;
+    const long long units = n_rows * (d_model / 8);
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (wdtype == HALO_BF16)
+        dequantize_mx4_kernel<__nv_bfloat16><<<grid_for(units), kThreads, 0, st>>>(
+            d_model, units, static_cast<const uint32_t*>(Q), static_cast<const uint8_t*>(scales), static_cast<__nv_bfloat16*>(W));
+    else
+        dequantize_mx4_kernel<float><<<grid_for(units), kThreads, 0, st>>>(
+            d_model, units, static_cast<const uint32_t*>(Q), static_cast<const uint8_t*>(scales), static_cast<float*>(W));
+    HALO_CHECK_LAUNCH();
+    return HALO_OK;
+}

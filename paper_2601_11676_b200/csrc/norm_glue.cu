@@ -1,0 +1,190 @@
+// halo_norm_glue: the residual between two blocks with a norm behind the one and a norm in front of the other,
+//     h_out = h + res_scale * gate * rms_norm(y) * w_post,   x_out = cast(rms_norm(h_out) * w_pre).
+// HBM-bound: h, y and the gate are read once, h_out and x_out written once; a row stays in registers between its two
+// sums of squares.  A row is held by 32 to 1024 threads, at most 16 elements each beyond d = 512 (see threads_for).
+#include <math.h>
+
+#include "common.cuh"
+
+namespace halo {
+namespace {
+
+struct GlueArgs {
+    int d, n_tok;
+    float eps, res_scale;
+    long long gate_stride;
+    const float* h;
+    const void* y;
+    const void* w_post;
+    const void* gate;
+    const void* w_pre;
+    float* h_out;
+    void* x_out;
+};
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
+    if constexpr (sizeof(T) == 4) {
+        const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+        f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    } else {
+        const uint4 w = *reinterpret_cast<const uint4*>(p);
+        Elem<__nv_bfloat16>::widen(w, f);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
+    if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+        *reinterpret_cast<float4*>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
+    } else {
+        __nv_bfloat162 v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+        *reinterpret_cast<uint4*>(p) =
+            make_uint4(*reinterpret_cast<uint32_t*>(&v[0]), *reinterpret_cast<uint32_t*>(&v[1]),
+                       *reinterpret_cast<uint32_t*>(&v[2]), *reinterpret_cast<uint32_t*>(&v[3]));
+    }
+}
+
+// sum over the ROW threads of a row; the same value in each of them
+template <int ROW>
+__device__ __forceinline__ float row_sum(float v, float* sh /*[ROW / 32]*/) {
+    v = warp_sum(v);
+    if constexpr (ROW > 32) {
+        const int lane = threadIdx.x & 31, warp = (threadIdx.x % ROW) >> 5;
+        if (lane == 0) sh[warp] = v;
+        __syncthreads();
+        v = lane < ROW / 32 ? sh[lane] : 0.0f;
+        v = warp_sum(v);
+    }
+    return v;
+}
+
+// ROW threads per row, IT units of 8 elements per thread; 128 / ROW rows per thread block where ROW < 128.
+template <typename TY, typename T, int ROW, int IT>
+__global__ void __launch_bounds__(ROW < 128 ? 128 : ROW) norm_glue_kernel(const __grid_constant__ GlueArgs a) {
+    constexpr int kRows = ROW < 128 ? 128 / ROW : 1;
+    __shared__ float sh[2][ROW / 32];
+    const int t = threadIdx.x % ROW;
+    const long long row = static_cast<long long>(blockIdx.x) * kRows + threadIdx.x / ROW;
+    if (row >= a.n_tok) return;   // whole warps only: a row of fewer than 128 threads is one warp
+    const long long base = row * a.d;
+    const int units = a.d / 8;
+    float h[IT][8], y[IT][8];
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+        const int u = t + i * ROW;
+        if (u < units) {
+            load8(a.h + base + u * 8, h[i]);
+            if (a.y) load8(static_cast<const TY*>(a.y) + base + u * 8, y[i]);
+        }
+        if (u >= units)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[i][e] = 0.0f;
+        if (u >= units || !a.y)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[i][e] = 0.0f;
+    }
+    if (a.y) {
+        float f = a.res_scale;
+        if (a.w_post) {
+            float ss = 0.0f;
+#pragma unroll
+            for (int i = 0; i < IT; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ss = fmaf(y[i][e], y[i][e], ss);
+            ss = row_sum<ROW>(ss, sh[0]);
+            f = rsqrtf(ss / static_cast<float>(a.d) + a.eps);
+        }
+#pragma unroll
+        for (int i = 0; i < IT; ++i) {
+            const int u = t + i * ROW;
+            if (u >= units) continue;
+            float w[8];
+            if (a.w_post) {
+                load8(static_cast<const T*>(a.w_post) + u * 8, w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[i][e] = y[i][e] * f * w[e] * a.res_scale;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[i][e] *= f;
+            }
+            if (a.gate) {
+                load8(static_cast<const T*>(a.gate) + row * a.gate_stride + u * 8, w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[i][e] *= w[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[i][e] += y[i][e];
+        }
+    }
+    float ss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < IT; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = fmaf(h[i][e], h[i][e], ss);
+    ss = row_sum<ROW>(ss, sh[1]);
+    const float f = rsqrtf(ss / static_cast<float>(a.d) + a.eps);
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+        const int u = t + i * ROW;
+        if (u >= units) continue;
+        store8(a.h_out + base + u * 8, h[i]);
+        float w[8];
+        if (a.w_pre) {
+            load8(static_cast<const T*>(a.w_pre) + u * 8, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[i][e] = h[i][e] * f * w[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[i][e] *= f;
+        }
+        store8(static_cast<T*>(a.x_out) + base + u * 8, h[i]);
+    }
+}
+
+template <typename TY, typename T, int ROW, int IT>
+halo_status go(const GlueArgs& a, cudaStream_t st) {
+    constexpr int kRows = ROW < 128 ? 128 / ROW : 1;
+    norm_glue_kernel<TY, T, ROW, IT><<<(a.n_tok + kRows - 1) / kRows, ROW < 128 ? 128 : ROW, 0, st>>>(a);
+    HALO_CHECK_LAUNCH();
+    return HALO_OK;
+}
+template <typename TY, typename T>
+halo_status launch(const GlueArgs& a, cudaStream_t st) {
+    const int units = a.d / 8;
+    if (units <= 32) return go<TY, T, 32, 1>(a, st);
+    if (units <= 64) return go<TY, T, 32, 2>(a, st);
+    if (units <= 256) return go<TY, T, 128, 2>(a, st);
+    if (units <= 512) return go<TY, T, 256, 2>(a, st);
+    if (units <= 1024) return go<TY, T, 512, 2>(a, st);
+    return go<TY, T, 1024, 2>(a, st);
+}
+
+}  // namespace
+}  // namespace halo
+
+using namespace halo;
+
+extern "C" halo_status halo_norm_glue(const halo_norm_shape* shape, int n_tok, const float* h, const void* y,
+                                      const void* w_post, const void* gate, long long gate_stride, float res_scale,
+                                      const void* w_pre, float* h_out, void* x_out, void* stream) {
+    if (!shape || !h || !h_out || !x_out) return HALO_ERR_ARG;
+    if (!y && (w_post || gate)) return HALO_ERR_ARG;
+    if ((shape->xdtype != HALO_F32 && shape->xdtype != HALO_BF16) || (shape->ydtype != HALO_F32 && shape->ydtype != HALO_BF16))
+        return HALO_ERR_DTYPE;
+    const int d = shape->d_model;
+    if (d <= 0 || d % 8 != 0 || d > HALO_MAX_NORM_WIDTH || n_tok <= 0) return HALO_ERR_SHAPE;
+    if (!(shape->eps > 0.0f) || !isfinite(shape->eps) || !isfinite(res_scale)) return HALO_ERR_ARG;
+    if (gate && gate_stride != 0 && gate_stride < d) return HALO_ERR_SHAPE;
+    if (!aligned16(h) || !aligned16(y) || !aligned16(w_post) || !aligned16(gate) || !aligned16(w_pre) || !aligned16(h_out) ||
+        !aligned16(x_out) || (gate && gate_stride * (shape->xdtype == HALO_F32 ? 4 : 2) % 16 != 0))
+        return HALO_ERR_ALIGN;
+    GlueArgs a = {d, n_tok, shape->eps, res_scale, gate_stride, h, y, w_post, gate, w_pre, h_out, x_out};
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (shape->ydtype == HALO_F32)
+        return shape->xdtype == HALO_F32 ? launch<float, float>(a, st) : launch<float, __nv_bfloat16>(a, st);
+    return shape->xdtype == HALO_F32 ? launch<__nv_bfloat16, float>(a, st) : launch<__nv_bfloat16, __nv_bfloat16>(a, st);
+}

@@ -207,3 +207,112 @@ def test_late_devices_match_the_oracle_and_feed_the_plan(lib):
     for bad in [([1, 2], [1.0, 0.0], 1.0, 0.0, 1.0), ([1, -1], [1.0, 1.0], 1.0, 0.0, 1.0), ([1], [1.0], -1.0, 0.0, 1.0)]:
         with pytest.raises(B.HaloError):
             B.halo_late_devices(*bad)
+
+
+def test_attention_block_entry_points_check_their_arguments_on_the_host(lib):
+    """Paged append / attention, the normalised residual and the mx4 calls refuse bad shapes, NULL and misaligned pointers,
+    strides, element types and workspaces before anything is launched."""
+    ref = ctypes.byref
+    ok = B.paged_shape(8, 2, 64, 16, 10, 4, B.BF16)
+    bad_shapes = [B.paged_shape(8, 3, 64, 16, 10, 4, B.BF16), B.paged_shape(0, 0, 64, 16, 10, 4, B.BF16),
+                  B.paged_shape(8, 2, 60, 16, 10, 4, B.BF16), B.paged_shape(8, 2, 272, 16, 10, 4, B.BF16),
+                  B.paged_shape(8, 2, 64, 0, 10, 4, B.BF16), B.paged_shape(8, 2, 64, 16, 0, 4, B.BF16),
+                  B.paged_shape(8, 2, 64, 16, 10, 0, B.BF16), B.paged_shape(8, 2, 64, 1 << 16, 10, 1 << 15, B.BF16),
+                  B.paged_shape(2048, 2, 64, 16, 10, 4, B.BF16), B.paged_shape(8, 2, 64, 16, 10, 4, B.BF16, 2040),
+                  B.paged_shape(8, 2, 64, 16, 10, 4, B.BF16, 2052)]
+
+    def append(sh=ok, n_tok=3, n_seq=3, q=16, qs=512, k=16, ks=128, v=16, vs=128, pos=16, seq=None, table=16, inv=16, rot=64,
+               q_out=16, qos=512, K=16, V=16):
+        return lib.halo_paged_kv_append(ref(sh), n_tok, n_seq, q, qs, k, ks, v, vs, pos, seq, table, inv, rot, 0, q_out, qos, K,
+                                        V, None, None)
+
+    def attend(sh=ok, n_seq=3, q=16, qs=512, K=16, V=16, table=16, lens=16, scale=1.0, out=16, ws=None, wb=0):
+        return lib.halo_paged_mha(ref(sh), n_seq, q, qs, K, V, table, lens, None, scale, out, None, ws, wb, None, None)
+
+    for sh in bad_shapes:
+        assert append(sh) == -2 and attend(sh) == -2 and B.halo_paged_mha_workspace_bytes(sh, 3) == 0
+    assert append(B.paged_shape(8, 2, 64, 16, 10, 4, 2)) == -4 and attend(B.paged_shape(8, 2, 64, 16, 10, 4, -1)) == -4
+    for kw in (dict(k=None), dict(v=None), dict(pos=None), dict(table=None), dict(K=None), dict(V=None), dict(q=None),
+               dict(q_out=None), dict(inv=None)):
+        assert append(**kw) == -1, kw
+    for kw in (dict(n_tok=0), dict(n_seq=0), dict(n_seq=2), dict(rot=63), dict(rot=66), dict(rot=-2), dict(qs=504), dict(ks=120),
+               dict(vs=-128), dict(qos=0)):
+        assert append(**kw) == -2, kw
+    for kw in (dict(q=24), dict(k=8), dict(v=18), dict(q_out=20), dict(K=24), dict(V=24), dict(qs=513), dict(ks=132), dict(qos=514)):
+        assert append(**kw) == -3, kw
+    for kw in (dict(q=None), dict(K=None), dict(V=None), dict(table=None), dict(lens=None), dict(out=None),
+               dict(scale=float("nan")), dict(scale=float("inf"))):
+        assert attend(**kw) == -1, kw
+    for kw in (dict(n_seq=0), dict(n_seq=8193), dict(qs=511)):
+        assert attend(**kw) == -2, kw
+    for kw in (dict(q=24), dict(K=24), dict(V=24), dict(out=8), dict(qs=513)):
+        assert attend(**kw) == -3, kw
+    long = B.paged_shape(8, 2, 64, 16, 10000, 8192, B.BF16)
+    need = B.halo_paged_mha_workspace_bytes(long, 1)
+    assert need > 0
+    assert attend(long, n_seq=1) == -8 and attend(long, n_seq=1, ws=16, wb=need - 1) == -8
+    assert attend(long, n_seq=1, ws=24, wb=need) == -3
+
+    def glue(sh=B.norm_shape(256, 1e-5, B.F32, B.BF16), n=2, h=16, y=16, w1=16, gate=16, gs=256, res=1.0, w2=16, ho=16, xo=16):
+        return lib.halo_norm_glue(ref(sh), n, h, y, w1, gate, gs, res, w2, ho, xo, None)
+
+    for kw in (dict(h=None), dict(ho=None), dict(xo=None), dict(y=None), dict(res=float("inf"))):
+        assert glue(**kw) == -1, kw
+    for eps in (0.0, -1e-5, float("nan"), float("inf")):
+        assert glue(B.norm_shape(256, eps, B.F32, B.BF16)) == -1
+    assert glue(B.norm_shape(256, 1e-5, 2, B.BF16)) == -4 and glue(B.norm_shape(256, 1e-5, B.F32, 3)) == -4
+    for sh in (B.norm_shape(0, 1e-5, B.F32, B.BF16), B.norm_shape(252, 1e-5, B.F32, B.BF16), B.norm_shape(16392, 1e-5, B.F32, B.BF16)):
+        assert glue(sh) == -2
+    assert glue(n=0) == -2 and glue(gs=128) == -2
+    for kw in (dict(h=24), dict(y=24), dict(w1=24), dict(gate=24), dict(w2=24), dict(ho=24), dict(xo=24), dict(gs=260)):
+        assert glue(**kw) == -3, kw
+
+    assert B.halo_mx4_scale_bytes(256, 129) == 2 * 2 * 512 and B.halo_mx4_scale_bytes(200, 1) == 0
+    for fn in (lib.halo_quantize_rows_mx4, lib.halo_dequantize_rows_mx4):
+        assert fn(256, 10, B.BF16, None, 16, 16, None) == -1 and fn(256, 10, B.BF16, 16, 16, None, None) == -1
+        assert fn(200, 10, B.BF16, 16, 16, 16, None) == -2 and fn(256, 0, B.BF16, 16, 16, 16, None) == -2
+        assert fn(256, 10, 5, 16, 16, 16, None) == -4 and fn(256, 10, B.F32, 16, 24, 16, None) == -3
+    product = lambda d=256, t=1, n=8, p=(16, 16, 16, 16), dt=B.BF16, y=16: lib.halo_product_mx4(d, t, n, *p, dt, y, None, None)  # noqa: E731
+    assert product(d=192) == -2 and product(t=0) == -2 and product(n=0) == -2 and product(t=(1 << 20) + 1) == -2
+    assert product(dt=2) == -4 and product(y=None) == -1 and product(y=24) == -3
+    for i in range(4):
+        ptrs = [16] * 4
+        ptrs[i] = None
+        assert product(p=ptrs) == -1
+        ptrs[i] = 24
+        assert product(p=ptrs) == -3
+
+
+def test_attention_block_binding_checks_tensors(lib):
+    """The Python layer compares tensors with the shape before any address is passed on (CPU tensors are enough to see it)."""
+    import torch
+    f, i = torch.bfloat16, torch.int32
+    sh = B.paged_shape(4, 2, 16, 16, 3, 2, B.BF16)
+    K = torch.zeros((3, 2, 16, 16), dtype=f)
+    q, kv, pos, table = torch.zeros((2, 4, 16), dtype=f), torch.zeros((2, 2, 16), dtype=f), torch.zeros(2, dtype=i), torch.zeros((2, 2), dtype=i)
+    good = dict(shape=sh, q=q, k=kv, v=kv, pos=pos, seq_of_tok=None, block_table=table, inv_freq=None, interleaved=False, q_out=q, K_cache=K,
+                V_cache=K)
+    for name, t in (("k", kv.float()), ("k", kv[:, :1]), ("v", kv[:1]), ("q", q.transpose(1, 2)), ("q_out", None), ("pos", pos.long()),
+                    ("pos", pos[:1]), ("block_table", table[:, :1]), ("inv_freq", torch.zeros(8)), ("K_cache", K[:2]), ("V_cache", K.float()),
+                    ("seq_of_tok", table)):
+        with pytest.raises(ValueError):
+            B.halo_paged_kv_append(**{**good, name: t})
+    with pytest.raises(ValueError):
+        B.halo_paged_kv_append(**good)                                   # not on a GPU
+    out = torch.zeros((2, 4, 16), dtype=f)
+    good = dict(shape=sh, q=q, K_cache=K, V_cache=K, block_table=table, seq_len=pos, scale=1.0, out=out, workspace=None)
+    for name, t in (("out", out[:1]), ("seq_len", pos[:1]), ("K_cache", K.transpose(2, 3)), ("workspace", torch.zeros(4)),
+                    ("keep", torch.zeros(3, dtype=torch.uint8)), ("lse", torch.zeros(8, dtype=f)), ("q", q.flatten())):
+        with pytest.raises(ValueError):
+            B.halo_paged_mha(**{**good, name: t})
+    ns, h, x = B.norm_shape(64, 1e-5, B.F32, B.BF16), torch.zeros((2, 64)), torch.zeros((2, 64), dtype=f)
+    for y, w, gate, xo in ((x, None, None, x), (h, h[0], None, x), (h, None, x[:, :32], x), (h, None, None, x[:1])):
+        with pytest.raises(ValueError):
+            B.halo_norm_glue(ns, h, y, w, gate, 1.0, None, h, xo)
+    Q, S = torch.zeros((5, 64), dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8)
+    for args in ((128, 5, B.BF16, torch.zeros((5, 128)), Q, S), (128, 5, B.F32, torch.zeros((5, 128)), Q[:4], S),
+                 (128, 5, B.F32, torch.zeros((5, 128)), Q, S[:511]), (100, 5, B.F32, torch.zeros((5, 100)), Q, S)):
+        with pytest.raises(ValueError):
+            B.halo_quantize_rows_mx4(*args)
+    with pytest.raises(ValueError):
+        B.halo_product_mx4(128, 5, 5, Q, S, Q, S, B.F32, torch.zeros((5, 4)))
