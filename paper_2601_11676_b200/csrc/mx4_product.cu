@@ -1,25 +1,29 @@
 // halo_product_mx4: y[t][r] = <x_t, w_r> of rows in microscaled 4-bit floating point, on the block-scaled tensor
 // cores (tcgen05.mma kind::mxf4, products of 64 elements with a power of two per 32, fp32 accumulators in TMEM).
 //
-// The weight rows are the 128 rows of A and the tokens the columns of B, so one token costs a tile of 16 columns and
-// not one of 128 rows, and a lane of the epilogue is a weight row: 32 lanes store 32 neighbouring outputs.
+// The weight rows are the rows of A and the tokens the columns of B, so one token costs a tile of 16 columns and not
+// one of 128 rows, and a lane of the epilogue is a weight row: 32 lanes store 32 neighbouring outputs.
 // Stages of 256 elements: 128-byte rows of codes by tensor-map TMA (128-byte swizzle), the scales as 512-byte blocks
 // by bulk copies, moved on to TMEM by tcgen05.cp in front of the products that use them.  Every stage of the ring has
 // its own columns of scales: a stage is refilled only when the products that read its old scales have completed.
 //
-// Bounds: few tokens HBM (0.53 bytes per weight element), prompts the tensor pipe.  With few tokens a cluster of up to
-// 8 thread blocks shares a tile's elements and adds its parts through distributed shared memory in rank order.
+// Two kernels:
+//   mx4_line_kernel  few tokens, bound by HBM (0.53 bytes per weight element): the weight rows in groups of 32 form a
+//     line (one per tile of tokens) that is cut into equal pieces, one thread block per SM; whole outputs per thread
+//     block, so nothing has to be added up between thread blocks.
+//   mx4_pair_kernel  prompts, bound by the L2-to-SM traffic and the tensor pipe: pairs of SMs (cta_group::2) on tiles
+//     of 256 rows x 256 tokens; each SM fetches half of either operand, 35 KB per 16.8 M products and SM where a
+//     single SM's 128 x 256 tile takes 51 KB.
 //
 // Every wait is bounded; when one runs out the block's roles leave their loops, the copies in flight are waited for,
 // TMEM is freed and HALO_DEV_TIMEOUT is raised.
-#include <cooperative_groups.h>
-
 #include "common.cuh"
 #include "umma.cuh"
 
 namespace halo {
 
 bool make_byte_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t row_bytes, uint32_t box_bytes, uint32_t box_rows);
+bool make_scale_map(CUtensorMap* map, const void* base, uint64_t tiles, uint64_t blocks, uint32_t box_tiles, uint32_t box_blocks);
 
 namespace {
 
@@ -38,18 +42,21 @@ __device__ __forceinline__ void umma_mxf4(uint32_t tmem_d, uint64_t a_desc, uint
 }
 // Instruction descriptor of kind::mxf4: e2m1 x e2m1 -> fp32, scales powers of two; sf = 0 or 2 picks the bytes of the
 // scale words that belong to these 64 elements.
-__device__ __forceinline__ constexpr uint32_t idesc_mxf4(int n, uint32_t sf) {
+__device__ __forceinline__ constexpr uint32_t idesc_mxf4(int m, int n, uint32_t sf) {
     return (sf << 4)                                // scale bytes of B
            | (1u << 7)                              // A: e2m1
            | (1u << 10)                             // B: e2m1
            | (static_cast<uint32_t>(n >> 3) << 17)  // N / 8
            | (1u << 23)                             // scales: powers of two
-           | (static_cast<uint32_t>(kRowsTile >> 7) << 27)
+           | (static_cast<uint32_t>(m >> 7) << 27)
            | (sf << 29);                            // scale bytes of A
 }
-// 512 bytes of shared memory (32 rows of 16 bytes) -> 4 columns, repeated in the four quarters of the lanes
-__device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint32_t smem) {
-    const uint64_t desc = static_cast<uint64_t>((smem & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(128u >> 4) << 32) | (1ull << 46);
+// 512 bytes of shared memory (32 rows of 16 bytes, no swizzle, 128 bytes per 8 rows) -> 4 columns, repeated in the four
+// quarters of the lanes
+__device__ __forceinline__ uint64_t scales_desc(uint32_t smem) {
+    return static_cast<uint64_t>((smem & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(128u >> 4) << 32) | (1ull << 46);
+}
+__device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint64_t desc) {
     asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
 }
 
@@ -61,39 +68,88 @@ struct Ring {
     static constexpr int kSfa = 1024, kSfb = 1024 * kTokTiles;
     static constexpr int kStage = kA + kB + kSfa + kSfb;
     static constexpr int kSfCols = 8 + 8 * kTokTiles;
-    static constexpr int kCols = NT + STAGES * kSfCols;
-    static constexpr int kTmem = kCols <= 32 ? 32 : kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-    static constexpr size_t kBars = 256;
-    static constexpr size_t kSmem = static_cast<size_t>(STAGES) * kStage + kBars;
+    static constexpr int kAcc = 2 * NT + STAGES * kSfCols <= 512 ? 2 : 1;   // accumulators
+    static constexpr int kCols = kAcc * NT + STAGES * kSfCols;
+    static constexpr int kTmem = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
+    static constexpr size_t kSmem = static_cast<size_t>(STAGES) * kStage + 512;
     static_assert(kCols <= 512, "tensor memory");
     static_assert(kStage % 1024 == 0, "swizzled tiles start on 1024 bytes");
+    static_assert(STAGES <= 12, "barriers");
 };
 
-struct Bars {
-    uint64_t full[8], empty[8], done;
+struct LineBars {
+    uint64_t full[12], empty[12], acc_full[2], acc_empty[2];
     uint32_t tmem;
     int abort_flag;
 };
 
+// The whole warp waits: the loops of the loader and MMA warps run in all lanes, so that addresses and descriptors stay
+// in uniform registers, and one elected lane issues.  (With one lane in the loops a stage of six scale copies and four
+// products took 510 ns to issue, more than the products themselves.)
+__device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    const bool ok = mbar_wait_bounded(bar, parity, abort_flag);
+    if (!ok) *abort_flag = 1;
+    return __all_sync(0xffffffffu, ok);
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+__device__ __forceinline__ int warp_index() { return __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0); }
+// stage of a ring and the parity of its current phase
+template <int STAGES>
+struct Slot {
+    uint32_t stage = 0, parity = 0;
+    __device__ __forceinline__ void advance() {
+        if (++stage == STAGES) { stage = 0; parity ^= 1u; }
+    }
+};
+
+// The line: token tile after token tile, in each the row groups of 32 in order.  A piece is a run of groups inside one
+// block of 128 rows, so the rows of a group stand where the block's scales expect them.
+struct Piece {
+    int tok0, block, g0, g1;   // groups of the block, 0..4
+};
+struct Line {
+    long long at, end;
+    int groups;                // per token tile
+    __device__ __forceinline__ bool next(Piece& p, int nt) {
+        if (at >= end) return false;
+        const long long tt = at / groups;
+        const int g = static_cast<int>(at - tt * groups);
+        p.tok0 = static_cast<int>(tt) * nt;
+        p.block = g >> 2;
+        p.g0 = g & 3;
+        const long long last = min(min(static_cast<long long>((p.block + 1) * 4), static_cast<long long>(groups)), g + (end - at));
+        p.g1 = static_cast<int>(last) - p.block * 4;
+        at += p.g1 - p.g0;
+        return true;
+    }
+};
+
+// grain: groups that are not cut apart (1 or 4)
 template <typename T, int NT, int STAGES>
-__global__ void __launch_bounds__(kThreads)
-mx4_product_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, int d, int n_tok,
-                   int n_rows, const uint8_t* __restrict__ Sw, const uint8_t* __restrict__ Sx, T* __restrict__ y, int split,
-                   uint32_t* status) {
+__global__ void __launch_bounds__(kThreads, 1)
+mx4_line_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_g,
+                const __grid_constant__ CUtensorMap map_x, int d, int n_tok,
+                int n_rows, int grain, const uint8_t* __restrict__ Sw, const uint8_t* __restrict__ Sx, T* __restrict__ y,
+                uint32_t* status) {
     using R = Ring<NT, STAGES>;
     extern __shared__ __align__(1024) unsigned char smem[];
-    Bars& bars = *reinterpret_cast<Bars*>(smem + static_cast<size_t>(STAGES) * R::kStage);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int rank = blockIdx.x % split;
-    const int rt = blockIdx.x / split, tt = blockIdx.y;
-    const int row0 = rt * kRowsTile, tok0 = tt * NT;
+    LineBars& bars = *reinterpret_cast<LineBars*>(smem + static_cast<size_t>(STAGES) * R::kStage);
+    const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
     const int atoms = d / 128;                       // 512-byte blocks of scales along a row
     const int nk = (d + kStageK - 1) / kStageK;
-    const int k0 = nk * rank / split, k1 = nk * (rank + 1) / split;
+    Line line;
+    line.groups = ((n_rows + 31) / 32 + grain - 1) / grain * grain;
+    const long long units = static_cast<long long>(line.groups / grain) * ((n_tok + NT - 1) / NT);
+    line.at = units * blockIdx.x / gridDim.x * grain;
+    line.end = units * (blockIdx.x + 1) / gridDim.x * grain;
 
     if (tid == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(&bars.full[s], 1); mbar_init(&bars.empty[s], 1); }
-        mbar_init(&bars.done, 1);
+        for (int b = 0; b < R::kAcc; ++b) { mbar_init(&bars.acc_full[b], 1); mbar_init(&bars.acc_empty[b], 4); }
         bars.abort_flag = 0;
         mbar_fence_init();
         tma_prefetch_descriptor(&map_w);
@@ -105,143 +161,431 @@ mx4_product_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     tcgen05_fence_after_sync();
     volatile int* abort_flag = &bars.abort_flag;
     const uint32_t tmem = bars.tmem;
+    Piece p;
 
     if (warp == 0) {
-        if (lane == 0) {
-            int it = 0;
-            for (int k = k0; k < k1; ++k, ++it) {
-                const int s = it % STAGES;
-                if (it >= STAGES && !mbar_wait_bounded(&bars.empty[s], ((it / STAGES) - 1) & 1, abort_flag)) {
-                    *abort_flag = 1;
-                    break;
+        const bool leader = elect_one();
+        Slot<STAGES> slot;
+        int it = 0;
+        bool alive = true;
+        while (alive && line.next(p, NT)) {
+            const int tiles = min(R::kTokTiles, (n_tok - p.tok0 + 127) / 128);
+            const uint8_t* sw = Sw + static_cast<size_t>(p.block) * atoms * 512;
+            const uint8_t* sx = Sx + static_cast<size_t>(p.tok0 / 128) * atoms * 512;
+            for (int k = 0; k < nk; ++k, ++it, slot.advance()) {
+                uint64_t* full = &bars.full[slot.stage];
+                if (it >= STAGES && !wait_or_abort(&bars.empty[slot.stage], slot.parity ^ 1u, abort_flag)) { alive = false; break; }
+                unsigned char* st = smem + slot.stage * R::kStage;
+                unsigned char* sc = st + R::kA + R::kB;
+                const uint32_t bytes = min(2, atoms - k * 2) * 512u;
+                if (leader) {
+                    mbar_arrive_expect_tx(full, (p.g1 - p.g0) * 32 * (kStageK / 2) + R::kB + bytes * (1 + tiles));
+                    if (p.g1 - p.g0 == 4)
+                        tma_load_2d(st, &map_w, k * (kStageK / 2), p.block * kRowsTile, full);
+                    else
+                        for (int g = p.g0; g < p.g1; ++g)
+                            tma_load_2d(st + g * 32 * (kStageK / 2), &map_g, k * (kStageK / 2), p.block * kRowsTile + g * 32, full);
+                    tma_load_2d(st + R::kA, &map_x, k * (kStageK / 2), p.tok0, full);
+                    bulk_copy_g2s(sc, sw + k * 1024, bytes, full);
+                    for (int t = 0; t < tiles; ++t)
+                        bulk_copy_g2s(sc + R::kSfa + t * 1024, sx + static_cast<size_t>(t) * atoms * 512 + k * 1024, bytes, full);
                 }
-                unsigned char* st = smem + static_cast<size_t>(s) * R::kStage;
-                const uint32_t n_at = min(2, atoms - k * 2);
-                const int tiles = min(R::kTokTiles, (n_tok - tok0 + 127) / 128);
-                mbar_arrive_expect_tx(&bars.full[s], R::kA + R::kB + n_at * 512u * (1 + tiles));
-                tma_load_2d(st, &map_w, k * (kStageK / 2), row0, &bars.full[s]);
-                tma_load_2d(st + R::kA, &map_x, k * (kStageK / 2), tok0, &bars.full[s]);
-                bulk_copy_g2s(st + R::kA + R::kB, Sw + (static_cast<size_t>(rt) * atoms + k * 2) * 512, n_at * 512u, &bars.full[s]);
-                for (int t = 0; t < tiles; ++t)
-                    bulk_copy_g2s(st + R::kA + R::kB + R::kSfa + t * 1024,
-                                  Sx + (static_cast<size_t>(tok0 / 128 + t) * atoms + k * 2) * 512, n_at * 512u, &bars.full[s]);
+                __syncwarp();
             }
-            if (*abort_flag) {
-                int never = 0;
-                for (int i = max(0, it - STAGES); i < it; ++i) mbar_wait_bounded(&bars.full[i % STAGES], (i / STAGES) & 1, &never);
-            }
+        }
+        if (*abort_flag && leader) {
+            int never = 0;
+            for (int i = max(0, it - STAGES); i < it; ++i) mbar_wait_bounded(&bars.full[i % STAGES], (i / STAGES) & 1, &never);
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            int it = 0;
-            for (int k = k0; k < k1; ++k, ++it) {
-                const int s = it % STAGES;
-                if (!mbar_wait_bounded(&bars.full[s], (it / STAGES) & 1, abort_flag)) { *abort_flag = 1; break; }
+        const bool leader = elect_one();
+        Slot<STAGES> slot;
+        int n = 0;
+        bool alive = true;
+        while (alive && line.next(p, NT)) {
+            const int acc = n % R::kAcc;
+            if (n >= R::kAcc && !wait_or_abort(&bars.acc_empty[acc], ((n / R::kAcc) - 1) & 1, abort_flag)) break;
+            tcgen05_fence_after_sync();
+            const uint32_t tmem_d = tmem + acc * NT;
+            for (int k = 0; k < nk; ++k, slot.advance()) {
+                if (!wait_or_abort(&bars.full[slot.stage], slot.parity, abort_flag)) { alive = false; break; }
                 tcgen05_fence_after_sync();
-                const uint32_t st = smem_u32(smem + static_cast<size_t>(s) * R::kStage);
-                const uint32_t sfa = tmem + NT + s * R::kSfCols, sfb = sfa + 8;
-                const int n_at = min(2, atoms - k * 2);
-                for (int at = 0; at < n_at; ++at) {
-                    tmem_cp_scales(sfa + at * 4, st + R::kA + R::kB + at * 512);
+                const uint32_t st = smem_u32(smem) + slot.stage * R::kStage, sc = st + R::kA + R::kB;
+                const uint32_t sfa = tmem + R::kAcc * NT + slot.stage * R::kSfCols, sfb = sfa + 8;
+                const uint64_t da = umma_smem_desc(st, 0, 1024), db = umma_smem_desc(st + R::kA, 0, 1024);
+                const uint64_t dsa = scales_desc(sc), dsb = scales_desc(sc + R::kSfa);
+                if (leader) {
 #pragma unroll
-                    for (int t = 0; t < R::kTokTiles; ++t)
-                        tmem_cp_scales(sfb + (at * R::kTokTiles + t) * 4, st + R::kA + R::kB + R::kSfa + t * 1024 + at * 512);
-                }
-                for (int j = 0; j < n_at * 2; ++j) {
-                    const uint32_t sf = (j & 1) * 2;
-                    umma_mxf4(tmem, umma_smem_desc(st + j * 32, 0, 1024), umma_smem_desc(st + R::kA + j * 32, 0, 1024),
-                              idesc_mxf4(NT, sf), sfa + (j >> 1) * 4, sfb + (j >> 1) * 4 * R::kTokTiles, it > 0 || j > 0);
-                }
-                umma_commit(&bars.empty[s]);
-            }
-            umma_commit(&bars.done);
-        }
-    }
-    if (warp >= 2) {
-        const bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(&bars.done, 0, abort_flag));
-        if (!ok) *abort_flag = 1;
-        tcgen05_fence_after_sync();
-        const int quad = warp & 3, row = row0 + quad * 32 + lane;
-        const uint32_t base = tmem + (static_cast<uint32_t>(quad * 32) << 16);
-        const int cols = min(NT, n_tok - tok0);
-        float* part = reinterpret_cast<float*>(smem);   // [cols][128]: the ring is drained
-        for (int c0 = 0; c0 < cols; c0 += 16) {
-            uint32_t v[16];
-            tmem_ld_32x16(base + c0, v);
-            tmem_ld_wait();
-            if (!ok) continue;
+                    for (int at = 0; at < 2; ++at) {
+                        if (at == 1 && atoms - k * 2 < 2) break;   // an odd number of runs of 128: half a stage
+                        tmem_cp_scales(sfa + at * 4, dsa + at * 32);
 #pragma unroll
-            for (int c = 0; c < 16; ++c) {
-                if (c0 + c >= cols) break;
-                const float f = k1 > k0 ? __uint_as_float(v[c]) : 0.0f;
-                if (split > 1)
-                    part[(c0 + c) * kRowsTile + quad * 32 + lane] = f;
-                else if (row < n_rows)
-                    y[static_cast<long long>(tok0 + c0 + c) * n_rows + row] = from_float<T>(f);
+                        for (int t = 0; t < R::kTokTiles; ++t)
+                            tmem_cp_scales(sfb + (at * R::kTokTiles + t) * 4, dsb + t * 64 + at * 32);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (j == 2 && atoms - k * 2 < 2) break;
+                        umma_mxf4(tmem_d, da + j * 2, db + j * 2, idesc_mxf4(kRowsTile, NT, (j & 1) * 2), sfa + (j >> 1) * 4,
+                                  sfb + (j >> 1) * 4 * R::kTokTiles, j > 0 || k > 0);
+                    }
+                    umma_commit(&bars.empty[slot.stage]);
+                }
+                __syncwarp();
             }
+            if (leader) umma_commit(&bars.acc_full[acc]);
+            __syncwarp();
+            ++n;
         }
-    }
-    __syncwarp();   // warps 0 and 1 worked with one lane
-    tcgen05_fence_before_sync();
-    if (split > 1) {
-        namespace cg = cooperative_groups;
-        cg::cluster_group cl = cg::this_cluster();
-        cl.sync();
-        // rank r adds up its share of the outputs over the thread blocks, in rank order
-        const int cols = min(NT, n_tok - tok0);
-        const float* part = reinterpret_cast<const float*>(smem);
-        for (int i = tid + rank * kThreads; i < cols * kRowsTile; i += kThreads * split) {
-            const int row = row0 + i % kRowsTile;
-            float sum = 0.0f;
-            for (int r = 0; r < split; ++r) sum += *cl.map_shared_rank(part + i, r);
-            if (row < n_rows) y[static_cast<long long>(tok0 + i / kRowsTile) * n_rows + row] = from_float<T>(sum);
-        }
-        cl.sync();
     } else {
-        __syncthreads();
+        int n = 0;
+        const int quad = warp & 3;
+        while (line.next(p, NT)) {
+            const int acc = n % R::kAcc;
+            if (!wait_or_abort(&bars.acc_full[acc], (n / R::kAcc) & 1, abort_flag)) break;
+            tcgen05_fence_after_sync();
+            const int row = p.block * kRowsTile + quad * 32 + lane;
+            const bool mine = quad >= p.g0 && quad < p.g1 && row < n_rows;
+            const uint32_t base = tmem + acc * NT + (static_cast<uint32_t>(quad * 32) << 16);
+            const int cols = min(NT, n_tok - p.tok0);
+            T* out = y + static_cast<long long>(p.tok0) * n_rows + row;
+            for (int c0 = 0; c0 < cols; c0 += 16) {
+                uint32_t v[16];
+                tmem_ld_32x16(base + c0, v);
+                tmem_ld_wait();
+                if (c0 + 16 >= cols) {   // the accumulator has been read
+                    tcgen05_fence_before_sync();
+                    if (lane == 0) mbar_arrive(&bars.acc_empty[acc]);
+                }
+#pragma unroll
+                for (int c = 0; c < 16; ++c)
+                    if (mine && c0 + c < cols) out[static_cast<long long>(c0 + c) * n_rows] = from_float<T>(__uint_as_float(v[c]));
+            }
+            ++n;
+        }
     }
+    __syncwarp();
+    tcgen05_fence_before_sync();
+    __syncthreads();
     if (warp == 1) { tcgen05_fence_after_sync(); tmem_dealloc(tmem, R::kTmem); }
     if (tid == 0 && *abort_flag) flag_status(status, HALO_DEV_TIMEOUT);
 }
 
+// ---- pairs of SMs -----------------------------------------------------------------------------------------------
+constexpr int kPairThreads = 320;      // loader warp, MMA warp, eight epilogue warps
+constexpr int kPairStages = 6;
+constexpr int kPairTile = 256;         // rows and tokens of a pair's tile; an SM fetches 128 of either
+struct PairRing {
+    static constexpr int kOp = 128 * (kStageK / 2);
+    static constexpr int kSfa = 1024, kSfb = 2048;     // the scales of all 256 tokens go to both SMs
+    static constexpr int kStage = 2 * kOp + kSfa + kSfb;
+    static constexpr int kSfCols = 24;
+    static constexpr size_t kSmem = static_cast<size_t>(kPairStages) * kStage + 512;
+};
+static_assert(PairRing::kStage % 1024 == 0 && kPairTile + kPairStages * PairRing::kSfCols <= 512, "layout");
+
+struct PairBars {
+    uint64_t full[kPairStages];        // first SM only: the copies of both have landed
+    uint64_t empty[kPairStages];       // the products that read the stage have completed
+    uint64_t acc_full, acc_empty;      // acc_empty: first SM only, all sixteen epilogue warps have read
+    uint32_t tmem;
+    int abort_flag;
+};
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t in_block_of(uint32_t rank, const void* p) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// a phase that threads or products of the other SM complete; the whole warp waits
+__device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    const long long t0 = clock64();
+    uint32_t spins = 0;
+    while (true) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(smem_u32(bar)), "r"(parity)
+            : "memory");
+        if (__all_sync(0xffffffffu, ok != 0)) return true;
+        if ((++spins & 255u) == 0u && __any_sync(0xffffffffu, *abort_flag || clock64() - t0 > kWaitLimitCycles)) {
+            *abort_flag = 1;
+            return false;
+        }
+    }
+}
+// Tensor-map copies into this SM's shared memory that count at a barrier of either SM of the pair (an address in the
+// cluster's shared memory).
+__device__ __forceinline__ void tma_pair_2d(void* dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+            smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void tma_pair_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+            smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void umma_mxf4_pair(uint32_t tmem_d, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t tmem_sfa,
+                                               uint32_t tmem_sfb, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(tmem_d),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(tmem_sfa), "r"(tmem_sfb), "r"(static_cast<uint32_t>(accumulate))
+        : "memory");
+}
+__device__ __forceinline__ void tmem_cp_scales_pair(uint32_t taddr, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+// arrives at the same barrier of both SMs once the products issued so far have completed
+__device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                     smem_u32(bar)),
+                 "h"(static_cast<uint16_t>(3))
+                 : "memory");
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kPairThreads, 1)
+mx4_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+                const __grid_constant__ CUtensorMap map_sw, const __grid_constant__ CUtensorMap map_sx, int d, int n_tok,
+                int n_rows, T* __restrict__ y, uint32_t* status) {
+    using R = PairRing;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    PairBars& bars = *reinterpret_cast<PairBars*>(smem + static_cast<size_t>(kPairStages) * R::kStage);
+    const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
+    const uint32_t rank = cluster_rank();
+    const int atoms = d / 128, nk = (d + kStageK - 1) / kStageK;
+    const int row_blocks = (n_rows + 127) / 128, tok_blocks = (n_tok + 127) / 128;
+    const int row_tiles = (row_blocks + 1) / 2, tok_tiles = (tok_blocks + 1) / 2;
+    const int tiles = row_tiles * tok_tiles, pairs = gridDim.x / 2, pair = blockIdx.x / 2;
+
+    if (tid == 0) {
+        for (int s = 0; s < kPairStages; ++s) {
+            mbar_init(&bars.full[s], 1);
+            mbar_init(&bars.empty[s], 1);
+        }
+        mbar_init(&bars.acc_full, 1);
+        mbar_init(&bars.acc_empty, 16);
+        bars.abort_flag = 0;
+        mbar_fence_init();
+        tma_prefetch_descriptor(&map_w);
+        tma_prefetch_descriptor(&map_x);
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bars.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    __syncwarp();
+    tcgen05_fence_before_sync();
+    __syncthreads();
+    cluster_sync_all();
+    tcgen05_fence_after_sync();
+    volatile int* abort_flag = &bars.abort_flag;
+    const uint32_t tmem = bars.tmem;
+
+    if (warp == 0) {
+        const bool leader = elect_one();
+        const uint32_t full0 = in_block_of(0, &bars.full[0]);
+        Slot<kPairStages> slot;
+        int it = 0;
+        bool alive = true;
+        for (int tile = pair; tile < tiles && alive; tile += pairs) {
+            const int rb = (tile % row_tiles) * 2 + static_cast<int>(rank);    // this SM's block of 128 rows
+            const int tb0 = (tile / row_tiles) * 2;                            // the pair's blocks of 128 tokens
+            for (int k = 0; k < nk; ++k, ++it, slot.advance()) {
+                if (it >= kPairStages && !wait_or_abort(&bars.empty[slot.stage], slot.parity ^ 1u, abort_flag)) { alive = false; break; }
+                unsigned char* st = smem + slot.stage * R::kStage;
+                unsigned char* sc = st + 2 * R::kOp;
+                const uint32_t full = full0 + slot.stage * 8;
+                if (leader) {
+                    // what lies outside a matrix arrives as zeros and counts: both SMs' bytes, the same for every stage
+                    if (rank == 0) mbar_arrive_expect_tx(&bars.full[slot.stage], 2 * R::kStage);
+                    tma_pair_2d(st, &map_w, k * (kStageK / 2), rb * 128, full);
+                    tma_pair_2d(st + R::kOp, &map_x, k * (kStageK / 2), (tb0 + static_cast<int>(rank)) * 128, full);
+                    tma_pair_3d(sc, &map_sw, 0, k * 2, rb, full);
+                    tma_pair_3d(sc + R::kSfa, &map_sx, 0, k * 2, tb0, full);
+                }
+                __syncwarp();
+            }
+        }
+        if (*abort_flag && leader && rank == 0) {   // the copies of both SMs; neither leaves before the other
+            int never = 0;
+            for (int i = max(0, it - kPairStages); i < it; ++i)
+                mbar_wait_bounded(&bars.full[i % kPairStages], (i / kPairStages) & 1, &never);
+        }
+    } else if (warp == 1) {
+        const bool leader = elect_one();
+        Slot<kPairStages> slot;
+        int n = 0;
+        bool alive = true;
+        for (int tile = pair; tile < tiles && alive && rank == 0; tile += pairs, ++n) {
+            if (n > 0 && !wait_cluster(&bars.acc_empty, (n - 1) & 1, abort_flag)) break;
+            tcgen05_fence_after_sync();
+            for (int k = 0; k < nk; ++k, slot.advance()) {
+                if (!wait_cluster(&bars.full[slot.stage], slot.parity, abort_flag)) { alive = false; break; }
+                tcgen05_fence_after_sync();
+                const uint32_t st = smem_u32(smem) + slot.stage * R::kStage, sc = st + 2 * R::kOp;
+                const uint32_t sfa = tmem + kPairTile + slot.stage * R::kSfCols, sfb = sfa + 8;
+                const uint64_t da = umma_smem_desc(st, 0, 1024), db = umma_smem_desc(st + R::kOp, 0, 1024);
+                const uint64_t dsa = scales_desc(sc), dsb = scales_desc(sc + R::kSfa);
+                if (leader) {
+#pragma unroll
+                    for (int at = 0; at < 2; ++at) {
+                        if (at == 1 && atoms - k * 2 < 2) break;
+                        tmem_cp_scales_pair(sfa + at * 4, dsa + at * 32);
+                        tmem_cp_scales_pair(sfb + at * 8, dsb + at * 32);
+                        tmem_cp_scales_pair(sfb + at * 8 + 4, dsb + 64 + at * 32);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (j == 2 && atoms - k * 2 < 2) break;
+                        umma_mxf4_pair(tmem, da + j * 2, db + j * 2, idesc_mxf4(kPairTile, kPairTile, (j & 1) * 2), sfa + (j >> 1) * 4,
+                                       sfb + (j >> 1) * 8, j > 0 || k > 0);
+                    }
+                    umma_commit_pair(&bars.empty[slot.stage]);
+                }
+                __syncwarp();
+            }
+            if (leader) umma_commit_pair(&bars.acc_full);
+            __syncwarp();
+        }
+    } else {
+        // a warp reads 32 rows x 128 tokens into registers and lets the accumulator go before it stores
+        const int quad = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t base = tmem + half * 128 + (static_cast<uint32_t>(quad * 32) << 16);
+        const uint32_t acc_empty = in_block_of(0, &bars.acc_empty);
+        int n = 0;
+        for (int tile = pair; tile < tiles; tile += pairs, ++n) {
+            if (!wait_cluster(&bars.acc_full, n & 1, abort_flag)) break;
+            tcgen05_fence_after_sync();
+            constexpr int kWords = sizeof(T) == 4 ? 128 : 64;
+            uint32_t out[kWords];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t v[32];
+                tmem_ld_32x32(base + c * 32, v);
+                tmem_ld_wait();
+                if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) out[c * 32 + i] = v[i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const __nv_bfloat162 two = __floats2bfloat162_rn(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+                        out[c * 16 + i] = *reinterpret_cast<const uint32_t*>(&two);
+                    }
+                }
+            }
+            tcgen05_fence_before_sync();
+            if (lane == 0) arrive_at(acc_empty);
+            const int row = (tile % row_tiles) * kPairTile + static_cast<int>(rank) * 128 + quad * 32 + lane;
+            const int tok0 = (tile / row_tiles) * kPairTile + half * 128;
+            if (row < n_rows) {
+                T* p = y + static_cast<long long>(tok0) * n_rows + row;
+#pragma unroll
+                for (int i = 0; i < 128; ++i) {
+                    if (tok0 + i < n_tok) {
+                        if constexpr (sizeof(T) == 4)
+                            *p = __uint_as_float(out[i]);
+                        else
+                            *p = __ushort_as_bfloat16(static_cast<unsigned short>(out[i >> 1] >> ((i & 1) * 16)));
+                    }
+                    p += n_rows;
+                }
+            }
+        }
+    }
+    __syncwarp();
+    tcgen05_fence_before_sync();
+    __syncthreads();
+    cluster_sync_all();   // neither SM leaves while the other may still read its memory or signal its barriers
+    if (warp == 1) {
+        tcgen05_fence_after_sync();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
+    if (tid == 0 && *abort_flag) flag_status(status, HALO_DEV_TIMEOUT);
+}
+
+struct Operands {
+    int d, n_tok, n_rows;
+    const void *Qx, *Sx, *Qw, *Sw;
+    uint32_t* status;
+    cudaStream_t st;
+};
+
 template <typename T, int NT, int STAGES>
-halo_status launch(int d, int n_tok, int n_rows, const void* Qx, const void* Sx, const void* Qw, const void* Sw, T* y,
-                   uint32_t* status, cudaStream_t st) {
+halo_status launch_line(const Operands& o, int grain, T* y) {
     using R = Ring<NT, STAGES>;
     static bool done[64];
-    if (!ensure_dynamic_smem(mx4_product_kernel<T, NT, STAGES>, R::kSmem, done)) return HALO_ERR_CUDA;
-    CUtensorMap map_w, map_x;
-    if (!make_byte_map(&map_w, Qw, n_rows, d / 2, kStageK / 2, kRowsTile) ||
-        !make_byte_map(&map_x, Qx, n_tok, d / 2, kStageK / 2, NT))
+    if (!ensure_dynamic_smem(mx4_line_kernel<T, NT, STAGES>, R::kSmem, done)) return HALO_ERR_CUDA;
+    CUtensorMap map_w, map_g, map_x;   // whole blocks of rows, groups of rows, tokens
+    if (!make_byte_map(&map_w, o.Qw, o.n_rows, o.d / 2, kStageK / 2, kRowsTile) ||
+        !make_byte_map(&map_g, o.Qw, o.n_rows, o.d / 2, kStageK / 2, 32) ||
+        !make_byte_map(&map_x, o.Qx, o.n_tok, o.d / 2, kStageK / 2, NT))
         return HALO_ERR_CUDA;
-    const int tiles = (n_rows + kRowsTile - 1) / kRowsTile, tok_tiles = (n_tok + NT - 1) / NT;
-    const int nk = (d + kStageK - 1) / kStageK;
-    int split = 1;
-    if (NT <= 64)
-        while (split < 8 && split * 2 <= nk && tiles * tok_tiles * split < 4 * kSmCount) split *= 2;
+    const long long units = static_cast<long long>(((o.n_rows + 31) / 32 + grain - 1) / grain) * ((o.n_tok + NT - 1) / NT);
+    const int blocks = units < kSmCount ? static_cast<int>(units) : kSmCount;
+    mx4_line_kernel<T, NT, STAGES><<<blocks, kThreads, R::kSmem, o.st>>>(
+        map_w, map_g, map_x, o.d, o.n_tok, o.n_rows, grain, static_cast<const uint8_t*>(o.Sw), static_cast<const uint8_t*>(o.Sx), y, o.status);
+    HALO_CHECK_LAUNCH();
+    return HALO_OK;
+}
+
+template <typename T>
+halo_status launch_pair(const Operands& o, T* y) {
+    static bool done[64];
+    if (!ensure_dynamic_smem(mx4_pair_kernel<T>, PairRing::kSmem, done)) return HALO_ERR_CUDA;
+    CUtensorMap map_w, map_x, map_sw, map_sx;
+    if (!make_byte_map(&map_w, o.Qw, o.n_rows, o.d / 2, kStageK / 2, 128) ||
+        !make_byte_map(&map_x, o.Qx, o.n_tok, o.d / 2, kStageK / 2, 128) ||
+        !make_scale_map(&map_sw, o.Sw, (o.n_rows + 127) / 128, o.d / 128, 1, 2) ||
+        !make_scale_map(&map_sx, o.Sx, (o.n_tok + 127) / 128, o.d / 128, 2, 2))
+        return HALO_ERR_CUDA;
+    const long long tiles = static_cast<long long>((o.n_rows + 255) / 256) * ((o.n_tok + 255) / 256);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(tiles * split, tok_tiles);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = R::kSmem;
-    cfg.stream = st;
+    cfg.gridDim = dim3(tiles < kSmCount / 2 ? static_cast<unsigned>(tiles) * 2 : kSmCount);
+    cfg.blockDim = dim3(kPairThreads);
+    cfg.dynamicSmemBytes = PairRing::kSmem;
+    cfg.stream = o.st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = split;
+    at[0].val.clusterDim.x = 2;
     at[0].val.clusterDim.y = 1;
     at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cuda_status(cudaLaunchKernelEx(&cfg, mx4_product_kernel<T, NT, STAGES>, map_w, map_x, d, n_tok, n_rows,
-                                          static_cast<const uint8_t*>(Sw), static_cast<const uint8_t*>(Sx), y, split, status));
+    return cuda_status(cudaLaunchKernelEx(&cfg, mx4_pair_kernel<T>, map_w, map_x, map_sw, map_sx, o.d, o.n_tok, o.n_rows, y,
+                                          o.status));
 }
 
 template <typename T>
-halo_status by_tokens(int d, int n_tok, int n_rows, const void* Qx, const void* Sx, const void* Qw, const void* Sw, void* y,
-                      uint32_t* status, cudaStream_t st) {
+halo_status by_tokens(const Operands& o, void* y) {
     T* out = static_cast<T*>(y);
-    if (n_tok <= 16) return launch<T, 16, 5>(d, n_tok, n_rows, Qx, Sx, Qw, Sw, out, status, st);
-    if (n_tok <= 64) return launch<T, 64, 4>(d, n_tok, n_rows, Qx, Sx, Qw, Sw, out, status, st);
-    return launch<T, 256, 4>(d, n_tok, n_rows, Qx, Sx, Qw, Sw, out, status, st);
+    if (o.n_tok <= 16) return launch_line<T, 16, 10>(o, 1, out);
+    if (o.n_tok <= 64) return launch_line<T, 64, 8>(o, 1, out);
+    if (o.n_tok <= 128) return launch_line<T, 128, 6>(o, 4, out);
+    if (o.n_tok <= 256) return launch_line<T, 256, 4>(o, 4, out);
+    return launch_pair<T>(o, out);
 }
 
 }  // namespace
@@ -257,7 +601,6 @@ extern "C" halo_status halo_product_mx4(int d_model, int n_tok, int n_rows, cons
         return HALO_ERR_SHAPE;
     if (!Qx || !Sx || !Qw || !Sw || !y) return HALO_ERR_ARG;
     if (!aligned16(Qx) || !aligned16(Sx) || !aligned16(Qw) || !aligned16(Sw) || !aligned16(y)) return HALO_ERR_ALIGN;
-    const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return ydtype == HALO_F32 ? by_tokens<float>(d_model, n_tok, n_rows, Qx, Sx, Qw, Sw, y, dev_status, st)
-                              : by_tokens<__nv_bfloat16>(d_model, n_tok, n_rows, Qx, Sx, Qw, Sw, y, dev_status, st);
+    const Operands o = {d_model, n_tok, n_rows, Qx, Sx, Qw, Sw, dev_status, static_cast<cudaStream_t>(stream)};
+    return ydtype == HALO_F32 ? by_tokens<float>(o, y) : by_tokens<__nv_bfloat16>(o, y);
 }

@@ -9,7 +9,8 @@
 // tensor cores take them from tensor memory (halo_product_mx4 copies a block there as it is).
 //
 // Four lanes hold a block of 32 (8 elements each), so a warp reads 256 consecutive elements, writes 128 consecutive
-// code bytes, and 16 lanes meet for one 4-byte word of scales.
+// code bytes, and 16 lanes meet for one 4-byte word of scales.  A warp takes kRun such runs of one row at once: kRun
+// independent loads per lane in flight.
 #include <cuda_fp16.h>
 
 #include "common.cuh"
@@ -40,43 +41,49 @@ __device__ __forceinline__ float scale_of(uint32_t code) {
     return __uint_as_float(code == 0 ? 0x00400000u : code == 255u ? 0x7fc00000u : code << 23);
 }
 
-// One unit = 8 elements of a row; the rows behind n_rows up to a multiple of 128 get scales of zero.
+constexpr int kRun = 4;                 // runs of 256 elements a warp takes at once
+constexpr int kWarps = kThreads / 32;
+
+// Warp w of the grid: row w / segs, run group w % segs.  The rows behind n_rows up to a multiple of 128 get scales of
+// zero.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
-quantize_mx4_kernel(int d, long long n_rows, long long units, const T* __restrict__ W, uint32_t* __restrict__ Q,
+quantize_mx4_kernel(int d, unsigned n_rows, unsigned segs, unsigned items, const T* __restrict__ W, uint32_t* __restrict__ Q,
                     uint32_t* __restrict__ S) {
-    const int per_row = d / 8;
+    const unsigned item = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    if (item >= items) return;
     const int lane = threadIdx.x & 31;
-    for (long long u = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x; u < units;
-         u += static_cast<long long>(gridDim.x) * kThreads) {
-        const long long row = u / per_row;
-        const int c = static_cast<int>(u - row * per_row);
-        uint32_t top = 0, word = 0, scale = 0;
-        float f[8];
-        const bool real = row < n_rows;
-        if (real) {
-            load8(W + row * d + c * 8, f);
+    const unsigned row = item / segs;
+    const int c0 = static_cast<int>(item - row * segs) * (256 * kRun) + lane * 8;
+    const long long at = static_cast<long long>(row) * d + c0;
+    const bool real = row < n_rows;
+    float f[kRun][8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
-        }
-        // per_row is a multiple of 16: the 16 lanes of a word of scales are always on one row, and alive together
+    for (int i = 0; i < kRun; ++i)
+        if (real && c0 + i * 256 < d) load8(W + at + i * 256, f[i]);
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+        if (c0 + i * 256 >= d) break;   // d is a multiple of 128: the 16 lanes of a word of scales leave together
+        uint32_t top = 0, word = 0, scale = 0;
         const uint32_t group = 0xffffu << (lane & 16);
-        top = max(top, __shfl_xor_sync(group, top, 1));
-        top = max(top, __shfl_xor_sync(group, top, 2));
         if (real) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[i][e]) & 0x7fffffffu);
+            top = max(top, __shfl_xor_sync(group, top, 1));
+            top = max(top, __shfl_xor_sync(group, top, 2));
             const uint32_t field = top >> 23;
             scale = field == 255u ? 255u : field < 2u ? 0u : field - 2u;
             const float inv = __uint_as_float((254u - min(scale, 252u)) << 23);   // 2^(127 - scale), exact
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) word |= e2m1x2(f[e] * inv, f[e + 1] * inv) << (e * 4);
+            for (int e = 0; e < 8; e += 2) word |= e2m1x2(f[i][e] * inv, f[i][e + 1] * inv) << (e * 4);
             if (scale == 255u) word = 0;
-            Q[(row * d + c * 8) >> 3] = word;
+            Q[(at + i * 256) >> 3] = word;
         }
         uint32_t four = scale << (((lane >> 2) & 3) * 8);
         four |= __shfl_xor_sync(group, four, 4);
         four |= __shfl_xor_sync(group, four, 8);
         if ((lane & 15) == 0) {
-            const long long block = (row >> 7) * (d >> 7) + (c >> 4);
+            const long long block = static_cast<long long>(row >> 7) * (d >> 7) + ((c0 + i * 256) >> 7);
             S[block * 128 + (row & 31) * 4 + ((row >> 5) & 3)] = four;
         }
     }
@@ -84,33 +91,43 @@ quantize_mx4_kernel(int d, long long n_rows, long long units, const T* __restric
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
-dequantize_mx4_kernel(int d, long long units, const uint32_t* __restrict__ Q, const uint8_t* __restrict__ S,
+dequantize_mx4_kernel(int d, unsigned segs, unsigned items, const uint32_t* __restrict__ Q, const uint8_t* __restrict__ S,
                       T* __restrict__ W) {
-    const int per_row = d / 8;
-    for (long long u = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x; u < units;
-         u += static_cast<long long>(gridDim.x) * kThreads) {
-        const long long row = u / per_row;
-        const int c = static_cast<int>(u - row * per_row);
-        const uint32_t word = __ldg(Q + u);
-        const long long block = (row >> 7) * (d >> 7) + (c >> 4);
-        const float scale = scale_of(__ldg(S + block * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + ((c >> 2) & 3)));
+    const unsigned item = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    if (item >= items) return;
+    const int lane = threadIdx.x & 31;
+    const unsigned row = item / segs;
+    const int c0 = static_cast<int>(item - row * segs) * (256 * kRun) + lane * 8;
+    const long long at = static_cast<long long>(row) * d + c0;
+    const uint8_t* srow = S + static_cast<long long>(row >> 7) * (d >> 7) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4;
+    uint32_t word[kRun], byte[kRun];
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+        const int c = c0 + i * 256;
+        word[i] = c < d ? __ldg(Q + ((at + i * 256) >> 3)) : 0u;
+        byte[i] = c < d ? __ldg(srow + static_cast<long long>(c >> 7) * 512 + ((c >> 5) & 3)) : 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+        if (c0 + i * 256 >= d) break;
+        const float scale = scale_of(byte[i]);
         float f[8];
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
             uint32_t h;
-            asm("{\n\t.reg .b8 t;\n\tcvt.u8.u32 t, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, t;\n\t}" : "=r"(h) : "r"((word >> (e * 4)) & 0xffu));
+            asm("{\n\t.reg .b8 t;\n\tcvt.u8.u32 t, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, t;\n\t}" : "=r"(h) : "r"((word[i] >> (e * 4)) & 0xffu));
             const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h));
             f[e] = v.x * scale;
             f[e + 1] = v.y * scale;
         }
-        T* out = W + u * 8;
+        T* out = W + at + i * 256;
         if constexpr (sizeof(T) == 4) {
             *reinterpret_cast<float4*>(out) = make_float4(f[0], f[1], f[2], f[3]);
             *reinterpret_cast<float4*>(out + 4) = make_float4(f[4], f[5], f[6], f[7]);
         } else {
             __nv_bfloat162 v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);   // exact: two significant bits
+            for (int j = 0; j < 4; ++j) v[j] = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);   // exact: two significant bits
             *reinterpret_cast<uint4*>(out) =
                 make_uint4(*reinterpret_cast<uint32_t*>(&v[0]), *reinterpret_cast<uint32_t*>(&v[1]),
                            *reinterpret_cast<uint32_t*>(&v[2]), *reinterpret_cast<uint32_t*>(&v[3]));
@@ -118,18 +135,14 @@ dequantize_mx4_kernel(int d, long long units, const uint32_t* __restrict__ Q, co
     }
 }
 
+unsigned segments(int d) { return (d + 256 * kRun - 1) / (256 * kRun); }
+
 halo_status check_rows(int d_model, long long n_rows, halo_dtype dtype) {
     if (dtype != HALO_F32 && dtype != HALO_BF16) return HALO_ERR_DTYPE;
     if (d_model <= 0 || d_model % 128 != 0 || d_model > HALO_MX4_MAX_WIDTH || n_rows <= 0 || n_rows > HALO_MX4_MAX_ROWS)
         return HALO_ERR_SHAPE;
     return HALO_OK;
 }
-unsigned grid_for(long long units) {
-    const long long blocks = (units + kThreads - 1) / kThreads;
-    const long long most = static_cast<long long>(kSmCount) * 8 * 4;
-    return static_cast<unsigned>(blocks < most ? blocks : most);
-}
-
 }  // namespace
 }  // namespace halo
 
@@ -146,14 +159,16 @@ extern "C" halo_status halo_quantize_rows_mx4(int d_model, long long n_rows, hal
     if (rc != HALO_OK) return rc;
     if (!W || !Q || !scales) return HALO_ERR_ARG;
     if (!aligned16(W) || !aligned16(Q) || !aligned16(scales)) return HALO_ERR_ALIGN;
-    const long long units = (n_rows + 127) / 128 * 128 * (d_model / 8);
+    // warps: rows padded to 128 x runs, below 2^32 by the limits on both
+    const unsigned segs = segments(d_model), items = static_cast<unsigned>((n_rows + 127) / 128 * 128 * segs);
+    const unsigned grid = (items + kWarps - 1) / kWarps;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (wdtype == HALO_BF16)
-        quantize_mx4_kernel<__nv_bfloat16><<<grid_for(units), kThreads, 0, st>>>(
-            d_model, n_rows, units, static_cast<const __nv_bfloat16*>(W), static_cast<uint32_t*>(Q), static_cast<uint32_t*>(scales));
+        quantize_mx4_kernel<__nv_bfloat16><<<grid, kThreads, 0, st>>>(
+            d_model, static_cast<unsigned>(n_rows), segs, items, static_cast<const __nv_bfloat16*>(W), static_cast<uint32_t*>(Q), static_cast<uint32_t*>(scales));
     else
-        quantize_mx4_kernel<float><<<grid_for(units), kThreads, 0, st>>>(
-            d_model, n_rows, units, static_cast<const float*>(W), static_cast<uint32_t*>(Q), static_cast<uint32_t*>(scales));
+        quantize_mx4_kernel<float><<<grid, kThreads, 0, st>>>(
+            d_model, static_cast<unsigned>(n_rows), segs, items, static_cast<const float*>(W), static_cast<uint32_t*>(Q), static_cast<uint32_t*>(scales));
     HALO_CHECK_LAUNCH();
     return HALO_OK;
 }
@@ -164,14 +179,15 @@ extern "C" halo_status halo_dequantize_rows_mx4(int d_model, long long n_rows, h
     if (rc != HALO_OK) return rc;
     if (!W || !Q || !scales) return HALO_ERR_ARG;
     if (!aligned16(W) || !aligned16(Q) || !aligned16(scales)) return HALO_ERR_ALIGN;
-    const long long units = n_rows * (d_model / 8);
+    const unsigned segs = segments(d_model), items = static_cast<unsigned>(n_rows * segs);
+    const unsigned grid = (items + kWarps - 1) / kWarps;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (wdtype == HALO_BF16)
-        dequantize_mx4_kernel<__nv_bfloat16><<<grid_for(units), kThreads, 0, st>>>(
-            d_model, units, static_cast<const uint32_t*>(Q), static_cast<const uint8_t*>(scales), static_cast<__nv_bfloat16*>(W));
+        dequantize_mx4_kernel<__nv_bfloat16><<<grid, kThreads, 0, st>>>(
+            d_model, segs, items, static_cast<const uint32_t*>(Q), static_cast<const uint8_t*>(scales), static_cast<__nv_bfloat16*>(W));
     else
-        dequantize_mx4_kernel<float><<<grid_for(units), kThreads, 0, st>>>(
-            d_model, units, static_cast<const uint32_t*>(Q), static_cast<const uint8_t*>(scales), static_cast<float*>(W));
+        dequantize_mx4_kernel<float><<<grid, kThreads, 0, st>>>(
+            d_model, segs, items, static_cast<const uint32_t*>(Q), static_cast<const uint8_t*>(scales), static_cast<float*>(W));
     HALO_CHECK_LAUNCH();
     return HALO_OK;
 }

@@ -1,7 +1,8 @@
 // halo_norm_glue: the residual between two blocks with a norm behind the one and a norm in front of the other,
 //     h_out = h + res_scale * gate * rms_norm(y) * w_post,   x_out = cast(rms_norm(h_out) * w_pre).
 // HBM-bound: h, y and the gate are read once, h_out and x_out written once; a row stays in registers between its two
-// sums of squares.  A row is held by 32 to 1024 threads, at most 16 elements each beyond d = 512 (see threads_for).
+// sums of squares.  A thread holds IT units of 8 elements, a row ceil(d / 8 / IT) threads; h, y and gate are all
+// requested before the first sum, so that a row waits for memory once.
 #include <math.h>
 
 #include "common.cuh"
@@ -48,88 +49,114 @@ __device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
     }
 }
 
-// sum over the ROW threads of a row; the same value in each of them
-template <int ROW>
-__device__ __forceinline__ float row_sum(float v, float* sh /*[ROW / 32]*/) {
+// sum over the threads of a row (a warp, or the whole thread block); the same value in each of them
+template <bool ONE_WARP>
+__device__ __forceinline__ float row_sum(float v, float* sh /*[32]*/) {
     v = warp_sum(v);
-    if constexpr (ROW > 32) {
-        const int lane = threadIdx.x & 31, warp = (threadIdx.x % ROW) >> 5;
-        if (lane == 0) sh[warp] = v;
+    if constexpr (!ONE_WARP) {
+        const int lane = threadIdx.x & 31;
+        if (lane == 0) sh[threadIdx.x >> 5] = v;
         __syncthreads();
-        v = lane < ROW / 32 ? sh[lane] : 0.0f;
+        v = lane < static_cast<int>(blockDim.x >> 5) ? sh[lane] : 0.0f;
         v = warp_sum(v);
     }
     return v;
 }
 
-// ROW threads per row, IT units of 8 elements per thread; 128 / ROW rows per thread block where ROW < 128.
-template <typename TY, typename T, int ROW, int IT>
-__global__ void __launch_bounds__(ROW < 128 ? 128 : ROW) norm_glue_kernel(const __grid_constant__ GlueArgs a) {
-    constexpr int kRows = ROW < 128 ? 128 / ROW : 1;
-    __shared__ float sh[2][ROW / 32];
-    const int t = threadIdx.x % ROW;
-    const long long row = static_cast<long long>(blockIdx.x) * kRows + threadIdx.x / ROW;
-    if (row >= a.n_tok) return;   // whole warps only: a row of fewer than 128 threads is one warp
+// 8 elements as they lie in memory
+template <typename T> struct Raw { uint4 w[sizeof(T) / 2]; };
+template <typename T>
+__device__ __forceinline__ Raw<T> fetch8(const T* p) {
+    Raw<T> r;
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) r.w[i] = *(reinterpret_cast<const uint4*>(p) + i);
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void widen8(const Raw<T>& r, float (&f)[8]) {
+    if constexpr (sizeof(T) == 4) {
+        f[0] = __uint_as_float(r.w[0].x); f[1] = __uint_as_float(r.w[0].y);
+        f[2] = __uint_as_float(r.w[0].z); f[3] = __uint_as_float(r.w[0].w);
+        f[4] = __uint_as_float(r.w[1].x); f[5] = __uint_as_float(r.w[1].y);
+        f[6] = __uint_as_float(r.w[1].z); f[7] = __uint_as_float(r.w[1].w);
+    } else {
+        Elem<__nv_bfloat16>::widen(r.w[0], f);
+    }
+}
+
+constexpr int kWarpRows = 4;   // rows per thread block where a row is one warp
+
+template <typename TY, typename T, int IT, bool ONE_WARP>
+__global__ void __launch_bounds__(ONE_WARP ? 32 * kWarpRows : IT == 4 ? 512 : 1024)
+norm_glue_kernel(const __grid_constant__ GlueArgs a) {
+    __shared__ float sh[2][32];
+    const int t = ONE_WARP ? threadIdx.x & 31 : threadIdx.x, n = ONE_WARP ? 32 : blockDim.x;
+    const long long row = ONE_WARP ? static_cast<long long>(blockIdx.x) * kWarpRows + (threadIdx.x >> 5) : blockIdx.x;
+    if (row >= a.n_tok) return;   // whole warps, and only where a row is one warp
     const long long base = row * a.d;
     const int units = a.d / 8;
-    float h[IT][8], y[IT][8];
+    float h[IT][8];
+    Raw<TY> y[IT];
+    Raw<T> g[IT];
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-        const int u = t + i * ROW;
+        const int u = t + i * n;
         if (u < units) {
             load8(a.h + base + u * 8, h[i]);
-            if (a.y) load8(static_cast<const TY*>(a.y) + base + u * 8, y[i]);
+            if (a.y) y[i] = fetch8(static_cast<const TY*>(a.y) + base + u * 8);
+            if (a.gate) g[i] = fetch8(static_cast<const T*>(a.gate) + row * a.gate_stride + u * 8);
         }
-        if (u >= units)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) h[i][e] = 0.0f;
-        if (u >= units || !a.y)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[i][e] = 0.0f;
     }
     if (a.y) {
         float f = a.res_scale;
         if (a.w_post) {
             float ss = 0.0f;
 #pragma unroll
-            for (int i = 0; i < IT; ++i)
+            for (int i = 0; i < IT; ++i) {
+                if (t + i * n >= units) continue;
+                float v[8];
+                widen8(y[i], v);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) ss = fmaf(y[i][e], y[i][e], ss);
-            ss = row_sum<ROW>(ss, sh[0]);
+                for (int e = 0; e < 8; ++e) ss = fmaf(v[e], v[e], ss);
+            }
+            ss = row_sum<ONE_WARP>(ss, sh[0]);
             f = rsqrtf(ss / static_cast<float>(a.d) + a.eps);
         }
 #pragma unroll
         for (int i = 0; i < IT; ++i) {
-            const int u = t + i * ROW;
+            const int u = t + i * n;
             if (u >= units) continue;
-            float w[8];
+            float v[8], w[8];
+            widen8(y[i], v);
             if (a.w_post) {
                 load8(static_cast<const T*>(a.w_post) + u * 8, w);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[i][e] = y[i][e] * f * w[e] * a.res_scale;
+                for (int e = 0; e < 8; ++e) v[e] = v[e] * f * w[e] * a.res_scale;
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[i][e] *= f;
+                for (int e = 0; e < 8; ++e) v[e] *= f;
             }
             if (a.gate) {
-                load8(static_cast<const T*>(a.gate) + row * a.gate_stride + u * 8, w);
+                widen8(g[i], w);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[i][e] *= w[e];
+                for (int e = 0; e < 8; ++e) v[e] *= w[e];
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) h[i][e] += y[i][e];
+            for (int e = 0; e < 8; ++e) h[i][e] += v[e];
         }
     }
     float ss = 0.0f;
 #pragma unroll
-    for (int i = 0; i < IT; ++i)
+    for (int i = 0; i < IT; ++i) {
+        if (t + i * n >= units) continue;
 #pragma unroll
         for (int e = 0; e < 8; ++e) ss = fmaf(h[i][e], h[i][e], ss);
-    ss = row_sum<ROW>(ss, sh[1]);
+    }
+    ss = row_sum<ONE_WARP>(ss, sh[1]);
     const float f = rsqrtf(ss / static_cast<float>(a.d) + a.eps);
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-        const int u = t + i * ROW;
+        const int u = t + i * n;
         if (u >= units) continue;
         store8(a.h_out + base + u * 8, h[i]);
         float w[8];
@@ -145,22 +172,25 @@ __global__ void __launch_bounds__(ROW < 128 ? 128 : ROW) norm_glue_kernel(const 
     }
 }
 
-template <typename TY, typename T, int ROW, int IT>
-halo_status go(const GlueArgs& a, cudaStream_t st) {
-    constexpr int kRows = ROW < 128 ? 128 / ROW : 1;
-    norm_glue_kernel<TY, T, ROW, IT><<<(a.n_tok + kRows - 1) / kRows, ROW < 128 ? 128 : ROW, 0, st>>>(a);
+template <typename TY, typename T, int IT, bool ONE_WARP>
+halo_status go(const GlueArgs& a, int threads, cudaStream_t st) {
+    const int blocks = ONE_WARP ? (a.n_tok + kWarpRows - 1) / kWarpRows : a.n_tok;
+    norm_glue_kernel<TY, T, IT, ONE_WARP><<<blocks, threads, 0, st>>>(a);
     HALO_CHECK_LAUNCH();
     return HALO_OK;
 }
 template <typename TY, typename T>
 halo_status launch(const GlueArgs& a, cudaStream_t st) {
     const int units = a.d / 8;
-    if (units <= 32) return go<TY, T, 32, 1>(a, st);
-    if (units <= 64) return go<TY, T, 32, 2>(a, st);
-    if (units <= 256) return go<TY, T, 128, 2>(a, st);
-    if (units <= 512) return go<TY, T, 256, 2>(a, st);
-    if (units <= 1024) return go<TY, T, 512, 2>(a, st);
-    return go<TY, T, 1024, 2>(a, st);
+    const auto threads = [&](int it) { return (units + 32 * it - 1) / (32 * it) * 32; };
+    // Many rows: four units per thread, the most bytes in flight per register.  Few rows: one unit per thread while a
+    // thread block can hold the row, the shortest time for a row.
+    const bool many = a.n_tok >= 2 * kSmCount;
+    if (units <= 32) return go<TY, T, 1, true>(a, 32 * kWarpRows, st);
+    if (many && units <= 128) return go<TY, T, 4, true>(a, 32 * kWarpRows, st);
+    if (many) return go<TY, T, 4, false>(a, threads(4), st);
+    if (units <= 1024) return go<TY, T, 1, false>(a, threads(1), st);
+    return go<TY, T, 2, false>(a, threads(2), st);
 }
 
 }  // namespace

@@ -4,8 +4,9 @@
 // Rotation: pair i of a head is turned by the angle pos * inv_freq[i].  The angle is formed and reduced to one turn in
 // fp64 (at position 1e5 an fp32 product is off by 4e-3 radians), cosine and sine are taken in fp32 of the reduced
 // angle, once per token and pair, and shared by all heads of the token through shared memory.
-// A thread block takes one token and part of its heads; the loads of a thread's first units are in flight while the
-// angles are computed.
+// A thread keeps its place inside a head (one 16-byte chunk, or the two chunks of its pairs) and walks over the heads
+// of q, k and v alike, so cosines, sines and offsets stay in registers; the loads of its first heads are in flight
+// while the angles are computed.  Few tokens: the heads of a token are spread over several thread blocks.
 #include "common.cuh"
 
 namespace halo {
@@ -14,8 +15,8 @@ long long paged_stride(const halo_paged_shape& s);
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kUnits = 3;   // units in flight per thread
+constexpr int kThreads = 128;
+constexpr int kHeads = 4;   // heads in flight per thread
 
 struct AppendArgs {
     int H, Hk, dh, page_size, n_pages, max_pages, n_seq, rotary;
@@ -35,128 +36,102 @@ struct AppendArgs {
 
 // A unit is one 16-byte chunk (interleaved pairs, or elements that are not turned), or the two chunks that hold pairs
 // (i, i + rotary / 2).  WIDE = false: chunks of one element, for rotary sizes whose half is not a whole number of
-// 16-byte chunks.
+// 16-byte chunks.  Thread block (token, part): heads part, part + parts, ... in runs of `lanes` heads.
 template <typename T, bool INTERLEAVED, bool WIDE>
-__global__ void __launch_bounds__(kThreads) paged_append_kernel(const __grid_constant__ AppendArgs a, int parts) {
-    constexpr int E = WIDE ? Elem<T>::kPerChunk : (INTERLEAVED ? 2 : 1);
+__global__ void __launch_bounds__(WIDE ? kThreads : 256)
+paged_append_kernel(const __grid_constant__ AppendArgs a, int parts, int units, int lanes) {
+    constexpr int E = WIDE ? Elem<T>::kPerChunk : 1;
+    constexpr int kPairs = INTERLEAVED ? E / 2 : E;
     extern __shared__ float2 turn[];   // [rotary / 2] cosine, sine
     const int tid = threadIdx.x;
     const int tok = blockIdx.x / parts, part = blockIdx.x % parts;
     const int pos = __ldg(a.pos + tok);
     if (pos < 0) return;               // a padding row: nothing of it is read or written
+    const int half = a.rotary / 2;
+    const int pair_units = INTERLEAVED ? 0 : half / E;   // units of two chunks per head
+    const int c = tid % units, hl = tid / units;
+    const int el = INTERLEAVED || c < pair_units ? c * E : a.rotary + (c - pair_units) * E;
+    const int gap = c < pair_units ? half : 0;           // distance of the second chunk
+    const int pair0 = INTERLEAVED ? el / 2 : el;         // first pair of the unit
+    const bool turned = INTERLEAVED ? el < a.rotary : c < pair_units;
+    const int heads = a.H + 2 * a.Hk;
+    const T* q = static_cast<const T*>(a.q) + static_cast<long long>(tok) * a.q_stride + el;
+    const T* k = static_cast<const T*>(a.k) + static_cast<long long>(tok) * a.k_stride + el;
+    const T* v = static_cast<const T*>(a.v) + static_cast<long long>(tok) * a.v_stride + el;
+    const int step = lanes * parts;
+    const int first = hl < lanes ? part * lanes + hl : heads;
+
+    alignas(16) T x[kHeads][2][E];
+    auto fetch = [&](int h0) {
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) {
+            const int h = h0 + i * step;
+            if (h >= heads) continue;
+            const T* src = h < a.H ? q + h * a.dh : h < a.H + a.Hk ? k + (h - a.H) * a.dh : v + (h - a.H - a.Hk) * a.dh;
+            if constexpr (WIDE) {
+                *reinterpret_cast<uint4*>(x[i][0]) = *reinterpret_cast<const uint4*>(src);
+                if (gap) *reinterpret_cast<uint4*>(x[i][1]) = *reinterpret_cast<const uint4*>(src + gap);
+            } else {
+                x[i][0][0] = src[0];
+                if (gap) x[i][1][0] = src[gap];
+            }
+        }
+    };
+    fetch(first);
+
     const int s = a.seq ? __ldg(a.seq + tok) : tok;
     const int pi = pos / a.page_size;
     int page = -1;
     if (s >= 0 && s < a.n_seq && pi < a.max_pages) page = __ldg(a.table + static_cast<long long>(s) * a.max_pages + pi);
-    if (page < 0 || page >= a.n_pages) {
+    for (int i = tid; i < half; i += blockDim.x) {
+        const double turns = static_cast<double>(pos) * __ldg(a.inv_freq + i) * 0.15915494309189533577;
+        float co, si;
+        sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &si, &co);
+        turn[i] = make_float2(co, si);
+    }
+    if (page < 0 || page >= a.n_pages) {   // the same in every thread
         if (tid == 0 && part == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
         return;
     }
-    const int half = a.rotary / 2;
-    const int pair_units = INTERLEAVED ? 0 : half / E;                          // units of two chunks per head
-    const int turned_units = INTERLEAVED ? (a.rotary + E - 1) / E : pair_units; // units that are turned per head
-    const int units = pair_units + (a.dh - (INTERLEAVED ? 0 : a.rotary)) / E;   // units per head
-    const int v_units = a.dh / E;
-    const int all = (a.H + a.Hk) * units + a.Hk * v_units;
-    const int per_part = (all + parts - 1) / parts;
-    const int u1 = min(all, (part + 1) * per_part);
-    const long long base = static_cast<long long>(page) * a.page_stride + static_cast<long long>(pos % a.page_size) * a.dh;
-    const T* q = static_cast<const T*>(a.q) + static_cast<long long>(tok) * a.q_stride;
-    const T* k = static_cast<const T*>(a.k) + static_cast<long long>(tok) * a.k_stride;
-    const T* v = static_cast<const T*>(a.v) + static_cast<long long>(tok) * a.v_stride;
-    T* qo = static_cast<T*>(a.q_out) + static_cast<long long>(tok) * a.qo_stride;
+    __syncthreads();
+    float co[kPairs], si[kPairs];
+#pragma unroll
+    for (int e = 0; e < kPairs; ++e) {
+        const bool in = turned && pair0 + e < half;      // an interleaved chunk may end behind the last pair
+        co[e] = in ? turn[pair0 + e].x : 1.0f;
+        si[e] = in ? turn[pair0 + e].y : 0.0f;
+    }
+    const long long base = static_cast<long long>(page) * a.page_stride + static_cast<long long>(pos % a.page_size) * a.dh + el;
+    const long long plane = static_cast<long long>(a.page_size) * a.dh;
+    T* qo = static_cast<T*>(a.q_out) + static_cast<long long>(tok) * a.qo_stride + el;
 
-    bool ready = false;
-    for (int u = part * per_part + tid; u - tid < u1; u += kThreads * kUnits) {
-        alignas(16) T x[kUnits][2][E];
-        const T* src[kUnits];
-        T* dst[kUnits];
-        int gap[kUnits];      // distance of the second chunk, 0: none
-        int pair0[kUnits];    // first pair of the unit, -1: not turned
+    for (int h0 = first; h0 < heads; h0 += step * kHeads) {
+        if (h0 != first) fetch(h0);
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-            const int w = u + i * kThreads;
-            src[i] = nullptr;
-            if (w >= u1) continue;
-            int head, c, el = 0;
-            gap[i] = 0;
-            pair0[i] = -1;
-            if (w < (a.H + a.Hk) * units) {
-                head = w / units;
-                c = w - head * units;
-                if (INTERLEAVED) {
-                    el = c * E;
-                    if (c < turned_units) pair0[i] = el / 2;
-                } else if (c < pair_units) {
-                    el = c * E;
-                    gap[i] = half;
-                    pair0[i] = el;
-                } else {
-                    el = a.rotary + (c - pair_units) * E;
-                }
-                if (head < a.H) {
-                    src[i] = q + head * a.dh + el;
-                    dst[i] = qo + head * a.dh + el;
-                } else {
-                    src[i] = k + (head - a.H) * a.dh + el;
-                    dst[i] = static_cast<T*>(a.K) + base + static_cast<long long>(head - a.H) * a.page_size * a.dh + el;
-                }
-            } else {
-                const int r = w - (a.H + a.Hk) * units;
-                head = r / v_units;
-                el = (r - head * v_units) * E;
-                src[i] = v + head * a.dh + el;
-                dst[i] = static_cast<T*>(a.V) + base + static_cast<long long>(head) * a.page_size * a.dh + el;
-            }
-            if constexpr (WIDE) {
-                *reinterpret_cast<uint4*>(x[i][0]) = *reinterpret_cast<const uint4*>(src[i]);
-                if (gap[i]) *reinterpret_cast<uint4*>(x[i][1]) = *reinterpret_cast<const uint4*>(src[i] + gap[i]);
-            } else {
+        for (int i = 0; i < kHeads; ++i) {
+            const int h = h0 + i * step;
+            if (h >= heads) continue;
+            T* dst = h < a.H           ? qo + h * a.dh
+                     : h < a.H + a.Hk ? static_cast<T*>(a.K) + base + (h - a.H) * plane
+                                      : static_cast<T*>(a.V) + base + (h - a.H - a.Hk) * plane;
+            if (turned && h < a.H + a.Hk) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) x[i][0][e] = src[i][e];
-                if (gap[i]) x[i][1][0] = src[i][gap[i]];
-            }
-        }
-        if (!ready) {
-            for (int i = tid; i < half; i += kThreads) {
-                const double turns = static_cast<double>(pos) * __ldg(a.inv_freq + i) * 0.15915494309189533577;
-                float c, sn;
-                sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &sn, &c);
-                turn[i] = make_float2(c, sn);
-            }
-            __syncthreads();
-            ready = true;
-        }
-#pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-            if (!src[i]) continue;
-            if (pair0[i] >= 0) {
-                if constexpr (INTERLEAVED) {
-#pragma unroll
-                    for (int e = 0; e < E; e += 2) {
-                        if (pair0[i] + e / 2 >= half) break;
-                        const float2 cs = turn[pair0[i] + e / 2];
-                        const float p = to_float(x[i][0][e]), o = to_float(x[i][0][e + 1]);
-                        x[i][0][e] = from_float<T>(p * cs.x - o * cs.y);
-                        x[i][0][e + 1] = from_float<T>(p * cs.y + o * cs.x);
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const float2 cs = turn[pair0[i] + e];
-                        const float p = to_float(x[i][0][e]), o = to_float(x[i][1][e]);
-                        x[i][0][e] = from_float<T>(p * cs.x - o * cs.y);
-                        x[i][1][e] = from_float<T>(p * cs.y + o * cs.x);
-                    }
+                for (int e = 0; e < kPairs; ++e) {
+                    T& first_of = INTERLEAVED ? x[i][0][2 * e] : x[i][0][e];
+                    T& second_of = INTERLEAVED ? x[i][0][2 * e + 1] : x[i][1][e];
+                    const float p = to_float(first_of), o = to_float(second_of);
+                    // a pair behind the last one is left as it is (infinity * 0 would not be)
+                    if (INTERLEAVED && pair0 + e >= half) continue;
+                    first_of = from_float<T>(p * co[e] - o * si[e]);
+                    second_of = from_float<T>(p * si[e] + o * co[e]);
                 }
             }
             if constexpr (WIDE) {
-                *reinterpret_cast<uint4*>(dst[i]) = *reinterpret_cast<const uint4*>(x[i][0]);
-                if (gap[i]) *reinterpret_cast<uint4*>(dst[i] + gap[i]) = *reinterpret_cast<const uint4*>(x[i][1]);
+                *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(x[i][0]);
+                if (gap) *reinterpret_cast<uint4*>(dst + gap) = *reinterpret_cast<const uint4*>(x[i][1]);
             } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e) dst[i][e] = x[i][0][e];
-                if (gap[i]) dst[i][gap[i]] = x[i][1][0];
+                dst[0] = x[i][0][0];
+                if (gap) dst[gap] = x[i][1][0];
             }
         }
     }
@@ -167,19 +142,22 @@ halo_status launch(const AppendArgs& a, int n_tok, int interleaved, cudaStream_t
     constexpr int E = Elem<T>::kPerChunk;
     const bool wide = interleaved || (a.rotary / 2) % E == 0;
     const int e = wide ? E : 1;
-    const int all = (a.H + a.Hk) * (interleaved ? a.dh / e : a.rotary / 2 / e + (a.dh - a.rotary) / e) + a.Hk * (a.dh / e);
-    const int most = (all + kThreads * kUnits - 1) / (kThreads * kUnits);
-    // few tokens: their heads are spread over thread blocks until the GPU is covered twice
-    int parts = (2 * kSmCount + n_tok - 1) / n_tok;
+    const int units = interleaved ? a.dh / e : a.rotary / 2 / e + (a.dh - a.rotary) / e;   // per head, <= 256
+    const int threads = wide ? kThreads : 256;
+    const int lanes = threads / units;          // heads side by side in a thread block
+    const int heads = a.H + 2 * a.Hk;
+    const int most = (heads + lanes - 1) / lanes;
+    // few tokens: their heads are spread over thread blocks until the GPU is covered four times
+    int parts = (4 * kSmCount + n_tok - 1) / n_tok;
     parts = parts < 1 ? 1 : parts > most ? most : parts;
     const unsigned grid = static_cast<unsigned>(n_tok) * parts;
     const size_t smem = sizeof(float2) * (a.rotary / 2);
     if (interleaved)
-        paged_append_kernel<T, true, true><<<grid, kThreads, smem, st>>>(a, parts);
+        paged_append_kernel<T, true, true><<<grid, threads, smem, st>>>(a, parts, units, lanes);
     else if (wide)
-        paged_append_kernel<T, false, true><<<grid, kThreads, smem, st>>>(a, parts);
+        paged_append_kernel<T, false, true><<<grid, threads, smem, st>>>(a, parts, units, lanes);
     else
-        paged_append_kernel<T, false, false><<<grid, kThreads, smem, st>>>(a, parts);
+        paged_append_kernel<T, false, false><<<grid, threads, smem, st>>>(a, parts, units, lanes);
     HALO_CHECK_LAUNCH();
     return HALO_OK;
 }

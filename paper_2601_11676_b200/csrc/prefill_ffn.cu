@@ -1096,6 +1096,19 @@ bool make_byte_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t r
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// the scale blocks of microscaled rows: [tiles][blocks] runs of 512 bytes, as they lie
+bool make_scale_map(CUtensorMap* map, const void* base, uint64_t tiles, uint64_t blocks, uint32_t box_tiles, uint32_t box_blocks) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {128, blocks, tiles};   // 32-bit words
+    const cuuint64_t strides[2] = {512, 512 * blocks};
+    const cuuint32_t box[3] = {128, box_blocks, box_tiles};
+    const cuuint32_t elem_strides[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void*>(base), dims, strides, box, elem_strides,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool prefill_supported(const halo_ffn_shape& sh, int n_tok) {
     return sh.wdtype == HALO_BF16 && n_tok >= 16 && (sh.group_size == 64 || sh.group_size == 128 || sh.group_size == 256) &&
            sh.d_model % 128 == 0 && sh.d_ffn / sh.group_size <= HALO_MAX_GROUPS;
