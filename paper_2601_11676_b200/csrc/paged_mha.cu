@@ -1,22 +1,22 @@
 // halo_paged_mha: attention of one new token per sequence over a paged K/V cache, split over the cache's length and
 // joined.  HBM-bound: every K and V row is read once, 4 * G flops per element of it (G = query heads per K/V head).
 //
-// Work line.  The cache is cut into tiles of kTile positions; an item is one (sequence, K/V head, block of 16 query
-// heads).  All tiles of all items, item after item, form one line of T tiles and thread block c of C takes the tiles
-// [c*T/C, (c+1)*T/C): whatever the lengths are, every thread block streams the same number of tiles.  A piece that
-// covers a whole item writes its output; the at most two pieces of a thread block that do not (its first and its last)
-// leave (maximum, sum, weighted sum of values) in the workspace and a second kernel, resident before the first ends
-// (programmatic dependent launch), joins them in line order, so results do not depend on timing.  Every thread block
-// computes the line from seq_len itself; the host never reads a length.
+// Work line.  The cache is cut into tiles of 16 positions per warp; an item is one (sequence, K/V head, block of 16
+// query heads).  All tiles of all items, item after item, form one line of T tiles and thread block c of C (at most T)
+// takes the tiles [c*T/C, (c+1)*T/C): whatever the lengths are, every thread block streams the same number of tiles.  A
+// piece that covers a whole item writes its output; the at most two pieces of a range that do not (its first and its
+// last) leave (maximum, sum, weighted sum of values) in the workspace and a second kernel, launched before the first
+// ends (programmatic dependent launch), joins them in line order, so results do not depend on timing.  Every thread
+// block computes the line from seq_len itself; the host never reads a length.
 //
-// Inside a thread block each warp takes 16 positions of a tile at a time through a shared-memory ring of its own
-// (cp.async, no block barrier in the loop) and keeps a running maximum and sum per query head.  Scores and weighted
-// sums go through mma.sync with the query heads as the 16 rows of A: one new token makes a matrix of at most 16 rows
-// that cannot fill a tcgen05 tile of 128, and the stream of K and V bounds the kernel, not the tensor pipe.
-//   bf16: m16n8k16, probabilities rounded to bf16 for the second product (relative 2^-9, below the rounding of the
-//         output), sums of probabilities in fp32 before that rounding.
-//   fp32: m16n8k8 tf32 with both operands split into two tf32 parts, three products (hi*hi + hi*lo + lo*hi): what is
-//         dropped is 2^-22 of a product.
+// The warps of a thread block take 16 positions of a tile each, with a shared-memory ring (cp.async), a running maximum
+// and a running sum per query head of their own; they meet once per piece.  Copies run ahead across pieces, so that a
+// short sequence's first rows are on their way while the one before it is still being summed.
+//   bf16: scores and weighted sums through mma.sync m16n8k16 with the query heads as the 16 rows of A: one new token
+//     makes a matrix of at most 16 rows that cannot fill a tcgen05 tile of 128, and the stream of K and V bounds the
+//     kernel, not the tensor pipe.  Weights are rounded to bf16 for the second product (relative 2^-8, like the output);
+//     their sum is taken in fp32 before that rounding.
+//   fp32: fused multiply-adds, two lanes per position for the scores, a column per lane for the weighted sums.
 #include <math.h>
 
 #include "common.cuh"
@@ -26,8 +26,18 @@ namespace {
 
 constexpr int kMaxSplitRows = 16;   // query heads per item
 
+// What the join has to know of a range whose last piece begins an item that it does not end; in front of the slots.
+struct __align__(32) Cut {
+    int opens, s, hi, rest;   // rest: tiles of the item behind the range
+    long long total;          // T
+    int fills, unused;        // the item's first piece is the whole range
+};
+
 struct PagedArgs {
-    int n_seq, H, Hk, G, qblocks, dh, page_size, n_pages, max_pages;
+    int n_seq, H, Hk, G, qblocks, dh, page_size, page_shift, n_pages, max_pages;   // page_shift: -1 = no power of two
+    int slot;    // floats of a workspace slot
+    int rows;    // query heads of an item, at most
+    int merge;   // bytes in front of the rings where the warps meet
     long long page_stride, q_stride;
     float scale_log2;
     const void* q;
@@ -38,6 +48,7 @@ struct PagedArgs {
     const uint8_t* keep;
     void* out;
     float* lse;
+    Cut* cuts;   // [C], then the slots: two per range
     float* ws;
     uint32_t* status;
     int whole;   // one thread block per item: no line, no join
@@ -65,43 +76,35 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], 
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t tf32_of(float x) {
-    uint32_t r;
-    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
-    return r;
-}
-// x = hi + lo + at most 2^-22 |x|; hi is cut off, not rounded, so it never overflows.
-__device__ __forceinline__ void split_tf32(float x, uint32_t& hi, uint32_t& lo) {
-    hi = __float_as_uint(x) & 0xffffe000u;
-    lo = tf32_of(x - __uint_as_float(hi));
-}
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// Tile shapes per element type and padded head size.  Ring bytes per SM are what keeps HBM busy: 6.5 TB/s x ~1 us of
-// latency / 148 SMs = 44 KB have to be in flight; stages x warps x thread blocks per SM below give 96 to 128 KB.
-template <typename T, int DP>
+constexpr int kRun = 16;            // positions of a tile that one warp takes
+constexpr float kLn2 = 0.693147180559945309f;
+constexpr int kSlotHead = 32;       // floats in front of a slot's values: maxima, sums
+// Shapes per element type, padded head size DP and (fp32) padded number of query heads GR.  Ring bytes are what keeps
+// HBM busy: 6.5 TB/s x ~1 us of latency / 148 SMs = 44 KB have to be in flight; the shapes below hold 96 to 200 KB.
+template <typename T, int DP, int GR>
 struct Cfg {
     static constexpr bool kF32 = sizeof(T) == 4;
-    static constexpr int kWarps = (kF32 && DP == 256) ? 2 : 4;
-    static constexpr int kStages = (kF32 && DP == 256) ? 2 : 3;
-    static constexpr int kTile = kWarps * 16;
-    static constexpr int kRowBytes = kF32 ? (DP + 4) * 4 : DP * 2;   // fp32: rows padded by 16 bytes; bf16: swizzled
-    static constexpr int kHalf = 16 * kRowBytes;                     // keys (or values) of one stage of one warp
+    static constexpr int kWarps = (kF32 && DP == 256) ? (GR == 16 ? 2 : 3) : 4;
+    static constexpr int kStages = kF32 && (DP == 256 || (DP == 128 && GR == 16)) ? 2 : 3;
+    static constexpr int kTile = kWarps * kRun;
+    static constexpr int kRowBytes = kF32 ? (DP + 8) * 4 : DP * 2;   // fp32: rows padded against bank conflicts; bf16: swizzled
+    static constexpr int kHalf = kRun * kRowBytes;                   // keys (or values) of one stage
     static constexpr int kStage = 2 * kHalf;
-    static constexpr int kRing = kWarps * kStages * kStage;
-    static constexpr int kQ = kF32 ? 2 * 16 * (DP + 4) * 4 : 0;      // fp32: the query rows split into two tf32 parts
-    static constexpr int kMerge = kWarps * 16 * (DP + 4) * 4;        // the warps' sums meet here, over the ring
-    static constexpr int kSmem = (kRing > kMerge ? kRing : kMerge) + kQ;
-    static constexpr int kBlocksPerSm = kSmem <= 56 * 1024 ? 4 : kSmem <= 113 * 1024 ? 2 : 1;
-    static constexpr int kSlot = 2 * 16 + 16 * DP;                   // floats of a workspace slot: maxima, sums, values
+    static constexpr int kRing = kStages * kStage;
+    static constexpr int kOwn = kF32 ? GR * DP * 4 + GR * kRun * 4 : 0;   // fp32: query rows and weights of the warp
+    static constexpr int kWarpBytes = kRing + kOwn;
+    static constexpr int kRings = kWarps * kWarpBytes;
+    static constexpr int kMergeRow = DP + 4;                         // floats
+    // two warps' sums at a time, of the item's query heads
+    static constexpr int merge_bytes(int rows) { return kWarps > 2 ? 2 * rows * kMergeRow * 4 : rows * kMergeRow * 4; }
+    static constexpr int kMaxSmem = kRings + merge_bytes(GR);
+    static constexpr int kBlocksPerSm = kMaxSmem <= 56 * 1024 ? 4 : kMaxSmem <= 75 * 1024 ? 3 : kMaxSmem <= 115200 ? 2 : 1;
+    static_assert(kMaxSmem <= 225 * 1024, "shared memory");
 };
 
 __device__ __forceinline__ int valid_len(const PagedArgs& a, int s, bool flag) {
@@ -113,20 +116,22 @@ __device__ __forceinline__ int valid_len(const PagedArgs& a, int s, bool flag) {
     return n;
 }
 template <int TILE>
-__device__ __forceinline__ long long tiles_of(const PagedArgs& a, int s) {
-    const int n = valid_len(a, s, false);
-    return n > 0 ? (n + TILE - 1) / TILE : 1;   // an empty sequence keeps one tile, which writes its zeros
+__device__ __forceinline__ int tiles_in(int len) {
+    return len > 0 ? (len - 1) / TILE + 1 : 1;   // an empty sequence keeps one tile, which writes its zeros
 }
+template <int TILE>
+__device__ __forceinline__ int tiles_of(const PagedArgs& a, int s) { return tiles_in<TILE>(valid_len(a, s, false)); }
 
-// The line: total number of tiles of one head's sequences (times items per sequence = T), and the sequence in which
-// line position x(T) falls.  All threads of the block call it.
+// The line: its length T, and the sequence that holds position_of(T) (T or more: none).  All threads of the block call
+// it.
 struct LinePos {
-    long long total;   // T
+    long long total;
     long long start;   // first line position of sequence s
     int s;
 };
 template <int TILE, int THREADS, typename F>
-__device__ __forceinline__ LinePos locate(const PagedArgs& a, F position_of, long long* sh /*[THREADS / 32 + 3]*/) {
+__device__ __forceinline__ LinePos locate(const PagedArgs& a, F position_of, long long* sh /*[THREADS / 32 + 2]*/) {
+    constexpr int W = THREADS / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (a.n_seq + THREADS - 1) / THREADS;
     const int s0 = min(tid * per, a.n_seq), s1 = min(s0 + per, a.n_seq);
@@ -143,7 +148,7 @@ __device__ __forceinline__ LinePos locate(const PagedArgs& a, F position_of, lon
     __syncthreads();
     long long before = 0, total = 0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
+    for (int w = 0; w < W; ++w) {
         if (w < warp) before += sh[w];
         total += sh[w];
     }
@@ -153,21 +158,21 @@ __device__ __forceinline__ LinePos locate(const PagedArgs& a, F position_of, lon
         for (int s = s0; s < s1; ++s) {
             const long long n = tiles_of<TILE>(a, s) * items;
             if (x < at + n) {
-                sh[THREADS / 32] = at;
-                sh[THREADS / 32 + 1] = s;
+                sh[W] = at;
+                sh[W + 1] = s;
                 break;
             }
             at += n;
         }
     }
     __syncthreads();
-    LinePos r;
-    r.total = total * items;
-    r.start = sh[THREADS / 32];
-    r.s = static_cast<int>(sh[THREADS / 32 + 1]);
-    return r;
+    return {total * items, sh[W], static_cast<int>(sh[W + 1])};
 }
+// Thread blocks that have a range (none of them empty), and where the c-th range begins.
+__device__ __forceinline__ int ranges(long long T, int blocks) { return T < blocks ? static_cast<int>(T) : blocks; }
 __device__ __forceinline__ long long cut(long long T, int c, int C) { return T * c / C; }
+// the range that holds line position x: the last c with T * c / C <= x
+__device__ __forceinline__ int range_of(long long T, long long x, int C) { return static_cast<int>(((x + 1) * C - 1) / T); }
 
 __device__ __forceinline__ bool head_kept(const PagedArgs& a, int h) { return !a.keep || a.keep[h] != 0; }
 
@@ -176,132 +181,128 @@ __device__ __forceinline__ void write_head(const PagedArgs& a, int s, int h, int
     static_cast<T*>(a.out)[(static_cast<long long>(s) * a.H + h) * a.dh + j] = from_float<T>(v);
 }
 
-template <typename T, int DP>
-__global__ void __launch_bounds__(Cfg<T, DP>::kWarps * 32, Cfg<T, DP>::kBlocksPerSm)
+// The way along a range: piece after piece.
+template <int TILE>
+struct Walk {
+    long long left;     // tiles from t0 of this piece to the end of the range
+    int s, hi;          // sequence and item of it
+    int len, nt;        // its valid length and tiles
+    int t0, t1;         // tiles of the piece
+    int reach;          // positions that take part: len, or 0 where every head of the item is lost
+    __device__ __forceinline__ void item(const PagedArgs& a) {
+        t1 = static_cast<int>(min(static_cast<long long>(nt), t0 + left));
+        reach = len;
+        if (a.keep) {
+            const int h0 = hi / a.qblocks * a.G + hi % a.qblocks * 16, n = min(16, a.G - hi % a.qblocks * 16);
+            bool any = false;
+            for (int r = 0; r < n; ++r) any |= head_kept(a, h0 + r);
+            if (!any) reach = 0;
+        }
+    }
+    __device__ __forceinline__ void begin(const PagedArgs& a, int s_, long long at, long long n) {   // at: tiles behind the sequence's first
+        s = s_;
+        left = n;
+        len = valid_len(a, s, false);
+        nt = tiles_in<TILE>(len);
+        hi = static_cast<int>(at / nt);
+        t0 = static_cast<int>(at - static_cast<long long>(hi) * nt);
+        item(a);
+    }
+    __device__ __forceinline__ void next(const PagedArgs& a) {
+        left -= t1 - t0;
+        if (left <= 0) return;
+        t0 = 0;
+        if (++hi == a.Hk * a.qblocks) {
+            hi = 0;
+            ++s;
+            len = valid_len(a, s, false);
+            nt = tiles_in<TILE>(len);
+        }
+        item(a);
+    }
+};
+
+template <typename T, int DP, int GR>
+__global__ void __launch_bounds__(Cfg<T, DP, GR>::kWarps * 32, Cfg<T, DP, GR>::kBlocksPerSm)
 paged_mha_kernel(const __grid_constant__ PagedArgs a) {
-    using C_ = Cfg<T, DP>;
+    using C_ = Cfg<T, DP, GR>;
     constexpr bool kF32 = C_::kF32;
+    constexpr int S = C_::kStages;
     constexpr int kThreads = C_::kWarps * 32;
     constexpr int kE = kF32 ? 4 : 8;              // elements per 16 bytes
     constexpr int kCpr = DP / kE;                 // 16-byte chunks per padded row
-    constexpr int kRowsPer = 32 / (kCpr < 32 ? kCpr : 32);   // rows a warp copies per instruction
-    constexpr int kChunkIters = kCpr / 32 > 0 ? kCpr / 32 : 1;   // instructions per row where a row is longer
-    constexpr int NT = DP / 8;                    // 8-wide column tiles of the output
+    constexpr int kLanesPerRow = kCpr < 32 ? kCpr : 32;
+    constexpr int kRowsPer = 32 / kLanesPerRow;   // rows a warp copies per instruction
+    constexpr int kChunkIters = kCpr / kLanesPerRow;
+    constexpr int NT = DP / 8;                    // bf16: 8-wide column tiles of the output
+    constexpr int V = DP / 32;                    // fp32: output columns per lane
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ long long scan[C_::kWarps + 3];
+    __shared__ long long scan[C_::kWarps + 2];
     __shared__ float wm[C_::kWarps][16], wl[C_::kWarps][16];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int items = a.Hk * a.qblocks;
 
     asm volatile("griddepcontrol.launch_dependents;");
-    long long x, x_end, start;
-    int s;
+    Walk<C_::kTile> con, iss;     // the piece that is summed, the piece whose rows are fetched
+    long long total = 0;
     if (a.whole) {
-        s = blockIdx.x / items;
-        const long long t = tiles_of<C_::kTile>(a, s);
-        start = 0;                                 // line positions relative to the sequence
-        x = (blockIdx.x % items) * t;
-        x_end = x + t;
+        const int s = blockIdx.x / items;
+        const int nt = tiles_of<C_::kTile>(a, s);
+        con.begin(a, s, static_cast<long long>(blockIdx.x % items) * nt, nt);
     } else {
         const LinePos p = locate<C_::kTile, kThreads>(
-            a, [&](long long T_) { return cut(T_, blockIdx.x, gridDim.x); }, scan);
-        x = cut(p.total, blockIdx.x, gridDim.x);
-        x_end = cut(p.total, blockIdx.x + 1, gridDim.x);
-        start = p.start;
-        s = p.s;
+            a, [&](long long t) {
+                const int C = ranges(t, gridDim.x);
+                return static_cast<int>(blockIdx.x) < C ? cut(t, blockIdx.x, C) : t;
+            }, scan);
+        total = p.total;
+        const int C = ranges(total, gridDim.x);
+        if (static_cast<int>(blockIdx.x) >= C) return;
+        const long long x = cut(total, blockIdx.x, C);
+        con.begin(a, p.s, x - p.start, cut(total, blockIdx.x + 1, C) - x);
     }
-    if (x >= x_end) return;
-    const long long x_first = x;
+    iss = con;
+    const long long range = con.left;
 
-    unsigned char* ring = smem + warp * (C_::kStages * C_::kStage);
+    float* mg = reinterpret_cast<float*>(smem);       // the warps meet here
+    unsigned char* ring = smem + a.merge + warp * C_::kWarpBytes;
     const uint32_t ring_a = smem_addr(ring);
     if (a.dh != DP) {   // columns behind the head's own stay zero: they meet zeros of q and give unused output columns
-        for (int i = tid * 16; i < C_::kRing; i += kThreads * 16) *reinterpret_cast<uint4*>(smem + i) = make_uint4(0, 0, 0, 0);
-        __syncthreads();
+        for (int i = lane * 16; i < C_::kRing; i += 32 * 16) *reinterpret_cast<uint4*>(ring + i) = make_uint4(0, 0, 0, 0);
+        __syncwarp();
     }
-    const int g = lane >> 2, t4 = lane & 3;
 
-    while (x < x_end) {
-        // ---- the piece: sequence s, item hi, tiles [t0, t1) of nt -------------------------------------------------
-        const int len_all = valid_len(a, s, x == x_first && tid == 0);
-        const long long nt = len_all > 0 ? (len_all + C_::kTile - 1) / C_::kTile : 1;
-        const int hi = static_cast<int>((x - start) / nt);
-        const int t0 = static_cast<int>((x - start) - hi * nt);
-        const int t1 = static_cast<int>(min(nt, t0 + (x_end - x)));
-        const int kvh = hi / a.qblocks, r0 = (hi % a.qblocks) * 16;
-        const int rows = min(16, a.G - r0), h0 = kvh * a.G + r0;
-        bool any = false;
-        for (int r = 0; r < rows; ++r) any |= head_kept(a, h0 + r);
-        const int len = any ? len_all : 0;
-
-        // ---- query rows -------------------------------------------------------------------------------------------
-        uint32_t qf[kF32 ? 1 : DP / 16][4];
-        float* q_hi = reinterpret_cast<float*>(smem + C_::kSmem - C_::kQ);
-        float* q_lo = q_hi + 16 * (DP + 4);
-        const T* qrow = static_cast<const T*>(a.q) + static_cast<long long>(s) * a.q_stride + static_cast<long long>(h0) * a.dh;
-        if constexpr (!kF32) {
-#pragma unroll
-            for (int k = 0; k < DP / 16; ++k)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int r = g + (j & 1) * 8, c = k * 16 + (j >> 1) * 8 + t4 * 2;
-                    qf[k][j] = (r < rows && c < a.dh)
-                                   ? __ldg(reinterpret_cast<const uint32_t*>(qrow + static_cast<long long>(r) * a.dh + c)) : 0u;
-                }
-        } else {
-            for (int i = tid; i < 16 * DP; i += kThreads) {
-                const int r = i / DP, c = i % DP;
-                uint32_t hi_, lo_;
-                split_tf32((r < rows && c < a.dh) ? __ldg(reinterpret_cast<const float*>(qrow) + static_cast<long long>(r) * a.dh + c) : 0.0f,
-                           hi_, lo_);
-                q_hi[r * (DP + 4) + c] = __uint_as_float(hi_);
-                q_lo[r * (DP + 4) + c] = __uint_as_float(lo_);
-            }
-            __syncthreads();
-        }
-
-        float o[NT][4];
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[n][j] = 0.0f;
-        float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
-
-        // ---- this warp's runs of 16 positions: first position (t0 * kWarps + warp) * 16, every kTile ------------
-        const int p_begin = t0 * C_::kTile + warp * 16;
-        const int p_end = min(len, t1 * C_::kTile);
-        const int n_run = p_end > p_begin ? (p_end - p_begin + C_::kTile - 1) / C_::kTile : 0;
-        const int32_t* trow = a.table + static_cast<long long>(s) * a.max_pages;
-        // page of position p + lane % 16, -1 behind the end
-        auto page_at = [&](int run) {
-            const int p = p_begin + run * C_::kTile + (lane & 15);
-            return run < n_run && p < p_end ? __ldg(trow + p / a.page_size) : -1;
-        };
-        uint32_t masks[C_::kStages];
-#pragma unroll
-        for (int i = 0; i < C_::kStages; ++i) masks[i] = 0;
-        int page_next = page_at(0);
-        bool bad = false;
-        auto issue = [&](int run) -> uint32_t {   // starts the copies of a run; returns its mask of present positions
-            uint32_t mask = 0;
-            if (run < n_run) {
-                const int p = p_begin + run * C_::kTile + (lane & 15);
-                const int page = page_next;
-                const bool in = p < p_end, ok = in && page >= 0 && page < a.n_pages;
-                bad |= in && !ok;
-                mask = __ballot_sync(0xffffffffu, ok) & 0xffffu;
-                const long long off = ok ? static_cast<long long>(page) * a.page_stride +
-                                               (static_cast<long long>(kvh) * a.page_size + p % a.page_size) * a.dh
+    // ---- fetching ---------------------------------------------------------------------------------------------------
+    int it = iss.t0, slot_in = 0;
+    const auto page_at = [&]() {   // page of this lane's position of the next run, -1 behind the end
+        const int p = it * C_::kTile + warp * kRun + (lane & 15);
+        if (iss.left <= 0 || p >= iss.reach) return -1;
+        return __ldg(a.table + static_cast<long long>(iss.s) * a.max_pages + (a.page_shift >= 0 ? p >> a.page_shift : p / a.page_size));
+    };
+    int page_next = page_at();
+    bool bad = false;
+    const auto issue = [&]() -> uint32_t {   // starts the copies of the next run; returns its mask of present positions
+        uint32_t mask = 0;
+        if (iss.left > 0) {
+            const int p = it * C_::kTile + warp * kRun + (lane & 15);
+            const bool in = p < iss.reach, ok = in && page_next >= 0 && page_next < a.n_pages;
+            bad |= in && !ok;
+            mask = __ballot_sync(0xffffffffu, ok) & 0xffffu;
+            if (mask) {
+                const int kvh = a.qblocks == 1 ? iss.hi : iss.hi / a.qblocks;
+                const int in_page = a.page_shift >= 0 ? p & (a.page_size - 1) : p % a.page_size;
+                const long long off = ok ? static_cast<long long>(page_next) * a.page_stride +
+                                               (static_cast<long long>(kvh) * a.page_size + in_page) * a.dh
                                          : 0;
-                const uint32_t st = ring_a + (run % C_::kStages) * C_::kStage;
+                const uint32_t st = ring_a + slot_in * C_::kStage;
 #pragma unroll
-                for (int it = 0; it < 16 / kRowsPer; ++it) {
-                    const int r = it * kRowsPer + (kCpr < 32 ? lane / kCpr : 0);
+                for (int i = 0; i < kRun / kRowsPer; ++i) {
+                    const int r = i * kRowsPer + lane / kLanesPerRow;
                     const long long ro = __shfl_sync(0xffffffffu, off, r);
                     const bool have = (mask >> r) & 1u;
 #pragma unroll
                     for (int ci = 0; ci < kChunkIters; ++ci) {
-                        const int c = (lane % (kCpr < 32 ? kCpr : 32)) + ci * 32;
+                        const int c = lane % kLanesPerRow + ci * 32;
                         if (c * kE < a.dh) {
                             const uint32_t d = st + r * C_::kRowBytes + (kF32 ? c * 16 : ((c & ~7) | ((c ^ r) & 7)) * 16);
                             cp_async16(d, static_cast<const T*>(a.K) + ro + c * kE, have);
@@ -310,97 +311,106 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                     }
                 }
             }
-            page_next = page_at(run + 1);
-            cp_commit();
-            return mask;
-        };
+            if (++it == iss.t1) {
+                iss.next(a);
+                it = iss.t0;
+            }
+            page_next = page_at();
+        }
+        if (++slot_in == S) slot_in = 0;
+        cp_commit();
+        return mask;
+    };
+    uint32_t masks[S];
 #pragma unroll
-        for (int i = 0; i < C_::kStages - 1; ++i) masks[i] = issue(i);
+    for (int i = 0; i < S - 1; ++i) masks[i] = issue();
 
-        for (int run = 0; run < n_run; ++run) {
-            masks[C_::kStages - 1] = issue(run + C_::kStages - 1);
-            cp_wait<C_::kStages - 1>();
-            __syncwarp();
-            const uint32_t mask = masks[0];
+    // ---- summing ----------------------------------------------------------------------------------------------------
+    const int g = lane >> 2, t4 = lane & 3;
+    int slot_out = 0;
+    while (con.left > 0) {
+        const int kvh = con.hi / a.qblocks, r0 = (con.hi % a.qblocks) * 16;
+        const int rows = min(16, a.G - r0), h0 = kvh * a.G + r0;
+        const T* qrow = static_cast<const T*>(a.q) + static_cast<long long>(con.s) * a.q_stride + static_cast<long long>(h0) * a.dh;
+        const bool complete = con.t0 == 0 && con.t1 == con.nt;
+        float* slot = a.ws + (static_cast<long long>(blockIdx.x) * 2 + (con.left == range ? 0 : 1)) * a.slot;
+
+        if constexpr (!kF32) {
+            uint32_t qf[DP / 16][4];
 #pragma unroll
-            for (int i = 0; i + 1 < C_::kStages; ++i) masks[i] = masks[i + 1];
-            const uint32_t st = ring_a + (run % C_::kStages) * C_::kStage;
-            // scores of 16 heads x 16 positions
-            float sc[2][4] = {};
-            if constexpr (!kF32) {
-                float sc2[2][4] = {};   // a second chain: products of odd steps
-                const int key = (lane >> 4) * 8 + (lane & 7), half = (lane >> 3) & 1;
+            for (int k = 0; k < DP / 16; ++k)
 #pragma unroll
-                for (int k = 0; k < DP / 16; ++k) {
-                    const int c = k * 2 + half;
-                    uint32_t b[4];
-                    ldsm4(b, st + key * C_::kRowBytes + ((c & ~7) | ((c ^ key) & 7)) * 16);
-                    mma_bf16(k & 1 ? sc2[0] : sc[0], qf[k], b[0], b[1]);
-                    mma_bf16(k & 1 ? sc2[1] : sc[1], qf[k], b[2], b[3]);
+                for (int j = 0; j < 4; ++j) {
+                    const int r = g + (j & 1) * 8, c = k * 16 + (j >> 1) * 8 + t4 * 2;
+                    qf[k][j] = (r < rows && c < a.dh)
+                                   ? __ldg(reinterpret_cast<const uint32_t*>(qrow + static_cast<long long>(r) * a.dh + c)) : 0u;
                 }
+            float o[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[n][j] = 0.0f;
+            float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+
+            for (int t = con.t0; t < con.t1; ++t) {
+                masks[S - 1] = issue();
+                cp_wait<S - 1>();
+                __syncwarp();
+                const uint32_t mask = masks[0];
+#pragma unroll
+                for (int i = 0; i + 1 < S; ++i) masks[i] = masks[i + 1];
+                const uint32_t st = ring_a + slot_out * C_::kStage;
+                if (++slot_out == S) slot_out = 0;
+                if (mask == 0) continue;
+                // scores of 16 heads x 16 positions, even and odd steps in two chains
+                float sc[2][4] = {}, sc2[2][4] = {};
+                {
+                    const int key = (lane >> 4) * 8 + (lane & 7), half = (lane >> 3) & 1;
+#pragma unroll
+                    for (int k = 0; k < DP / 16; ++k) {
+                        const int c = k * 2 + half;
+                        uint32_t b[4];
+                        ldsm4(b, st + key * C_::kRowBytes + ((c & ~7) | ((c ^ key) & 7)) * 16);
+                        mma_bf16(k & 1 ? sc2[0] : sc[0], qf[k], b[0], b[1]);
+                        mma_bf16(k & 1 ? sc2[1] : sc[1], qf[k], b[2], b[3]);
+                    }
+                }
+                // running softmax; a lane holds rows g and g + 8, positions 2 * t4 + {0, 1} and 8 more
+                float mx0 = m0, mx1 = m1;
 #pragma unroll
                 for (int n = 0; n < 2; ++n)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) sc[n][j] += sc2[n][j];
-            } else {
-                const float* kp = reinterpret_cast<const float*>(ring + (run % C_::kStages) * C_::kStage);
-                for (int k = 0; k < DP / 8; ++k) {
-                    uint32_t ah[4], al[4];
+                    for (int j = 0; j < 4; ++j) {
+                        const int key = n * 8 + t4 * 2 + (j & 1);
+                        sc[n][j] = (mask >> key) & 1u ? (sc[n][j] + sc2[n][j]) * a.scale_log2 : -INFINITY;
+                        if (j < 2) mx0 = fmaxf(mx0, sc[n][j]); else mx1 = fmaxf(mx1, sc[n][j]);
+                    }
+#pragma unroll
+                for (int d = 1; d < 4; d <<= 1) {
+                    mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, d));
+                    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, d));
+                }
+                const float b0 = mx0 == -INFINITY ? 0.0f : mx0, b1 = mx1 == -INFINITY ? 0.0f : mx1;
+                const float f0 = exp2f(m0 - b0), f1 = exp2f(m1 - b1);
+                if (__any_sync(0xffffffffu, m0 != mx0 || m1 != mx1)) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        o[n][0] *= f0; o[n][1] *= f0;
+                        o[n][2] *= f1; o[n][3] *= f1;
+                    }
+                }
+                m0 = mx0; m1 = mx1;
+                float a0 = 0.0f, a1 = 0.0f;
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const int at = (g + (j & 1) * 8) * (DP + 4) + k * 8 + (j >> 1) * 4 + t4;
-                        ah[j] = __float_as_uint(q_hi[at]);
-                        al[j] = __float_as_uint(q_lo[at]);
+                        sc[n][j] = exp2f(sc[n][j] - (j < 2 ? b0 : b1));
+                        if (j < 2) a0 += sc[n][j]; else a1 += sc[n][j];
                     }
-#pragma unroll
-                    for (int n = 0; n < 2; ++n) {
-                        uint32_t bh[2], bl[2];
-#pragma unroll
-                        for (int j = 0; j < 2; ++j)
-                            split_tf32(kp[(n * 8 + g) * (DP + 4) + k * 8 + j * 4 + t4], bh[j], bl[j]);
-                        mma_tf32(sc[n], al, bh[0], bh[1]);
-                        mma_tf32(sc[n], ah, bl[0], bl[1]);
-                        mma_tf32(sc[n], ah, bh[0], bh[1]);
-                    }
-                }
-            }
-            // running softmax; a lane holds rows g and g + 8, positions 2 * t4 + {0, 1} and 8 more
-            float mx0 = m0, mx1 = m1;
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int key = n * 8 + t4 * 2 + (j & 1);
-                    sc[n][j] = (mask >> key) & 1u ? sc[n][j] * a.scale_log2 : -INFINITY;
-                    if (j < 2) mx0 = fmaxf(mx0, sc[n][j]); else mx1 = fmaxf(mx1, sc[n][j]);
-                }
-#pragma unroll
-            for (int d = 1; d < 4; d <<= 1) {
-                mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, d));
-                mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, d));
-            }
-            const float b0 = mx0 == -INFINITY ? 0.0f : mx0, b1 = mx1 == -INFINITY ? 0.0f : mx1;
-            const float f0 = exp2f(m0 - b0), f1 = exp2f(m1 - b1);
-            if (__any_sync(0xffffffffu, m0 != mx0 || m1 != mx1)) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    o[n][0] *= f0; o[n][1] *= f0;
-                    o[n][2] *= f1; o[n][3] *= f1;
-                }
-            }
-            m0 = mx0; m1 = mx1;
-            float a0 = 0.0f, a1 = 0.0f;
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    sc[n][j] = exp2f(sc[n][j] - (j < 2 ? b0 : b1));
-                    if (j < 2) a0 += sc[n][j]; else a1 += sc[n][j];
-                }
-            l0 = fmaf(l0, f0, a0);
-            l1 = fmaf(l1, f1, a1);
-            // weighted sum of the values
-            if constexpr (!kF32) {
+                l0 = fmaf(l0, f0, a0);
+                l1 = fmaf(l1, f1, a1);
+                // weighted sum of the values
                 const uint32_t pa[4] = {pack_bf16(sc[0][0], sc[0][1]), pack_bf16(sc[0][2], sc[0][3]),
                                         pack_bf16(sc[1][0], sc[1][1]), pack_bf16(sc[1][2], sc[1][3])};
                 const int key = ((lane >> 3) & 1) * 8 + (lane & 7), half = lane >> 4;
@@ -412,212 +422,421 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                     mma_bf16(o[n], pa, b[0], b[1]);
                     mma_bf16(o[n + 1], pa, b[2], b[3]);
                 }
-            } else {
-                // positions 2 * t4 and 2 * t4 + 1 of an 8-run stand at k = t4 and t4 + 4, in A and in B alike
-                const float* vp = reinterpret_cast<const float*>(ring + (run % C_::kStages) * C_::kStage + C_::kHalf);
-                uint32_t ph[2][4], pl[2][4];
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    split_tf32(sc[n][0], ph[n][0], pl[n][0]);
-                    split_tf32(sc[n][2], ph[n][1], pl[n][1]);
-                    split_tf32(sc[n][1], ph[n][2], pl[n][2]);
-                    split_tf32(sc[n][3], ph[n][3], pl[n][3]);
-                }
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int kk = 0; kk < 2; ++kk) {
-                        uint32_t bh[2], bl[2];
-#pragma unroll
-                        for (int j = 0; j < 2; ++j)
-                            split_tf32(vp[(kk * 8 + t4 * 2 + j) * (DP + 4) + n * 8 + g], bh[j], bl[j]);
-                        mma_tf32(o[n], pl[kk], bh[0], bh[1]);
-                        mma_tf32(o[n], ph[kk], bl[0], bl[1]);
-                        mma_tf32(o[n], ph[kk], bh[0], bh[1]);
-                    }
+                __syncwarp();   // the stage is free for the copies that the next round starts
             }
-            __syncwarp();   // the stage is free for the copies that the next round starts
-        }
-        cp_wait<0>();
-        if (__any_sync(0xffffffffu, bad) && lane == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
-
-        // ---- the warps meet ---------------------------------------------------------------------------------------
 #pragma unroll
-        for (int d = 1; d < 4; d <<= 1) {
-            l0 += __shfl_xor_sync(0xffffffffu, l0, d);
-            l1 += __shfl_xor_sync(0xffffffffu, l1, d);
-        }
-        __syncthreads();   // every ring is drained: the sums go over it
-        float* mg = reinterpret_cast<float*>(smem);
-        if (t4 == 0) {
-            wm[warp][g] = m0; wm[warp][g + 8] = m1;
-            wl[warp][g] = l0; wl[warp][g + 8] = l1;
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            float* p0 = mg + (warp * 16 + g) * (DP + 4) + n * 8 + t4 * 2;
-            if (g < rows) { p0[0] = o[n][0]; p0[1] = o[n][1]; }
-            if (g + 8 < rows) { p0[8 * (DP + 4)] = o[n][2]; p0[8 * (DP + 4) + 1] = o[n][3]; }
-        }
-        __syncthreads();
-        const bool complete = t0 == 0 && t1 == nt;
-        float* slot = complete ? nullptr : a.ws + (static_cast<long long>(blockIdx.x) * 2 + (x == x_first ? 0 : 1)) * C_::kSlot;
-        for (int i = tid; i < rows * a.dh; i += kThreads) {
-            const int r = i / a.dh, j = i % a.dh;
-            float M = wm[0][r];
-#pragma unroll
-            for (int w = 1; w < C_::kWarps; ++w) M = fmaxf(M, wm[w][r]);
-            const float base = M == -INFINITY ? 0.0f : M;
-            float L = 0.0f, v = 0.0f;
-#pragma unroll
-            for (int w = 0; w < C_::kWarps; ++w) {
-                const float f = exp2f(wm[w][r] - base);
-                L = fmaf(wl[w][r], f, L);
-                v = fmaf(mg[(w * 16 + r) * (DP + 4) + j], f, v);
+            for (int d = 1; d < 4; d <<= 1) {
+                l0 += __shfl_xor_sync(0xffffffffu, l0, d);
+                l1 += __shfl_xor_sync(0xffffffffu, l1, d);
             }
-            if (complete) {
-                const bool kept = head_kept(a, h0 + r);
-                write_head<T>(a, s, h0 + r, j, L != 0.0f && kept ? v / L : 0.0f);
-                if (j == 0 && a.lse)
-                    a.lse[static_cast<long long>(s) * a.H + h0 + r] =
-                        L != 0.0f && kept ? (M + log2f(L)) * 0.693147180559945309f : -INFINITY;
-            } else {
-                slot[32 + r * DP + j] = v;
-                if (j == 0) { slot[r] = M; slot[16 + r] = L; }
+            // the warps meet: common maxima and sums, then the weighted sums of warps 2 and 3 go to 0 and 1, of 1 to 0
+            if (t4 == 0) {
+                wm[warp][g] = m0; wm[warp][g + 8] = m1;
+                wl[warp][g] = l0; wl[warp][g + 8] = l1;
             }
-        }
-        if (a.dh != DP) {   // the sums were written over the padding
             __syncthreads();
-            for (int i = tid * 16; i < C_::kRing; i += kThreads * 16) *reinterpret_cast<uint4*>(smem + i) = make_uint4(0, 0, 0, 0);
+            float M[2], L[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int r = g + k * 8;
+                M[k] = wm[0][r];
+#pragma unroll
+                for (int w = 1; w < C_::kWarps; ++w) M[k] = fmaxf(M[k], wm[w][r]);
+                const float base = M[k] == -INFINITY ? 0.0f : M[k];
+                L[k] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < C_::kWarps; ++w) L[k] = fmaf(wl[w][r], exp2f(wm[w][r] - base), L[k]);
+                const float f = exp2f((k ? m1 : m0) - base);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) { o[n][2 * k] *= f; o[n][2 * k + 1] *= f; }
+            }
+            const auto put = [&](int b) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    if (g + k * 8 < rows) {
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            *reinterpret_cast<float2*>(mg + (b * rows + g + k * 8) * C_::kMergeRow + n * 8 + t4 * 2) =
+                                make_float2(o[n][2 * k], o[n][2 * k + 1]);
+                    }
+            };
+            const auto add = [&](int b) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    if (g + k * 8 < rows) {
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const float2 v = *reinterpret_cast<const float2*>(mg + (b * rows + g + k * 8) * C_::kMergeRow + n * 8 + t4 * 2);
+                            o[n][2 * k] += v.x;
+                            o[n][2 * k + 1] += v.y;
+                        }
+                    }
+            };
+            if (warp >= 2) put(warp - 2);
+            __syncthreads();
+            if (warp < 2) add(warp);
+            if (warp == 1) put(1);
+            __syncthreads();
+            if (warp == 0) {
+                add(1);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int r = g + k * 8;
+                    if (r >= rows) continue;
+                    if (complete) {
+                        const bool some = L[k] != 0.0f && head_kept(a, h0 + r);
+                        const long long row = static_cast<long long>(con.s) * a.H + h0 + r;
+                        const float f = some ? 1.0f / L[k] : 0.0f;
+                        uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + row * a.dh);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            if (n * 8 + t4 * 2 < a.dh) out[n * 4 + t4] = some ? pack_bf16(o[n][2 * k] * f, o[n][2 * k + 1] * f) : 0u;
+                        if (t4 == 0 && a.lse) a.lse[row] = some ? (M[k] + log2f(L[k])) * kLn2 : -INFINITY;
+                    } else {
+                        if (t4 == 0) { slot[r] = M[k]; slot[16 + r] = L[k]; }
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            *reinterpret_cast<float2*>(slot + kSlotHead + r * DP + n * 8 + t4 * 2) = make_float2(o[n][2 * k], o[n][2 * k + 1]);
+                    }
+                }
+            }
+        } else {
+            float* q = reinterpret_cast<float*>(ring + C_::kRing);
+            float* w = q + GR * DP;               // [GR][16]
+            __syncwarp();
+            for (int i = lane; i < GR * DP; i += 32) {
+                const int r = i / DP, c = i % DP;
+                q[i] = (r < rows && c < a.dh) ? __ldg(reinterpret_cast<const float*>(qrow) + static_cast<long long>(r) * a.dh + c) : 0.0f;
+            }
+            __syncwarp();
+            float o[GR][V], m[GR], l[GR];
+#pragma unroll
+            for (int r = 0; r < GR; ++r) {
+                m[r] = -INFINITY;
+                l[r] = 0.0f;
+#pragma unroll
+                for (int v = 0; v < V; ++v) o[r][v] = 0.0f;
+            }
+            for (int t = con.t0; t < con.t1; ++t) {
+                masks[S - 1] = issue();
+                cp_wait<S - 1>();
+                __syncwarp();
+                const uint32_t mask = masks[0];
+#pragma unroll
+                for (int i = 0; i + 1 < S; ++i) masks[i] = masks[i + 1];
+                const float* kp = reinterpret_cast<const float*>(ring + slot_out * C_::kStage);
+                const float* vp = kp + C_::kHalf / 4;
+                if (++slot_out == S) slot_out = 0;
+                if (mask == 0) continue;
+                // scores: lanes 2p and 2p + 1 take the even and the odd 16-byte chunks of position p
+                const int key = lane >> 1;
+                float sc[GR];
+#pragma unroll
+                for (int r = 0; r < GR; ++r) sc[r] = 0.0f;
+#pragma unroll 4
+                for (int i = lane & 1; i < DP / 4; i += 2) {
+                    const float4 kv = *reinterpret_cast<const float4*>(kp + key * (DP + 8) + i * 4);
+#pragma unroll
+                    for (int r = 0; r < GR; ++r) {
+                        const float4 qv = *reinterpret_cast<const float4*>(q + r * DP + i * 4);
+                        sc[r] = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, sc[r]))));
+                    }
+                }
+                float f[GR];
+                bool moved = false;
+#pragma unroll
+                for (int r = 0; r < GR; ++r) {
+                    const float full = sc[r] + __shfl_xor_sync(0xffffffffu, sc[r], 1);
+                    sc[r] = (mask >> key) & 1u ? full * a.scale_log2 : -INFINITY;
+                    float mx = fmaxf(m[r], sc[r]);
+#pragma unroll
+                    for (int d = 2; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+                    const float base = mx == -INFINITY ? 0.0f : mx;
+                    f[r] = exp2f(m[r] - base);
+                    moved |= m[r] != mx;
+                    m[r] = mx;
+                    const float e = exp2f(sc[r] - base);
+                    l[r] = fmaf(l[r], f[r], e);
+                    if ((lane & 1) == 0) w[r * kRun + key] = e;
+                }
+                __syncwarp();
+                if (moved) {   // the same in every lane
+#pragma unroll
+                    for (int r = 0; r < GR; ++r)
+#pragma unroll
+                        for (int v = 0; v < V; ++v) o[r][v] *= f[r];
+                }
+                // weighted sum of the values: columns lane * 2, or lane * 4 (and 128 more)
+#pragma unroll
+                for (int kk = 0; kk < kRun; kk += 4) {
+                    float vv[4][V];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float* row = vp + (kk + e) * (DP + 8);
+                        if constexpr (V == 2) {
+                            const float2 x = *reinterpret_cast<const float2*>(row + lane * 2);
+                            vv[e][0] = x.x; vv[e][1] = x.y;
+                        } else {
+#pragma unroll
+                            for (int b = 0; b < V / 4; ++b) {
+                                const float4 x = *reinterpret_cast<const float4*>(row + lane * 4 + b * 128);
+                                vv[e][b * 4] = x.x; vv[e][b * 4 + 1] = x.y; vv[e][b * 4 + 2] = x.z; vv[e][b * 4 + 3] = x.w;
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int r = 0; r < GR; ++r) {
+                        const float4 wv = *reinterpret_cast<const float4*>(w + r * kRun + kk);
+#pragma unroll
+                        for (int v = 0; v < V; ++v)
+                            o[r][v] = fmaf(wv.x, vv[0][v], fmaf(wv.y, vv[1][v], fmaf(wv.z, vv[2][v], fmaf(wv.w, vv[3][v], o[r][v]))));
+                    }
+                }
+                __syncwarp();   // the stage and the weights are free
+            }
+            // the warps meet, as above
+#pragma unroll
+            for (int r = 0; r < GR; ++r) {
+#pragma unroll
+                for (int d = 2; d < 32; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+                if (lane == 0) { wm[warp][r] = m[r]; wl[warp][r] = l[r]; }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < GR; ++r) {
+                float M = wm[0][r];
+#pragma unroll
+                for (int w2 = 1; w2 < C_::kWarps; ++w2) M = fmaxf(M, wm[w2][r]);
+                const float base = M == -INFINITY ? 0.0f : M;
+                l[r] = 0.0f;
+#pragma unroll
+                for (int w2 = 0; w2 < C_::kWarps; ++w2) l[r] = fmaf(wl[w2][r], exp2f(wm[w2][r] - base), l[r]);
+                const float f = exp2f(m[r] - base);
+                m[r] = M;
+#pragma unroll
+                for (int v = 0; v < V; ++v) o[r][v] *= f;
+            }
+            const auto at = [&](int r, int v) { return V == 2 ? lane * 2 + v : lane * 4 + (v & 3) + (v >> 2) * 128; };
+            const auto put = [&](int b) {
+#pragma unroll
+                for (int r = 0; r < GR; ++r)
+                    if (r < rows)
+#pragma unroll
+                        for (int v = 0; v < V; ++v) mg[(b * rows + r) * C_::kMergeRow + at(r, v)] = o[r][v];
+            };
+            const auto add = [&](int b) {
+#pragma unroll
+                for (int r = 0; r < GR; ++r)
+                    if (r < rows)
+#pragma unroll
+                        for (int v = 0; v < V; ++v) o[r][v] += mg[(b * rows + r) * C_::kMergeRow + at(r, v)];
+            };
+            constexpr int kB = C_::kWarps > 2 ? 1 : 0;
+            if (warp >= 2) put(warp - 2);
+            if (C_::kWarps > 2) __syncthreads();
+            if (warp + 2 < C_::kWarps) add(warp);
+            if (warp == 1) put(kB);
+            __syncthreads();
+            if (warp == 0) {
+                add(kB);
+#pragma unroll
+                for (int r = 0; r < GR; ++r) {
+                    if (r >= rows) continue;
+                    const bool some = l[r] != 0.0f && head_kept(a, h0 + r);
+                    const long long row = static_cast<long long>(con.s) * a.H + h0 + r;
+                    float* out = complete ? static_cast<float*>(a.out) + row * a.dh : slot + kSlotHead + r * DP;
+                    const float n = complete ? (some ? 1.0f / l[r] : 0.0f) : 1.0f;
+                    const bool zero = complete && !some;
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+                        if (at(r, v) < a.dh || !complete) out[at(r, v)] = zero ? 0.0f : o[r][v] * n;
+                    if (lane == 0) {
+                        if (!complete) {
+                            slot[r] = m[r];
+                            slot[16 + r] = l[r];
+                        } else if (a.lse) {
+                            a.lse[row] = some ? (m[r] + log2f(l[r])) * kLn2 : -INFINITY;
+                        }
+                    }
+                }
+            }
         }
-        __syncthreads();
-        // ---- next piece -------------------------------------------------------------------------------------------
-        x += t1 - t0;
-        if (x - start >= nt * items) {
-            start += nt * items;
-            ++s;
-        }
-        if (x < x_end && x == start && tid == 0) (void)valid_len(a, s, true);
+        if (!a.whole && tid == 0 && con.left == con.t1 - con.t0)   // the range's last piece
+            a.cuts[blockIdx.x] = {con.t0 == 0 && con.t1 < con.nt, con.s, con.hi, con.nt - con.t1, total, con.left == range, 0};
+        // a length out of range is reported where the sequence's first tile is
+        if (con.t0 == 0 && con.hi == 0 && tid == 0) (void)valid_len(a, con.s, true);
+        con.next(a);
     }
+    cp_wait<0>();
+    if (__any_sync(0xffffffffu, bad) && lane == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
 }
 
-// Joins the pieces of the items that were cut.  Block (c, r): the item that holds line position cut(c) strictly inside,
-// if thread block c - 1 of the first kernel is the one that began it; query head r of it.
-template <typename T, int DP>
-__global__ void __launch_bounds__(128) paged_mha_join_kernel(const __grid_constant__ PagedArgs a, int C) {
-    using C_ = Cfg<T, DP>;
-    __shared__ long long scan[128 / 32 + 3];
-    const int c = blockIdx.x + 1, r = blockIdx.y, tid = threadIdx.x;
-    const LinePos p = locate<C_::kTile, 128>(a, [&](long long T_) { return cut(T_, c, C); }, scan);
-    const long long x = cut(p.total, c, C);
+// Joins the pieces of the items that were cut.  Block (c, r): the item that range c begins and does not end, query head
+// r of it.  A group of DP threads (a column each) takes every kGroups-th piece; the first kAhead values of a thread are
+// requested together with the pieces' maxima and sums (one piece per thread), so that a join waits for memory twice: for
+// the record of the cut and for the pieces.
+template <typename T, int DP, int THREADS>
+__global__ void __launch_bounds__(THREADS) paged_mha_join_kernel(const __grid_constant__ PagedArgs a, int blocks) {
+    static_assert(THREADS % DP == 0 && DP % 32 == 0, "groups of whole warps");
+    constexpr int kGroups = THREADS / DP, kAhead = 16;
+    __shared__ float red[2][THREADS / 32];
+    __shared__ float part[kGroups > 1 ? THREADS : 1];
+    extern __shared__ float weight[];   // [pieces]
+    const int r = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c0 = blockIdx.x;
     asm volatile("griddepcontrol.wait;" ::: "memory");   // in every block: this grid may not end before the first one
-    const long long nt = tiles_of<C_::kTile>(a, p.s);
-    const int hi = static_cast<int>((x - p.start) / nt);
-    const long long first = p.start + hi * nt, end = first + nt;
-    const long long prev = cut(p.total, c - 1, C);
-    if (x == first || prev > first) return;   // not cut here / begun by an earlier thread block
+    const int4 cut_ = __ldcg(reinterpret_cast<const int4*>(a.cuts + c0));
+    const int4 line = __ldcg(reinterpret_cast<const int4*>(a.cuts + c0) + 1);
+    const long long total = __ldcg(&a.cuts[0].total);
+    const int C = ranges(total, blocks);
+    if (c0 + 1 >= C || !cut_.x) return;      // a block behind the last range reads a record that nobody wrote, and drops it
+    const int s = cut_.y, hi = cut_.z;
     const int kvh = hi / a.qblocks, r0 = (hi % a.qblocks) * 16;
     if (r >= min(16, a.G - r0)) return;
     const int h = kvh * a.G + r0 + r;
-    const float* head = a.ws + (static_cast<long long>(c - 1) * 2 + (prev == first ? 0 : 1)) * C_::kSlot;
-    // pieces: `head`, then slot 0 of thread blocks c, c + 1, ... as long as they begin inside the item
-    float M = __ldcg(head + r);
-    int last = c;
-    for (int k = c; k < C; ++k) {
-        const long long b = cut(p.total, k, C);
-        if (b >= end) break;
-        last = k + 1;
-        if (cut(p.total, k + 1, C) == b) continue;   // an empty range
-        M = fmaxf(M, __ldcg(a.ws + static_cast<long long>(k) * 2 * C_::kSlot + r));
+    // piece 0 in the slot of range c0 that holds its end (its first one if the item fills the range), the others in the
+    // first slots of the ranges behind it
+    const long long end = cut(total, c0 + 1, C);
+    const int pieces = range_of(total, end + cut_.w - 1, C) - c0 + 1;
+    const float* ws0 = a.ws + (static_cast<long long>(c0) * 2 + (line.z ? 0 : 1)) * a.slot;
+    const float* ws1 = a.ws + static_cast<long long>(c0) * 2 * a.slot;
+    const auto slot = [&](int k) { return k == 0 ? ws0 : ws1 + static_cast<long long>(k) * 2 * a.slot; };
+    const int grp = tid / DP, j = tid % DP;
+    const int at = kSlotHead + r * DP + j;
+
+    float ahead[kAhead];
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+        const int k = grp + e * kGroups;
+        ahead[e] = k < pieces ? __ldcg(slot(k) + at) : 0.0f;
     }
+    float M = -INFINITY, l_own = 0.0f;
+    for (int k = tid; k < pieces; k += THREADS) {
+        const float m = __ldcg(slot(k) + r);
+        if (k == tid) l_own = __ldcg(slot(k) + 16 + r);
+        weight[k] = m;
+        M = fmaxf(M, m);
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+    if (lane == 0) red[0][warp] = M;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) M = fmaxf(M, red[0][w]);
     const float base = M == -INFINITY ? 0.0f : M;
-    float f = exp2f(__ldcg(head + r) - base);
-    float L = __ldcg(head + 16 + r) * f;
-    float v[(DP + 127) / 128];
-#pragma unroll
-    for (int i = 0; i < (DP + 127) / 128; ++i) {
-        const int j = tid + i * 128;
-        v[i] = j < a.dh ? __ldcg(head + 32 + r * DP + j) * f : 0.0f;
+    float L = 0.0f;
+    for (int k = tid; k < pieces; k += THREADS) {
+        const float f = exp2f(weight[k] - base);
+        weight[k] = f;
+        L = fmaf(k == tid ? l_own : __ldcg(slot(k) + 16 + r), f, L);
     }
-#pragma unroll 4
-    for (int k = c; k < last; ++k) {
-        if (cut(p.total, k, C) == cut(p.total, k + 1, C)) continue;
-        const float* sl = a.ws + static_cast<long long>(k) * 2 * C_::kSlot;
-        f = exp2f(__ldcg(sl + r) - base);
-        L = fmaf(__ldcg(sl + 16 + r), f, L);
+    L = warp_sum(L);
+    if (lane == 0) red[1][warp] = L;
+    __syncthreads();
+    L = 0.0f;
 #pragma unroll
-        for (int i = 0; i < (DP + 127) / 128; ++i) {
-            const int j = tid + i * 128;
-            if (j < a.dh) v[i] = fmaf(__ldcg(sl + 32 + r * DP + j), f, v[i]);
+    for (int w = 0; w < THREADS / 32; ++w) L += red[1][w];
+    const bool some = L != 0.0f && head_kept(a, h);
+    float v = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+        const int k = grp + e * kGroups;
+        if (k < pieces) v = fmaf(ahead[e], weight[k], v);
+    }
+#pragma unroll 8
+    for (int k = grp + kAhead * kGroups; k < pieces; k += kGroups) v = fmaf(__ldcg(slot(k) + at), weight[k], v);
+    if constexpr (kGroups > 1) {
+        part[tid] = v;
+        __syncthreads();
+        if (grp == 0) {
+#pragma unroll
+            for (int e = 1; e < kGroups; ++e) v += part[tid + e * DP];
         }
     }
-    const bool some = L != 0.0f && head_kept(a, h);
-#pragma unroll
-    for (int i = 0; i < (DP + 127) / 128; ++i) {
-        const int j = tid + i * 128;
-        if (j < a.dh) write_head<T>(a, p.s, h, j, some ? v[i] / L : 0.0f);
-    }
-    if (tid == 0 && a.lse)
-        a.lse[static_cast<long long>(p.s) * a.H + h] = some ? (M + log2f(L)) * 0.693147180559945309f : -INFINITY;
+    if (grp == 0 && j < a.dh) write_head<T>(a, s, h, j, some ? v / L : 0.0f);
+    if (tid == 0 && a.lse) a.lse[static_cast<long long>(s) * a.H + h] = some ? (M + log2f(L)) * kLn2 : -INFINITY;
 }
 
-// Thread blocks of the first kernel, or 0 for one per item.
 struct LaunchPlan {
     int blocks, whole;
-    size_t slot_floats;
+    int slot, rows, merge;   // as in PagedArgs
+    long long items;
 };
-template <typename T, int DP>
+template <typename T, int DP, int GR>
 LaunchPlan plan_of(const halo_paged_shape& sh, int n_seq) {
-    using C_ = Cfg<T, DP>;
+    using C_ = Cfg<T, DP, GR>;
+    const int G = sh.n_heads / sh.n_kv_heads;
     const long long cap = static_cast<long long>(sh.max_pages) * sh.page_size;
     const long long tiles = (cap + C_::kTile - 1) / C_::kTile;
-    const long long items = static_cast<long long>(n_seq) * sh.n_kv_heads * ((sh.n_heads / sh.n_kv_heads + 15) / 16);
-    const long long resident = static_cast<long long>(kSmCount) * C_::kBlocksPerSm;
     LaunchPlan p;
-    p.slot_floats = C_::kSlot;
-    p.whole = tiles <= 2;
-    const long long want = tiles * items < resident ? tiles * items : resident;
-    p.blocks = static_cast<int>(p.whole ? items : want);
+    p.items = static_cast<long long>(n_seq) * sh.n_kv_heads * ((G + 15) / 16);
+    p.rows = G < 16 ? G : 16;
+    p.slot = kSlotHead + p.rows * DP;
+    p.merge = (C_::merge_bytes(p.rows) + 15) / 16 * 16;
+    const long long resident = static_cast<long long>(kSmCount) * C_::kBlocksPerSm;
+    // A thread block per item where the items are short and no thread block would get a second one.
+    p.whole = tiles <= 4 && p.items <= resident;
+    p.blocks = static_cast<int>(p.whole ? p.items : tiles * p.items < resident ? tiles * p.items : resident);
     return p;
 }
+size_t workspace_of(const LaunchPlan& p) {
+    return p.whole ? 0 : static_cast<size_t>(p.blocks) * (sizeof(Cut) + sizeof(float) * 2 * p.slot);
+}
 
-template <typename T, int DP>
-halo_status launch(const PagedArgs& args, const LaunchPlan& p, cudaStream_t st) {
-    using C_ = Cfg<T, DP>;
-    static bool done[64];
-    if (!ensure_dynamic_smem(paged_mha_kernel<T, DP>, C_::kSmem, done)) return HALO_ERR_CUDA;
-    PagedArgs a = args;
-    a.whole = p.whole;
-    paged_mha_kernel<T, DP><<<p.blocks, C_::kWarps * 32, C_::kSmem, st>>>(a);
-    HALO_CHECK_LAUNCH();
-    if (p.whole || p.blocks < 2) return HALO_OK;
+template <typename T, int DP, int THREADS>
+halo_status launch_join(const PagedArgs& a, const LaunchPlan& p, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(p.blocks - 1, a.G < 16 ? a.G : 16);
-    cfg.blockDim = dim3(128);
+    cfg.gridDim = dim3(p.blocks - 1, p.rows);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = sizeof(float) * p.blocks;
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cuda_status(cudaLaunchKernelEx(&cfg, paged_mha_join_kernel<T, DP>, a, p.blocks));
+    return cuda_status(cudaLaunchKernelEx(&cfg, paged_mha_join_kernel<T, DP, THREADS>, a, p.blocks));
 }
 
+template <typename T, int DP, int GR>
+halo_status launch(const PagedArgs& args, const LaunchPlan& p, cudaStream_t st) {
+    using C_ = Cfg<T, DP, GR>;
+    static bool done[64];
+    if (!ensure_dynamic_smem(paged_mha_kernel<T, DP, GR>, C_::kMaxSmem, done)) return HALO_ERR_CUDA;
+    PagedArgs a = args;
+    a.whole = p.whole;
+    a.slot = p.slot;
+    a.rows = p.rows;
+    a.merge = p.merge;
+    paged_mha_kernel<T, DP, GR><<<p.blocks, C_::kWarps * 32, C_::kRings + p.merge, st>>>(a);
+    HALO_CHECK_LAUNCH();
+    if (p.whole || p.blocks < 2) return HALO_OK;
+    // few items, many pieces each: several groups of threads
+    constexpr int kWide = DP == 256 ? 512 : 256;
+    return p.blocks >= 8 * p.items ? launch_join<T, DP, kWide>(a, p, st) : launch_join<T, DP, DP>(a, p, st);
+}
+
+template <typename T, int DP, typename F>
+auto by_rows(const halo_paged_shape& sh, F f) {
+    using D = std::integral_constant<int, DP>;
+    if constexpr (sizeof(T) == 2) {
+        return f(T(), D(), std::integral_constant<int, 16>());
+    } else {
+        const int G = sh.n_heads / sh.n_kv_heads;
+        if (G == 1) return f(T(), D(), std::integral_constant<int, 1>());
+        if (G <= 4) return f(T(), D(), std::integral_constant<int, 4>());
+        return f(T(), D(), std::integral_constant<int, 16>());
+    }
+}
 template <typename F>
 auto by_type(const halo_paged_shape& sh, F f) {
-    const int dp = sh.head_dim <= 64 ? 64 : sh.head_dim <= 128 ? 128 : 256;
-    if (sh.dtype == HALO_BF16) {
-        if (dp == 64) return f(__nv_bfloat16(), std::integral_constant<int, 64>());
-        if (dp == 128) return f(__nv_bfloat16(), std::integral_constant<int, 128>());
-        return f(__nv_bfloat16(), std::integral_constant<int, 256>());
-    }
-    if (dp == 64) return f(float(), std::integral_constant<int, 64>());
-    if (dp == 128) return f(float(), std::integral_constant<int, 128>());
-    return f(float(), std::integral_constant<int, 256>());
+    using H = __nv_bfloat16;
+    if (sh.dtype == HALO_BF16)
+        return sh.head_dim <= 64 ? by_rows<H, 64>(sh, f) : sh.head_dim <= 128 ? by_rows<H, 128>(sh, f) : by_rows<H, 256>(sh, f);
+    return sh.head_dim <= 64 ? by_rows<float, 64>(sh, f) : sh.head_dim <= 128 ? by_rows<float, 128>(sh, f) : by_rows<float, 256>(sh, f);
 }
 
 LaunchPlan plan_for(const halo_paged_shape& sh, int n_seq) {
-    return by_type(sh, [&](auto t, auto dp) { return plan_of<decltype(t), decltype(dp)::value>(sh, n_seq); });
+    return by_type(sh, [&](auto t, auto dp, auto gr) { return plan_of<decltype(t), decltype(dp)::value, decltype(gr)::value>(sh, n_seq); });
 }
 
 }  // namespace
@@ -644,8 +863,7 @@ using namespace halo;
 
 extern "C" size_t halo_paged_mha_workspace_bytes(const halo_paged_shape* shape, int n_seq) {
     if (check_paged_shape(shape) != HALO_OK || n_seq <= 0 || n_seq > HALO_MAX_SEQUENCES) return 0;
-    const LaunchPlan p = plan_for(*shape, n_seq);
-    return p.whole || p.blocks < 2 ? 0 : sizeof(float) * 2 * p.slot_floats * static_cast<size_t>(p.blocks);
+    return workspace_of(plan_for(*shape, n_seq));
 }
 
 extern "C" halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, const void* q, long long q_stride,
@@ -673,6 +891,9 @@ extern "C" halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, 
     a.qblocks = (a.G + kMaxSplitRows - 1) / kMaxSplitRows;
     a.dh = shape->head_dim;
     a.page_size = shape->page_size;
+    a.page_shift = -1;
+    for (int b = 0; b < 31; ++b)
+        if (shape->page_size == 1 << b) a.page_shift = b;
     a.n_pages = shape->n_pages;
     a.max_pages = shape->max_pages;
     a.page_stride = paged_stride(*shape);
@@ -686,10 +907,11 @@ extern "C" halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, 
     a.keep = keep;
     a.out = out;
     a.lse = lse;
-    a.ws = static_cast<float*>(workspace);
     a.status = dev_status;
     const LaunchPlan p = plan_for(*shape, n_seq);
-    return by_type(*shape, [&](auto t, auto dp) {
-        return launch<decltype(t), decltype(dp)::value>(a, p, static_cast<cudaStream_t>(stream));
+    a.cuts = static_cast<Cut*>(workspace);
+    a.ws = reinterpret_cast<float*>(a.cuts + p.blocks);
+    return by_type(*shape, [&](auto t, auto dp, auto gr) {
+        return launch<decltype(t), decltype(dp)::value, decltype(gr)::value>(a, p, static_cast<cudaStream_t>(stream));
     });
 }
