@@ -456,94 +456,38 @@ def halo_group_ffn_i4(shape: FfnShape, Q, scales, x, n_tok, keep_list, n_keep, d
 
 
 # ---- batched token step: paged cache, residual between blocks, microscaled 4-bit rows -------------------------------
-# These calls check what they are given against the shape (sizes, element types, one device) before they pass pointers
-# on, and run on the device of their tensors whichever device is current.
+# These calls compare what they are given with the shape (sizes, element types, strides, one device; ValueError) before an
+# address is passed on, and run on the device of their tensors whichever device is current.  The comparison and the
+# marshalling are native (csrc_py/marshal.cpp): in Python they took longer than the smallest kernels.
 
-_DTYPES = (torch.float32, torch.bfloat16)
-
-
-def _need(cond: bool, what: str, why: str) -> None:
-    if not cond:
-        raise ValueError(f"{what}: {why}")
+_native = None
 
 
-def _tensor(t, what, name, dtype, numel, dev, exact=True):
-    """Address of a dense tensor of `dtype` on device `dev` with (at least, if not exact) `numel` elements; None stays."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.device != dev or not t.is_contiguous() or (t.numel() != numel if exact else t.numel() < numel):
-        raise ValueError(f"{what}: {name} has to be a contiguous {dtype} tensor of {'' if exact else 'at least '}{numel} "
-                         f"elements on {dev}; got {t.dtype}, {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
-    return t.data_ptr()
-
-
-def _rows(t, what, name, dtype, n, width, dev):
-    """(address, row stride) of n rows of `width` elements that are dense in themselves: [n][width] or [n][a][b]."""
-    shape, stride = t.shape, t.stride()
-    ok = t.dtype is dtype and t.device == dev and len(shape) in (2, 3) and shape[0] == n and stride[-1] == 1
-    if ok:
-        ok = shape[1] == width if len(shape) == 2 else (shape[1] * shape[2] == width and stride[1] == shape[2])
-    if not ok:
-        raise ValueError(f"{what}: {name} has to be {n} rows of {width} {dtype} elements, dense within a row, on {dev}; got "
-                         f"{t.dtype}, {tuple(shape)}, strides {stride}, on {t.device}")
-    return t.data_ptr(), max(stride[0], width)
-
-
-def _run(what, dev, stream, fn, *args) -> None:
-    _need(dev.type == "cuda", what, "tensors have to be on a GPU")
-    if dev.index == torch.cuda.current_device():
-        code = fn(*args, (stream or torch.cuda.current_stream()).cuda_stream)
-    else:
-        with torch.cuda.device(dev):
-            code = fn(*args, (stream or torch.cuda.current_stream()).cuda_stream)
-    if code != 0:
-        raise HaloError(code, what)
+def _marshal():
+    """The _marshal module, bound to this library's entry points."""
+    global _native
+    if _native is None:
+        L = lib()
+        from . import _marshal as m
+        names = ("halo_paged_kv_append", "halo_paged_mha", "halo_norm_glue", "halo_quantize_rows_mx4", "halo_dequantize_rows_mx4",
+                 "halo_product_mx4")
+        m.bind(*(ctypes.cast(getattr(L, n), c_void_p).value for n in names))
+        _native = m
+    return _native
 
 
 def paged_shape(n_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, dtype, page_stride=0) -> PagedShape:
     return PagedShape(n_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, page_stride, dtype)
 
 
-def _caches(shape: PagedShape, what, K_cache, V_cache, dev):
-    """Addresses of the caches: dense tensors, or (page_stride != 0) views whose first axis has that stride."""
-    dt = _DTYPES[shape.dtype]
-    dense = shape.n_kv_heads * shape.page_size * shape.head_dim
-    out = []
-    for name, t in (("K_cache", K_cache), ("V_cache", V_cache)):
-        ok = t.dtype is dt and t.device == dev
-        if ok and (shape.page_stride == 0 or shape.page_stride == dense):
-            ok = t.is_contiguous() and t.numel() == shape.n_pages * dense
-        elif ok:
-            ok = t.shape[0] == shape.n_pages and t[0].is_contiguous() and t[0].numel() == dense and \
-                (shape.n_pages == 1 or t.stride(0) == shape.page_stride)
-        _need(ok, what, f"{name} does not fit the shape: {t.dtype}, {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
-        out.append(t.data_ptr())
-    return out
-
-
 def halo_paged_kv_append(shape: PagedShape, q, k, v, pos, seq_of_tok, block_table, inv_freq, interleaved, q_out, K_cache,
                          V_cache, dev_status=None, stream=None) -> None:
     """q, k, v, q_out: [n_tok][heads * head_dim] or [n_tok][heads][head_dim], rows may be strided; q and q_out may both be
     None.  seq_of_tok None: token t is sequence t.  inv_freq (float64) of rotary_dim / 2 elements or None."""
-    what = "halo_paged_kv_append"
-    _need(0 <= shape.dtype < 2, what, "unknown element type in the shape")
-    dt, dev = _DTYPES[shape.dtype], k.device
-    n_tok, n_seq = k.shape[0], block_table.shape[0]
-    kp, ks = _rows(k, what, "k", dt, n_tok, shape.n_kv_heads * shape.head_dim, dev)
-    vp, vs = _rows(v, what, "v", dt, n_tok, shape.n_kv_heads * shape.head_dim, dev)
-    qp = qs = op = os_ = None
-    if q is not None or q_out is not None:
-        _need(q is not None and q_out is not None, what, "q and q_out go together")
-        qp, qs = _rows(q, what, "q", dt, n_tok, shape.n_heads * shape.head_dim, dev)
-        op, os_ = _rows(q_out, what, "q_out", dt, n_tok, shape.n_heads * shape.head_dim, dev)
-    Kp, Vp = _caches(shape, what, K_cache, V_cache, dev)
-    i32 = torch.int32
-    _run(what, dev, stream, lib().halo_paged_kv_append, byref(shape), n_tok, n_seq, qp, qs or 0, kp, ks, vp, vs,
-         _tensor(pos, what, "pos", i32, n_tok, dev), _tensor(seq_of_tok, what, "seq_of_tok", i32, n_tok, dev),
-         _tensor(block_table, what, "block_table", i32, n_seq * shape.max_pages, dev),
-         _tensor(inv_freq, what, "inv_freq", torch.float64, 0, dev, exact=False),
-         0 if inv_freq is None else 2 * inv_freq.numel(), int(bool(interleaved)), op, os_ or 0, Kp, Vp,
-         _tensor(dev_status, what, "dev_status", i32, 1, dev, exact=False))
+    code = (_native or _marshal()).kv_append(shape, q, k, v, pos, seq_of_tok, block_table, inv_freq, interleaved, q_out, K_cache,
+                                             V_cache, dev_status, stream)
+    if code:
+        raise HaloError(code, "halo_paged_kv_append")
 
 
 def halo_paged_mha_workspace_bytes(shape: PagedShape, n_seq: int) -> int:
@@ -554,20 +498,10 @@ def halo_paged_mha(shape: PagedShape, q, K_cache, V_cache, block_table, seq_len,
                    dev_status=None, stream=None) -> None:
     """q: [n_seq][n_heads * head_dim] or [n_seq][n_heads][head_dim], rows may be strided; workspace: uint8 tensor of
     halo_paged_mha_workspace_bytes (None where that is 0)."""
-    what = "halo_paged_mha"
-    _need(0 <= shape.dtype < 2, what, "unknown element type in the shape")
-    dt, dev, n_seq = _DTYPES[shape.dtype], q.device, q.shape[0]
-    qp, qs = _rows(q, what, "q", dt, n_seq, shape.n_heads * shape.head_dim, dev)
-    Kp, Vp = _caches(shape, what, K_cache, V_cache, dev)
-    i32 = torch.int32
-    _run(what, dev, stream, lib().halo_paged_mha, byref(shape), n_seq, qp, qs, Kp, Vp,
-         _tensor(block_table, what, "block_table", i32, n_seq * shape.max_pages, dev),
-         _tensor(seq_len, what, "seq_len", i32, n_seq, dev), _tensor(keep, what, "keep", torch.uint8, shape.n_heads, dev),
-         scale, _tensor(out, what, "out", dt, n_seq * shape.n_heads * shape.head_dim, dev),
-         _tensor(lse, what, "lse", torch.float32, n_seq * shape.n_heads, dev),
-         _tensor(workspace, what, "workspace", torch.uint8, 0, dev, exact=False),
-         0 if workspace is None else workspace.numel(),
-         _tensor(dev_status, what, "dev_status", i32, 1, dev, exact=False))
+    code = (_native or _marshal()).paged_mha(shape, q, K_cache, V_cache, block_table, seq_len, scale, out, workspace, keep, lse,
+                                             dev_status, stream)
+    if code:
+        raise HaloError(code, "halo_paged_mha")
 
 
 def norm_shape(d_model, eps, ydtype, xdtype) -> NormShape:
@@ -577,58 +511,33 @@ def norm_shape(d_model, eps, ydtype, xdtype) -> NormShape:
 def halo_norm_glue(shape: NormShape, h, y, w_post, gate, res_scale, w_pre, h_out, x_out, stream=None) -> None:
     """gate: [n_tok][d], rows may be strided, or [d] / [1][d] (one row for all tokens); y, w_post, gate, w_pre may be
     None."""
-    what = "halo_norm_glue"
-    _need(0 <= shape.ydtype < 2 and 0 <= shape.xdtype < 2, what, "unknown element type in the shape")
-    dev, d, xt = h.device, shape.d_model, _DTYPES[shape.xdtype]
-    n_tok = h.numel() // max(d, 1)
-    gp, gs = None, 0
-    if gate is not None:
-        if gate.numel() == d and (gate.dim() == 1 or n_tok > 1):
-            gp = _tensor(gate, what, "gate", xt, d, dev)
-        else:
-            gp, gs = _rows(gate, what, "gate", xt, n_tok, d, dev)
-    _run(what, dev, stream, lib().halo_norm_glue, byref(shape), n_tok, _tensor(h, what, "h", torch.float32, n_tok * d, dev),
-         _tensor(y, what, "y", _DTYPES[shape.ydtype], n_tok * d, dev), _tensor(w_post, what, "w_post", xt, d, dev), gp, gs,
-         res_scale, _tensor(w_pre, what, "w_pre", xt, d, dev),
-         _tensor(h_out, what, "h_out", torch.float32, n_tok * d, dev), _tensor(x_out, what, "x_out", xt, n_tok * d, dev))
+    code = (_native or _marshal()).norm_glue(shape, h, y, w_post, gate, res_scale, w_pre, h_out, x_out, stream)
+    if code:
+        raise HaloError(code, "halo_norm_glue")
 
 
 def halo_mx4_scale_bytes(d_model: int, n_rows: int) -> int:
     return int(lib().halo_mx4_scale_bytes(d_model, n_rows))
 
 
-def _mx4(what, d_model, n_rows, Q, scales, dev):
-    _need(d_model > 0 and d_model % 128 == 0, what, "d_model has to be a positive multiple of 128")
-    return (_tensor(Q, what, "Q", torch.uint8, n_rows * (d_model // 2), dev),
-            _tensor(scales, what, "scales", torch.uint8, -(-n_rows // 128) * (d_model // 128) * 512, dev, exact=False))
-
-
 def halo_quantize_rows_mx4(d_model: int, n_rows: int, wdtype: int, W, Q, scales, stream=None) -> None:
-    what, dev = "halo_quantize_rows_mx4", W.device
-    _need(0 <= wdtype < 2, what, "unknown element type")
-    Qp, Sp = _mx4(what, d_model, n_rows, Q, scales, dev)
-    _run(what, dev, stream, lib().halo_quantize_rows_mx4, d_model, n_rows, wdtype,
-         _tensor(W, what, "W", _DTYPES[wdtype], n_rows * d_model, dev), Qp, Sp)
+    code = (_native or _marshal()).quantize_rows_mx4(d_model, n_rows, wdtype, W, Q, scales, stream)
+    if code:
+        raise HaloError(code, "halo_quantize_rows_mx4")
 
 
 def halo_dequantize_rows_mx4(d_model: int, n_rows: int, wdtype: int, Q, scales, W, stream=None) -> None:
-    what, dev = "halo_dequantize_rows_mx4", W.device
-    _need(0 <= wdtype < 2, what, "unknown element type")
-    Qp, Sp = _mx4(what, d_model, n_rows, Q, scales, dev)
-    _run(what, dev, stream, lib().halo_dequantize_rows_mx4, d_model, n_rows, wdtype, Qp, Sp,
-         _tensor(W, what, "W", _DTYPES[wdtype], n_rows * d_model, dev))
+    code = (_native or _marshal()).dequantize_rows_mx4(d_model, n_rows, wdtype, W, Q, scales, stream)
+    if code:
+        raise HaloError(code, "halo_dequantize_rows_mx4")
 
 
 def halo_product_mx4(d_model: int, n_tok: int, n_rows: int, Qx, Sx, Qw, Sw, ydtype: int, y, dev_status=None,
                      stream=None) -> None:
     """y[t][r] = <x_t, w_r> of quantised rows (Qx, Sx: n_tok of them; Qw, Sw: n_rows)."""
-    what, dev = "halo_product_mx4", y.device
-    _need(0 <= ydtype < 2, what, "unknown element type")
-    Qxp, Sxp = _mx4(what, d_model, n_tok, Qx, Sx, dev)
-    Qwp, Swp = _mx4(what, d_model, n_rows, Qw, Sw, dev)
-    _run(what, dev, stream, lib().halo_product_mx4, d_model, n_tok, n_rows, Qxp, Sxp, Qwp, Swp, ydtype,
-         _tensor(y, what, "y", _DTYPES[ydtype], n_tok * n_rows, dev),
-         _tensor(dev_status, what, "dev_status", torch.int32, 1, dev, exact=False))
+    code = (_native or _marshal()).product_mx4(d_model, n_tok, n_rows, Qx, Sx, Qw, Sw, ydtype, y, dev_status, stream)
+    if code:
+        raise HaloError(code, "halo_product_mx4")
 
 
 def halo_selftest_bounded_wait(never_set_flag, limit_cycles, report, dev_status, stream=None) -> None:

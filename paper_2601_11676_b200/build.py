@@ -1,4 +1,5 @@
-"""Builds libhalo.so (CUDA, sm_100a) in-tree with nvcc.  `python -m paper_2601_11676_b200.build [--force] [-v]`."""
+"""Builds libhalo.so (CUDA, sm_100a, nvcc) and _marshal.so (argument marshalling, g++ against torch's headers) in-tree.
+`python -m paper_2601_11676_b200.build [--force] [-v]`."""
 from __future__ import annotations
 
 import os
@@ -11,6 +12,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libhalo.so")
+MARSHAL_SRC = os.path.join(PKG, "csrc_py", "marshal.cpp")
+MARSHAL = os.path.join(PKG, "_marshal.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -33,6 +36,35 @@ def _deps_mtime() -> float:
     hdrs = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))]
     hdrs.append(os.path.join(ROOT, "include", "halo.h"))
     return max(os.path.getmtime(p) for p in hdrs)
+
+
+def build_marshal(force: bool = False) -> str:
+    """_marshal.so; rebuilt when its source, halo.h or the torch it was built against changed."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    stamp = os.path.join(OBJ, "marshal.torch")
+    made_with = f"{torch.__version__} {torch.__file__} {sys.version}"
+    newest = max(os.path.getmtime(p) for p in (MARSHAL_SRC, os.path.join(ROOT, "include", "halo.h")))
+    fresh = os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= newest and os.path.exists(stamp) and \
+        open(stamp).read() == made_with
+    if fresh and not force:
+        return MARSHAL
+    lib_dir = os.path.join(os.path.dirname(torch.__file__), "lib")
+    includes = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], "/usr/local/cuda/include",
+                                                os.path.join(ROOT, "include")]
+    tmp = MARSHAL + f".tmp{os.getpid()}"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *(f"-I{p}" for p in includes), MARSHAL_SRC, "-o", tmp, f"-L{lib_dir}", f"-Wl,-rpath,{lib_dir}", "-lc10", "-lc10_cuda",
+           "-ltorch_cpu", "-ltorch", "-ltorch_python"]
+    p = subprocess.run(cmd, capture_output=True, text=True)
+    if p.returncode != 0:
+        raise RuntimeError("g++ failed: " + " ".join(cmd) + "\n" + p.stdout + p.stderr)
+    os.replace(tmp, MARSHAL)
+    with open(stamp, "w") as f:
+        f.write(made_with)
+    return MARSHAL
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -63,6 +95,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         tmp = LIB + f".tmp{os.getpid()}"
         run([_nvcc(), "-shared", "-o", tmp, *objs, "-lcudart"])
         os.replace(tmp, LIB)
+    build_marshal(force)
     return LIB
 
 
