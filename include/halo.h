@@ -424,7 +424,7 @@ halo_status halo_group_lm_head_i4(const halo_lm_shape* shape, const void* Q, con
  *   q, q_out device [n_tok] rows of n_heads * head_dim; k, v rows of n_kv_heads * head_dim; rows every *_stride elements
  *     (a whole number of 16 bytes), so that they may lie side by side in one projection's output.  q_out may be q.
  *     q and q_out NULL: keys and values only.
- *   pos device int32 [n_tok]; a negative position marks a padding row: nothing of it is read or written.
+ *   pos device int32 [n_tok]; a negative position marks a padding row: nothing is written for it.
  *   seq_of_tok device int32 [n_tok], or NULL: token t belongs to sequence t (n_tok <= n_seq).
  *   inv_freq device double [rotary_dim / 2]: pair i is turned by the angle pos * inv_freq[i] (formed in fp64, so far
  *     positions keep their angle).  Pairs are (2i, 2i + 1) if interleaved != 0, else (i, i + rotary_dim / 2);

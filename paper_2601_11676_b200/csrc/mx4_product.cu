@@ -7,7 +7,9 @@
 // by bulk copies, moved on to TMEM by tcgen05.cp in front of the products that use them.  Every stage of the ring has
 // its own columns of scales: a stage is refilled only when the products that read its old scales have completed.
 //
-// Two kernels:
+// Three kernels:
+//   mx4_one_kernel   one token, bound by HBM: integer products (a 4-bit value is a whole number of halves) on the
+//     ordinary pipe, described at the kernel.
 //   mx4_line_kernel  few tokens, bound by HBM (0.53 bytes per weight element): the weight rows in groups of 32 form a
 //     line (one per tile of tokens) that is cut into equal pieces, one thread block per SM; whole outputs per thread
 //     block, so nothing has to be added up between thread blocks.
@@ -58,6 +60,104 @@ __device__ __forceinline__ uint64_t scales_desc(uint32_t smem) {
 }
 __device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint64_t desc) {
     asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
+// ---- one token -----------------------------------------------------------------------------------------------------
+// Twice a 4-bit value is a whole number of at most 12, so a run of 32 elements is an exact integer product: the byte
+// permute picks four magnitudes at a time from an eight-byte table with the codes themselves as selectors; a selector's
+// top bit (the code's sign) gives 0 instead, so one pass with the codes and one with their signs turned sum the positive
+// and the negative weights (11 instructions for 8 elements).  The integer of a run meets both its scales in fp32.  The
+// token sits in shared memory as bytes; a warp takes kRows rows at once, a lane the runs lane, lane + 32, ... of them,
+// with kAhead 16-byte loads per row in flight.  A thread block's rows are neighbours: they share the lines of the scale
+// blocks.
+constexpr int kOneThreads = 256;
+constexpr size_t kOneSmem = 74 * 1024;   // the widest row
+// bytes of {high, low} by the four lower nibbles of sel; a nibble of 8 or more gives the sign of its byte, 0 in this table
+__device__ __forceinline__ uint32_t permute(uint32_t low, uint32_t high, uint32_t sel) {
+    uint32_t r;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(low), "r"(high), "r"(sel));
+    return r;
+}
+__device__ __forceinline__ float power(uint32_t byte) {   // 2^(byte - 127); 255 is NaN
+    return __uint_as_float(byte == 0 ? 0x00400000u : byte == 255u ? 0x7fc00000u : byte << 23);
+}
+template <typename T>
+__global__ void __launch_bounds__(kOneThreads, 3)
+mx4_one_kernel(int d, int n_rows, const uint8_t* __restrict__ Qx, const uint8_t* __restrict__ Sx,
+               const uint8_t* __restrict__ Qw, const uint8_t* __restrict__ Sw, T* __restrict__ y) {
+    constexpr int kRows = 2, kAhead = 4, kWarps = kOneThreads / 32;
+    constexpr uint32_t kLow = 0x03020100u, kHigh = 0x0C080604u;   // twice 0, 0.5, 1, 1.5 and 2, 3, 4, 6
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int runs = d / 32;                       // of a row
+    // [half of a run][run] 16 bytes, then [run] a quarter of the token's scale
+    uint4* xs = reinterpret_cast<uint4*>(smem);
+    float* sx = reinterpret_cast<float*>(xs + 2 * runs);
+    for (int b = tid; b < runs; b += kOneThreads) {
+        const uint4 code = *reinterpret_cast<const uint4*>(Qx + b * 16);
+        const uint32_t word[4] = {code.x, code.y, code.z, code.w};
+        uint32_t out[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t sel = word[k >> 1] >> ((k & 1) * 16);
+            out[k] = __vsub4(permute(kLow, kHigh, sel), permute(kLow, kHigh, sel ^ 0x8888u));
+        }
+        xs[b] = make_uint4(out[0], out[1], out[2], out[3]);
+        xs[runs + b] = make_uint4(out[4], out[5], out[6], out[7]);
+        sx[b] = 0.25f * power(Sx[(b >> 2) * 512 + (b & 3)]);
+    }
+    __syncthreads();
+    const int first = static_cast<int>(static_cast<long long>(n_rows) * blockIdx.x / gridDim.x);
+    const int end = static_cast<int>(static_cast<long long>(n_rows) * (blockIdx.x + 1) / gridDim.x);
+    for (int r0 = first + warp * kRows; r0 < end; r0 += kWarps * kRows) {
+        const uint8_t* q[kRows];
+        const uint8_t* sc[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const int row = min(r0 + r, end - 1);
+            q[r] = Qw + static_cast<size_t>(row) * (d / 2);
+            sc[r] = Sw + static_cast<size_t>(row >> 7) * (d >> 7) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4;
+        }
+        float sum[kRows] = {};
+        for (int b0 = 0; b0 < runs; b0 += 32 * kAhead) {
+            uint4 code[kAhead][kRows];
+            uint32_t scale[kAhead][kRows];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) {
+                    const int b = b0 + i * 32 + lane;
+                    code[i][r] = b < runs ? ldg_stream16(q[r] + b * 16) : make_uint4(0, 0, 0, 0);
+                    scale[i][r] = b < runs ? __ldg(sc[r] + (b >> 2) * 512 + (b & 3)) : 0u;
+                }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int b = b0 + i * 32 + lane;
+                if (b >= runs) break;
+                const uint4 x0 = xs[b], x1 = xs[runs + b];
+                const uint32_t x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) {
+                    const uint32_t word[4] = {code[i][r].x, code[i][r].y, code[i][r].z, code[i][r].w};
+                    int up = 0, down = 0;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const uint32_t sel = word[k >> 1] >> ((k & 1) * 16);
+                        const uint32_t turned = (word[k >> 1] ^ 0x88888888u) >> ((k & 1) * 16);
+                        up = __dp4a(static_cast<int>(permute(kLow, kHigh, sel)), static_cast<int>(x[k]), up);
+                        down = __dp4a(static_cast<int>(permute(kLow, kHigh, turned)), static_cast<int>(x[k]), down);
+                    }
+                    // integer x scale of x first: exact, and 0 stays 0 before a scale of 2^127
+                    sum[r] = fmaf(static_cast<float>(up - down) * sx[b], power(scale[i][r]), sum[r]);
+                }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const float v = warp_sum(sum[r]);
+            if (lane == 0 && r0 + r < end) y[r0 + r] = from_float<T>(v);
+        }
+    }
 }
 
 template <int NT, int STAGES>
@@ -533,6 +633,19 @@ struct Operands {
     cudaStream_t st;
 };
 
+template <typename T>
+halo_status launch_one(const Operands& o, T* y) {
+    static bool done[64];
+    if (!ensure_dynamic_smem(mx4_one_kernel<T>, kOneSmem, done)) return HALO_ERR_CUDA;
+    static_assert(HALO_MX4_MAX_WIDTH + HALO_MX4_MAX_WIDTH / 8 <= kOneSmem, "the widest row fits");
+    const int most = 3 * kSmCount, want = (o.n_rows + 15) / 16;   // a pair of rows per warp at least
+    mx4_one_kernel<T><<<want < most ? want : most, kOneThreads, o.d + o.d / 8, o.st>>>(
+        o.d, o.n_rows, static_cast<const uint8_t*>(o.Qx), static_cast<const uint8_t*>(o.Sx), static_cast<const uint8_t*>(o.Qw),
+        static_cast<const uint8_t*>(o.Sw), y);
+    HALO_CHECK_LAUNCH();
+    return HALO_OK;
+}
+
 template <typename T, int NT, int STAGES>
 halo_status launch_line(const Operands& o, int grain, T* y) {
     using R = Ring<NT, STAGES>;
@@ -581,6 +694,7 @@ halo_status launch_pair(const Operands& o, T* y) {
 template <typename T>
 halo_status by_tokens(const Operands& o, void* y) {
     T* out = static_cast<T*>(y);
+    if (o.n_tok == 1) return launch_one<T>(o, out);
     if (o.n_tok <= 16) return launch_line<T, 16, 10>(o, 1, out);
     if (o.n_tok <= 64) return launch_line<T, 64, 8>(o, 1, out);
     if (o.n_tok <= 128) return launch_line<T, 128, 6>(o, 4, out);

@@ -20,14 +20,39 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// 8 elements as they lie in memory; widened only when they are used, so that several are in flight
+template <typename T> struct Raw { uint4 w[sizeof(T) / 2]; };
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
+__device__ __forceinline__ Raw<T> fetch8(const T* p) {
+    Raw<T> r;
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) r.w[i] = ldg_stream16(reinterpret_cast<const uint4*>(p) + i);
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void widen8(const Raw<T>& r, float (&f)[8]) {
     if constexpr (sizeof(T) == 4) {
-        const uint4 a = ldg_stream16(p), b = ldg_stream16(p + 4);
-        f[0] = __uint_as_float(a.x); f[1] = __uint_as_float(a.y); f[2] = __uint_as_float(a.z); f[3] = __uint_as_float(a.w);
-        f[4] = __uint_as_float(b.x); f[5] = __uint_as_float(b.y); f[6] = __uint_as_float(b.z); f[7] = __uint_as_float(b.w);
+        f[0] = __uint_as_float(r.w[0].x); f[1] = __uint_as_float(r.w[0].y);
+        f[2] = __uint_as_float(r.w[0].z); f[3] = __uint_as_float(r.w[0].w);
+        f[4] = __uint_as_float(r.w[1].x); f[5] = __uint_as_float(r.w[1].y);
+        f[6] = __uint_as_float(r.w[1].z); f[7] = __uint_as_float(r.w[1].w);
     } else {
-        Elem<__nv_bfloat16>::widen(ldg_stream16(p), f);
+        Elem<__nv_bfloat16>::widen(r.w[0], f);
+    }
+}
+// bits of the largest magnitude as fp32; a NaN counts as one
+template <typename T>
+__device__ __forceinline__ uint32_t top8(const Raw<T>& r) {
+    if constexpr (sizeof(T) == 4) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            top = max(top, max(max(r.w[i].x & 0x7fffffffu, r.w[i].y & 0x7fffffffu), max(r.w[i].z & 0x7fffffffu, r.w[i].w & 0x7fffffffu)));
+        return top;
+    } else {
+        const uint32_t m = 0x7fff7fffu;
+        const uint32_t two = __vmaxu2(__vmaxu2(r.w[0].x & m, r.w[0].y & m), __vmaxu2(r.w[0].z & m, r.w[0].w & m));
+        return max(two << 16, two & 0xffff0000u);
     }
 }
 // two values -> two codes in a byte, the first in the low half (round to nearest even, 6 at most)
@@ -57,25 +82,26 @@ quantize_mx4_kernel(int d, unsigned n_rows, unsigned segs, unsigned items, const
     const int c0 = static_cast<int>(item - row * segs) * (256 * kRun) + lane * 8;
     const long long at = static_cast<long long>(row) * d + c0;
     const bool real = row < n_rows;
-    float f[kRun][8];
+    Raw<T> raw[kRun];
 #pragma unroll
     for (int i = 0; i < kRun; ++i)
-        if (real && c0 + i * 256 < d) load8(W + at + i * 256, f[i]);
+        if (real && c0 + i * 256 < d) raw[i] = fetch8(W + at + i * 256);
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
         if (c0 + i * 256 >= d) break;   // d is a multiple of 128: the 16 lanes of a word of scales leave together
-        uint32_t top = 0, word = 0, scale = 0;
+        uint32_t word = 0, scale = 0;
         const uint32_t group = 0xffffu << (lane & 16);
         if (real) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[i][e]) & 0x7fffffffu);
+            uint32_t top = top8(raw[i]);
             top = max(top, __shfl_xor_sync(group, top, 1));
             top = max(top, __shfl_xor_sync(group, top, 2));
             const uint32_t field = top >> 23;
             scale = field == 255u ? 255u : field < 2u ? 0u : field - 2u;
             const float inv = __uint_as_float((254u - min(scale, 252u)) << 23);   // 2^(127 - scale), exact
+            float f[8];
+            widen8(raw[i], f);
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) word |= e2m1x2(f[i][e] * inv, f[i][e + 1] * inv) << (e * 4);
+            for (int e = 0; e < 8; e += 2) word |= e2m1x2(f[e] * inv, f[e + 1] * inv) << (e * 4);
             if (scale == 255u) word = 0;
             Q[(at + i * 256) >> 3] = word;
         }

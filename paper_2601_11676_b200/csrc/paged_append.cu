@@ -16,7 +16,7 @@ long long paged_stride(const halo_paged_shape& s);
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kHeads = 4;   // heads in flight per thread
+constexpr int kHeads = 3;   // heads in flight per thread
 
 struct AppendArgs {
     int H, Hk, dh, page_size, n_pages, max_pages, n_seq, rotary;
@@ -45,8 +45,9 @@ paged_append_kernel(const __grid_constant__ AppendArgs a, int parts, int units, 
     extern __shared__ float2 turn[];   // [rotary / 2] cosine, sine
     const int tid = threadIdx.x;
     const int tok = blockIdx.x / parts, part = blockIdx.x % parts;
+    // everything that depends on the token alone is requested at once
     const int pos = __ldg(a.pos + tok);
-    if (pos < 0) return;               // a padding row: nothing of it is read or written
+    const int s = a.seq ? __ldg(a.seq + tok) : tok;
     const int half = a.rotary / 2;
     const int pair_units = INTERLEAVED ? 0 : half / E;   // units of two chunks per head
     const int c = tid % units, hl = tid / units;
@@ -77,17 +78,18 @@ paged_append_kernel(const __grid_constant__ AppendArgs a, int parts, int units, 
             }
         }
     };
+    const double freq = tid < half ? __ldg(a.inv_freq + tid) : 0.0;   // half <= 128 threads
     fetch(first);
 
-    const int s = a.seq ? __ldg(a.seq + tok) : tok;
+    if (pos < 0) return;               // a padding row: nothing is written for it
     const int pi = pos / a.page_size;
     int page = -1;
     if (s >= 0 && s < a.n_seq && pi < a.max_pages) page = __ldg(a.table + static_cast<long long>(s) * a.max_pages + pi);
-    for (int i = tid; i < half; i += blockDim.x) {
-        const double turns = static_cast<double>(pos) * __ldg(a.inv_freq + i) * 0.15915494309189533577;
+    if (tid < half) {
+        const double turns = static_cast<double>(pos) * freq * 0.15915494309189533577;
         float co, si;
         sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &si, &co);
-        turn[i] = make_float2(co, si);
+        turn[tid] = make_float2(co, si);
     }
     if (page < 0 || page >= a.n_pages) {   // the same in every thread
         if (tid == 0 && part == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);

@@ -242,7 +242,8 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int items = a.Hk * a.qblocks;
 
-    asm volatile("griddepcontrol.launch_dependents;");
+    // Only the join may start early: another kernel behind this one may read before it waits.
+    if (!a.whole && gridDim.x > 1) asm volatile("griddepcontrol.launch_dependents;");
     Walk<C_::kTile> con, iss;     // the piece that is summed, the piece whose rows are fetched
     long long total = 0;
     if (a.whole) {
