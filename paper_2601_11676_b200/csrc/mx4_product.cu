@@ -578,38 +578,34 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         for (int tile = pair; tile < tiles; tile += pairs, ++n) {
             if (!wait_cluster(&bars.acc_full, n & 1, abort_flag)) break;
             tcgen05_fence_after_sync();
-            constexpr int kWords = sizeof(T) == 4 ? 128 : 64;
-            uint32_t out[kWords];
+            uint32_t v[4][32];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t v[32];
-                tmem_ld_32x32(base + c * 32, v);
-                tmem_ld_wait();
-                if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) out[c * 32 + i] = v[i];
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const __nv_bfloat162 two = __floats2bfloat162_rn(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
-                        out[c * 16 + i] = *reinterpret_cast<const uint32_t*>(&two);
-                    }
-                }
-            }
+            for (int c = 0; c < 4; ++c) tmem_ld_32x32(base + c * 32, v[c]);
+            tmem_ld_wait();
             tcgen05_fence_before_sync();
             if (lane == 0) arrive_at(acc_empty);
             const int row = (tile % row_tiles) * kPairTile + static_cast<int>(rank) * 128 + quad * 32 + lane;
             const int tok0 = (tile / row_tiles) * kPairTile + half * 128;
+            if constexpr (sizeof(T) == 2) {
+                if ((n_rows & 1) == 0) {
+                    // two rows per word: lanes 2i and 2i + 1 exchange one token each of a pair of tokens
+                    T* p = y + static_cast<long long>(tok0 + (lane & 1)) * n_rows + (row & ~1);
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) {
+                        const float a0 = __uint_as_float(v[i >> 4][(i & 15) * 2]), a1 = __uint_as_float(v[i >> 4][(i & 15) * 2 + 1]);
+                        const float other = __shfl_xor_sync(0xffffffffu, lane & 1 ? a0 : a1, 1);
+                        const __nv_bfloat162 two = lane & 1 ? __floats2bfloat162_rn(other, a1) : __floats2bfloat162_rn(a0, other);
+                        if (row < n_rows && tok0 + 2 * i + (lane & 1) < n_tok) *reinterpret_cast<__nv_bfloat162*>(p) = two;
+                        p += 2ll * n_rows;
+                    }
+                    continue;
+                }
+            }
             if (row < n_rows) {
                 T* p = y + static_cast<long long>(tok0) * n_rows + row;
 #pragma unroll
                 for (int i = 0; i < 128; ++i) {
-                    if (tok0 + i < n_tok) {
-                        if constexpr (sizeof(T) == 4)
-                            *p = __uint_as_float(out[i]);
-                        else
-                            *p = __ushort_as_bfloat16(static_cast<unsigned short>(out[i >> 1] >> ((i & 1) * 16)));
-                    }
+                    if (tok0 + i < n_tok) *p = from_float<T>(__uint_as_float(v[i >> 5][i & 31]));
                     p += n_rows;
                 }
             }
