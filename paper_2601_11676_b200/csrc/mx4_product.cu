@@ -10,9 +10,9 @@
 // Three kernels:
 //   mx4_one_kernel   one token, bound by HBM: integer products (a 4-bit value is a whole number of halves) on the
 //     ordinary pipe, described at the kernel.
-//   mx4_line_kernel  few tokens, bound by HBM (0.53 bytes per weight element): the weight rows in groups of 32 form a
-//     line (one per tile of tokens) that is cut into equal pieces, one thread block per SM; whole outputs per thread
-//     block, so nothing has to be added up between thread blocks.
+//   mx4_line_kernel  up to 64 tokens, bound by HBM (0.53 bytes per weight element): the weight rows in groups of 32 form
+//     a line that is cut into equal pieces, one thread block per SM; whole outputs per thread block, so nothing has to
+//     be added up between thread blocks.
 //   mx4_pair_kernel  prompts, bound by the L2-to-SM traffic and the tensor pipe: pairs of SMs (cta_group::2) on tiles
 //     of 256 rows x 256 tokens; each SM fetches half of either operand, 35 KB per 16.8 M products and SM where a
 //     single SM's 128 x 256 tile takes 51 KB.
@@ -160,17 +160,17 @@ mx4_one_kernel(int d, int n_rows, const uint8_t* __restrict__ Qx, const uint8_t*
     }
 }
 
+// NT tokens (at most 64: one block of scales)
 template <int NT, int STAGES>
 struct Ring {
     static constexpr int kA = kRowsTile * (kStageK / 2);
     static constexpr int kB = NT * (kStageK / 2);
-    static constexpr int kTokTiles = (NT + 127) / 128;
-    static constexpr int kSfa = 1024, kSfb = 1024 * kTokTiles;
-    static constexpr int kStage = kA + kB + kSfa + kSfb;
-    static constexpr int kSfCols = 8 + 8 * kTokTiles;
-    static constexpr int kAcc = 2 * NT + STAGES * kSfCols <= 512 ? 2 : 1;   // accumulators
+    static constexpr int kSf = 1024;
+    static constexpr int kStage = kA + kB + 2 * kSf;
+    static constexpr int kSfCols = 16;
+    static constexpr int kAcc = 2;   // accumulators: one is read while the next fills
     static constexpr int kCols = kAcc * NT + STAGES * kSfCols;
-    static constexpr int kTmem = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
+    static constexpr int kTmem = kCols <= 256 ? 256 : 512;
     static constexpr size_t kSmem = static_cast<size_t>(STAGES) * kStage + 512;
     static_assert(kCols <= 512, "tensor memory");
     static_assert(kStage % 1024 == 0, "swizzled tiles start on 1024 bytes");
@@ -206,34 +206,28 @@ struct Slot {
     }
 };
 
-// The line: token tile after token tile, in each the row groups of 32 in order.  A piece is a run of groups inside one
-// block of 128 rows, so the rows of a group stand where the block's scales expect them.
+// The line: the row groups of 32 in order.  A piece is a run of groups inside one block of 128 rows, so the rows of a
+// group stand where the block's scales expect them.
 struct Piece {
-    int tok0, block, g0, g1;   // groups of the block, 0..4
+    int block, g0, g1;   // groups of the block, 0..4
 };
 struct Line {
-    long long at, end;
-    int groups;                // per token tile
-    __device__ __forceinline__ bool next(Piece& p, int nt) {
+    int at, end;
+    __device__ __forceinline__ bool next(Piece& p) {
         if (at >= end) return false;
-        const long long tt = at / groups;
-        const int g = static_cast<int>(at - tt * groups);
-        p.tok0 = static_cast<int>(tt) * nt;
-        p.block = g >> 2;
-        p.g0 = g & 3;
-        const long long last = min(min(static_cast<long long>((p.block + 1) * 4), static_cast<long long>(groups)), g + (end - at));
-        p.g1 = static_cast<int>(last) - p.block * 4;
+        p.block = at >> 2;
+        p.g0 = at & 3;
+        p.g1 = min(4, end - p.block * 4);
         at += p.g1 - p.g0;
         return true;
     }
 };
 
-// grain: groups that are not cut apart (1 or 4)
 template <typename T, int NT, int STAGES>
 __global__ void __launch_bounds__(kThreads, 1)
 mx4_line_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_g,
                 const __grid_constant__ CUtensorMap map_x, int d, int n_tok,
-                int n_rows, int grain, const uint8_t* __restrict__ Sw, const uint8_t* __restrict__ Sx, T* __restrict__ y,
+                int n_rows, const uint8_t* __restrict__ Sw, const uint8_t* __restrict__ Sx, T* __restrict__ y,
                 uint32_t* status) {
     using R = Ring<NT, STAGES>;
     extern __shared__ __align__(1024) unsigned char smem[];
@@ -242,10 +236,9 @@ mx4_line_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     const int atoms = d / 128;                       // 512-byte blocks of scales along a row
     const int nk = (d + kStageK - 1) / kStageK;
     Line line;
-    line.groups = ((n_rows + 31) / 32 + grain - 1) / grain * grain;
-    const long long units = static_cast<long long>(line.groups / grain) * ((n_tok + NT - 1) / NT);
-    line.at = units * blockIdx.x / gridDim.x * grain;
-    line.end = units * (blockIdx.x + 1) / gridDim.x * grain;
+    const long long groups = (n_rows + 31) / 32;
+    line.at = static_cast<int>(groups * blockIdx.x / gridDim.x);
+    line.end = static_cast<int>(groups * (blockIdx.x + 1) / gridDim.x);
 
     if (tid == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(&bars.full[s], 1); mbar_init(&bars.empty[s], 1); }
@@ -268,10 +261,8 @@ mx4_line_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         Slot<STAGES> slot;
         int it = 0;
         bool alive = true;
-        while (alive && line.next(p, NT)) {
-            const int tiles = min(R::kTokTiles, (n_tok - p.tok0 + 127) / 128);
+        while (alive && line.next(p)) {
             const uint8_t* sw = Sw + static_cast<size_t>(p.block) * atoms * 512;
-            const uint8_t* sx = Sx + static_cast<size_t>(p.tok0 / 128) * atoms * 512;
             for (int k = 0; k < nk; ++k, ++it, slot.advance()) {
                 uint64_t* full = &bars.full[slot.stage];
                 if (it >= STAGES && !wait_or_abort(&bars.empty[slot.stage], slot.parity ^ 1u, abort_flag)) { alive = false; break; }
@@ -279,16 +270,15 @@ mx4_line_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                 unsigned char* sc = st + R::kA + R::kB;
                 const uint32_t bytes = min(2, atoms - k * 2) * 512u;
                 if (leader) {
-                    mbar_arrive_expect_tx(full, (p.g1 - p.g0) * 32 * (kStageK / 2) + R::kB + bytes * (1 + tiles));
+                    mbar_arrive_expect_tx(full, (p.g1 - p.g0) * 32 * (kStageK / 2) + R::kB + 2 * bytes);
                     if (p.g1 - p.g0 == 4)
                         tma_load_2d(st, &map_w, k * (kStageK / 2), p.block * kRowsTile, full);
                     else
                         for (int g = p.g0; g < p.g1; ++g)
                             tma_load_2d(st + g * 32 * (kStageK / 2), &map_g, k * (kStageK / 2), p.block * kRowsTile + g * 32, full);
-                    tma_load_2d(st + R::kA, &map_x, k * (kStageK / 2), p.tok0, full);
+                    tma_load_2d(st + R::kA, &map_x, k * (kStageK / 2), 0, full);
                     bulk_copy_g2s(sc, sw + k * 1024, bytes, full);
-                    for (int t = 0; t < tiles; ++t)
-                        bulk_copy_g2s(sc + R::kSfa + t * 1024, sx + static_cast<size_t>(t) * atoms * 512 + k * 1024, bytes, full);
+                    bulk_copy_g2s(sc + R::kSf, Sx + k * 1024, bytes, full);
                 }
                 __syncwarp();
             }
@@ -302,7 +292,7 @@ mx4_line_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         Slot<STAGES> slot;
         int n = 0;
         bool alive = true;
-        while (alive && line.next(p, NT)) {
+        while (alive && line.next(p)) {
             const int acc = n % R::kAcc;
             if (n >= R::kAcc && !wait_or_abort(&bars.acc_empty[acc], ((n / R::kAcc) - 1) & 1, abort_flag)) break;
             tcgen05_fence_after_sync();
@@ -313,21 +303,19 @@ mx4_line_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                 const uint32_t st = smem_u32(smem) + slot.stage * R::kStage, sc = st + R::kA + R::kB;
                 const uint32_t sfa = tmem + R::kAcc * NT + slot.stage * R::kSfCols, sfb = sfa + 8;
                 const uint64_t da = umma_smem_desc(st, 0, 1024), db = umma_smem_desc(st + R::kA, 0, 1024);
-                const uint64_t dsa = scales_desc(sc), dsb = scales_desc(sc + R::kSfa);
+                const uint64_t dsa = scales_desc(sc), dsb = scales_desc(sc + R::kSf);
                 if (leader) {
 #pragma unroll
                     for (int at = 0; at < 2; ++at) {
                         if (at == 1 && atoms - k * 2 < 2) break;   // an odd number of runs of 128: half a stage
                         tmem_cp_scales(sfa + at * 4, dsa + at * 32);
-#pragma unroll
-                        for (int t = 0; t < R::kTokTiles; ++t)
-                            tmem_cp_scales(sfb + (at * R::kTokTiles + t) * 4, dsb + t * 64 + at * 32);
+                        tmem_cp_scales(sfb + at * 4, dsb + at * 32);
                     }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         if (j == 2 && atoms - k * 2 < 2) break;
                         umma_mxf4(tmem_d, da + j * 2, db + j * 2, idesc_mxf4(kRowsTile, NT, (j & 1) * 2), sfa + (j >> 1) * 4,
-                                  sfb + (j >> 1) * 4 * R::kTokTiles, j > 0 || k > 0);
+                                  sfb + (j >> 1) * 4, j > 0 || k > 0);
                     }
                     umma_commit(&bars.empty[slot.stage]);
                 }
@@ -340,26 +328,25 @@ mx4_line_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     } else {
         int n = 0;
         const int quad = warp & 3;
-        while (line.next(p, NT)) {
+        while (line.next(p)) {
             const int acc = n % R::kAcc;
             if (!wait_or_abort(&bars.acc_full[acc], (n / R::kAcc) & 1, abort_flag)) break;
             tcgen05_fence_after_sync();
             const int row = p.block * kRowsTile + quad * 32 + lane;
             const bool mine = quad >= p.g0 && quad < p.g1 && row < n_rows;
             const uint32_t base = tmem + acc * NT + (static_cast<uint32_t>(quad * 32) << 16);
-            const int cols = min(NT, n_tok - p.tok0);
-            T* out = y + static_cast<long long>(p.tok0) * n_rows + row;
-            for (int c0 = 0; c0 < cols; c0 += 16) {
+            T* out = y + row;
+            for (int c0 = 0; c0 < n_tok; c0 += 16) {
                 uint32_t v[16];
                 tmem_ld_32x16(base + c0, v);
                 tmem_ld_wait();
-                if (c0 + 16 >= cols) {   // the accumulator has been read
+                if (c0 + 16 >= n_tok) {   // the accumulator has been read
                     tcgen05_fence_before_sync();
                     if (lane == 0) mbar_arrive(&bars.acc_empty[acc]);
                 }
 #pragma unroll
                 for (int c = 0; c < 16; ++c)
-                    if (mine && c0 + c < cols) out[static_cast<long long>(c0 + c) * n_rows] = from_float<T>(__uint_as_float(v[c]));
+                    if (mine && c0 + c < n_tok) out[static_cast<long long>(c0 + c) * n_rows] = from_float<T>(__uint_as_float(v[c]));
             }
             ++n;
         }
@@ -643,7 +630,7 @@ halo_status launch_one(const Operands& o, T* y) {
 }
 
 template <typename T, int NT, int STAGES>
-halo_status launch_line(const Operands& o, int grain, T* y) {
+halo_status launch_line(const Operands& o, T* y) {
     using R = Ring<NT, STAGES>;
     static bool done[64];
     if (!ensure_dynamic_smem(mx4_line_kernel<T, NT, STAGES>, R::kSmem, done)) return HALO_ERR_CUDA;
@@ -652,10 +639,9 @@ halo_status launch_line(const Operands& o, int grain, T* y) {
         !make_byte_map(&map_g, o.Qw, o.n_rows, o.d / 2, kStageK / 2, 32) ||
         !make_byte_map(&map_x, o.Qx, o.n_tok, o.d / 2, kStageK / 2, NT))
         return HALO_ERR_CUDA;
-    const long long units = static_cast<long long>(((o.n_rows + 31) / 32 + grain - 1) / grain) * ((o.n_tok + NT - 1) / NT);
-    const int blocks = units < kSmCount ? static_cast<int>(units) : kSmCount;
+    const int groups = (o.n_rows + 31) / 32, blocks = groups < kSmCount ? groups : kSmCount;
     mx4_line_kernel<T, NT, STAGES><<<blocks, kThreads, R::kSmem, o.st>>>(
-        map_w, map_g, map_x, o.d, o.n_tok, o.n_rows, grain, static_cast<const uint8_t*>(o.Sw), static_cast<const uint8_t*>(o.Sx), y, o.status);
+        map_w, map_g, map_x, o.d, o.n_tok, o.n_rows, static_cast<const uint8_t*>(o.Sw), static_cast<const uint8_t*>(o.Sx), y, o.status);
     HALO_CHECK_LAUNCH();
     return HALO_OK;
 }
@@ -690,11 +676,13 @@ halo_status launch_pair(const Operands& o, T* y) {
 template <typename T>
 halo_status by_tokens(const Operands& o, void* y) {
     T* out = static_cast<T*>(y);
+    // At d = 4096, us (line / pair): 32 tokens 4096 rows 7.4 / 9.7, 11008 rows 11.3 / 10.3; 64 tokens 4096 rows 8.7 / 9.9,
+    // 11008 rows 12.6 / 9.9; 17 tokens 32000 rows 17.9 / 20.9.  One token (one / line): 4096 rows 4.3 / 6.6, 11008 rows
+    // 7.7 / 10.4, 32000 rows 17.1 / 17.1.
     if (o.n_tok == 1) return launch_one<T>(o, out);
-    if (o.n_tok <= 16) return launch_line<T, 16, 10>(o, 1, out);
-    if (o.n_tok <= 64) return launch_line<T, 64, 8>(o, 1, out);
-    if (o.n_tok <= 128) return launch_line<T, 128, 6>(o, 4, out);
-    if (o.n_tok <= 256) return launch_line<T, 256, 4>(o, 4, out);
+    if (o.n_tok <= 16) return launch_line<T, 16, 10>(o, out);
+    if (o.n_tok <= 32) return launch_line<T, 32, 9>(o, out);
+    if (o.n_tok <= 64 && o.n_rows <= 8192) return launch_line<T, 64, 8>(o, out);
     return launch_pair<T>(o, out);
 }
 
