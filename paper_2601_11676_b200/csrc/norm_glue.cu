@@ -87,7 +87,7 @@ __device__ __forceinline__ void widen8(const Raw<T>& r, float (&f)[8]) {
 constexpr int kWarpRows = 4;   // rows per thread block where a row is one warp
 
 template <typename TY, typename T, int IT, bool ONE_WARP>
-__global__ void __launch_bounds__(ONE_WARP ? 32 * kWarpRows : IT == 4 ? 512 : 1024)
+__global__ void __launch_bounds__(ONE_WARP ? 32 * kWarpRows : 1024)
 norm_glue_kernel(const __grid_constant__ GlueArgs a) {
     __shared__ float sh[2][32];
     const int t = ONE_WARP ? threadIdx.x & 31 : threadIdx.x, n = ONE_WARP ? 32 : blockDim.x;
@@ -183,14 +183,14 @@ template <typename TY, typename T>
 halo_status launch(const GlueArgs& a, cudaStream_t st) {
     const int units = a.d / 8;
     const auto threads = [&](int it) { return (units + 32 * it - 1) / (32 * it) * 32; };
-    // Many rows: four units per thread, the most bytes in flight per register.  Few rows: one unit per thread while a
-    // thread block can hold the row, the shortest time for a row.
+    // Many rows: two units per thread (8191 rows of 5120, us: two 91, three 93, four 102, five
+    // 105: more units per thread leave fewer rows in flight per SM).  Few rows: one unit per thread while a thread block
+    // can hold the row, the shortest time for a row.
     const bool many = a.n_tok >= 2 * kSmCount;
     if (units <= 32) return go<TY, T, 1, true>(a, 32 * kWarpRows, st);
-    if (many && units <= 128) return go<TY, T, 4, true>(a, 32 * kWarpRows, st);
-    if (many) return go<TY, T, 4, false>(a, threads(4), st);
-    if (units <= 1024) return go<TY, T, 1, false>(a, threads(1), st);
-    return go<TY, T, 2, false>(a, threads(2), st);
+    if (many && units <= 64) return go<TY, T, 2, true>(a, 32 * kWarpRows, st);
+    if (many || units > 1024) return go<TY, T, 2, false>(a, threads(2), st);
+    return go<TY, T, 1, false>(a, threads(1), st);
 }
 
 }  // namespace
