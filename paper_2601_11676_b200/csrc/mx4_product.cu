@@ -8,8 +8,7 @@
 // its own columns of scales: a stage is refilled only when the products that read its old scales have completed.
 //
 // Three kernels:
-//   mx4_one_kernel   one token, bound by HBM: integer products (a 4-bit value is a whole number of halves) on the
-//     ordinary pipe, described at the kernel.
+//   mx4_one_kernel   one token, bound by HBM: exact fp16 products on the ordinary pipe, described at the kernel.
 //   mx4_line_kernel  up to 64 tokens, bound by HBM (0.53 bytes per weight element): the weight rows in groups of 32 form
 //     a line that is cut into equal pieces, one thread block per SM; whole outputs per thread block, so nothing has to
 //     be added up between thread blocks.
@@ -19,6 +18,8 @@
 //
 // Every wait is bounded; when one runs out the block's roles leave their loops, the copies in flight are waited for,
 // TMEM is freed and HALO_DEV_TIMEOUT is raised.
+#include <cuda_fp16.h>
+
 #include "common.cuh"
 #include "umma.cuh"
 
@@ -63,48 +64,46 @@ __device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint64_t desc) {
 }
 
 // ---- one token -----------------------------------------------------------------------------------------------------
-// Twice a 4-bit value is a whole number of at most 12, so a run of 32 elements is an exact integer product: the byte
-// permute picks four magnitudes at a time from an eight-byte table with the codes themselves as selectors; a selector's
-// top bit (the code's sign) gives 0 instead, so one pass with the codes and one with their signs turned sum the positive
-// and the negative weights (11 instructions for 8 elements).  The integer of a run meets both its scales in fp32.  The
-// token sits in shared memory as bytes; a warp takes kRows rows at once, a lane the runs lane, lane + 32, ... of them,
-// with kAhead 16-byte loads per row in flight.  A thread block's rows are neighbours: they share the lines of the scale
-// blocks.
+// A run of 32 elements shares a scale on either side, so it is a sum of 32 products of plain 4-bit values, which fp16
+// holds exactly: a product is a whole number of quarters of at most 36, and 8 of them (what one half of one accumulator
+// takes here) stay below 2^11 quarters.  So a byte of codes is one conversion to two fp16 values and one packed
+// multiply-add; the run's sum meets both scales in fp32.  The token sits in shared memory as fp16; a warp takes kRows
+// rows at once, a lane the runs lane, lane + 32, ... of them, with kAhead 16-byte loads per row in flight.  A thread
+// block's rows are neighbours: they share the lines of the scale blocks.  32000 x 4096: 16.1 us = 4.3 TB/s (17.1 with
+// integer products of bytes, dp4a and the byte permute as a table, which the wide multiplier bounds).
 constexpr int kOneThreads = 256;
-constexpr size_t kOneSmem = 74 * 1024;   // the widest row
-// bytes of {high, low} by the four lower nibbles of sel; a nibble of 8 or more gives the sign of its byte, 0 in this table
-__device__ __forceinline__ uint32_t permute(uint32_t low, uint32_t high, uint32_t sel) {
-    uint32_t r;
-    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(low), "r"(high), "r"(sel));
-    return r;
-}
+constexpr size_t kOneSmem = 140 * 1024;   // the widest row
 __device__ __forceinline__ float power(uint32_t byte) {   // 2^(byte - 127); 255 is NaN
     return __uint_as_float(byte == 0 ? 0x00400000u : byte == 255u ? 0x7fc00000u : byte << 23);
+}
+__device__ __forceinline__ void unpack(uint32_t w, __half2 (&h)[4]) {   // eight codes, exactly
+    uint32_t r[4];
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\tcvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(w));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = *reinterpret_cast<const __half2*>(&r[i]);
 }
 template <typename T>
 __global__ void __launch_bounds__(kOneThreads, 3)
 mx4_one_kernel(int d, int n_rows, const uint8_t* __restrict__ Qx, const uint8_t* __restrict__ Sx,
                const uint8_t* __restrict__ Qw, const uint8_t* __restrict__ Sw, T* __restrict__ y) {
     constexpr int kRows = 2, kAhead = 4, kWarps = kOneThreads / 32;
-    constexpr uint32_t kLow = 0x03020100u, kHigh = 0x0C080604u;   // twice 0, 0.5, 1, 1.5 and 2, 3, 4, 6
     extern __shared__ __align__(16) unsigned char smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int runs = d / 32;                       // of a row
-    // [half of a run][run] 16 bytes, then [run] a quarter of the token's scale
-    uint4* xs = reinterpret_cast<uint4*>(smem);
-    float* sx = reinterpret_cast<float*>(xs + 2 * runs);
+    uint4* xs = reinterpret_cast<uint4*>(smem);    // [quarter of a run][run] 8 values, then [run] the token's scale
+    float* sx = reinterpret_cast<float*>(xs + 4 * runs);
     for (int b = tid; b < runs; b += kOneThreads) {
         const uint4 code = *reinterpret_cast<const uint4*>(Qx + b * 16);
         const uint32_t word[4] = {code.x, code.y, code.z, code.w};
-        uint32_t out[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const uint32_t sel = word[k >> 1] >> ((k & 1) * 16);
-            out[k] = __vsub4(permute(kLow, kHigh, sel), permute(kLow, kHigh, sel ^ 0x8888u));
+        for (int k = 0; k < 4; ++k) {
+            alignas(16) __half2 h[4];
+            unpack(word[k], h);
+            xs[k * runs + b] = *reinterpret_cast<uint4*>(h);
         }
-        xs[b] = make_uint4(out[0], out[1], out[2], out[3]);
-        xs[runs + b] = make_uint4(out[4], out[5], out[6], out[7]);
-        sx[b] = 0.25f * power(Sx[(b >> 2) * 512 + (b & 3)]);
+        sx[b] = power(Sx[(b >> 2) * 512 + (b & 3)]);
     }
     __syncthreads();
     const int first = static_cast<int>(static_cast<long long>(n_rows) * blockIdx.x / gridDim.x);
@@ -134,21 +133,27 @@ mx4_one_kernel(int d, int n_rows, const uint8_t* __restrict__ Qx, const uint8_t*
             for (int i = 0; i < kAhead; ++i) {
                 const int b = b0 + i * 32 + lane;
                 if (b >= runs) break;
-                const uint4 x0 = xs[b], x1 = xs[runs + b];
-                const uint32_t x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+                __half2 acc[kRows][2];
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) acc[r][0] = acc[r][1] = __float2half2_rn(0.0f);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint4 xv = xs[k * runs + b];
+                    const __half2* xh = reinterpret_cast<const __half2*>(&xv);
+#pragma unroll
+                    for (int r = 0; r < kRows; ++r) {
+                        const uint32_t w = k == 0 ? code[i][r].x : k == 1 ? code[i][r].y : k == 2 ? code[i][r].z : code[i][r].w;
+                        __half2 h[4];
+                        unpack(w, h);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[r][k >> 1] = __hfma2(h[e], xh[e], acc[r][k >> 1]);
+                    }
+                }
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) {
-                    const uint32_t word[4] = {code[i][r].x, code[i][r].y, code[i][r].z, code[i][r].w};
-                    int up = 0, down = 0;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const uint32_t sel = word[k >> 1] >> ((k & 1) * 16);
-                        const uint32_t turned = (word[k >> 1] ^ 0x88888888u) >> ((k & 1) * 16);
-                        up = __dp4a(static_cast<int>(permute(kLow, kHigh, sel)), static_cast<int>(x[k]), up);
-                        down = __dp4a(static_cast<int>(permute(kLow, kHigh, turned)), static_cast<int>(x[k]), down);
-                    }
-                    // integer x scale of x first: exact, and 0 stays 0 before a scale of 2^127
-                    sum[r] = fmaf(static_cast<float>(up - down) * sx[b], power(scale[i][r]), sum[r]);
+                    const float2 f0 = __half22float2(acc[r][0]), f1 = __half22float2(acc[r][1]);
+                    // the plain sum x scale of x first: exact, and 0 stays 0 before a scale of 2^127
+                    sum[r] = fmaf(((f0.x + f0.y) + (f1.x + f1.y)) * sx[b], power(scale[i][r]), sum[r]);
                 }
             }
         }
@@ -620,9 +625,9 @@ template <typename T>
 halo_status launch_one(const Operands& o, T* y) {
     static bool done[64];
     if (!ensure_dynamic_smem(mx4_one_kernel<T>, kOneSmem, done)) return HALO_ERR_CUDA;
-    static_assert(HALO_MX4_MAX_WIDTH + HALO_MX4_MAX_WIDTH / 8 <= kOneSmem, "the widest row fits");
+    static_assert(2 * HALO_MX4_MAX_WIDTH + HALO_MX4_MAX_WIDTH / 8 <= kOneSmem, "the widest row fits");
     const int most = 3 * kSmCount, want = (o.n_rows + 15) / 16;   // a pair of rows per warp at least
-    mx4_one_kernel<T><<<want < most ? want : most, kOneThreads, o.d + o.d / 8, o.st>>>(
+    mx4_one_kernel<T><<<want < most ? want : most, kOneThreads, 2 * o.d + o.d / 8, o.st>>>(
         o.d, o.n_rows, static_cast<const uint8_t*>(o.Qx), static_cast<const uint8_t*>(o.Sx), static_cast<const uint8_t*>(o.Qw),
         static_cast<const uint8_t*>(o.Sw), y);
     HALO_CHECK_LAUNCH();
@@ -678,7 +683,7 @@ halo_status by_tokens(const Operands& o, void* y) {
     T* out = static_cast<T*>(y);
     // At d = 4096, us (line / pair): 32 tokens 4096 rows 7.4 / 9.7, 11008 rows 11.3 / 10.3; 64 tokens 4096 rows 8.7 / 9.9,
     // 11008 rows 12.6 / 9.9; 17 tokens 32000 rows 17.9 / 20.9.  One token (one / line): 4096 rows 4.3 / 6.6, 11008 rows
-    // 7.7 / 10.4, 32000 rows 17.1 / 17.1.
+    // 7.4 / 10.4, 32000 rows 16.1 / 16.6.
     if (o.n_tok == 1) return launch_one<T>(o, out);
     if (o.n_tok <= 16) return launch_line<T, 16, 10>(o, out);
     if (o.n_tok <= 32) return launch_line<T, 32, 9>(o, out);
