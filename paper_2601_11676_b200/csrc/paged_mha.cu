@@ -17,6 +17,7 @@
 //     kernel, not the tensor pipe.  Weights are rounded to bf16 for the second product (relative 2^-8, like the output);
 //     their sum is taken in fp32 before that rounding.
 //   fp32: fused multiply-adds, two lanes per position for the scores, a column per lane for the weighted sums.
+#include <cooperative_groups.h>
 #include <math.h>
 
 #include "common.cuh"
@@ -51,7 +52,7 @@ struct PagedArgs {
     Cut* cuts;   // [C], then the slots: two per range
     float* ws;
     uint32_t* status;
-    int whole;   // one thread block per item: no line, no join
+    int split;   // > 0: a cluster of that many thread blocks per item, no line and no join kernel
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
@@ -243,13 +244,17 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
     const int items = a.Hk * a.qblocks;
 
     // Only the join may start early: another kernel behind this one may read before it waits.
-    if (!a.whole && gridDim.x > 1) asm volatile("griddepcontrol.launch_dependents;");
+    if (!a.split && gridDim.x > 1) asm volatile("griddepcontrol.launch_dependents;");
     Walk<C_::kTile> con, iss;     // the piece that is summed, the piece whose rows are fetched
     long long total = 0;
-    if (a.whole) {
-        const int s = blockIdx.x / items;
+    if (a.split) {
+        const int rank = blockIdx.x % a.split, item = blockIdx.x / a.split, s = item / items;
         const int nt = tiles_of<C_::kTile>(a, s);
-        con.begin(a, s, static_cast<long long>(blockIdx.x % items) * nt, nt);
+        const int t0 = static_cast<int>(static_cast<long long>(nt) * rank / a.split);
+        con.begin(a, s, static_cast<long long>(item % items) * nt, 0);
+        con.t0 = t0;
+        con.t1 = static_cast<int>(static_cast<long long>(nt) * (rank + 1) / a.split);
+        con.left = con.t1 - t0;     // may be 0: the thread block still meets the others
     } else {
         const LinePos p = locate<C_::kTile, kThreads>(
             a, [&](long long t) {
@@ -282,33 +287,55 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
     };
     int page_next = page_at();
     bool bad = false;
+    // Pages of whole runs: a run's positions are neighbours in memory and share a page.
+    const bool neighbours = a.page_size % kRun == 0;
+    const int lr = lane / kLanesPerRow, lc = lane % kLanesPerRow;
+    const auto put_row = [&](uint32_t st, int i, int ci, const T* k, const T* v, bool have) {
+        const int r = i * kRowsPer + lr, c = lc + ci * 32;   // the swizzle: c ^ r, as i * kRowsPer and lr have no bit in common
+        const uint32_t d = st + r * C_::kRowBytes + (kF32 ? c * 16 : ((c & ~7) | (((c ^ lr) ^ (i * kRowsPer)) & 7)) * 16);
+        cp_async16(d, k, have);
+        cp_async16(d + C_::kHalf, v, have);
+    };
     const auto issue = [&]() -> uint32_t {   // starts the copies of the next run; returns its mask of present positions
         uint32_t mask = 0;
         if (iss.left > 0) {
-            const int p = it * C_::kTile + warp * kRun + (lane & 15);
+            const int p0 = it * C_::kTile + warp * kRun, p = p0 + (lane & 15);
             const bool in = p < iss.reach, ok = in && page_next >= 0 && page_next < a.n_pages;
             bad |= in && !ok;
             mask = __ballot_sync(0xffffffffu, ok) & 0xffffu;
             if (mask) {
                 const int kvh = a.qblocks == 1 ? iss.hi : iss.hi / a.qblocks;
-                const int in_page = a.page_shift >= 0 ? p & (a.page_size - 1) : p % a.page_size;
-                const long long off = ok ? static_cast<long long>(page_next) * a.page_stride +
-                                               (static_cast<long long>(kvh) * a.page_size + in_page) * a.dh
-                                         : 0;
                 const uint32_t st = ring_a + slot_in * C_::kStage;
+                if (neighbours) {
+                    const int page = __shfl_sync(0xffffffffu, page_next, 0);   // mask: position 0 is there
+                    const int in_page = a.page_shift >= 0 ? p0 & (a.page_size - 1) : p0 % a.page_size;
+                    const long long off = static_cast<long long>(page) * a.page_stride +
+                                          (static_cast<long long>(kvh) * a.page_size + in_page + lr) * a.dh + lc * kE;
+                    const T* k = static_cast<const T*>(a.K) + off;
+                    const T* v = static_cast<const T*>(a.V) + off;
+                    const int step = kRowsPer * a.dh;
 #pragma unroll
-                for (int i = 0; i < kRun / kRowsPer; ++i) {
-                    const int r = i * kRowsPer + lane / kLanesPerRow;
-                    const long long ro = __shfl_sync(0xffffffffu, off, r);
-                    const bool have = (mask >> r) & 1u;
+                    for (int i = 0; i < kRun / kRowsPer; ++i) {
 #pragma unroll
-                    for (int ci = 0; ci < kChunkIters; ++ci) {
-                        const int c = lane % kLanesPerRow + ci * 32;
-                        if (c * kE < a.dh) {
-                            const uint32_t d = st + r * C_::kRowBytes + (kF32 ? c * 16 : ((c & ~7) | ((c ^ r) & 7)) * 16);
-                            cp_async16(d, static_cast<const T*>(a.K) + ro + c * kE, have);
-                            cp_async16(d + C_::kHalf, static_cast<const T*>(a.V) + ro + c * kE, have);
-                        }
+                        for (int ci = 0; ci < kChunkIters; ++ci)
+                            if ((lc + ci * 32) * kE < a.dh)
+                                put_row(st, i, ci, k + ci * 32 * kE, v + ci * 32 * kE, (mask >> (i * kRowsPer + lr)) & 1u);
+                        k += step;
+                        v += step;
+                    }
+                } else {
+                    const int in_page = a.page_shift >= 0 ? p & (a.page_size - 1) : p % a.page_size;
+                    const long long off = ok ? static_cast<long long>(page_next) * a.page_stride +
+                                                   (static_cast<long long>(kvh) * a.page_size + in_page) * a.dh
+                                             : 0;
+#pragma unroll
+                    for (int i = 0; i < kRun / kRowsPer; ++i) {
+                        const long long ro = __shfl_sync(0xffffffffu, off, i * kRowsPer + lr) + lc * kE;
+#pragma unroll
+                        for (int ci = 0; ci < kChunkIters; ++ci)
+                            if ((lc + ci * 32) * kE < a.dh)
+                                put_row(st, i, ci, static_cast<const T*>(a.K) + ro + ci * 32 * kE,
+                                        static_cast<const T*>(a.V) + ro + ci * 32 * kE, (mask >> (i * kRowsPer + lr)) & 1u);
                     }
                 }
             }
@@ -329,7 +356,9 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
     // ---- summing ----------------------------------------------------------------------------------------------------
     const int g = lane >> 2, t4 = lane & 3;
     int slot_out = 0;
-    while (con.left > 0) {
+    bool first = true;
+    while (con.left > 0 || (first && a.split)) {
+        first = false;
         const int kvh = con.hi / a.qblocks, r0 = (con.hi % a.qblocks) * 16;
         const int rows = min(16, a.G - r0), h0 = kvh * a.G + r0;
         const T* qrow = static_cast<const T*>(a.q) + static_cast<long long>(con.s) * a.q_stride + static_cast<long long>(h0) * a.dh;
@@ -480,10 +509,16 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
             __syncthreads();
             if (warp == 0) {
                 add(1);
+                if (a.split > 1) {
+                    put(0);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        if (t4 == 0) { wm[0][g + k * 8] = M[k]; wl[0][g + k * 8] = L[k]; }
+                }
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int r = g + k * 8;
-                    if (r >= rows) continue;
+                    if (r >= rows || a.split > 1) continue;
                     if (complete) {
                         const bool some = L[k] != 0.0f && head_kept(a, h0 + r);
                         const long long row = static_cast<long long>(con.s) * a.H + h0 + r;
@@ -640,9 +675,15 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
             __syncthreads();
             if (warp == 0) {
                 add(kB);
+                if (a.split > 1) {
+                    put(0);
+#pragma unroll
+                    for (int r = 0; r < GR; ++r)
+                        if (lane == 0) { wm[0][r] = m[r]; wl[0][r] = l[r]; }
+                }
 #pragma unroll
                 for (int r = 0; r < GR; ++r) {
-                    if (r >= rows) continue;
+                    if (r >= rows || a.split > 1) continue;
                     const bool some = l[r] != 0.0f && head_kept(a, h0 + r);
                     const long long row = static_cast<long long>(con.s) * a.H + h0 + r;
                     float* out = complete ? static_cast<float*>(a.out) + row * a.dh : slot + kSlotHead + r * DP;
@@ -662,7 +703,29 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                 }
             }
         }
-        if (!a.whole && tid == 0 && con.left == con.t1 - con.t0)   // the range's last piece
+        if (a.split > 1) {   // the thread blocks of the item meet: sums through distributed shared memory, in rank order
+            namespace cg = cooperative_groups;
+            const cg::cluster_group cl = cg::this_cluster();
+            cl.sync();
+            for (int i = tid + static_cast<int>(cl.block_rank()) * kThreads; i < rows * a.dh; i += kThreads * a.split) {
+                const int r = i / a.dh, j = i - r * a.dh;
+                float M = -INFINITY;
+                for (int k = 0; k < a.split; ++k) M = fmaxf(M, *cl.map_shared_rank(&wm[0][r], k));
+                const float base = M == -INFINITY ? 0.0f : M;
+                float L = 0.0f, v = 0.0f;
+                for (int k = 0; k < a.split; ++k) {
+                    const float f = exp2f(*cl.map_shared_rank(&wm[0][r], k) - base);
+                    L = fmaf(*cl.map_shared_rank(&wl[0][r], k), f, L);
+                    v = fmaf(*cl.map_shared_rank(mg + r * C_::kMergeRow + j, k), f, v);
+                }
+                const bool some = L != 0.0f && head_kept(a, h0 + r);
+                write_head<T>(a, con.s, h0 + r, j, some ? v / L : 0.0f);
+                if (j == 0 && a.lse)
+                    a.lse[static_cast<long long>(con.s) * a.H + h0 + r] = some ? (M + log2f(L)) * kLn2 : -INFINITY;
+            }
+            cl.sync();       // nobody leaves while its sums may still be read
+        }
+        if (!a.split && tid == 0 && con.left == con.t1 - con.t0)   // the range's last piece
             a.cuts[blockIdx.x] = {con.t0 == 0 && con.t1 < con.nt, con.s, con.hi, con.nt - con.t1, total, con.left == range, 0};
         // a length out of range is reported where the sequence's first tile is
         if (con.t0 == 0 && con.hi == 0 && tid == 0) (void)valid_len(a, con.s, true);
@@ -758,7 +821,7 @@ __global__ void __launch_bounds__(THREADS) paged_mha_join_kernel(const __grid_co
 }
 
 struct LaunchPlan {
-    int blocks, whole;
+    int blocks, split;
     int slot, rows, merge;   // as in PagedArgs
     long long items;
 };
@@ -774,13 +837,20 @@ LaunchPlan plan_of(const halo_paged_shape& sh, int n_seq) {
     p.slot = kSlotHead + p.rows * DP;
     p.merge = (C_::merge_bytes(p.rows) + 15) / 16 * 16;
     const long long resident = static_cast<long long>(kSmCount) * C_::kBlocksPerSm;
-    // A thread block per item where the items are short and no thread block would get a second one.
-    p.whole = tiles <= 4 && p.items <= resident;
-    p.blocks = static_cast<int>(p.whole ? p.items : tiles * p.items < resident ? tiles * p.items : resident);
+    // Few and short items: a cluster per item, one launch (one sequence of 700 positions, 32 / 4 heads of 64: 8.6 us as a
+    // line with a join, 7.1 as clusters of 8).  A cluster's meeting costs 1.3 us, a tile about 0.8: two tiles are not
+    // split (128 positions, 5.5 us and 6.8).  Elsewhere the line: it balances lengths and fills the GPU.
+    p.split = 0;
+    if (p.items <= resident) {
+        int n = 1;
+        while (n < 8 && tiles > 2 && 2 * n <= tiles && 2 * n * p.items <= resident) n *= 2;
+        if (tiles <= 8ll * n) p.split = n;
+    }
+    p.blocks = static_cast<int>(p.split ? p.items * p.split : tiles * p.items < resident ? tiles * p.items : resident);
     return p;
 }
 size_t workspace_of(const LaunchPlan& p) {
-    return p.whole ? 0 : static_cast<size_t>(p.blocks) * (sizeof(Cut) + sizeof(float) * 2 * p.slot);
+    return p.split ? 0 : static_cast<size_t>(p.blocks) * (sizeof(Cut) + sizeof(float) * 2 * p.slot);
 }
 
 template <typename T, int DP, int THREADS>
@@ -804,13 +874,24 @@ halo_status launch(const PagedArgs& args, const LaunchPlan& p, cudaStream_t st) 
     static bool done[64];
     if (!ensure_dynamic_smem(paged_mha_kernel<T, DP, GR>, C_::kMaxSmem, done)) return HALO_ERR_CUDA;
     PagedArgs a = args;
-    a.whole = p.whole;
+    a.split = p.split;
     a.slot = p.slot;
     a.rows = p.rows;
     a.merge = p.merge;
-    paged_mha_kernel<T, DP, GR><<<p.blocks, C_::kWarps * 32, C_::kRings + p.merge, st>>>(a);
-    HALO_CHECK_LAUNCH();
-    if (p.whole || p.blocks < 2) return HALO_OK;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(p.blocks);
+    cfg.blockDim = dim3(C_::kWarps * 32);
+    cfg.dynamicSmemBytes = C_::kRings + p.merge;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = p.split > 1 ? p.split : 1;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = p.split > 1 ? 1 : 0;
+    const halo_status rc = cuda_status(cudaLaunchKernelEx(&cfg, paged_mha_kernel<T, DP, GR>, a));
+    if (rc != HALO_OK || p.split || p.blocks < 2) return rc;
     // few items, many pieces each: several groups of threads
     constexpr int kWide = DP == 256 ? 512 : 256;
     return p.blocks >= 8 * p.items ? launch_join<T, DP, kWide>(a, p, st) : launch_join<T, DP, DP>(a, p, st);
