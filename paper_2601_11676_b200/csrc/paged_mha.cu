@@ -77,6 +77,12 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], 
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// 2^x, results below 2^-126 as 0
+__device__ __forceinline__ float pow2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
@@ -85,7 +91,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 constexpr int kRun = 16;            // positions of a tile that one warp takes
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr int kSlotHead = 32;       // floats in front of a slot's values: maxima, sums
-// Shapes per element type, padded head size DP and (fp32) padded number of query heads GR.  Ring bytes are what keeps
+// Shapes per element type, padded head size DP and padded number of query heads GR (bf16: 8 or 16 of 16 rows in use).  Ring bytes are what keeps
 // HBM busy: 6.5 TB/s x ~1 us of latency / 148 SMs = 44 KB have to be in flight; the shapes below hold 96 to 200 KB.
 template <typename T, int DP, int GR>
 struct Cfg {
@@ -366,21 +372,28 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
         float* slot = a.ws + (static_cast<long long>(blockIdx.x) * 2 + (con.left == range ? 0 : 1)) * a.slot;
 
         if constexpr (!kF32) {
+            constexpr int kK = GR > 8 ? 2 : 1;    // rows of a lane: g, and g + 8 where an item has more than 8 heads
             uint32_t qf[DP / 16][4];
 #pragma unroll
-            for (int k = 0; k < DP / 16; ++k)
+            for (int j = 0; j < 4; ++j) {
+                const int r = g + (j & 1) * 8;
+                const bool there = (kK == 2 || !(j & 1)) && r < rows;
+                const T* q = qrow + static_cast<long long>(r) * a.dh + (j >> 1) * 8 + t4 * 2;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int r = g + (j & 1) * 8, c = k * 16 + (j >> 1) * 8 + t4 * 2;
-                    qf[k][j] = (r < rows && c < a.dh)
-                                   ? __ldg(reinterpret_cast<const uint32_t*>(qrow + static_cast<long long>(r) * a.dh + c)) : 0u;
-                }
+                for (int k = 0; k < DP / 16; ++k)
+                    qf[k][j] = there && k * 16 < a.dh ? __ldg(reinterpret_cast<const uint32_t*>(q + k * 16)) : 0u;   // dh % 16 == 0
+            }
             float o[NT][4];
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) o[n][j] = 0.0f;
-            float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+            float m[kK], l[kK];
+#pragma unroll
+            for (int k = 0; k < kK; ++k) {
+                m[k] = -INFINITY;
+                l[k] = 0.0f;
+            }
 
             for (int t = con.t0; t < con.t1; ++t) {
                 masks[S - 1] = issue();
@@ -405,44 +418,45 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                         mma_bf16(k & 1 ? sc2[1] : sc[1], qf[k], b[2], b[3]);
                     }
                 }
-                // running softmax; a lane holds rows g and g + 8, positions 2 * t4 + {0, 1} and 8 more
-                float mx0 = m0, mx1 = m1;
+                // running softmax; a lane holds rows g (and g + 8), positions 2 * t4 + {0, 1} and 8 more
 #pragma unroll
                 for (int n = 0; n < 2; ++n)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int key = n * 8 + t4 * 2 + (j & 1);
-                        sc[n][j] = (mask >> key) & 1u ? (sc[n][j] + sc2[n][j]) * a.scale_log2 : -INFINITY;
-                        if (j < 2) mx0 = fmaxf(mx0, sc[n][j]); else mx1 = fmaxf(mx1, sc[n][j]);
-                    }
+                    for (int j = 0; j < 2 * kK; ++j) sc[n][j] = (sc[n][j] + sc2[n][j]) * a.scale_log2;
+                if (mask != 0xffffu) {
 #pragma unroll
-                for (int d = 1; d < 4; d <<= 1) {
-                    mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, d));
-                    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, d));
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int j = 0; j < 2 * kK; ++j)
+                            if (!((mask >> (n * 8 + t4 * 2 + (j & 1))) & 1u)) sc[n][j] = -INFINITY;
                 }
-                const float b0 = mx0 == -INFINITY ? 0.0f : mx0, b1 = mx1 == -INFINITY ? 0.0f : mx1;
-                const float f0 = exp2f(m0 - b0), f1 = exp2f(m1 - b1);
-                if (__any_sync(0xffffffffu, m0 != mx0 || m1 != mx1)) {
+                float f[kK];
+                bool moved = false;
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        o[n][0] *= f0; o[n][1] *= f0;
-                        o[n][2] *= f1; o[n][3] *= f1;
-                    }
+                for (int k = 0; k < kK; ++k) {
+                    float mx = fmaxf(fmaxf(sc[0][2 * k], sc[0][2 * k + 1]), fmaxf(sc[1][2 * k], sc[1][2 * k + 1]));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                    mx = fmaxf(mx, m[k]);
+                    const float base = mx == -INFINITY ? 0.0f : mx;
+                    f[k] = pow2(m[k] - base);
+                    moved |= m[k] != mx;
+                    m[k] = mx;
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int j = 2 * k; j < 2 * k + 2; ++j) sc[n][j] = pow2(sc[n][j] - base);
+                    l[k] = fmaf(l[k], f[k], (sc[0][2 * k] + sc[0][2 * k + 1]) + (sc[1][2 * k] + sc[1][2 * k + 1]));
                 }
-                m0 = mx0; m1 = mx1;
-                float a0 = 0.0f, a1 = 0.0f;
+                if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        sc[n][j] = exp2f(sc[n][j] - (j < 2 ? b0 : b1));
-                        if (j < 2) a0 += sc[n][j]; else a1 += sc[n][j];
-                    }
-                l0 = fmaf(l0, f0, a0);
-                l1 = fmaf(l1, f1, a1);
+                        for (int j = 0; j < 2 * kK; ++j) o[n][j] *= f[j >> 1];
+                }
                 // weighted sum of the values
-                const uint32_t pa[4] = {pack_bf16(sc[0][0], sc[0][1]), pack_bf16(sc[0][2], sc[0][3]),
-                                        pack_bf16(sc[1][0], sc[1][1]), pack_bf16(sc[1][2], sc[1][3])};
+                const uint32_t pa[4] = {pack_bf16(sc[0][0], sc[0][1]), kK == 2 ? pack_bf16(sc[0][2], sc[0][3]) : 0u,
+                                        pack_bf16(sc[1][0], sc[1][1]), kK == 2 ? pack_bf16(sc[1][2], sc[1][3]) : 0u};
                 const int key = ((lane >> 3) & 1) * 8 + (lane & 7), half = lane >> 4;
 #pragma unroll
                 for (int n = 0; n < NT; n += 2) {
@@ -454,20 +468,17 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                 }
                 __syncwarp();   // the stage is free for the copies that the next round starts
             }
-#pragma unroll
-            for (int d = 1; d < 4; d <<= 1) {
-                l0 += __shfl_xor_sync(0xffffffffu, l0, d);
-                l1 += __shfl_xor_sync(0xffffffffu, l1, d);
-            }
             // the warps meet: common maxima and sums, then the weighted sums of warps 2 and 3 go to 0 and 1, of 1 to 0
-            if (t4 == 0) {
-                wm[warp][g] = m0; wm[warp][g + 8] = m1;
-                wl[warp][g] = l0; wl[warp][g + 8] = l1;
+#pragma unroll
+            for (int k = 0; k < kK; ++k) {
+                l[k] += __shfl_xor_sync(0xffffffffu, l[k], 1);
+                l[k] += __shfl_xor_sync(0xffffffffu, l[k], 2);
+                if (t4 == 0) { wm[warp][g + k * 8] = m[k]; wl[warp][g + k * 8] = l[k]; }
             }
             __syncthreads();
-            float M[2], L[2];
+            float M[kK], L[kK];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < kK; ++k) {
                 const int r = g + k * 8;
                 M[k] = wm[0][r];
 #pragma unroll
@@ -475,14 +486,14 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                 const float base = M[k] == -INFINITY ? 0.0f : M[k];
                 L[k] = 0.0f;
 #pragma unroll
-                for (int w = 0; w < C_::kWarps; ++w) L[k] = fmaf(wl[w][r], exp2f(wm[w][r] - base), L[k]);
-                const float f = exp2f((k ? m1 : m0) - base);
+                for (int w = 0; w < C_::kWarps; ++w) L[k] = fmaf(wl[w][r], pow2(wm[w][r] - base), L[k]);
+                const float f = pow2(m[k] - base);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) { o[n][2 * k] *= f; o[n][2 * k + 1] *= f; }
             }
             const auto put = [&](int b) {
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+                for (int k = 0; k < kK; ++k)
                     if (g + k * 8 < rows) {
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
@@ -492,7 +503,7 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
             };
             const auto add = [&](int b) {
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+                for (int k = 0; k < kK; ++k)
                     if (g + k * 8 < rows) {
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
@@ -512,11 +523,11 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                 if (a.split > 1) {
                     put(0);
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
+                    for (int k = 0; k < kK; ++k)
                         if (t4 == 0) { wm[0][g + k * 8] = M[k]; wl[0][g + k * 8] = L[k]; }
                 }
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
+                for (int k = 0; k < kK; ++k) {
                     const int r = g + k * 8;
                     if (r >= rows || a.split > 1) continue;
                     if (complete) {
@@ -588,10 +599,10 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
 #pragma unroll
                     for (int d = 2; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
                     const float base = mx == -INFINITY ? 0.0f : mx;
-                    f[r] = exp2f(m[r] - base);
+                    f[r] = pow2(m[r] - base);
                     moved |= m[r] != mx;
                     m[r] = mx;
-                    const float e = exp2f(sc[r] - base);
+                    const float e = pow2(sc[r] - base);
                     l[r] = fmaf(l[r], f[r], e);
                     if ((lane & 1) == 0) w[r * kRun + key] = e;
                 }
@@ -646,8 +657,8 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                 const float base = M == -INFINITY ? 0.0f : M;
                 l[r] = 0.0f;
 #pragma unroll
-                for (int w2 = 0; w2 < C_::kWarps; ++w2) l[r] = fmaf(wl[w2][r], exp2f(wm[w2][r] - base), l[r]);
-                const float f = exp2f(m[r] - base);
+                for (int w2 = 0; w2 < C_::kWarps; ++w2) l[r] = fmaf(wl[w2][r], pow2(wm[w2][r] - base), l[r]);
+                const float f = pow2(m[r] - base);
                 m[r] = M;
 #pragma unroll
                 for (int v = 0; v < V; ++v) o[r][v] *= f;
@@ -714,7 +725,7 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                 const float base = M == -INFINITY ? 0.0f : M;
                 float L = 0.0f, v = 0.0f;
                 for (int k = 0; k < a.split; ++k) {
-                    const float f = exp2f(*cl.map_shared_rank(&wm[0][r], k) - base);
+                    const float f = pow2(*cl.map_shared_rank(&wm[0][r], k) - base);
                     L = fmaf(*cl.map_shared_rank(&wl[0][r], k), f, L);
                     v = fmaf(*cl.map_shared_rank(mg + r * C_::kMergeRow + j, k), f, v);
                 }
@@ -900,10 +911,10 @@ halo_status launch(const PagedArgs& args, const LaunchPlan& p, cudaStream_t st) 
 template <typename T, int DP, typename F>
 auto by_rows(const halo_paged_shape& sh, F f) {
     using D = std::integral_constant<int, DP>;
+    const int G = sh.n_heads / sh.n_kv_heads;
     if constexpr (sizeof(T) == 2) {
-        return f(T(), D(), std::integral_constant<int, 16>());
+        return G <= 8 ? f(T(), D(), std::integral_constant<int, 8>()) : f(T(), D(), std::integral_constant<int, 16>());
     } else {
-        const int G = sh.n_heads / sh.n_kv_heads;
         if (G == 1) return f(T(), D(), std::integral_constant<int, 1>());
         if (G <= 4) return f(T(), D(), std::integral_constant<int, 4>());
         return f(T(), D(), std::integral_constant<int, 16>());
