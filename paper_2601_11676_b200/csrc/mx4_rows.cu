@@ -8,8 +8,8 @@
 // elements, byte (r % 32) * 16 + (r / 32) * 4 + j for row r of the 128 and block j of the 4, the order in which the
 // tensor cores take them from tensor memory (halo_product_mx4 copies a block there as it is).
 //
-// Four lanes hold a block of 32 (8 elements each), so a warp reads 256 consecutive elements, writes 128 consecutive
-// code bytes, and 16 lanes meet for one 4-byte word of scales.  A warp takes kRun such runs of one row at once: kRun
+// Four lanes hold a block of 32 (8 elements each), so a warp reads 256 consecutive elements and writes 128 consecutive
+// code bytes; one lane of four writes the block's scale byte.  A warp takes kRun such runs of one row at once: kRun
 // independent loads per lane in flight.
 #include <cuda_fp16.h>
 
@@ -50,16 +50,34 @@ __device__ __forceinline__ uint32_t top8(const Raw<T>& r) {
             top = max(top, max(max(r.w[i].x & 0x7fffffffu, r.w[i].y & 0x7fffffffu), max(r.w[i].z & 0x7fffffffu, r.w[i].w & 0x7fffffffu)));
         return top;
     } else {
-        const uint32_t m = 0x7fff7fffu;
-        const uint32_t two = __vmaxu2(__vmaxu2(r.w[0].x & m, r.w[0].y & m), __vmaxu2(r.w[0].z & m, r.w[0].w & m));
-        return max(two << 16, two & 0xffff0000u);
+        const __nv_bfloat162* v = reinterpret_cast<const __nv_bfloat162*>(&r.w[0]);
+        const __nv_bfloat162 two = __hmax2_nan(__hmax2_nan(__habs2(v[0]), __habs2(v[1])), __hmax2_nan(__habs2(v[2]), __habs2(v[3])));
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(&two);
+        return max(w << 16, w & 0xffff0000u);
     }
 }
-// two values -> two codes in a byte, the first in the low half (round to nearest even, 6 at most)
-__device__ __forceinline__ uint32_t e2m1x2(float lo, float hi) {
+// eight values -> eight codes, the first in the lowest half byte (round to nearest even, 6 at most)
+__device__ __forceinline__ uint32_t codes8(const float (&f)[8]) {
     uint32_t r;
-    asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u32.u8 %0, t;\n\t}" : "=r"(r) : "f"(hi), "f"(lo));
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
+        "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
+        : "=r"(r) : "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]));
     return r;
+}
+// eight codes -> eight values
+__device__ __forceinline__ void values8(uint32_t word, float (&f)[8]) {
+    uint32_t h[4];
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\tcvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(word));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+        f[2 * i] = v.x;
+        f[2 * i + 1] = v.y;
+    }
 }
 // 2^(code - 127); 255 is NaN
 __device__ __forceinline__ float scale_of(uint32_t code) {
@@ -70,52 +88,50 @@ constexpr int kRun = 4;                 // runs of 256 elements a warp takes at 
 constexpr int kWarps = kThreads / 32;
 
 // Warp w of the grid: row w / segs, run group w % segs.  The rows behind n_rows up to a multiple of 128 get scales of
-// zero.
-template <typename T>
+// zero.  FULL: d is a whole number of run groups.
+template <typename T, bool FULL>
 __global__ void __launch_bounds__(kThreads)
 quantize_mx4_kernel(int d, unsigned n_rows, unsigned segs, unsigned items, const T* __restrict__ W, uint32_t* __restrict__ Q,
-                    uint32_t* __restrict__ S) {
+                    uint8_t* __restrict__ S) {
     const unsigned item = blockIdx.x * kWarps + (threadIdx.x >> 5);
     if (item >= items) return;
     const int lane = threadIdx.x & 31;
     const unsigned row = item / segs;
     const int c0 = static_cast<int>(item - row * segs) * (256 * kRun) + lane * 8;
     const long long at = static_cast<long long>(row) * d + c0;
-    const bool real = row < n_rows;
+    const T* w = W + at;
+    uint32_t* q = Q + (at >> 3);
+    uint8_t* s = S + (static_cast<long long>(row >> 7) * (d >> 7) + (c0 >> 7)) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + ((c0 >> 5) & 3);
+    const bool real = row < n_rows, writes = (lane & 3) == 0;   // four lanes hold a block
     Raw<T> raw[kRun];
 #pragma unroll
     for (int i = 0; i < kRun; ++i)
-        if (real && c0 + i * 256 < d) raw[i] = fetch8(W + at + i * 256);
+        if (real && (FULL || c0 + i * 256 < d)) raw[i] = fetch8(w + i * 256);
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
-        if (c0 + i * 256 >= d) break;   // d is a multiple of 128: the 16 lanes of a word of scales leave together
-        uint32_t word = 0, scale = 0;
-        const uint32_t group = 0xffffu << (lane & 16);
+        if (!FULL && c0 + i * 256 >= d) break;   // d is a multiple of 128: the lanes of a block leave together
+        uint32_t scale = 0;
         if (real) {
+            const uint32_t group = 0xfu << (lane & 28);
             uint32_t top = top8(raw[i]);
             top = max(top, __shfl_xor_sync(group, top, 1));
             top = max(top, __shfl_xor_sync(group, top, 2));
             const uint32_t field = top >> 23;
-            scale = field == 255u ? 255u : field < 2u ? 0u : field - 2u;
-            const float inv = __uint_as_float((254u - min(scale, 252u)) << 23);   // 2^(127 - scale), exact
+            scale = max(field, 2u) - 2u;
+            const float inv = __uint_as_float((254u - scale) << 23);   // 2^(127 - scale), exact: scale <= 252
             float f[8];
             widen8(raw[i], f);
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) word |= e2m1x2(f[e] * inv, f[e + 1] * inv) << (e * 4);
-            if (scale == 255u) word = 0;
-            Q[(at + i * 256) >> 3] = word;
+            for (int e = 0; e < 8; ++e) f[e] *= inv;
+            uint32_t word = codes8(f);
+            if (field == 255u) { scale = 255u; word = 0; }             // a NaN or an infinity
+            q[i * 32] = word;
         }
-        uint32_t four = scale << (((lane >> 2) & 3) * 8);
-        four |= __shfl_xor_sync(group, four, 4);
-        four |= __shfl_xor_sync(group, four, 8);
-        if ((lane & 15) == 0) {
-            const long long block = static_cast<long long>(row >> 7) * (d >> 7) + ((c0 + i * 256) >> 7);
-            S[block * 128 + (row & 31) * 4 + ((row >> 5) & 3)] = four;
-        }
+        if (writes) s[i * 1024] = static_cast<uint8_t>(scale);
     }
 }
 
-template <typename T>
+template <typename T, bool FULL>
 __global__ void __launch_bounds__(kThreads)
 dequantize_mx4_kernel(int d, unsigned segs, unsigned items, const uint32_t* __restrict__ Q, const uint8_t* __restrict__ S,
                       T* __restrict__ W) {
@@ -125,27 +141,23 @@ dequantize_mx4_kernel(int d, unsigned segs, unsigned items, const uint32_t* __re
     const unsigned row = item / segs;
     const int c0 = static_cast<int>(item - row * segs) * (256 * kRun) + lane * 8;
     const long long at = static_cast<long long>(row) * d + c0;
-    const uint8_t* srow = S + static_cast<long long>(row >> 7) * (d >> 7) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4;
+    const uint32_t* q = Q + (at >> 3);
+    const uint8_t* s = S + (static_cast<long long>(row >> 7) * (d >> 7) + (c0 >> 7)) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + ((c0 >> 5) & 3);
     uint32_t word[kRun], byte[kRun];
 #pragma unroll
-    for (int i = 0; i < kRun; ++i) {
-        const int c = c0 + i * 256;
-        word[i] = c < d ? __ldg(Q + ((at + i * 256) >> 3)) : 0u;
-        byte[i] = c < d ? __ldg(srow + static_cast<long long>(c >> 7) * 512 + ((c >> 5) & 3)) : 0u;
-    }
+    for (int i = 0; i < kRun; ++i)
+        if (FULL || c0 + i * 256 < d) {
+            word[i] = __ldg(q + i * 32);
+            byte[i] = __ldg(s + i * 1024);
+        }
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
-        if (c0 + i * 256 >= d) break;
+        if (!FULL && c0 + i * 256 >= d) break;
         const float scale = scale_of(byte[i]);
         float f[8];
+        values8(word[i], f);
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-            uint32_t h;
-            asm("{\n\t.reg .b8 t;\n\tcvt.u8.u32 t, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, t;\n\t}" : "=r"(h) : "r"((word[i] >> (e * 4)) & 0xffu));
-            const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h));
-            f[e] = v.x * scale;
-            f[e + 1] = v.y * scale;
-        }
+        for (int e = 0; e < 8; ++e) f[e] *= scale;
         T* out = W + at + i * 256;
         if constexpr (sizeof(T) == 4) {
             *reinterpret_cast<float4*>(out) = make_float4(f[0], f[1], f[2], f[3]);
@@ -189,12 +201,15 @@ extern "C" halo_status halo_quantize_rows_mx4(int d_model, long long n_rows, hal
     const unsigned segs = segments(d_model), items = static_cast<unsigned>((n_rows + 127) / 128 * 128 * segs);
     const unsigned grid = (items + kWarps - 1) / kWarps;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const auto go = [&](auto kernel, auto* w) {
+        kernel<<<grid, kThreads, 0, st>>>(d_model, static_cast<unsigned>(n_rows), segs, items, w, static_cast<uint32_t*>(Q),
+                                          static_cast<uint8_t*>(scales));
+    };
+    const bool full = d_model % (256 * kRun) == 0;
     if (wdtype == HALO_BF16)
-        quantize_mx4_kernel<__nv_bfloat16><<<grid, kThreads, 0, st>>>(
-            d_model, static_cast<unsigned>(n_rows), segs, items, static_cast<const __nv_bfloat16*>(W), static_cast<uint32_t*>(Q), static_cast<uint32_t*>(scales));
+        go(full ? quantize_mx4_kernel<__nv_bfloat16, true> : quantize_mx4_kernel<__nv_bfloat16, false>, static_cast<const __nv_bfloat16*>(W));
     else
-        quantize_mx4_kernel<float><<<grid, kThreads, 0, st>>>(
-            d_model, static_cast<unsigned>(n_rows), segs, items, static_cast<const float*>(W), static_cast<uint32_t*>(Q), static_cast<uint32_t*>(scales));
+        go(full ? quantize_mx4_kernel<float, true> : quantize_mx4_kernel<float, false>, static_cast<const float*>(W));
     HALO_CHECK_LAUNCH();
     return HALO_OK;
 }
@@ -208,12 +223,14 @@ extern "C" halo_status halo_dequantize_rows_mx4(int d_model, long long n_rows, h
     const unsigned segs = segments(d_model), items = static_cast<unsigned>(n_rows * segs);
     const unsigned grid = (items + kWarps - 1) / kWarps;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const auto go = [&](auto kernel, auto* w) {
+        kernel<<<grid, kThreads, 0, st>>>(d_model, segs, items, static_cast<const uint32_t*>(Q), static_cast<const uint8_t*>(scales), w);
+    };
+    const bool full = d_model % (256 * kRun) == 0;
     if (wdtype == HALO_BF16)
-        dequantize_mx4_kernel<__nv_bfloat16><<<grid, kThreads, 0, st>>>(
-            d_model, segs, items, static_cast<const uint32_t*>(Q), static_cast<const uint8_t*>(scales), static_cast<__nv_bfloat16*>(W));
+        go(full ? dequantize_mx4_kernel<__nv_bfloat16, true> : dequantize_mx4_kernel<__nv_bfloat16, false>, static_cast<__nv_bfloat16*>(W));
     else
-        dequantize_mx4_kernel<float><<<grid, kThreads, 0, st>>>(
-            d_model, segs, items, static_cast<const uint32_t*>(Q), static_cast<const uint8_t*>(scales), static_cast<float*>(W));
+        go(full ? dequantize_mx4_kernel<float, true> : dequantize_mx4_kernel<float, false>, static_cast<float*>(W));
     HALO_CHECK_LAUNCH();
     return HALO_OK;
 }
