@@ -451,7 +451,10 @@ group_ffn_i4_ring_kernel(int d, int S, int G, const uint8_t* __restrict__ Q, con
     const long long total = static_cast<long long>(nk) * per_group;  // batches
     const int lo = static_cast<int>(total * blockIdx.x / gridDim.x);
     const int hi = static_cast<int>(total * (blockIdx.x + 1) / gridDim.x);
-    if (lo >= hi) return;
+    if (lo >= hi) {   // nothing to add, but the grid must not end before the kernels in front of it
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        return;
+    }
     const int n_it = hi - lo;
 
     if (tid == 0) {
@@ -569,6 +572,7 @@ group_ffn_i4_ring_kernel(int d, int S, int G, const uint8_t* __restrict__ Q, con
         if (slot >= 0) {
             if (slot != cur_slot) {
                 if (cur_slot >= 0) flush(cur_slot);
+    if (!dep_waited) asm volatile("griddepcontrol.wait;" ::: "memory");   // only groups out of range: as above
                 cur_slot = slot;
             }
             // phase 1: code rows 0..15 of the stage are the 8 gate rows then the 8 up rows (planes 0, 1 adjacent)

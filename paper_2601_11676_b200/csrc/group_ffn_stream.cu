@@ -69,7 +69,10 @@ group_ffn_stream_kernel(int d, int S, int G, const __nv_bfloat16* __restrict__ W
     const long long total = static_cast<long long>(nk) * per_group;  // batches
     const int lo = static_cast<int>(total * blockIdx.x / gridDim.x);
     const int hi = static_cast<int>(total * (blockIdx.x + 1) / gridDim.x);
-    if (lo >= hi) return;
+    if (lo >= hi) {   // nothing to add, but the grid must not end before the kernels in front of it
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        return;
+    }
     const int n_it = hi - lo;
 
     if (tid == 0) {
@@ -203,6 +206,7 @@ group_ffn_stream_kernel(int d, int S, int G, const __nv_bfloat16* __restrict__ W
         if (lane == 0) mbar_arrive(&hd.empty[s]);
     }
     if (cur_slot >= 0) flush(cur_slot);
+    if (!dep_waited) asm volatile("griddepcontrol.wait;" ::: "memory");   // only groups out of range: as above
     if (tid == 0 && *abort_flag) flag_status(dev_status, HALO_DEV_TIMEOUT);
 }
 

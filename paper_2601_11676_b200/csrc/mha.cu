@@ -395,11 +395,15 @@ mha_fused_kernel(int d, int H, int dh, int Lmax, int pos, const T* __restrict__ 
             if (e == h) found = 1;
             if ((e < 0 || e >= H) && h == 0 && r == 0) flag_status(dev_status, HALO_DEV_BAD_INDEX);
         }
-        if (!__syncthreads_or(found)) return;            // the same decision in every block of the cluster
+        if (!__syncthreads_or(found)) {                  // the same decision in every block of the cluster
+            asm volatile("griddepcontrol.wait;" ::: "memory");   // the grid must not end before the kernels in front of it
+            return;
+        }
         if (dev_of_group) {
             slot = dev_of_group[h] + 1;
             if (slot < 0 || slot > n_dev) {
                 if (tid == 0 && r == 0) flag_status(dev_status, HALO_DEV_BAD_INDEX);
+                asm volatile("griddepcontrol.wait;" ::: "memory");
                 return;
             }
         }
