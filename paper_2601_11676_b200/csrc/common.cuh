@@ -46,7 +46,28 @@ inline bool ensure_dynamic_smem(Kernel kernel, size_t bytes, bool (&done)[64]) {
         if (e__ != cudaSuccess) return HALO_ERR_CUDA;         \
     } while (0)
 
+// Launch as a programmatic dependent of whatever precedes on the stream: the launch itself is prepared while the preceding
+// kernel still runs.  The kernel calls chain_wait() before it touches global memory, in every thread block (also in those
+// that have nothing to do), so it sees all of the preceding kernel's writes and does not end before it.  No kernel that
+// is launched this way releases its dependents early: another kernel behind it may read before it waits.
+template <typename... P, typename... A>
+inline halo_status launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cuda_status(cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...));
+}
+
 // ---- device helpers ------------------------------------------------------
+
+__device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll

@@ -94,6 +94,7 @@ mx4_one_kernel(int d, int n_rows, const uint8_t* __restrict__ Qx, const uint8_t*
     const int runs = d / 32;                       // of a row
     uint4* xs = reinterpret_cast<uint4*>(smem);    // [quarter of a run][run] 8 values, then [run] the token's scale
     float* sx = reinterpret_cast<float*>(xs + 4 * runs);
+    chain_wait();
     for (int b = tid; b < runs; b += kOneThreads) {
         const uint4 code = *reinterpret_cast<const uint4*>(Qx + b * 16);
         const uint32_t word[4] = {code.x, code.y, code.z, code.w};
@@ -257,6 +258,7 @@ mx4_line_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     tcgen05_fence_before_sync();
     __syncthreads();
     tcgen05_fence_after_sync();
+    chain_wait();
     volatile int* abort_flag = &bars.abort_flag;
     const uint32_t tmem = bars.tmem;
     Piece p;
@@ -494,6 +496,7 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     __syncthreads();
     cluster_sync_all();
     tcgen05_fence_after_sync();
+    chain_wait();
     volatile int* abort_flag = &bars.abort_flag;
     const uint32_t tmem = bars.tmem;
 
@@ -629,11 +632,9 @@ halo_status launch_one(const Operands& o, T* y) {
     if (!ensure_dynamic_smem(mx4_one_kernel<T>, kOneSmem, done)) return HALO_ERR_CUDA;
     static_assert(2 * HALO_MX4_MAX_WIDTH + HALO_MX4_MAX_WIDTH / 8 <= kOneSmem, "the widest row fits");
     const int most = 3 * kSmCount, want = (o.n_rows + 15) / 16;   // a pair of rows per warp at least
-    mx4_one_kernel<T><<<want < most ? want : most, kOneThreads, 2 * o.d + o.d / 8, o.st>>>(
-        o.d, o.n_rows, static_cast<const uint8_t*>(o.Qx), static_cast<const uint8_t*>(o.Sx), static_cast<const uint8_t*>(o.Qw),
-        static_cast<const uint8_t*>(o.Sw), y);
-    HALO_CHECK_LAUNCH();
-    return HALO_OK;
+    return launch_chained(mx4_one_kernel<T>, want < most ? want : most, kOneThreads, 2 * o.d + o.d / 8, o.st, o.d, o.n_rows,
+                          static_cast<const uint8_t*>(o.Qx), static_cast<const uint8_t*>(o.Sx), static_cast<const uint8_t*>(o.Qw),
+                          static_cast<const uint8_t*>(o.Sw), y);
 }
 
 template <typename T, int NT, int STAGES>
@@ -647,10 +648,8 @@ halo_status launch_line(const Operands& o, T* y) {
         !make_byte_map(&map_x, o.Qx, o.n_tok, o.d / 2, kStageK / 2, NT))
         return HALO_ERR_CUDA;
     const int groups = (o.n_rows + 31) / 32, blocks = groups < kSmCount ? groups : kSmCount;
-    mx4_line_kernel<T, NT, STAGES><<<blocks, kThreads, R::kSmem, o.st>>>(
-        map_w, map_g, map_x, o.d, o.n_tok, o.n_rows, static_cast<const uint8_t*>(o.Sw), static_cast<const uint8_t*>(o.Sx), y, o.status);
-    HALO_CHECK_LAUNCH();
-    return HALO_OK;
+    return launch_chained(mx4_line_kernel<T, NT, STAGES>, blocks, kThreads, R::kSmem, o.st, map_w, map_g, map_x, o.d, o.n_tok, o.n_rows,
+                          static_cast<const uint8_t*>(o.Sw), static_cast<const uint8_t*>(o.Sx), y, o.status);
 }
 
 template <typename T>
@@ -669,13 +668,15 @@ halo_status launch_pair(const Operands& o, T* y) {
     cfg.blockDim = dim3(kPairThreads);
     cfg.dynamicSmemBytes = PairRing::kSmem;
     cfg.stream = o.st;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = 2;
     at[0].val.clusterDim.y = 1;
     at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // as in launch_chained
+    at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     return cuda_status(cudaLaunchKernelEx(&cfg, mx4_pair_kernel<T>, map_w, map_x, map_sw, map_sx, o.d, o.n_tok, o.n_rows, y,
                                           o.status));
 }

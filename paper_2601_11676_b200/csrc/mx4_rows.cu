@@ -94,6 +94,7 @@ __global__ void __launch_bounds__(kThreads)
 quantize_mx4_kernel(int d, unsigned n_rows, unsigned segs, unsigned items, const T* __restrict__ W, uint32_t* __restrict__ Q,
                     uint8_t* __restrict__ S) {
     const unsigned item = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    chain_wait();
     if (item >= items) return;
     const int lane = threadIdx.x & 31;
     const unsigned row = item / segs;
@@ -136,6 +137,7 @@ __global__ void __launch_bounds__(kThreads)
 dequantize_mx4_kernel(int d, unsigned segs, unsigned items, const uint32_t* __restrict__ Q, const uint8_t* __restrict__ S,
                       T* __restrict__ W) {
     const unsigned item = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    chain_wait();
     if (item >= items) return;
     const int lane = threadIdx.x & 31;
     const unsigned row = item / segs;
@@ -202,16 +204,13 @@ extern "C" halo_status halo_quantize_rows_mx4(int d_model, long long n_rows, hal
     const unsigned grid = (items + kWarps - 1) / kWarps;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const auto go = [&](auto kernel, auto* w) {
-        kernel<<<grid, kThreads, 0, st>>>(d_model, static_cast<unsigned>(n_rows), segs, items, w, static_cast<uint32_t*>(Q),
-                                          static_cast<uint8_t*>(scales));
+        return launch_chained(kernel, grid, kThreads, 0, st, d_model, static_cast<unsigned>(n_rows), segs, items, w,
+                              static_cast<uint32_t*>(Q), static_cast<uint8_t*>(scales));
     };
     const bool full = d_model % (256 * kRun) == 0;
     if (wdtype == HALO_BF16)
-        go(full ? quantize_mx4_kernel<__nv_bfloat16, true> : quantize_mx4_kernel<__nv_bfloat16, false>, static_cast<const __nv_bfloat16*>(W));
-    else
-        go(full ? quantize_mx4_kernel<float, true> : quantize_mx4_kernel<float, false>, static_cast<const float*>(W));
-    HALO_CHECK_LAUNCH();
-    return HALO_OK;
+        return go(full ? quantize_mx4_kernel<__nv_bfloat16, true> : quantize_mx4_kernel<__nv_bfloat16, false>, static_cast<const __nv_bfloat16*>(W));
+    return go(full ? quantize_mx4_kernel<float, true> : quantize_mx4_kernel<float, false>, static_cast<const float*>(W));
 }
 
 extern "C" halo_status halo_dequantize_rows_mx4(int d_model, long long n_rows, halo_dtype wdtype, const void* Q,
@@ -224,13 +223,11 @@ extern "C" halo_status halo_dequantize_rows_mx4(int d_model, long long n_rows, h
     const unsigned grid = (items + kWarps - 1) / kWarps;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const auto go = [&](auto kernel, auto* w) {
-        kernel<<<grid, kThreads, 0, st>>>(d_model, segs, items, static_cast<const uint32_t*>(Q), static_cast<const uint8_t*>(scales), w);
+        return launch_chained(kernel, grid, kThreads, 0, st, d_model, segs, items, static_cast<const uint32_t*>(Q),
+                              static_cast<const uint8_t*>(scales), w);
     };
     const bool full = d_model % (256 * kRun) == 0;
     if (wdtype == HALO_BF16)
-        go(full ? dequantize_mx4_kernel<__nv_bfloat16, true> : dequantize_mx4_kernel<__nv_bfloat16, false>, static_cast<__nv_bfloat16*>(W));
-    else
-        go(full ? dequantize_mx4_kernel<float, true> : dequantize_mx4_kernel<float, false>, static_cast<float*>(W));
-    HALO_CHECK_LAUNCH();
-    return HALO_OK;
+        return go(full ? dequantize_mx4_kernel<__nv_bfloat16, true> : dequantize_mx4_kernel<__nv_bfloat16, false>, static_cast<__nv_bfloat16*>(W));
+    return go(full ? dequantize_mx4_kernel<float, true> : dequantize_mx4_kernel<float, false>, static_cast<float*>(W));
 }

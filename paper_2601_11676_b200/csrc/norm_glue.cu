@@ -92,6 +92,7 @@ norm_glue_kernel(const __grid_constant__ GlueArgs a) {
     __shared__ float sh[2][32];
     const int t = ONE_WARP ? threadIdx.x & 31 : threadIdx.x, n = ONE_WARP ? 32 : blockDim.x;
     const long long row = ONE_WARP ? static_cast<long long>(blockIdx.x) * kWarpRows + (threadIdx.x >> 5) : blockIdx.x;
+    chain_wait();
     if (row >= a.n_tok) return;   // whole warps, and only where a row is one warp
     const long long base = row * a.d;
     const int units = a.d / 8;
@@ -175,9 +176,7 @@ norm_glue_kernel(const __grid_constant__ GlueArgs a) {
 template <typename TY, typename T, int IT, bool ONE_WARP>
 halo_status go(const GlueArgs& a, int threads, cudaStream_t st) {
     const int blocks = ONE_WARP ? (a.n_tok + kWarpRows - 1) / kWarpRows : a.n_tok;
-    norm_glue_kernel<TY, T, IT, ONE_WARP><<<blocks, threads, 0, st>>>(a);
-    HALO_CHECK_LAUNCH();
-    return HALO_OK;
+    return launch_chained(norm_glue_kernel<TY, T, IT, ONE_WARP>, blocks, threads, 0, st, a);
 }
 template <typename TY, typename T>
 halo_status launch(const GlueArgs& a, cudaStream_t st) {

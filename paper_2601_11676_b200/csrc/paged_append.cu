@@ -45,6 +45,7 @@ paged_append_kernel(const __grid_constant__ AppendArgs a, int parts, int units, 
     extern __shared__ float2 turn[];   // [rotary / 2] cosine, sine
     const int tid = threadIdx.x;
     const int tok = blockIdx.x / parts, part = blockIdx.x % parts;
+    chain_wait();
     // everything that depends on the token alone is requested at once
     const int pos = __ldg(a.pos + tok);
     const int s = a.seq ? __ldg(a.seq + tok) : tok;
@@ -154,14 +155,10 @@ halo_status launch(const AppendArgs& a, int n_tok, int interleaved, cudaStream_t
     parts = parts < 1 ? 1 : parts > most ? most : parts;
     const unsigned grid = static_cast<unsigned>(n_tok) * parts;
     const size_t smem = sizeof(float2) * (a.rotary / 2);
-    if (interleaved)
-        paged_append_kernel<T, true, true><<<grid, threads, smem, st>>>(a, parts, units, lanes);
-    else if (wide)
-        paged_append_kernel<T, false, true><<<grid, threads, smem, st>>>(a, parts, units, lanes);
-    else
-        paged_append_kernel<T, false, false><<<grid, threads, smem, st>>>(a, parts, units, lanes);
-    HALO_CHECK_LAUNCH();
-    return HALO_OK;
+    const auto kernel = interleaved ? paged_append_kernel<T, true, true>
+                        : wide      ? paged_append_kernel<T, false, true>
+                                    : paged_append_kernel<T, false, false>;
+    return launch_chained(kernel, grid, threads, smem, st, a, parts, units, lanes);
 }
 
 }  // namespace

@@ -251,6 +251,7 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
 
     // Only the join may start early: another kernel behind this one may read before it waits.
     if (!a.split && gridDim.x > 1) asm volatile("griddepcontrol.launch_dependents;");
+    chain_wait();
     Walk<C_::kTile> con, iss;     // the piece that is summed, the piece whose rows are fetched
     long long total = 0;
     if (a.split) {
@@ -758,7 +759,7 @@ __global__ void __launch_bounds__(THREADS) paged_mha_join_kernel(const __grid_co
     __shared__ float part[kGroups > 1 ? THREADS : 1];
     extern __shared__ float weight[];   // [pieces]
     const int r = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c0 = blockIdx.x;
-    asm volatile("griddepcontrol.wait;" ::: "memory");   // in every block: this grid may not end before the first one
+    chain_wait();   // in every block: this grid may not end before the first one
     const int4 cut_ = __ldcg(reinterpret_cast<const int4*>(a.cuts + c0));
     const int4 line = __ldcg(reinterpret_cast<const int4*>(a.cuts + c0) + 1);
     const long long total = __ldcg(&a.cuts[0].total);
@@ -866,17 +867,8 @@ size_t workspace_of(const LaunchPlan& p) {
 
 template <typename T, int DP, int THREADS>
 halo_status launch_join(const PagedArgs& a, const LaunchPlan& p, cudaStream_t st) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(p.blocks - 1, p.rows);
-    cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = sizeof(float) * p.blocks;
-    cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    return cuda_status(cudaLaunchKernelEx(&cfg, paged_mha_join_kernel<T, DP, THREADS>, a, p.blocks));
+    return launch_chained(paged_mha_join_kernel<T, DP, THREADS>, dim3(p.blocks - 1, p.rows), THREADS, sizeof(float) * p.blocks, st, a,
+                          p.blocks);
 }
 
 template <typename T, int DP, int GR>
@@ -894,13 +886,15 @@ halo_status launch(const PagedArgs& args, const LaunchPlan& p, cudaStream_t st) 
     cfg.blockDim = dim3(C_::kWarps * 32);
     cfg.dynamicSmemBytes = C_::kRings + p.merge;
     cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = p.split > 1 ? p.split : 1;
-    at[0].val.clusterDim.y = 1;
-    at[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // as in launch_chained
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = p.split > 1 ? p.split : 1;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = p.split > 1 ? 1 : 0;
+    cfg.numAttrs = p.split > 1 ? 2 : 1;
     const halo_status rc = cuda_status(cudaLaunchKernelEx(&cfg, paged_mha_kernel<T, DP, GR>, a));
     if (rc != HALO_OK || p.split || p.blocks < 2) return rc;
     // few items, many pieces each: several groups of threads

@@ -522,3 +522,51 @@ def test_paged_attention_agrees_with_group_mha_on_a_dense_cache():
     out, _, bad = attend(sh, q, K[None], V[None], table, n, dh ** -0.5)
     y = out.view(1, H * dh).double() @ Wo.double().t()
     assert bad == 0 and float((y - P.double()).abs().max()) <= 2e-2 * float(P.double().square().mean().sqrt())
+
+
+@pytest.mark.parametrize("form", ["bf16", "i4"])
+@pytest.mark.parametrize("kept", ["all", "none", "bad"])
+def test_calls_behind_a_group_ffn_see_its_result_and_what_ran_before_it(form, kept):
+    """norm_glue -> group FFN -> norm_glue on the partial slot, back to back without a wait, over and over in one buffer: a
+    later call that started before an earlier one had ended would read the values of another turn.  The FFN kernels
+    overlap with their neighbours on purpose, and with no (or no valid) group in the list they have nothing to wait for."""
+    d, F, S, turns = 2048, 1024, 64, 40
+    G, t = F // S, torch.bfloat16
+    g = gen(31)
+    sh = B.ffn_shape(d, F, S, B.BF16)
+    W = randn(g, (G, 3, S, d), t) * 0.02
+    Q, sc = torch.empty((G, 3, S, d // 2), dtype=torch.uint8, device=DEV), torch.empty((G, 3, S, d // 128), dtype=t, device=DEV)
+    B.halo_quantize_weights_i4(sh, W, Q, sc)
+    kl = torch.arange(G, dtype=torch.int32, device=DEV) + (1000 if kept == "bad" else 0)
+    nk = torch.tensor([0 if kept == "none" else G], dtype=torch.int32, device=DEV)
+    norm = B.norm_shape(d, 1e-5, B.F32, B.BF16)
+    w = torch.rand((turns, d), device=DEV, generator=g).to(t)
+    h0 = randn(g, (1, d), torch.float32)
+
+    def run(wait):
+        h, x, P = h0.clone(), torch.zeros((1, d), dtype=t, device=DEV), torch.full((1, 1, d), 1e30, device=DEV)
+        st, seen = status(), torch.empty((turns, 2, d), dtype=t, device=DEV)
+        for i in range(turns):
+            B.halo_norm_glue(norm, h, None, None, None, 1.0, w[i], h, x)
+            if wait:
+                torch.cuda.synchronize()
+            if form == "bf16":
+                B.halo_group_ffn(sh, W, x, 1, kl, nk, None, 0, P, None, st)
+            else:
+                B.halo_group_ffn_i4(sh, Q, sc, x, 1, kl, nk, None, 0, P, st)
+            if wait:
+                torch.cuda.synchronize()
+            B.halo_norm_glue(norm, h, P, None, None, 1.0, w[i], h, seen[i, 0:1])
+            if wait:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return h, seen[:, 0].float(), int(st.item())
+
+    h1, seen1, st1 = run(True)
+    h2, seen2, st2 = run(False)
+    assert st1 == st2 == (B.DEV_BAD_INDEX if kept == "bad" else 0)
+    if kept != "all":
+        assert torch.equal(h1, h0) and torch.equal(h2, h0) and torch.equal(seen1, seen2)
+    else:   # atomic sums: the order of additions differs between runs
+        assert float((h1 - h2).abs().max()) <= 1e-3 * float(h1.abs().max())
+        assert float((seen1 - seen2).abs().max()) <= 0.02 * float(seen1.abs().max())
