@@ -440,9 +440,9 @@ halo_status halo_group_lm_head_i4(const halo_lm_shape* shape, const void* Q, con
  *   keep device uint8 [n_heads] or NULL: heads with 0 (what halo_select_groups lost) give zeros; K/V heads of which
  *     every head is lost are not read.
  *   A row without positions (length 0, a lost head, scores that are all -infinity) gives zeros and lse = -infinity.
- *   Cache rows behind the length are never read into the result, whatever they hold.  In fp32 an infinity among the
- *   values that are read may come out as NaN (products are formed from two parts); bf16 follows the formula.
- *   fp32 sums and softmax; bf16 caches: weights rounded to bf16 before they meet the values.
+ *   Cache rows behind the length are not read, whatever they hold.
+ *   fp32 sums and softmax (a weight below 2^-126 of the largest counts as 0); bf16 caches: weights rounded to bf16 before
+ *   they meet the values.
  *   A length that is negative or behind the table counts as 0, positions on a page out of range are left out; both set
  *   HALO_DEV_BAD_INDEX.
  *   workspace: halo_paged_mha_workspace_bytes(shape, n_seq) bytes, device; calls that may overlap on the GPU need one

@@ -103,7 +103,7 @@ struct Call {
         const size_t d = size.size();
         const bool fits = (d == 2 && size[1] == width) || (d == 3 && size[1] * size[2] == width && (size[1] == 1 || step[1] == size[2]));
         if (!fits || size[0] != n || (width > 1 && step[d - 1] != 1)) refuse(what, name, "has to be rows as wide as the shape says, dense in themselves", o);
-        stride = step[0] > width || n > 1 ? step[0] : width;
+        stride = n > 1 ? step[0] : width;
         return t.data_ptr();
     }
     // [n_pages][n_kv_heads][page_size][head_dim], dense or one page every page_stride elements

@@ -69,6 +69,8 @@ APPEND = [
     ("f32", 3, 1, 48, 16, 20, True, [1, 15, 16], None, True),
     ("f32", 4, 2, 32, 1, 24, False, [0, 1, 2, 3, 4], [0, 0, 0, 1, 1], False),                  # pages of one position
     ("f32", 2, 2, 64, 16, 10, False, [11, 33], None, False),
+    ("bf16", 6, 3, 48, 48, 20, True, [47, 48, 95, 1], None, False),                           # a chunk ends behind the last pair
+    ("bf16", 16, 2, 128, 16, 128, False, list(range(128)) * 6, [i // 128 for i in range(768)], True),   # more tokens than thread blocks at once
 ]
 
 
@@ -183,6 +185,11 @@ ATTENTION = [
     ("f32", 6, 2, 48, 5, [64, 65, 31], False),
     ("f32", 17, 1, 256, 16, [129, 40], False),
     ("f32", 4, 4, 256, 128, [1030], False),
+    ("bf16", 4, 2, 64, 48, [48, 49, 400, 0, 97], False),                      # whole runs, no power of two
+    ("bf16", 2, 1, 64, 16, [i % 23 for i in range(700)], False),              # more sequences than thread blocks
+    ("bf16", 32, 1, 128, 16, [130, 7], True),
+    ("f32", 3, 3, 64, 16, [(i * 7) % 40 for i in range(400)], False),
+    ("f32", 12, 2, 64, 24, [333, 20, 1], True),
 ]
 
 
@@ -372,6 +379,54 @@ def test_attention_captured_into_a_graph_and_on_another_stream():
         side.synchronize()
         assert torch.equal(out, replayed) and torch.equal(K, K1)
         check_attention(q_out, K, V, table, lens, 0.125, out, None, None, u, 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_on_two_streams_at_once_and_for_single_rows(dtype):
+    """Two calls that overlap, each with its own workspace and outputs; then rows cut out of wider tensors, one at a time."""
+    t, code, u = TYPES[dtype]
+    g, H, Hk, dh, page, lens = gen(17), 8, 2, 64, 16, [3000, 12, 700]
+    table, n_pages = block_table(g, lens, page)
+    K, V, _ = caches(g, t, n_pages, Hk, page, dh, False)
+    sh = B.paged_shape(H, Hk, dh, page, n_pages, table.shape[1], code)
+    n = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    qs = [randn(g, (3, H, dh), t) for _ in range(2)]
+    alone = [attend(sh, q, K, V, table, n, 0.125)[0] for q in qs]
+    streams = [torch.cuda.Stream() for _ in qs]
+    outs = [torch.empty_like(q) for q in qs]
+    ws = [torch.empty(B.halo_paged_mha_workspace_bytes(sh, 3) + 16, dtype=torch.uint8, device=DEV) for _ in qs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for q, o, w, st in zip(qs, outs, ws, streams):
+            B.halo_paged_mha(sh, q, K, V, table, n, 0.125, o, w, stream=st)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], alone[0]) and torch.equal(outs[1], alone[1])
+    wide = torch.zeros((1, H * dh + 5), dtype=t, device=DEV)
+    wide[0, : H * dh] = qs[0][2].flatten()
+    out = torch.empty((1, H, dh), dtype=t, device=DEV)
+    B.halo_paged_mha(sh, wide[:, : H * dh], K, V, table[2:], n[2:], 0.125, out, ws[0])
+    torch.cuda.synchronize()
+    assert float((out - alone[0][2]).abs().max()) <= 2e-2
+
+
+def test_the_largest_number_of_sequences():
+    t, code, u = TYPES["bf16"]
+    g, n_seq, page, dh = gen(18), 8192, 16, 16
+    K, V, _ = caches(g, t, 64, 1, page, dh, False)
+    table = torch.randint(0, 64, (n_seq, 2), dtype=torch.int32, device=DEV, generator=g)
+    lens = torch.randint(0, 33, (n_seq,), dtype=torch.int32, device=DEV, generator=g)
+    sh = B.paged_shape(1, 1, dh, page, 64, 2, code)
+    q = randn(g, (n_seq, 1, dh), t)
+    out, lse, bad = attend(sh, q, K, V, table, lens, 0.25)
+    assert bad == 0
+    k = K[table.long()].reshape(n_seq, 2 * page, dh).double()
+    v = V[table.long()].reshape(n_seq, 2 * page, dh).double()
+    there = torch.arange(2 * page, device=DEV)[None] < lens[:, None]
+    score = torch.einsum("nd,npd->np", q[:, 0].double(), k) * 0.25
+    w = torch.softmax(score.masked_fill(~there, -1e30), -1) * (lens > 0)[:, None]
+    ref, size = torch.einsum("np,npd->nd", w, v), torch.einsum("np,npd->nd", w, v.abs())
+    assert ((out[:, 0].double() - ref).abs() <= (2.0 ** -8 + 1e-4) * size + u * ref.abs()).all()
+    assert torch.equal(torch.isinf(lse[:, 0]), lens == 0)
 
 
 # ---- the residual between blocks ------------------------------------------------------------------------------------

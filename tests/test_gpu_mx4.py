@@ -122,3 +122,35 @@ def test_product_places_every_element_and_scale():
         y = torch.empty((T_, n), device=DEV)
         B.halo_product_mx4(d, T_, n, Qx, Sx, Qw, Sw, B.F32, y)
         assert torch.equal(y.double(), x.double() @ wv.t())
+
+
+@pytest.mark.parametrize("T", [1, 7, 300])
+def test_quantise_and_product_captured_into_a_graph_and_on_another_stream(T):
+    """One captured pair of calls replayed on new activations; the same bits as calls on a side stream."""
+    g, n, d = gen(9), 520, 1152
+    Qw, Sw = quantize(torch.randn((n, d), generator=g, device=DEV))
+    x = torch.randn((T, d), generator=g, device=DEV).bfloat16()
+    Q, S = torch.empty((T, d // 2), dtype=torch.uint8, device=DEV), torch.empty(B.halo_mx4_scale_bytes(d, T), dtype=torch.uint8, device=DEV)
+    y, side = torch.empty((T, n), dtype=torch.bfloat16, device=DEV), torch.cuda.Stream()
+
+    def step(stream=None):
+        B.halo_quantize_rows_mx4(d, T, B.BF16, x, Q, S, stream=stream)
+        B.halo_product_mx4(d, T, n, Q, S, Qw, Sw, B.BF16, y, stream=stream)
+
+    side.wait_stream(torch.cuda.current_stream())
+    step(side)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        x.copy_(torch.randn((T, d), generator=g, device=DEV))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone()
+        side.wait_stream(torch.cuda.current_stream())
+        step(side)
+        side.synchronize()
+        assert torch.equal(got, y)
+        ref = values(Q, S, T, d) @ values(Qw, Sw, n, d).t()
+        assert ((got.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 1e-4 * ref.abs().max()).all()
