@@ -422,7 +422,8 @@ halo_status halo_group_lm_head_i4(const halo_lm_shape* shape, const void* Q, con
  * halo_paged_kv_append: for every token t with pos[t] >= 0: its keys, turned by the position, and its values are
  *   written at position pos[t] of sequence seq_of_tok[t], its queries, turned, to q_out.
  *   q, q_out device [n_tok] rows of n_heads * head_dim; k, v rows of n_kv_heads * head_dim; rows every *_stride elements
- *     (a whole number of 16 bytes), so that they may lie side by side in one projection's output.  q_out may be q.
+ *     (a whole number of 16 bytes), so that they may lie side by side in one projection's output.  q_out may be q
+ *     (with the same stride).
  *     q and q_out NULL: keys and values only.
  *   pos device int32 [n_tok]; a negative position marks a padding row: nothing is written for it.
  *   seq_of_tok device int32 [n_tok], or NULL: token t belongs to sequence t (n_tok <= n_seq).

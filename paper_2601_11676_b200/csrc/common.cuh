@@ -4,6 +4,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+#include <string.h>
 
 #include "halo.h"
 
@@ -68,6 +69,28 @@ inline halo_status launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, s
 // ---- device helpers ------------------------------------------------------
 
 __device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// A read-only load that stays behind chain_wait(): the compiler may move a __ldg(), which it takes for a load of memory
+// that never changes, in front of the wait.
+template <typename T>
+__device__ __forceinline__ T ldg_waited(const T* p) {
+    static_assert(sizeof(T) == 1 || sizeof(T) == 4 || sizeof(T) == 8, "plain words");
+    T v;
+    if constexpr (sizeof(T) == 1) {
+        uint32_t w;
+        asm volatile("ld.global.nc.u8 %0, [%1];" : "=r"(w) : "l"(p));
+        v = static_cast<T>(w);
+    } else if constexpr (sizeof(T) == 4) {
+        uint32_t w;
+        asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(w) : "l"(p));
+        memcpy(&v, &w, 4);
+    } else {
+        unsigned long long w;
+        asm volatile("ld.global.nc.u64 %0, [%1];" : "=l"(w) : "l"(p));
+        memcpy(&v, &w, 8);
+    }
+    return v;
+}
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll

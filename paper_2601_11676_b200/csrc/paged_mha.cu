@@ -17,6 +17,11 @@
 //     kernel, not the tensor pipe.  Weights are rounded to bf16 for the second product (relative 2^-8, like the output);
 //     their sum is taken in fp32 before that rounding.
 //   fp32: fused multiply-adds, two lanes per position for the scores, a column per lane for the weighted sums.
+//
+// bf16, 32 / 8 heads of 128: one sequence of 131071 positions 86 us + 4 for the join (537 MB: 6.2 TB/s in the first
+// kernel, HBM), 64 sequences of up to 4096 positions 89 + 5 us (a piece's start and meeting); one sequence of 700
+// positions, 32 / 4 heads of 64: 6.1 us (launch, one chain of loads, a cluster's meeting); fp32, 7 sequences of up to
+// 1500 positions, 8 / 8 heads of 64: 9.5 us (the same chain, 18 MB).
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -91,8 +96,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 constexpr int kRun = 16;            // positions of a tile that one warp takes
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr int kSlotHead = 32;       // floats in front of a slot's values: maxima, sums
-// Shapes per element type, padded head size DP and padded number of query heads GR (bf16: 8 or 16 of 16 rows in use).  Ring bytes are what keeps
-// HBM busy: 6.5 TB/s x ~1 us of latency / 148 SMs = 44 KB have to be in flight; the shapes below hold 96 to 200 KB.
+// Shapes per element type, padded head size DP and padded number of query heads GR (bf16: 8 or 16 of 16 rows in use).
+// Ring bytes are what keeps HBM busy: 6.5 TB/s x ~1 us of latency / 148 SMs = 44 KB have to be in flight; the shapes below hold 96 to 200 KB.
 template <typename T, int DP, int GR>
 struct Cfg {
     static constexpr bool kF32 = sizeof(T) == 4;
@@ -115,7 +120,7 @@ struct Cfg {
 };
 
 __device__ __forceinline__ int valid_len(const PagedArgs& a, int s, bool flag) {
-    const int n = __ldg(a.seq_len + s);
+    const int n = ldg_waited(a.seq_len + s);
     if (n < 0 || static_cast<long long>(n) > static_cast<long long>(a.max_pages) * a.page_size) {
         if (flag) flag_status(a.status, HALO_DEV_BAD_INDEX);
         return 0;
@@ -290,7 +295,7 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
     const auto page_at = [&]() {   // page of this lane's position of the next run, -1 behind the end
         const int p = it * C_::kTile + warp * kRun + (lane & 15);
         if (iss.left <= 0 || p >= iss.reach) return -1;
-        return __ldg(a.table + static_cast<long long>(iss.s) * a.max_pages + (a.page_shift >= 0 ? p >> a.page_shift : p / a.page_size));
+        return ldg_waited(a.table + static_cast<long long>(iss.s) * a.max_pages + (a.page_shift >= 0 ? p >> a.page_shift : p / a.page_size));
     };
     int page_next = page_at();
     bool bad = false;
@@ -382,7 +387,7 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                 const T* q = qrow + static_cast<long long>(r) * a.dh + (j >> 1) * 8 + t4 * 2;
 #pragma unroll
                 for (int k = 0; k < DP / 16; ++k)
-                    qf[k][j] = there && k * 16 < a.dh ? __ldg(reinterpret_cast<const uint32_t*>(q + k * 16)) : 0u;   // dh % 16 == 0
+                    qf[k][j] = there && k * 16 < a.dh ? ldg_waited(reinterpret_cast<const uint32_t*>(q + k * 16)) : 0u;   // dh % 16 == 0
             }
             float o[NT][4];
 #pragma unroll
@@ -554,7 +559,7 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
             __syncwarp();
             for (int i = lane; i < GR * DP; i += 32) {
                 const int r = i / DP, c = i % DP;
-                q[i] = (r < rows && c < a.dh) ? __ldg(reinterpret_cast<const float*>(qrow) + static_cast<long long>(r) * a.dh + c) : 0.0f;
+                q[i] = (r < rows && c < a.dh) ? ldg_waited(reinterpret_cast<const float*>(qrow) + static_cast<long long>(r) * a.dh + c) : 0.0f;
             }
             __syncwarp();
             float o[GR][V], m[GR], l[GR];

@@ -316,3 +316,14 @@ def test_attention_block_binding_checks_tensors(lib):
             B.halo_quantize_rows_mx4(*args)
     with pytest.raises(ValueError):
         B.halo_product_mx4(128, 5, 5, Q, S, Q, S, B.F32, torch.zeros((5, 4)))
+
+
+def test_append_in_place_needs_one_stride(lib):
+    """q_out = q with another stride would write a token's row over rows that are still to be read."""
+    sh = B.paged_shape(8, 2, 64, 16, 10, 4, B.BF16)
+
+    def append(n_tok, qs, qos):
+        return lib.halo_paged_kv_append(ctypes.byref(sh), n_tok, 3, 16, qs, 16, 128, 16, 128, 16, None, 16, 16, 64, 0, 16, qos, 16, 16,
+                                        None, None)
+
+    assert append(3, 512, 520) == -1 and append(2, 768, 512) == -1
