@@ -8,13 +8,15 @@
 // its own columns of scales: a stage is refilled only when the products that read its old scales have completed.
 //
 // Three kernels:
-//   mx4_one_kernel   one token, bound by HBM: exact fp16 products on the ordinary pipe, described at the kernel.
+//   mx4_one_kernel   one token and some thousand rows: exact fp16 products on the ordinary pipe, described at the kernel.
 //   mx4_line_kernel  up to 64 tokens, bound by HBM (0.53 bytes per weight element): the weight rows in groups of 32 form
 //     a line that is cut into equal pieces, one thread block per SM; whole outputs per thread block, so nothing has to
-//     be added up between thread blocks.
+//     be added up between thread blocks.  32000 x 4096: 16.1 us for up to 16 tokens, 4.3 TB/s of weights.
 //   mx4_pair_kernel  prompts, bound by the L2-to-SM traffic and the tensor pipe: pairs of SMs (cta_group::2) on tiles
 //     of 256 rows x 256 tokens; each SM fetches half of either operand, 35 KB per 16.8 M products and SM where a
-//     single SM's 128 x 256 tile takes 51 KB.
+//     single SM's 128 x 256 tile takes 51 KB.  4096 x 11008 x 4096: 70 us = 5.3 PFLOP/s, tensor pipe 68 % active; a
+//     stage takes 0.37 us and a tile 0.85 us beyond its stages (one accumulator: a second one would leave no tensor
+//     memory for the scales at this tile, and smaller tiles fetch more per product).
 //
 // Every wait is bounded; when one runs out the block's roles leave their loops, the copies in flight are waited for,
 // TMEM is freed and HALO_DEV_TIMEOUT is raised.
@@ -69,8 +71,10 @@ __device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint64_t desc) {
 // takes here) stay below 2^11 quarters.  So a byte of codes is one conversion to two fp16 values and one packed
 // multiply-add; the run's sum meets both scales in fp32.  The token sits in shared memory as fp16; a warp takes kRows
 // rows at once, a lane the runs lane, lane + 32, ... of them, with kAhead 16-byte loads per row in flight.  A thread
-// block's rows are neighbours: they share the lines of the scale blocks.  32000 x 4096: 16.1 us = 4.3 TB/s (17.1 with
-// integer products of bytes, dp4a and the byte permute as a table, which the wide multiplier bounds).
+// block's rows are neighbours: they share the lines of the scale blocks.  11008 x 4096: 7.3 us = 3.3 TB/s of weights, bound
+// by issue and by the latency of a warp's few rounds (32000 x 4096: 16.7 us = 4.2 TB/s; 17.1 with integer products of
+// bytes, dp4a and the byte permute as a table, which the wide multiplier bounds; loads of the next rows issued ahead of
+// the products 19.5, half as many loads in flight 20).
 constexpr int kOneThreads = 256;
 constexpr size_t kOneSmem = 140 * 1024;   // the widest row
 __device__ __forceinline__ float power(uint32_t byte) {   // 2^(byte - 127); 255 is NaN
@@ -95,8 +99,9 @@ mx4_one_kernel(int d, int n_rows, const uint8_t* __restrict__ Qx, const uint8_t*
     uint4* xs = reinterpret_cast<uint4*>(smem);    // [quarter of a run][run] 8 values, then [run] the token's scale
     float* sx = reinterpret_cast<float*>(xs + 4 * runs);
     chain_wait();
+    bool large = false;
     for (int b = tid; b < runs; b += kOneThreads) {
-        const uint4 code = *reinterpret_cast<const uint4*>(Qx + b * 16);
+        const uint4 code = ldg_stream16(Qx + b * 16);
         const uint32_t word[4] = {code.x, code.y, code.z, code.w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -104,9 +109,18 @@ mx4_one_kernel(int d, int n_rows, const uint8_t* __restrict__ Qx, const uint8_t*
             unpack(word[k], h);
             xs[k * runs + b] = *reinterpret_cast<uint4*>(h);
         }
-        sx[b] = power(Sx[(b >> 2) * 512 + (b & 3)]);
+        const uint32_t byte = ldg_waited(Sx + (b >> 2) * 512 + (b & 3));
+        large |= byte > 240u;
+        sx[b] = power(byte);
     }
-    __syncthreads();
+    // A run's sum times a scale near 2^127 would leave the range before a small scale of w brings it back: a token with
+    // such a scale is summed 2^-16 times its size (exact: scales are 2^-143 at least).
+    const bool reduced = __syncthreads_or(large);
+    if (reduced) {
+        for (int b = tid; b < runs; b += kOneThreads) sx[b] *= 0x1p-16f;
+        __syncthreads();
+    }
+    const float back = reduced ? 0x1p16f : 1.0f;
     const int first = static_cast<int>(static_cast<long long>(n_rows) * blockIdx.x / gridDim.x);
     const int end = static_cast<int>(static_cast<long long>(n_rows) * (blockIdx.x + 1) / gridDim.x);
     for (int r0 = first + warp * kRows; r0 < end; r0 += kWarps * kRows) {
@@ -128,7 +142,7 @@ mx4_one_kernel(int d, int n_rows, const uint8_t* __restrict__ Qx, const uint8_t*
                 for (int r = 0; r < kRows; ++r) {
                     const int b = b0 + i * 32 + lane;
                     code[i][r] = b < runs ? ldg_stream16(q[r] + b * 16) : make_uint4(0, 0, 0, 0);
-                    scale[i][r] = b < runs ? __ldg(sc[r] + (b >> 2) * 512 + (b & 3)) : 0u;
+                    scale[i][r] = b < runs ? ldg_waited(sc[r] + (b >> 2) * 512 + (b & 3)) : 0u;
                 }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
@@ -161,7 +175,7 @@ mx4_one_kernel(int d, int n_rows, const uint8_t* __restrict__ Qx, const uint8_t*
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
             const float v = warp_sum(sum[r]);
-            if (lane == 0 && r0 + r < end) y[r0 + r] = from_float<T>(v);
+            if (lane == 0 && r0 + r < end) y[r0 + r] = from_float<T>(v * back);
         }
     }
 }
@@ -684,13 +698,17 @@ halo_status launch_pair(const Operands& o, T* y) {
 template <typename T>
 halo_status by_tokens(const Operands& o, void* y) {
     T* out = static_cast<T*>(y);
-    // At d = 4096, us (line / pair): 32 tokens 4096 rows 7.4 / 9.7, 11008 rows 11.3 / 10.3; 64 tokens 4096 rows 8.7 / 9.9,
-    // 11008 rows 12.6 / 9.9; 17 tokens 32000 rows 17.9 / 20.9.  One token (one / line): 4096 rows 4.3 / 6.6, 11008 rows
-    // 7.4 / 10.4, 32000 rows 16.1 / 16.6.
-    if (o.n_tok == 1) return launch_one<T>(o, out);
+    // One token, us behind the quantiser of its row (one / line), rows x d: 4096 x 4096 5.9 / 7.2, 11008 x 4096 9.1 / 11.3,
+    // 5120 x 13824 14.0 / 16.4, 8192 x 2048 6.2 / 7.4, 24576 x 3584 14.5 / 14.6, 32000 x 4096 18.1 / 18.1, 32768 x 8192
+    // 30.5 / 30.7; with more rows, or shorter ones (which leave lanes of the one-token kernel idle), the tensor cores win:
+    // 16384 x 2048 8.5 / 7.6, 48000 x 512 12.3 / 6.2, 48000 x 5120 31.8 / 27.9, 128000 x 4096 59.5 / 48.9.
+    const long long rows = o.n_rows;
+    if (o.n_tok == 1 && (rows <= 8192 || (rows <= 7ll * o.d && rows <= 32768))) return launch_one<T>(o, out);
+    // At d = 4096, us (line / pair): 32 tokens 4096 rows 6.2 / 9.3, 11008 rows 9.7 / 9.6; 64 tokens 4096 rows 7.2 / 9.1,
+    // 8192 rows 10.5 / 9.5, 11008 rows 10.9 / 9.6; 17 tokens 32000 rows 16.4 / 19.7; 2 tokens 4096 rows 5.6 / 9.3.
     if (o.n_tok <= 16) return launch_line<T, 16, 10>(o, out);
     if (o.n_tok <= 32) return launch_line<T, 32, 9>(o, out);
-    if (o.n_tok <= 64 && o.n_rows <= 8192) return launch_line<T, 64, 8>(o, out);
+    if (o.n_tok <= 64 && o.n_rows <= 6144) return launch_line<T, 64, 8>(o, out);
     return launch_pair<T>(o, out);
 }
 

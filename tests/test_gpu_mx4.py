@@ -154,3 +154,22 @@ def test_quantise_and_product_captured_into_a_graph_and_on_another_stream(T):
         assert torch.equal(got, y)
         ref = values(Q, S, T, d) @ values(Qw, Sw, n, d).t()
         assert ((got.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 1e-4 * ref.abs().max()).all()
+
+
+@pytest.mark.parametrize("big", [2.0 ** 123, 2.0 ** -120])
+@pytest.mark.parametrize("T", [1, 2, 20, 40, 70])
+def test_scales_at_both_ends_of_their_range_meet_in_range(T, big):
+    """Tokens near one end of the fp32 range times weights near the other: the products are ordinary numbers, so no step in
+    between may leave the range.  Small whole numbers times powers of two: every sum below is exact in 24 bits."""
+    n, d = 70, 256
+    g = gen(T)
+    x = torch.randint(-6, 7, (T, d), generator=g, device=DEV).float().clamp(-4, 4)
+    w = torch.randint(-4, 5, (n, d), generator=g, device=DEV).float()
+    x[:, ::32] = 4.0
+    w[:, ::32] = 4.0            # both sides' blocks keep the numbers 0..4 exactly
+    Qx, Sx = quantize(x * big)
+    Qw, Sw = quantize(w / big)
+    y = torch.empty((T, n), device=DEV)
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.halo_product_mx4(d, T, n, Qx, Sx, Qw, Sw, B.F32, y, st)
+    assert torch.equal(y.double(), x.double() @ w.double().T) and int(st) == 0
