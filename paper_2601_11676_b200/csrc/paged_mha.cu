@@ -759,7 +759,7 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
 template <typename T, int DP, int THREADS>
 __global__ void __launch_bounds__(THREADS) paged_mha_join_kernel(const __grid_constant__ PagedArgs a, int blocks) {
     static_assert(THREADS % DP == 0 && DP % 32 == 0, "groups of whole warps");
-    constexpr int kGroups = THREADS / DP, kAhead = 16;
+    constexpr int kGroups = THREADS / DP, kAhead = kGroups > 1 ? 20 : 16;
     __shared__ float red[2][THREADS / 32];
     __shared__ float part[kGroups > 1 ? THREADS : 1];
     extern __shared__ float weight[];   // [pieces]
