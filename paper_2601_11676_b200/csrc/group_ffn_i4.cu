@@ -572,7 +572,6 @@ group_ffn_i4_ring_kernel(int d, int S, int G, const uint8_t* __restrict__ Q, con
         if (slot >= 0) {
             if (slot != cur_slot) {
                 if (cur_slot >= 0) flush(cur_slot);
-    if (!dep_waited) asm volatile("griddepcontrol.wait;" ::: "memory");   // only groups out of range: as above
                 cur_slot = slot;
             }
             // phase 1: code rows 0..15 of the stage are the 8 gate rows then the 8 up rows (planes 0, 1 adjacent)
@@ -645,6 +644,7 @@ group_ffn_i4_ring_kernel(int d, int S, int G, const uint8_t* __restrict__ Q, con
         if (lane == 0) mbar_arrive(&hd.empty[s]);
     }
     if (cur_slot >= 0) flush(cur_slot);
+    if (!dep_waited) asm volatile("griddepcontrol.wait;" ::: "memory");   // only groups out of range: as above
     if (tid == 0 && *abort_flag) flag_status(dev_status, HALO_DEV_TIMEOUT);
 }
 
