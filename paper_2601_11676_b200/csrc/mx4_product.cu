@@ -9,14 +9,16 @@
 //
 // Three kernels:
 //   mx4_one_kernel   one token and some thousand rows: exact fp16 products on the ordinary pipe, described at the kernel.
-//   mx4_line_kernel  up to 64 tokens, bound by HBM (0.53 bytes per weight element): the weight rows in groups of 32 form
+//   mx4_line_kernel  up to 32 tokens, bound by HBM (0.53 bytes per weight element): the weight rows in groups of 32 form
 //     a line that is cut into equal pieces, one thread block per SM; whole outputs per thread block, so nothing has to
 //     be added up between thread blocks.  32000 x 4096: 16.1 us for up to 16 tokens, 4.3 TB/s of weights.
-//   mx4_pair_kernel  prompts, bound by the L2-to-SM traffic and the tensor pipe: pairs of SMs (cta_group::2) on tiles
-//     of 256 rows x 256 tokens; each SM fetches half of either operand, 35 KB per 16.8 M products and SM where a
-//     single SM's 128 x 256 tile takes 51 KB.  4096 x 11008 x 4096: 70 us = 5.3 PFLOP/s, tensor pipe 68 % active; a
-//     stage takes 0.37 us and a tile 0.85 us beyond its stages (one accumulator: a second one would leave no tensor
-//     memory for the scales at this tile, and smaller tiles fetch more per product).
+//   mx4_pair_kernel  more tokens, or fewer through many long rows: pairs of SMs (cta_group::2) on tiles of 256 rows x 256
+//     tokens; each SM fetches half of either operand, 35 KB per 16.8 M products and SM where a single SM's 128 x 256
+//     tile takes 51 KB.  Prompts are bound by the L2-to-SM traffic and the tensor pipe: 4096 x 11008 x 4096 70 us = 5.3
+//     PFLOP/s, tensor pipe 68 % active; a stage takes 0.37 us and a tile 0.85 us beyond its stages (one accumulator: a
+//     second one would leave no tensor memory for the scales at this tile, and smaller tiles fetch more per product).
+//     A last round that fits twice is halved into 128 tokens a tile, as are tiles with no more tokens left: 300 x 4096 x
+//     4096 9.5 -> 7.5 us, 512 x 11008 x 4096 15.9 -> 14.4.
 //
 // Every wait is bounded; when one runs out the block's roles leave their loops, the copies in flight are waited for,
 // TMEM is freed and HALO_DEV_TIMEOUT is raised.
@@ -180,7 +182,7 @@ mx4_one_kernel(int d, int n_rows, const uint8_t* __restrict__ Qx, const uint8_t*
     }
 }
 
-// NT tokens (at most 64: one block of scales)
+// NT tokens (at most 128: one block of scales)
 template <int NT, int STAGES>
 struct Ring {
     static constexpr int kA = kRowsTile * (kStageK / 2);
@@ -474,20 +476,37 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
                  : "memory");
 }
 
+// The tiles of a product, 256 rows each, in the order of the pairs: whole rounds of 256 tokens, then the tiles of the
+// last round, in halves of 128 tokens where these fit one round.  A tile that has at most 128 tokens left takes 128.
+struct PairTiles {
+    int row_tiles, whole, items;   // whole: tiles that are not halved; items: those and the halves
+    int halves;                    // 0 or 1
+};
+struct PairTile {
+    int row, tok, n;               // first row, first token, tokens (128 or 256; 0: nothing is left)
+};
+__device__ __forceinline__ PairTile tile_at(const PairTiles& t, int u, int n_tok) {
+    const int half = u < t.whole ? 0 : (u - t.whole) & t.halves;
+    const int tile = u < t.whole ? u : t.whole + ((u - t.whole) >> t.halves);
+    PairTile p;
+    p.row = tile % t.row_tiles * kPairTile;
+    p.tok = tile / t.row_tiles * kPairTile + half * 128;
+    p.n = p.tok >= n_tok ? 0 : n_tok - p.tok <= 128 || (u >= t.whole && t.halves) ? 128 : kPairTile;
+    return p;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kPairThreads, 1)
 mx4_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
-                const __grid_constant__ CUtensorMap map_sw, const __grid_constant__ CUtensorMap map_sx, int d, int n_tok,
-                int n_rows, T* __restrict__ y, uint32_t* status) {
+                const __grid_constant__ CUtensorMap map_x64, const __grid_constant__ CUtensorMap map_sw, const __grid_constant__ CUtensorMap map_sx, PairTiles list,
+                int d, int n_tok, int n_rows, T* __restrict__ y, uint32_t* status) {
     using R = PairRing;
     extern __shared__ __align__(1024) unsigned char smem[];
     PairBars& bars = *reinterpret_cast<PairBars*>(smem + static_cast<size_t>(kPairStages) * R::kStage);
     const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
     const uint32_t rank = cluster_rank();
     const int atoms = d / 128, nk = (d + kStageK - 1) / kStageK;
-    const int row_blocks = (n_rows + 127) / 128, tok_blocks = (n_tok + 127) / 128;
-    const int row_tiles = (row_blocks + 1) / 2, tok_tiles = (tok_blocks + 1) / 2;
-    const int tiles = row_tiles * tok_tiles, pairs = gridDim.x / 2, pair = blockIdx.x / 2;
+    const int pairs = gridDim.x / 2, pair = blockIdx.x / 2;
 
     if (tid == 0) {
         for (int s = 0; s < kPairStages; ++s) {
@@ -520,9 +539,12 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         Slot<kPairStages> slot;
         int it = 0;
         bool alive = true;
-        for (int tile = pair; tile < tiles && alive; tile += pairs) {
-            const int rb = (tile % row_tiles) * 2 + static_cast<int>(rank);    // this SM's block of 128 rows
-            const int tb0 = (tile / row_tiles) * 2;                            // the pair's blocks of 128 tokens
+        for (int u = pair; u < list.items && alive; u += pairs) {
+            const PairTile tile = tile_at(list, u, n_tok);
+            if (tile.n == 0) continue;
+            const int rb = tile.row / 128 + static_cast<int>(rank);            // this SM's block of 128 rows
+            const int tb0 = tile.tok / 128;                                    // the pair's blocks of 128 tokens
+            const bool wide = tile.n == kPairTile;
             for (int k = 0; k < nk; ++k, ++it, slot.advance()) {
                 if (it >= kPairStages && !wait_or_abort(&bars.empty[slot.stage], slot.parity ^ 1u, abort_flag)) { alive = false; break; }
                 unsigned char* st = smem + slot.stage * R::kStage;
@@ -530,9 +552,12 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                 const uint32_t full = full0 + slot.stage * 8;
                 if (leader) {
                     // what lies outside a matrix arrives as zeros and counts: both SMs' bytes, the same for every stage
-                    if (rank == 0) mbar_arrive_expect_tx(&bars.full[slot.stage], 2 * R::kStage);
+                    if (rank == 0) mbar_arrive_expect_tx(&bars.full[slot.stage], 2 * (wide ? R::kStage : R::kStage - R::kOp / 2));
                     tma_pair_2d(st, &map_w, k * (kStageK / 2), rb * 128, full);
-                    tma_pair_2d(st + R::kOp, &map_x, k * (kStageK / 2), (tb0 + static_cast<int>(rank)) * 128, full);
+                    if (wide)
+                        tma_pair_2d(st + R::kOp, &map_x, k * (kStageK / 2), tile.tok + static_cast<int>(rank) * 128, full);
+                    else
+                        tma_pair_2d(st + R::kOp, &map_x64, k * (kStageK / 2), tile.tok + static_cast<int>(rank) * 64, full);
                     tma_pair_3d(sc, &map_sw, 0, k * 2, rb, full);
                     tma_pair_3d(sc + R::kSfa, &map_sx, 0, k * 2, tb0, full);
                 }
@@ -549,7 +574,9 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         Slot<kPairStages> slot;
         int n = 0;
         bool alive = true;
-        for (int tile = pair; tile < tiles && alive && rank == 0; tile += pairs, ++n) {
+        for (int u = pair; u < list.items && alive && rank == 0; u += pairs) {
+            const PairTile tile = tile_at(list, u, n_tok);
+            if (tile.n == 0) continue;
             if (n > 0 && !wait_cluster(&bars.acc_empty, (n - 1) & 1, abort_flag)) break;
             tcgen05_fence_after_sync();
             for (int k = 0; k < nk; ++k, slot.advance()) {
@@ -570,7 +597,7 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         if (j == 2 && atoms - k * 2 < 2) break;
-                        umma_mxf4_pair(tmem, da + j * 2, db + j * 2, idesc_mxf4(kPairTile, kPairTile, (j & 1) * 2), sfa + (j >> 1) * 4,
+                        umma_mxf4_pair(tmem, da + j * 2, db + j * 2, idesc_mxf4(kPairTile, tile.n, (j & 1) * 2), sfa + (j >> 1) * 4,
                                        sfb + (j >> 1) * 8, j > 0 || k > 0);
                     }
                     umma_commit_pair(&bars.empty[slot.stage]);
@@ -579,6 +606,7 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             }
             if (leader) umma_commit_pair(&bars.acc_full);
             __syncwarp();
+            ++n;
         }
     } else {
         // a warp reads 32 rows x 128 tokens into registers and lets the accumulator go before it stores
@@ -586,17 +614,23 @@ mx4_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         const uint32_t base = tmem + half * 128 + (static_cast<uint32_t>(quad * 32) << 16);
         const uint32_t acc_empty = in_block_of(0, &bars.acc_empty);
         int n = 0;
-        for (int tile = pair; tile < tiles; tile += pairs, ++n) {
-            if (!wait_cluster(&bars.acc_full, n & 1, abort_flag)) break;
+        for (int u = pair; u < list.items; u += pairs) {
+            const PairTile tile = tile_at(list, u, n_tok);
+            if (tile.n == 0) continue;
+            if (!wait_cluster(&bars.acc_full, n++ & 1, abort_flag)) break;
             tcgen05_fence_after_sync();
+            if (half * 128 >= tile.n) {
+                if (lane == 0) arrive_at(acc_empty);
+                continue;
+            }
             uint32_t v[4][32];
 #pragma unroll
             for (int c = 0; c < 4; ++c) tmem_ld_32x32(base + c * 32, v[c]);
             tmem_ld_wait();
             tcgen05_fence_before_sync();
             if (lane == 0) arrive_at(acc_empty);
-            const int row = (tile % row_tiles) * kPairTile + static_cast<int>(rank) * 128 + quad * 32 + lane;
-            const int tok0 = (tile / row_tiles) * kPairTile + half * 128;
+            const int row = tile.row + static_cast<int>(rank) * 128 + quad * 32 + lane;
+            const int tok0 = tile.tok + half * 128;
             if constexpr (sizeof(T) == 2) {
                 if ((n_rows & 1) == 0) {
                     // two rows per word: lanes 2i and 2i + 1 exchange one token each of a pair of tokens
@@ -670,15 +704,23 @@ template <typename T>
 halo_status launch_pair(const Operands& o, T* y) {
     static bool done[64];
     if (!ensure_dynamic_smem(mx4_pair_kernel<T>, PairRing::kSmem, done)) return HALO_ERR_CUDA;
-    CUtensorMap map_w, map_x, map_sw, map_sx;
+    CUtensorMap map_w, map_x, map_x64, map_sw, map_sx;
     if (!make_byte_map(&map_w, o.Qw, o.n_rows, o.d / 2, kStageK / 2, 128) ||
         !make_byte_map(&map_x, o.Qx, o.n_tok, o.d / 2, kStageK / 2, 128) ||
+        !make_byte_map(&map_x64, o.Qx, o.n_tok, o.d / 2, kStageK / 2, 64) ||
         !make_scale_map(&map_sw, o.Sw, (o.n_rows + 127) / 128, o.d / 128, 1, 2) ||
         !make_scale_map(&map_sx, o.Sx, (o.n_tok + 127) / 128, o.d / 128, 2, 2))
         return HALO_ERR_CUDA;
-    const long long tiles = static_cast<long long>((o.n_rows + 255) / 256) * ((o.n_tok + 255) / 256);
+    constexpr int kPairs = kSmCount / 2;
+    PairTiles list;
+    list.row_tiles = (o.n_rows + kPairTile - 1) / kPairTile;
+    const int tiles = list.row_tiles * ((o.n_tok + kPairTile - 1) / kPairTile);   // at most 2^28
+    const int rest = tiles % kPairs;
+    list.halves = 2 * rest <= kPairs;
+    list.whole = tiles - rest;
+    list.items = tiles + (list.halves ? rest : 0);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(tiles < kSmCount / 2 ? static_cast<unsigned>(tiles) * 2 : kSmCount);
+    cfg.gridDim = dim3(2 * (list.items < kPairs ? list.items : kPairs));
     cfg.blockDim = dim3(kPairThreads);
     cfg.dynamicSmemBytes = PairRing::kSmem;
     cfg.stream = o.st;
@@ -691,24 +733,26 @@ halo_status launch_pair(const Operands& o, T* y) {
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    return cuda_status(cudaLaunchKernelEx(&cfg, mx4_pair_kernel<T>, map_w, map_x, map_sw, map_sx, o.d, o.n_tok, o.n_rows, y,
+    return cuda_status(cudaLaunchKernelEx(&cfg, mx4_pair_kernel<T>, map_w, map_x, map_x64, map_sw, map_sx, list, o.d, o.n_tok, o.n_rows, y,
                                           o.status));
 }
 
 template <typename T>
 halo_status by_tokens(const Operands& o, void* y) {
     T* out = static_cast<T*>(y);
-    // One token, us behind the quantiser of its row (one / line), rows x d: 4096 x 4096 5.9 / 7.2, 11008 x 4096 9.1 / 11.3,
-    // 5120 x 13824 14.0 / 16.4, 8192 x 2048 6.2 / 7.4, 24576 x 3584 14.5 / 14.6, 32000 x 4096 18.1 / 18.1, 32768 x 8192
-    // 30.5 / 30.7; with more rows, or shorter ones (which leave lanes of the one-token kernel idle), the tensor cores win:
-    // 16384 x 2048 8.5 / 7.6, 48000 x 512 12.3 / 6.2, 48000 x 5120 31.8 / 27.9, 128000 x 4096 59.5 / 48.9.
+    // us, rows x d.  One token (one / line / pair): 4096 x 4096 4.2 / 5.6 / 7.0, 11008 x 4096 7.2 / 8.9 / 9.0, 24576 x 4096
+    // 13.1 / 13.7 / 15.4, 4096 x 11008 8.0 / 10.9 / 12.5, 32000 x 8192 27.8 / 28.1 / 30.0; with more rows, or rows so short
+    // that lanes of the one-token kernel stay idle, the line: 16384 x 2048 6.6 / 5.9 / 7.3, 32000 x 256 7.9 / 3.9 / 5.4,
+    // 64000 x 5120 37.9 / 31.6 / 36.2.
     const long long rows = o.n_rows;
     if (o.n_tok == 1 && (rows <= 8192 || (rows <= 7ll * o.d && rows <= 32768))) return launch_one<T>(o, out);
-    // At d = 4096, us (line / pair): 32 tokens 4096 rows 6.2 / 9.3, 11008 rows 9.7 / 9.6; 64 tokens 4096 rows 7.2 / 9.1,
-    // 8192 rows 10.5 / 9.5, 11008 rows 10.9 / 9.6; 17 tokens 32000 rows 16.4 / 19.7; 2 tokens 4096 rows 5.6 / 9.3.
-    if (o.n_tok <= 16) return launch_line<T, 16, 10>(o, out);
-    if (o.n_tok <= 32) return launch_line<T, 32, 9>(o, out);
-    if (o.n_tok <= 64 && o.n_rows <= 6144) return launch_line<T, 64, 8>(o, out);
+    // 8 tokens (line / pair): 4096 x 4096 5.6 / 7.0, 11008 x 2048 5.8 / 6.0, 32000 x 2048 8.4 / 10.9, 24576 x 4096 13.8 / 14.9.
+    // A second group of rows per SM costs the line as much as the first, the pairs take 256 x 74 rows at once: 6144 x 4096
+    // 8.6 / 7.2, 11008 x 4096 9.0 / 7.9, 8192 x 11008 19.5 / 14.5, 32000 x 11008 37.2 / 34.2.  64 tokens in a line of their
+    // own: 4096 x 4096 7.4 / 7.2, 11008 x 4096 10.8 / 7.6.
+    const bool line = rows <= 32 * kSmCount || o.d <= 2048 || (rows > kPairTile * (kSmCount / 2) && o.d <= 4096);
+    if ((line && o.n_tok <= 16) || o.n_tok == 1) return launch_line<T, 16, 10>(o, out);
+    if (line && o.n_tok <= 32) return launch_line<T, 32, 9>(o, out);
     return launch_pair<T>(o, out);
 }
 
