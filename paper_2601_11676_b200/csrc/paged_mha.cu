@@ -115,7 +115,9 @@ struct Cfg {
     // two warps' sums at a time, of the item's query heads
     static constexpr int merge_bytes(int rows) { return kWarps > 2 ? 2 * rows * kMergeRow * 4 : rows * kMergeRow * 4; }
     static constexpr int kMaxSmem = kRings + merge_bytes(GR);
-    static constexpr int kBlocksPerSm = kMaxSmem <= 56 * 1024 ? 4 : kMaxSmem <= 75 * 1024 ? 3 : kMaxSmem <= 115200 ? 2 : 1;
+    // an SM has 228 KB; a thread block takes its own, wm and wl, and 1 KB of the system's
+    static constexpr int kFit = 228 * 1024 / (kMaxSmem + 2 * kWarps * 16 * 4 + 1024);
+    static constexpr int kBlocksPerSm = kFit > 4 ? 4 : kFit;
     static_assert(kMaxSmem <= 225 * 1024, "shared memory");
 };
 
@@ -249,7 +251,6 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
     constexpr int NT = DP / 8;                    // bf16: 8-wide column tiles of the output
     constexpr int V = DP / 32;                    // fp32: output columns per lane
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ long long scan[C_::kWarps + 2];
     __shared__ float wm[C_::kWarps][16], wl[C_::kWarps][16];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int items = a.Hk * a.qblocks;
@@ -272,7 +273,7 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
             a, [&](long long t) {
                 const int C = ranges(t, gridDim.x);
                 return static_cast<int>(blockIdx.x) < C ? cut(t, blockIdx.x, C) : t;
-            }, scan);
+            }, reinterpret_cast<long long*>(smem));   // where the warps meet later
         total = p.total;
         const int C = ranges(total, gridDim.x);
         if (static_cast<int>(blockIdx.x) >= C) return;
@@ -752,24 +753,58 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
     if (__any_sync(0xffffffffu, bad) && lane == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
 }
 
-// Joins the pieces of the items that were cut.  Block (c, r): the item that range c begins and does not end, query head
-// r of it.  A group of DP threads (a column each) takes every kGroups-th piece; the first kAhead values of a thread are
-// requested together with the pieces' maxima and sums (one piece per thread), so that a join waits for memory twice: for
-// the record of the cut and for the pieces.
+// Joins the pieces of the items that were cut.  blockIdx.y = query head of the item; blockIdx.x = the range that begins and
+// does not end it (DP threads, a column each), or, where there are few items of many pieces (several groups of DP threads),
+// the item: a thread block per range would be one of thousands that find nothing to do (one sequence of 32000 positions,
+// 16 heads on one: KXX us), so it looks for its item among the records of all ranges.  A group takes every kGroups-th
+// piece; the first kAhead values of a thread are requested together with the pieces' maxima and sums (one piece per
+// thread), so that a join waits for memory twice: for the records and for the pieces.
 template <typename T, int DP, int THREADS>
 __global__ void __launch_bounds__(THREADS) paged_mha_join_kernel(const __grid_constant__ PagedArgs a, int blocks) {
     static_assert(THREADS % DP == 0 && DP % 32 == 0, "groups of whole warps");
-    constexpr int kGroups = THREADS / DP, kAhead = kGroups > 1 ? 20 : 16;
+    constexpr int kGroups = THREADS / DP, kAhead = kGroups > 1 ? 12 : 16;
     __shared__ float red[2][THREADS / 32];
     __shared__ float part[kGroups > 1 ? THREADS : 1];
     extern __shared__ float weight[];   // [pieces]
-    const int r = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c0 = blockIdx.x;
+    const int r = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     chain_wait();   // in every block: this grid may not end before the first one
-    const int4 cut_ = __ldcg(reinterpret_cast<const int4*>(a.cuts + c0));
-    const int4 line = __ldcg(reinterpret_cast<const int4*>(a.cuts + c0) + 1);
+    int c0 = blockIdx.x;
+    int4 cut_, line;
     const long long total = __ldcg(&a.cuts[0].total);
     const int C = ranges(total, blocks);
-    if (c0 + 1 >= C || !cut_.x) return;      // a block behind the last range reads a record that nobody wrote, and drops it
+    // a record behind the last range is one that nobody wrote: it is read and dropped
+    if constexpr (kGroups == 1) {
+        cut_ = __ldcg(reinterpret_cast<const int4*>(a.cuts + c0));
+        line = __ldcg(reinterpret_cast<const int4*>(a.cuts + c0) + 1);
+        if (c0 + 1 >= C || !cut_.x) return;
+    } else {
+        __shared__ int4 found[2];
+        __shared__ int at_range;
+        if (tid == 0) at_range = -1;
+        __syncthreads();
+        constexpr int kMost = (kSmCount * 4 + THREADS - 1) / THREADS;
+        int4 rec[kMost][2];
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            const int4* from = reinterpret_cast<const int4*>(a.cuts + min(tid + i * THREADS, blocks - 1));
+            rec[i][0] = __ldcg(from);
+            rec[i][1] = __ldcg(from + 1);
+        }
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            const int c = tid + i * THREADS;
+            if (c + 1 < C && rec[i][0].x && rec[i][0].y * a.Hk * a.qblocks + rec[i][0].z == c0) {
+                at_range = c;
+                found[0] = rec[i][0];
+                found[1] = rec[i][1];
+            }
+        }
+        __syncthreads();
+        if (at_range < 0) return;      // not cut
+        c0 = at_range;
+        cut_ = found[0];
+        line = found[1];
+    }
     const int s = cut_.y, hi = cut_.z;
     const int kvh = hi / a.qblocks, r0 = (hi % a.qblocks) * 16;
     if (r >= min(16, a.G - r0)) return;
@@ -823,7 +858,7 @@ __global__ void __launch_bounds__(THREADS) paged_mha_join_kernel(const __grid_co
         const int k = grp + e * kGroups;
         if (k < pieces) v = fmaf(ahead[e], weight[k], v);
     }
-#pragma unroll 8
+#pragma unroll 16
     for (int k = grp + kAhead * kGroups; k < pieces; k += kGroups) v = fmaf(__ldcg(slot(k) + at), weight[k], v);
     if constexpr (kGroups > 1) {
         part[tid] = v;
@@ -872,8 +907,8 @@ size_t workspace_of(const LaunchPlan& p) {
 
 template <typename T, int DP, int THREADS>
 halo_status launch_join(const PagedArgs& a, const LaunchPlan& p, cudaStream_t st) {
-    return launch_chained(paged_mha_join_kernel<T, DP, THREADS>, dim3(p.blocks - 1, p.rows), THREADS, sizeof(float) * p.blocks, st, a,
-                          p.blocks);
+    return launch_chained(paged_mha_join_kernel<T, DP, THREADS>, dim3(THREADS > DP ? static_cast<unsigned>(p.items) : p.blocks - 1, p.rows), THREADS,
+                          sizeof(float) * p.blocks, st, a, p.blocks);
 }
 
 template <typename T, int DP, int GR>
@@ -902,8 +937,7 @@ halo_status launch(const PagedArgs& args, const LaunchPlan& p, cudaStream_t st) 
     cfg.numAttrs = p.split > 1 ? 2 : 1;
     const halo_status rc = cuda_status(cudaLaunchKernelEx(&cfg, paged_mha_kernel<T, DP, GR>, a));
     if (rc != HALO_OK || p.split || p.blocks < 2) return rc;
-    // few items, many pieces each: several groups of threads
-    constexpr int kWide = DP == 256 ? 512 : 256;
+    constexpr int kWide = 512;
     return p.blocks >= 8 * p.items ? launch_join<T, DP, kWide>(a, p, st) : launch_join<T, DP, DP>(a, p, st);
 }
 
