@@ -753,69 +753,112 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
     if (__any_sync(0xffffffffu, bad) && lane == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
 }
 
-// Joins the pieces of the items that were cut.  blockIdx.y = query head of the item; blockIdx.x = the range that begins and
-// does not end it (DP threads, a column each), or, where there are few items of many pieces (several groups of DP threads),
-// the item: a thread block per range would be one of thousands that find nothing to do (one sequence of 32000 positions,
-// 16 heads on one: KXX us), so it looks for its item among the records of all ranges.  A group takes every kGroups-th
-// piece; the first kAhead values of a thread are requested together with the pieces' maxima and sums (one piece per
-// thread), so that a join waits for memory twice: for the records and for the pieces.
-template <typename T, int DP, int THREADS>
-__global__ void __launch_bounds__(THREADS) paged_mha_join_kernel(const __grid_constant__ PagedArgs a, int blocks) {
-    static_assert(THREADS % DP == 0 && DP % 32 == 0, "groups of whole warps");
-    constexpr int kGroups = THREADS / DP, kAhead = kGroups > 1 ? 12 : 16;
-    __shared__ float red[2][THREADS / 32];
-    __shared__ float part[kGroups > 1 ? THREADS : 1];
-    extern __shared__ float weight[];   // [pieces]
-    const int r = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+// Joining the pieces of the items that were cut: two kernels, each of which waits for memory twice, for the records and for
+// the pieces.  What a range has written of a cut that it opens:
+struct Opened {
+    int s, kvh, r0, rows;   // the item, and its first query head and their number
+    int pieces;
+    const float *ws0, *ws1;
+    int slot;
+    __device__ __forceinline__ Opened(const PagedArgs& a, const int4& head, bool fills, int c0, long long total, int C) {
+        s = head.y;
+        kvh = head.z / a.qblocks;
+        r0 = (head.z % a.qblocks) * 16;
+        rows = min(16, a.G - r0);
+        pieces = range_of(total, cut(total, c0 + 1, C) + head.w - 1, C) - c0 + 1;
+        // piece 0 in the slot of range c0 that holds its end (its first one if the item fills the range), the others in
+        // the first slots of the ranges behind it
+        ws0 = a.ws + (static_cast<long long>(c0) * 2 + (fills ? 0 : 1)) * a.slot;
+        ws1 = a.ws + static_cast<long long>(c0) * 2 * a.slot;
+        slot = a.slot;
+    }
+    __device__ __forceinline__ const float* piece(int k) const { return k == 0 ? ws0 : ws1 + static_cast<long long>(k) * 2 * slot; }
+};
+
+// Many items of few pieces.  blockIdx.x = the range that begins an item and does not end it; DP threads, a column each, for
+// a query head, several heads per thread block.
+constexpr int kRangeJoin = 256;
+template <typename T, int DP>
+__global__ void __launch_bounds__(kRangeJoin) paged_mha_join_range_kernel(const __grid_constant__ PagedArgs a, int blocks) {
+    constexpr int kAhead = 4;
+    const int r = blockIdx.y * (kRangeJoin / DP) + threadIdx.x / DP, j = threadIdx.x % DP, c0 = blockIdx.x;
     chain_wait();   // in every block: this grid may not end before the first one
-    int c0 = blockIdx.x;
-    int4 cut_, line;
+    const int4 head = __ldcg(reinterpret_cast<const int4*>(a.cuts + c0)), line = __ldcg(reinterpret_cast<const int4*>(a.cuts + c0) + 1);
     const long long total = __ldcg(&a.cuts[0].total);
     const int C = ranges(total, blocks);
-    // a record behind the last range is one that nobody wrote: it is read and dropped
-    if constexpr (kGroups == 1) {
-        cut_ = __ldcg(reinterpret_cast<const int4*>(a.cuts + c0));
-        line = __ldcg(reinterpret_cast<const int4*>(a.cuts + c0) + 1);
-        if (c0 + 1 >= C || !cut_.x) return;
-    } else {
-        __shared__ int4 found[2];
-        __shared__ int at_range;
-        if (tid == 0) at_range = -1;
-        __syncthreads();
-        constexpr int kMost = (kSmCount * 4 + THREADS - 1) / THREADS;
-        int4 rec[kMost][2];
+    if (c0 + 1 >= C || !head.x) return;      // a block behind the last range reads a record that nobody wrote, and drops it
+    const Opened o(a, head, line.z, c0, total, C);
+    if (r >= o.rows) return;
+    float M = -INFINITY, L = 0.0f, v = 0.0f;
+    for (int k0 = 0; k0 < o.pieces; k0 += kAhead) {
+        float m[kAhead], l[kAhead], x[kAhead];
 #pragma unroll
-        for (int i = 0; i < kMost; ++i) {
-            const int4* from = reinterpret_cast<const int4*>(a.cuts + min(tid + i * THREADS, blocks - 1));
-            rec[i][0] = __ldcg(from);
-            rec[i][1] = __ldcg(from + 1);
+        for (int e = 0; e < kAhead; ++e) {
+            const bool there = k0 + e < o.pieces;
+            const float* p = o.piece(k0 + e);
+            m[e] = there ? __ldcg(p + r) : -INFINITY;
+            l[e] = there ? __ldcg(p + 16 + r) : 0.0f;
+            x[e] = there ? __ldcg(p + kSlotHead + r * DP + j) : 0.0f;
         }
 #pragma unroll
-        for (int i = 0; i < kMost; ++i) {
-            const int c = tid + i * THREADS;
-            if (c + 1 < C && rec[i][0].x && rec[i][0].y * a.Hk * a.qblocks + rec[i][0].z == c0) {
-                at_range = c;
-                found[0] = rec[i][0];
-                found[1] = rec[i][1];
-            }
+        for (int e = 0; e < kAhead; ++e) {
+            const float mx = fmaxf(M, m[e]), base = mx == -INFINITY ? 0.0f : mx;
+            const float f = pow2(M - base), w = pow2(m[e] - base);
+            M = mx;
+            L = fmaf(L, f, l[e] * w);
+            v = fmaf(v, f, x[e] * w);
         }
-        __syncthreads();
-        if (at_range < 0) return;      // not cut
-        c0 = at_range;
-        cut_ = found[0];
-        line = found[1];
     }
-    const int s = cut_.y, hi = cut_.z;
-    const int kvh = hi / a.qblocks, r0 = (hi % a.qblocks) * 16;
-    if (r >= min(16, a.G - r0)) return;
-    const int h = kvh * a.G + r0 + r;
-    // piece 0 in the slot of range c0 that holds its end (its first one if the item fills the range), the others in the
-    // first slots of the ranges behind it
-    const long long end = cut(total, c0 + 1, C);
-    const int pieces = range_of(total, end + cut_.w - 1, C) - c0 + 1;
-    const float* ws0 = a.ws + (static_cast<long long>(c0) * 2 + (line.z ? 0 : 1)) * a.slot;
-    const float* ws1 = a.ws + static_cast<long long>(c0) * 2 * a.slot;
-    const auto slot = [&](int k) { return k == 0 ? ws0 : ws1 + static_cast<long long>(k) * 2 * a.slot; };
+    const int h = o.kvh * a.G + o.r0 + r;
+    const bool some = L != 0.0f && head_kept(a, h);
+    if (j < a.dh) write_head<T>(a, o.s, h, j, some ? v / L : 0.0f);
+    if (j == 0 && a.lse) a.lse[static_cast<long long>(o.s) * a.H + h] = some ? (M + log2f(L)) * kLn2 : -INFINITY;
+}
+
+// Few items of many pieces.  blockIdx.x = item, blockIdx.y = query head of it; the thread block looks for the item among the
+// records of all ranges (a thread block per range would be one of thousands that find nothing to do: one sequence of 32000
+// positions, 16 heads on one, 32 us and 23 as here).  Groups of DP threads, a column each, take every kGroups-th piece; the
+// first kAhead values of a thread are requested together with the pieces' maxima and sums (one piece per thread).
+constexpr int kItemJoin = 512;
+template <typename T, int DP>
+__global__ void __launch_bounds__(kItemJoin) paged_mha_join_item_kernel(const __grid_constant__ PagedArgs a, int blocks) {
+    static_assert(kItemJoin % DP == 0 && DP % 32 == 0, "groups of whole warps");
+    constexpr int kGroups = kItemJoin / DP, kAhead = 12, THREADS = kItemJoin;
+    constexpr int kMost = (kSmCount * 4 + THREADS - 1) / THREADS;      // records per thread
+    __shared__ float red[2][THREADS / 32];
+    __shared__ float part[THREADS];
+    __shared__ int4 found[2];
+    __shared__ int at_range;
+    extern __shared__ float weight[];   // [pieces]
+    const int r = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid == 0) at_range = -1;
+    chain_wait();   // in every block: this grid may not end before the first one
+    __syncthreads();
+    const long long total = __ldcg(&a.cuts[0].total);
+    int4 rec[kMost][2];
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        const int4* from = reinterpret_cast<const int4*>(a.cuts + min(tid + i * THREADS, blocks - 1));
+        rec[i][0] = __ldcg(from);
+        rec[i][1] = __ldcg(from + 1);
+    }
+    const int C = ranges(total, blocks);
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        const int c = tid + i * THREADS;      // behind the last range: a record that nobody wrote
+        if (c + 1 < C && rec[i][0].x && static_cast<long long>(rec[i][0].y) * a.Hk * a.qblocks + rec[i][0].z == blockIdx.x) {
+            at_range = c;
+            found[0] = rec[i][0];
+            found[1] = rec[i][1];
+        }
+    }
+    __syncthreads();
+    const int c0 = at_range;
+    if (c0 < 0) return;      // not cut
+    const Opened o(a, found[0], found[1].z, c0, total, C);
+    if (r >= o.rows) return;
+    const int s = o.s, pieces = o.pieces, h = o.kvh * a.G + o.r0 + r;
+    const auto slot = [&](int k) { return o.piece(k); };
     const int grp = tid / DP, j = tid % DP;
     const int at = kSlotHead + r * DP + j;
 
@@ -860,13 +903,11 @@ __global__ void __launch_bounds__(THREADS) paged_mha_join_kernel(const __grid_co
     }
 #pragma unroll 16
     for (int k = grp + kAhead * kGroups; k < pieces; k += kGroups) v = fmaf(__ldcg(slot(k) + at), weight[k], v);
-    if constexpr (kGroups > 1) {
-        part[tid] = v;
-        __syncthreads();
-        if (grp == 0) {
+    part[tid] = v;
+    __syncthreads();
+    if (grp == 0) {
 #pragma unroll
-            for (int e = 1; e < kGroups; ++e) v += part[tid + e * DP];
-        }
+        for (int e = 1; e < kGroups; ++e) v += part[tid + e * DP];
     }
     if (grp == 0 && j < a.dh) write_head<T>(a, s, h, j, some ? v / L : 0.0f);
     if (tid == 0 && a.lse) a.lse[static_cast<long long>(s) * a.H + h] = some ? (M + log2f(L)) * kLn2 : -INFINITY;
@@ -905,12 +946,6 @@ size_t workspace_of(const LaunchPlan& p) {
     return p.split ? 0 : static_cast<size_t>(p.blocks) * (sizeof(Cut) + sizeof(float) * 2 * p.slot);
 }
 
-template <typename T, int DP, int THREADS>
-halo_status launch_join(const PagedArgs& a, const LaunchPlan& p, cudaStream_t st) {
-    return launch_chained(paged_mha_join_kernel<T, DP, THREADS>, dim3(THREADS > DP ? static_cast<unsigned>(p.items) : p.blocks - 1, p.rows), THREADS,
-                          sizeof(float) * p.blocks, st, a, p.blocks);
-}
-
 template <typename T, int DP, int GR>
 halo_status launch(const PagedArgs& args, const LaunchPlan& p, cudaStream_t st) {
     using C_ = Cfg<T, DP, GR>;
@@ -937,8 +972,12 @@ halo_status launch(const PagedArgs& args, const LaunchPlan& p, cudaStream_t st) 
     cfg.numAttrs = p.split > 1 ? 2 : 1;
     const halo_status rc = cuda_status(cudaLaunchKernelEx(&cfg, paged_mha_kernel<T, DP, GR>, a));
     if (rc != HALO_OK || p.split || p.blocks < 2) return rc;
-    constexpr int kWide = 512;
-    return p.blocks >= 8 * p.items ? launch_join<T, DP, kWide>(a, p, st) : launch_join<T, DP, DP>(a, p, st);
+    if (p.blocks >= 8 * p.items)
+        return launch_chained(paged_mha_join_item_kernel<T, DP>, dim3(static_cast<unsigned>(p.items), p.rows), kItemJoin,
+                              sizeof(float) * p.blocks, st, a, p.blocks);
+    constexpr int kHeads = kRangeJoin / DP;
+    return launch_chained(paged_mha_join_range_kernel<T, DP>, dim3(p.blocks - 1, (p.rows + kHeads - 1) / kHeads), kRangeJoin, 0, st, a,
+                          p.blocks);
 }
 
 template <typename T, int DP, typename F>
