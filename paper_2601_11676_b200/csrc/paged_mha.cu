@@ -18,8 +18,8 @@
 //     their sum is taken in fp32 before that rounding.
 //   fp32: fused multiply-adds, two lanes per position for the scores, a column per lane for the weighted sums.
 //
-// bf16, 32 / 8 heads of 128: one sequence of 131071 positions 84 us + 6 for the join (537 MB: 6.4 TB/s in the first
-// kernel, HBM), 64 sequences of up to 4096 positions 87 + 7 us (a piece's start and meeting); one sequence of 700
+// bf16, 32 / 8 heads of 128: one sequence of 131071 positions 84 us + 5 for the join (537 MB: 6.4 TB/s in the first
+// kernel, HBM), 64 sequences of up to 4096 positions 87 + 4 us (a piece's start and meeting); one sequence of 700
 // positions, 32 / 4 heads of 64: 6.1 us (launch, one chain of loads, a cluster's meeting); fp32, 7 sequences of up to
 // 1500 positions, 8 / 8 heads of 64: 9.5 us (the same chain, 18 MB).
 #include <cooperative_groups.h>
