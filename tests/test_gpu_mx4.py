@@ -78,7 +78,8 @@ def test_a_block_with_a_value_that_is_not_finite_reads_back_as_nan(what):
 
 PRODUCT = [(1, 1, 128), (1, 130, 256), (1, 8300, 256), (1, 8300, 2048), (1, 33001, 128), (2, 257, 384), (8, 128, 128), (15, 1000, 2048), (16, 64, 640), (17, 300, 256), (31, 90, 256), (32, 8300, 256), (33, 129, 512), (40, 8193, 128),
            (64, 1111, 1024), (65, 128, 128), (100, 333, 384), (129, 256, 4096), (256, 640, 1152), (257, 100, 256), (700, 1030, 512),
-           (1, 32000, 4096), (5, 4096, 11008), (300, 4096, 4096), (1, 40, 65536), (3, 40, 65536), (70, 40, 65536)]
+           (1, 32000, 4096), (5, 4096, 11008), (300, 4096, 4096), (1, 40, 65536), (3, 40, 65536), (70, 40, 65536),
+           (300, 11008, 256), (1000, 9601, 256), (390, 9600, 384), (100, 20000, 2176)]   # a round of whole tiles and halves behind it
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
