@@ -97,12 +97,15 @@ constexpr int kRun = 16;            // positions of a tile that one warp takes
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr int kSlotHead = 32;       // floats in front of a slot's values: maxima, sums
 // Shapes per element type, padded head size DP and padded number of query heads GR (bf16: 8 or 16 of 16 rows in use).
-// Ring bytes are what keeps HBM busy: 6.5 TB/s x ~1 us of latency / 148 SMs = 44 KB have to be in flight; the shapes below hold 96 to 200 KB.
+// Ring bytes are what keeps HBM busy: 6.5 TB/s x ~1 us of latency / 148 SMs = 44 KB have to be in flight; the shapes below hold 100 to 210 KB.
 template <typename T, int DP, int GR>
 struct Cfg {
     static constexpr bool kF32 = sizeof(T) == 4;
-    static constexpr int kWarps = (kF32 && DP == 256) ? (GR == 16 ? 2 : 3) : 4;
-    static constexpr int kStages = kF32 && (DP == 256 || (DP == 128 && GR == 16)) ? 2 : 3;
+    static constexpr int kWarps = kF32 && DP == 256 ? (GR == 16 ? 2 : 3) : kF32 && DP == 128 && GR == 1 ? 3 : 4;
+    // fp32: two stages, so that two thread blocks of four warps fit an SM at head sizes up to 64, or of three at 128 with
+    // one query head per K/V head.  64 sequences of up to 2000 positions, 32 / 8 heads of 64: 77 us with three stages and
+    // one thread block, 59 so; 5 of up to 900, 8 / 8 heads of 128: 13.1 us with one thread block of four warps, 10.4 so.
+    static constexpr int kStages = kF32 ? 2 : 3;
     static constexpr int kTile = kWarps * kRun;
     static constexpr int kRowBytes = kF32 ? (DP + 8) * 4 : DP * 2;   // fp32: rows padded against bank conflicts; bf16: swizzled
     static constexpr int kHalf = kRun * kRowBytes;                   // keys (or values) of one stage
