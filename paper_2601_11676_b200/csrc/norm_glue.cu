@@ -50,11 +50,12 @@ __device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
     }
 }
 
-// sum over the threads of a row (a warp, or the whole thread block); the same value in each of them
-template <bool ONE_WARP>
+// sum over the threads of a row (LANES of a warp, or, 0, the whole thread block); the same value in each of them
+template <int LANES>
 __device__ __forceinline__ float row_sum(float v, float* sh /*[32]*/) {
-    v = warp_sum(v);
-    if constexpr (!ONE_WARP) {
+#pragma unroll
+    for (int o = (LANES ? LANES : 32) / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if constexpr (LANES == 0) {
         const int lane = threadIdx.x & 31;
         if (lane == 0) sh[threadIdx.x >> 5] = v;
         __syncthreads();
@@ -85,16 +86,18 @@ __device__ __forceinline__ void widen8(const Raw<T>& r, float (&f)[8]) {
     }
 }
 
-constexpr int kWarpRows = 4;   // rows per thread block where a row is one warp
+constexpr int kRowThreads = 128;   // of a thread block where a row is a warp or less
 
-template <typename TY, typename T, int IT, bool ONE_WARP>
-__global__ void __launch_bounds__(ONE_WARP ? 32 * kWarpRows : 1024)
+template <typename TY, typename T, int IT, int LANES>
+__global__ void __launch_bounds__(LANES ? kRowThreads : 1024)
 norm_glue_kernel(const __grid_constant__ GlueArgs a) {
     __shared__ float sh[2][32];
-    const int t = ONE_WARP ? threadIdx.x & 31 : threadIdx.x, n = ONE_WARP ? 32 : blockDim.x;
-    const long long row = ONE_WARP ? static_cast<long long>(blockIdx.x) * kWarpRows + (threadIdx.x >> 5) : blockIdx.x;
+    constexpr int kPart = LANES ? LANES : 32;
+    const int t = LANES ? threadIdx.x % kPart : threadIdx.x, n = LANES ? LANES : blockDim.x;
+    const long long mine = LANES ? static_cast<long long>(blockIdx.x) * (kRowThreads / kPart) + threadIdx.x / kPart : blockIdx.x;
     chain_wait();
-    if (row >= a.n_tok) return;   // whole warps, and only where a row is one warp
+    const long long row = LANES && mine >= a.n_tok ? a.n_tok - 1 : mine;   // behind the last row: its sums once more, no output
+    const bool live = row == mine;
     const long long base = row * a.d;
     const int units = a.d / 8;
     float h[IT][8];
@@ -121,7 +124,7 @@ norm_glue_kernel(const __grid_constant__ GlueArgs a) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) ss = fmaf(v[e], v[e], ss);
             }
-            ss = row_sum<ONE_WARP>(ss, sh[0]);
+            ss = row_sum<LANES>(ss, sh[0]);
             f = rsqrtf(ss / static_cast<float>(a.d) + a.eps);
         }
 #pragma unroll
@@ -154,12 +157,12 @@ norm_glue_kernel(const __grid_constant__ GlueArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) ss = fmaf(h[i][e], h[i][e], ss);
     }
-    ss = row_sum<ONE_WARP>(ss, sh[1]);
+    ss = row_sum<LANES>(ss, sh[1]);
     const float f = rsqrtf(ss / static_cast<float>(a.d) + a.eps);
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
         const int u = t + i * n;
-        if (u >= units) continue;
+        if (u >= units || !live) continue;
         store8(a.h_out + base + u * 8, h[i]);
         float w[8];
         if (a.w_pre) {
@@ -174,10 +177,11 @@ norm_glue_kernel(const __grid_constant__ GlueArgs a) {
     }
 }
 
-template <typename TY, typename T, int IT, bool ONE_WARP>
+template <typename TY, typename T, int IT, int LANES>
 halo_status go(const GlueArgs& a, int threads, cudaStream_t st) {
-    const int blocks = ONE_WARP ? (a.n_tok - 1) / kWarpRows + 1 : a.n_tok;
-    return launch_chained(norm_glue_kernel<TY, T, IT, ONE_WARP>, blocks, threads, 0, st, a);
+    constexpr int kPart = LANES ? LANES : 32;
+    const int rows = LANES ? kRowThreads / kPart : 1;   // per thread block
+    return launch_chained(norm_glue_kernel<TY, T, IT, LANES>, (a.n_tok - 1) / rows + 1, LANES ? kRowThreads : threads, 0, st, a);
 }
 template <typename TY, typename T>
 halo_status launch(const GlueArgs& a, cudaStream_t st) {
@@ -186,11 +190,14 @@ halo_status launch(const GlueArgs& a, cudaStream_t st) {
     // Many rows: two units per thread (8191 rows of 5120, us: two 91, three 93, four 102, five
     // 105: more units per thread leave fewer rows in flight per SM).  Few rows: one unit per thread while a thread block
     // can hold the row, the shortest time for a row.
+    // Short rows: a part of a warp each (100000 rows of 64, us: 31 with a warp per row, 15; of 128: 34 and 29).
     const bool many = a.n_tok >= 2 * kSmCount;
-    if (units <= 32) return go<TY, T, 1, true>(a, 32 * kWarpRows, st);
-    if (many && units <= 64) return go<TY, T, 2, true>(a, 32 * kWarpRows, st);
-    if (many || units > 1024) return go<TY, T, 2, false>(a, threads(2), st);
-    return go<TY, T, 1, false>(a, threads(1), st);
+    if (units <= 8) return go<TY, T, 1, 8>(a, 0, st);
+    if (units <= 16) return go<TY, T, 1, 16>(a, 0, st);
+    if (units <= 32) return go<TY, T, 1, 32>(a, 0, st);
+    if (many && units <= 64) return go<TY, T, 2, 32>(a, 0, st);
+    if (many || units > 1024) return go<TY, T, 2, 0>(a, threads(2), st);
+    return go<TY, T, 1, 0>(a, threads(1), st);
 }
 
 }  // namespace

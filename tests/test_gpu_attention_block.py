@@ -435,7 +435,8 @@ GLUE = [(ty, tx, n, d, post, gate, pre)
         for (ty, tx) in (("f32", "bf16"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32"))
         for (n, d, post, gate, pre) in ((1, 8, True, "full", True), (3, 4096, True, "row", True), (130, 264, False, "full", False),
                                         (5, 512, True, None, False), (7, 5120, False, None, True), (2, 16384, True, "wide", True),
-                                        (33, 2048, False, "row", True), (9, 128, True, "wide", False))]
+                                        (33, 2048, False, "row", True), (9, 128, True, "wide", False), (37, 64, True, "full", True), (21, 40, True, "row", True),
+                                        (13, 120, True, "wide", True), (1, 16, False, None, True))]
 
 
 @pytest.mark.parametrize("case", range(len(GLUE)))

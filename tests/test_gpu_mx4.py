@@ -33,7 +33,7 @@ def values(Q, S, n, d):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("n,d", [(1, 128), (3, 384), (127, 128), (130, 256), (33, 2048)])
+@pytest.mark.parametrize("n,d", [(1, 128), (3, 384), (127, 128), (130, 256), (33, 2048), (5, 1152), (8191, 128), (8200, 384)])
 def test_rows_match_oracle_bit_for_bit(dtype, n, d):
     t, code, _ = TYPES[dtype]
     g = gen(n + d)
