@@ -2,7 +2,7 @@
 // joined.  HBM-bound: every K and V row is read once, 4 * G flops per element of it (G = query heads per K/V head).
 //
 // Work line.  The cache is cut into tiles of 16 positions per warp; an item is one (sequence, K/V head, block of 16
-// query heads).  All tiles of all items, item after item, form one line of T tiles and thread block c of C (at most T)
+// query heads; fp32: of 4).  All tiles of all items, item after item, form one line of T tiles and thread block c of C (at most T)
 // takes the tiles [c*T/C, (c+1)*T/C): whatever the lengths are, every thread block streams the same number of tiles.  A
 // piece that covers a whole item writes its output; the at most two pieces of a range that do not (its first and its
 // last) leave (maximum, sum, weighted sum of values) in the workspace and a second kernel, launched before the first
@@ -30,7 +30,10 @@
 namespace halo {
 namespace {
 
-constexpr int kMaxSplitRows = 16;   // query heads per item
+// Query heads per item, at most.  bf16: the rows of an mma.  fp32: more rows per warp would leave few warps per SM that take
+// long over a run; the cache is read once per four heads instead, from L2 but for the first (64 sequences of up to 1000
+// positions, 8 heads of 128 on one: 46 us with 16 rows, 25; one of 29000, 16 heads of 256 on one: 92 and 50).
+__host__ __device__ constexpr int item_rows(bool f32) { return f32 ? 4 : 16; }
 
 // What the join has to know of a range whose last piece begins an item that it does not end; in front of the slots.
 struct __align__(32) Cut {
@@ -43,6 +46,7 @@ struct PagedArgs {
     int n_seq, H, Hk, G, qblocks, dh, page_size, page_shift, n_pages, max_pages;   // page_shift: -1 = no power of two
     int slot;    // floats of a workspace slot
     int rows;    // query heads of an item, at most
+    int block;   // query heads from one item of a K/V head to the next
     int merge;   // bytes in front of the rings where the warps meet
     long long page_stride, q_stride;
     float scale_log2;
@@ -101,7 +105,7 @@ constexpr int kSlotHead = 32;       // floats in front of a slot's values: maxim
 template <typename T, int DP, int GR>
 struct Cfg {
     static constexpr bool kF32 = sizeof(T) == 4;
-    static constexpr int kWarps = kF32 && DP == 256 ? (GR == 16 ? 2 : 3) : kF32 && DP == 128 && GR == 1 ? 3 : 4;
+    static constexpr int kWarps = kF32 && (DP == 256 || (DP == 128 && GR == 1)) ? 3 : 4;
     // fp32: two stages, so that two thread blocks of four warps fit an SM at head sizes up to 64, or of three at 128 with
     // one query head per K/V head.  64 sequences of up to 2000 positions, 32 / 8 heads of 64: 77 us with three stages and
     // one thread block, 59 so; 5 of up to 900, 8 / 8 heads of 128: 13.1 us with one thread block of four warps, 10.4 so.
@@ -116,12 +120,12 @@ struct Cfg {
     static constexpr int kRings = kWarps * kWarpBytes;
     static constexpr int kMergeRow = DP + 4;                         // floats
     // two warps' sums at a time, of the item's query heads
-    static constexpr int merge_bytes(int rows) { return kWarps > 2 ? 2 * rows * kMergeRow * 4 : rows * kMergeRow * 4; }
+    static constexpr int merge_bytes(int rows) { return 2 * rows * kMergeRow * 4; }
     static constexpr int kMaxSmem = kRings + merge_bytes(GR);
     // an SM has 228 KB; a thread block takes its own, wm and wl, and 1 KB of the system's
     static constexpr int kFit = 228 * 1024 / (kMaxSmem + 2 * kWarps * 16 * 4 + 1024);
     static constexpr int kBlocksPerSm = kFit > 4 ? 4 : kFit;
-    static_assert(kMaxSmem <= 225 * 1024, "shared memory");
+    static_assert(kMaxSmem <= 225 * 1024 && (kWarps == 3 || kWarps == 4), "shared memory; the warps meet in two steps");
 };
 
 __device__ __forceinline__ int valid_len(const PagedArgs& a, int s, bool flag) {
@@ -210,7 +214,7 @@ struct Walk {
         t1 = static_cast<int>(min(static_cast<long long>(nt), t0 + left));
         reach = len;
         if (a.keep) {
-            const int h0 = hi / a.qblocks * a.G + hi % a.qblocks * 16, n = min(16, a.G - hi % a.qblocks * 16);
+            const int first = hi % a.qblocks * a.block, h0 = hi / a.qblocks * a.G + first, n = min(a.block, a.G - first);
             bool any = false;
             for (int r = 0; r < n; ++r) any |= head_kept(a, h0 + r);
             if (!any) reach = 0;
@@ -375,8 +379,8 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
     bool first = true;
     while (con.left > 0 || (first && a.split)) {
         first = false;
-        const int kvh = con.hi / a.qblocks, r0 = (con.hi % a.qblocks) * 16;
-        const int rows = min(16, a.G - r0), h0 = kvh * a.G + r0;
+        const int kvh = con.hi / a.qblocks, r0 = (con.hi % a.qblocks) * a.block;
+        const int rows = min(a.block, a.G - r0), h0 = kvh * a.G + r0;
         const T* qrow = static_cast<const T*>(a.q) + static_cast<long long>(con.s) * a.q_stride + static_cast<long long>(h0) * a.dh;
         const bool complete = con.t0 == 0 && con.t1 == con.nt;
         float* slot = a.ws + (static_cast<long long>(blockIdx.x) * 2 + (con.left == range ? 0 : 1)) * a.slot;
@@ -688,14 +692,13 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
 #pragma unroll
                         for (int v = 0; v < V; ++v) o[r][v] += mg[(b * rows + r) * C_::kMergeRow + at(r, v)];
             };
-            constexpr int kB = C_::kWarps > 2 ? 1 : 0;
             if (warp >= 2) put(warp - 2);
-            if (C_::kWarps > 2) __syncthreads();
+            __syncthreads();
             if (warp + 2 < C_::kWarps) add(warp);
-            if (warp == 1) put(kB);
+            if (warp == 1) put(1);
             __syncthreads();
             if (warp == 0) {
-                add(kB);
+                add(1);
                 if (a.split > 1) {
                     put(0);
 #pragma unroll
@@ -766,8 +769,8 @@ struct Opened {
     __device__ __forceinline__ Opened(const PagedArgs& a, const int4& head, bool fills, int c0, long long total, int C) {
         s = head.y;
         kvh = head.z / a.qblocks;
-        r0 = (head.z % a.qblocks) * 16;
-        rows = min(16, a.G - r0);
+        r0 = (head.z % a.qblocks) * a.block;
+        rows = min(a.block, a.G - r0);
         pieces = range_of(total, cut(total, c0 + 1, C) + head.w - 1, C) - c0 + 1;
         // piece 0 in the slot of range c0 that holds its end (its first one if the item fills the range), the others in
         // the first slots of the ranges behind it
@@ -928,8 +931,9 @@ LaunchPlan plan_of(const halo_paged_shape& sh, int n_seq) {
     const long long cap = static_cast<long long>(sh.max_pages) * sh.page_size;
     const long long tiles = (cap + C_::kTile - 1) / C_::kTile;
     LaunchPlan p;
-    p.items = static_cast<long long>(n_seq) * sh.n_kv_heads * ((G + 15) / 16);
-    p.rows = G < 16 ? G : 16;
+    constexpr int kBlock = item_rows(C_::kF32);
+    p.items = static_cast<long long>(n_seq) * sh.n_kv_heads * ((G + kBlock - 1) / kBlock);
+    p.rows = G < kBlock ? G : kBlock;
     p.slot = kSlotHead + p.rows * DP;
     p.merge = (C_::merge_bytes(p.rows) + 15) / 16 * 16;
     const long long resident = static_cast<long long>(kSmCount) * C_::kBlocksPerSm;
@@ -991,8 +995,7 @@ auto by_rows(const halo_paged_shape& sh, F f) {
         return G <= 8 ? f(T(), D(), std::integral_constant<int, 8>()) : f(T(), D(), std::integral_constant<int, 16>());
     } else {
         if (G == 1) return f(T(), D(), std::integral_constant<int, 1>());
-        if (G <= 4) return f(T(), D(), std::integral_constant<int, 4>());
-        return f(T(), D(), std::integral_constant<int, 16>());
+        return f(T(), D(), std::integral_constant<int, 4>());
     }
 }
 template <typename F>
@@ -1056,7 +1059,8 @@ extern "C" halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, 
     a.H = shape->n_heads;
     a.Hk = shape->n_kv_heads;
     a.G = a.H / a.Hk;
-    a.qblocks = (a.G + kMaxSplitRows - 1) / kMaxSplitRows;
+    a.block = item_rows(shape->dtype == HALO_F32);
+    a.qblocks = (a.G + a.block - 1) / a.block;
     a.dh = shape->head_dim;
     a.page_size = shape->page_size;
     a.page_shift = -1;
