@@ -14,8 +14,9 @@
 // short sequence's first rows are on their way while the one before it is still being summed.
 //   bf16: scores and weighted sums through mma.sync m16n8k16 with the query heads as the 16 rows of A: one new token
 //     makes a matrix of at most 16 rows that cannot fill a tcgen05 tile of 128, and the stream of K and V bounds the
-//     kernel, not the tensor pipe.  Weights are rounded to bf16 for the second product (relative 2^-8, like the output);
-//     their sum is taken in fp32 before that rounding.
+//     kernel, not the tensor pipe.  A weight meets the values as two bf16 numbers, its upper bits and what they leave
+//     (together 2^-15 of it): one of them alone would be as far off as the output's own rounding.  With up to 8 heads
+//     the second numbers take the rows of A that are otherwise empty and cost no instruction of their own.
 //   fp32: fused multiply-adds, two lanes per position for the scores, a column per lane for the weighted sums.
 //
 // bf16, 32 / 8 heads of 128: one sequence of 131071 positions 84 us + 5 for the join (537 MB: 6.4 TB/s in the first
@@ -92,6 +93,13 @@ __device__ __forceinline__ float pow2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// A weight p of at most 1 as two bf16 numbers, neither negative: its upper 16 bits, and the rest rounded.  The rest is kept
+// above 2^-126 (weights are relative to the largest, 1, and smaller ones count as 0), so that a value of infinity meets two
+// positive factors where the weight is positive, and not the zero that the rest of a power of two would be.
+__device__ __forceinline__ uint32_t upper_bf16(float a, float b) {
+    return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+}
+__device__ __forceinline__ float rest_of(float p) { return fmaxf(p - __uint_as_float(__float_as_uint(p) & 0xffff0000u), 0x1p-126f); }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
@@ -466,11 +474,17 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int j = 0; j < 2 * kK; ++j) o[n][j] *= f[j >> 1];
+                        for (int j = 0; j < 4; ++j) o[n][j] *= f[kK == 2 ? j >> 1 : 0];
                 }
-                // weighted sum of the values
-                const uint32_t pa[4] = {pack_bf16(sc[0][0], sc[0][1]), kK == 2 ? pack_bf16(sc[0][2], sc[0][3]) : 0u,
-                                        pack_bf16(sc[1][0], sc[1][1]), kK == 2 ? pack_bf16(sc[1][2], sc[1][3]) : 0u};
+                // weighted sum of the values: the weights' upper bits and their rests, these in the rows 8 to 15 of the
+                // same product (up to 8 heads; o[n][2], o[n][3] are their sums) or in one of their own
+                uint32_t pa[4], pr[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float* w = &sc[j >> 1][kK == 2 ? (j & 1) * 2 : 0];
+                    if (kK == 2 || !(j & 1)) pa[j] = upper_bf16(w[0], w[1]);
+                    if (kK == 2 || (j & 1)) (kK == 2 ? pr : pa)[j] = pack_bf16(rest_of(w[0]), rest_of(w[1]));
+                }
                 const int key = ((lane >> 3) & 1) * 8 + (lane & 7), half = lane >> 4;
 #pragma unroll
                 for (int n = 0; n < NT; n += 2) {
@@ -479,8 +493,16 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                     ldsm4t(b, st + C_::kHalf + key * C_::kRowBytes + ((c & ~7) | ((c ^ key) & 7)) * 16);
                     mma_bf16(o[n], pa, b[0], b[1]);
                     mma_bf16(o[n + 1], pa, b[2], b[3]);
+                    if constexpr (kK == 2) {
+                        mma_bf16(o[n], pr, b[0], b[1]);
+                        mma_bf16(o[n + 1], pr, b[2], b[3]);
+                    }
                 }
                 __syncwarp();   // the stage is free for the copies that the next round starts
+            }
+            if constexpr (kK == 1) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) { o[n][0] += o[n][2]; o[n][1] += o[n][3]; }
             }
             // the warps meet: common maxima and sums, then the weighted sums of warps 2 and 3 go to 0 and 1, of 1 to 0
 #pragma unroll
