@@ -446,8 +446,8 @@ halo_status halo_group_lm_head_i4(const halo_lm_shape* shape, const void* Q, con
  *   values as the sum of two bf16 numbers (off by at most 2^-15 of it, the output's rounding by 2^-8).
  *   A length that is negative or behind the table counts as 0, positions on a page out of range are left out; both set
  *   HALO_DEV_BAD_INDEX.
- *   workspace: halo_paged_mha_workspace_bytes(shape, n_seq) bytes, device; calls that may overlap on the GPU need one
- *   each.  The result does not depend on timing.  n_seq <= HALO_MAX_SEQUENCES.
+ *   workspace: halo_paged_mha_workspace_bytes(shape, n_seq) bytes, device, 16-byte aligned; calls that may overlap on the
+ *   GPU, or that host threads make to one stream at the same time, need one each.  The result does not depend on timing.  n_seq <= HALO_MAX_SEQUENCES.
  *
  * halo_norm_glue: halo_glue with a norm behind the block, gains, a gate and a residual scale:
  *     n(v) = v / sqrt(mean(v^2) + eps),  u = w_post ? n(y) * w_post : y,

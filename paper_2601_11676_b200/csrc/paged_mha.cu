@@ -36,12 +36,14 @@ namespace {
 // positions, 8 heads of 128 on one: 46 us with 16 rows, 25; one of 29000, 16 heads of 256 on one: 92 and 50).
 __host__ __device__ constexpr int item_rows(bool f32) { return f32 ? 4 : 16; }
 
-// What the join has to know of a range whose last piece begins an item that it does not end; in front of the slots.
-struct __align__(32) Cut {
+// What the join has to know of a range whose last piece begins an item that it does not end; in front of the slots, at the
+// start of a workspace that the caller aligns to 16 bytes and no more.
+struct __align__(16) Cut {
     int opens, s, hi, rest;   // rest: tiles of the item behind the range
     long long total;          // T
     int fills, unused;        // the item's first piece is the whole range
 };
+static_assert(alignof(Cut) == 16 && sizeof(Cut) == 32, "two 16-byte words, anywhere in a workspace");
 
 struct PagedArgs {
     int n_seq, H, Hk, G, qblocks, dh, page_size, page_shift, n_pages, max_pages;   // page_shift: -1 = no power of two

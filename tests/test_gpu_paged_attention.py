@@ -137,3 +137,30 @@ def test_the_bound_itself_follows_the_oracle():
         assert np.allclose(got[i].cpu().numpy(), want[i], rtol=1e-12, atol=1e-14)
     kept = keep.cpu().numpy() != 0
     assert np.allclose(got[3].cpu().numpy()[:, kept], want[3][:, kept], rtol=1e-12) and got[4] == want[4]
+
+
+# ---- the line: items cut over thread blocks and joined --------------------------------------------------------------
+
+def line_case(dtype, H, Hk, dh, page, lens, seed, cols=None):
+    t, g = TYPES[dtype][0], gen(seed)
+    table, n_pages = block_table(g, lens, page, cols)
+    K, V = (randn(g, (n_pages, Hk, page, dh), t) for _ in range(2))
+    q, n = randn(g, (len(lens), H, dh), t), torch.tensor(lens, dtype=torch.int32, device=DEV)
+    sh = B.paged_shape(H, Hk, dh, page, n_pages, table.shape[1], TYPES[dtype][1])
+    assert B.halo_paged_mha_workspace_bytes(sh, len(lens)) > 0      # no clusters: what is tested here is the line
+    return sh, q, K, V, table, n
+
+
+@pytest.mark.parametrize("dtype,lens", [("bf16", [20000]), ("bf16", [i * 31 % 3000 for i in range(100)]), ("f32", [9001, 3000])])
+def test_a_workspace_is_aligned_to_16_bytes_and_no_more(dtype, lens):
+    sh, q, K, V, table, n = line_case(dtype, 8, 2, 64, 16, lens, 3)
+    need = B.halo_paged_mha_workspace_bytes(sh, len(lens))
+    out, lse = check(dtype, q, K, V, table, n, 0.125)
+    for offset in (16, 48):
+        pool = torch.full((need + 128,), 255, dtype=torch.uint8, device=DEV)
+        at = -pool.data_ptr() % 64 + offset
+        ws = pool[at:at + need]
+        assert ws.data_ptr() % 32 == 16
+        again, lse2, _ = attend(sh, q, K, V, table, n, 0.125, ws=ws)
+        assert torch.equal(again, out) and torch.equal(lse2, lse)
+        assert (pool[:at] == 255).all() and (pool[at + need:] == 255).all()
