@@ -164,3 +164,119 @@ def test_a_workspace_is_aligned_to_16_bytes_and_no_more(dtype, lens):
         again, lse2, _ = attend(sh, q, K, V, table, n, 0.125, ws=ws)
         assert torch.equal(again, out) and torch.equal(lse2, lse)
         assert (pool[:at] == 255).all() and (pool[at + need:] == 255).all()
+
+
+# Many items of a few pieces each (the join by range) and few of many (by item); several blocks of query heads, pages that end
+# inside a run, heads that are not as wide as their tiles, empty sequences between long ones.
+LINE = [
+    # dtype, H, Hk, dh, page, lengths
+    ("bf16", 32, 8, 128, 16, [(i * 613) % 1500 for i in range(64)]),
+    ("f32", 8, 1, 128, 16, [(i * 211) % 900 for i in range(40)]),
+    ("bf16", 20, 1, 80, 7, [(i * 613) % 1500 for i in range(60)]),
+    ("bf16", 8, 2, 256, 16, [(i * 389) % 900 for i in range(64)]),
+    ("f32", 6, 2, 48, 5, [(i * 389) % 900 for i in range(80)]),
+    ("f32", 17, 1, 256, 16, [(i * 127) % 300 for i in range(60)]),
+    ("bf16", 40, 2, 64, 3, [(i * 523) % 1200 for i in range(150)]),
+    ("bf16", 8, 8, 128, 48, [(i * 239) % 500 for i in range(64)]),
+    ("f32", 5, 5, 128, 16, [(i * 311) % 700 for i in range(120)]),
+    ("bf16", 20, 1, 80, 7, [7000, 0, 2500]),
+    ("f32", 10, 2, 80, 16, [6000, 1, 0]),
+    ("bf16", 32, 1, 128, 16, [9000]),
+]
+
+
+@pytest.mark.parametrize("case", range(len(LINE)))
+@pytest.mark.parametrize("spoilt", [False, True])
+def test_items_cut_over_thread_blocks(case, spoilt):
+    """spoilt: lost heads (a whole block of query heads among them), pages out of range, lengths out of range."""
+    dtype, H, Hk, dh, page, lens = LINE[case]
+    sh, q, K, V, table, n = line_case(dtype, H, Hk, dh, page, lens, 50 + case)
+    assert (B.halo_paged_mha_workspace_bytes(sh, len(lens)) > 0) and max(lens) > 64
+    keep = None
+    if spoilt:
+        block, G = 16 if dtype == "bf16" else 4, H // Hk
+        keep = torch.tensor([int(h % 3 != 1 and not (G > block and h % G < block)) for h in range(H)], dtype=torch.uint8, device=DEV)
+        if not bool(keep.any()):
+            keep[-1] = 1
+        longest = int(n.argmax())
+        table[longest, (max(lens) - 1) // page // 2] = sh.n_pages      # a page of a sequence that is cut
+        table[longest, 0] = -7
+        if len(lens) > 4:
+            n[1], n[3] = -2, sh.max_pages * page + 1
+    out, lse = check(dtype, q, K, V, table, n, dh ** -0.5, keep)
+    for _ in range(2):
+        again, lse2, _ = attend(sh, q, K, V, table, n, dh ** -0.5, keep)
+        assert torch.equal(again, out) and torch.equal(lse2, lse)
+
+
+@pytest.mark.parametrize("dtype,lens", [("bf16", [(i * 613) % 1500 for i in range(64)]), ("bf16", [20000, 5]), ("f32", [(i * 211) % 900 for i in range(40)])])
+def test_joined_calls_on_two_streams_at_once(dtype, lens):
+    """Two calls that overlap, each with its own workspace; then one workspace for calls in a row on one stream."""
+    H, Hk = (32, 8) if dtype == "bf16" else (8, 1)
+    sh, q, K, V, table, n = line_case(dtype, H, Hk, 128, 16, lens, 4)
+    need = B.halo_paged_mha_workspace_bytes(sh, len(lens))
+    qs = [q, randn(gen(5), q.shape, q.dtype)]
+    alone = [check(dtype, x, K, V, table, n, 0.09) for x in qs]
+    streams, outs = [torch.cuda.Stream() for _ in qs], [torch.empty_like(q) for _ in qs]
+    lses = [torch.empty(q.shape[:2], dtype=torch.float32, device=DEV) for _ in qs]
+    ws = [torch.empty(need, dtype=torch.uint8, device=DEV) for _ in qs]
+    torch.cuda.synchronize()
+    for _ in range(30):
+        for x, o, l, w, st in zip(qs, outs, lses, ws, streams):
+            B.halo_paged_mha(sh, x, K, V, table, n, 0.09, o, w, lse=l, stream=st)
+    torch.cuda.synchronize()
+    for (a, b), o, l in zip(alone, outs, lses):
+        assert torch.equal(o, a) and torch.equal(l, b)
+    for _ in range(10):
+        for x, o, l in zip(qs, outs, lses):
+            B.halo_paged_mha(sh, x, K, V, table, n, 0.09, o, ws[0], lse=l)
+    torch.cuda.synchronize()
+    for (a, b), o, l in zip(alone, outs, lses):
+        assert torch.equal(o, a) and torch.equal(l, b)
+
+
+@pytest.mark.parametrize("n_seq,cap", [(64, 1500), (2, 20000)])
+def test_append_and_joined_attention_captured_into_a_graph(n_seq, cap):
+    """One captured append + attention (line and join) replayed for new tokens and lengths, as on a side stream."""
+    H, Hk, dh, page, t = 32, 8, 128, 16, torch.bfloat16
+    sh, q, K, V, table, n = line_case("bf16", H, Hk, dh, page, [cap] * n_seq, 6)
+    ws = torch.empty(B.halo_paged_mha_workspace_bytes(sh, n_seq), dtype=torch.uint8, device=DEV)
+    inv = 10000.0 ** (-torch.arange(0, dh, 2, dtype=torch.float64, device=DEV) / dh)
+    g = gen(7)
+    qkv = randn(g, (n_seq, H + 2 * Hk, dh), t)
+    pos = n - 1
+    q_out, out = torch.empty_like(q), torch.empty_like(q)
+    lse = torch.empty((n_seq, H), dtype=torch.float32, device=DEV)
+    side = torch.cuda.Stream()
+
+    def step(stream=None):
+        B.halo_paged_kv_append(sh, qkv[:, :H], qkv[:, H:H + Hk], qkv[:, H + Hk:], pos, None, table, inv, False, q_out, K, V,
+                               stream=stream)
+        B.halo_paged_mha(sh, q_out, K, V, table, n, dh ** -0.5, out, ws, lse=lse, stream=stream)
+
+    side.wait_stream(torch.cuda.current_stream())
+    step(side)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn in range(3):
+        qkv.copy_(randn(g, qkv.shape, t))
+        pos.copy_(torch.randint(0, cap, (n_seq,), generator=g, device=DEV))
+        n.copy_(pos + 1)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed, lse1 = out.clone(), lse.clone()
+        side.wait_stream(torch.cuda.current_stream())
+        step(side)
+        side.synchronize()
+        assert torch.equal(out, replayed) and torch.equal(lse, lse1)
+        again, _ = check("bf16", q_out, K, V, table, n, dh ** -0.5)
+        assert torch.equal(again, replayed)
+
+
+def test_short_sequences_under_a_wide_table():
+    """A table as wide as the longest context that a server admits; what is in use is short."""
+    for dtype, lens, cols in (("bf16", [700], 8192), ("bf16", [3, 0, 17, 200], 4096), ("f32", [40, 1], 2048)):
+        sh, q, K, V, table, n = line_case(dtype, 32 if dtype == "bf16" else 4, 4, 64, 16, lens, 8, cols)
+        check(dtype, q, K, V, table, n, 0.125)
