@@ -210,13 +210,15 @@ group_ffn_stream_kernel(int d, int S, int G, const __nv_bfloat16* __restrict__ W
     if (tid == 0 && *abort_flag) flag_status(dev_status, HALO_DEV_TIMEOUT);
 }
 
-// Zero-fill of the partial slots; lets the dependent streaming kernel start at once.
+// Zero-fill of the partial slots; lets the dependent kernel start under the fill.
 __global__ void __launch_bounds__(256)
 zero_partials_kernel(float4* __restrict__ p, size_t n4) {
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    // itself launched as a programmatic dependent: whatever ran before it on the stream (say the previous call's
-    // streaming kernel, which may still be adding to these very slots) must have completed before anything is zeroed
+    // Itself launched as a programmatic dependent: whatever ran before it on the stream (say the previous call's
+    // streaming kernel, which may still be adding to these very slots) must have completed before anything is zeroed,
+    // and before the dependent is released: that one reads its tokens and its group list, and mha_fused_kernel appends
+    // to the caches, ahead of its own wait.
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const size_t i = static_cast<size_t>(blockIdx.x) * blockDim.x + threadIdx.x;
     if (i < n4) p[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 }
@@ -275,7 +277,7 @@ halo_status launch_stream_cfg(const halo_ffn_shape& sh, const void* W, const voi
         HALO_CHECK_LAUNCH();
         return HALO_OK;
     }
-    // zero-fill as a kernel that releases its dependent at once, then the streaming kernel as that dependent: its
+    // zero-fill as a kernel that releases its dependent before it fills, then the streaming kernel as that dependent: its
     // prologue and its weight stream run under the zero-fill; it waits for it only before it first adds to `partials`
     if (launch_zero_partials(partials, static_cast<size_t>(n_dev + 1) * n_tok * sh.d_model, st) != HALO_OK) return HALO_ERR_CUDA;
     cudaLaunchConfig_t cfg{};

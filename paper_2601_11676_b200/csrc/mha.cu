@@ -876,7 +876,7 @@ static halo_status mha_block_typed(const halo_mha_shape& sh, const void* Wp, con
                                    cudaStream_t st, bool already_zero) {
     constexpr int E = Elem<T>::kPerChunk;
     const int d = sh.d_model, H = sh.n_heads, dh = sh.head_dim;
-    // the zero-fill releases this launch at once: the row products and the attention run under it
+    // the zero-fill releases this launch before it fills: the row products and the attention run under it
     if (!already_zero && launch_zero_partials(partials, static_cast<size_t>(n_dev + 1) * d, st) != HALO_OK) return HALO_ERR_CUDA;
     const int iters = (d / E + 255) / 256;
     cudaLaunchConfig_t cfg{};

@@ -230,3 +230,35 @@ def test_mha_block_on_int4_weights_matches_the_oracle(d, H, dh, L, positions):
             ref = R.group_mha_i4(Qp_h, Sp_h, H, hb(x)[0], Kh, Vh, pos, keep, dev, 3)
             rms = np.sqrt(np.mean(ref.sum(0) ** 2))
             assert np.abs(P.cpu().numpy() - ref).max() <= U.TOL_BF16 * rms, (pos, len(keep))
+
+
+def test_mha_block_calls_in_a_row_at_one_position_of_one_cache():
+    """Calls back to back that write the same place of one cache: each sees its own keys and values, not those of the call
+    behind it, which starts its row products under the zero-fill of its slots.  A column is 64 fp32 additions in any order:
+    off by at most 64 * 2^-24 of the sum of their sizes, which is 1e-4 rms where that sum is 26 rms (64 terms of a random
+    sign: about 6).  A foreign key among the four of each head would show at a tenth of it."""
+    d, H, dh, L, pos, turns = 512, 8, 64, 64, 3, 24
+    wl = _wl("bf16", d)
+    sh = B.mha_shape(d, H, dh, L, B.BF16)
+    Wq, Wk, Wv, Wo = synth.mha_matrices(wl, 0, H, DEV)
+    Wp = torch.empty((H, 2, dh, d), dtype=torch.bfloat16, device=DEV)
+    B.halo_pack_mha_weights(sh, Wq, Wo, Wp)
+    K0, V0 = _caches(wl, H, L, dh, L)
+    kl, nk = torch.arange(H, dtype=torch.int32, device=DEV), torch.tensor([H], dtype=torch.int32, device=DEV)
+    xs = [synth.activation(wl, 900 + i, DEV) * (1 + i % 5) for i in range(turns)]
+
+    def run(wait):
+        K, V = K0.clone(), V0.clone()
+        P = [torch.full((1, d), float("nan"), dtype=torch.float32, device=DEV) for _ in xs]
+        torch.cuda.synchronize()
+        for x, p in zip(xs, P):
+            B.halo_mha_block(sh, Wp, Wk, Wv, x, K, V, pos, kl, nk, None, 0, p)
+            if wait:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return torch.stack(P), K, V
+
+    (P1, K1, V1), (P2, K2, V2) = run(True), run(False)
+    assert torch.equal(K1, K2) and torch.equal(V1, V2)
+    rms = P1.square().mean(-1, keepdim=True).sqrt()
+    assert ((P1 - P2).abs() <= 1e-4 * rms).all()
