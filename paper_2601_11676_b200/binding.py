@@ -7,6 +7,7 @@ built (``python -m paper_2601_11676_b200.build``); there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import importlib
 import os
 from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int, c_int32, c_longlong, c_size_t, \
     c_uint8, c_uint32, c_uint64, c_void_p
@@ -464,11 +465,19 @@ _native = None
 
 
 def _marshal():
-    """The _marshal module, bound to this library's entry points."""
+    """The _marshal module, bound to this library's entry points; raises if it is missing or was made for another torch."""
     global _native
     if _native is None:
         L = lib()
-        from . import _marshal as m
+        from .build import marshal_made_for
+        again = "build it with `python -m paper_2601_11676_b200.build`"
+        try:
+            m = importlib.import_module("._marshal", __package__)
+        except ImportError as e:
+            raise ImportError(f"_marshal.so is missing or cannot be loaded ({e}): {again}") from e
+        made_for = getattr(m, "made_for", "an older source")
+        if made_for != marshal_made_for():
+            raise ImportError(f"_marshal.so was made for {made_for}, this is {marshal_made_for()}: {again}")
         names = ("halo_paged_kv_append", "halo_paged_mha", "halo_norm_glue", "halo_quantize_rows_mx4", "halo_dequantize_rows_mx4",
                  "halo_product_mx4")
         m.bind(*(ctypes.cast(getattr(L, n), c_void_p).value for n in names))

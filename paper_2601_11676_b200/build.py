@@ -5,6 +5,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import warnings
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -38,6 +39,12 @@ def _deps_mtime() -> float:
     return max(os.path.getmtime(p) for p in hdrs)
 
 
+def marshal_made_for() -> str:
+    """What _marshal.so depends on beside its source; compiled into it and compared when it is loaded."""
+    import torch
+    return f"torch {torch.__version__}, python {sys.version_info.major}.{sys.version_info.minor}"
+
+
 def build_marshal(force: bool = False) -> str:
     """_marshal.so; rebuilt when its source, halo.h or the torch it was built against changed."""
     import sysconfig
@@ -56,6 +63,7 @@ def build_marshal(force: bool = False) -> str:
                                                 os.path.join(ROOT, "include")]
     tmp = MARSHAL + f".tmp{os.getpid()}"
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           f'-DMARSHAL_MADE_FOR="{marshal_made_for()}"',
            *(f"-I{p}" for p in includes), MARSHAL_SRC, "-o", tmp, f"-L{lib_dir}", f"-Wl,-rpath,{lib_dir}", "-lc10", "-lc10_cuda",
            "-ltorch_cpu", "-ltorch", "-ltorch_python"]
     p = subprocess.run(cmd, capture_output=True, text=True)
@@ -95,7 +103,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
         tmp = LIB + f".tmp{os.getpid()}"
         run([_nvcc(), "-shared", "-o", tmp, *objs, "-lcudart"])
         os.replace(tmp, LIB)
-    build_marshal(force)
+    try:
+        build_marshal(force)
+    except Exception as e:     # no g++, no headers of Python or torch: the library is complete without it
+        if os.path.exists(MARSHAL):
+            os.remove(MARSHAL)     # of an older source
+        warnings.warn(f"{MARSHAL} was not built, so the entry points of a batched token step (halo_paged_*, halo_norm_glue, "
+                      f"halo_*_mx4) cannot be called from Python: {e}")
     return LIB
 
 

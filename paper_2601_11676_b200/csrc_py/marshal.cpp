@@ -323,4 +323,14 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, method
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__marshal() { return PyModule_Create(&module_def); }
+#ifndef MARSHAL_MADE_FOR
+#define MARSHAL_MADE_FOR ""
+#endif
+PyMODINIT_FUNC PyInit__marshal() {
+    PyObject* m = PyModule_Create(&module_def);
+    if (m && PyModule_AddStringConstant(m, "made_for", MARSHAL_MADE_FOR) != 0) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}
