@@ -480,7 +480,7 @@ def _marshal():
             raise ImportError(f"_marshal.so was made for {made_for}, this is {marshal_made_for()}: {again}")
         names = ("halo_paged_kv_append", "halo_paged_mha", "halo_norm_glue", "halo_quantize_rows_mx4", "halo_dequantize_rows_mx4",
                  "halo_product_mx4")
-        m.bind(*(ctypes.cast(getattr(L, n), c_void_p).value for n in names))
+        m.bind(*(ctypes.cast(getattr(L, n), c_void_p).value for n in names), PagedShape, NormShape)
         _native = m
     return _native
 

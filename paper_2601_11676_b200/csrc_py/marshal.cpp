@@ -9,6 +9,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <exception>
+#include <type_traits>
 
 #include "halo.h"
 
@@ -62,15 +63,20 @@ c10::ScalarType type_of(const char* what, int code) {
     if (code == HALO_BF16) return c10::kBFloat16;
     refuse(what, "the element type", "is unknown");
 }
+PyObject *paged_shape_type, *norm_shape_type;   // the binding's structures
+// A ctypes structure: its bytes.  Compared by type, not by size: other shapes of the library have as many.
 template <typename S>
-S shape_of(const char* what, PyObject* o) {   // a ctypes structure: its bytes
+S shape_of(const char* what, PyObject* o) {
+    const int is = PyObject_IsInstance(o, std::is_same<S, halo_paged_shape>::value ? paged_shape_type : norm_shape_type);
+    if (is < 0) throw Refused();
+    if (is == 0) refuse(what, "the shape", "has another type");
     Py_buffer b;
     if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) throw Refused();
     S s;
     const bool ok = b.len == static_cast<Py_ssize_t>(sizeof(S));
     if (ok) memcpy(&s, b.buf, sizeof(S));
     PyBuffer_Release(&b);
-    if (!ok) refuse(what, "the shape", "has another type");
+    if (!ok) refuse(what, "the shape", "has another size");
     return s;
 }
 
@@ -287,9 +293,9 @@ PyObject* product(PyObject*, PyObject* const* a, Py_ssize_t n) {   // d, n_tok, 
     });
 }
 
-PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {   // addresses, in the order of Entry
-    if (n != 6) {
-        PyErr_SetString(PyExc_TypeError, "_marshal.bind: six addresses");
+PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {   // addresses, in the order of Entry, and the two types of shape
+    if (n != 8) {
+        PyErr_SetString(PyExc_TypeError, "_marshal.bind: six addresses and two types");
         return nullptr;
     }
     void* p[6];
@@ -306,6 +312,10 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {   // addresses, in
     entry.quantize = reinterpret_cast<decltype(entry.quantize)>(p[3]);
     entry.dequantize = reinterpret_cast<decltype(entry.dequantize)>(p[4]);
     entry.product = reinterpret_cast<decltype(entry.product)>(p[5]);
+    Py_INCREF(a[6]);
+    Py_INCREF(a[7]);
+    paged_shape_type = a[6];
+    norm_shape_type = a[7];
     bound = true;
     Py_RETURN_NONE;
 }

@@ -327,3 +327,16 @@ def test_append_in_place_needs_one_stride(lib):
                                         None, None)
 
     assert append(3, 512, 520) == -1 and append(2, 768, 512) == -1
+
+
+def test_attention_block_binding_refuses_a_shape_of_another_kind(lib):
+    """Other shapes have as many bytes: a head's {d, vocab, group, type} would pass for a norm's {d, eps, type, type}."""
+    import torch
+    h, x = torch.zeros((2, 64)), torch.zeros((2, 64), dtype=torch.bfloat16)
+    for sh in (B.lm_shape(64, 1 << 23, B.F32, B.BF16), B.ffn_shape(64, 1 << 23, B.F32, B.BF16), None, b"0123456789abcdef"):
+        with pytest.raises(ValueError, match="another type"):
+            B.halo_norm_glue(sh, h, None, None, None, 1.0, None, h, x)
+        with pytest.raises(ValueError, match="another type"):
+            B.halo_paged_mha(sh, x, x, x, x, x, 1.0, x, None)
+    with pytest.raises(ValueError, match="GPU"):
+        B.halo_norm_glue(B.norm_shape(64, 1e-5, B.F32, B.BF16), h, None, None, None, 1.0, None, h, x)
