@@ -740,7 +740,8 @@ halo_status launch_pair(const Operands& o, T* y) {
 template <typename T>
 halo_status by_tokens(const Operands& o, void* y) {
     T* out = static_cast<T*>(y);
-    // us, rows x d.  One token (one / line / pair): 4096 x 4096 4.2 / 5.6 / 7.0, 11008 x 4096 7.2 / 8.9 / 9.0, 24576 x 4096
+    // us, rows x d, the same weights call after call: up to some 100 MB come from L2 (11008 x 4096 for 8 to 64 tokens 7.4 to 7.6
+    // so, 9.4 to 9.6 from HBM).  One token (one / line / pair): 4096 x 4096 4.2 / 5.6 / 7.0, 11008 x 4096 7.2 / 8.9 / 9.0, 24576 x 4096
     // 13.1 / 13.7 / 15.4, 4096 x 11008 8.0 / 10.9 / 12.5, 32000 x 8192 27.8 / 28.1 / 30.0; with more rows, or rows so short
     // that lanes of the one-token kernel stay idle, the line: 16384 x 2048 6.6 / 5.9 / 7.3, 32000 x 256 7.9 / 3.9 / 5.4,
     // 64000 x 5120 37.9 / 31.6 / 36.2.

@@ -8,7 +8,10 @@
 // of q, k and v alike, so cosines, sines and offsets stay in registers; the loads of its first heads are in flight
 // while the angles are computed.  Few tokens: the heads of a token are spread over several thread blocks.
 // Heads of 128, 32 + 2 * 8 of them: 8297 tokens (204 MB read and written) 37 us = 5.5 TB/s, what is left being the two
-// dependent loads (position, page) in front of a thread block's stores; 32 tokens 3.3 to 3.7 us, the launch.
+// dependent loads (position, page) in front of a thread block's stores; fp32 (408 MB) 63 us = 6.5 TB/s; 32 tokens 3.3 to
+// 3.7 us, the launch.  Pairs (i, i + rotary / 2) whose distance is no whole number of 16-byte chunks go an element at a time:
+// heads of 80 (127 MB) 31 us with 80 elements turned and 67 with 40, heads of 96 (153 MB) 41 with 32 turned and 85 with
+// 24; interleaved pairs, fp32 (heads of 80, 40 turned, 255 MB: 42) and few tokens do not have the step.
 #include "common.cuh"
 
 namespace halo {

@@ -16,13 +16,16 @@
 //     makes a matrix of at most 16 rows that cannot fill a tcgen05 tile of 128, and the stream of K and V bounds the
 //     kernel, not the tensor pipe.  A weight meets the values as two bf16 numbers, its upper bits and what they leave
 //     (together 2^-15 of it): one of them alone would be as far off as the output's own rounding.  With up to 8 heads
-//     the second numbers take the rows of A that are otherwise empty and cost no instruction of their own.
+//     the second numbers take the rows of A that are otherwise empty and cost no product of their own (64 sequences of up to
+//     4096 positions 92.7 us with one number, 93.1 with two; 128 of up to 300 positions, 32 / 32 heads, 96 and 99; 16 heads on
+//     one, a sequence of 131071 29.0 and 29.8).
 //   fp32: fused multiply-adds, two lanes per position for the scores, a column per lane for the weighted sums.
 //
-// bf16, 32 / 8 heads of 128: one sequence of 131071 positions 84 us + 5 for the join (537 MB: 6.4 TB/s in the first
-// kernel, HBM), 64 sequences of up to 4096 positions 87 + 4 us (a piece's start and meeting); one sequence of 700
-// positions, 32 / 4 heads of 64: 6.1 us (launch, one chain of loads, a cluster's meeting); fp32, 7 sequences of up to
-// 1500 positions, 8 / 8 heads of 64: 9.5 us (the same chain, 18 MB).
+// bf16, 32 / 8 heads of 128, both kernels: one sequence of 131071 positions 91 us (537 MB: 5.9 TB/s; HBM, and the join
+// behind it), 64 sequences of up to 4096 positions 93 to 95 us (besides, a piece's start and meeting); one sequence of 700
+// positions, 32 / 4 heads of 64: 6.3 us (launch, one chain of loads, a cluster's meeting), 8.5 under a table of 131072
+// positions (the line: the plan goes by the table's width); fp32, 7 sequences of up to 1500 positions, 8 / 8 heads of 64:
+// 9.3 us (the same chain, 18 MB).
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -33,7 +36,8 @@ namespace {
 
 // Query heads per item, at most.  bf16: the rows of an mma.  fp32: more rows per warp would leave few warps per SM that take
 // long over a run; the cache is read once per four heads instead, from L2 but for the first (64 sequences of up to 1000
-// positions, 8 heads of 128 on one: 46 us with 16 rows, 25; one of 29000, 16 heads of 256 on one: 92 and 50).
+// positions, 8 heads of 128 on one: 46 us with 16 rows, 25; one of 29000, 16 heads of 256 on one: 92 and 50; with the cache
+// not in L2 when the call begins 29 and 54).
 __host__ __device__ constexpr int item_rows(bool f32) { return f32 ? 4 : 16; }
 
 // What the join has to know of a range whose last piece begins an item that it does not end; in front of the slots, at the
@@ -847,7 +851,7 @@ __global__ void __launch_bounds__(kRangeJoin) paged_mha_join_range_kernel(const 
 
 // Few items of many pieces.  blockIdx.x = item, blockIdx.y = query head of it; the thread block looks for the item among the
 // records of all ranges (a thread block per range would be one of thousands that find nothing to do: one sequence of 32000
-// positions, 16 heads on one, 32 us and 23 as here).  Groups of DP threads, a column each, take every kGroups-th piece; the
+// positions, 16 heads on one, 32 us and 20 as here).  Groups of DP threads, a column each, take every kGroups-th piece; the
 // first kAhead values of a thread are requested together with the pieces' maxima and sums (one piece per thread).
 constexpr int kItemJoin = 512;
 template <typename T, int DP>
