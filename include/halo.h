@@ -442,12 +442,13 @@ halo_status halo_group_lm_head_i4(const halo_lm_shape* shape, const void* Q, con
  *     every head is lost are not read.
  *   A row without positions (length 0, a lost head, scores that are all -infinity) gives zeros and lse = -infinity.
  *   Cache rows behind the length are not read, whatever they hold.
- *   fp32 sums and softmax (weights to within 2^-126 of the largest); bf16 caches: a weight meets the
- *   values as the sum of two bf16 numbers (off by at most 2^-15 of it, the output's rounding by 2^-8).
+ *   fp32 sums and softmax (weights to within 2^-126 of the largest); bf16 caches: a weight meets the values as the sum of two
+ *   bf16 numbers (off by at most 2^-15 of it; the output's rounding: 2^-8).
  *   A length that is negative or behind the table counts as 0, positions on a page out of range are left out; both set
  *   HALO_DEV_BAD_INDEX.
  *   workspace: halo_paged_mha_workspace_bytes(shape, n_seq) bytes, device, 16-byte aligned; calls that may overlap on the
- *   GPU, or that host threads make to one stream at the same time, need one each.  The result does not depend on timing.  n_seq <= HALO_MAX_SEQUENCES.
+ *   GPU, or that host threads make to one stream at the same time, need one each.  The result does not depend on timing.
+ *   n_seq <= HALO_MAX_SEQUENCES.
  *
  * halo_norm_glue: halo_glue with a norm behind the block, gains, a gate and a residual scale:
  *     n(v) = v / sqrt(mean(v^2) + eps),  u = w_post ? n(y) * w_post : y,
