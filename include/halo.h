@@ -480,6 +480,70 @@ halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, const void*
                            const void* V_cache, const int32_t* block_table, const int32_t* seq_len, const uint8_t* keep,
                            float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
                            uint32_t* dev_status, void* stream);
+
+/* Prompts and 8-bit rows on the same cache: beside the calls above, the append for models that norm queries and keys per head,
+ * caches at half the bytes, and attention of more than one new token per sequence.
+ *
+ * 8-bit caches: K_cache, V_cache uint8 [n_pages][n_kv_heads][page_size][head_dim], one page every page_stride bytes (0 = dense;
+ *   else a multiple of 16); K_scale, V_scale uint8 [n_pages][n_kv_heads][page_size], dense.  A row (one K/V head at one
+ *   position) shares a power of two 2^e, e the smallest integer with amax <= 448 * 2^e, within [-117, 119], stored as the byte
+ *   e + 127; a code is the e4m3 number nearest to x * 2^-e, ties to even.  Every value read back is a bf16 number, exactly.
+ *   A row that holds a NaN or an infinity gets the scale byte 255 and reads back as NaN.  Scale bytes below 10 or above 246
+ *   (but 255) and the codes 0x7f and 0xff are not written; what they read back as is not said.
+ *   shape->dtype (queries, new keys and values, outputs) has to be HALO_BF16.  The calls below take K_scale and V_scale NULL for
+ *   caches in shape->dtype.
+ *
+ * halo_paged_norm_append: halo_paged_kv_append with a norm in front of the rotation, into caches of either kind:
+ *     y = x / sqrt(mean(x^2) + eps) * w   per head, queries with w = w_q, keys with w_k (device [head_dim] in dtype, or NULL:
+ *     y = x); then the rotation of halo_paged_kv_append, the elements that it turns times turn_scale (> 0; 1 for none:
+ *     what frequencies stretched for a long context ask for).  Values are stored as they are.  fp32 between the load and the
+ *     one rounding (to dtype, or to an 8-bit row).  eps > 0 where there is a norm.  Everything else as halo_paged_kv_append.
+ *
+ * halo_paged_kv_read: the keys and values at position pos[t] of sequence seq_of_tok[t] (as in the append) to rows t of k_out and
+ *   v_out, device, n_kv_heads * head_dim elements of dtype every *_stride elements.  Rows with a negative position, and those
+ *   out of range (HALO_DEV_BAD_INDEX), are left as they are.
+ *
+ * halo_paged_mha_f8: halo_paged_mha over an 8-bit cache; its own workspace size.  A query enters the scores with the bits of
+ *   fp16 relative to its row's largest element (8 bits of bf16 fit; what is below 2^-39 of the largest loses some); a weight
+ *   meets the values rounded to fp16 (off by at most 2^-11 of itself, or by 2^-40 of what the largest can be).
+ *
+ * halo_paged_prompt_mha: causal attention of packed chunks of new tokens.  Rows q_start[s] .. q_start[s + 1] - 1 of q are the n_s
+ *   newest tokens of sequence s, whose keys and values are in the cache already: row i of them is at position
+ *   P = seq_len[s] - n_s + i and attends to the positions p <= P, as in halo_paged_mha:
+ *     w = softmax(scale * <q, K_p>),  out = sum_p w_p V_p,  lse = log sum_p exp(scale * <q, K_p>)    per row and head.
+ *   q device, n_tok rows of n_heads * head_dim every q_stride elements; q_start device int32 [n_seq + 1], not decreasing,
+ *   q_start[n_seq] <= n_tok; out device [n_tok][n_heads][head_dim], must not overlap q; lse device fp32 [n_tok][n_heads] or
+ *   NULL.  Rows of no sequence are neither read nor written.  keep as in halo_paged_mha.
+ *   A row that sees nothing (P < 0, a lost head, scores that are all -infinity) gives zeros and lse = -infinity.  What a row does
+ *   not see has no influence on it, NaN and infinities included.
+ *   fp32 sums and softmax; bf16 and 8-bit caches: a weight meets the values rounded to bf16 (2^-8 of itself).
+ *   A sequence whose rows are out of range or decrease is left out, one whose length is negative or behind the table
+ *   counts as empty, positions on a page out of range are left out; each sets HALO_DEV_BAD_INDEX.
+ *   workspace: halo_paged_prompt_mha_workspace_bytes(shape, n_tok, n_seq) bytes, as for halo_paged_mha.  The result does not depend
+ *   on timing.  n_seq <= HALO_MAX_SEQUENCES, n_tok <= HALO_MAX_PROMPT_ROWS.
+ */
+#define HALO_MAX_PROMPT_ROWS (1 << 20)
+halo_status halo_paged_norm_append(const halo_paged_shape* shape, int n_tok, int n_seq, const void* q, long long q_stride,
+                                   const void* k, long long k_stride, const void* v, long long v_stride, const void* w_q,
+                                   const void* w_k, float eps, const int32_t* pos, const int32_t* seq_of_tok,
+                                   const int32_t* block_table, const double* inv_freq, int rotary_dim, int interleaved,
+                                   float turn_scale, void* q_out, long long q_out_stride, void* K_cache, void* V_cache,
+                                   uint8_t* K_scale, uint8_t* V_scale, uint32_t* dev_status, void* stream);
+halo_status halo_paged_kv_read(const halo_paged_shape* shape, int n_tok, int n_seq, const int32_t* pos, const int32_t* seq_of_tok,
+                               const int32_t* block_table, const void* K_cache, const void* V_cache, const uint8_t* K_scale,
+                               const uint8_t* V_scale, void* k_out, long long k_stride, void* v_out, long long v_stride,
+                               uint32_t* dev_status, void* stream);
+size_t halo_paged_mha_f8_workspace_bytes(const halo_paged_shape* shape, int n_seq);
+halo_status halo_paged_mha_f8(const halo_paged_shape* shape, int n_seq, const void* q, long long q_stride, const void* K_cache,
+                              const void* V_cache, const uint8_t* K_scale, const uint8_t* V_scale, const int32_t* block_table,
+                              const int32_t* seq_len, const uint8_t* keep, float scale, void* out, float* lse, void* workspace,
+                              size_t workspace_bytes, uint32_t* dev_status, void* stream);
+size_t halo_paged_prompt_mha_workspace_bytes(const halo_paged_shape* shape, int n_tok, int n_seq);
+halo_status halo_paged_prompt_mha(const halo_paged_shape* shape, int n_tok, int n_seq, const void* q, long long q_stride,
+                                  const int32_t* q_start, const void* K_cache, const void* V_cache, const uint8_t* K_scale,
+                                  const uint8_t* V_scale, const int32_t* block_table, const int32_t* seq_len, const uint8_t* keep,
+                                  float scale, void* out, float* lse, void* workspace, size_t workspace_bytes, uint32_t* dev_status,
+                                  void* stream);
 halo_status halo_norm_glue(const halo_norm_shape* shape, int n_tok, const float* h, const void* y, const void* w_post,
                            const void* gate, long long gate_stride, float res_scale, const void* w_pre, float* h_out,
                            void* x_out, void* stream);

@@ -40,6 +40,8 @@ EXPORTS = [
     "halo_block_stack_create", "halo_block_stack_destroy", "halo_block_stack_decode", "halo_block_stack_status",
     "halo_block_stack_last_launches", "halo_stack_create_i4", "halo_mha_block",
     "halo_paged_kv_append", "halo_paged_mha_workspace_bytes", "halo_paged_mha", "halo_norm_glue",
+    "halo_paged_norm_append", "halo_paged_kv_read", "halo_paged_mha_f8_workspace_bytes", "halo_paged_mha_f8",
+    "halo_paged_prompt_mha_workspace_bytes", "halo_paged_prompt_mha",
     "halo_mx4_scale_bytes", "halo_quantize_rows_mx4", "halo_dequantize_rows_mx4", "halo_product_mx4",
 ]
 
@@ -203,6 +205,22 @@ def lib() -> ctypes.CDLL:
                                      c_void_p, c_float, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p, c_void_p]
         L.halo_norm_glue.argtypes = [POINTER(NormShape), c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_longlong, c_float,
                                      c_void_p, c_void_p, c_void_p, c_void_p]
+        L.halo_paged_norm_append.argtypes = [POINTER(PagedShape), c_int, c_int, c_void_p, c_longlong, c_void_p, c_longlong,
+                                             c_void_p, c_longlong, c_void_p, c_void_p, c_float, c_void_p, c_void_p, c_void_p,
+                                             c_void_p, c_int, c_int, c_float, c_void_p, c_longlong, c_void_p, c_void_p, c_void_p,
+                                             c_void_p, c_void_p, c_void_p]
+        L.halo_paged_kv_read.argtypes = [POINTER(PagedShape), c_int, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                         c_void_p, c_void_p, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_void_p]
+        L.halo_paged_mha_f8_workspace_bytes.argtypes = [POINTER(PagedShape), c_int]
+        L.halo_paged_mha_f8_workspace_bytes.restype = c_size_t
+        L.halo_paged_mha_f8.argtypes = [POINTER(PagedShape), c_int, c_void_p, c_longlong, c_void_p, c_void_p, c_void_p, c_void_p,
+                                        c_void_p, c_void_p, c_void_p, c_float, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p,
+                                        c_void_p]
+        L.halo_paged_prompt_mha_workspace_bytes.argtypes = [POINTER(PagedShape), c_int, c_int]
+        L.halo_paged_prompt_mha_workspace_bytes.restype = c_size_t
+        L.halo_paged_prompt_mha.argtypes = [POINTER(PagedShape), c_int, c_int, c_void_p, c_longlong, c_void_p, c_void_p, c_void_p,
+                                            c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_float, c_void_p, c_void_p,
+                                            c_void_p, c_size_t, c_void_p, c_void_p]
         L.halo_mx4_scale_bytes.argtypes = [c_int, c_longlong]
         L.halo_mx4_scale_bytes.restype = c_size_t
         L.halo_quantize_rows_mx4.argtypes = [c_int, c_longlong, c_int, c_void_p, c_void_p, c_void_p, c_void_p]
@@ -479,7 +497,7 @@ def _marshal():
         if made_for != marshal_made_for():
             raise ImportError(f"_marshal.so was made for {made_for}, this is {marshal_made_for()}: {again}")
         names = ("halo_paged_kv_append", "halo_paged_mha", "halo_norm_glue", "halo_quantize_rows_mx4", "halo_dequantize_rows_mx4",
-                 "halo_product_mx4")
+                 "halo_product_mx4", "halo_paged_norm_append", "halo_paged_kv_read", "halo_paged_mha_f8", "halo_paged_prompt_mha")
         m.bind(*(ctypes.cast(getattr(L, n), c_void_p).value for n in names), PagedShape, NormShape)
         _native = m
     return _native
@@ -511,6 +529,54 @@ def halo_paged_mha(shape: PagedShape, q, K_cache, V_cache, block_table, seq_len,
                                              dev_status, stream)
     if code:
         raise HaloError(code, "halo_paged_mha")
+
+
+def halo_paged_norm_append(shape: PagedShape, q, k, v, w_q, w_k, eps, pos, seq_of_tok, block_table, inv_freq, interleaved,
+                           turn_scale, q_out, K_cache, V_cache, K_scale=None, V_scale=None, dev_status=None, stream=None) -> None:
+    """halo_paged_kv_append with norms of queries and keys per head (w_q, w_k: [head_dim] or None) in front of the rotation.
+    K_scale, V_scale (uint8 [n_pages][n_kv_heads][page_size]): the caches are 8-bit rows, uint8 of the same sizes."""
+    code = (_native or _marshal()).norm_append(shape, q, k, v, w_q, w_k, eps, pos, seq_of_tok, block_table, inv_freq, interleaved,
+                                               turn_scale, q_out, K_cache, V_cache, K_scale, V_scale, dev_status, stream)
+    if code:
+        raise HaloError(code, "halo_paged_norm_append")
+
+
+def halo_paged_kv_read(shape: PagedShape, pos, seq_of_tok, block_table, K_cache, V_cache, k_out, v_out, K_scale=None, V_scale=None,
+                       dev_status=None, stream=None) -> None:
+    """Rows of the cache at pos[t] of sequence seq_of_tok[t] (None: t) to rows t of k_out and v_out, [n_tok][n_kv_heads * head_dim]
+    or [n_tok][n_kv_heads][head_dim], rows may be strided."""
+    code = (_native or _marshal()).kv_read(shape, pos, seq_of_tok, block_table, K_cache, V_cache, k_out, v_out, K_scale, V_scale,
+                                           dev_status, stream)
+    if code:
+        raise HaloError(code, "halo_paged_kv_read")
+
+
+def halo_paged_mha_f8_workspace_bytes(shape: PagedShape, n_seq: int) -> int:
+    return int(lib().halo_paged_mha_f8_workspace_bytes(byref(shape), n_seq))
+
+
+def halo_paged_mha_f8(shape: PagedShape, q, K_cache, V_cache, K_scale, V_scale, block_table, seq_len, scale, out, workspace, keep=None,
+                      lse=None, dev_status=None, stream=None) -> None:
+    """halo_paged_mha over 8-bit rows (uint8 caches and their scale bytes); workspace of halo_paged_mha_f8_workspace_bytes."""
+    code = (_native or _marshal()).paged_mha_f8(shape, q, K_cache, V_cache, K_scale, V_scale, block_table, seq_len, scale, out,
+                                                workspace, keep, lse, dev_status, stream)
+    if code:
+        raise HaloError(code, "halo_paged_mha_f8")
+
+
+def halo_paged_prompt_mha_workspace_bytes(shape: PagedShape, n_tok: int, n_seq: int) -> int:
+    return int(lib().halo_paged_prompt_mha_workspace_bytes(byref(shape), n_tok, n_seq))
+
+
+def halo_paged_prompt_mha(shape: PagedShape, q, q_start, K_cache, V_cache, block_table, seq_len, scale, out, workspace, K_scale=None,
+                          V_scale=None, keep=None, lse=None, dev_status=None, stream=None) -> None:
+    """Causal attention of packed chunks: rows q_start[s] to q_start[s + 1] of q are the newest tokens of sequence s.  q:
+    [n_tok][n_heads * head_dim] or [n_tok][n_heads][head_dim], rows may be strided; workspace: uint8 tensor of
+    halo_paged_prompt_mha_workspace_bytes(shape, n_tok, n_seq).  K_scale, V_scale: the caches are 8-bit rows."""
+    code = (_native or _marshal()).prompt_mha(shape, q, q_start, K_cache, V_cache, block_table, seq_len, scale, out, workspace, K_scale,
+                                              V_scale, keep, lse, dev_status, stream)
+    if code:
+        raise HaloError(code, "halo_paged_prompt_mha")
 
 
 def norm_shape(d_model, eps, ydtype, xdtype) -> NormShape:

@@ -20,6 +20,13 @@
 //     4096 positions 92.7 us with one number, 93.1 with two; 128 of up to 300 positions, 32 / 32 heads, 96 and 99; 16 heads on
 //     one, a sequence of 131071 29.0 and 29.8).
 //   fp32: fused multiply-adds, two lanes per position for the scores, a column per lane for the weighted sums.
+//   8-bit rows (halo_paged_mha_f8): as bf16, through mma.sync on fp16.  A code's bits, shifted by one, are an fp16 number 2^-8
+//     of its value, so three instructions bring two codes to the tensor cores and no product is rounded; which two codes
+//     share a register decides the order of the elements, and the queries' registers follow it.  Queries come as fp16, a row times
+//     the power of two that brings its largest element to 2^14 (their 8 bits fit; elements below 2^-39 of the largest lose
+//     some).  A position's power of two of the keys multiplies its scores; that of the values its weights, relative to
+//     the largest so far.  Weights are rounded to fp16 once, times 2^15 (off by at most 2^-11 of themselves, an
+//     eighth of what the output's own rounding is; those below 2^-29 of the largest lose bits, 2^-40 of it at most).
 //
 // bf16, 32 / 8 heads of 128, both kernels: one sequence of 131071 positions 91 us (537 MB: 5.9 TB/s; HBM, and the join
 // behind it), 64 sequences of up to 4096 positions 93 to 95 us (besides, a piece's start and meeting); one sequence of 700
@@ -29,9 +36,13 @@
 #include <cooperative_groups.h>
 #include <math.h>
 
-#include "common.cuh"
+#include <type_traits>
+
+#include "eight.cuh"
 
 namespace halo {
+halo_status check_eight(const halo_paged_shape& s, const void* K_scale, const void* V_scale);
+
 namespace {
 
 // Query heads per item, at most.  bf16: the rows of an mma.  fp32: more rows per warp would leave few warps per SM that take
@@ -49,6 +60,17 @@ struct __align__(16) Cut {
 };
 static_assert(alignof(Cut) == 16 && sizeof(Cut) == 32, "two 16-byte words, anywhere in a workspace");
 
+// Element types: of queries and outputs, and of the caches' rows.
+struct Eight {};
+template <typename T> struct Kind {
+    using Io = T;
+    using Row = T;
+};
+template <> struct Kind<Eight> {
+    using Io = __nv_bfloat16;
+    using Row = uint8_t;
+};
+
 struct PagedArgs {
     int n_seq, H, Hk, G, qblocks, dh, page_size, page_shift, n_pages, max_pages;   // page_shift: -1 = no power of two
     int slot;    // floats of a workspace slot
@@ -60,6 +82,8 @@ struct PagedArgs {
     const void* q;
     const void* K;
     const void* V;
+    const uint8_t* K_scale;   // 8-bit rows
+    const uint8_t* V_scale;
     const int32_t* table;
     const int32_t* seq_len;
     const uint8_t* keep;
@@ -93,6 +117,21 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], 
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Codes 1 and 3 of a word, and 0 and 2, as fp16 numbers 2^-8 of their values.
+__device__ __forceinline__ uint32_t odd_codes(uint32_t w) { return ((w >> 1) & 0x3f803f80u) | (w & 0x80008000u); }
+__device__ __forceinline__ uint32_t even_codes(uint32_t w) { return odd_codes(w << 8); }
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
+}
+// 2^n for n <= 127, exactly; 0 below 2^-126
+__device__ __forceinline__ float power(int n) { return n < -126 ? 0.0f : eight_power(n); }
 // 2^x, results below 2^-126 as 0
 __device__ __forceinline__ float pow2(float x) {
     float r;
@@ -118,14 +157,15 @@ constexpr int kSlotHead = 32;       // floats in front of a slot's values: maxim
 // Ring bytes are what keeps HBM busy: 6.5 TB/s x ~1 us of latency / 148 SMs = 44 KB have to be in flight; the shapes below hold 100 to 210 KB.
 template <typename T, int DP, int GR>
 struct Cfg {
-    static constexpr bool kF32 = sizeof(T) == 4;
+    static constexpr bool kF32 = std::is_same<T, float>::value, kEight = std::is_same<T, Eight>::value;
     static constexpr int kWarps = kF32 && (DP == 256 || (DP == 128 && GR == 1)) ? 3 : 4;
     // fp32: two stages, so that two thread blocks of four warps fit an SM at head sizes up to 64, or of three at 128 with
     // one query head per K/V head.  64 sequences of up to 2000 positions, 32 / 8 heads of 64: 77 us with three stages and
     // one thread block, 59 so; 5 of up to 900, 8 / 8 heads of 128: 13.1 us with one thread block of four warps, 10.4 so.
-    static constexpr int kStages = kF32 ? 2 : 3;
+    // 8-bit rows: half the bytes a stage, one more of them where that leaves several thread blocks per SM.
+    static constexpr int kStages = kF32 ? 2 : kEight && DP < 256 ? 4 : 3;
     static constexpr int kTile = kWarps * kRun;
-    static constexpr int kRowBytes = kF32 ? (DP + 8) * 4 : DP * 2;   // fp32: rows padded against bank conflicts; bf16: swizzled
+    static constexpr int kRowBytes = kF32 ? (DP + 8) * 4 : kEight ? DP : DP * 2;   // fp32: rows padded against bank conflicts; else swizzled
     static constexpr int kHalf = kRun * kRowBytes;                   // keys (or values) of one stage
     static constexpr int kStage = 2 * kHalf;
     static constexpr int kRing = kStages * kStage;
@@ -213,7 +253,8 @@ __device__ __forceinline__ bool head_kept(const PagedArgs& a, int h) { return !a
 
 template <typename T>
 __device__ __forceinline__ void write_head(const PagedArgs& a, int s, int h, int j, float v) {
-    static_cast<T*>(a.out)[(static_cast<long long>(s) * a.H + h) * a.dh + j] = from_float<T>(v);
+    using Io = typename Kind<T>::Io;
+    static_cast<Io*>(a.out)[(static_cast<long long>(s) * a.H + h) * a.dh + j] = from_float<Io>(v);
 }
 
 // The way along a range: piece after piece.
@@ -257,14 +298,22 @@ struct Walk {
     }
 };
 
+// Where 16-byte chunk c of row r of 8-bit rows lies in it: eight rows' same chunks fall on all banks, also where a row is 64 bytes.
+template <int DP>
+__device__ __forceinline__ uint32_t eight_chunk(int r, int c) {
+    return (DP == 64 ? c ^ ((r >> 1) & 3) : (c & ~7) | ((c ^ r) & 7)) * 16;
+}
+
 template <typename T, int DP, int GR>
 __global__ void __launch_bounds__(Cfg<T, DP, GR>::kWarps * 32, Cfg<T, DP, GR>::kBlocksPerSm)
 paged_mha_kernel(const __grid_constant__ PagedArgs a) {
     using C_ = Cfg<T, DP, GR>;
-    constexpr bool kF32 = C_::kF32;
+    using Io = typename Kind<T>::Io;
+    using Row = typename Kind<T>::Row;
+    constexpr bool kF32 = C_::kF32, kEight = C_::kEight;
     constexpr int S = C_::kStages;
     constexpr int kThreads = C_::kWarps * 32;
-    constexpr int kE = kF32 ? 4 : 8;              // elements per 16 bytes
+    constexpr int kE = 16 / static_cast<int>(sizeof(Row));   // elements per 16 bytes
     constexpr int kCpr = DP / kE;                 // 16-byte chunks per padded row
     constexpr int kLanesPerRow = kCpr < 32 ? kCpr : 32;
     constexpr int kRowsPer = 32 / kLanesPerRow;   // rows a warp copies per instruction
@@ -324,14 +373,17 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
     // Pages of whole runs: a run's positions are neighbours in memory and share a page.
     const bool neighbours = a.page_size % kRun == 0;
     const int lr = lane / kLanesPerRow, lc = lane % kLanesPerRow;
-    const auto put_row = [&](uint32_t st, int i, int ci, const T* k, const T* v, bool have) {
+    const auto put_row = [&](uint32_t st, int i, int ci, const Row* k, const Row* v, bool have) {
         const int r = i * kRowsPer + lr, c = lc + ci * 32;   // the swizzle: c ^ r, as i * kRowsPer and lr have no bit in common
-        const uint32_t d = st + r * C_::kRowBytes + (kF32 ? c * 16 : ((c & ~7) | (((c ^ lr) ^ (i * kRowsPer)) & 7)) * 16);
+        const uint32_t d = st + r * C_::kRowBytes +
+                           (kF32 ? c * 16 : kEight ? eight_chunk<DP>(r, c) : ((c & ~7) | (((c ^ lr) ^ (i * kRowsPer)) & 7)) * 16);
         cp_async16(d, k, have);
         cp_async16(d + C_::kHalf, v, have);
     };
+    [[maybe_unused]] uint32_t bytes[S];   // 8-bit rows: scale byte of a run's position, of its key in lanes 0 to 15, of its value behind
     const auto issue = [&]() -> uint32_t {   // starts the copies of the next run; returns its mask of present positions
         uint32_t mask = 0;
+        if constexpr (kEight) bytes[S - 1] = 0;
         if (iss.left > 0) {
             const int p0 = it * C_::kTile + warp * kRun, p = p0 + (lane & 15);
             const bool in = p < iss.reach, ok = in && page_next >= 0 && page_next < a.n_pages;
@@ -340,13 +392,17 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
             if (mask) {
                 const int kvh = a.qblocks == 1 ? iss.hi : iss.hi / a.qblocks;
                 const uint32_t st = ring_a + slot_in * C_::kStage;
+                if constexpr (kEight) {
+                    const int in_page = a.page_shift >= 0 ? p & (a.page_size - 1) : p % a.page_size;
+                    if (ok) bytes[S - 1] = ldg_waited((lane < 16 ? a.K_scale : a.V_scale) + (static_cast<long long>(page_next) * a.Hk + kvh) * a.page_size + in_page);
+                }
                 if (neighbours) {
                     const int page = __shfl_sync(0xffffffffu, page_next, 0);   // mask: position 0 is there
                     const int in_page = a.page_shift >= 0 ? p0 & (a.page_size - 1) : p0 % a.page_size;
                     const long long off = static_cast<long long>(page) * a.page_stride +
                                           (static_cast<long long>(kvh) * a.page_size + in_page + lr) * a.dh + lc * kE;
-                    const T* k = static_cast<const T*>(a.K) + off;
-                    const T* v = static_cast<const T*>(a.V) + off;
+                    const Row* k = static_cast<const Row*>(a.K) + off;
+                    const Row* v = static_cast<const Row*>(a.V) + off;
                     const int step = kRowsPer * a.dh;
 #pragma unroll
                     for (int i = 0; i < kRun / kRowsPer; ++i) {
@@ -368,8 +424,8 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
 #pragma unroll
                         for (int ci = 0; ci < kChunkIters; ++ci)
                             if ((lc + ci * 32) * kE < a.dh)
-                                put_row(st, i, ci, static_cast<const T*>(a.K) + ro + ci * 32 * kE,
-                                        static_cast<const T*>(a.V) + ro + ci * 32 * kE, (mask >> (i * kRowsPer + lr)) & 1u);
+                                put_row(st, i, ci, static_cast<const Row*>(a.K) + ro + ci * 32 * kE,
+                                        static_cast<const Row*>(a.V) + ro + ci * 32 * kE, (mask >> (i * kRowsPer + lr)) & 1u);
                     }
                 }
             }
@@ -385,7 +441,10 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
     };
     uint32_t masks[S];
 #pragma unroll
-    for (int i = 0; i < S - 1; ++i) masks[i] = issue();
+    for (int i = 0; i < S - 1; ++i) {
+        masks[i] = issue();
+        if constexpr (kEight) bytes[i] = bytes[S - 1];
+    }
 
     // ---- summing ----------------------------------------------------------------------------------------------------
     const int g = lane >> 2, t4 = lane & 3;
@@ -395,22 +454,54 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
         first = false;
         const int kvh = con.hi / a.qblocks, r0 = (con.hi % a.qblocks) * a.block;
         const int rows = min(a.block, a.G - r0), h0 = kvh * a.G + r0;
-        const T* qrow = static_cast<const T*>(a.q) + static_cast<long long>(con.s) * a.q_stride + static_cast<long long>(h0) * a.dh;
+        const Io* qrow = static_cast<const Io*>(a.q) + static_cast<long long>(con.s) * a.q_stride + static_cast<long long>(h0) * a.dh;
         const bool complete = con.t0 == 0 && con.t1 == con.nt;
         float* slot = a.ws + (static_cast<long long>(blockIdx.x) * 2 + (con.left == range ? 0 : 1)) * a.slot;
 
         if constexpr (!kF32) {
             constexpr int kK = GR > 8 ? 2 : 1;    // rows of a lane: g, and g + 8 where an item has more than 8 heads
             uint32_t qf[DP / 16][4];
+            [[maybe_unused]] float unit[kK];   // 8-bit rows: what a row's products are multiplied with
+            if constexpr (kEight) {
+                // elements 4 t4 to 4 t4 + 3 of every 16, in the order of the codes' registers
+#pragma unroll
+                for (int j = 0; j < kK; ++j) {
+                    const int r = g + j * 8;
+                    uint2 w[DP / 16];
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int k = 0; k < DP / 16; ++k) {
+                        const unsigned long long v = r < rows && k * 16 < a.dh   // dh % 16 == 0
+                            ? ldg_waited(reinterpret_cast<const unsigned long long*>(qrow + static_cast<long long>(r) * a.dh + k * 16 + t4 * 4)) : 0ull;
+                        w[k] = make_uint2(static_cast<uint32_t>(v), static_cast<uint32_t>(v >> 32));
+                        top = max(max(top, w[k].x & 0x7fffu), (w[k].x >> 16) & 0x7fffu);
+                        top = max(max(top, w[k].y & 0x7fffu), (w[k].y >> 16) & 0x7fffu);
+                    }
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                    // 2^up brings the largest element below 2^15; at least 2^-113, at most 2^120 (tiny rows stay smaller)
+                    const int up = min(14 + 127 - static_cast<int>(top >> 7), 120);
+                    const float n = eight_power(up);
+                    unit[j] = a.scale_log2 * eight_power(8 - up);
+#pragma unroll
+                    for (int k = 0; k < DP / 16; ++k) {
+                        qf[k][j] = pack_f16(bf16_lo(w[k].x) * n, bf16_lo(w[k].y) * n);
+                        qf[k][2 + j] = pack_f16(bf16_hi(w[k].x) * n, bf16_hi(w[k].y) * n);
+                        if (kK == 1) qf[k][1] = qf[k][3] = 0u;
+                    }
+                }
+            } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int r = g + (j & 1) * 8;
                 const bool there = (kK == 2 || !(j & 1)) && r < rows;
-                const T* q = qrow + static_cast<long long>(r) * a.dh + (j >> 1) * 8 + t4 * 2;
+                const Io* q = qrow + static_cast<long long>(r) * a.dh + (j >> 1) * 8 + t4 * 2;
 #pragma unroll
                 for (int k = 0; k < DP / 16; ++k)
                     qf[k][j] = there && k * 16 < a.dh ? ldg_waited(reinterpret_cast<const uint32_t*>(q + k * 16)) : 0u;   // dh % 16 == 0
             }
+            }
+            [[maybe_unused]] int top_byte = 0;   // 8-bit rows: the largest scale byte of the values so far; o is relative to it
             float o[NT][4];
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -428,14 +519,50 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                 cp_wait<S - 1>();
                 __syncwarp();
                 const uint32_t mask = masks[0];
+                [[maybe_unused]] uint32_t byte = 0;
+                if constexpr (kEight) byte = bytes[0];
 #pragma unroll
-                for (int i = 0; i + 1 < S; ++i) masks[i] = masks[i + 1];
+                for (int i = 0; i + 1 < S; ++i) {
+                    masks[i] = masks[i + 1];
+                    if constexpr (kEight) bytes[i] = bytes[i + 1];
+                }
                 const uint32_t st = ring_a + slot_out * C_::kStage;
                 if (++slot_out == S) slot_out = 0;
                 if (mask == 0) continue;
                 // scores of 16 heads x 16 positions, even and odd steps in two chains
                 float sc[2][4] = {}, sc2[2][4] = {};
-                {
+                [[maybe_unused]] float vf[2][2];   // 8-bit rows: what the weights of this lane's positions are multiplied with
+                [[maybe_unused]] float down = 1.0f;
+                if constexpr (kEight) {
+                    const int key = ((lane >> 3) & 1) * 8 + (lane & 7), second = lane >> 4;
+#pragma unroll
+                    for (int k = 0; k < DP / 16; k += 2) {
+                        uint32_t b[4];
+                        ldsm4(b, st + key * C_::kRowBytes + eight_chunk<DP>(key, k + second));
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            mma_f16(e ? sc2[0] : sc[0], qf[k + e], even_codes(b[2 * e]), odd_codes(b[2 * e]));
+                            mma_f16(e ? sc2[1] : sc[1], qf[k + e], even_codes(b[2 * e + 1]), odd_codes(b[2 * e + 1]));
+                        }
+                    }
+                    // lanes 0 to 15: the keys' powers of two; 16 to 31: the values', relative to the largest
+                    const int most = __reduce_max_sync(0xffffffffu, lane < 16 || byte == kEightNan ? 0 : static_cast<int>(byte));
+                    float own = eight_unit(byte);
+                    if (most > top_byte) {
+                        down = power(top_byte - most);
+                        top_byte = most;
+                    }
+                    if (lane >= 16 && byte != kEightNan) own = power(static_cast<int>(byte) - top_byte + 15);
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float kf = __shfl_sync(0xffffffffu, own, n * 8 + t4 * 2 + e);
+                            vf[n][e] = __shfl_sync(0xffffffffu, own, 16 + n * 8 + t4 * 2 + e);
+#pragma unroll
+                            for (int j = 0; j < kK; ++j) sc[n][2 * j + e] = (sc[n][2 * j + e] + sc2[n][2 * j + e]) * unit[j] * kf;
+                        }
+                } else {
                     const int key = (lane >> 4) * 8 + (lane & 7), half = (lane >> 3) & 1;
 #pragma unroll
                     for (int k = 0; k < DP / 16; ++k) {
@@ -447,10 +574,12 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                     }
                 }
                 // running softmax; a lane holds rows g (and g + 8), positions 2 * t4 + {0, 1} and 8 more
+                if constexpr (!kEight) {
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                    for (int n = 0; n < 2; ++n)
 #pragma unroll
-                    for (int j = 0; j < 2 * kK; ++j) sc[n][j] = (sc[n][j] + sc2[n][j]) * a.scale_log2;
+                        for (int j = 0; j < 2 * kK; ++j) sc[n][j] = (sc[n][j] + sc2[n][j]) * a.scale_log2;
+                }
                 if (mask != 0xffffu) {
 #pragma unroll
                     for (int n = 0; n < 2; ++n)
@@ -475,7 +604,9 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
 #pragma unroll
                         for (int j = 2 * k; j < 2 * k + 2; ++j) sc[n][j] = pow2(sc[n][j] - base);
                     l[k] = fmaf(l[k], f[k], (sc[0][2 * k] + sc[0][2 * k + 1]) + (sc[1][2 * k] + sc[1][2 * k + 1]));
+                    if constexpr (kEight) f[k] *= down;
                 }
+                if constexpr (kEight) moved |= down != 1.0f;
                 if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
@@ -485,6 +616,22 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                 // weighted sum of the values: the weights' upper bits and their rests, these in the rows 8 to 15 of the
                 // same product (up to 8 heads; o[n][2], o[n][3] are their sums) or in one of their own
                 uint32_t pa[4], pr[4];
+                if constexpr (kEight) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        pa[j] = kK == 2 || !(j & 1) ? pack_f16(sc[j >> 1][(j & 1) * 2] * vf[j >> 1][0], sc[j >> 1][(j & 1) * 2 + 1] * vf[j >> 1][1]) : 0u;
+                    const int key = ((lane >> 3) & 1) * 8 + (lane & 7), second = lane >> 4;
+#pragma unroll
+                    for (int n = 0; n < NT; n += 4) {   // 32 columns; o[n], o[n + 1]: the even and the odd ones of 16
+                        uint32_t b[4];
+                        ldsm4t(b, st + C_::kHalf + key * C_::kRowBytes + eight_chunk<DP>(key, n / 2 + second));
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            mma_f16(o[n + 2 * e], pa, even_codes(b[2 * e]), even_codes(b[2 * e + 1]));
+                            mma_f16(o[n + 2 * e + 1], pa, odd_codes(b[2 * e]), odd_codes(b[2 * e + 1]));
+                        }
+                    }
+                } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float* w = &sc[j >> 1][kK == 2 ? (j & 1) * 2 : 0];
@@ -504,9 +651,23 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                         mma_bf16(o[n + 1], pr, b[2], b[3]);
                     }
                 }
+                }
                 __syncwarp();   // the stage is free for the copies that the next round starts
             }
-            if constexpr (kK == 1) {
+            // columns of o[n][0], o[n][1] (and 2, 3)
+            const auto col = [&](int n) { return kEight ? (n >> 1) * 16 + t4 * 4 + (n & 1) * 2 : n * 8 + t4 * 2; };
+            if constexpr (kEight) {   // neighbours side by side, and the values' own size: codes are 2^-8 of it, weights 2^15
+                const float size = eight_unit(static_cast<uint32_t>(top_byte));
+#pragma unroll
+                for (int n = 0; n < NT; n += 2)
+#pragma unroll
+                    for (int k = 0; k < kK; ++k) {
+                        const float x[4] = {o[n][2 * k], o[n + 1][2 * k], o[n][2 * k + 1], o[n + 1][2 * k + 1]};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[n + (e >> 1)][2 * k + (e & 1)] = x[e] * 0x1p-7f * size;
+                    }
+            }
+            if constexpr (kK == 1 && !kEight) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n) { o[n][0] += o[n][2]; o[n][1] += o[n][3]; }
             }
@@ -539,7 +700,7 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                     if (g + k * 8 < rows) {
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
-                            *reinterpret_cast<float2*>(mg + (b * rows + g + k * 8) * C_::kMergeRow + n * 8 + t4 * 2) =
+                            *reinterpret_cast<float2*>(mg + (b * rows + g + k * 8) * C_::kMergeRow + col(n)) =
                                 make_float2(o[n][2 * k], o[n][2 * k + 1]);
                     }
             };
@@ -549,7 +710,7 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                     if (g + k * 8 < rows) {
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            const float2 v = *reinterpret_cast<const float2*>(mg + (b * rows + g + k * 8) * C_::kMergeRow + n * 8 + t4 * 2);
+                            const float2 v = *reinterpret_cast<const float2*>(mg + (b * rows + g + k * 8) * C_::kMergeRow + col(n));
                             o[n][2 * k] += v.x;
                             o[n][2 * k + 1] += v.y;
                         }
@@ -576,16 +737,16 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                         const bool some = L[k] != 0.0f && head_kept(a, h0 + r);
                         const long long row = static_cast<long long>(con.s) * a.H + h0 + r;
                         const float f = some ? 1.0f / L[k] : 0.0f;
-                        uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + row * a.dh);
+                        uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<Io*>(a.out) + row * a.dh);
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
-                            if (n * 8 + t4 * 2 < a.dh) out[n * 4 + t4] = some ? pack_bf16(o[n][2 * k] * f, o[n][2 * k + 1] * f) : 0u;
+                            if (col(n) < a.dh) out[col(n) / 2] = some ? pack_bf16(o[n][2 * k] * f, o[n][2 * k + 1] * f) : 0u;
                         if (t4 == 0 && a.lse) a.lse[row] = some ? (M[k] + log2f(L[k])) * kLn2 : -INFINITY;
                     } else {
                         if (t4 == 0) { slot[r] = M[k]; slot[16 + r] = L[k]; }
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
-                            *reinterpret_cast<float2*>(slot + kSlotHead + r * DP + n * 8 + t4 * 2) = make_float2(o[n][2 * k], o[n][2 * k + 1]);
+                            *reinterpret_cast<float2*>(slot + kSlotHead + r * DP + col(n)) = make_float2(o[n][2 * k], o[n][2 * k + 1]);
                     }
                 }
             }
@@ -1008,10 +1169,10 @@ halo_status launch(const PagedArgs& args, const LaunchPlan& p, cudaStream_t st) 
     const halo_status rc = cuda_status(cudaLaunchKernelEx(&cfg, paged_mha_kernel<T, DP, GR>, a));
     if (rc != HALO_OK || p.split || p.blocks < 2) return rc;
     if (p.blocks >= 8 * p.items)
-        return launch_chained(paged_mha_join_item_kernel<T, DP>, dim3(static_cast<unsigned>(p.items), p.rows), kItemJoin,
+        return launch_chained(paged_mha_join_item_kernel<typename Kind<T>::Io, DP>, dim3(static_cast<unsigned>(p.items), p.rows), kItemJoin,
                               sizeof(float) * p.blocks, st, a, p.blocks);
     constexpr int kHeads = kRangeJoin / DP;
-    return launch_chained(paged_mha_join_range_kernel<T, DP>, dim3(p.blocks - 1, (p.rows + kHeads - 1) / kHeads), kRangeJoin, 0, st, a,
+    return launch_chained(paged_mha_join_range_kernel<typename Kind<T>::Io, DP>, dim3(p.blocks - 1, (p.rows + kHeads - 1) / kHeads), kRangeJoin, 0, st, a,
                           p.blocks);
 }
 
@@ -1019,23 +1180,25 @@ template <typename T, int DP, typename F>
 auto by_rows(const halo_paged_shape& sh, F f) {
     using D = std::integral_constant<int, DP>;
     const int G = sh.n_heads / sh.n_kv_heads;
-    if constexpr (sizeof(T) == 2) {
+    if constexpr (!std::is_same<T, float>::value) {
         return G <= 8 ? f(T(), D(), std::integral_constant<int, 8>()) : f(T(), D(), std::integral_constant<int, 16>());
     } else {
         if (G == 1) return f(T(), D(), std::integral_constant<int, 1>());
         return f(T(), D(), std::integral_constant<int, 4>());
     }
 }
+template <typename T, typename F>
+auto by_width(const halo_paged_shape& sh, F f) {
+    return sh.head_dim <= 64 ? by_rows<T, 64>(sh, f) : sh.head_dim <= 128 ? by_rows<T, 128>(sh, f) : by_rows<T, 256>(sh, f);
+}
 template <typename F>
-auto by_type(const halo_paged_shape& sh, F f) {
-    using H = __nv_bfloat16;
-    if (sh.dtype == HALO_BF16)
-        return sh.head_dim <= 64 ? by_rows<H, 64>(sh, f) : sh.head_dim <= 128 ? by_rows<H, 128>(sh, f) : by_rows<H, 256>(sh, f);
-    return sh.head_dim <= 64 ? by_rows<float, 64>(sh, f) : sh.head_dim <= 128 ? by_rows<float, 128>(sh, f) : by_rows<float, 256>(sh, f);
+auto by_type(const halo_paged_shape& sh, bool eight, F f) {
+    if (eight) return by_width<Eight>(sh, f);
+    return sh.dtype == HALO_BF16 ? by_width<__nv_bfloat16>(sh, f) : by_width<float>(sh, f);
 }
 
-LaunchPlan plan_for(const halo_paged_shape& sh, int n_seq) {
-    return by_type(sh, [&](auto t, auto dp, auto gr) { return plan_of<decltype(t), decltype(dp)::value, decltype(gr)::value>(sh, n_seq); });
+LaunchPlan plan_for(const halo_paged_shape& sh, int n_seq, bool eight) {
+    return by_type(sh, eight, [&](auto t, auto dp, auto gr) { return plan_of<decltype(t), decltype(dp)::value, decltype(gr)::value>(sh, n_seq); });
 }
 
 }  // namespace
@@ -1056,22 +1219,15 @@ long long paged_stride(const halo_paged_shape& s) {
     return s.page_stride ? s.page_stride : static_cast<long long>(s.n_kv_heads) * s.page_size * s.head_dim;
 }
 
-}  // namespace halo
-
-using namespace halo;
-
-extern "C" size_t halo_paged_mha_workspace_bytes(const halo_paged_shape* shape, int n_seq) {
-    if (check_paged_shape(shape) != HALO_OK || n_seq <= 0 || n_seq > HALO_MAX_SEQUENCES) return 0;
-    return workspace_of(plan_for(*shape, n_seq));
-}
-
-extern "C" halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, const void* q, long long q_stride,
-                                      const void* K_cache, const void* V_cache, const int32_t* block_table,
-                                      const int32_t* seq_len, const uint8_t* keep, float scale, void* out, float* lse,
-                                      void* workspace, size_t workspace_bytes, uint32_t* dev_status, void* stream) {
-    const halo_status rc = check_paged_shape(shape);
+namespace {
+// halo_paged_mha and halo_paged_mha_f8 (scales: the latter)
+halo_status attend(const halo_paged_shape* shape, int n_seq, const void* q, long long q_stride, const void* K_cache,
+                   const void* V_cache, bool eight, const uint8_t* K_scale, const uint8_t* V_scale, const int32_t* block_table,
+                   const int32_t* seq_len, const uint8_t* keep, float scale, void* out, float* lse, void* workspace,
+                   size_t workspace_bytes, uint32_t* dev_status, void* stream) {
+    halo_status rc = check_paged_shape(shape);
     if (rc != HALO_OK) return rc;
-    if (!q || !K_cache || !V_cache || !block_table || !seq_len || !out) return HALO_ERR_ARG;
+    if (!q || !K_cache || !V_cache || !block_table || !seq_len || !out || (eight && (!K_scale || !V_scale))) return HALO_ERR_ARG;
     if (!isfinite(scale)) return HALO_ERR_ARG;
     if (n_seq <= 0 || n_seq > HALO_MAX_SEQUENCES) return HALO_ERR_SHAPE;
     const int elem = shape->dtype == HALO_F32 ? 4 : 2;
@@ -1079,7 +1235,10 @@ extern "C" halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, 
     if (q_stride < row) return HALO_ERR_SHAPE;
     if (!aligned16(q) || !aligned16(K_cache) || !aligned16(V_cache) || !aligned16(out) || q_stride * elem % 16 != 0)
         return HALO_ERR_ALIGN;
-    const size_t need = halo_paged_mha_workspace_bytes(shape, n_seq);
+    rc = check_eight(*shape, K_scale, V_scale);
+    if (rc != HALO_OK) return rc;
+    const LaunchPlan p = plan_for(*shape, n_seq, eight);
+    const size_t need = workspace_of(p);
     if (need > 0 && (!workspace || workspace_bytes < need)) return HALO_ERR_WORKSPACE;
     if (need > 0 && !aligned16(workspace)) return HALO_ERR_ALIGN;
     PagedArgs a = {};
@@ -1102,16 +1261,51 @@ extern "C" halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, 
     a.q = q;
     a.K = K_cache;
     a.V = V_cache;
+    a.K_scale = K_scale;
+    a.V_scale = V_scale;
     a.table = block_table;
     a.seq_len = seq_len;
     a.keep = keep;
     a.out = out;
     a.lse = lse;
     a.status = dev_status;
-    const LaunchPlan p = plan_for(*shape, n_seq);
     a.cuts = static_cast<Cut*>(workspace);
     a.ws = reinterpret_cast<float*>(a.cuts + p.blocks);
-    return by_type(*shape, [&](auto t, auto dp, auto gr) {
+    return by_type(*shape, eight, [&](auto t, auto dp, auto gr) {
         return launch<decltype(t), decltype(dp)::value, decltype(gr)::value>(a, p, static_cast<cudaStream_t>(stream));
     });
+}
+
+size_t workspace_bytes_of(const halo_paged_shape* shape, int n_seq, bool eight) {
+    if (check_paged_shape(shape) != HALO_OK || n_seq <= 0 || n_seq > HALO_MAX_SEQUENCES) return 0;
+    return workspace_of(plan_for(*shape, n_seq, eight));
+}
+}  // namespace
+}  // namespace halo
+
+using namespace halo;
+
+extern "C" size_t halo_paged_mha_workspace_bytes(const halo_paged_shape* shape, int n_seq) {
+    return workspace_bytes_of(shape, n_seq, false);
+}
+
+extern "C" halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, const void* q, long long q_stride,
+                                      const void* K_cache, const void* V_cache, const int32_t* block_table,
+                                      const int32_t* seq_len, const uint8_t* keep, float scale, void* out, float* lse,
+                                      void* workspace, size_t workspace_bytes, uint32_t* dev_status, void* stream) {
+    return attend(shape, n_seq, q, q_stride, K_cache, V_cache, false, nullptr, nullptr, block_table, seq_len, keep, scale, out, lse,
+                  workspace, workspace_bytes, dev_status, stream);
+}
+
+extern "C" size_t halo_paged_mha_f8_workspace_bytes(const halo_paged_shape* shape, int n_seq) {
+    return shape && shape->dtype == HALO_BF16 ? workspace_bytes_of(shape, n_seq, true) : 0;
+}
+
+extern "C" halo_status halo_paged_mha_f8(const halo_paged_shape* shape, int n_seq, const void* q, long long q_stride,
+                                         const void* K_cache, const void* V_cache, const uint8_t* K_scale, const uint8_t* V_scale,
+                                         const int32_t* block_table, const int32_t* seq_len, const uint8_t* keep, float scale,
+                                         void* out, float* lse, void* workspace, size_t workspace_bytes, uint32_t* dev_status,
+                                         void* stream) {
+    return attend(shape, n_seq, q, q_stride, K_cache, V_cache, true, K_scale, V_scale, block_table, seq_len, keep, scale, out, lse,
+                  workspace, workspace_bytes, dev_status, stream);
 }

@@ -1,0 +1,316 @@
+// halo_paged_prompt_mha by fused multiply-adds: 64 rows against tiles of 64 keys.  Bound by them: 4 flops per key, row and
+// column of the head at 2 * 128 a clock and SM.
+//
+// 128 threads; a thread has 8 rows x 4 keys of the scores and 8 rows x DP / 16 columns of the weighted sums, so that twelve 16-byte
+// words from shared memory feed 128 multiply-adds.  Rows in shared memory are padded by four floats, which spreads the
+// eight rows of a phase over all banks.  The sixteen lanes of a row keep its maximum and sum by shuffles; weights go through
+// shared memory that only their own half warp reads.  Copies of the next keys run under the softmax and the weighted sums, of
+// the next values under the scores.
+#include "prompt_line.cuh"
+
+#include <type_traits>
+
+namespace halo {
+namespace prompt {
+namespace {
+
+constexpr int kRows = 64, kTile = 64, kThreads = 128;
+
+struct Eight {};
+template <typename T> struct Kind {
+    using Io = T;
+    using Row = T;
+};
+template <> struct Kind<Eight> {
+    using Io = __nv_bfloat16;
+    using Row = uint8_t;
+};
+
+template <int DP>
+struct Smem {
+    static constexpr int kStride = DP + 4, kWeights = kTile + 4;
+    float q[kRows * kStride], k[kTile * kStride], v[kTile * kStride], w[kRows * kWeights];
+    long long row[2][kTile];     // of the caches' rows: page * page_stride + ..., -1: no such position
+    long long scale[2][kTile];   // 8-bit rows: where their bytes are
+    long long sh[kThreads / 32 + 3];
+};
+
+__device__ __forceinline__ void cp_async16(float* dst, const void* src, bool valid) {
+    const int n = valid ? 16 : 0;   // 0: the 16 bytes are filled with zeros and src is not read
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(dst))), "l"(src), "r"(n)
+                 : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads) paged_prompt_rows_kernel(const __grid_constant__ Args a) {
+    using Io = typename Kind<T>::Io;
+    using S_ = Smem<DP>;
+    constexpr int kStride = S_::kStride, kWeights = S_::kWeights, kCpr = DP / 4, V = DP / 64;
+    extern __shared__ __align__(16) unsigned char raw[];
+    S_& sm = *reinterpret_cast<S_*>(raw);
+    const int tid = threadIdx.x, lane = tid & 31, tx = tid & 15, ty = tid >> 4;
+    chain_wait();
+    Found<kRows, kTile> f = locate<kRows, kTile, kThreads>(a, sm.sh);
+    Walk<kRows, kTile>& w = f.walk;
+    const long long range = w.left;
+    bool bad = false;
+
+    while (w.left > 0) {
+        const int kvh = w.kvh, nt = w.reach > 0 ? w.t1 - w.t0 : 0;
+        // where the tile's rows are
+        const auto places = [&](int t) {
+            if (tid >= kTile) return;
+            const int p = (w.t0 + t) * kTile + tid;
+            long long at = -1;
+            if (p < w.reach) {
+                const int pi = a.page_shift >= 0 ? p >> a.page_shift : p / a.page_size, in = p - pi * a.page_size;
+                const int page = ldg_waited(a.table + static_cast<long long>(w.s) * a.max_pages + pi);
+                if (page >= 0 && page < a.n_pages) {
+                    at = static_cast<long long>(page) * a.page_stride + (static_cast<long long>(kvh) * a.page_size + in) * a.dh;
+                    sm.scale[t & 1][tid] = (static_cast<long long>(page) * a.Hk + kvh) * a.page_size + in;
+                } else {
+                    bad = true;
+                }
+            }
+            sm.row[t & 1][tid] = at;
+        };
+        const auto fetch = [&](float* dst, const void* cache, const uint8_t* scale, int t) {
+#pragma unroll 4
+            for (int i = tid; i < kTile * kCpr; i += kThreads) {
+                const int r = i / kCpr, c = i % kCpr;
+                const long long at = sm.row[t & 1][r];
+                const bool there = at >= 0 && c * 4 < a.dh;
+                float* to = dst + r * kStride + c * 4;
+                if constexpr (std::is_same<T, float>::value) {
+                    cp_async16(to, static_cast<const float*>(cache) + (there ? at + c * 4 : 0), there);
+                } else if constexpr (std::is_same<T, Eight>::value) {
+                    float x[4] = {};
+                    if (there) {
+                        eight_widen(*reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(cache) + at + c * 4), x);
+                        const float unit = eight_unit(scale[sm.scale[t & 1][r]]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] *= unit;
+                    }
+                    *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
+                } else {
+                    uint2 x = make_uint2(0, 0);
+                    if (there) x = *reinterpret_cast<const uint2*>(static_cast<const T*>(cache) + at + c * 4);
+                    *reinterpret_cast<float4*>(to) = make_float4(bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y));
+                }
+            }
+            cp_commit();
+        };
+
+        // the rows
+        {
+            const int i = tid & (kRows - 1);
+            const Row row = row_at<kRows>(a, w.r, kvh, w.rb, i);
+            const Io* q = static_cast<const Io*>(a.q) + static_cast<long long>(row.token) * a.q_stride + static_cast<long long>(row.head) * a.dh;
+#pragma unroll 4
+            for (int c = tid / kRows; c < kCpr; c += kThreads / kRows) {
+                float x[4] = {};
+                if (row.there && c * 4 < a.dh) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = to_float(q[c * 4 + e]);
+                }
+                *reinterpret_cast<float4*>(sm.q + i * kStride + c * 4) = make_float4(x[0], x[1], x[2], x[3]);
+            }
+        }
+        int sees[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) sees[r] = row_at<kRows>(a, w.r, kvh, w.rb, ty * 8 + r).sees;
+        // every row sees what the item's first token sees
+        const int all_see = w.r.len - w.r.n + static_cast<int>(static_cast<long long>(w.rb) * kRows / a.G) + 1;
+        if (nt > 0) {
+            places(0);
+            places(1);
+            __syncthreads();
+            fetch(sm.k, a.K, a.K_scale, 0);
+            fetch(sm.v, a.V, a.V_scale, 0);
+        } else {
+            __syncthreads();
+        }
+
+        float o[8][V * 4], m[8], l[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            m[r] = -INFINITY;
+            l[r] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < V * 4; ++j) o[r][j] = 0.0f;
+        }
+        for (int t = 0; t < nt; ++t) {
+            cp_wait<1>();
+            __syncthreads();
+            float sc[8][4] = {};
+#pragma unroll 2
+            for (int d = 0; d < DP; d += 4) {
+                float4 k[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const float4*>(sm.k + (tx + 16 * j) * kStride + d);
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const float4 q = *reinterpret_cast<const float4*>(sm.q + (ty * 8 + r) * kStride + d);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sc[r][j] = fmaf(q.x, k[j].x, fmaf(q.y, k[j].y, fmaf(q.z, k[j].z, fmaf(q.w, k[j].w, sc[r][j]))));
+                }
+            }
+            const int p0 = (w.t0 + t) * kTile;
+            bool there[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) there[j] = sm.row[t & 1][tx + 16 * j] >= 0;
+            __syncthreads();
+            if (t + 1 < nt) fetch(sm.k, a.K, a.K_scale, t + 1);
+            else cp_commit();
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                float mx = m[r];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    sc[r][j] = there[j] && p0 + tx + 16 * j < sees[r] ? sc[r][j] * a.scale_log2 : -INFINITY;
+                    mx = fmaxf(mx, sc[r][j]);
+                }
+#pragma unroll
+                for (int d = 1; d < 16; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+                const float base = mx == -INFINITY ? 0.0f : mx, g = pow2(m[r] - base);
+                m[r] = mx;
+                float sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float e = pow2(sc[r][j] - base);
+                    sum += e;
+                    sm.w[(ty * 8 + r) * kWeights + tx + 16 * j] = e;
+                }
+                l[r] = fmaf(l[r], g, sum);       // of this lane's keys; the lanes meet at the end
+#pragma unroll
+                for (int j = 0; j < V * 4; ++j) o[r][j] *= g;
+            }
+            cp_wait<1>();
+            __syncthreads();
+            const bool whole = p0 + kTile <= all_see;   // else: a weight of zero meets nothing, so that a value behind a row's last cannot reach it
+#pragma unroll 1
+            for (int k0 = 0; k0 < kTile; k0 += 4) {
+                float4 v[4][V];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int g = 0; g < V; ++g) v[e][g] = *reinterpret_cast<const float4*>(sm.v + (k0 + e) * kStride + tx * 4 + 64 * g);
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const float4 e4 = *reinterpret_cast<const float4*>(sm.w + (ty * 8 + r) * kWeights + k0);
+                    const float e[4] = {e4.x, e4.y, e4.z, e4.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (!whole && e[i] == 0.0f) continue;
+#pragma unroll
+                        for (int g = 0; g < V; ++g) {
+                            o[r][4 * g] = fmaf(e[i], v[i][g].x, o[r][4 * g]);
+                            o[r][4 * g + 1] = fmaf(e[i], v[i][g].y, o[r][4 * g + 1]);
+                            o[r][4 * g + 2] = fmaf(e[i], v[i][g].z, o[r][4 * g + 2]);
+                            o[r][4 * g + 3] = fmaf(e[i], v[i][g].w, o[r][4 * g + 3]);
+                        }
+                    }
+                }
+            }
+            __syncthreads();
+            if (t + 1 < nt) fetch(sm.v, a.V, a.V_scale, t + 1);
+            else cp_commit();
+            if (t + 2 < nt) places(t + 2);
+        }
+        cp_wait<0>();
+
+        const bool complete = w.complete();
+        float* slot = a.ws + (static_cast<long long>(blockIdx.x) * 2 + (w.left == range ? 0 : 1)) * a.slot;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+            const int i = ty * 8 + r;
+            if (complete) {
+                const Row row = row_at<kRows>(a, w.r, kvh, w.rb, i);
+                if (!row.there) continue;
+                const bool some = l[r] != 0.0f && row.kept;
+                const float n = some ? 1.0f / l[r] : 0.0f;
+                const long long at = static_cast<long long>(row.token) * a.H + row.head;
+                Io* out = static_cast<Io*>(a.out) + at * a.dh;
+#pragma unroll
+                for (int g = 0; g < V; ++g)
+                    if (tx * 4 + 64 * g < a.dh) {
+                        alignas(16) Io y[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[e] = from_float<Io>(some ? o[r][4 * g + e] * n : 0.0f);
+                        if constexpr (sizeof(Io) == 4) *reinterpret_cast<uint4*>(out + tx * 4 + 64 * g) = *reinterpret_cast<const uint4*>(y);
+                        else *reinterpret_cast<uint2*>(out + tx * 4 + 64 * g) = *reinterpret_cast<const uint2*>(y);
+                    }
+                if (tx == 0 && a.lse) a.lse[at] = some ? (m[r] + log2f(l[r])) * kLn2 : -INFINITY;
+            } else {
+                if (tx == 0) {
+                    slot[i] = m[r];
+                    slot[kRows + i] = l[r];
+                }
+#pragma unroll
+                for (int g = 0; g < V; ++g)
+                    if (tx * 4 + 64 * g < a.dh)
+                        reinterpret_cast<float4*>(slot + 2 * kRows)[(tx + 16 * g) * kRows + i] =
+                            make_float4(o[r][4 * g], o[r][4 * g + 1], o[r][4 * g + 2], o[r][4 * g + 3]);
+            }
+        }
+        if (tid == 0 && w.left == w.t1 - w.t0)   // the range's last piece
+            a.openings[blockIdx.x] = {w.t0 == 0 && w.t1 < w.nt, w.s, w.kvh, w.rb, w.nt - w.t1, w.left == range, f.total};
+        w.next(a);
+        __syncthreads();
+    }
+    if (f.total == 0 && blockIdx.x == 0 && tid == 0) a.openings[0] = {0, 0, 0, 0, 0, 0, 0};
+    if (__any_sync(0xffffffffu, bad) && lane == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
+}
+
+// Thread blocks: as many as stay resident, no more than the line can have tiles.
+template <int DP>
+int blocks_of(const halo_paged_shape& sh, int n_tok, int n_seq) {
+    const int per_sm = static_cast<int>(227 * 1024 / (sizeof(Smem<DP>) + 1024));
+    const long long G = sh.n_heads / sh.n_kv_heads, cap = static_cast<long long>(sh.max_pages) * sh.page_size;
+    const long long items = (n_tok * G / kRows + (n_seq < n_tok ? n_seq : n_tok) + 1) * sh.n_kv_heads;
+    const long long tiles = items * ((cap + kTile - 1) / kTile), most = static_cast<long long>(kSmCount) * (per_sm < 4 ? per_sm : 4);
+    return static_cast<int>(tiles / kMinTiles < 1 ? 1 : tiles / kMinTiles < most ? tiles / kMinTiles : most);
+}
+template <typename F>
+auto by_width(const halo_paged_shape& sh, F f) {
+    return sh.head_dim <= 64    ? f(std::integral_constant<int, 64>())
+           : sh.head_dim <= 128 ? f(std::integral_constant<int, 128>())
+                                : f(std::integral_constant<int, 256>());
+}
+
+template <typename T>
+halo_status launch(const Args& args, const halo_paged_shape& sh, void* workspace, cudaStream_t st) {
+    return by_width(sh, [&](auto dp) -> halo_status {
+        constexpr int DP = decltype(dp)::value;
+        static bool done[64];
+        if (!ensure_dynamic_smem(paged_prompt_rows_kernel<T, DP>, sizeof(Smem<DP>), done)) return HALO_ERR_CUDA;
+        Args a = args;
+        a.blocks = blocks_of<DP>(sh, a.n_tok, a.n_seq);
+        a.slot = slot_floats(kRows, a.dh);
+        a.openings = static_cast<Opening*>(workspace);
+        a.ws = reinterpret_cast<float*>(a.openings + a.blocks);
+        const halo_status rc = launch_chained(paged_prompt_rows_kernel<T, DP>, a.blocks, kThreads, sizeof(Smem<DP>), st, a);
+        return rc != HALO_OK ? rc : launch_join<typename Kind<T>::Io, kRows>(a, st);
+    });
+}
+
+}  // namespace
+
+size_t f32_workspace(const halo_paged_shape& sh, int n_tok, int n_seq) {
+    return by_width(sh, [&](auto dp) {
+        return static_cast<size_t>(blocks_of<decltype(dp)::value>(sh, n_tok, n_seq)) *
+               (sizeof(Opening) + 2 * sizeof(float) * slot_floats(kRows, sh.head_dim));
+    });
+}
+halo_status f32_launch(const Args& a, const halo_paged_shape& sh, void* workspace, cudaStream_t st) {
+    if (sh.dtype == HALO_F32) return launch<float>(a, sh, workspace, st);
+    return a.K_scale ? launch<Eight>(a, sh, workspace, st) : launch<__nv_bfloat16>(a, sh, workspace, st);
+}
+
+}  // namespace prompt
+}  // namespace halo

@@ -1,0 +1,333 @@
+// The work line of halo_paged_prompt_mha, shared by its kernels.
+//
+// An item is ROWS rows of one (sequence, K/V head): row token * G + g of them is query head g of the G that share the K/V head, so
+// keys and values that come into an SM serve all of them.  Its keys, up to the last position that a row sees, are cut
+// into tiles of TILE.  All tiles of all items, item after item, form one line of T tiles and thread block c of C takes
+// [c * T / C, (c + 1) * T / C): however long prompts and caches are, every thread block sums the same number of tiles, and
+// few rows over a long cache fill the GPU as well as many.  A piece that covers a whole item writes its output; the at most two
+// pieces of a range that do not (its first and its last) leave (maximum, sum, weighted sum of values) per row in the workspace, and
+// a second kernel joins them in line order, so results do not depend on timing.  Every thread block computes the line from
+// q_start and seq_len itself; the host never reads a length.
+#pragma once
+
+#include "eight.cuh"
+
+namespace halo {
+namespace prompt {
+
+// What the join has to know of a range whose last piece begins an item that it does not end.
+struct __align__(16) Opening {
+    int opens, s, kvh, rb;
+    int rest, fills;      // tiles of the item behind the range; the item's first piece is the whole range
+    long long total;      // T
+};
+
+struct Args {
+    int n_tok, n_seq, H, Hk, G, dh, page_size, page_shift, n_pages, max_pages;   // page_shift: -1 = no power of two
+    int blocks;              // thread blocks of the first kernel
+    long long slot;          // floats of a workspace slot
+    long long page_stride, q_stride;
+    float scale_log2;
+    const void* q;
+    const void* K;
+    const void* V;
+    const uint8_t* K_scale;  // 8-bit rows
+    const uint8_t* V_scale;
+    const int32_t* q_start;
+    const int32_t* table;
+    const int32_t* seq_len;
+    const uint8_t* keep;
+    void* out;
+    float* lse;
+    Opening* openings;       // [blocks], then the slots: two per thread block
+    float* ws;
+    uint32_t* status;
+};
+
+constexpr float kLn2 = 0.693147180559945309f;
+
+// A slot: maxima [ROWS], sums [ROWS], weighted sums [dh / 4][ROWS][4]: neighbouring rows side by side, as threads hold them.
+__host__ __device__ constexpr long long slot_floats(int rows, int dh) { return static_cast<long long>(rows) * (dh + 2); }
+
+// 2^x, results below 2^-126 as 0
+__device__ __forceinline__ float pow2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ bool head_kept(const Args& a, int h) { return !a.keep || a.keep[h] != 0; }
+
+struct Rows {      // of a sequence
+    int first, n, len;
+};
+__device__ __forceinline__ Rows rows_of(const Args& a, int s, bool flag) {
+    const int q0 = ldg_waited(a.q_start + s), q1 = ldg_waited(a.q_start + s + 1), len = ldg_waited(a.seq_len + s);
+    const bool rows = q0 >= 0 && q1 >= q0 && q1 <= a.n_tok;
+    const bool fits = len >= 0 && len <= static_cast<long long>(a.max_pages) * a.page_size;
+    if (flag && !(rows && fits)) flag_status(a.status, HALO_DEV_BAD_INDEX);
+    return {q0, rows ? q1 - q0 : 0, fits ? len : 0};
+}
+
+// sum over i < n of floor((step * i + from) / m), by exchanging the roles of step and m until nothing is left (Euclid's way)
+__device__ __forceinline__ unsigned long long sum_of_floors(unsigned long long n, unsigned long long m, unsigned long long step,
+                                                            unsigned long long from) {
+    unsigned long long sum = 0;
+    while (n > 0) {
+        sum += n * (n - 1) / 2 * (step / m) + n * (from / m);
+        step %= m;
+        from %= m;
+        const unsigned long long top = step * n + from;
+        n = top / m;
+        from = top % m;
+        const unsigned long long t = m;
+        m = step;
+        step = t;
+        if (m == 0) break;      // n is 0 then
+    }
+    return sum;
+}
+
+template <int ROWS, int TILE>
+struct Line {
+    static __device__ __forceinline__ int blocks_of(const Args& a, const Rows& r) {
+        return static_cast<int>((static_cast<long long>(r.n) * a.G + ROWS - 1) / ROWS);
+    }
+    // positions that the last row of an item sees
+    static __device__ __forceinline__ int reach(const Args& a, const Rows& r, int rb) {
+        const long long u = (rb + 1ll) * ROWS - 1, all = static_cast<long long>(r.n) * a.G - 1;
+        const int token = u < all ? static_cast<int>(u / a.G) : r.n - 1;
+        return max(r.len - r.n + token + 1, 0);
+    }
+    static __device__ __forceinline__ int tiles(const Args& a, const Rows& r, int rb) {
+        return max((reach(a, r, rb) + TILE - 1) / TILE, 1);     // an item that sees nothing keeps one tile, which writes its zeros
+    }
+    // tiles of all items of one K/V head of a sequence
+    static __device__ __forceinline__ long long tiles_per_head(const Args& a, const Rows& r) {
+        if (r.n == 0) return 0;
+        const long long nb = blocks_of(a, r), last = tiles(a, r, static_cast<int>(nb - 1));
+        if (nb == 1) return last;
+        // item rb < nb - 1: max(1, floor((ROWS * (rb + 1) - 1 + G * (len - n + TILE)) / (G * TILE)))
+        const long long m = static_cast<long long>(a.G) * TILE, base = static_cast<long long>(r.len - r.n) * a.G;
+        long long ones = base < 0 ? (-base) / ROWS : 0;          // items of which no row sees anything
+        if (ones > nb - 1) ones = nb - 1;
+        return last + ones + static_cast<long long>(sum_of_floors(nb - 1 - ones, m, ROWS, ROWS * (ones + 1) - 1 + base + m));
+    }
+};
+
+// Thread blocks that have a range, and where the c-th range begins.  A range has at least kMinTiles tiles unless there are fewer: a
+// cut costs two slots of traffic and a join.
+constexpr int kMinTiles = 2;
+__device__ __forceinline__ int ranges(long long T, int blocks) {
+    const long long n = T / kMinTiles;
+    return n < 1 ? 1 : n < blocks ? static_cast<int>(n) : blocks;
+}
+__device__ __forceinline__ long long cut(long long T, int c, int C) { return T * c / C; }
+// the range that holds line position x: the last c with T * c / C <= x
+__device__ __forceinline__ int range_of(long long T, long long x, int C) { return static_cast<int>(((x + 1) * C - 1) / T); }
+
+// The way along a range: piece after piece.
+template <int ROWS, int TILE>
+struct Walk {
+    using L = Line<ROWS, TILE>;
+    long long left;      // tiles from t0 of this piece to the end of the range
+    Rows r;
+    int s, kvh, rb, nb;
+    int nt, t0, t1;      // tiles of the item, of the piece
+    int reach;           // positions that take part: 0 where every head of the item is lost
+    __device__ __forceinline__ void item(const Args& a) {
+        nt = L::tiles(a, r, rb);
+        t1 = static_cast<int>(min(static_cast<long long>(nt), t0 + left));
+        reach = L::reach(a, r, rb);
+        if (a.keep) {
+            bool any = false;
+            for (int g = 0; g < a.G; ++g) any |= head_kept(a, kvh * a.G + g);
+            if (!any) reach = 0;
+        }
+    }
+    __device__ __forceinline__ bool complete() const { return t0 == 0 && t1 == nt; }
+    __device__ __forceinline__ void next(const Args& a) {
+        left -= t1 - t0;
+        if (left <= 0) return;
+        t0 = 0;
+        if (++rb == nb) {
+            rb = 0;
+            if (++kvh == a.Hk) {
+                kvh = 0;
+                do r = rows_of(a, ++s, false);
+                while (r.n == 0);      // a range ends with the last item: there is one
+                nb = L::blocks_of(a, r);
+            }
+        }
+        item(a);
+    }
+};
+
+template <int ROWS, int TILE>
+struct Found {
+    Walk<ROWS, TILE> walk;
+    long long total;
+    int C;
+};
+// The range of this thread block; all its THREADS threads call it.  left = 0: none.
+template <int ROWS, int TILE, int THREADS>
+__device__ __forceinline__ Found<ROWS, TILE> locate(const Args& a, long long* sh /*[THREADS / 32 + 3]*/) {
+    using L = Line<ROWS, TILE>;
+    constexpr int W = THREADS / 32;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (a.n_seq + THREADS - 1) / THREADS;
+    const int s0 = min(tid * per, a.n_seq), s1 = min(s0 + per, a.n_seq);
+    long long own = 0;
+    for (int s = s0; s < s1; ++s) own += L::tiles_per_head(a, rows_of(a, s, blockIdx.x == 0));
+    long long incl = own;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) sh[warp] = incl;
+    __syncthreads();
+    long long before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        if (w < warp) before += sh[w];
+        total += sh[w];
+    }
+    Found<ROWS, TILE> f;
+    f.total = total * a.Hk;
+    f.C = ranges(f.total, a.blocks);
+    f.walk.left = 0;
+    if (f.total == 0 || static_cast<int>(blockIdx.x) >= f.C) return f;     // the same in every thread
+    const long long x = cut(f.total, blockIdx.x, f.C);
+    long long at = (before + incl - own) * a.Hk;
+    if (x >= at && x < at + own * a.Hk) {
+        for (int s = s0; s < s1; ++s) {
+            const long long n = L::tiles_per_head(a, rows_of(a, s, false));
+            if (x < at + n * a.Hk) {
+                sh[W] = x - at;
+                sh[W + 1] = s;
+                sh[W + 2] = n;
+                break;
+            }
+            at += n * a.Hk;
+        }
+    }
+    __syncthreads();
+    Walk<ROWS, TILE>& w = f.walk;
+    const long long inside = sh[W], per_head = sh[W + 2];
+    w.s = static_cast<int>(sh[W + 1]);
+    w.left = cut(f.total, blockIdx.x + 1, f.C) - x;
+    w.r = rows_of(a, w.s, false);
+    w.nb = L::blocks_of(a, w.r);
+    w.kvh = static_cast<int>(inside / per_head);
+    // the item: 32 at a time
+    long long rem = inside - w.kvh * per_head;
+    for (int b = 0;; b += 32) {
+        const int n = b + lane < w.nb ? L::tiles(a, w.r, b + lane) : 0;
+        long long upto = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const uint32_t past = __ballot_sync(0xffffffffu, upto > rem);
+        if (past) {
+            const int at_lane = __ffs(past) - 1;
+            w.rb = b + at_lane;
+            w.t0 = static_cast<int>(rem - __shfl_sync(0xffffffffu, upto - n, at_lane));
+            break;
+        }
+        rem -= __shfl_sync(0xffffffffu, upto, 31);
+    }
+    w.item(a);
+    __syncthreads();      // sh may be used for something else
+    return f;
+}
+
+// Row i of an item: its token and head, or no row.
+struct Row {
+    int token, head;      // row of q; query head
+    int sees;             // positions
+    bool there, kept;
+};
+template <int ROWS>
+__device__ __forceinline__ Row row_at(const Args& a, const Rows& r, int kvh, int rb, int i) {
+    const long long u = static_cast<long long>(rb) * ROWS + i;
+    Row w;
+    w.there = u < static_cast<long long>(r.n) * a.G;
+    const int token = w.there ? static_cast<int>(u / a.G) : 0;
+    w.token = r.first + token;
+    w.head = kvh * a.G + (w.there ? static_cast<int>(u - static_cast<long long>(token) * a.G) : 0);
+    w.kept = w.there && head_kept(a, w.head);
+    w.sees = w.kept ? max(r.len - r.n + token + 1, 0) : 0;
+    return w;
+}
+
+// Pieces of cut items: blockIdx.x = the range that begins an item and does not end it, blockIdx.y = 32 rows and 32 columns of it.
+// A lane has a row, a warp four columns.
+template <typename Io, int ROWS>
+__global__ void __launch_bounds__(256) paged_prompt_join_kernel(const __grid_constant__ Args a) {
+    constexpr int kAhead = 4;
+    const int lane = threadIdx.x & 31, c0 = blockIdx.x;
+    const int row = (blockIdx.y % (ROWS / 32)) * 32 + lane, c4 = (blockIdx.y / (ROWS / 32)) * 8 + (threadIdx.x >> 5);
+    chain_wait();   // in every block: this grid may not end before the first one
+    const int4 head = __ldcg(reinterpret_cast<const int4*>(a.openings + c0));
+    const int4 more = __ldcg(reinterpret_cast<const int4*>(a.openings + c0) + 1);
+    const long long total = __ldcg(&a.openings[0].total);
+    const int C = ranges(total, a.blocks);
+    if (c0 + 1 >= C || !head.x || c4 * 4 >= a.dh) return;   // behind the last range: a record that nobody wrote
+    const Rows r = rows_of(a, head.y, false);
+    const Row w = row_at<ROWS>(a, r, head.z, head.w, row);
+    if (!w.there) return;
+    const int pieces = range_of(total, cut(total, c0 + 1, C) + more.x - 1, C) - c0 + 1;
+    // piece 0 in the slot of range c0 that holds its end (its first one if the item fills the range), the others in the
+    // first slots of the ranges behind it
+    const float* ws0 = a.ws + (static_cast<long long>(c0) * 2 + (more.y ? 0 : 1)) * a.slot;
+    const float* ws1 = a.ws + static_cast<long long>(c0) * 2 * a.slot;
+    float M = -INFINITY, L = 0.0f;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int k0 = 0; k0 < pieces; k0 += kAhead) {
+        float m[kAhead], l[kAhead];
+        float4 x[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            const bool there = k0 + e < pieces;
+            const float* p = k0 + e == 0 ? ws0 : ws1 + static_cast<long long>(k0 + e) * 2 * a.slot;
+            m[e] = there ? __ldcg(p + row) : -INFINITY;
+            l[e] = there ? __ldcg(p + ROWS + row) : 0.0f;
+            x[e] = there ? __ldcg(reinterpret_cast<const float4*>(p + 2 * ROWS) + c4 * ROWS + row) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            const float mx = fmaxf(M, m[e]), base = mx == -INFINITY ? 0.0f : mx;
+            const float f = pow2(M - base), g = pow2(m[e] - base);
+            M = mx;
+            L = fmaf(L, f, l[e] * g);
+            v.x = fmaf(v.x, f, x[e].x * g);
+            v.y = fmaf(v.y, f, x[e].y * g);
+            v.z = fmaf(v.z, f, x[e].z * g);
+            v.w = fmaf(v.w, f, x[e].w * g);
+        }
+    }
+    const bool some = L != 0.0f && w.kept;
+    const float n = some ? 1.0f / L : 0.0f;
+    const long long at = static_cast<long long>(w.token) * a.H + w.head;
+    Io* out = static_cast<Io*>(a.out) + at * a.dh + c4 * 4;
+    alignas(16) Io y[4] = {from_float<Io>(some ? v.x * n : 0.0f), from_float<Io>(some ? v.y * n : 0.0f),
+                           from_float<Io>(some ? v.z * n : 0.0f), from_float<Io>(some ? v.w * n : 0.0f)};
+    if constexpr (sizeof(Io) == 4) *reinterpret_cast<uint4*>(out) = *reinterpret_cast<const uint4*>(y);
+    else *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(y);
+    if (c4 == 0 && a.lse) a.lse[at] = some ? (M + log2f(L)) * kLn2 : -INFINITY;
+}
+
+template <typename Io, int ROWS>
+halo_status launch_join(const Args& a, cudaStream_t st) {
+    if (a.blocks < 2) return HALO_OK;
+    return launch_chained(paged_prompt_join_kernel<Io, ROWS>, dim3(a.blocks - 1, ROWS / 32 * ((a.dh + 31) / 32)), 256, 0, st, a);
+}
+
+// The f32 form (paged_prompt_f32.cu)
+size_t f32_workspace(const halo_paged_shape& sh, int n_tok, int n_seq);
+halo_status f32_launch(const Args& a, const halo_paged_shape& sh, void* workspace, cudaStream_t st);
+
+}  // namespace prompt
+}  // namespace halo

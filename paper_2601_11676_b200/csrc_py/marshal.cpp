@@ -22,6 +22,10 @@ struct Entry {
     decltype(&halo_quantize_rows_mx4) quantize;
     decltype(&halo_dequantize_rows_mx4) dequantize;
     decltype(&halo_product_mx4) product;
+    decltype(&halo_paged_norm_append) norm_append;
+    decltype(&halo_paged_kv_read) kv_read;
+    decltype(&halo_paged_mha_f8) paged_mha_f8;
+    decltype(&halo_paged_prompt_mha) prompt_mha;
 } entry;
 bool bound = false;
 
@@ -128,6 +132,10 @@ struct Call {
         if (!ok) refuse(what, name, "does not fit the shape", o);
         return t.data_ptr();
     }
+    // scale bytes of an 8-bit cache [n_pages][n_kv_heads][page_size], or None
+    uint8_t* scales(const char* name, PyObject* o, const halo_paged_shape& s) const {
+        return static_cast<uint8_t*>(dense(name, o, c10::kByte, static_cast<long long>(s.n_pages) * s.n_kv_heads * s.page_size));
+    }
     cudaStream_t stream(PyObject* o) const {
         if (!device.is_cuda()) refuse(what, "the tensors", "have to be on a GPU");
         if (o == Py_None) return c10::cuda::getCurrentCUDAStream(device.index()).stream();
@@ -223,6 +231,146 @@ PyObject* paged_mha(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// shape, q, k, v, w_q, w_k, eps, pos, seq, table, inv_freq, interleaved, turn_scale, q_out, K, V, K_scale, V_scale, status, stream
+PyObject* norm_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 20, [&]() -> halo_status {
+        Call c{"halo_paged_norm_append"};
+        const auto s = shape_of<halo_paged_shape>(c.what, a[0]);
+        const auto type = type_of(c.what, s.dtype);
+        c.lead("k", a[2]);
+        const at::Tensor &k = c.tensor("k", a[2]), &table = c.tensor("block_table", a[9]);
+        if (k.dim() < 1 || table.dim() < 1) refuse(c.what, "k and block_table", "have to have rows");
+        const long long n_tok = k.size(0), n_seq = table.size(0);
+        if (n_tok > INT_MAX || n_seq > INT_MAX) refuse(c.what, "k", "has too many rows");
+        const long long qw = static_cast<long long>(s.n_heads) * s.head_dim, kw = static_cast<long long>(s.n_kv_heads) * s.head_dim;
+        long long qs = 0, ks = 0, vs = 0, os = 0;
+        void *q = nullptr, *qo = nullptr;
+        if ((a[1] == Py_None) != (a[13] == Py_None)) refuse(c.what, "q and q_out", "go together");
+        if (a[1] != Py_None) {
+            q = c.rows("q", a[1], type, n_tok, qw, qs);
+            qo = c.rows("q_out", a[13], type, n_tok, qw, os);
+        }
+        void* kp = c.rows("k", a[2], type, n_tok, kw, ks);
+        void* vp = c.rows("v", a[3], type, n_tok, kw, vs);
+        void* wq = c.dense("w_q", a[4], type, s.head_dim);
+        void* wk = c.dense("w_k", a[5], type, s.head_dim);
+        const float eps = static_cast<float>(real(a[6]));
+        auto* pos = static_cast<const int32_t*>(c.dense("pos", a[7], c10::kInt, n_tok));
+        auto* seq = static_cast<const int32_t*>(c.dense("seq_of_tok", a[8], c10::kInt, n_tok));
+        auto* tab = static_cast<const int32_t*>(c.dense("block_table", a[9], c10::kInt, n_seq * s.max_pages));
+        auto* inv = static_cast<const double*>(c.dense("inv_freq", a[10], c10::kDouble, 0, false));
+        const long long pairs = inv ? c.tensor("inv_freq", a[10]).numel() : 0;
+        if (pairs > 1 << 20) refuse(c.what, "inv_freq", "is too long", a[10]);
+        const int inter = PyObject_IsTrue(a[11]);
+        if (inter < 0) throw Refused();
+        const float turn_scale = static_cast<float>(real(a[12]));
+        const auto row = a[16] == Py_None ? type : c10::kByte;
+        void* K = c.cache("K_cache", a[14], row, s);
+        void* V = c.cache("V_cache", a[15], row, s);
+        uint8_t* Ks = c.scales("K_scale", a[16], s);
+        uint8_t* Vs = c.scales("V_scale", a[17], s);
+        auto* status = static_cast<uint32_t*>(c.dense("dev_status", a[18], c10::kInt, 1, false));
+        const cudaStream_t st = c.stream(a[19]);
+        const c10::cuda::CUDAGuard guard(c.device);
+        return entry.norm_append(&s, static_cast<int>(n_tok), static_cast<int>(n_seq), q, qs, kp, ks, vp, vs, wq, wk, eps, pos, seq, tab,
+                                 inv, static_cast<int>(2 * pairs), inter, turn_scale, qo, os, K, V, Ks, Vs, status, st);
+    });
+}
+
+// shape, pos, seq, table, K, V, k_out, v_out, K_scale, V_scale, status, stream
+PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 12, [&]() -> halo_status {
+        Call c{"halo_paged_kv_read"};
+        const auto s = shape_of<halo_paged_shape>(c.what, a[0]);
+        const auto type = type_of(c.what, s.dtype), row = a[8] == Py_None ? type : c10::kByte;
+        c.lead("k_out", a[6]);
+        const at::Tensor &k = c.tensor("k_out", a[6]), &table = c.tensor("block_table", a[3]);
+        if (k.dim() < 1 || table.dim() < 1) refuse(c.what, "k_out and block_table", "have to have rows");
+        const long long n_tok = k.size(0), n_seq = table.size(0), kw = static_cast<long long>(s.n_kv_heads) * s.head_dim;
+        if (n_tok > INT_MAX || n_seq > INT_MAX) refuse(c.what, "k_out", "has too many rows");
+        long long ks = 0, vs = 0;
+        auto* pos = static_cast<const int32_t*>(c.dense("pos", a[1], c10::kInt, n_tok));
+        auto* seq = static_cast<const int32_t*>(c.dense("seq_of_tok", a[2], c10::kInt, n_tok));
+        auto* tab = static_cast<const int32_t*>(c.dense("block_table", a[3], c10::kInt, n_seq * s.max_pages));
+        void* K = c.cache("K_cache", a[4], row, s);
+        void* V = c.cache("V_cache", a[5], row, s);
+        void* ko = c.rows("k_out", a[6], type, n_tok, kw, ks);
+        void* vo = c.rows("v_out", a[7], type, n_tok, kw, vs);
+        uint8_t* Ks = c.scales("K_scale", a[8], s);
+        uint8_t* Vs = c.scales("V_scale", a[9], s);
+        auto* status = static_cast<uint32_t*>(c.dense("dev_status", a[10], c10::kInt, 1, false));
+        const cudaStream_t st = c.stream(a[11]);
+        const c10::cuda::CUDAGuard guard(c.device);
+        return entry.kv_read(&s, static_cast<int>(n_tok), static_cast<int>(n_seq), pos, seq, tab, K, V, Ks, Vs, ko, ks, vo, vs, status, st);
+    });
+}
+
+// shape, q, K, V, K_scale, V_scale, table, seq_len, scale, out, workspace, keep, lse, status, stream
+PyObject* paged_mha_f8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 15, [&]() -> halo_status {
+        Call c{"halo_paged_mha_f8"};
+        const auto s = shape_of<halo_paged_shape>(c.what, a[0]);
+        const auto type = type_of(c.what, s.dtype);
+        c.lead("q", a[1]);
+        const at::Tensor& qt = c.tensor("q", a[1]);
+        if (qt.dim() < 1) refuse(c.what, "q", "has to have rows");
+        const long long n_seq = qt.size(0), width = static_cast<long long>(s.n_heads) * s.head_dim;
+        if (n_seq > INT_MAX) refuse(c.what, "q", "has too many rows");
+        long long qs = 0;
+        void* q = c.rows("q", a[1], type, n_seq, width, qs);
+        void* K = c.cache("K_cache", a[2], c10::kByte, s);
+        void* V = c.cache("V_cache", a[3], c10::kByte, s);
+        uint8_t* Ks = c.scales("K_scale", a[4], s);
+        uint8_t* Vs = c.scales("V_scale", a[5], s);
+        auto* tab = static_cast<const int32_t*>(c.dense("block_table", a[6], c10::kInt, n_seq * s.max_pages));
+        auto* len = static_cast<const int32_t*>(c.dense("seq_len", a[7], c10::kInt, n_seq));
+        const float scale = static_cast<float>(real(a[8]));
+        void* out = c.dense("out", a[9], type, n_seq * width);
+        void* ws = c.dense("workspace", a[10], c10::kByte, 0, false);
+        const size_t ws_bytes = ws ? static_cast<size_t>(c.tensor("workspace", a[10]).numel()) : 0;
+        auto* keep = static_cast<const uint8_t*>(c.dense("keep", a[11], c10::kByte, s.n_heads));
+        auto* lse = static_cast<float*>(c.dense("lse", a[12], c10::kFloat, n_seq * s.n_heads));
+        auto* status = static_cast<uint32_t*>(c.dense("dev_status", a[13], c10::kInt, 1, false));
+        const cudaStream_t st = c.stream(a[14]);
+        const c10::cuda::CUDAGuard guard(c.device);
+        return entry.paged_mha_f8(&s, static_cast<int>(n_seq), q, qs, K, V, Ks, Vs, tab, len, keep, scale, out, lse, ws, ws_bytes, status, st);
+    });
+}
+
+// shape, q, q_start, K, V, table, seq_len, scale, out, workspace, K_scale, V_scale, keep, lse, status, stream
+PyObject* prompt_mha(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 16, [&]() -> halo_status {
+        Call c{"halo_paged_prompt_mha"};
+        const auto s = shape_of<halo_paged_shape>(c.what, a[0]);
+        const auto type = type_of(c.what, s.dtype), row = a[10] == Py_None ? type : c10::kByte;
+        c.lead("q", a[1]);
+        const at::Tensor &qt = c.tensor("q", a[1]), &lens = c.tensor("seq_len", a[6]);
+        if (qt.dim() < 1) refuse(c.what, "q", "has to have rows");
+        const long long n_tok = qt.size(0), n_seq = lens.numel(), width = static_cast<long long>(s.n_heads) * s.head_dim;
+        if (n_tok > INT_MAX || n_seq > INT_MAX) refuse(c.what, "q", "has too many rows");
+        long long qs = 0;
+        void* q = c.rows("q", a[1], type, n_tok, width, qs);
+        auto* start = static_cast<const int32_t*>(c.dense("q_start", a[2], c10::kInt, n_seq + 1));
+        void* K = c.cache("K_cache", a[3], row, s);
+        void* V = c.cache("V_cache", a[4], row, s);
+        auto* tab = static_cast<const int32_t*>(c.dense("block_table", a[5], c10::kInt, n_seq * s.max_pages));
+        auto* len = static_cast<const int32_t*>(c.dense("seq_len", a[6], c10::kInt, n_seq));
+        const float scale = static_cast<float>(real(a[7]));
+        void* out = c.dense("out", a[8], type, n_tok * width);
+        void* ws = c.dense("workspace", a[9], c10::kByte, 0, false);
+        const size_t ws_bytes = ws ? static_cast<size_t>(c.tensor("workspace", a[9]).numel()) : 0;
+        uint8_t* Ks = c.scales("K_scale", a[10], s);
+        uint8_t* Vs = c.scales("V_scale", a[11], s);
+        auto* keep = static_cast<const uint8_t*>(c.dense("keep", a[12], c10::kByte, s.n_heads));
+        auto* lse = static_cast<float*>(c.dense("lse", a[13], c10::kFloat, n_tok * s.n_heads));
+        auto* status = static_cast<uint32_t*>(c.dense("dev_status", a[14], c10::kInt, 1, false));
+        const cudaStream_t st = c.stream(a[15]);
+        const c10::cuda::CUDAGuard guard(c.device);
+        return entry.prompt_mha(&s, static_cast<int>(n_tok), static_cast<int>(n_seq), q, qs, start, K, V, Ks, Vs, tab, len, keep, scale, out,
+                                lse, ws, ws_bytes, status, st);
+    });
+}
+
 PyObject* norm_glue(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(n, 10, [&]() -> halo_status {
         Call c{"halo_norm_glue"};
@@ -294,12 +442,13 @@ PyObject* product(PyObject*, PyObject* const* a, Py_ssize_t n) {   // d, n_tok, 
 }
 
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {   // addresses, in the order of Entry, and the two types of shape
-    if (n != 8) {
-        PyErr_SetString(PyExc_TypeError, "_marshal.bind: six addresses and two types");
+    constexpr int kEntries = 10;
+    if (n != kEntries + 2) {
+        PyErr_SetString(PyExc_TypeError, "_marshal.bind: ten addresses and two types");
         return nullptr;
     }
-    void* p[6];
-    for (int i = 0; i < 6; ++i) {
+    void* p[kEntries];
+    for (int i = 0; i < kEntries; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (!p[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "_marshal.bind: no address");
@@ -312,10 +461,14 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {   // addresses, in
     entry.quantize = reinterpret_cast<decltype(entry.quantize)>(p[3]);
     entry.dequantize = reinterpret_cast<decltype(entry.dequantize)>(p[4]);
     entry.product = reinterpret_cast<decltype(entry.product)>(p[5]);
-    Py_INCREF(a[6]);
-    Py_INCREF(a[7]);
-    paged_shape_type = a[6];
-    norm_shape_type = a[7];
+    entry.norm_append = reinterpret_cast<decltype(entry.norm_append)>(p[6]);
+    entry.kv_read = reinterpret_cast<decltype(entry.kv_read)>(p[7]);
+    entry.paged_mha_f8 = reinterpret_cast<decltype(entry.paged_mha_f8)>(p[8]);
+    entry.prompt_mha = reinterpret_cast<decltype(entry.prompt_mha)>(p[9]);
+    Py_INCREF(a[kEntries]);
+    Py_INCREF(a[kEntries + 1]);
+    paged_shape_type = a[kEntries];
+    norm_shape_type = a[kEntries + 1];
     bound = true;
     Py_RETURN_NONE;
 }
@@ -328,6 +481,10 @@ PyMethodDef methods[] = {METHOD("bind", bind),
                          METHOD("quantize_rows_mx4", rows_mx4<false>),
                          METHOD("dequantize_rows_mx4", rows_mx4<true>),
                          METHOD("product_mx4", product),
+                         METHOD("norm_append", norm_append),
+                         METHOD("kv_read", kv_read),
+                         METHOD("paged_mha_f8", paged_mha_f8),
+                         METHOD("prompt_mha", prompt_mha),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
