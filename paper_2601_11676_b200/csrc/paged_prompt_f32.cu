@@ -246,15 +246,15 @@ __global__ void __launch_bounds__(kThreads) paged_prompt_rows_kernel(const __gri
                         else *reinterpret_cast<uint2*>(out + tx * 4 + 64 * g) = *reinterpret_cast<const uint2*>(y);
                     }
                 if (tx == 0 && a.lse) a.lse[at] = some ? (m[r] + log2f(l[r])) * kLn2 : -INFINITY;
-            } else {
+            } else if (i < a.rows) {
                 if (tx == 0) {
                     slot[i] = m[r];
-                    slot[kRows + i] = l[r];
+                    slot[a.rows + i] = l[r];
                 }
 #pragma unroll
                 for (int g = 0; g < V; ++g)
                     if (tx * 4 + 64 * g < a.dh)
-                        reinterpret_cast<float4*>(slot + 2 * kRows)[(tx + 16 * g) * kRows + i] =
+                        reinterpret_cast<float4*>(slot + 2 * a.rows)[(tx + 16 * g) * a.rows + i] =
                             make_float4(o[r][4 * g], o[r][4 * g + 1], o[r][4 * g + 2], o[r][4 * g + 3]);
             }
         }
@@ -291,7 +291,8 @@ halo_status launch(const Args& args, const halo_paged_shape& sh, void* workspace
         if (!ensure_dynamic_smem(paged_prompt_rows_kernel<T, DP>, sizeof(Smem<DP>), done)) return HALO_ERR_CUDA;
         Args a = args;
         a.blocks = blocks_of<DP>(sh, a.n_tok, a.n_seq);
-        a.slot = slot_floats(kRows, a.dh);
+        a.rows = slot_rows(kRows, a.n_tok, sh);
+        a.slot = slot_floats(a.rows, a.dh);
         a.openings = static_cast<Opening*>(workspace);
         a.ws = reinterpret_cast<float*>(a.openings + a.blocks);
         const halo_status rc = launch_chained(paged_prompt_rows_kernel<T, DP>, a.blocks, kThreads, sizeof(Smem<DP>), st, a);
@@ -304,7 +305,7 @@ halo_status launch(const Args& args, const halo_paged_shape& sh, void* workspace
 size_t f32_workspace(const halo_paged_shape& sh, int n_tok, int n_seq) {
     return by_width(sh, [&](auto dp) {
         return static_cast<size_t>(blocks_of<decltype(dp)::value>(sh, n_tok, n_seq)) *
-               (sizeof(Opening) + 2 * sizeof(float) * slot_floats(kRows, sh.head_dim));
+               (sizeof(Opening) + 2 * sizeof(float) * slot_floats(slot_rows(kRows, n_tok, sh), sh.head_dim));
     });
 }
 halo_status f32_launch(const Args& a, const halo_paged_shape& sh, void* workspace, cudaStream_t st) {

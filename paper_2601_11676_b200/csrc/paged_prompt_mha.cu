@@ -1,19 +1,690 @@
-// halo_paged_prompt_mha: causal attention of packed chunks of new tokens over a paged K/V cache.
+// halo_paged_prompt_mha: causal attention of packed chunks of new tokens over a paged K/V cache, on the tensor cores
+// (tcgen05).  Bound by them for prompts (4 flops per row, key and column of the head), by HBM for a few rows over a long cache.
+//
+// Per thread block, one to an SM:
+//   - warps 8 to 11 gather K and V rows of 128 keys from their pages into a ring of stages (cp.async; 128 keys x 128 columns a
+//     stage, in the 128-byte swizzle that the tensor cores read), and an item's rows of Q;
+//   - one thread of warp 12 issues the products: S = Q K^T into tensor memory, O += P V with P in tensor memory;
+//   - warps 0 to 3 and 4 to 7 take a row per thread: running maximum and sum, P = 2^(S scale - maximum) as bf16 in place of S.
+// An item has 256 rows in two streams of 128: while one stream's rows are in the softmax, the other's products run.  Head sizes
+// above 128 (whose O fills half of tensor memory) and items of up to 128 rows have one stream with two S buffers instead.
+//
+// The running maximum that weights are relative to moves only when a row's maximum has grown by 2^8: O and the sum are in fp32, so
+// nothing is lost by weights up to 2^8, and O, which would have to be read, multiplied and written back for every move, is left
+// alone after the first tiles.
+//
+// What a row does not see must not reach it, and 0 * infinity would: in tiles that not every row sees, value rows with a NaN or an
+// infinity are taken out of the stage, and each thread adds them to its row of O by itself where its row sees them.
 #include <math.h>
 
+#include <type_traits>
+
 #include "prompt_line.cuh"
+#include "umma.cuh"
 
 namespace halo {
 halo_status check_paged_shape(const halo_paged_shape* s);
 halo_status check_eight(const halo_paged_shape& s, const void* K_scale, const void* V_scale);
 long long paged_stride(const halo_paged_shape& s);
+
+namespace prompt {
+namespace {
+
+constexpr int kTile = 128;         // keys
+constexpr int kThreads = 512;
+constexpr int kFlags = 8;          // tiles whose flags are kept
+
+// DP: head size padded to 64, 128 or 256.
+template <int DP>
+struct Cfg {
+    static constexpr int kStreams = DP > 128 ? 1 : 2;
+    static constexpr int kRows = 128 * kStreams;
+    static constexpr int kCols = DP < 128 ? DP : 128;         // of a stage
+    static constexpr int kParts = DP / kCols;                 // stages of a K or V tile
+    static constexpr int kStage = kTile * kCols * 2;
+    static constexpr int kStages = DP == 64 ? 8 : 5;
+    static constexpr int kQTile = 128 * DP * 2;               // Q of a stream
+    static constexpr int kQ = kStreams * kQTile;
+    static constexpr int kO = 256;                            // tensor memory: S at 0 and 128, O behind
+};
+
+struct Flags {
+    uint32_t there[kFlags][4];       // which of a tile's keys are there
+    uint32_t odd[kFlags][2][4];      // which of a tile's value rows were taken out, per part
+};
+struct Bars {
+    uint64_t full[8], empty[8], q_full, q_empty, s_full[2], p_full[2], pv_done[2];
+    uint32_t tmem;
+    int abort;
+    uint32_t o_set[2];               // the last piece whose O held something before its first product, per stream
+};
+template <int DP>
+struct Smem {
+    unsigned char q[Cfg<DP>::kQ];
+    unsigned char ring[Cfg<DP>::kStages * Cfg<DP>::kStage];
+    long long q_row[Cfg<DP>::kRows];     // where the item's rows of q are, -1: none
+    Flags flags;
+    Bars bars;
+    long long sh[kThreads / 32 + 3];
+};
+
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t phase, int* abort) {
+    if (mbar_wait_bounded(bar, phase & 1u, abort)) return true;
+    *reinterpret_cast<volatile int*>(abort) = 1;
+    return false;
+}
+// by a whole warp: the same answer in every lane
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t phase, int* abort) {
+    return __all_sync(0xffffffffu, wait(bar, phase, abort));
+}
+// D[tmem] (+)= A[tmem] * B[smem], issued by one thread
+__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b_desc, uint32_t idesc, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b_desc), "r"(idesc), "r"(static_cast<uint32_t>(accumulate))
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+        "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+__device__ __forceinline__ uint32_t tmem_ld_word(uint32_t taddr) {
+    uint32_t v;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(v) : "r"(taddr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+// 512 threads start with 128 registers each: 2 * 128 * 192 + 128 * 88 + 128 * 40 = 512 * 128
+constexpr int kRowRegs = 192, kCopyRegs = 88, kIssueRegs = 40;
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
+    const int n = valid ? 16 : 0;   // 0: the 16 bytes are filled with zeros and src is not read
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ bool odd_word(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+
+// A piece as every role sees it: its tiles, its streams and how many of the tiles each of them takes part in.
+template <int DP>
+struct Piece {
+    using C = Cfg<DP>;
+    int n, streams, tiles[2];
+    int sees_first;      // positions that every row of the item sees
+    __device__ __forceinline__ Piece(const Args& a, const Walk<C::kRows, kTile>& w) {
+        const long long base = static_cast<long long>(w.rb) * C::kRows, all = static_cast<long long>(w.r.n) * a.G;
+        const int first = w.r.len - w.r.n + 1;
+        n = w.reach > 0 ? w.t1 - w.t0 : 0;
+        streams = C::kStreams == 2 && base + 128 < all ? 2 : 1;
+        sees_first = first + static_cast<int>(base / a.G);
+        tiles[0] = tiles[1] = n;
+        if (C::kStreams == 2 && streams == 2) {      // the first stream's last row may not see the last tiles
+            const int sees = first + static_cast<int>((base + 127) / a.G);
+            tiles[0] = min(n, max((sees + kTile - 1) / kTile - w.t0, 0));
+        }
+        if (streams == 1) tiles[1] = 0;
+    }
+    // whether some row does not see all of the tile
+    __device__ __forceinline__ bool partial(int tile) const { return (tile + 1) * kTile > sees_first; }
+    // buffer of tile j of a stream
+    __device__ __forceinline__ int buffer(int stream, int j) const { return streams == 2 ? stream : j & 1; }
+    __device__ __forceinline__ uint32_t uses(int buffer) const { return streams == 2 ? tiles[buffer] : (n + 1 - buffer) / 2; }
+};
+
+// ---- gathering ------------------------------------------------------------------------------------------------------------------
+
+template <int DP>
+struct Gather {
+    using C = Cfg<DP>;
+    static constexpr int kChunks = C::kCols / 8;           // 16-byte chunks of a stage's row
+    static constexpr int kAtOnce = 32 / kChunks;           // rows per instruction
+    const Args& a;
+    Smem<DP>& sm;
+    int* abort;
+    const int warp, lane;
+    uint32_t fill = 0;                  // stages filled so far
+    uint32_t waiting[2];                // barriers of copies that are on their way
+    int n_waiting = 0;
+    bool alive = true;
+
+    __device__ __forceinline__ Gather(const Args& a_, Smem<DP>& sm_) : a(a_), sm(sm_), abort(&sm_.bars.abort), warp((threadIdx.x >> 5) & 3), lane(threadIdx.x & 31) {}
+    __device__ __forceinline__ void signal(uint32_t bar) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+    }
+    __device__ __forceinline__ void flush() {
+        cp_wait<0>();
+        if (n_waiting > 0) signal(waiting[0]);
+        if (n_waiting > 1) signal(waiting[1]);
+        n_waiting = 0;
+    }
+    // copies that were just issued: the ones two before them are complete behind the wait
+    __device__ __forceinline__ void issued(uint32_t bar) {
+        cp_commit();
+        if (n_waiting == 2) {
+            cp_wait<2>();
+            signal(waiting[0]);
+            waiting[0] = waiting[1];
+            waiting[1] = bar;
+        } else {
+            waiting[n_waiting++] = bar;
+        }
+    }
+    __device__ __forceinline__ void await(uint64_t* bar, uint32_t parity) {
+        if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity & 1u))) return;
+        flush();             // nobody frees anything before it has what is on its way
+        alive = warp_wait(bar, parity, abort) && alive;
+    }
+    // 128 keys x kCols columns; at: this lane's key's row of the cache, -1: zeros
+    __device__ __forceinline__ void stage(const void* cache, long long at, int part, bool check, uint32_t* odd) {
+        const uint32_t s = fill % C::kStages, phase = fill / C::kStages;
+        await(&sm.bars.empty[s], phase + 1);     // parity of the phase before: passes at once the first time
+        if (!alive) return;
+        const uint32_t dst = smem_u32(sm.ring) + s * C::kStage;
+        const int c = lane % kChunks, r0 = lane / kChunks;
+        const int col = part * C::kCols + c * 8;
+        const bool in = col < a.dh;
+        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(cache) + col;
+        // block of 64 columns, row of 128 bytes, chunk of 16 turned by the row
+        const uint32_t to = dst + (c >> 3) * (kTile * 128) + warp * 32 * 128;
+#pragma unroll
+        for (int i = 0; i < 32 / kAtOnce; ++i) {
+            const int r = i * kAtOnce + r0;
+            const long long from = __shfl_sync(0xffffffffu, at, r);
+            if (in) cp_async16(to + r * 128 + (((c & 7) ^ (r & 7)) << 4), from >= 0 ? src + from : src, from >= 0);
+        }
+        const uint32_t bar = smem_u32(&sm.bars.full[s]);
+        ++fill;
+        if (!check) {
+            issued(bar);
+            return;
+        }
+        // values of a tile that not every row sees: rows that hold a NaN or an infinity become zeros, and are told
+        cp_commit();
+        flush();
+        uint32_t mine = 0;
+#pragma unroll 4
+        for (int i = 0; i < 32 / kAtOnce; ++i) {
+            const int r = i * kAtOnce + r0;
+            uint4 v;
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(to + r * 128 + (((c & 7) ^ (r & 7)) << 4)));
+            if (in && (odd_word(v.x) || odd_word(v.y) || odd_word(v.z) || odd_word(v.w))) mine |= 1u << r;
+        }
+        mine = __reduce_or_sync(0xffffffffu, mine);
+        if (mine) {
+            for (int i = 0; i < 32 / kAtOnce; ++i) {
+                const int r = i * kAtOnce + r0;
+                if (in && (mine >> r & 1u))
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(to + r * 128 + (((c & 7) ^ (r & 7)) << 4)), "r"(0) : "memory");
+            }
+        }
+        if (lane == 0) odd[warp] = mine;
+        signal(bar);
+    }
+    __device__ __forceinline__ void queries(const Walk<C::kRows, kTile>& w, uint32_t piece) {
+        await(&sm.bars.q_empty, piece + 1);
+        if (!alive) return;
+        constexpr int kOwn = C::kRows / 4, kWide = DP / 8, kRowsAtOnce = 32 / kWide;      // rows of a warp
+#pragma unroll
+        for (int i = lane; i < kOwn; i += 32) {
+            const Row r = row_at<C::kRows>(a, w.r, w.kvh, w.rb, warp * kOwn + i);
+            sm.q_row[warp * kOwn + i] = r.there ? static_cast<long long>(r.token) * a.q_stride + static_cast<long long>(r.head) * a.dh : -1;
+        }
+        __syncwarp();
+        const int c = lane % kWide, r0 = lane / kWide;
+        const bool in = c * 8 < a.dh;
+        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + c * 8;
+        const uint32_t dst = smem_u32(sm.q) + (c >> 3) * (128 * 128) + ((c & 7) << 4);
+#pragma unroll 4
+        for (int i = 0; i < kOwn / kRowsAtOnce; ++i) {
+            const int r = warp * kOwn + i * kRowsAtOnce + r0;
+            const long long from = sm.q_row[r];
+            if (in) cp_async16((dst + (r >> 7) * C::kQTile + (r & 127) * 128) ^ ((r & 7) << 4), from >= 0 ? src + from : src, from >= 0);
+        }
+        __syncwarp();      // q_row may be written again
+        issued(smem_u32(&sm.bars.q_full));
+    }
+    __device__ void run(Walk<C::kRows, kTile> w) {
+        bool bad = false;
+        uint32_t tile = 0, piece = 0;
+        while (w.left > 0 && alive) {
+            const Piece<DP> p(a, w);
+            const auto page_of = [&](int j) {     // of this lane's key of the j-th tile
+                const int at = (w.t0 + j) * kTile + warp * 32 + lane;
+                if (j >= p.n || at >= w.reach) return -1;
+                return ldg_waited(a.table + static_cast<long long>(w.s) * a.max_pages + (a.page_shift >= 0 ? at >> a.page_shift : at / a.page_size));
+            };
+            int page = page_of(0);
+            for (int j = 0; j < p.n && alive; ++j, ++tile) {
+                const int next = page_of(j + 1);
+                const int pos = (w.t0 + j) * kTile + warp * 32 + lane;
+                const bool in = pos < w.reach, ok = in && page >= 0 && page < a.n_pages;
+                bad |= in && !ok;
+                const int in_page = a.page_shift >= 0 ? pos & (a.page_size - 1) : pos % a.page_size;
+                const long long at = ok ? static_cast<long long>(page) * a.page_stride + (static_cast<long long>(w.kvh) * a.page_size + in_page) * a.dh : -1;
+                const uint32_t there = __ballot_sync(0xffffffffu, ok);
+                // the slot's last readers are done: their P went into a product behind which K stages were freed for this tile
+                if (lane == 0) sm.flags.there[tile % kFlags][warp] = there;
+                const bool check = p.partial(w.t0 + j);
+#pragma unroll
+                for (int h = 0; h < C::kParts; ++h) stage(a.K, at, h, false, nullptr);
+#pragma unroll
+                for (int h = 0; h < C::kParts; ++h) stage(a.V, at, h, check, sm.flags.odd[tile % kFlags][h]);
+                if (j == 0) queries(w, piece++);
+                page = next;
+            }
+            w.next(a);
+        }
+        flush();
+        if (__any_sync(0xffffffffu, bad) && lane == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
+    }
+};
+
+// ---- products -------------------------------------------------------------------------------------------------------------------
+
+template <int DP>
+__device__ void issue_products(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, kTile> w) {
+    using C = Cfg<DP>;
+    Bars& bars = sm.bars;
+    int* abort = &bars.abort;
+    const uint32_t tmem = bars.tmem, q0 = smem_u32(sm.q), ring = smem_u32(sm.ring);
+    // a negative scale: -Q instead, so that the largest score stays the largest product
+    const uint32_t idesc_s = umma_idesc_bf16(128, kTile, false) | (a.scale_log2 < 0.0f ? 1u << 13 : 0u);
+    uint32_t first_fill = 0, piece = 0, use[2] = {0, 0};
+    while (w.left > 0) {
+        const Piece<DP> p(a, w);
+        if (p.n > 0) {
+            if (!wait(&bars.q_full, piece++, abort)) return;      // from here on piece counts from 1
+            const auto scores = [&](int t, int j) {
+                const int b = p.buffer(t, j);
+                // S lies where the P of the buffer's last tile was read from
+                if (use[b] > 0 && !wait(&bars.pv_done[b], use[b] - 1, abort)) return false;
+#pragma unroll
+                for (int h = 0; h < C::kParts; ++h) {
+                    const uint32_t f = first_fill + j * 2 * C::kParts + h, s = f % C::kStages;
+                    if (!wait(&bars.full[s], f / C::kStages, abort)) return false;
+                    tcgen05_fence_after_sync();
+                    const int steps = min(a.dh - h * C::kCols, C::kCols) / 16;
+                    for (int k = 0; k < steps; ++k) {
+                        const uint32_t block = (k >> 2) * (128 * 128) + (k & 3) * 32;
+                        umma_bf16(tmem + b * 128, umma_smem_desc(q0 + t * C::kQTile + h * (C::kCols / 64) * (128 * 128) + block, 16, 1024),
+                                  umma_smem_desc(ring + s * C::kStage + block, 16, 1024), idesc_s, h > 0 || k > 0);
+                    }
+                    if (t == p.streams - 1) umma_commit(&bars.empty[s]);
+                }
+                umma_commit(&bars.s_full[b]);
+                ++use[b];
+                if (t == p.streams - 1 && j == p.n - 1) umma_commit(&bars.q_empty);
+                return true;
+            };
+            const auto sums = [&](int t, int j) {
+                const int b = p.buffer(t, j);
+                if (!wait(&bars.p_full[b], use[b] - 1, abort)) return false;
+                tcgen05_fence_after_sync();
+                const bool on_top = j > 0 || *reinterpret_cast<volatile uint32_t*>(&bars.o_set[t]) == piece;
+#pragma unroll
+                for (int h = 0; h < C::kParts; ++h) {
+                    const uint32_t f = first_fill + (j * 2 + 1) * C::kParts + h, s = f % C::kStages;
+                    if (!wait(&bars.full[s], f / C::kStages, abort)) return false;
+                    tcgen05_fence_after_sync();
+                    const uint32_t idesc = umma_idesc_bf16(128, min(a.dh - h * C::kCols, C::kCols), true);
+#pragma unroll
+                    for (int k = 0; k < kTile / 16; ++k)
+                        umma_ts(tmem + C::kO + t * DP + h * C::kCols, tmem + b * 128 + k * 8,
+                                umma_smem_desc(ring + s * C::kStage + k * 2048, kTile * 128, 1024), idesc, on_top || k > 0);
+                    if (t == p.streams - 1) umma_commit(&bars.empty[s]);
+                }
+                umma_commit(&bars.pv_done[b]);
+                return true;
+            };
+            if (p.streams == 2) {
+                if (p.tiles[0] > 0 && !scores(0, 0)) return;
+                if (!scores(1, 0)) return;
+                for (int j = 0; j < p.n; ++j) {
+                    if (j < p.tiles[0] && !sums(0, j)) return;
+                    if (j + 1 < p.tiles[0] && !scores(0, j + 1)) return;
+                    if (!sums(1, j)) return;
+                    if (j + 1 < p.n && !scores(1, j + 1)) return;
+                }
+            } else {
+                if (!scores(0, 0)) return;
+                if (p.n > 1 && !scores(0, 1)) return;
+                for (int j = 0; j < p.n; ++j) {
+                    if (!sums(0, j)) return;
+                    if (j + 2 < p.n && !scores(0, j + 2)) return;
+                }
+            }
+            first_fill += p.n * 2 * C::kParts;
+        }
+        w.next(a);
+    }
+}
+
+// ---- rows -----------------------------------------------------------------------------------------------------------------------
+
+// The value rows that were taken out of a tile's stage, for the rows that see them: O += p * v, before the tile's product.
+template <int DP>
+__device__ __noinline__ void add_odd_rows(const Args& a, const Smem<DP>& sm, int s, int kvh, int p0, int sees, uint32_t slot, uint32_t p_addr, uint32_t o_addr) {
+    using C = Cfg<DP>;
+    for (int h = 0; h < C::kParts; ++h)
+        for (int q = 0; q < 4; ++q) {
+            uint32_t left = sm.flags.odd[slot][h][q];
+            while (left) {
+                const int i = q * 32 + __ffs(left) - 1;
+                left &= left - 1;
+                const uint32_t pair = tmem_ld_word(p_addr + i / 2);
+                tmem_ld_wait();
+                const float p = __uint_as_float(i & 1 ? pair & 0xffff0000u : pair << 16);
+                const int at = p0 + i, pi = at / a.page_size;
+                const int page = ldg_waited(a.table + static_cast<long long>(s) * a.max_pages + pi);
+                const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.V) + static_cast<long long>(page) * a.page_stride +
+                                         (static_cast<long long>(kvh) * a.page_size + (at - pi * a.page_size)) * a.dh;
+                for (int c = h * C::kCols; c < min(a.dh, (h + 1) * C::kCols); c += 16) {
+                    uint32_t o[16];
+                    tmem_ld_32x16(o_addr + c, o);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (at < sees) o[e] = __float_as_uint(fmaf(p, a.K_scale ? __uint_as_float(0x7fc00000u) : __bfloat162float(v[c + e]), __uint_as_float(o[e])));
+                    tmem_st_32x16(o_addr + c, o);
+                    tmem_st_wait();
+                }
+            }
+        }
+}
+
+template <int DP>
+__device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, kTile> w, long long total) {
+    using C = Cfg<DP>;
+    constexpr float kSlack = 8.0f;      // powers of two that a maximum may lag behind
+    Bars& bars = sm.bars;
+    int* abort = &bars.abort;
+    const int t = threadIdx.x >> 7, i = threadIdx.x & 127, lane = threadIdx.x & 31, item_row = t * 128 + i;
+    const uint32_t lanes = bars.tmem + (static_cast<uint32_t>(i & ~31) << 16);
+    const uint32_t o_addr = lanes + C::kO + t * DP;
+    const float scale = fabsf(a.scale_log2);
+    const long long range = w.left;
+    uint32_t tile = 0, piece = 0, use[2] = {0, 0};
+    bool alive = true;
+    while (w.left > 0 && alive) {
+        const Piece<DP> p(a, w);
+        if (p.n > 0) ++piece;
+        if (t < p.streams) {
+            const Row row = row_at<C::kRows>(a, w.r, w.kvh, w.rb, item_row);
+            const int first = w.r.len - w.r.n + 1, n = p.tiles[t];
+            const int sees = first + row.token - w.r.first;      // kept or not
+            const int all_see = first + static_cast<int>((static_cast<long long>(w.rb) * C::kRows + t * 128) / a.G);
+            float m = -INFINITY, l = 0.0f;
+            uint32_t used[2] = {use[0], use[1]};
+            const auto await_sums = [&](int j) {      // of tile j, the last one that was counted in its buffer
+                const int b = p.buffer(t, j);
+                alive = warp_wait(&bars.pv_done[b], used[b] - 1, abort);
+                tcgen05_fence_after_sync();
+            };
+            for (int j = 0; j < n && alive; ++j) {
+                const int b = p.buffer(t, j), p0 = (w.t0 + j) * kTile;
+                const uint32_t slot = (tile + j) % kFlags, fill = (tile + j) * 2 * C::kParts;
+                alive = warp_wait(&bars.s_full[b], used[b], abort) && warp_wait(&bars.full[fill % C::kStages], fill / C::kStages, abort);
+                if (!alive) break;
+                tcgen05_fence_after_sync();
+                const uint32_t s_addr = lanes + b * 128;
+                uint32_t sc[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld_32x32(s_addr + c * 32, sc[c]);
+                uint32_t there[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) there[c] = *const_cast<volatile const uint32_t*>(&sm.flags.there[slot][c]);
+                tmem_ld_wait();
+                if (p0 + kTile > all_see || (there[0] & there[1] & there[2] & there[3]) != 0xffffffffu) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int left = sees - p0 - c * 32;
+                        const uint32_t in = left >= 32 ? there[c] : left <= 0 ? 0u : there[c] & ((1u << left) - 1u);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (!(in >> e & 1u)) sc[c][e] = 0xff800000u;
+                    }
+                }
+                float mx = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) mx = fmaxf(mx, __uint_as_float(sc[c][e]));
+                if (__any_sync(0xffffffffu, (mx - m) * scale > kSlack)) {
+                    const float to = fmaxf(m, mx), f = m == -INFINITY ? 0.0f : pow2((m - to) * scale);
+                    if (j > 0) {
+                        await_sums(j - 1);
+                        if (!alive) break;
+                        for (int c = 0; c < a.dh; c += 16) {
+                            uint32_t o[16];
+                            tmem_ld_32x16(o_addr + c, o);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            tmem_st_32x16(o_addr + c, o);
+                        }
+                    }
+                    l *= f;
+                    m = to;
+                }
+                const float base = m == -INFINITY ? 0.0f : m * scale;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float x = pow2(fmaf(__uint_as_float(sc[c][2 * e]), scale, -base));
+                        const float y = pow2(fmaf(__uint_as_float(sc[c][2 * e + 1]), scale, -base));
+                        l += x + y;
+                        pk[e] = pack_bf16(x, y);
+                    }
+                    tmem_st_32x16(s_addr + c * 16, pk);
+                }
+                tmem_st_wait();
+                if (p.partial(w.t0 + j)) {
+                    uint32_t odd = 0;
+#pragma unroll
+                    for (int h = 0; h < C::kParts; ++h) {
+                        const uint32_t f = fill + C::kParts + h;
+                        alive = warp_wait(&bars.full[f % C::kStages], f / C::kStages, abort) && alive;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) odd |= *const_cast<volatile const uint32_t*>(&sm.flags.odd[slot][h][q]);
+                    }
+                    if (odd && alive) {
+                        if (j > 0) {
+                            await_sums(j - 1);
+                            if (!alive) break;
+                        } else {
+                            const uint32_t zero[16] = {};
+                            for (int c = 0; c < a.dh; c += 16) tmem_st_32x16(o_addr + c, zero);
+                            tmem_st_wait();
+                            *const_cast<volatile uint32_t*>(&bars.o_set[t]) = piece;
+                        }
+                        add_odd_rows<DP>(a, sm, w.s, w.kvh, p0, sees, slot, s_addr, o_addr);
+                    }
+                }
+                ++used[b];
+                tcgen05_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.p_full[b]);
+            }
+            if (n > 0 && alive) await_sums(n - 1);
+            if (!alive) break;
+            const bool some = l != 0.0f && row.kept;
+            if (w.complete()) {
+                const long long at = static_cast<long long>(row.token) * a.H + row.head;
+                const float f = some ? 1.0f / l : 0.0f;
+                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + at * a.dh;
+                for (int c = 0; c < a.dh; c += 16) {
+                    uint32_t o[16];
+                    if (n > 0) {
+                        tmem_ld_32x16(o_addr + c, o);
+                        tmem_ld_wait();
+                    }
+                    if (row.there) {
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            uint32_t y[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                y[e] = some ? pack_bf16(__uint_as_float(o[8 * q + 2 * e]) * f, __uint_as_float(o[8 * q + 2 * e + 1]) * f) : 0u;
+                            *reinterpret_cast<uint4*>(out + c + 8 * q) = make_uint4(y[0], y[1], y[2], y[3]);
+                        }
+                    }
+                }
+                if (row.there && a.lse) a.lse[at] = some ? (m * scale + log2f(l)) * kLn2 : -INFINITY;
+            } else {
+                float* slot = a.ws + (static_cast<long long>(blockIdx.x) * 2 + (w.left == range ? 0 : 1)) * a.slot;
+                if (row.there) {
+                    slot[item_row] = m * scale;
+                    slot[a.rows + item_row] = l;
+                }
+                for (int c = 0; c < a.dh; c += 16) {
+                    uint32_t o[16] = {};
+                    if (n > 0) {
+                        tmem_ld_32x16(o_addr + c, o);
+                        tmem_ld_wait();
+                    }
+                    if (row.there) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            reinterpret_cast<uint4*>(slot + 2 * a.rows)[static_cast<long long>(c / 4 + q) * a.rows + item_row] =
+                                make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+                    }
+                }
+            }
+        }
+        if (threadIdx.x == 0 && w.left == w.t1 - w.t0)   // the range's last piece
+            a.openings[blockIdx.x] = {w.t0 == 0 && w.t1 < w.nt, w.s, w.kvh, w.rb, w.nt - w.t1, w.left == range, total};
+        tile += p.n;
+        use[0] += p.uses(0);
+        use[1] += p.uses(1);
+        w.next(a);
+    }
+}
+
+template <int DP>
+__global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __grid_constant__ Args a) {
+    using C = Cfg<DP>;
+    extern __shared__ __align__(1024) unsigned char raw[];
+    Smem<DP>& sm = *reinterpret_cast<Smem<DP>*>(raw);
+    Bars& bars = sm.bars;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    chain_wait();
+    const Found<C::kRows, kTile> f = locate<C::kRows, kTile, kThreads>(a, sm.sh);
+    if (f.walk.left <= 0) {      // the same in every thread
+        if (f.total == 0 && blockIdx.x == 0 && tid == 0) a.openings[0] = {0, 0, 0, 0, 0, 0, 0};
+        return;
+    }
+    if (tid == 0) {
+        for (int i = 0; i < C::kStages; ++i) {
+            mbar_init(&bars.full[i], 4);      // the gathering warps
+            mbar_init(&bars.empty[i], 1);
+        }
+        mbar_init(&bars.q_full, 4);
+        mbar_init(&bars.q_empty, 1);
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&bars.s_full[b], 1);
+            mbar_init(&bars.p_full[b], 4);    // a stream's warps
+            mbar_init(&bars.pv_done[b], 1);
+            bars.o_set[b] = 0;
+        }
+        bars.abort = 0;
+        mbar_fence_init();
+    }
+    if (warp == 12) {
+        tmem_alloc(&bars.tmem, 512);
+        tmem_relinquish_alloc_permit();
+    }
+    tcgen05_fence_before_sync();
+    __syncthreads();
+    tcgen05_fence_after_sync();
+    if (warp < 8) {
+        more_registers<kRowRegs>();
+        softmax_rows<DP>(a, sm, f.walk, f.total);
+    } else if (warp < 12) {
+        fewer_registers<kCopyRegs>();
+        Gather<DP>(a, sm).run(f.walk);
+    } else {
+        fewer_registers<kIssueRegs>();
+        if (warp == 12 && lane == 0) issue_products<DP>(a, sm, f.walk);
+    }
+    __syncwarp();
+    tcgen05_fence_before_sync();
+    __syncthreads();
+    if (warp == 12) {
+        tcgen05_fence_after_sync();
+        tmem_dealloc(bars.tmem, 512);
+    }
+    if (tid == 0 && bars.abort) flag_status(a.status, HALO_DEV_TIMEOUT);
+}
+
+template <int DP>
+int blocks_of(const halo_paged_shape& sh, int n_tok, int n_seq) {
+    const long long G = sh.n_heads / sh.n_kv_heads, cap = static_cast<long long>(sh.max_pages) * sh.page_size;
+    const long long items = (n_tok * G / Cfg<DP>::kRows + (n_seq < n_tok ? n_seq : n_tok) + 1) * sh.n_kv_heads;
+    const long long pieces = items * ((cap + kTile - 1) / kTile) / kMinTiles;
+    return static_cast<int>(pieces < 1 ? 1 : pieces < kSmCount ? pieces : kSmCount);
+}
+template <typename F>
+auto by_width(const halo_paged_shape& sh, F f) {
+    return sh.head_dim <= 64    ? f(std::integral_constant<int, 64>())
+           : sh.head_dim <= 128 ? f(std::integral_constant<int, 128>())
+                                : f(std::integral_constant<int, 256>());
+}
+bool tensor_cores(const halo_paged_shape& sh, bool eight) { return sh.dtype == HALO_BF16 && !eight; }
+
+size_t workspace(const halo_paged_shape& sh, int n_tok, int n_seq) {
+    return by_width(sh, [&](auto dp) {
+        constexpr int DP = decltype(dp)::value;
+        return static_cast<size_t>(blocks_of<DP>(sh, n_tok, n_seq)) *
+               (sizeof(Opening) + 2 * sizeof(float) * slot_floats(slot_rows(Cfg<DP>::kRows, n_tok, sh), sh.head_dim));
+    });
+}
+halo_status launch(const Args& args, const halo_paged_shape& sh, void* ws, cudaStream_t st) {
+    return by_width(sh, [&](auto dp) -> halo_status {
+        constexpr int DP = decltype(dp)::value;
+        static bool done[64];
+        if (!ensure_dynamic_smem(paged_prompt_mha_kernel<DP>, sizeof(Smem<DP>), done)) return HALO_ERR_CUDA;
+        Args a = args;
+        a.blocks = blocks_of<DP>(sh, a.n_tok, a.n_seq);
+        a.rows = slot_rows(Cfg<DP>::kRows, a.n_tok, sh);
+        a.slot = slot_floats(a.rows, a.dh);
+        a.openings = static_cast<Opening*>(ws);
+        a.ws = reinterpret_cast<float*>(a.openings + a.blocks);
+        const halo_status rc = launch_chained(paged_prompt_mha_kernel<DP>, a.blocks, kThreads, sizeof(Smem<DP>), st, a);
+        return rc != HALO_OK ? rc : launch_join<__nv_bfloat16, Cfg<DP>::kRows>(a, st);
+    });
+}
+
+}  // namespace
+}  // namespace prompt
 }  // namespace halo
 
 using namespace halo;
 
 extern "C" size_t halo_paged_prompt_mha_workspace_bytes(const halo_paged_shape* shape, int n_tok, int n_seq) {
     if (check_paged_shape(shape) != HALO_OK || n_seq <= 0 || n_seq > HALO_MAX_SEQUENCES || n_tok <= 0 || n_tok > HALO_MAX_PROMPT_ROWS) return 0;
-    return prompt::f32_workspace(*shape, n_tok, n_seq);
+    const size_t rows = prompt::f32_workspace(*shape, n_tok, n_seq);
+    if (shape->dtype == HALO_F32) return rows;
+    const size_t ts = prompt::workspace(*shape, n_tok, n_seq);
+    return rows > ts ? rows : ts;
 }
 
 extern "C" halo_status halo_paged_prompt_mha(const halo_paged_shape* shape, int n_tok, int n_seq, const void* q, long long q_stride,
@@ -50,6 +721,7 @@ extern "C" halo_status halo_paged_prompt_mha(const halo_paged_shape* shape, int 
     a.page_stride = paged_stride(*shape);
     a.q_stride = q_stride;
     a.scale_log2 = scale * 1.44269504088896340736f;
+    if (a.scale_log2 == 0.0f) a.scale_log2 = 1.0e-45f;      // scores of zero, and -infinity for what is not seen
     a.q = q;
     a.K = K_cache;
     a.V = V_cache;
@@ -62,5 +734,6 @@ extern "C" halo_status halo_paged_prompt_mha(const halo_paged_shape* shape, int 
     a.out = out;
     a.lse = lse;
     a.status = dev_status;
-    return prompt::f32_launch(a, *shape, workspace, static_cast<cudaStream_t>(stream));
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return prompt::tensor_cores(*shape, K_scale != nullptr) ? prompt::launch(a, *shape, workspace, st) : prompt::f32_launch(a, *shape, workspace, st);
 }

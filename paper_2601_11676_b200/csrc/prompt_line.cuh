@@ -25,7 +25,8 @@ struct __align__(16) Opening {
 struct Args {
     int n_tok, n_seq, H, Hk, G, dh, page_size, page_shift, n_pages, max_pages;   // page_shift: -1 = no power of two
     int blocks;              // thread blocks of the first kernel
-    long long slot;          // floats of a workspace slot
+    int rows;                // rows of a workspace slot
+    long long slot;          // floats of it
     long long page_stride, q_stride;
     float scale_log2;
     const void* q;
@@ -46,7 +47,12 @@ struct Args {
 
 constexpr float kLn2 = 0.693147180559945309f;
 
-// A slot: maxima [ROWS], sums [ROWS], weighted sums [dh / 4][ROWS][4]: neighbouring rows side by side, as threads hold them.
+// A slot: maxima [rows], sums [rows], weighted sums [dh / 4][rows][4]: neighbouring rows side by side, as threads hold them.  rows
+// is what an item can have.
+inline int slot_rows(int item_rows, int n_tok, const halo_paged_shape& sh) {
+    const long long all = static_cast<long long>(n_tok) * (sh.n_heads / sh.n_kv_heads);
+    return all < item_rows ? static_cast<int>((all + 3) / 4 * 4) : item_rows;
+}
 __host__ __device__ constexpr long long slot_floats(int rows, int dh) { return static_cast<long long>(rows) * (dh + 2); }
 
 // 2^x, results below 2^-126 as 0
@@ -293,8 +299,8 @@ __global__ void __launch_bounds__(256) paged_prompt_join_kernel(const __grid_con
             const bool there = k0 + e < pieces;
             const float* p = k0 + e == 0 ? ws0 : ws1 + static_cast<long long>(k0 + e) * 2 * a.slot;
             m[e] = there ? __ldcg(p + row) : -INFINITY;
-            l[e] = there ? __ldcg(p + ROWS + row) : 0.0f;
-            x[e] = there ? __ldcg(reinterpret_cast<const float4*>(p + 2 * ROWS) + c4 * ROWS + row) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            l[e] = there ? __ldcg(p + a.rows + row) : 0.0f;
+            x[e] = there ? __ldcg(reinterpret_cast<const float4*>(p + 2 * a.rows) + static_cast<long long>(c4) * a.rows + row) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
 #pragma unroll
         for (int e = 0; e < kAhead; ++e) {
