@@ -52,8 +52,12 @@ struct Flags {
     uint32_t there[kFlags][4];       // which of a tile's keys are there
     uint32_t odd[kFlags][2][4];      // which of a tile's value rows were taken out, per part
 };
+// S, P and O of a tile hand over through barriers of the lane that it is in: a stream's own in items of two streams, 0 and 2 in
+// turn in items of one.  Lanes 1 and 2 share the buffer behind 0, but not the warps that wait: 1 belongs to the second stream's,
+// 0 and 2 to the first's, so that nobody waits for a phase of a barrier without having seen the one before it.
+constexpr int kLanes = 3;
 struct Bars {
-    uint64_t full[8], empty[8], q_full, q_empty, s_full[2], p_full[2], pv_done[2];
+    uint64_t full[8], empty[8], q_full, q_empty, s_full[kLanes], p_full[kLanes], pv_done[kLanes];
     uint32_t tmem;
     int abort;
     uint32_t o_set[2];               // the last piece whose O held something before its first product, per stream
@@ -141,9 +145,9 @@ struct Piece {
     }
     // whether some row does not see all of the tile
     __device__ __forceinline__ bool partial(int tile) const { return (tile + 1) * kTile > sees_first; }
-    // buffer of tile j of a stream
-    __device__ __forceinline__ int buffer(int stream, int j) const { return streams == 2 ? stream : j & 1; }
-    __device__ __forceinline__ uint32_t uses(int buffer) const { return streams == 2 ? tiles[buffer] : (n + 1 - buffer) / 2; }
+    // lane of tile j of a stream; its buffer of S and P
+    __device__ __forceinline__ int lane(int stream, int j) const { return streams == 2 ? stream : (j & 1) * 2; }
+    static __device__ __forceinline__ int buffer(int lane) { return lane != 0; }
 };
 
 // ---- gathering ------------------------------------------------------------------------------------------------------------------
@@ -306,15 +310,17 @@ __device__ void issue_products(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows,
     const uint32_t tmem = bars.tmem, q0 = smem_u32(sm.q), ring = smem_u32(sm.ring);
     // a negative scale: -Q instead, so that the largest score stays the largest product
     const uint32_t idesc_s = umma_idesc_bf16(128, kTile, false) | (a.scale_log2 < 0.0f ? 1u << 13 : 0u);
-    uint32_t first_fill = 0, piece = 0, use[2] = {0, 0};
+    uint32_t first_fill = 0, piece = 0, use[kLanes] = {0, 0, 0};
+    int last[2] = {0, 1};      // lane that a buffer was used in last
     while (w.left > 0) {
         const Piece<DP> p(a, w);
         if (p.n > 0) {
             if (!wait(&bars.q_full, piece++, abort)) return;      // from here on piece counts from 1
             const auto scores = [&](int t, int j) {
-                const int b = p.buffer(t, j);
+                const int b = p.lane(t, j), buffer = p.buffer(b);
                 // S lies where the P of the buffer's last tile was read from
-                if (use[b] > 0 && !wait(&bars.pv_done[b], use[b] - 1, abort)) return false;
+                if (use[last[buffer]] > 0 && !wait(&bars.pv_done[last[buffer]], use[last[buffer]] - 1, abort)) return false;
+                last[buffer] = b;
 #pragma unroll
                 for (int h = 0; h < C::kParts; ++h) {
                     const uint32_t f = first_fill + j * 2 * C::kParts + h, s = f % C::kStages;
@@ -323,18 +329,19 @@ __device__ void issue_products(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows,
                     const int steps = min(a.dh - h * C::kCols, C::kCols) / 16;
                     for (int k = 0; k < steps; ++k) {
                         const uint32_t block = (k >> 2) * (128 * 128) + (k & 3) * 32;
-                        umma_bf16(tmem + b * 128, umma_smem_desc(q0 + t * C::kQTile + h * (C::kCols / 64) * (128 * 128) + block, 16, 1024),
+                        umma_bf16(tmem + buffer * 128, umma_smem_desc(q0 + t * C::kQTile + h * (C::kCols / 64) * (128 * 128) + block, 16, 1024),
                                   umma_smem_desc(ring + s * C::kStage + block, 16, 1024), idesc_s, h > 0 || k > 0);
                     }
                     if (t == p.streams - 1) umma_commit(&bars.empty[s]);
                 }
                 umma_commit(&bars.s_full[b]);
+                mbar_arrive(&bars.s_full[b]);      // what this thread has seen of the gathering warps, the tile's flags among it
                 ++use[b];
                 if (t == p.streams - 1 && j == p.n - 1) umma_commit(&bars.q_empty);
                 return true;
             };
             const auto sums = [&](int t, int j) {
-                const int b = p.buffer(t, j);
+                const int b = p.lane(t, j);
                 if (!wait(&bars.p_full[b], use[b] - 1, abort)) return false;
                 tcgen05_fence_after_sync();
                 const bool on_top = j > 0 || *reinterpret_cast<volatile uint32_t*>(&bars.o_set[t]) == piece;
@@ -346,7 +353,7 @@ __device__ void issue_products(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows,
                     const uint32_t idesc = umma_idesc_bf16(128, min(a.dh - h * C::kCols, C::kCols), true);
 #pragma unroll
                     for (int k = 0; k < kTile / 16; ++k)
-                        umma_ts(tmem + C::kO + t * DP + h * C::kCols, tmem + b * 128 + k * 8,
+                        umma_ts(tmem + C::kO + t * DP + h * C::kCols, tmem + p.buffer(b) * 128 + k * 8,
                                 umma_smem_desc(ring + s * C::kStage + k * 2048, kTile * 128, 1024), idesc, on_top || k > 0);
                     if (t == p.streams - 1) umma_commit(&bars.empty[s]);
                 }
@@ -420,7 +427,7 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
     const uint32_t o_addr = lanes + C::kO + t * DP;
     const float scale = fabsf(a.scale_log2);
     const long long range = w.left;
-    uint32_t tile = 0, piece = 0, use[2] = {0, 0};
+    uint32_t tile = 0, piece = 0, used[kLanes] = {0, 0, 0};      // of the lanes of this stream
     bool alive = true;
     while (w.left > 0 && alive) {
         const Piece<DP> p(a, w);
@@ -431,19 +438,18 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
             const int sees = first + row.token - w.r.first;      // kept or not
             const int all_see = first + static_cast<int>((static_cast<long long>(w.rb) * C::kRows + t * 128) / a.G);
             float m = -INFINITY, l = 0.0f;
-            uint32_t used[2] = {use[0], use[1]};
-            const auto await_sums = [&](int j) {      // of tile j, the last one that was counted in its buffer
-                const int b = p.buffer(t, j);
+            const auto await_sums = [&](int j) {      // of tile j, the last one that was counted in its lane
+                const int b = p.lane(t, j);
                 alive = warp_wait(&bars.pv_done[b], used[b] - 1, abort);
                 tcgen05_fence_after_sync();
             };
             for (int j = 0; j < n && alive; ++j) {
-                const int b = p.buffer(t, j), p0 = (w.t0 + j) * kTile;
+                const int b = p.lane(t, j), p0 = (w.t0 + j) * kTile;
                 const uint32_t slot = (tile + j) % kFlags, fill = (tile + j) * 2 * C::kParts;
-                alive = warp_wait(&bars.s_full[b], used[b], abort) && warp_wait(&bars.full[fill % C::kStages], fill / C::kStages, abort);
+                alive = warp_wait(&bars.s_full[b], used[b], abort);
                 if (!alive) break;
                 tcgen05_fence_after_sync();
-                const uint32_t s_addr = lanes + b * 128;
+                const uint32_t s_addr = lanes + p.buffer(b) * 128;
                 uint32_t sc[4][32];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld_32x32(s_addr + c * 32, sc[c]);
@@ -500,7 +506,7 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
                 if (p.partial(w.t0 + j)) {
                     uint32_t odd = 0;
 #pragma unroll
-                    for (int h = 0; h < C::kParts; ++h) {
+                    for (int h = 0; h < C::kParts; ++h) {      // the stage is not filled again before this tile's products
                         const uint32_t f = fill + C::kParts + h;
                         alive = warp_wait(&bars.full[f % C::kStages], f / C::kStages, abort) && alive;
 #pragma unroll
@@ -573,8 +579,6 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
         if (threadIdx.x == 0 && w.left == w.t1 - w.t0)   // the range's last piece
             a.openings[blockIdx.x] = {w.t0 == 0 && w.t1 < w.nt, w.s, w.kvh, w.rb, w.nt - w.t1, w.left == range, total};
         tile += p.n;
-        use[0] += p.uses(0);
-        use[1] += p.uses(1);
         w.next(a);
     }
 }
@@ -599,12 +603,12 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __g
         }
         mbar_init(&bars.q_full, 4);
         mbar_init(&bars.q_empty, 1);
-        for (int b = 0; b < 2; ++b) {
-            mbar_init(&bars.s_full[b], 1);
+        for (int b = 0; b < kLanes; ++b) {
+            mbar_init(&bars.s_full[b], 2);    // the products, and the thread that issues them
             mbar_init(&bars.p_full[b], 4);    // a stream's warps
             mbar_init(&bars.pv_done[b], 1);
-            bars.o_set[b] = 0;
         }
+        bars.o_set[0] = bars.o_set[1] = 0;
         bars.abort = 0;
         mbar_fence_init();
     }

@@ -196,6 +196,13 @@ def test_items_that_are_cut_and_joined(kind, H, Hk, dh, chunks):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("H,Hk,dh", [(32, 32, 128), (32, 16, 64), (8, 8, 256)])
+def test_long_and_short_items_in_turn(kind, H, Hk, dh):
+    """A thread block goes from items of a few rows to items of many and back."""
+    Case(kind, H, Hk, dh, 32, [(1, 345), (300, 200), (2, 700), (290, 10), (100, 600), (257, 3), (40, 900), (513, 0)]).check()
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_many_sequences(kind):
     """More sequences than a thread block has threads; one-token chunks and empty ones among them."""
     n = np.random.default_rng(3).integers(0, 4, 700).tolist()
