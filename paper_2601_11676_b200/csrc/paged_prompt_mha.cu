@@ -2,8 +2,9 @@
 // (tcgen05).  Bound by them for prompts (4 flops per row, key and column of the head), by HBM for a few rows over a long cache.
 //
 // Per thread block, one to an SM:
-//   - warps 8 to 11 gather K and V rows of 128 keys from their pages into a ring of stages (cp.async; 128 keys x 128 columns a
-//     stage, in the 128-byte swizzle that the tensor cores read), and an item's rows of Q;
+//   - warps 8 to 11 gather K and V rows of 128 keys from their pages into a ring of stages (128 keys x 128 columns a stage, in the
+//     128-byte swizzle that the tensor cores read) and an item's rows of Q: boxes of a page's rows by the copy engine, or, where
+//     pages are no whole number of eight rows, row by row;
 //   - one thread of warp 12 issues the products: S = Q K^T into tensor memory, O += P V with P in tensor memory;
 //   - warps 0 to 3 and 4 to 7 take a row per thread: running maximum and sum, P = 2^(S scale - maximum) as bf16 in place of S.
 // An item has 256 rows in two streams of 128: while one stream's rows are in the softmax, the other's products run.  Head sizes
@@ -26,6 +27,7 @@ namespace halo {
 halo_status check_paged_shape(const halo_paged_shape* s);
 halo_status check_eight(const halo_paged_shape& s, const void* K_scale, const void* V_scale);
 long long paged_stride(const halo_paged_shape& s);
+bool make_bf16_map_nd(CUtensorMap* map, const void* base, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box);
 
 namespace prompt {
 namespace {
@@ -58,6 +60,7 @@ struct Flags {
 constexpr int kLanes = 3;
 struct Bars {
     uint64_t full[8], empty[8], q_full, q_empty, s_full[kLanes], p_full[kLanes], pv_done[kLanes];
+    uint64_t raw[4];                 // a gathering warp's own: values that it looks through before it hands them on
     uint32_t tmem;
     int abort;
     uint32_t o_set[2];               // the last piece whose O held something before its first product, per stream
@@ -81,14 +84,42 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t phase, int* abort) 
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t phase, int* abort) {
     return __all_sync(0xffffffffu, wait(bar, phase, abort));
 }
-// D[tmem] (+)= A[tmem] * B[smem], issued by one thread
-__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b_desc, uint32_t idesc, bool accumulate) {
+// Products issued by one lane of a warp that runs together: D[tmem] (+)= A * B, A in shared memory or (ts) in tensor memory, B in shared memory.  Descriptors by
+// their lower words (address, distance of 64-column blocks); the upper word is the same for every tile here.
+constexpr uint32_t kDescHigh = (1024u >> 4) | 1u << 14 | 2u << 29;      // eight rows 1024 bytes, descriptor version, 128-byte swizzle
+__device__ __forceinline__ void umma_ss(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 x, y;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "l"(b_desc), "r"(idesc), "r"(static_cast<uint32_t>(accumulate))
+        "setp.ne.b32 q, %6, 0;\n\t"
+        "mov.b64 x, {%1, %5};\n\t"
+        "mov.b64 y, {%2, %5};\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate)), "n"(kDescHigh), "r"(lead)
         : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 y;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 q, %6, 0;\n\t"
+        "mov.b64 y, {%2, %5};\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate)), "n"(kDescHigh), "r"(lead)
+        : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t lead, uint64_t* bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %1, 0;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)), "r"(lead)
+        : "memory");
+}
+// 1 in one lane of the warp
+__device__ __forceinline__ uint32_t elect() {
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+    return e;
 }
 __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&v)[16]) {
     asm volatile(
@@ -108,8 +139,8 @@ template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-// 512 threads start with 128 registers each: 2 * 128 * 192 + 128 * 88 + 128 * 40 = 512 * 128
-constexpr int kRowRegs = 192, kCopyRegs = 88, kIssueRegs = 40;
+// 512 threads start with 128 registers each: 2 * 128 * 192 + 2 * 128 * 64 = 512 * 128
+constexpr int kRowRegs = 192, kCopyRegs = 64, kIssueRegs = 64;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
     const int n = valid ? 16 : 0;   // 0: the 16 bytes are filled with zeros and src is not read
@@ -152,98 +183,150 @@ struct Piece {
 
 // ---- gathering ------------------------------------------------------------------------------------------------------------------
 
+// What the copy engine is told: the caches as [page][K/V head][row][column], boxes of box_rows rows of a page (a power of two from 8
+// to 32 that divides the page) x 64 columns; q as [token][head][column], boxes of 128 rows x 64 columns.
+struct Maps {
+    CUtensorMap q, K, V;
+    int box_rows, whole_q;      // 0: rows are gathered one by one (pages of odd sizes, head sizes below 64, head counts that do not divide 128)
+};
+
 template <int DP>
 struct Gather {
     using C = Cfg<DP>;
     static constexpr int kChunks = C::kCols / 8;           // 16-byte chunks of a stage's row
     static constexpr int kAtOnce = 32 / kChunks;           // rows per instruction
     const Args& a;
+    const Maps& maps;
     Smem<DP>& sm;
     int* abort;
     const int warp, lane;
-    uint32_t fill = 0;                  // stages filled so far
-    uint32_t waiting[2];                // barriers of copies that are on their way
+    uint32_t fill = 0, looked = 0;      // stages filled, and looked through, so far
+    uint32_t waiting0 = 0, waiting1 = 0;      // barriers of row copies that are on their way
     int n_waiting = 0;
     bool alive = true;
 
-    __device__ __forceinline__ Gather(const Args& a_, Smem<DP>& sm_) : a(a_), sm(sm_), abort(&sm_.bars.abort), warp((threadIdx.x >> 5) & 3), lane(threadIdx.x & 31) {}
+    __device__ __forceinline__ Gather(const Args& a_, const Maps& m_, Smem<DP>& sm_)
+        : a(a_), maps(m_), sm(sm_), abort(&sm_.bars.abort), warp((threadIdx.x >> 5) & 3), lane(threadIdx.x & 31) {}
     __device__ __forceinline__ void signal(uint32_t bar) {
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
     }
     __device__ __forceinline__ void flush() {
+        if (n_waiting == 0) return;
         cp_wait<0>();
-        if (n_waiting > 0) signal(waiting[0]);
-        if (n_waiting > 1) signal(waiting[1]);
+        signal(waiting0);
+        if (n_waiting > 1) signal(waiting1);
         n_waiting = 0;
     }
-    // copies that were just issued: the ones two before them are complete behind the wait
+    // row copies that were just issued: the ones two before them are complete behind the wait
     __device__ __forceinline__ void issued(uint32_t bar) {
         cp_commit();
         if (n_waiting == 2) {
             cp_wait<2>();
-            signal(waiting[0]);
-            waiting[0] = waiting[1];
-            waiting[1] = bar;
+            signal(waiting0);
+            waiting0 = waiting1;
+            waiting1 = bar;
         } else {
-            waiting[n_waiting++] = bar;
+            (n_waiting == 0 ? waiting0 : waiting1) = bar;
+            ++n_waiting;
         }
     }
-    __device__ __forceinline__ void await(uint64_t* bar, uint32_t parity) {
-        if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity & 1u))) return;
+    __device__ __forceinline__ bool ready(uint64_t* bar, uint32_t phase) { return __all_sync(0xffffffffu, mbar_try_wait(bar, phase & 1u)); }
+    __device__ __forceinline__ void await(uint64_t* bar, uint32_t phase) {
+        if (ready(bar, phase)) return;
         flush();             // nobody frees anything before it has what is on its way
-        alive = warp_wait(bar, parity, abort) && alive;
+        alive = warp_wait(bar, phase, abort) && alive;
     }
-    // 128 keys x kCols columns; at: this lane's key's row of the cache, -1: zeros
-    __device__ __forceinline__ void stage(const void* cache, long long at, int part, bool check, uint32_t* odd) {
-        const uint32_t s = fill % C::kStages, phase = fill / C::kStages;
-        await(&sm.bars.empty[s], phase + 1);     // parity of the phase before: passes at once the first time
-        if (!alive) return;
-        const uint32_t dst = smem_u32(sm.ring) + s * C::kStage;
+    // chunk c of row r of this warp's 32 rows of a stage: block of 64 columns, row of 128 bytes, chunk of 16 turned by the row
+    __device__ __forceinline__ uint32_t place(uint32_t stage, int r, int c) const {
+        return stage + (c >> 3) * (kTile * 128) + (warp * 32 + r) * 128 + (((c & 7) ^ (r & 7)) << 4);
+    }
+    // values of a tile that not every row sees: rows that hold a NaN or an infinity become zeros, and are told
+    __device__ __forceinline__ void look_through(uint32_t stage, int part, uint32_t* odd) {
         const int c = lane % kChunks, r0 = lane / kChunks;
-        const int col = part * C::kCols + c * 8;
-        const bool in = col < a.dh;
-        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(cache) + col;
-        // block of 64 columns, row of 128 bytes, chunk of 16 turned by the row
-        const uint32_t to = dst + (c >> 3) * (kTile * 128) + warp * 32 * 128;
-#pragma unroll
-        for (int i = 0; i < 32 / kAtOnce; ++i) {
-            const int r = i * kAtOnce + r0;
-            const long long from = __shfl_sync(0xffffffffu, at, r);
-            if (in) cp_async16(to + r * 128 + (((c & 7) ^ (r & 7)) << 4), from >= 0 ? src + from : src, from >= 0);
-        }
-        const uint32_t bar = smem_u32(&sm.bars.full[s]);
-        ++fill;
-        if (!check) {
-            issued(bar);
-            return;
-        }
-        // values of a tile that not every row sees: rows that hold a NaN or an infinity become zeros, and are told
-        cp_commit();
-        flush();
+        const bool in = part * C::kCols + c * 8 < a.dh;
         uint32_t mine = 0;
 #pragma unroll 4
         for (int i = 0; i < 32 / kAtOnce; ++i) {
             const int r = i * kAtOnce + r0;
             uint4 v;
-            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(to + r * 128 + (((c & 7) ^ (r & 7)) << 4)));
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(place(stage, r, c)));
             if (in && (odd_word(v.x) || odd_word(v.y) || odd_word(v.z) || odd_word(v.w))) mine |= 1u << r;
         }
         mine = __reduce_or_sync(0xffffffffu, mine);
         if (mine) {
             for (int i = 0; i < 32 / kAtOnce; ++i) {
                 const int r = i * kAtOnce + r0;
-                if (in && (mine >> r & 1u))
-                    asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(to + r * 128 + (((c & 7) ^ (r & 7)) << 4)), "r"(0) : "memory");
+                if (in && (mine >> r & 1u)) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(place(stage, r, c)), "r"(0) : "memory");
             }
         }
         if (lane == 0) odd[warp] = mine;
-        signal(bar);
     }
-    __device__ __forceinline__ void queries(const Walk<C::kRows, kTile>& w, uint32_t piece) {
+    // 128 keys x kCols columns.  page: of this lane's key, n_pages: none, which reads as zeros; pos: of the tile; odd: told, or null.
+    __device__ __forceinline__ void stage(const CUtensorMap* map, const void* cache, int page, int pos, int kvh, int part, uint32_t* odd) {
+        const uint32_t s = fill % C::kStages, phase = fill / C::kStages;
+        await(&sm.bars.empty[s], phase + 1);     // the phase before: passes at once the first time
+        if (!alive) return;
+        ++fill;
+        const uint32_t dst = smem_u32(sm.ring) + s * C::kStage, full = smem_u32(&sm.bars.full[s]);
+        const int first = pos + warp * 32;       // of this warp's keys
+        if (maps.box_rows) {
+            const int boxes = 32 / maps.box_rows, blocks = min(C::kCols / 64, (a.dh - part * C::kCols + 63) / 64);
+            const int box = lane % boxes, block = lane / boxes, row = box * maps.box_rows;
+            const int from = __shfl_sync(0xffffffffu, page, row), at = first + row;
+            uint64_t* bar = odd ? &sm.bars.raw[warp] : &sm.bars.full[s];
+            if (lane == 0) mbar_arrive_expect_tx(bar, blocks * 32 * 128);
+            __syncwarp();
+            if (block < blocks)
+                tma_load_4d(dst + block * (kTile * 128) + (warp * 32 + row) * 128, map, part * C::kCols + block * 64,
+                            a.page_shift >= 0 ? at & (a.page_size - 1) : at % a.page_size, kvh, from, smem_u32(bar));
+            if (odd) {
+                alive = warp_wait(bar, looked++, abort) && alive;
+                look_through(dst, part, odd);
+                signal(full);
+            }
+            return;
+        }
+        const int mine = first + lane, in_page = a.page_shift >= 0 ? mine & (a.page_size - 1) : mine % a.page_size;
+        const long long at = page < a.n_pages ? static_cast<long long>(page) * a.page_stride + (static_cast<long long>(kvh) * a.page_size + in_page) * a.dh : -1;
+        const int c = lane % kChunks, r0 = lane / kChunks, col = part * C::kCols + c * 8;
+        const bool in = col < a.dh;
+        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(cache) + col;
+#pragma unroll
+        for (int i = 0; i < 32 / kAtOnce; ++i) {
+            const int r = i * kAtOnce + r0;
+            const long long from = __shfl_sync(0xffffffffu, at, r);
+            if (in) cp_async16(place(dst, r, c), from >= 0 ? src + from : src, from >= 0);
+        }
+        if (!odd) {
+            issued(full);
+            return;
+        }
+        cp_commit();
+        cp_wait<0>();
+        flush();
+        look_through(dst, part, odd);
+        signal(full);
+    }
+    __device__ __forceinline__ void queries(const Walk<C::kRows, kTile>& w, const Piece<DP>& p, uint32_t piece) {
         await(&sm.bars.q_empty, piece + 1);
         if (!alive) return;
+        const uint32_t q = smem_u32(sm.q), full = smem_u32(&sm.bars.q_full);
+        if (maps.whole_q) {      // tokens behind the sequence's last come along, and go nowhere
+            const int blocks = (a.dh + 63) / 64, boxes = p.streams * blocks, mine = (boxes - warp + 3) / 4;
+            if (lane == 0) {
+                if (mine > 0) mbar_arrive_expect_tx(&sm.bars.q_full, mine * 128 * 128);
+                else mbar_arrive(&sm.bars.q_full);
+            }
+            __syncwarp();
+            if (lane < mine) {
+                const int box = lane * 4 + warp, t = box / blocks, block = box - t * blocks;
+                const int token = w.r.first + static_cast<int>((static_cast<long long>(w.rb) * C::kRows + t * 128) / a.G);
+                tma_load_3d(q + t * C::kQTile + block * (128 * 128), &maps.q, block * 64, w.kvh * a.G, token, full);
+            }
+            return;
+        }
         constexpr int kOwn = C::kRows / 4, kWide = DP / 8, kRowsAtOnce = 32 / kWide;      // rows of a warp
 #pragma unroll
         for (int i = lane; i < kOwn; i += 32) {
@@ -254,7 +337,7 @@ struct Gather {
         const int c = lane % kWide, r0 = lane / kWide;
         const bool in = c * 8 < a.dh;
         const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + c * 8;
-        const uint32_t dst = smem_u32(sm.q) + (c >> 3) * (128 * 128) + ((c & 7) << 4);
+        const uint32_t dst = q + (c >> 3) * (128 * 128) + ((c & 7) << 4);
 #pragma unroll 4
         for (int i = 0; i < kOwn / kRowsAtOnce; ++i) {
             const int r = warp * kOwn + i * kRowsAtOnce + r0;
@@ -262,7 +345,7 @@ struct Gather {
             if (in) cp_async16((dst + (r >> 7) * C::kQTile + (r & 127) * 128) ^ ((r & 7) << 4), from >= 0 ? src + from : src, from >= 0);
         }
         __syncwarp();      // q_row may be written again
-        issued(smem_u32(&sm.bars.q_full));
+        issued(full);
     }
     __device__ void run(Walk<C::kRows, kTile> w) {
         bool bad = false;
@@ -275,24 +358,33 @@ struct Gather {
                 return ldg_waited(a.table + static_cast<long long>(w.s) * a.max_pages + (a.page_shift >= 0 ? at >> a.page_shift : at / a.page_size));
             };
             int page = page_of(0);
+            // ahead of the keys where the item before is through with its own, else behind the first keys and values
+            bool asked = p.n == 0;
+            if (!asked && ready(&sm.bars.q_empty, piece + 1)) {
+                queries(w, p, piece);
+                asked = true;
+            }
             for (int j = 0; j < p.n && alive; ++j, ++tile) {
                 const int next = page_of(j + 1);
-                const int pos = (w.t0 + j) * kTile + warp * 32 + lane;
-                const bool in = pos < w.reach, ok = in && page >= 0 && page < a.n_pages;
+                const int pos = (w.t0 + j) * kTile;
+                const bool in = pos + warp * 32 + lane < w.reach, ok = in && page >= 0 && page < a.n_pages;
                 bad |= in && !ok;
-                const int in_page = a.page_shift >= 0 ? pos & (a.page_size - 1) : pos % a.page_size;
-                const long long at = ok ? static_cast<long long>(page) * a.page_stride + (static_cast<long long>(w.kvh) * a.page_size + in_page) * a.dh : -1;
                 const uint32_t there = __ballot_sync(0xffffffffu, ok);
-                // the slot's last readers are done: their P went into a product behind which K stages were freed for this tile
+                // the slot's last readers are done: their P went into a product behind which stages were freed for this tile
                 if (lane == 0) sm.flags.there[tile % kFlags][warp] = there;
+                const int from = ok ? page : a.n_pages;
                 const bool check = p.partial(w.t0 + j);
 #pragma unroll
-                for (int h = 0; h < C::kParts; ++h) stage(a.K, at, h, false, nullptr);
+                for (int h = 0; h < C::kParts; ++h) stage(&maps.K, a.K, from, pos, w.kvh, h, nullptr);
 #pragma unroll
-                for (int h = 0; h < C::kParts; ++h) stage(a.V, at, h, check, sm.flags.odd[tile % kFlags][h]);
-                if (j == 0) queries(w, piece++);
+                for (int h = 0; h < C::kParts; ++h) stage(&maps.V, a.V, from, pos, w.kvh, h, check ? sm.flags.odd[tile % kFlags][h] : nullptr);
+                if (!asked && alive) {
+                    queries(w, p, piece);
+                    asked = true;
+                }
                 page = next;
             }
+            if (p.n > 0) ++piece;
             w.next(a);
         }
         flush();
@@ -302,85 +394,150 @@ struct Gather {
 
 // ---- products -------------------------------------------------------------------------------------------------------------------
 
+template <int N>
+using Const = std::integral_constant<int, N>;
+
+// One warp, one lane of which issues.  Lanes (of barriers) are constants, so that counters and addresses stay in registers: the tensor cores take a product of 16
+// columns in 64 clocks, and one must not take longer to issue.
 template <int DP>
 __device__ void issue_products(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, kTile> w) {
     using C = Cfg<DP>;
     Bars& bars = sm.bars;
     int* abort = &bars.abort;
-    const uint32_t tmem = bars.tmem, q0 = smem_u32(sm.q), ring = smem_u32(sm.ring);
+    const uint32_t lead = elect();
+    const uint32_t tmem = bars.tmem, q0 = smem_u32(sm.q) >> 4, ring = smem_u32(sm.ring) >> 4;
     // a negative scale: -Q instead, so that the largest score stays the largest product
     const uint32_t idesc_s = umma_idesc_bf16(128, kTile, false) | (a.scale_log2 < 0.0f ? 1u << 13 : 0u);
-    uint32_t first_fill = 0, piece = 0, use[kLanes] = {0, 0, 0};
-    int last[2] = {0, 1};      // lane that a buffer was used in last
+    uint32_t first_fill = 0, piece = 0, use0 = 0, use1 = 0, use2 = 0;      // tiles of each lane so far
+    int last = 1;                                                          // lane that the second buffer was used in last
     while (w.left > 0) {
         const Piece<DP> p(a, w);
         if (p.n > 0) {
-            if (!wait(&bars.q_full, piece++, abort)) return;      // from here on piece counts from 1
-            const auto scores = [&](int t, int j) {
-                const int b = p.lane(t, j), buffer = p.buffer(b);
+            if (!warp_wait(&bars.q_full, piece++, abort)) return;      // from here on piece counts from 1
+            // stream t, lane b, tile j; end: the last stream's, after which the stages are free
+            const auto scores = [&](auto t_, auto b_, int j, bool end) {
+                constexpr int t = decltype(t_)::value, b = decltype(b_)::value, buffer = b != 0;
                 // S lies where the P of the buffer's last tile was read from
-                if (use[last[buffer]] > 0 && !wait(&bars.pv_done[last[buffer]], use[last[buffer]] - 1, abort)) return false;
-                last[buffer] = b;
+                if (buffer == 0) {
+                    if (use0 > 0 && !warp_wait(&bars.pv_done[0], use0 - 1, abort)) return false;
+                    ++use0;
+                } else {
+                    const uint32_t used = last == 1 ? use1 : use2;
+                    if (used > 0 && !warp_wait(last == 1 ? &bars.pv_done[1] : &bars.pv_done[2], used - 1, abort)) return false;
+                    last = b;
+                    ++(b == 1 ? use1 : use2);
+                }
+                const uint32_t d = tmem + buffer * 128;
 #pragma unroll
                 for (int h = 0; h < C::kParts; ++h) {
                     const uint32_t f = first_fill + j * 2 * C::kParts + h, s = f % C::kStages;
-                    if (!wait(&bars.full[s], f / C::kStages, abort)) return false;
+                    if (!warp_wait(&bars.full[s], f / C::kStages, abort)) return false;
                     tcgen05_fence_after_sync();
-                    const int steps = min(a.dh - h * C::kCols, C::kCols) / 16;
-                    for (int k = 0; k < steps; ++k) {
-                        const uint32_t block = (k >> 2) * (128 * 128) + (k & 3) * 32;
-                        umma_bf16(tmem + buffer * 128, umma_smem_desc(q0 + t * C::kQTile + h * (C::kCols / 64) * (128 * 128) + block, 16, 1024),
-                                  umma_smem_desc(ring + s * C::kStage + block, 16, 1024), idesc_s, h > 0 || k > 0);
+                    const uint32_t q = q0 + ((t * C::kQTile + h * (C::kCols / 64) * (128 * 128)) >> 4), k = ring + s * (C::kStage >> 4);
+                    const int steps = (a.dh - h * C::kCols) / 16;
+                    if (steps >= C::kCols / 16) {
+#pragma unroll
+                        for (int e = 0; e < C::kCols / 16; ++e)
+                            umma_ss(lead, d, q + (e >> 2) * 1024 + (e & 3) * 2, k + (e >> 2) * 1024 + (e & 3) * 2, idesc_s, h > 0 || e > 0);
+                    } else {
+                        for (int e = 0; e < steps; ++e)
+                            umma_ss(lead, d, q + (e >> 2) * 1024 + (e & 3) * 2, k + (e >> 2) * 1024 + (e & 3) * 2, idesc_s, h > 0 || e > 0);
                     }
-                    if (t == p.streams - 1) umma_commit(&bars.empty[s]);
+                    if (end) commit(lead, &bars.empty[s]);
                 }
-                umma_commit(&bars.s_full[b]);
-                mbar_arrive(&bars.s_full[b]);      // what this thread has seen of the gathering warps, the tile's flags among it
-                ++use[b];
-                if (t == p.streams - 1 && j == p.n - 1) umma_commit(&bars.q_empty);
+                commit(lead, &bars.s_full[b]);
+                if (lead) mbar_arrive(&bars.s_full[b]);      // what this thread has seen of the gathering warps, the tile's flags among it
+                if (end && j == p.n - 1) commit(lead, &bars.q_empty);
                 return true;
             };
-            const auto sums = [&](int t, int j) {
-                const int b = p.lane(t, j);
-                if (!wait(&bars.p_full[b], use[b] - 1, abort)) return false;
+            const auto sums = [&](auto t_, auto b_, int j, bool end) {
+                constexpr int t = decltype(t_)::value, b = decltype(b_)::value;
+                if (!warp_wait(&bars.p_full[b], (b == 0 ? use0 : b == 1 ? use1 : use2) - 1, abort)) return false;
                 tcgen05_fence_after_sync();
                 const bool on_top = j > 0 || *reinterpret_cast<volatile uint32_t*>(&bars.o_set[t]) == piece;
 #pragma unroll
                 for (int h = 0; h < C::kParts; ++h) {
                     const uint32_t f = first_fill + (j * 2 + 1) * C::kParts + h, s = f % C::kStages;
-                    if (!wait(&bars.full[s], f / C::kStages, abort)) return false;
+                    if (!warp_wait(&bars.full[s], f / C::kStages, abort)) return false;
                     tcgen05_fence_after_sync();
                     const uint32_t idesc = umma_idesc_bf16(128, min(a.dh - h * C::kCols, C::kCols), true);
+                    const uint32_t v = (ring + s * (C::kStage >> 4)) | ((kTile * 128) >> 4) << 16;
 #pragma unroll
-                    for (int k = 0; k < kTile / 16; ++k)
-                        umma_ts(tmem + C::kO + t * DP + h * C::kCols, tmem + p.buffer(b) * 128 + k * 8,
-                                umma_smem_desc(ring + s * C::kStage + k * 2048, kTile * 128, 1024), idesc, on_top || k > 0);
-                    if (t == p.streams - 1) umma_commit(&bars.empty[s]);
+                    for (int e = 0; e < kTile / 16; ++e)
+                        umma_ts(lead, tmem + C::kO + t * DP + h * C::kCols, tmem + (b != 0) * 128 + e * 8, v + e * 128, idesc, on_top || e > 0);
+                    if (end) commit(lead, &bars.empty[s]);
                 }
-                umma_commit(&bars.pv_done[b]);
+                commit(lead, &bars.pv_done[b]);
                 return true;
             };
-            if (p.streams == 2) {
-                if (p.tiles[0] > 0 && !scores(0, 0)) return;
-                if (!scores(1, 0)) return;
+            if (C::kStreams == 2 && p.streams == 2) {
+                if (p.tiles[0] > 0 && !scores(Const<0>(), Const<0>(), 0, false)) return;
+                if (!scores(Const<C::kStreams - 1>(), Const<1>(), 0, true)) return;
                 for (int j = 0; j < p.n; ++j) {
-                    if (j < p.tiles[0] && !sums(0, j)) return;
-                    if (j + 1 < p.tiles[0] && !scores(0, j + 1)) return;
-                    if (!sums(1, j)) return;
-                    if (j + 1 < p.n && !scores(1, j + 1)) return;
+                    if (j < p.tiles[0] && !sums(Const<0>(), Const<0>(), j, false)) return;
+                    if (j + 1 < p.tiles[0] && !scores(Const<0>(), Const<0>(), j + 1, false)) return;
+                    if (!sums(Const<C::kStreams - 1>(), Const<1>(), j, true)) return;
+                    if (j + 1 < p.n && !scores(Const<C::kStreams - 1>(), Const<1>(), j + 1, true)) return;
                 }
             } else {
-                if (!scores(0, 0)) return;
-                if (p.n > 1 && !scores(0, 1)) return;
-                for (int j = 0; j < p.n; ++j) {
-                    if (!sums(0, j)) return;
-                    if (j + 2 < p.n && !scores(0, j + 2)) return;
+                if (!scores(Const<0>(), Const<0>(), 0, true)) return;
+                if (p.n > 1 && !scores(Const<0>(), Const<2>(), 1, true)) return;
+                for (int j = 0; j < p.n; j += 2) {
+                    if (!sums(Const<0>(), Const<0>(), j, true)) return;
+                    if (j + 2 < p.n && !scores(Const<0>(), Const<0>(), j + 2, true)) return;
+                    if (j + 1 < p.n && !sums(Const<0>(), Const<2>(), j + 1, true)) return;
+                    if (j + 3 < p.n && !scores(Const<0>(), Const<2>(), j + 3, true)) return;
                 }
             }
             first_fill += p.n * 2 * C::kParts;
         }
         w.next(a);
     }
+}
+
+// ---- two fp32 numbers at a time ----
+using Pair = unsigned long long;
+__device__ __forceinline__ Pair pair_of(float a, float b) {
+    Pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 both(Pair x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ Pair twice(float a) { return pair_of(a, a); }
+// NaN if one of them is
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// 2^x of two numbers up to 126 without the special-function unit, which does 16 a clock and SM and bounds the softmax: x = n + f with n
+// the nearest whole number (the low bits of x + 1.5 * 2^23), 2^f by the polynomial of degree 4 with the least largest relative
+// error on [-1/2, 1/2] (2.7e-6, evaluated in fp32; found by linear programming), n into the exponent.  Below -126: 2^-126.
+__device__ __forceinline__ float2 pow2_by_polynomial(Pair x) {
+    const float2 low = both(x);
+    x = pair_of(fmaxf(low.x, -126.0f), fmaxf(low.y, -126.0f));
+    const Pair shifted = add2(x, twice(12582912.0f)), f = fma2(add2(shifted, twice(-12582912.0f)), twice(-1.0f), x);
+    Pair y = fma2(twice(0.009569705463945866f), f, twice(0.05591819807887077f));
+    y = fma2(y, f, twice(0.24024765193462372f));
+    y = fma2(y, f, twice(0.6931217312812805f));
+    y = fma2(y, f, twice(0.9999992251396179f));
+    const float2 n = both(shifted), v = both(y);
+    return make_float2(__uint_as_float(__float_as_uint(v.x) + (__float_as_uint(n.x) << 23)),
+                       __uint_as_float(__float_as_uint(v.y) + (__float_as_uint(n.y) << 23)));
 }
 
 // ---- rows -----------------------------------------------------------------------------------------------------------------------
@@ -457,7 +614,8 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
 #pragma unroll
                 for (int c = 0; c < 4; ++c) there[c] = *const_cast<volatile const uint32_t*>(&sm.flags.there[slot][c]);
                 tmem_ld_wait();
-                if (p0 + kTile > all_see || (there[0] & there[1] & there[2] & there[3]) != 0xffffffffu) {
+                const bool masked = p0 + kTile > all_see || (there[0] & there[1] & there[2] & there[3]) != 0xffffffffu;
+                if (masked) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         const int left = sees - p0 - c * 32;
@@ -467,11 +625,16 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
                             if (!(in >> e & 1u)) sc[c][e] = 0xff800000u;
                     }
                 }
-                float mx = -INFINITY;
+                float most[4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
+                for (int c = 0; c < 4; ++c) most[c] = max3(__uint_as_float(sc[c][0]), __uint_as_float(sc[c][1]), __uint_as_float(sc[c][2]));
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) mx = fmaxf(mx, __uint_as_float(sc[c][e]));
+                for (int e = 3; e < 31; e += 2)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) most[c] = max3(most[c], __uint_as_float(sc[c][e]), __uint_as_float(sc[c][e + 1]));
+#pragma unroll
+                for (int c = 0; c < 4; ++c) most[c] = max3(most[c], most[c], __uint_as_float(sc[c][31]));
+                const float mx = max3(max3(most[0], most[1], most[2]), most[3], most[3]);
                 if (__any_sync(0xffffffffu, (mx - m) * scale > kSlack)) {
                     const float to = fmaxf(m, mx), f = m == -INFINITY ? 0.0f : pow2((m - to) * scale);
                     if (j > 0) {
@@ -490,17 +653,34 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
                     m = to;
                 }
                 const float base = m == -INFINITY ? 0.0f : m * scale;
+                const Pair times = twice(scale), minus = twice(-base);
+                Pair sum[2] = {0, 0};
+                // A quarter of the powers by polynomial, unless something is masked, infinite or NaN: those have to come out exactly.
+                const auto weights = [&](auto by_polynomial) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t pk[16];
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t pk[16];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const float x = pow2(fmaf(__uint_as_float(sc[c][2 * e]), scale, -base));
-                        const float y = pow2(fmaf(__uint_as_float(sc[c][2 * e + 1]), scale, -base));
-                        l += x + y;
-                        pk[e] = pack_bf16(x, y);
+                        for (int e = 0; e < 16; ++e) {
+                            const Pair x = fma2(pair_of(__uint_as_float(sc[c][2 * e]), __uint_as_float(sc[c][2 * e + 1])), times, minus);
+                            float2 y;
+                            if (decltype(by_polynomial)::value && e % 4 == 3) {
+                                y = pow2_by_polynomial(x);
+                            } else {
+                                y = both(x);
+                                y = make_float2(pow2(y.x), pow2(y.y));
+                            }
+                            sum[e & 1] = add2(sum[e & 1], pair_of(y.x, y.y));
+                            pk[e] = pack_bf16(y.x, y.y);
+                        }
+                        tmem_st_32x16(s_addr + c * 16, pk);
                     }
-                    tmem_st_32x16(s_addr + c * 16, pk);
+                };
+                if (!masked && __all_sync(0xffffffffu, fabsf(mx) < INFINITY)) weights(Const<1>());
+                else weights(Const<0>());
+                {
+                    const float2 s0 = both(sum[0]), s1 = both(sum[1]);
+                    l += (s0.x + s0.y) + (s1.x + s1.y);
                 }
                 tmem_st_wait();
                 if (p.partial(w.t0 + j)) {
@@ -584,12 +764,12 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
 }
 
 template <int DP>
-__global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
     using C = Cfg<DP>;
     extern __shared__ __align__(1024) unsigned char raw[];
     Smem<DP>& sm = *reinterpret_cast<Smem<DP>*>(raw);
     Bars& bars = sm.bars;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = tid >> 5;
     chain_wait();
     const Found<C::kRows, kTile> f = locate<C::kRows, kTile, kThreads>(a, sm.sh);
     if (f.walk.left <= 0) {      // the same in every thread
@@ -608,6 +788,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __g
             mbar_init(&bars.p_full[b], 4);    // a stream's warps
             mbar_init(&bars.pv_done[b], 1);
         }
+        for (int i = 0; i < 4; ++i) mbar_init(&bars.raw[i], 1);
         bars.o_set[0] = bars.o_set[1] = 0;
         bars.abort = 0;
         mbar_fence_init();
@@ -624,10 +805,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __g
         softmax_rows<DP>(a, sm, f.walk, f.total);
     } else if (warp < 12) {
         fewer_registers<kCopyRegs>();
-        Gather<DP>(a, sm).run(f.walk);
+        Gather<DP>(a, maps, sm).run(f.walk);
     } else {
         fewer_registers<kIssueRegs>();
-        if (warp == 12 && lane == 0) issue_products<DP>(a, sm, f.walk);
+        if (warp == 12) issue_products<DP>(a, sm, f.walk);
     }
     __syncwarp();
     tcgen05_fence_before_sync();
@@ -672,7 +853,24 @@ halo_status launch(const Args& args, const halo_paged_shape& sh, void* ws, cudaS
         a.slot = slot_floats(a.rows, a.dh);
         a.openings = static_cast<Opening*>(ws);
         a.ws = reinterpret_cast<float*>(a.openings + a.blocks);
-        const halo_status rc = launch_chained(paged_prompt_mha_kernel<DP>, a.blocks, kThreads, sizeof(Smem<DP>), st, a);
+        Maps maps = {};
+        const uint64_t wide = sh.head_dim, row = wide * 2;
+        const int page_bits = sh.page_size & -sh.page_size;
+        if (wide >= 64 && page_bits >= 8) {
+            maps.box_rows = page_bits < 32 ? page_bits : 32;
+            const uint64_t dims[4] = {wide, static_cast<uint64_t>(sh.page_size), static_cast<uint64_t>(a.Hk), static_cast<uint64_t>(sh.n_pages)};
+            const uint64_t strides[3] = {row, row * sh.page_size, static_cast<uint64_t>(a.page_stride) * 2};
+            const uint32_t box[4] = {64, static_cast<uint32_t>(maps.box_rows), 1, 1};
+            if (!make_bf16_map_nd(&maps.K, a.K, 4, dims, strides, box) || !make_bf16_map_nd(&maps.V, a.V, 4, dims, strides, box)) return HALO_ERR_CUDA;
+        }
+        if (wide >= 64 && 128 % a.G == 0 && a.n_tok >= 128 / a.G) {
+            maps.whole_q = 1;
+            const uint64_t dims[3] = {wide, static_cast<uint64_t>(a.H), static_cast<uint64_t>(a.n_tok)};
+            const uint64_t strides[2] = {row, static_cast<uint64_t>(a.q_stride) * 2};
+            const uint32_t box[3] = {64, static_cast<uint32_t>(a.G), static_cast<uint32_t>(128 / a.G)};
+            if (!make_bf16_map_nd(&maps.q, a.q, 3, dims, strides, box)) return HALO_ERR_CUDA;
+        }
+        const halo_status rc = launch_chained(paged_prompt_mha_kernel<DP>, a.blocks, kThreads, sizeof(Smem<DP>), st, a, maps);
         return rc != HALO_OK ? rc : launch_join<__nv_bfloat16, Cfg<DP>::kRows>(a, st);
     });
 }

@@ -1083,6 +1083,22 @@ bool make_bf16_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t c
     return make_map(map, base, rows, cols, row_stride_elems, box_cols, box_rows);
 }
 
+// bf16 array of 3 or 4 dimensions, innermost first; strides in bytes of the dimensions behind it; 128-byte swizzle, zero fill
+bool make_bf16_map_nd(CUtensorMap* map, const void* base, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn || rank < 3 || rank > 4) return false;
+    cuuint64_t d[4], s[3];
+    cuuint32_t b[4];
+    const cuuint32_t elem_strides[4] = {1, 1, 1, 1};
+    for (int i = 0; i < rank; ++i) {
+        d[i] = dims[i];
+        b[i] = box[i];
+        if (i > 0) s[i - 1] = strides[i - 1];
+    }
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), d, s, b, elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // the same for a matrix of bytes [rows][row_bytes]
 bool make_byte_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t row_bytes, uint32_t box_bytes, uint32_t box_rows) {
     EncodeTiledFn fn = encode_tiled_fn();
