@@ -515,7 +515,7 @@ halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, const void*
  *   q_start[n_seq] <= n_tok; out device [n_tok][n_heads][head_dim], must not overlap q; lse device fp32 [n_tok][n_heads] or
  *   NULL.  Rows of no sequence are neither read nor written.  keep as in halo_paged_mha.
  *   A row that sees nothing (P < 0, a lost head, scores that are all -infinity) gives zeros and lse = -infinity.  What a row does
- *   not see has no influence on it, NaN and infinities included.
+ *   not see has no influence on it, NaN and infinities included (which may change the order of its sums).
  *   fp32 sums and softmax; bf16 and 8-bit caches: a weight meets the values rounded to bf16 (2^-8 of itself).
  *   A sequence whose rows are out of range or decrease is left out, one whose length is negative or behind the table
  *   counts as empty, positions on a page out of range are left out; each sets HALO_DEV_BAD_INDEX.

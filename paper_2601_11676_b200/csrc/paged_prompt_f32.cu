@@ -14,7 +14,7 @@ namespace halo {
 namespace prompt {
 namespace {
 
-constexpr int kRows = 64, kTile = 64, kThreads = 128;
+constexpr int kRows = 64, kTile = 64, kThreads = 128, kOver = 1;
 
 struct Eight {};
 template <typename T> struct Kind {
@@ -53,9 +53,8 @@ __global__ void __launch_bounds__(kThreads) paged_prompt_rows_kernel(const __gri
     S_& sm = *reinterpret_cast<S_*>(raw);
     const int tid = threadIdx.x, lane = tid & 31, tx = tid & 15, ty = tid >> 4;
     chain_wait();
-    Found<kRows, kTile> f = locate<kRows, kTile, kThreads>(a, sm.sh);
-    Walk<kRows, kTile>& w = f.walk;
-    const long long range = w.left;
+    Found<kRows, kTile, kOver> f = locate<kRows, kTile, kOver, kThreads>(a, sm.sh);
+    Walk<kRows, kTile, kOver>& w = f.walk;
     bool bad = false;
 
     while (w.left > 0) {
@@ -121,9 +120,12 @@ __global__ void __launch_bounds__(kThreads) paged_prompt_rows_kernel(const __gri
         }
         int sees[8];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) sees[r] = row_at<kRows>(a, w.r, kvh, w.rb, ty * 8 + r).sees;
+        for (int r = 0; r < 8; ++r) {
+            const Row row = row_at<kRows>(a, w.r, kvh, w.rb, ty * 8 + r);
+            sees[r] = row.kept ? row.sees : 0;
+        }
         // every row sees what the item's first token sees
-        const int all_see = w.r.len - w.r.n + static_cast<int>(static_cast<long long>(w.rb) * kRows / a.G) + 1;
+        const int all_see = w.r.len - w.r.n + w.rb * kRows / a.G + 1;
         if (nt > 0) {
             places(0);
             places(1);
@@ -223,7 +225,7 @@ __global__ void __launch_bounds__(kThreads) paged_prompt_rows_kernel(const __gri
         cp_wait<0>();
 
         const bool complete = w.complete();
-        float* slot = a.ws + (static_cast<long long>(blockIdx.x) * 2 + (w.left == range ? 0 : 1)) * a.slot;
+        float* slot = w.slot(a);
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
 #pragma unroll
@@ -258,23 +260,17 @@ __global__ void __launch_bounds__(kThreads) paged_prompt_rows_kernel(const __gri
                             make_float4(o[r][4 * g], o[r][4 * g + 1], o[r][4 * g + 2], o[r][4 * g + 3]);
             }
         }
-        if (tid == 0 && w.left == w.t1 - w.t0)   // the range's last piece
-            a.openings[blockIdx.x] = {w.t0 == 0 && w.t1 < w.nt, w.s, w.kvh, w.rb, w.nt - w.t1, w.left == range, f.total};
+        if (tid == 0 && w.opens()) a.openings[blockIdx.x] = w.opening(f.total);
         w.next(a);
         __syncthreads();
     }
-    if (f.total == 0 && blockIdx.x == 0 && tid == 0) a.openings[0] = {0, 0, 0, 0, 0, 0, 0};
     if (__any_sync(0xffffffffu, bad) && lane == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
 }
 
-// Thread blocks: as many as stay resident, no more than the line can have tiles.
 template <int DP>
 int blocks_of(const halo_paged_shape& sh, int n_tok, int n_seq) {
-    const int per_sm = static_cast<int>(227 * 1024 / (sizeof(Smem<DP>) + 1024));
-    const long long G = sh.n_heads / sh.n_kv_heads, cap = static_cast<long long>(sh.max_pages) * sh.page_size;
-    const long long items = (n_tok * G / kRows + (n_seq < n_tok ? n_seq : n_tok) + 1) * sh.n_kv_heads;
-    const long long tiles = items * ((cap + kTile - 1) / kTile), most = static_cast<long long>(kSmCount) * (per_sm < 4 ? per_sm : 4);
-    return static_cast<int>(tiles / kMinTiles < 1 ? 1 : tiles / kMinTiles < most ? tiles / kMinTiles : most);
+    constexpr int kFit = 227 * 1024 / static_cast<int>(sizeof(Smem<DP>) + 1024);
+    return line_blocks(sh, n_tok, n_seq, kRows, kTile, kOver, kSmCount * (kFit < 4 ? kFit : 4));
 }
 template <typename F>
 auto by_width(const halo_paged_shape& sh, F f) {

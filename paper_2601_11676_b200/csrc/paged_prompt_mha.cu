@@ -10,12 +10,12 @@
 // An item has 256 rows in two streams of 128: while one stream's rows are in the softmax, the other's products run.  Head sizes
 // above 128 (whose O fills half of tensor memory) and items of up to 128 rows have one stream with two S buffers instead.
 //
-// The running maximum that weights are relative to moves only when a row's maximum has grown by 2^8: O and the sum are in fp32, so
-// nothing is lost by weights up to 2^8, and O, which would have to be read, multiplied and written back for every move, is left
-// alone after the first tiles.
+// Weights are powers of two relative to a reference that is a row's maximum when it is set, and set again only when a tile's
+// weights sum to more than 2^20: O and the sum are in fp32, so weights above 1 lose nothing, O, which would have to be read,
+// multiplied and written back for every new reference, is left alone after the first tiles, and a tile needs no maximum.
 //
-// What a row does not see must not reach it, and 0 * infinity would: in tiles that not every row sees, value rows with a NaN or an
-// infinity are taken out of the stage, and each thread adds them to its row of O by itself where its row sees them.
+// What a row does not see must not reach it.  Weights of 0 see to that but for values that are infinite or NaN; a row whose
+// sums come out as neither although its weights are finite is summed again, key by key (resum).
 #include <math.h>
 
 #include <type_traits>
@@ -34,6 +34,7 @@ namespace {
 
 constexpr int kTile = 128;         // keys
 constexpr int kThreads = 512;
+constexpr int kOver = 2;           // an item's rows, first scores and outputs cost about as much as two tiles
 constexpr int kFlags = 8;          // tiles whose flags are kept
 
 // DP: head size padded to 64, 128 or 256.
@@ -52,7 +53,6 @@ struct Cfg {
 
 struct Flags {
     uint32_t there[kFlags][4];       // which of a tile's keys are there
-    uint32_t odd[kFlags][2][4];      // which of a tile's value rows were taken out, per part
 };
 // S, P and O of a tile hand over through barriers of the lane that it is in: a stream's own in items of two streams, 0 and 2 in
 // turn in items of one.  Lanes 1 and 2 share the buffer behind 0, but not the warps that wait: 1 belongs to the second stream's,
@@ -60,10 +60,9 @@ struct Flags {
 constexpr int kLanes = 3;
 struct Bars {
     uint64_t full[8], empty[8], q_full, q_empty, s_full[kLanes], p_full[kLanes], pv_done[kLanes];
-    uint64_t raw[4];                 // a gathering warp's own: values that it looks through before it hands them on
+    uint64_t raw[4];                 // a gathering warp's own: values of which it hands on a part
     uint32_t tmem;
     int abort;
-    uint32_t o_set[2];               // the last piece whose O held something before its first product, per stream
 };
 template <int DP>
 struct Smem {
@@ -129,18 +128,13 @@ __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&v
         "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
         : "memory");
 }
-__device__ __forceinline__ uint32_t tmem_ld_word(uint32_t taddr) {
-    uint32_t v;
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(v) : "r"(taddr) : "memory");
-    return v;
-}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-// 512 threads start with 128 registers each: 2 * 128 * 192 + 2 * 128 * 64 = 512 * 128
-constexpr int kRowRegs = 192, kCopyRegs = 64, kIssueRegs = 64;
+// 512 threads start with 128 registers each: 2 * 128 * 208 + 2 * 128 * 48 = 512 * 128
+constexpr int kRowRegs = 208, kCopyRegs = 48, kIssueRegs = 48;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
     const int n = valid ? 16 : 0;   // 0: the 16 bytes are filled with zeros and src is not read
@@ -153,29 +147,22 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ bool odd_word(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
-
 // A piece as every role sees it: its tiles, its streams and how many of the tiles each of them takes part in.
 template <int DP>
 struct Piece {
     using C = Cfg<DP>;
     int n, streams, tiles[2];
-    int sees_first;      // positions that every row of the item sees
-    __device__ __forceinline__ Piece(const Args& a, const Walk<C::kRows, kTile>& w) {
-        const long long base = static_cast<long long>(w.rb) * C::kRows, all = static_cast<long long>(w.r.n) * a.G;
-        const int first = w.r.len - w.r.n + 1;
+    __device__ __forceinline__ Piece(const Args& a, const Walk<C::kRows, kTile, kOver>& w) {
+        const int base = w.rb * C::kRows, all = w.r.n * a.G, first = w.r.len - w.r.n + 1;
         n = w.reach > 0 ? w.t1 - w.t0 : 0;
         streams = C::kStreams == 2 && base + 128 < all ? 2 : 1;
-        sees_first = first + static_cast<int>(base / a.G);
         tiles[0] = tiles[1] = n;
         if (C::kStreams == 2 && streams == 2) {      // the first stream's last row may not see the last tiles
-            const int sees = first + static_cast<int>((base + 127) / a.G);
+            const int sees = first + (base + 127) / a.G;
             tiles[0] = min(n, max((sees + kTile - 1) / kTile - w.t0, 0));
         }
         if (streams == 1) tiles[1] = 0;
     }
-    // whether some row does not see all of the tile
-    __device__ __forceinline__ bool partial(int tile) const { return (tile + 1) * kTile > sees_first; }
     // lane of tile j of a stream; its buffer of S and P
     __device__ __forceinline__ int lane(int stream, int j) const { return streams == 2 ? stream : (j & 1) * 2; }
     static __device__ __forceinline__ int buffer(int lane) { return lane != 0; }
@@ -200,7 +187,7 @@ struct Gather {
     Smem<DP>& sm;
     int* abort;
     const int warp, lane;
-    uint32_t fill = 0, looked = 0;      // stages filled, and looked through, so far
+    uint32_t fill = 0, cleared = 0;      // stages filled so far, and stages of values that rows were taken out of
     uint32_t waiting0 = 0, waiting1 = 0;      // barriers of row copies that are on their way
     int n_waiting = 0;
     bool alive = true;
@@ -242,29 +229,17 @@ struct Gather {
     __device__ __forceinline__ uint32_t place(uint32_t stage, int r, int c) const {
         return stage + (c >> 3) * (kTile * 128) + (warp * 32 + r) * 128 + (((c & 7) ^ (r & 7)) << 4);
     }
-    // values of a tile that not every row sees: rows that hold a NaN or an infinity become zeros, and are told
-    __device__ __forceinline__ void look_through(uint32_t stage, int part, uint32_t* odd) {
+    // rows of this warp's that are not there become zeros: a box brings whatever the page holds
+    __device__ __forceinline__ void clear(uint32_t stage, uint32_t there) {
         const int c = lane % kChunks, r0 = lane / kChunks;
-        const bool in = part * C::kCols + c * 8 < a.dh;
-        uint32_t mine = 0;
-#pragma unroll 4
         for (int i = 0; i < 32 / kAtOnce; ++i) {
             const int r = i * kAtOnce + r0;
-            uint4 v;
-            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(place(stage, r, c)));
-            if (in && (odd_word(v.x) || odd_word(v.y) || odd_word(v.z) || odd_word(v.w))) mine |= 1u << r;
+            if (!(there >> r & 1u)) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(place(stage, r, c)), "r"(0) : "memory");
         }
-        mine = __reduce_or_sync(0xffffffffu, mine);
-        if (mine) {
-            for (int i = 0; i < 32 / kAtOnce; ++i) {
-                const int r = i * kAtOnce + r0;
-                if (in && (mine >> r & 1u)) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(place(stage, r, c)), "r"(0) : "memory");
-            }
-        }
-        if (lane == 0) odd[warp] = mine;
     }
-    // 128 keys x kCols columns.  page: of this lane's key, n_pages: none, which reads as zeros; pos: of the tile; odd: told, or null.
-    __device__ __forceinline__ void stage(const CUtensorMap* map, const void* cache, int page, int pos, int kvh, int part, uint32_t* odd) {
+    // 128 keys x kCols columns.  page: of this lane's key, n_pages: none, which reads as zeros; pos: of the tile; there: which of
+    // this warp's rows are, the others have to be zeros.
+    __device__ __forceinline__ void stage(const CUtensorMap* map, const void* cache, int page, int pos, int kvh, int part, uint32_t there) {
         const uint32_t s = fill % C::kStages, phase = fill / C::kStages;
         await(&sm.bars.empty[s], phase + 1);     // the phase before: passes at once the first time
         if (!alive) return;
@@ -275,15 +250,15 @@ struct Gather {
             const int boxes = 32 / maps.box_rows, blocks = min(C::kCols / 64, (a.dh - part * C::kCols + 63) / 64);
             const int box = lane % boxes, block = lane / boxes, row = box * maps.box_rows;
             const int from = __shfl_sync(0xffffffffu, page, row), at = first + row;
-            uint64_t* bar = odd ? &sm.bars.raw[warp] : &sm.bars.full[s];
+            uint64_t* bar = there != 0xffffffffu ? &sm.bars.raw[warp] : &sm.bars.full[s];
             if (lane == 0) mbar_arrive_expect_tx(bar, blocks * 32 * 128);
             __syncwarp();
             if (block < blocks)
                 tma_load_4d(dst + block * (kTile * 128) + (warp * 32 + row) * 128, map, part * C::kCols + block * 64,
                             a.page_shift >= 0 ? at & (a.page_size - 1) : at % a.page_size, kvh, from, smem_u32(bar));
-            if (odd) {
-                alive = warp_wait(bar, looked++, abort) && alive;
-                look_through(dst, part, odd);
+            if (there != 0xffffffffu) {
+                alive = warp_wait(bar, cleared++, abort) && alive;
+                clear(dst, there);
                 signal(full);
             }
             return;
@@ -299,17 +274,9 @@ struct Gather {
             const long long from = __shfl_sync(0xffffffffu, at, r);
             if (in) cp_async16(place(dst, r, c), from >= 0 ? src + from : src, from >= 0);
         }
-        if (!odd) {
-            issued(full);
-            return;
-        }
-        cp_commit();
-        cp_wait<0>();
-        flush();
-        look_through(dst, part, odd);
-        signal(full);
+        issued(full);
     }
-    __device__ __forceinline__ void queries(const Walk<C::kRows, kTile>& w, const Piece<DP>& p, uint32_t piece) {
+    __device__ __forceinline__ void queries(const Walk<C::kRows, kTile, kOver>& w, const Piece<DP>& p, uint32_t piece) {
         await(&sm.bars.q_empty, piece + 1);
         if (!alive) return;
         const uint32_t q = smem_u32(sm.q), full = smem_u32(&sm.bars.q_full);
@@ -322,7 +289,7 @@ struct Gather {
             __syncwarp();
             if (lane < mine) {
                 const int box = lane * 4 + warp, t = box / blocks, block = box - t * blocks;
-                const int token = w.r.first + static_cast<int>((static_cast<long long>(w.rb) * C::kRows + t * 128) / a.G);
+                const int token = w.r.first + (w.rb * C::kRows + t * 128) / a.G;
                 tma_load_3d(q + t * C::kQTile + block * (128 * 128), &maps.q, block * 64, w.kvh * a.G, token, full);
             }
             return;
@@ -347,7 +314,7 @@ struct Gather {
         __syncwarp();      // q_row may be written again
         issued(full);
     }
-    __device__ void run(Walk<C::kRows, kTile> w) {
+    __device__ void run(Walk<C::kRows, kTile, kOver> w) {
         bool bad = false;
         uint32_t tile = 0, piece = 0;
         while (w.left > 0 && alive) {
@@ -373,11 +340,10 @@ struct Gather {
                 // the slot's last readers are done: their P went into a product behind which stages were freed for this tile
                 if (lane == 0) sm.flags.there[tile % kFlags][warp] = there;
                 const int from = ok ? page : a.n_pages;
-                const bool check = p.partial(w.t0 + j);
 #pragma unroll
-                for (int h = 0; h < C::kParts; ++h) stage(&maps.K, a.K, from, pos, w.kvh, h, nullptr);
+                for (int h = 0; h < C::kParts; ++h) stage(&maps.K, a.K, from, pos, w.kvh, h, 0xffffffffu);      // scores of absent keys are masked
 #pragma unroll
-                for (int h = 0; h < C::kParts; ++h) stage(&maps.V, a.V, from, pos, w.kvh, h, check ? sm.flags.odd[tile % kFlags][h] : nullptr);
+                for (int h = 0; h < C::kParts; ++h) stage(&maps.V, a.V, from, pos, w.kvh, h, there);
                 if (!asked && alive) {
                     queries(w, p, piece);
                     asked = true;
@@ -400,7 +366,7 @@ using Const = std::integral_constant<int, N>;
 // One warp, one lane of which issues.  Lanes (of barriers) are constants, so that counters and addresses stay in registers: the tensor cores take a product of 16
 // columns in 64 clocks, and one must not take longer to issue.
 template <int DP>
-__device__ void issue_products(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, kTile> w) {
+__device__ void issue_products(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, kTile, kOver> w) {
     using C = Cfg<DP>;
     Bars& bars = sm.bars;
     int* abort = &bars.abort;
@@ -413,7 +379,7 @@ __device__ void issue_products(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows,
     while (w.left > 0) {
         const Piece<DP> p(a, w);
         if (p.n > 0) {
-            if (!warp_wait(&bars.q_full, piece++, abort)) return;      // from here on piece counts from 1
+            if (!warp_wait(&bars.q_full, piece++, abort)) return;
             // stream t, lane b, tile j; end: the last stream's, after which the stages are free
             const auto scores = [&](auto t_, auto b_, int j, bool end) {
                 constexpr int t = decltype(t_)::value, b = decltype(b_)::value, buffer = b != 0;
@@ -454,7 +420,6 @@ __device__ void issue_products(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows,
                 constexpr int t = decltype(t_)::value, b = decltype(b_)::value;
                 if (!warp_wait(&bars.p_full[b], (b == 0 ? use0 : b == 1 ? use1 : use2) - 1, abort)) return false;
                 tcgen05_fence_after_sync();
-                const bool on_top = j > 0 || *reinterpret_cast<volatile uint32_t*>(&bars.o_set[t]) == piece;
 #pragma unroll
                 for (int h = 0; h < C::kParts; ++h) {
                     const uint32_t f = first_fill + (j * 2 + 1) * C::kParts + h, s = f % C::kStages;
@@ -464,7 +429,7 @@ __device__ void issue_products(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows,
                     const uint32_t v = (ring + s * (C::kStage >> 4)) | ((kTile * 128) >> 4) << 16;
 #pragma unroll
                     for (int e = 0; e < kTile / 16; ++e)
-                        umma_ts(lead, tmem + C::kO + t * DP + h * C::kCols, tmem + (b != 0) * 128 + e * 8, v + e * 128, idesc, on_top || e > 0);
+                        umma_ts(lead, tmem + C::kO + t * DP + h * C::kCols, tmem + (b != 0) * 128 + e * 8, v + e * 128, idesc, j > 0 || e > 0);
                     if (end) commit(lead, &bars.empty[s]);
                 }
                 commit(lead, &bars.pv_done[b]);
@@ -519,6 +484,11 @@ __device__ __forceinline__ Pair add2(Pair a, Pair b) {
 }
 __device__ __forceinline__ Pair twice(float a) { return pair_of(a, a); }
 // NaN if one of them is
+__device__ __forceinline__ float max2(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -526,10 +496,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 // 2^x of two numbers up to 126 without the special-function unit, which does 16 a clock and SM and bounds the softmax: x = n + f with n
 // the nearest whole number (the low bits of x + 1.5 * 2^23), 2^f by the polynomial of degree 4 with the least largest relative
-// error on [-1/2, 1/2] (2.7e-6, evaluated in fp32; found by linear programming), n into the exponent.  Below -126: 2^-126.
+// error on [-1/2, 1/2] (2.7e-6, evaluated in fp32; found by linear programming), n into the exponent.  Below -126: 2^-126; NaN: NaN or
+// more than 2^127.
 __device__ __forceinline__ float2 pow2_by_polynomial(Pair x) {
     const float2 low = both(x);
-    x = pair_of(fmaxf(low.x, -126.0f), fmaxf(low.y, -126.0f));
+    x = pair_of(max2(low.x, -126.0f), max2(low.y, -126.0f));
     const Pair shifted = add2(x, twice(12582912.0f)), f = fma2(add2(shifted, twice(-12582912.0f)), twice(-1.0f), x);
     Pair y = fma2(twice(0.009569705463945866f), f, twice(0.05591819807887077f));
     y = fma2(y, f, twice(0.24024765193462372f));
@@ -542,58 +513,86 @@ __device__ __forceinline__ float2 pow2_by_polynomial(Pair x) {
 
 // ---- rows -----------------------------------------------------------------------------------------------------------------------
 
-// The value rows that were taken out of a tile's stage, for the rows that see them: O += p * v, before the tile's product.
-template <int DP>
-__device__ __noinline__ void add_odd_rows(const Args& a, const Smem<DP>& sm, int s, int kvh, int p0, int sees, uint32_t slot, uint32_t p_addr, uint32_t o_addr) {
-    using C = Cfg<DP>;
-    for (int h = 0; h < C::kParts; ++h)
-        for (int q = 0; q < 4; ++q) {
-            uint32_t left = sm.flags.odd[slot][h][q];
-            while (left) {
-                const int i = q * 32 + __ffs(left) - 1;
-                left &= left - 1;
-                const uint32_t pair = tmem_ld_word(p_addr + i / 2);
-                tmem_ld_wait();
-                const float p = __uint_as_float(i & 1 ? pair & 0xffff0000u : pair << 16);
-                const int at = p0 + i, pi = at / a.page_size;
-                const int page = ldg_waited(a.table + static_cast<long long>(s) * a.max_pages + pi);
-                const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.V) + static_cast<long long>(page) * a.page_stride +
-                                         (static_cast<long long>(kvh) * a.page_size + (at - pi * a.page_size)) * a.dh;
-                for (int c = h * C::kCols; c < min(a.dh, (h + 1) * C::kCols); c += 16) {
-                    uint32_t o[16];
-                    tmem_ld_32x16(o_addr + c, o);
-                    tmem_ld_wait();
+// One element of the caches
+__device__ __forceinline__ float cache_at(const Args& a, const void* cache, const uint8_t* scale, int page, int kvh, int in_page, int c) {
+    const long long row = static_cast<long long>(kvh) * a.page_size + in_page, at = page * a.page_stride + row * a.dh + c;
+    if (!a.K_scale) return __bfloat162float(static_cast<const __nv_bfloat16*>(cache)[at]);
+    float f[4];
+    eight_widen(static_cast<const uint8_t*>(cache)[at], f);
+    return f[0] * eight_unit(scale[static_cast<long long>(page) * a.Hk * a.page_size + row]);
+}
+
+// A row's weighted sum of values over the positions p0 to p1 - 1 of sequence s, key by key: a lane has a key for its score, and columns
+// lane, lane + 32, ... for the sums.  By a whole warp; to: fp32, every `step` floats four columns, or bf16 (step 0) times f.
+__device__ __noinline__ void resum(const Args& a, int s, int kvh, int token, int head, int p0, int p1, float base, float f, void* to, long long step) {
+    const int lane = threadIdx.x & 31;
+    const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + static_cast<long long>(token) * a.q_stride + static_cast<long long>(head) * a.dh;
+    float o[8] = {};
+    for (int p = p0; p < p1; p += 32) {
+        const int at = p + lane, pi = at / a.page_size, in_page = at - pi * a.page_size;
+        int page = at < p1 ? ldg_waited(a.table + static_cast<long long>(s) * a.max_pages + pi) : -1;
+        if (page < 0 || page >= a.n_pages) page = -1;
+        float score = 0.0f;
+        if (page >= 0)
+            for (int c = 0; c < a.dh; ++c) score = fmaf(__bfloat162float(q[c]), cache_at(a, a.K, a.K_scale, page, kvh, in_page, c), score);
+        const float w = page >= 0 ? __bfloat162float(__float2bfloat16_rn(pow2(fmaf(score, a.scale_log2, -base)))) : 0.0f;
+        for (int k = 0; k < 32; ++k) {
+            const int from = __shfl_sync(0xffffffffu, page, k), in = __shfl_sync(0xffffffffu, in_page, k);
+            const float x = __shfl_sync(0xffffffffu, w, k);
+            if (from < 0) continue;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (at < sees) o[e] = __float_as_uint(fmaf(p, a.K_scale ? __uint_as_float(0x7fc00000u) : __bfloat162float(v[c + e]), __uint_as_float(o[e])));
-                    tmem_st_32x16(o_addr + c, o);
-                    tmem_st_wait();
-                }
-            }
+            for (int e = 0; e < 8; ++e)
+                if (lane + e * 32 < a.dh) o[e] = fmaf(x, cache_at(a, a.V, a.V_scale, from, kvh, in, lane + e * 32), o[e]);
         }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int c = lane + e * 32;
+        if (c >= a.dh) continue;
+        if (step) static_cast<float*>(to)[c / 4 * step + c % 4] = o[e];
+        else static_cast<__nv_bfloat16*>(to)[c] = __float2bfloat16_rn(o[e] * f);
+    }
+}
+
+// Four lanes with four 16-byte words each, of the rows l, to a word each of four rows: 2 x 2 blocks, then halves of them.  Stores of
+// 64 bytes of a row by four neighbours instead of 16 bytes of 32 rows.
+__device__ __forceinline__ void turn_words(uint4 (&w)[4], int lane) {
+#pragma unroll
+    for (int d = 1; d < 4; d <<= 1) {
+        const bool upper = lane & d;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i & d) continue;
+            uint4 send = upper ? w[i] : w[i + d];
+            send.x = __shfl_xor_sync(0xffffffffu, send.x, d);
+            send.y = __shfl_xor_sync(0xffffffffu, send.y, d);
+            send.z = __shfl_xor_sync(0xffffffffu, send.z, d);
+            send.w = __shfl_xor_sync(0xffffffffu, send.w, d);
+            if (upper) w[i] = send;
+            else w[i + d] = send;
+        }
+    }
 }
 
 template <int DP>
-__device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, kTile> w, long long total) {
+__device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, kTile, kOver> w, long long total) {
     using C = Cfg<DP>;
-    constexpr float kSlack = 8.0f;      // powers of two that a maximum may lag behind
+    constexpr float kSlack = 8.0f;            // powers of two that a reference may lag behind where it is looked at
+    constexpr float kSum = 1048576.0f;        // what a tile's weights may sum to before it is
     Bars& bars = sm.bars;
     int* abort = &bars.abort;
     const int t = threadIdx.x >> 7, i = threadIdx.x & 127, lane = threadIdx.x & 31, item_row = t * 128 + i;
     const uint32_t lanes = bars.tmem + (static_cast<uint32_t>(i & ~31) << 16);
     const uint32_t o_addr = lanes + C::kO + t * DP;
     const float scale = fabsf(a.scale_log2);
-    const long long range = w.left;
-    uint32_t tile = 0, piece = 0, used[kLanes] = {0, 0, 0};      // of the lanes of this stream
+    uint32_t tile = 0, used[kLanes] = {0, 0, 0};      // tiles so far; of the lanes of this stream
     bool alive = true;
     while (w.left > 0 && alive) {
         const Piece<DP> p(a, w);
-        if (p.n > 0) ++piece;
         if (t < p.streams) {
             const Row row = row_at<C::kRows>(a, w.r, w.kvh, w.rb, item_row);
-            const int first = w.r.len - w.r.n + 1, n = p.tiles[t];
-            const int sees = first + row.token - w.r.first;      // kept or not
-            const int all_see = first + static_cast<int>((static_cast<long long>(w.rb) * C::kRows + t * 128) / a.G);
+            const int n = p.tiles[t];
+            const int all_see = w.r.len - w.r.n + 1 + (w.rb * C::kRows + t * 128) / a.G;
             float m = -INFINITY, l = 0.0f;
             const auto await_sums = [&](int j) {      // of tile j, the last one that was counted in its lane
                 const int b = p.lane(t, j);
@@ -602,109 +601,91 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
             };
             for (int j = 0; j < n && alive; ++j) {
                 const int b = p.lane(t, j), p0 = (w.t0 + j) * kTile;
-                const uint32_t slot = (tile + j) % kFlags, fill = (tile + j) * 2 * C::kParts;
                 alive = warp_wait(&bars.s_full[b], used[b], abort);
                 if (!alive) break;
                 tcgen05_fence_after_sync();
                 const uint32_t s_addr = lanes + p.buffer(b) * 128;
-                uint32_t sc[4][32];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld_32x32(s_addr + c * 32, sc[c]);
                 uint32_t there[4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) there[c] = *const_cast<volatile const uint32_t*>(&sm.flags.there[slot][c]);
+                for (int c = 0; c < 4; ++c) there[c] = *const_cast<volatile const uint32_t*>(&sm.flags.there[(tile + j) % kFlags][c]);
+                uint32_t sc[4][32], pk[4][16];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld_32x32(s_addr + c * 32, sc[c]);
                 tmem_ld_wait();
                 const bool masked = p0 + kTile > all_see || (there[0] & there[1] & there[2] & there[3]) != 0xffffffffu;
-                if (masked) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const int left = sees - p0 - c * 32;
-                        const uint32_t in = left >= 32 ? there[c] : left <= 0 ? 0u : there[c] & ((1u << left) - 1u);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (!(in >> e & 1u)) sc[c][e] = 0xff800000u;
-                    }
-                }
-                float most[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) most[c] = max3(__uint_as_float(sc[c][0]), __uint_as_float(sc[c][1]), __uint_as_float(sc[c][2]));
-#pragma unroll
-                for (int e = 3; e < 31; e += 2)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) most[c] = max3(most[c], __uint_as_float(sc[c][e]), __uint_as_float(sc[c][e + 1]));
-#pragma unroll
-                for (int c = 0; c < 4; ++c) most[c] = max3(most[c], most[c], __uint_as_float(sc[c][31]));
-                const float mx = max3(max3(most[0], most[1], most[2]), most[3], most[3]);
-                if (__any_sync(0xffffffffu, (mx - m) * scale > kSlack)) {
-                    const float to = fmaxf(m, mx), f = m == -INFINITY ? 0.0f : pow2((m - to) * scale);
-                    if (j > 0) {
-                        await_sums(j - 1);
-                        if (!alive) break;
-                        for (int c = 0; c < a.dh; c += 16) {
-                            uint32_t o[16];
-                            tmem_ld_32x16(o_addr + c, o);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                            tmem_st_32x16(o_addr + c, o);
-                        }
-                    }
-                    l *= f;
-                    m = to;
-                }
-                const float base = m == -INFINITY ? 0.0f : m * scale;
-                const Pair times = twice(scale), minus = twice(-base);
-                Pair sum[2] = {0, 0};
-                // A quarter of the powers by polynomial, unless something is masked, infinite or NaN: those have to come out exactly.
+                Pair sum[2];
                 const auto weights = [&](auto by_polynomial) {
+                    const Pair times = twice(scale), minus = twice(m == -INFINITY ? 0.0f : -m * scale);
+                    sum[0] = sum[1] = 0;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t pk[16];
+                    for (int c = 0; c < 4; ++c)
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             const Pair x = fma2(pair_of(__uint_as_float(sc[c][2 * e]), __uint_as_float(sc[c][2 * e + 1])), times, minus);
                             float2 y;
-                            if (decltype(by_polynomial)::value && e % 4 == 3) {
+                            // 6 of 16: as long as the special-function unit takes for the others
+                            if (decltype(by_polynomial)::value && e * 6 / 16 != (e + 1) * 6 / 16) {
                                 y = pow2_by_polynomial(x);
                             } else {
                                 y = both(x);
                                 y = make_float2(pow2(y.x), pow2(y.y));
                             }
                             sum[e & 1] = add2(sum[e & 1], pair_of(y.x, y.y));
-                            pk[e] = pack_bf16(y.x, y.y);
+                            pk[c][e] = pack_bf16(y.x, y.y);
                         }
-                        tmem_st_32x16(s_addr + c * 16, pk);
-                    }
-                };
-                if (!masked && __all_sync(0xffffffffu, fabsf(mx) < INFINITY)) weights(Const<1>());
-                else weights(Const<0>());
-                {
                     const float2 s0 = both(sum[0]), s1 = both(sum[1]);
-                    l += (s0.x + s0.y) + (s1.x + s1.y);
-                }
-                tmem_st_wait();
-                if (p.partial(w.t0 + j)) {
-                    uint32_t odd = 0;
+                    return (s0.x + s0.y) + (s1.x + s1.y);
+                };
+                float more = INFINITY;
+                if (!masked && __all_sync(0xffffffffu, m > -INFINITY)) more = weights(Const<1>());
+                if (__any_sync(0xffffffffu, !(more < kSum))) {
+                    // masks, a new reference, or something infinite or NaN: from the scores again, exactly
 #pragma unroll
-                    for (int h = 0; h < C::kParts; ++h) {      // the stage is not filled again before this tile's products
-                        const uint32_t f = fill + C::kParts + h;
-                        alive = warp_wait(&bars.full[f % C::kStages], f / C::kStages, abort) && alive;
+                    for (int c = 0; c < 4; ++c) tmem_ld_32x32(s_addr + c * 32, sc[c]);
+                    tmem_ld_wait();
+                    if (masked) {
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) odd |= *const_cast<volatile const uint32_t*>(&sm.flags.odd[slot][h][q]);
+                        for (int c = 0; c < 4; ++c) {
+                            const int left = row.sees - p0 - c * 32;
+                            const uint32_t in = left >= 32 ? there[c] : left <= 0 ? 0u : there[c] & ((1u << left) - 1u);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!(in >> e & 1u)) sc[c][e] = 0xff800000u;
+                        }
                     }
-                    if (odd && alive) {
+                    float most[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) most[c] = max3(__uint_as_float(sc[c][0]), __uint_as_float(sc[c][1]), __uint_as_float(sc[c][2]));
+#pragma unroll
+                    for (int e = 3; e < 31; e += 2)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) most[c] = max3(most[c], __uint_as_float(sc[c][e]), __uint_as_float(sc[c][e + 1]));
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) most[c] = max2(most[c], __uint_as_float(sc[c][31]));
+                    const float mx = max2(max3(most[0], most[1], most[2]), most[3]);
+                    if (__any_sync(0xffffffffu, (mx - m) * scale > kSlack)) {      // not where it is NaN: all weights of the row are
+                        const float to = fmaxf(m, mx), f = m == -INFINITY ? 0.0f : pow2((m - to) * scale);
                         if (j > 0) {
                             await_sums(j - 1);
                             if (!alive) break;
-                        } else {
-                            const uint32_t zero[16] = {};
-                            for (int c = 0; c < a.dh; c += 16) tmem_st_32x16(o_addr + c, zero);
-                            tmem_st_wait();
-                            *const_cast<volatile uint32_t*>(&bars.o_set[t]) = piece;
+                            for (int c = 0; c < a.dh; c += 16) {
+                                uint32_t o[16];
+                                tmem_ld_32x16(o_addr + c, o);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                tmem_st_32x16(o_addr + c, o);
+                            }
                         }
-                        add_odd_rows<DP>(a, sm, w.s, w.kvh, p0, sees, slot, s_addr, o_addr);
+                        l *= f;
+                        m = to;
                     }
+                    more = weights(Const<0>());
                 }
+                l += more;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_st_32x16(s_addr + c * 16, pk[c]);
+                tmem_st_wait();
                 ++used[b];
                 tcgen05_fence_before_sync();
                 __syncwarp();
@@ -713,33 +694,47 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
             if (n > 0 && alive) await_sums(n - 1);
             if (!alive) break;
             const bool some = l != 0.0f && row.kept;
-            if (w.complete()) {
-                const long long at = static_cast<long long>(row.token) * a.H + row.head;
-                const float f = some ? 1.0f / l : 0.0f;
-                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + at * a.dh;
-                for (int c = 0; c < a.dh; c += 16) {
-                    uint32_t o[16];
+            const long long at = static_cast<long long>(row.token) * a.H + row.head;
+            const float f = some ? 1.0f / l : 0.0f, base = m == -INFINITY ? 0.0f : m * scale;
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + at * a.dh;
+            float* slot = w.slot(a) + 2ll * a.rows + static_cast<long long>(item_row) * 4;
+            const bool complete = w.complete();
+            bool odd = false;
+            if (complete) {
+                const long long mine = row.there ? at * a.dh : -1;
+                long long rows[4];      // of the four lanes' rows of the output
+#pragma unroll
+                for (int q = 0; q < 4; ++q) rows[q] = __shfl_sync(0xffffffffu, mine, (lane & ~3) + q);
+                for (int c = 0; c < a.dh; c += 32) {
+                    uint32_t o[2][16] = {};
                     if (n > 0) {
-                        tmem_ld_32x16(o_addr + c, o);
+                        tmem_ld_32x16(o_addr + c, o[0]);
+                        if (c + 16 < a.dh) tmem_ld_32x16(o_addr + c + 16, o[1]);
                         tmem_ld_wait();
                     }
-                    if (row.there) {
+                    uint4 y[4];
 #pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            uint32_t y[4];
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t v[4];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                y[e] = some ? pack_bf16(__uint_as_float(o[8 * q + 2 * e]) * f, __uint_as_float(o[8 * q + 2 * e + 1]) * f) : 0u;
-                            *reinterpret_cast<uint4*>(out + c + 8 * q) = make_uint4(y[0], y[1], y[2], y[3]);
+                        for (int e = 0; e < 4; ++e) {
+                            const float x = __uint_as_float(o[q >> 1][(q & 1) * 8 + 2 * e]), z = __uint_as_float(o[q >> 1][(q & 1) * 8 + 2 * e + 1]);
+                            odd |= !(fabsf(x) < INFINITY) || !(fabsf(z) < INFINITY);
+                            v[e] = some ? pack_bf16(x * f, z * f) : 0u;
                         }
+                        y[q] = make_uint4(v[0], v[1], v[2], v[3]);
                     }
+                    turn_words(y, lane);
+                    const int col = c + (lane & 3) * 8;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (rows[q] >= 0 && col < a.dh) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + rows[q] + col) = y[q];
                 }
                 if (row.there && a.lse) a.lse[at] = some ? (m * scale + log2f(l)) * kLn2 : -INFINITY;
             } else {
-                float* slot = a.ws + (static_cast<long long>(blockIdx.x) * 2 + (w.left == range ? 0 : 1)) * a.slot;
                 if (row.there) {
-                    slot[item_row] = m * scale;
-                    slot[a.rows + item_row] = l;
+                    w.slot(a)[item_row] = m * scale;
+                    w.slot(a)[a.rows + item_row] = l;
                 }
                 for (int c = 0; c < a.dh; c += 16) {
                     uint32_t o[16] = {};
@@ -747,17 +742,29 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
                         tmem_ld_32x16(o_addr + c, o);
                         tmem_ld_wait();
                     }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) odd |= !(fabsf(__uint_as_float(o[e])) < INFINITY);
                     if (row.there) {
 #pragma unroll
                         for (int q = 0; q < 4; ++q)
-                            reinterpret_cast<uint4*>(slot + 2 * a.rows)[static_cast<long long>(c / 4 + q) * a.rows + item_row] =
-                                make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+                            *reinterpret_cast<uint4*>(slot + (c / 4 + q) * 4ll * a.rows) = make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
                     }
                 }
             }
+            // a value that is infinite or NaN, in a tile that the row does not see all of: what it does see, on its own
+            uint32_t again = __ballot_sync(0xffffffffu, odd && some && fabsf(l) < INFINITY && (w.t0 + n) * kTile > all_see);
+            while (again) {
+                const int q = __ffs(again) - 1;
+                again &= again - 1;
+                const int p1 = min((w.t0 + n) * kTile, row.sees);
+                const unsigned long long to = reinterpret_cast<unsigned long long>(complete ? static_cast<void*>(out) : static_cast<void*>(slot));
+                resum(a, w.s, w.kvh, __shfl_sync(0xffffffffu, row.token, q), __shfl_sync(0xffffffffu, row.head, q), w.t0 * kTile,
+                      __shfl_sync(0xffffffffu, p1, q), __shfl_sync(0xffffffffu, base, q), __shfl_sync(0xffffffffu, f, q),
+                      reinterpret_cast<void*>(__shfl_sync(0xffffffffu, to, q)), complete ? 0 : 4ll * a.rows);
+                __syncwarp();
+            }
         }
-        if (threadIdx.x == 0 && w.left == w.t1 - w.t0)   // the range's last piece
-            a.openings[blockIdx.x] = {w.t0 == 0 && w.t1 < w.nt, w.s, w.kvh, w.rb, w.nt - w.t1, w.left == range, total};
+        if (threadIdx.x == 0 && w.opens()) a.openings[blockIdx.x] = w.opening(total);
         tile += p.n;
         w.next(a);
     }
@@ -771,11 +778,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __g
     Bars& bars = sm.bars;
     const int tid = threadIdx.x, warp = tid >> 5;
     chain_wait();
-    const Found<C::kRows, kTile> f = locate<C::kRows, kTile, kThreads>(a, sm.sh);
-    if (f.walk.left <= 0) {      // the same in every thread
-        if (f.total == 0 && blockIdx.x == 0 && tid == 0) a.openings[0] = {0, 0, 0, 0, 0, 0, 0};
-        return;
-    }
+    const Found<C::kRows, kTile, kOver> f = locate<C::kRows, kTile, kOver, kThreads>(a, sm.sh);
+    if (f.walk.left <= 0) return;      // the same in every thread
     if (tid == 0) {
         for (int i = 0; i < C::kStages; ++i) {
             mbar_init(&bars.full[i], 4);      // the gathering warps
@@ -789,7 +793,6 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __g
             mbar_init(&bars.pv_done[b], 1);
         }
         for (int i = 0; i < 4; ++i) mbar_init(&bars.raw[i], 1);
-        bars.o_set[0] = bars.o_set[1] = 0;
         bars.abort = 0;
         mbar_fence_init();
     }
@@ -822,10 +825,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __g
 
 template <int DP>
 int blocks_of(const halo_paged_shape& sh, int n_tok, int n_seq) {
-    const long long G = sh.n_heads / sh.n_kv_heads, cap = static_cast<long long>(sh.max_pages) * sh.page_size;
-    const long long items = (n_tok * G / Cfg<DP>::kRows + (n_seq < n_tok ? n_seq : n_tok) + 1) * sh.n_kv_heads;
-    const long long pieces = items * ((cap + kTile - 1) / kTile) / kMinTiles;
-    return static_cast<int>(pieces < 1 ? 1 : pieces < kSmCount ? pieces : kSmCount);
+    return line_blocks(sh, n_tok, n_seq, Cfg<DP>::kRows, kTile, kOver, kSmCount);
 }
 template <typename F>
 auto by_width(const halo_paged_shape& sh, F f) {

@@ -2,12 +2,13 @@
 //
 // An item is ROWS rows of one (sequence, K/V head): row token * G + g of them is query head g of the G that share the K/V head, so
 // keys and values that come into an SM serve all of them.  Its keys, up to the last position that a row sees, are cut
-// into tiles of TILE.  All tiles of all items, item after item, form one line of T tiles and thread block c of C takes
-// [c * T / C, (c + 1) * T / C): however long prompts and caches are, every thread block sums the same number of tiles, and
-// few rows over a long cache fill the GPU as well as many.  A piece that covers a whole item writes its output; the at most two
-// pieces of a range that do not (its first and its last) leave (maximum, sum, weighted sum of values) per row in the workspace, and
-// a second kernel joins them in line order, so results do not depend on timing.  Every thread block computes the line from
-// q_start and seq_len itself; the host never reads a length.
+// into tiles of TILE.  An item is as many units long as it has tiles, and OVER more in front of them, which stand for what
+// an item costs besides (its rows, an empty pipeline, its outputs).  All items, one after another, form one line of T units and thread
+// block c of C takes [c * T / C, (c + 1) * T / C): however long prompts and caches are, every thread block has the same to do, and
+// few rows over a long cache fill the GPU as well as many.  A piece that has all of an item's tiles writes its output; the at
+// most two pieces of a range that do not leave (maximum, sum, weighted sum of values) per row in the workspace, and a second kernel
+// joins them in line order, so results do not depend on timing.  Every thread block computes the line from q_start and seq_len
+// itself; the host never reads a length.
 #pragma once
 
 #include "eight.cuh"
@@ -17,10 +18,11 @@ namespace prompt {
 
 // What the join has to know of a range whose last piece begins an item that it does not end.
 struct __align__(16) Opening {
-    int opens, s, kvh, rb;
-    int rest, fills;      // tiles of the item behind the range; the item's first piece is the whole range
-    long long total;      // T
+    int opens, kvh, rb, first, n;   // the item, its sequence's rows of q
+    int rest;                       // units of the item behind the range
+    long long total;                // T
 };
+static_assert(sizeof(Opening) == 32, "two 16-byte words");
 
 struct Args {
     int n_tok, n_seq, H, Hk, G, dh, page_size, page_shift, n_pages, max_pages;   // page_shift: -1 = no power of two
@@ -74,57 +76,57 @@ __device__ __forceinline__ Rows rows_of(const Args& a, int s, bool flag) {
     return {q0, rows ? q1 - q0 : 0, fits ? len : 0};
 }
 
-// sum over i < n of floor((step * i + from) / m), by exchanging the roles of step and m until nothing is left (Euclid's way)
-__device__ __forceinline__ unsigned long long sum_of_floors(unsigned long long n, unsigned long long m, unsigned long long step,
-                                                            unsigned long long from) {
+// sum over i < n of floor((step * i + from) / m), by exchanging the roles of step and m until nothing is left (Euclid's way);
+// step * n + from < 2^32
+__device__ __forceinline__ unsigned long long sum_of_floors(uint32_t n, uint32_t m, uint32_t step, uint32_t from) {
     unsigned long long sum = 0;
     while (n > 0) {
-        sum += n * (n - 1) / 2 * (step / m) + n * (from / m);
+        sum += static_cast<unsigned long long>(n) * (n - 1) / 2 * (step / m) + static_cast<unsigned long long>(n) * (from / m);
         step %= m;
         from %= m;
-        const unsigned long long top = step * n + from;
+        const uint32_t top = step * n + from;
         n = top / m;
-        from = top % m;
-        const unsigned long long t = m;
+        from = top - n * m;
+        const uint32_t t = m;
         m = step;
-        step = t;
-        if (m == 0) break;      // n is 0 then
+        step = t;      // m = 0: n is 0 too
     }
     return sum;
 }
 
-template <int ROWS, int TILE>
+// Rows times heads of a call stay below 2^30 (HALO_MAX_PROMPT_ROWS, HALO_MAX_GROUPS).
+template <int ROWS, int TILE, int OVER>
 struct Line {
-    static __device__ __forceinline__ int blocks_of(const Args& a, const Rows& r) {
-        return static_cast<int>((static_cast<long long>(r.n) * a.G + ROWS - 1) / ROWS);
-    }
+    static __device__ __forceinline__ int blocks_of(const Args& a, const Rows& r) { return (r.n * a.G + ROWS - 1) / ROWS; }
     // positions that the last row of an item sees
     static __device__ __forceinline__ int reach(const Args& a, const Rows& r, int rb) {
-        const long long u = (rb + 1ll) * ROWS - 1, all = static_cast<long long>(r.n) * a.G - 1;
-        const int token = u < all ? static_cast<int>(u / a.G) : r.n - 1;
-        return max(r.len - r.n + token + 1, 0);
+        const int u = (rb + 1) * ROWS - 1, all = r.n * a.G - 1;
+        return max(r.len - r.n + (u < all ? u / a.G : r.n - 1) + 1, 0);
     }
-    static __device__ __forceinline__ int tiles(const Args& a, const Rows& r, int rb) {
-        return max((reach(a, r, rb) + TILE - 1) / TILE, 1);     // an item that sees nothing keeps one tile, which writes its zeros
-    }
-    // tiles of all items of one K/V head of a sequence
-    static __device__ __forceinline__ long long tiles_per_head(const Args& a, const Rows& r) {
+    // an item that sees nothing keeps one tile, which writes its zeros
+    static __device__ __forceinline__ int tiles_of(int reach) { return reach > 0 ? (reach - 1) / TILE + 1 : 1; }
+    static __device__ __forceinline__ int tiles(const Args& a, const Rows& r, int rb) { return tiles_of(reach(a, r, rb)); }
+    // units of all items of one K/V head of a sequence
+    static __device__ __forceinline__ long long per_head(const Args& a, const Rows& r) {
         if (r.n == 0) return 0;
-        const long long nb = blocks_of(a, r), last = tiles(a, r, static_cast<int>(nb - 1));
-        if (nb == 1) return last;
-        // item rb < nb - 1: max(1, floor((ROWS * (rb + 1) - 1 + G * (len - n + TILE)) / (G * TILE)))
-        const long long m = static_cast<long long>(a.G) * TILE, base = static_cast<long long>(r.len - r.n) * a.G;
-        long long ones = base < 0 ? (-base) / ROWS : 0;          // items of which no row sees anything
-        if (ones > nb - 1) ones = nb - 1;
-        return last + ones + static_cast<long long>(sum_of_floors(nb - 1 - ones, m, ROWS, ROWS * (ones + 1) - 1 + base + m));
+        const int nb = blocks_of(a, r), last = tiles_of(r.len);
+        if (nb == 1) return last + OVER;
+        // item rb < nb - 1: max(1, floor((ROWS * (rb + 1) - 1 + G * (base + TILE)) / (G * TILE))), base = len - n; base = TILE * q + rest
+        const int base = r.len - r.n, m = a.G * TILE;
+        int ones = base < 0 ? static_cast<int>(min(-static_cast<long long>(base) * a.G / ROWS, nb - 1ll)) : 0;      // items of which no row sees anything
+        const int q = base >= 0 ? base / TILE : -((TILE - 1 - base) / TILE), rest = base - q * TILE;
+        const int n = nb - 1 - ones;
+        const long long some = n > 0 ? static_cast<long long>(n) * (q + 1) + static_cast<long long>(
+                                           sum_of_floors(n, m, ROWS, ROWS * (ones + 1) - 1 + rest * a.G)) : 0;
+        return last + ones + some + static_cast<long long>(OVER) * nb;
     }
 };
 
-// Thread blocks that have a range, and where the c-th range begins.  A range has at least kMinTiles tiles unless there are fewer: a
+// Thread blocks that have a range, and where the c-th range begins.  A range has at least kMinUnits unless there are fewer: a
 // cut costs two slots of traffic and a join.
-constexpr int kMinTiles = 2;
+constexpr int kMinUnits = 4;
 __device__ __forceinline__ int ranges(long long T, int blocks) {
-    const long long n = T / kMinTiles;
+    const long long n = T / kMinUnits;
     return n < 1 ? 1 : n < blocks ? static_cast<int>(n) : blocks;
 }
 __device__ __forceinline__ long long cut(long long T, int c, int C) { return T * c / C; }
@@ -132,18 +134,21 @@ __device__ __forceinline__ long long cut(long long T, int c, int C) { return T *
 __device__ __forceinline__ int range_of(long long T, long long x, int C) { return static_cast<int>(((x + 1) * C - 1) / T); }
 
 // The way along a range: piece after piece.
-template <int ROWS, int TILE>
+template <int ROWS, int TILE, int OVER>
 struct Walk {
-    using L = Line<ROWS, TILE>;
-    long long left;      // tiles from t0 of this piece to the end of the range
+    using L = Line<ROWS, TILE, OVER>;
+    long long left;      // units from u0 of this item to the end of the range
     Rows r;
     int s, kvh, rb, nb;
-    int nt, t0, t1;      // tiles of the item, of the piece
+    int u0, u1;          // units of the item that the range has
+    int nt, t0, t1;      // tiles of the item, and of them this piece's
     int reach;           // positions that take part: 0 where every head of the item is lost
     __device__ __forceinline__ void item(const Args& a) {
-        nt = L::tiles(a, r, rb);
-        t1 = static_cast<int>(min(static_cast<long long>(nt), t0 + left));
         reach = L::reach(a, r, rb);
+        nt = L::tiles_of(reach);
+        u1 = static_cast<int>(min(static_cast<long long>(nt + OVER), u0 + left));
+        t0 = max(u0 - OVER, 0);
+        t1 = max(u1 - OVER, 0);
         if (a.keep) {
             bool any = false;
             for (int g = 0; g < a.G; ++g) any |= head_kept(a, kvh * a.G + g);
@@ -151,39 +156,48 @@ struct Walk {
         }
     }
     __device__ __forceinline__ bool complete() const { return t0 == 0 && t1 == nt; }
+    __device__ __forceinline__ bool opens() const { return t0 == 0 && t1 < nt; }
     __device__ __forceinline__ void next(const Args& a) {
-        left -= t1 - t0;
-        if (left <= 0) return;
-        t0 = 0;
-        if (++rb == nb) {
-            rb = 0;
-            if (++kvh == a.Hk) {
-                kvh = 0;
-                do r = rows_of(a, ++s, false);
-                while (r.n == 0);      // a range ends with the last item: there is one
-                nb = L::blocks_of(a, r);
+        do {
+            left -= u1 - u0;
+            if (left <= 0) return;
+            u0 = 0;
+            if (++rb == nb) {
+                rb = 0;
+                if (++kvh == a.Hk) {
+                    kvh = 0;
+                    do r = rows_of(a, ++s, false);
+                    while (r.n == 0);      // a range ends with the last item: there is one
+                    nb = L::blocks_of(a, r);
+                }
             }
-        }
-        item(a);
+            item(a);
+        } while (t1 <= t0);      // a piece of the units in front alone: its tiles are the next range's
     }
+    // where the sums of a piece that is not complete go: a range's first piece has no first tile, its last one has
+    __device__ __forceinline__ float* slot(const Args& a) const { return a.ws + (static_cast<long long>(blockIdx.x) * 2 + (t0 > 0 ? 0 : 1)) * a.slot; }
+    __device__ __forceinline__ Opening opening(long long total) const { return {opens(), kvh, rb, r.first, r.n, nt + OVER - u1, total}; }
 };
 
-template <int ROWS, int TILE>
+template <int ROWS, int TILE, int OVER>
 struct Found {
-    Walk<ROWS, TILE> walk;
+    Walk<ROWS, TILE, OVER> walk;
     long long total;
-    int C;
 };
-// The range of this thread block; all its THREADS threads call it.  left = 0: none.
-template <int ROWS, int TILE, int THREADS>
-__device__ __forceinline__ Found<ROWS, TILE> locate(const Args& a, long long* sh /*[THREADS / 32 + 3]*/) {
-    using L = Line<ROWS, TILE>;
+// The range of this thread block; all its THREADS threads call it.  left <= 0: nothing to do.
+template <int ROWS, int TILE, int OVER, int THREADS>
+__device__ __forceinline__ Found<ROWS, TILE, OVER> locate(const Args& a, long long* sh /*[THREADS / 32 + 3]*/) {
+    using L = Line<ROWS, TILE, OVER>;
     constexpr int W = THREADS / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (a.n_seq + THREADS - 1) / THREADS;
     const int s0 = min(tid * per, a.n_seq), s1 = min(s0 + per, a.n_seq);
-    long long own = 0;
-    for (int s = s0; s < s1; ++s) own += L::tiles_per_head(a, rows_of(a, s, blockIdx.x == 0));
+    long long own = 0, first = 0;      // units of one K/V head: of all this thread's sequences, of its first
+    for (int s = s0; s < s1; ++s) {
+        const long long n = L::per_head(a, rows_of(a, s, blockIdx.x == 0));
+        if (s == s0) first = n;
+        own += n;
+    }
     long long incl = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -198,16 +212,19 @@ __device__ __forceinline__ Found<ROWS, TILE> locate(const Args& a, long long* sh
         if (w < warp) before += sh[w];
         total += sh[w];
     }
-    Found<ROWS, TILE> f;
+    Found<ROWS, TILE, OVER> f;
+    Walk<ROWS, TILE, OVER>& w = f.walk;
     f.total = total * a.Hk;
-    f.C = ranges(f.total, a.blocks);
-    f.walk.left = 0;
-    if (f.total == 0 || static_cast<int>(blockIdx.x) >= f.C) return f;     // the same in every thread
-    const long long x = cut(f.total, blockIdx.x, f.C);
+    w.left = 0;
+    const int C = ranges(f.total, a.blocks);
+    if (static_cast<int>(blockIdx.x) >= C) return f;                         // the same in every thread
+    if (tid == 0) a.openings[blockIdx.x] = {0, 0, 0, 0, 0, 0, f.total};      // unless a piece opens an item
+    if (f.total == 0) return f;
+    const long long x = cut(f.total, blockIdx.x, C);
     long long at = (before + incl - own) * a.Hk;
     if (x >= at && x < at + own * a.Hk) {
         for (int s = s0; s < s1; ++s) {
-            const long long n = L::tiles_per_head(a, rows_of(a, s, false));
+            const long long n = s == s0 ? first : L::per_head(a, rows_of(a, s, false));
             if (x < at + n * a.Hk) {
                 sh[W] = x - at;
                 sh[W + 1] = s;
@@ -218,17 +235,16 @@ __device__ __forceinline__ Found<ROWS, TILE> locate(const Args& a, long long* sh
         }
     }
     __syncthreads();
-    Walk<ROWS, TILE>& w = f.walk;
     const long long inside = sh[W], per_head = sh[W + 2];
     w.s = static_cast<int>(sh[W + 1]);
-    w.left = cut(f.total, blockIdx.x + 1, f.C) - x;
+    w.left = cut(f.total, blockIdx.x + 1, C) - x;
     w.r = rows_of(a, w.s, false);
     w.nb = L::blocks_of(a, w.r);
     w.kvh = static_cast<int>(inside / per_head);
     // the item: 32 at a time
     long long rem = inside - w.kvh * per_head;
     for (int b = 0;; b += 32) {
-        const int n = b + lane < w.nb ? L::tiles(a, w.r, b + lane) : 0;
+        const int n = b + lane < w.nb ? L::tiles(a, w.r, b + lane) + OVER : 0;
         long long upto = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -239,12 +255,13 @@ __device__ __forceinline__ Found<ROWS, TILE> locate(const Args& a, long long* sh
         if (past) {
             const int at_lane = __ffs(past) - 1;
             w.rb = b + at_lane;
-            w.t0 = static_cast<int>(rem - __shfl_sync(0xffffffffu, upto - n, at_lane));
+            w.u0 = static_cast<int>(rem - __shfl_sync(0xffffffffu, upto - n, at_lane));
             break;
         }
         rem -= __shfl_sync(0xffffffffu, upto, 31);
     }
     w.item(a);
+    if (w.t1 <= w.t0) w.next(a);
     __syncthreads();      // sh may be used for something else
     return f;
 }
@@ -257,50 +274,48 @@ struct Row {
 };
 template <int ROWS>
 __device__ __forceinline__ Row row_at(const Args& a, const Rows& r, int kvh, int rb, int i) {
-    const long long u = static_cast<long long>(rb) * ROWS + i;
+    const int u = rb * ROWS + i;
     Row w;
-    w.there = u < static_cast<long long>(r.n) * a.G;
-    const int token = w.there ? static_cast<int>(u / a.G) : 0;
+    w.there = u < r.n * a.G;
+    const int token = w.there ? u / a.G : 0;
     w.token = r.first + token;
-    w.head = kvh * a.G + (w.there ? static_cast<int>(u - static_cast<long long>(token) * a.G) : 0);
+    w.head = kvh * a.G + (w.there ? u - token * a.G : 0);
     w.kept = w.there && head_kept(a, w.head);
-    w.sees = w.kept ? max(r.len - r.n + token + 1, 0) : 0;
+    w.sees = max(r.len - r.n + token + 1, 0);
     return w;
 }
 
-// Pieces of cut items: blockIdx.x = the range that begins an item and does not end it, blockIdx.y = 32 rows and 32 columns of it.
-// A lane has a row, a warp four columns.
+// Pieces of cut items: blockIdx.x = the range that begins an item and does not end it, blockIdx.y = 32 rows and 64 columns of it.
+// A lane has a row, a warp eight columns.
 template <typename Io, int ROWS>
 __global__ void __launch_bounds__(256) paged_prompt_join_kernel(const __grid_constant__ Args a) {
     constexpr int kAhead = 4;
-    const int lane = threadIdx.x & 31, c0 = blockIdx.x;
-    const int row = (blockIdx.y % (ROWS / 32)) * 32 + lane, c4 = (blockIdx.y / (ROWS / 32)) * 8 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31, c0 = blockIdx.x, groups = (a.rows + 31) / 32;
+    const int row = (blockIdx.y % groups) * 32 + lane, c4 = (blockIdx.y / groups) * 16 + (threadIdx.x >> 5) * 2;      // of four columns
     chain_wait();   // in every block: this grid may not end before the first one
     const int4 head = __ldcg(reinterpret_cast<const int4*>(a.openings + c0));
     const int4 more = __ldcg(reinterpret_cast<const int4*>(a.openings + c0) + 1);
     const long long total = __ldcg(&a.openings[0].total);
     const int C = ranges(total, a.blocks);
     if (c0 + 1 >= C || !head.x || c4 * 4 >= a.dh) return;   // behind the last range: a record that nobody wrote
-    const Rows r = rows_of(a, head.y, false);
-    const Row w = row_at<ROWS>(a, r, head.z, head.w, row);
+    const Row w = row_at<ROWS>(a, {head.w, more.x, 0}, head.y, head.z, row);
     if (!w.there) return;
-    const int pieces = range_of(total, cut(total, c0 + 1, C) + more.x - 1, C) - c0 + 1;
-    // piece 0 in the slot of range c0 that holds its end (its first one if the item fills the range), the others in the
-    // first slots of the ranges behind it
-    const float* ws0 = a.ws + (static_cast<long long>(c0) * 2 + (more.y ? 0 : 1)) * a.slot;
-    const float* ws1 = a.ws + static_cast<long long>(c0) * 2 * a.slot;
-    float M = -INFINITY, L = 0.0f;
-    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const int pieces = range_of(total, cut(total, c0 + 1, C) + more.y - 1, C) - c0 + 1;
+    // piece 0 in the second slot of range c0, the others in the first slots of the ranges behind it
+    const float* ws = a.ws + static_cast<long long>(c0) * 2 * a.slot;
+    const auto four = [&](const float* p, int c) { return __ldcg(reinterpret_cast<const float4*>(p + 2 * a.rows) + static_cast<long long>(c) * a.rows + row); };
+    float M = -INFINITY, L = 0.0f, v[8] = {};
     for (int k0 = 0; k0 < pieces; k0 += kAhead) {
         float m[kAhead], l[kAhead];
-        float4 x[kAhead];
+        float4 x[kAhead][2];
 #pragma unroll
         for (int e = 0; e < kAhead; ++e) {
             const bool there = k0 + e < pieces;
-            const float* p = k0 + e == 0 ? ws0 : ws1 + static_cast<long long>(k0 + e) * 2 * a.slot;
+            const float* p = ws + (k0 + e == 0 ? 1 : static_cast<long long>(k0 + e) * 2) * a.slot;
             m[e] = there ? __ldcg(p + row) : -INFINITY;
             l[e] = there ? __ldcg(p + a.rows + row) : 0.0f;
-            x[e] = there ? __ldcg(reinterpret_cast<const float4*>(p + 2 * a.rows) + static_cast<long long>(c4) * a.rows + row) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) x[e][h] = there ? four(p, c4 + h) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);      // dh % 16 == 0
         }
 #pragma unroll
         for (int e = 0; e < kAhead; ++e) {
@@ -308,27 +323,39 @@ __global__ void __launch_bounds__(256) paged_prompt_join_kernel(const __grid_con
             const float f = pow2(M - base), g = pow2(m[e] - base);
             M = mx;
             L = fmaf(L, f, l[e] * g);
-            v.x = fmaf(v.x, f, x[e].x * g);
-            v.y = fmaf(v.y, f, x[e].y * g);
-            v.z = fmaf(v.z, f, x[e].z * g);
-            v.w = fmaf(v.w, f, x[e].w * g);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                v[4 * h] = fmaf(v[4 * h], f, x[e][h].x * g);
+                v[4 * h + 1] = fmaf(v[4 * h + 1], f, x[e][h].y * g);
+                v[4 * h + 2] = fmaf(v[4 * h + 2], f, x[e][h].z * g);
+                v[4 * h + 3] = fmaf(v[4 * h + 3], f, x[e][h].w * g);
+            }
         }
     }
     const bool some = L != 0.0f && w.kept;
     const float n = some ? 1.0f / L : 0.0f;
     const long long at = static_cast<long long>(w.token) * a.H + w.head;
     Io* out = static_cast<Io*>(a.out) + at * a.dh + c4 * 4;
-    alignas(16) Io y[4] = {from_float<Io>(some ? v.x * n : 0.0f), from_float<Io>(some ? v.y * n : 0.0f),
-                           from_float<Io>(some ? v.z * n : 0.0f), from_float<Io>(some ? v.w * n : 0.0f)};
-    if constexpr (sizeof(Io) == 4) *reinterpret_cast<uint4*>(out) = *reinterpret_cast<const uint4*>(y);
-    else *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(y);
+    alignas(16) Io y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = from_float<Io>(some ? v[e] * n : 0.0f);
+#pragma unroll
+    for (int e = 0; e < static_cast<int>(sizeof(Io) / 2); ++e) reinterpret_cast<uint4*>(out)[e] = reinterpret_cast<const uint4*>(y)[e];
     if (c4 == 0 && a.lse) a.lse[at] = some ? (M + log2f(L)) * kLn2 : -INFINITY;
 }
 
 template <typename Io, int ROWS>
 halo_status launch_join(const Args& a, cudaStream_t st) {
     if (a.blocks < 2) return HALO_OK;
-    return launch_chained(paged_prompt_join_kernel<Io, ROWS>, dim3(a.blocks - 1, ROWS / 32 * ((a.dh + 31) / 32)), 256, 0, st, a);
+    return launch_chained(paged_prompt_join_kernel<Io, ROWS>, dim3(a.blocks - 1, (a.rows + 31) / 32 * ((a.dh + 63) / 64)), 256, 0, st, a);
+}
+
+// Thread blocks for a call: as many as are resident together, no more than the line has ranges whatever the lengths are.
+inline int line_blocks(const halo_paged_shape& sh, int n_tok, int n_seq, int rows, int tile, int over, int resident) {
+    const long long G = sh.n_heads / sh.n_kv_heads, cap = static_cast<long long>(sh.max_pages) * sh.page_size;
+    const long long items = (n_tok * G / rows + (n_seq < n_tok ? n_seq : n_tok) + 1) * sh.n_kv_heads;
+    const long long most = items * ((cap + tile - 1) / tile + over) / kMinUnits;
+    return static_cast<int>(most < 1 ? 1 : most < resident ? most : resident);
 }
 
 // The f32 form (paged_prompt_f32.cu)

@@ -284,10 +284,13 @@ def test_what_a_row_does_not_see_has_no_influence(kind, what, dh):
     c.refresh()
     out, lse, _ = c.run()
     c.compare(out, lse)
-    before = slice(0, 100 - 37)                  # rows in front of the first of them, the same as without any
+    before = slice(0, 100 - 37)                  # rows in front of the first of them: those that it reached would not be finite
     assert torch.isfinite(out[before]).all() and torch.isfinite(lse[before]).all()
     c.K, c.V = torch.nan_to_num(c.K, 0.0, 0.0, 0.0), torch.nan_to_num(c.V, 0.0, 0.0, 0.0)
-    assert torch.equal(c.run()[0][before], out[before])
+    c.refresh()
+    clean, clean_lse, _ = c.run()
+    c.compare(clean, clean_lse)                  # both within the bound of the same definition: sums may be formed in another order
+    assert torch.equal(clean_lse[before], lse[before])
 
 
 @pytest.mark.parametrize("dh", [64, 256])
