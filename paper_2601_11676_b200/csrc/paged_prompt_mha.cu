@@ -34,7 +34,7 @@ namespace {
 
 constexpr int kTile = 128;         // keys
 constexpr int kThreads = 512;
-constexpr int kOver = 2;           // an item's rows, first scores and outputs cost about as much as two tiles
+constexpr int kOver = 4;           // an item's rows, first scores and outputs cost about as much as four tiles
 constexpr int kFlags = 8;          // tiles whose flags are kept
 
 // DP: head size padded to 64, 128 or 256.
@@ -48,7 +48,10 @@ struct Cfg {
     static constexpr int kStages = DP == 64 ? 8 : 5;
     static constexpr int kQTile = 128 * DP * 2;               // Q of a stream
     static constexpr int kQ = kStreams * kQTile;
-    static constexpr int kO = 256;                            // tensor memory: S at 0 and 128, O behind
+    // tensor memory: S at 0 and 128, O behind; P in a place of its own where there is one, else over the S that it comes from
+    static constexpr int kO = 256;
+    static constexpr bool kApart = DP == 64;
+    static constexpr int kP = kApart ? 384 : 0, kPStep = kApart ? 64 : 128;
 };
 
 struct Flags {
@@ -313,6 +316,7 @@ struct Gather {
         }
         __syncwarp();      // q_row may be written again
         issued(full);
+        flush();           // the first scores wait for them
     }
     __device__ void run(Walk<C::kRows, kTile, kOver> w) {
         bool bad = false;
@@ -363,102 +367,156 @@ struct Gather {
 template <int N>
 using Const = std::integral_constant<int, N>;
 
-// One warp, one lane of which issues.  Lanes (of barriers) are constants, so that counters and addresses stay in registers: the tensor cores take a product of 16
-// columns in 64 clocks, and one must not take longer to issue.
+// One warp, one lane of which issues.  Lanes (of barriers) are constants, so that counters and addresses stay in registers: the
+// tensor cores take a product of 16 columns in 64 clocks, and one must not take longer to issue.  What is issued next goes by what is
+// ready: a stream's weights (P V), else its next scores, so that a stream never waits behind the other's softmax.
 template <int DP>
-__device__ void issue_products(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, kTile, kOver> w) {
+struct Issue {
     using C = Cfg<DP>;
-    Bars& bars = sm.bars;
-    int* abort = &bars.abort;
-    const uint32_t lead = elect();
-    const uint32_t tmem = bars.tmem, q0 = smem_u32(sm.q) >> 4, ring = smem_u32(sm.ring) >> 4;
-    // a negative scale: -Q instead, so that the largest score stays the largest product
-    const uint32_t idesc_s = umma_idesc_bf16(128, kTile, false) | (a.scale_log2 < 0.0f ? 1u << 13 : 0u);
-    uint32_t first_fill = 0, piece = 0, use0 = 0, use1 = 0, use2 = 0;      // tiles of each lane so far
-    int last = 1;                                                          // lane that the second buffer was used in last
-    while (w.left > 0) {
-        const Piece<DP> p(a, w);
-        if (p.n > 0) {
-            if (!warp_wait(&bars.q_full, piece++, abort)) return;
-            // stream t, lane b, tile j; end: the last stream's, after which the stages are free
-            const auto scores = [&](auto t_, auto b_, int j, bool end) {
-                constexpr int t = decltype(t_)::value, b = decltype(b_)::value, buffer = b != 0;
-                // S lies where the P of the buffer's last tile was read from
-                if (buffer == 0) {
-                    if (use0 > 0 && !warp_wait(&bars.pv_done[0], use0 - 1, abort)) return false;
-                    ++use0;
-                } else {
-                    const uint32_t used = last == 1 ? use1 : use2;
-                    if (used > 0 && !warp_wait(last == 1 ? &bars.pv_done[1] : &bars.pv_done[2], used - 1, abort)) return false;
-                    last = b;
-                    ++(b == 1 ? use1 : use2);
-                }
-                const uint32_t d = tmem + buffer * 128;
+    const Args& a;
+    Smem<DP>& sm;
+    Bars& bars;
+    int* abort;
+    const uint32_t lead, tmem, q0, ring, idesc_s;
+    uint32_t first_fill = 0, use0 = 0, use1 = 0, use2 = 0;      // stages of the pieces before; tiles of each lane so far
+    int last = 1;                                               // lane that the second buffer was used in last
+
+    __device__ __forceinline__ Issue(const Args& a_, Smem<DP>& sm_)
+        : a(a_), sm(sm_), bars(sm_.bars), abort(&sm_.bars.abort), lead(elect()), tmem(sm_.bars.tmem), q0(smem_u32(sm_.q) >> 4),
+          ring(smem_u32(sm_.ring) >> 4),
+          // a negative scale: -Q instead, so that the largest score stays the largest product
+          idesc_s(umma_idesc_bf16(128, kTile, false) | (a_.scale_log2 < 0.0f ? 1u << 13 : 0u)) {}
+    static __device__ __forceinline__ bool done(uint64_t* bar, uint32_t phase) { return __all_sync(0xffffffffu, mbar_test(bar, phase & 1u)); }
+    // the K (v = 0) or V (1) stages of tile j
+    __device__ __forceinline__ bool there(int j, int v) const {
+        bool all = true;
 #pragma unroll
-                for (int h = 0; h < C::kParts; ++h) {
-                    const uint32_t f = first_fill + j * 2 * C::kParts + h, s = f % C::kStages;
-                    if (!warp_wait(&bars.full[s], f / C::kStages, abort)) return false;
-                    tcgen05_fence_after_sync();
-                    const uint32_t q = q0 + ((t * C::kQTile + h * (C::kCols / 64) * (128 * 128)) >> 4), k = ring + s * (C::kStage >> 4);
-                    const int steps = (a.dh - h * C::kCols) / 16;
-                    if (steps >= C::kCols / 16) {
-#pragma unroll
-                        for (int e = 0; e < C::kCols / 16; ++e)
-                            umma_ss(lead, d, q + (e >> 2) * 1024 + (e & 3) * 2, k + (e >> 2) * 1024 + (e & 3) * 2, idesc_s, h > 0 || e > 0);
-                    } else {
-                        for (int e = 0; e < steps; ++e)
-                            umma_ss(lead, d, q + (e >> 2) * 1024 + (e & 3) * 2, k + (e >> 2) * 1024 + (e & 3) * 2, idesc_s, h > 0 || e > 0);
-                    }
-                    if (end) commit(lead, &bars.empty[s]);
-                }
-                commit(lead, &bars.s_full[b]);
-                if (lead) mbar_arrive(&bars.s_full[b]);      // what this thread has seen of the gathering warps, the tile's flags among it
-                if (end && j == p.n - 1) commit(lead, &bars.q_empty);
-                return true;
-            };
-            const auto sums = [&](auto t_, auto b_, int j, bool end) {
-                constexpr int t = decltype(t_)::value, b = decltype(b_)::value;
-                if (!warp_wait(&bars.p_full[b], (b == 0 ? use0 : b == 1 ? use1 : use2) - 1, abort)) return false;
-                tcgen05_fence_after_sync();
-#pragma unroll
-                for (int h = 0; h < C::kParts; ++h) {
-                    const uint32_t f = first_fill + (j * 2 + 1) * C::kParts + h, s = f % C::kStages;
-                    if (!warp_wait(&bars.full[s], f / C::kStages, abort)) return false;
-                    tcgen05_fence_after_sync();
-                    const uint32_t idesc = umma_idesc_bf16(128, min(a.dh - h * C::kCols, C::kCols), true);
-                    const uint32_t v = (ring + s * (C::kStage >> 4)) | ((kTile * 128) >> 4) << 16;
-#pragma unroll
-                    for (int e = 0; e < kTile / 16; ++e)
-                        umma_ts(lead, tmem + C::kO + t * DP + h * C::kCols, tmem + (b != 0) * 128 + e * 8, v + e * 128, idesc, j > 0 || e > 0);
-                    if (end) commit(lead, &bars.empty[s]);
-                }
-                commit(lead, &bars.pv_done[b]);
-                return true;
-            };
-            if (C::kStreams == 2 && p.streams == 2) {
-                if (p.tiles[0] > 0 && !scores(Const<0>(), Const<0>(), 0, false)) return;
-                if (!scores(Const<C::kStreams - 1>(), Const<1>(), 0, true)) return;
-                for (int j = 0; j < p.n; ++j) {
-                    if (j < p.tiles[0] && !sums(Const<0>(), Const<0>(), j, false)) return;
-                    if (j + 1 < p.tiles[0] && !scores(Const<0>(), Const<0>(), j + 1, false)) return;
-                    if (!sums(Const<C::kStreams - 1>(), Const<1>(), j, true)) return;
-                    if (j + 1 < p.n && !scores(Const<C::kStreams - 1>(), Const<1>(), j + 1, true)) return;
-                }
-            } else {
-                if (!scores(Const<0>(), Const<0>(), 0, true)) return;
-                if (p.n > 1 && !scores(Const<0>(), Const<2>(), 1, true)) return;
-                for (int j = 0; j < p.n; j += 2) {
-                    if (!sums(Const<0>(), Const<0>(), j, true)) return;
-                    if (j + 2 < p.n && !scores(Const<0>(), Const<0>(), j + 2, true)) return;
-                    if (j + 1 < p.n && !sums(Const<0>(), Const<2>(), j + 1, true)) return;
-                    if (j + 3 < p.n && !scores(Const<0>(), Const<2>(), j + 3, true)) return;
-                }
-            }
-            first_fill += p.n * 2 * C::kParts;
+        for (int h = 0; h < C::kParts; ++h) {
+            const uint32_t f = first_fill + (j * 2 + v) * C::kParts + h;
+            all = all && done(&bars.full[f % C::kStages], f / C::kStages);
         }
-        w.next(a);
+        return all;
     }
-}
+    template <int b>
+    __device__ __forceinline__ uint32_t& use() { return b == 0 ? use0 : b == 1 ? use1 : use2; }
+    // S of lane b may be written: the buffer's last P has been read (its S, where P lies apart and the same warps write the next)
+    template <int b>
+    __device__ __forceinline__ bool free_scores() {
+        const int was = b == 0 ? 0 : last;
+        const uint32_t used = was == 0 ? use0 : was == 1 ? use1 : use2;
+        if (used == 0) return true;
+        return C::kApart && was == b ? done(&bars.p_full[b], used - 1)
+                                     : done(was == 0 ? &bars.pv_done[0] : was == 1 ? &bars.pv_done[1] : &bars.pv_done[2], used - 1);
+    }
+    // stream t, lane b, tile j; end: nobody else needs the stages
+    template <int t, int b>
+    __device__ __forceinline__ void scores(int j, bool end) {
+        tcgen05_fence_after_sync();
+        const uint32_t d = tmem + (b != 0) * 128;
+        if (b != 0) last = b;
+        ++use<b>();
+#pragma unroll
+        for (int h = 0; h < C::kParts; ++h) {
+            const uint32_t s = (first_fill + j * 2 * C::kParts + h) % C::kStages;
+            const uint32_t q = q0 + ((t * C::kQTile + h * (C::kCols / 64) * (128 * 128)) >> 4), k = ring + s * (C::kStage >> 4);
+            const int steps = (a.dh - h * C::kCols) / 16;
+            if (steps >= C::kCols / 16) {
+#pragma unroll
+                for (int e = 0; e < C::kCols / 16; ++e)
+                    umma_ss(lead, d, q + (e >> 2) * 1024 + (e & 3) * 2, k + (e >> 2) * 1024 + (e & 3) * 2, idesc_s, h > 0 || e > 0);
+            } else {
+                for (int e = 0; e < steps; ++e)
+                    umma_ss(lead, d, q + (e >> 2) * 1024 + (e & 3) * 2, k + (e >> 2) * 1024 + (e & 3) * 2, idesc_s, h > 0 || e > 0);
+            }
+            if (end) commit(lead, &bars.empty[s]);
+        }
+        commit(lead, &bars.s_full[b]);
+        if (lead) mbar_arrive(&bars.s_full[b]);      // what this thread has seen of the gathering warps, the tile's flags among it
+    }
+    template <int t, int b>
+    __device__ __forceinline__ void sums(int j, bool end) {
+        tcgen05_fence_after_sync();
+#pragma unroll
+        for (int h = 0; h < C::kParts; ++h) {
+            const uint32_t s = (first_fill + (j * 2 + 1) * C::kParts + h) % C::kStages;
+            const uint32_t idesc = umma_idesc_bf16(128, min(a.dh - h * C::kCols, C::kCols), true);
+            const uint32_t v = (ring + s * (C::kStage >> 4)) | ((kTile * 128) >> 4) << 16;
+#pragma unroll
+            for (int e = 0; e < kTile / 16; ++e)
+                umma_ts(lead, tmem + C::kO + t * DP + h * C::kCols, tmem + C::kP + (b != 0) * C::kPStep + e * 8, v + e * 128, idesc, j > 0 || e > 0);
+            if (end) commit(lead, &bars.empty[s]);
+        }
+        commit(lead, &bars.pv_done[b]);
+    }
+    // One step of a stream that has had q scores and s sums of its n tiles: true if something was issued.  o: the other stream's.
+    template <int t, int b, int b2>
+    __device__ __forceinline__ bool step(int& q, int& s, int n, int oq, int os, int on) {
+        // lane of tile j: b, or b and b2 in turn
+        const bool odd = b != b2;
+        if (s < q) {
+            const bool second = odd && (s & 1);
+            const uint32_t phase = second ? use<b2>() - 1 : use<b>() - (odd ? 1 : q - s);
+            if (done(second ? &bars.p_full[b2] : &bars.p_full[b], phase) && there(s, 1)) {
+                const bool end = os > s || s >= on;
+                if (second) sums<t, b2>(s, end);
+                else sums<t, b>(s, end);
+                ++s;
+                return true;
+            }
+        }
+        // scores in every buffer of S that the stream has; two ahead of the sums where P lies apart
+        if (q < n && q - s < (odd || C::kApart ? 2 : 1)) {
+            const bool second = odd && (q & 1);
+            if ((second ? free_scores<b2>() : free_scores<b>()) && there(q, 0)) {
+                const bool end = oq > q || q >= on;
+                if (second) scores<t, b2>(q, end);
+                else scores<t, b>(q, end);
+                ++q;
+                return true;
+            }
+        }
+        return false;
+    }
+    __device__ void run(Walk<C::kRows, kTile, kOver> w) {
+        uint32_t piece = 0;
+        while (w.left > 0) {
+            const Piece<DP> p(a, w);
+            if (p.n > 0) {
+                if (!warp_wait(&bars.q_full, piece++, abort)) return;
+                int q0_ = 0, s0_ = 0, q1_ = 0, s1_ = 0;      // scores and sums issued, per stream
+                bool asked = false;
+                long long since = clock64();
+                uint32_t idle = 0;
+                while (s0_ < p.tiles[0] || s1_ < p.tiles[1]) {
+                    bool any;
+                    if (C::kStreams == 2 && p.streams == 2) {
+                        any = step<0, 0, 0>(q0_, s0_, p.tiles[0], q1_, s1_, p.tiles[1]);
+                        any |= step<C::kStreams - 1, 1, 1>(q1_, s1_, p.tiles[1], q0_, s0_, p.tiles[0]);
+                    } else {
+                        any = step<0, 0, 2>(q0_, s0_, p.tiles[0], 0, 0, 0);
+                    }
+                    if (!asked && q0_ == p.tiles[0] && q1_ == p.tiles[1]) {
+                        commit(lead, &bars.q_empty);
+                        asked = true;
+                    }
+                    if (any) {
+                        idle = 0;
+                    } else if ((++idle & 255u) == 0u) {      // bounded, as every wait
+                        const long long now = clock64();
+                        if (idle == 256u) since = now;
+                        const bool stop = *reinterpret_cast<volatile int*>(abort) || now - since > kWaitLimitCycles;
+                        if (__any_sync(0xffffffffu, stop)) {
+                            *reinterpret_cast<volatile int*>(abort) = 1;
+                            return;
+                        }
+                    }
+                }
+                first_fill += p.n * 2 * C::kParts;
+            }
+            w.next(a);
+        }
+    }
+};
 
 // ---- two fp32 numbers at a time ----
 using Pair = unsigned long long;
@@ -494,23 +552,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-// 2^x of two numbers up to 126 without the special-function unit, which does 16 a clock and SM and bounds the softmax: x = n + f with n
-// the nearest whole number (the low bits of x + 1.5 * 2^23), 2^f by the polynomial of degree 4 with the least largest relative
-// error on [-1/2, 1/2] (2.7e-6, evaluated in fp32; found by linear programming), n into the exponent.  Below -126: 2^-126; NaN: NaN or
-// more than 2^127.
-__device__ __forceinline__ float2 pow2_by_polynomial(Pair x) {
-    const float2 low = both(x);
-    x = pair_of(max2(low.x, -126.0f), max2(low.y, -126.0f));
-    const Pair shifted = add2(x, twice(12582912.0f)), f = fma2(add2(shifted, twice(-12582912.0f)), twice(-1.0f), x);
-    Pair y = fma2(twice(0.009569705463945866f), f, twice(0.05591819807887077f));
-    y = fma2(y, f, twice(0.24024765193462372f));
-    y = fma2(y, f, twice(0.6931217312812805f));
-    y = fma2(y, f, twice(0.9999992251396179f));
-    const float2 n = both(shifted), v = both(y);
-    return make_float2(__uint_as_float(__float_as_uint(v.x) + (__float_as_uint(n.x) << 23)),
-                       __uint_as_float(__float_as_uint(v.y) + (__float_as_uint(n.y) << 23)));
-}
-
 // ---- rows -----------------------------------------------------------------------------------------------------------------------
 
 // One element of the caches
@@ -524,7 +565,7 @@ __device__ __forceinline__ float cache_at(const Args& a, const void* cache, cons
 
 // A row's weighted sum of values over the positions p0 to p1 - 1 of sequence s, key by key: a lane has a key for its score, and columns
 // lane, lane + 32, ... for the sums.  By a whole warp; to: fp32, every `step` floats four columns, or bf16 (step 0) times f.
-__device__ __noinline__ void resum(const Args& a, int s, int kvh, int token, int head, int p0, int p1, float base, float f, void* to, long long step) {
+__device__ __forceinline__ void resum(const Args& a, int s, int kvh, int token, int head, int p0, int p1, float base, float f, void* to, long long step) {
     const int lane = threadIdx.x & 31;
     const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + static_cast<long long>(token) * a.q_stride + static_cast<long long>(head) * a.dh;
     float o[8] = {};
@@ -604,7 +645,7 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
                 alive = warp_wait(&bars.s_full[b], used[b], abort);
                 if (!alive) break;
                 tcgen05_fence_after_sync();
-                const uint32_t s_addr = lanes + p.buffer(b) * 128;
+                const uint32_t s_addr = lanes + p.buffer(b) * 128, p_addr = lanes + C::kP + p.buffer(b) * C::kPStep;
                 uint32_t there[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) there[c] = *const_cast<volatile const uint32_t*>(&sm.flags.there[(tile + j) % kFlags][c]);
@@ -614,7 +655,7 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
                 tmem_ld_wait();
                 const bool masked = p0 + kTile > all_see || (there[0] & there[1] & there[2] & there[3]) != 0xffffffffu;
                 Pair sum[2];
-                const auto weights = [&](auto by_polynomial) {
+                const auto weights = [&]() {
                     const Pair times = twice(scale), minus = twice(m == -INFINITY ? 0.0f : -m * scale);
                     sum[0] = sum[1] = 0;
 #pragma unroll
@@ -622,14 +663,8 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             const Pair x = fma2(pair_of(__uint_as_float(sc[c][2 * e]), __uint_as_float(sc[c][2 * e + 1])), times, minus);
-                            float2 y;
-                            // 6 of 16: as long as the special-function unit takes for the others
-                            if (decltype(by_polynomial)::value && e * 6 / 16 != (e + 1) * 6 / 16) {
-                                y = pow2_by_polynomial(x);
-                            } else {
-                                y = both(x);
-                                y = make_float2(pow2(y.x), pow2(y.y));
-                            }
+                            float2 y = both(x);
+                            y = make_float2(pow2(y.x), pow2(y.y));
                             sum[e & 1] = add2(sum[e & 1], pair_of(y.x, y.y));
                             pk[c][e] = pack_bf16(y.x, y.y);
                         }
@@ -637,7 +672,7 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
                     return (s0.x + s0.y) + (s1.x + s1.y);
                 };
                 float more = INFINITY;
-                if (!masked && __all_sync(0xffffffffu, m > -INFINITY)) more = weights(Const<1>());
+                if (!masked && __all_sync(0xffffffffu, m > -INFINITY)) more = weights();
                 if (__any_sync(0xffffffffu, !(more < kSum))) {
                     // masks, a new reference, or something infinite or NaN: from the scores again, exactly
 #pragma unroll
@@ -680,11 +715,16 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
                         l *= f;
                         m = to;
                     }
-                    more = weights(Const<0>());
+                    more = weights();
                 }
                 l += more;
+                if (C::kApart && j > (p.streams == 2 ? 0 : 1)) {      // the P before it in its place has been read
+                    alive = warp_wait(&bars.pv_done[b], used[b] - 1, abort);
+                    if (!alive) break;
+                    tcgen05_fence_after_sync();
+                }
 #pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_st_32x16(s_addr + c * 16, pk[c]);
+                for (int c = 0; c < 4; ++c) tmem_st_32x16(p_addr + c * 16, pk[c]);
                 tmem_st_wait();
                 ++used[b];
                 tcgen05_fence_before_sync();
@@ -811,7 +851,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __g
         Gather<DP>(a, maps, sm).run(f.walk);
     } else {
         fewer_registers<kIssueRegs>();
-        if (warp == 12) issue_products<DP>(a, sm, f.walk);
+        if (warp == 12) Issue<DP>(a, sm).run(f.walk);
     }
     __syncwarp();
     tcgen05_fence_before_sync();
