@@ -1,4 +1,4 @@
-// halo_paged_prompt_mha by fused multiply-adds: 64 rows against tiles of 64 keys.  Bound by them: 4 flops per key, row and
+// halo_paged_prompt_mha on fp32 caches, by fused multiply-adds: 64 rows against tiles of 64 keys.  Bound by them: 4 flops per key, row and
 // column of the head at 2 * 128 a clock and SM.
 //
 // 128 threads; a thread has 8 rows x 4 keys of the scores and 8 rows x DP / 16 columns of the weighted sums, so that twelve 16-byte
@@ -16,22 +16,11 @@ namespace {
 
 constexpr int kRows = 64, kTile = 64, kThreads = 128, kOver = 1;
 
-struct Eight {};
-template <typename T> struct Kind {
-    using Io = T;
-    using Row = T;
-};
-template <> struct Kind<Eight> {
-    using Io = __nv_bfloat16;
-    using Row = uint8_t;
-};
-
 template <int DP>
 struct Smem {
     static constexpr int kStride = DP + 4, kWeights = kTile + 4;
     float q[kRows * kStride], k[kTile * kStride], v[kTile * kStride], w[kRows * kWeights];
     long long row[2][kTile];     // of the caches' rows: page * page_stride + ..., -1: no such position
-    long long scale[2][kTile];   // 8-bit rows: where their bytes are
     long long sh[kThreads / 32 + 3];
 };
 
@@ -44,9 +33,8 @@ __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_grou
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(kThreads) paged_prompt_rows_kernel(const __grid_constant__ Args a) {
-    using Io = typename Kind<T>::Io;
     using S_ = Smem<DP>;
     constexpr int kStride = S_::kStride, kWeights = S_::kWeights, kCpr = DP / 4, V = DP / 64;
     extern __shared__ __align__(16) unsigned char raw[];
@@ -67,38 +55,18 @@ __global__ void __launch_bounds__(kThreads) paged_prompt_rows_kernel(const __gri
             if (p < w.reach) {
                 const int pi = a.page_shift >= 0 ? p >> a.page_shift : p / a.page_size, in = p - pi * a.page_size;
                 const int page = ldg_waited(a.table + static_cast<long long>(w.s) * a.max_pages + pi);
-                if (page >= 0 && page < a.n_pages) {
-                    at = static_cast<long long>(page) * a.page_stride + (static_cast<long long>(kvh) * a.page_size + in) * a.dh;
-                    sm.scale[t & 1][tid] = (static_cast<long long>(page) * a.Hk + kvh) * a.page_size + in;
-                } else {
-                    bad = true;
-                }
+                if (page >= 0 && page < a.n_pages) at = static_cast<long long>(page) * a.page_stride + (static_cast<long long>(kvh) * a.page_size + in) * a.dh;
+                else bad = true;
             }
             sm.row[t & 1][tid] = at;
         };
-        const auto fetch = [&](float* dst, const void* cache, const uint8_t* scale, int t) {
+        const auto fetch = [&](float* dst, const void* cache, int t) {
 #pragma unroll 4
             for (int i = tid; i < kTile * kCpr; i += kThreads) {
                 const int r = i / kCpr, c = i % kCpr;
                 const long long at = sm.row[t & 1][r];
                 const bool there = at >= 0 && c * 4 < a.dh;
-                float* to = dst + r * kStride + c * 4;
-                if constexpr (std::is_same<T, float>::value) {
-                    cp_async16(to, static_cast<const float*>(cache) + (there ? at + c * 4 : 0), there);
-                } else if constexpr (std::is_same<T, Eight>::value) {
-                    float x[4] = {};
-                    if (there) {
-                        eight_widen(*reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(cache) + at + c * 4), x);
-                        const float unit = eight_unit(scale[sm.scale[t & 1][r]]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) x[e] *= unit;
-                    }
-                    *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
-                } else {
-                    uint2 x = make_uint2(0, 0);
-                    if (there) x = *reinterpret_cast<const uint2*>(static_cast<const T*>(cache) + at + c * 4);
-                    *reinterpret_cast<float4*>(to) = make_float4(bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y));
-                }
+                cp_async16(dst + r * kStride + c * 4, static_cast<const float*>(cache) + (there ? at + c * 4 : 0), there);
             }
             cp_commit();
         };
@@ -107,16 +75,11 @@ __global__ void __launch_bounds__(kThreads) paged_prompt_rows_kernel(const __gri
         {
             const int i = tid & (kRows - 1);
             const Row row = row_at<kRows>(a, w.r, kvh, w.rb, i);
-            const Io* q = static_cast<const Io*>(a.q) + static_cast<long long>(row.token) * a.q_stride + static_cast<long long>(row.head) * a.dh;
+            const float* q = static_cast<const float*>(a.q) + static_cast<long long>(row.token) * a.q_stride + static_cast<long long>(row.head) * a.dh;
 #pragma unroll 4
-            for (int c = tid / kRows; c < kCpr; c += kThreads / kRows) {
-                float x[4] = {};
-                if (row.there && c * 4 < a.dh) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = to_float(q[c * 4 + e]);
-                }
-                *reinterpret_cast<float4*>(sm.q + i * kStride + c * 4) = make_float4(x[0], x[1], x[2], x[3]);
-            }
+            for (int c = tid / kRows; c < kCpr; c += kThreads / kRows)
+                *reinterpret_cast<float4*>(sm.q + i * kStride + c * 4) =
+                    row.there && c * 4 < a.dh ? *reinterpret_cast<const float4*>(q + c * 4) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
         int sees[8];
 #pragma unroll
@@ -130,8 +93,8 @@ __global__ void __launch_bounds__(kThreads) paged_prompt_rows_kernel(const __gri
             places(0);
             places(1);
             __syncthreads();
-            fetch(sm.k, a.K, a.K_scale, 0);
-            fetch(sm.v, a.V, a.V_scale, 0);
+            fetch(sm.k, a.K, 0);
+            fetch(sm.v, a.V, 0);
         } else {
             __syncthreads();
         }
@@ -165,7 +128,7 @@ __global__ void __launch_bounds__(kThreads) paged_prompt_rows_kernel(const __gri
 #pragma unroll
             for (int j = 0; j < 4; ++j) there[j] = sm.row[t & 1][tx + 16 * j] >= 0;
             __syncthreads();
-            if (t + 1 < nt) fetch(sm.k, a.K, a.K_scale, t + 1);
+            if (t + 1 < nt) fetch(sm.k, a.K, t + 1);
             else cp_commit();
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
@@ -218,7 +181,7 @@ __global__ void __launch_bounds__(kThreads) paged_prompt_rows_kernel(const __gri
                 }
             }
             __syncthreads();
-            if (t + 1 < nt) fetch(sm.v, a.V, a.V_scale, t + 1);
+            if (t + 1 < nt) fetch(sm.v, a.V, t + 1);
             else cp_commit();
             if (t + 2 < nt) places(t + 2);
         }
@@ -237,16 +200,12 @@ __global__ void __launch_bounds__(kThreads) paged_prompt_rows_kernel(const __gri
                 const bool some = l[r] != 0.0f && row.kept;
                 const float n = some ? 1.0f / l[r] : 0.0f;
                 const long long at = static_cast<long long>(row.token) * a.H + row.head;
-                Io* out = static_cast<Io*>(a.out) + at * a.dh;
+                float* out = static_cast<float*>(a.out) + at * a.dh;
 #pragma unroll
                 for (int g = 0; g < V; ++g)
-                    if (tx * 4 + 64 * g < a.dh) {
-                        alignas(16) Io y[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) y[e] = from_float<Io>(some ? o[r][4 * g + e] * n : 0.0f);
-                        if constexpr (sizeof(Io) == 4) *reinterpret_cast<uint4*>(out + tx * 4 + 64 * g) = *reinterpret_cast<const uint4*>(y);
-                        else *reinterpret_cast<uint2*>(out + tx * 4 + 64 * g) = *reinterpret_cast<const uint2*>(y);
-                    }
+                    if (tx * 4 + 64 * g < a.dh)
+                        *reinterpret_cast<float4*>(out + tx * 4 + 64 * g) = some ? make_float4(o[r][4 * g] * n, o[r][4 * g + 1] * n, o[r][4 * g + 2] * n, o[r][4 * g + 3] * n)
+                                                                                 : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 if (tx == 0 && a.lse) a.lse[at] = some ? (m[r] + log2f(l[r])) * kLn2 : -INFINITY;
             } else if (i < a.rows) {
                 if (tx == 0) {
@@ -279,23 +238,6 @@ auto by_width(const halo_paged_shape& sh, F f) {
                                 : f(std::integral_constant<int, 256>());
 }
 
-template <typename T>
-halo_status launch(const Args& args, const halo_paged_shape& sh, void* workspace, cudaStream_t st) {
-    return by_width(sh, [&](auto dp) -> halo_status {
-        constexpr int DP = decltype(dp)::value;
-        static bool done[64];
-        if (!ensure_dynamic_smem(paged_prompt_rows_kernel<T, DP>, sizeof(Smem<DP>), done)) return HALO_ERR_CUDA;
-        Args a = args;
-        a.blocks = blocks_of<DP>(sh, a.n_tok, a.n_seq);
-        a.rows = slot_rows(kRows, a.n_tok, sh);
-        a.slot = slot_floats(a.rows, a.dh);
-        a.openings = static_cast<Opening*>(workspace);
-        a.ws = reinterpret_cast<float*>(a.openings + a.blocks);
-        const halo_status rc = launch_chained(paged_prompt_rows_kernel<T, DP>, a.blocks, kThreads, sizeof(Smem<DP>), st, a);
-        return rc != HALO_OK ? rc : launch_join<typename Kind<T>::Io, kRows>(a, st);
-    });
-}
-
 }  // namespace
 
 size_t f32_workspace(const halo_paged_shape& sh, int n_tok, int n_seq) {
@@ -304,9 +246,20 @@ size_t f32_workspace(const halo_paged_shape& sh, int n_tok, int n_seq) {
                (sizeof(Opening) + 2 * sizeof(float) * slot_floats(slot_rows(kRows, n_tok, sh), sh.head_dim));
     });
 }
-halo_status f32_launch(const Args& a, const halo_paged_shape& sh, void* workspace, cudaStream_t st) {
-    if (sh.dtype == HALO_F32) return launch<float>(a, sh, workspace, st);
-    return a.K_scale ? launch<Eight>(a, sh, workspace, st) : launch<__nv_bfloat16>(a, sh, workspace, st);
+halo_status f32_launch(const Args& args, const halo_paged_shape& sh, void* workspace, cudaStream_t st) {
+    return by_width(sh, [&](auto dp) -> halo_status {
+        constexpr int DP = decltype(dp)::value;
+        static bool done[64];
+        if (!ensure_dynamic_smem(paged_prompt_rows_kernel<DP>, sizeof(Smem<DP>), done)) return HALO_ERR_CUDA;
+        Args a = args;
+        a.blocks = blocks_of<DP>(sh, a.n_tok, a.n_seq);
+        a.rows = slot_rows(kRows, a.n_tok, sh);
+        a.slot = slot_floats(a.rows, a.dh);
+        a.openings = static_cast<Opening*>(workspace);
+        a.ws = reinterpret_cast<float*>(a.openings + a.blocks);
+        const halo_status rc = launch_chained(paged_prompt_rows_kernel<DP>, a.blocks, kThreads, sizeof(Smem<DP>), st, a);
+        return rc != HALO_OK ? rc : launch_join<float, kRows>(a, st);
+    });
 }
 
 }  // namespace prompt

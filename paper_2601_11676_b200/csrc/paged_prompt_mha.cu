@@ -4,7 +4,7 @@
 // Per thread block, one to an SM:
 //   - warps 8 to 11 gather K and V rows of 128 keys from their pages into a ring of stages (128 keys x 128 columns a stage, in the
 //     128-byte swizzle that the tensor cores read) and an item's rows of Q: boxes of a page's rows by the copy engine, or, where
-//     pages are no whole number of eight rows, row by row;
+//     pages are no whole number of eight rows, row by row; 8-bit rows row by row as codes, widened to bf16 on the way to a stage;
 //   - one thread of warp 12 issues the products: S = Q K^T into tensor memory, O += P V with P in tensor memory;
 //   - warps 0 to 3 and 4 to 7 take a row per thread: running maximum and sum, P = 2^(S scale - maximum) as bf16 in place of S.
 // An item has 256 rows in two streams of 128: while one stream's rows are in the softmax, the other's products run.  Head sizes
@@ -37,15 +37,16 @@ constexpr int kThreads = 512;
 constexpr int kOver = 4;           // an item's rows, first scores and outputs cost about as much as four tiles
 constexpr int kFlags = 8;          // tiles whose flags are kept
 
-// DP: head size padded to 64, 128 or 256.
-template <int DP>
+// DP: head size padded to 64, 128 or 256.  EIGHT: 8-bit rows.
+template <int DP, bool EIGHT = false>
 struct Cfg {
     static constexpr int kStreams = DP > 128 ? 1 : 2;
     static constexpr int kRows = 128 * kStreams;
     static constexpr int kCols = DP < 128 ? DP : 128;         // of a stage
     static constexpr int kParts = DP / kCols;                 // stages of a K or V tile
     static constexpr int kStage = kTile * kCols * 2;
-    static constexpr int kStages = DP == 64 ? 8 : 5;
+    static constexpr int kStages = DP == 64 ? 8 : EIGHT ? 4 : 5;
+    static constexpr int kRaw = EIGHT ? kTile * kCols : 0;    // codes of a stage
     static constexpr int kQTile = 128 * DP * 2;               // Q of a stream
     static constexpr int kQ = kStreams * kQTile;
     // tensor memory: S at 0 and 128, O behind; P in a place of its own where there is one, else over the S that it comes from
@@ -67,10 +68,11 @@ struct Bars {
     uint32_t tmem;
     int abort;
 };
-template <int DP>
+template <int DP, bool EIGHT>
 struct Smem {
-    unsigned char q[Cfg<DP>::kQ];
-    unsigned char ring[Cfg<DP>::kStages * Cfg<DP>::kStage];
+    unsigned char q[Cfg<DP, EIGHT>::kQ];
+    unsigned char ring[Cfg<DP, EIGHT>::kStages * Cfg<DP>::kStage];
+    unsigned char raw[2 * Cfg<DP, EIGHT>::kRaw + 16];
     long long q_row[Cfg<DP>::kRows];     // where the item's rows of q are, -1: none
     Flags flags;
     Bars bars;
@@ -131,13 +133,26 @@ __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&v
         "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
         : "memory");
 }
+// tcgen05.ld has delivered v: nothing that uses it can be moved in front of the wait
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
+                   "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]),
+                   "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]),
+                   "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])::"memory");
+}
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&v)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
+                   "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-// 512 threads start with 128 registers each: 2 * 128 * 208 + 2 * 128 * 48 = 512 * 128
-constexpr int kRowRegs = 208, kCopyRegs = 48, kIssueRegs = 48;
+// 512 threads start with 128 registers each: 2 * 128 * 176 + 128 * 88 + 128 * 72 = 512 * 128
+constexpr int kRowRegs = 176, kCopyRegs = 88, kIssueRegs = 72;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
     const int n = valid ? 16 : 0;   // 0: the 16 bytes are filled with zeros and src is not read
@@ -146,6 +161,11 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool v
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint32_t times_bf16(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
@@ -180,14 +200,14 @@ struct Maps {
     int box_rows, whole_q;      // 0: rows are gathered one by one (pages of odd sizes, head sizes below 64, head counts that do not divide 128)
 };
 
-template <int DP>
+template <int DP, bool EIGHT>
 struct Gather {
-    using C = Cfg<DP>;
-    static constexpr int kChunks = C::kCols / 8;           // 16-byte chunks of a stage's row
-    static constexpr int kAtOnce = 32 / kChunks;           // rows per instruction
+    using C = Cfg<DP, EIGHT>;
+    [[maybe_unused]] static constexpr int kChunks = C::kCols / 8;           // 16-byte chunks of a stage's row
+    [[maybe_unused]] static constexpr int kAtOnce = 32 / kChunks;           // rows per instruction
     const Args& a;
     const Maps& maps;
-    Smem<DP>& sm;
+    Smem<DP, EIGHT>& sm;
     int* abort;
     const int warp, lane;
     uint32_t fill = 0, cleared = 0;      // stages filled so far, and stages of values that rows were taken out of
@@ -195,7 +215,7 @@ struct Gather {
     int n_waiting = 0;
     bool alive = true;
 
-    __device__ __forceinline__ Gather(const Args& a_, const Maps& m_, Smem<DP>& sm_)
+    __device__ __forceinline__ Gather(const Args& a_, const Maps& m_, Smem<DP, EIGHT>& sm_)
         : a(a_), maps(m_), sm(sm_), abort(&sm_.bars.abort), warp((threadIdx.x >> 5) & 3), lane(threadIdx.x & 31) {}
     __device__ __forceinline__ void signal(uint32_t bar) {
         fence_proxy_async_smem();
@@ -318,6 +338,59 @@ struct Gather {
         issued(full);
         flush();           // the first scores wait for them
     }
+    // 8-bit rows: codes of this warp's 32 keys into a slot of their own, 16 a lane and instruction
+    [[maybe_unused]] static constexpr int kCodes = C::kCols / 16, kCodeRows = 32 / kCodes;
+    __device__ __forceinline__ uint32_t code_place(int slot, int r) const {
+        return smem_u32(sm.raw) + slot * C::kRaw + (warp * 32 + r) * C::kCols + (lane % kCodes) * 16;
+    }
+    __device__ __forceinline__ void codes(const void* cache, long long at, int part, int slot) {
+        const int col = part * C::kCols + (lane % kCodes) * 16;
+        const uint8_t* src = static_cast<const uint8_t*>(cache) + col;
+#pragma unroll
+        for (int i = 0; i < 32 / kCodeRows; ++i) {
+            const int r = i * kCodeRows + lane / kCodes;
+            const long long from = __shfl_sync(0xffffffffu, at, r);
+            const bool there = from >= 0 && col < a.dh;
+            cp_async16(code_place(slot, r), there ? src + from : src, there);
+        }
+        cp_commit();
+    }
+    // ... and on to a stage as bf16.  A code's bits are a bf16 number's exponent and significand, of 2^-120 of its value; the row's power
+    // of two puts that right: without rounding, as every value of a row is a bf16 number.  byte: of this lane's key's row.
+    __device__ __forceinline__ void widen(uint32_t byte, int slot) {
+        const uint32_t s = fill % C::kStages, phase = fill / C::kStages;
+        await(&sm.bars.empty[s], phase + 1);
+        if (!alive) return;
+        ++fill;
+        const uint32_t dst = smem_u32(sm.ring) + s * C::kStage;
+        // 2^(120 + e), in two steps where that is past the largest power; 0 for a row that is not there
+        const int e = static_cast<int>(byte) - 127;
+        const float one = byte == 0 ? 0.0f : byte == kEightNan ? __uint_as_float(0x7fc00000u) : eight_power(120 + min(e, 7));
+        const float two = byte == kEightNan ? 1.0f : eight_power(max(e, 7) - 7);
+        const uint32_t steps = pack_bf16(one, two);
+        const bool far = __any_sync(0xffffffffu, two != 1.0f);
+#pragma unroll
+        for (int i = 0; i < 32 / kCodeRows; ++i) {
+            const int r = i * kCodeRows + lane / kCodes, c = lane % kCodes;
+            const uint32_t by = __shfl_sync(0xffffffffu, steps, r);
+            const uint32_t by_one = __byte_perm(by, by, 0x1010), by_two = __byte_perm(by, by, 0x3232);
+            uint4 v;
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(code_place(slot, r)));
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            uint32_t o[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t t = __byte_perm(w[k >> 1], 0, k & 1 ? 0x3424 : 0x1404);      // a code in the upper byte of each half
+                o[k] = times_bf16(((t >> 4) & 0x07f007f0u) | (t & 0x80008000u), by_one);
+                if (far) o[k] = times_bf16(o[k], by_two);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(place(dst, r, 2 * c + h)), "r"(o[4 * h]), "r"(o[4 * h + 1]), "r"(o[4 * h + 2]),
+                             "r"(o[4 * h + 3]) : "memory");
+        }
+        signal(smem_u32(&sm.bars.full[s]));
+    }
     __device__ void run(Walk<C::kRows, kTile, kOver> w) {
         bool bad = false;
         uint32_t tile = 0, piece = 0;
@@ -335,6 +408,48 @@ struct Gather {
                 queries(w, p, piece);
                 asked = true;
             }
+            if constexpr (EIGHT) {
+                // a stage's codes are on their way while the ones before them are widened
+                constexpr int kFills = 2 * C::kParts;
+                long long at = -1;               // of this lane's key's rows in the tile whose codes are asked for
+                uint32_t kb = 0, vb = 0;         // their scale bytes
+                const auto ask = [&](int f) {    // the codes of the f-th stage of the piece
+                    const int j = f / kFills, h = f % kFills;
+                    if (h == 0) {
+                        const int pos = (w.t0 + j) * kTile + warp * 32 + lane;
+                        const bool in = pos < w.reach, ok = in && page >= 0 && page < a.n_pages;
+                        bad |= in && !ok;
+                        const int in_page = a.page_shift >= 0 ? pos & (a.page_size - 1) : pos % a.page_size;
+                        const long long row = static_cast<long long>(w.kvh) * a.page_size + in_page;
+                        at = ok ? page * a.page_stride + row * a.dh : -1;
+                        kb = vb = 0;
+                        if (ok) {
+                            kb = ldg_waited(a.K_scale + static_cast<long long>(page) * a.Hk * a.page_size + row);
+                            vb = ldg_waited(a.V_scale + static_cast<long long>(page) * a.Hk * a.page_size + row);
+                        }
+                        page = page_of(j + 1);
+                    }
+                    codes(h < C::kParts ? a.K : a.V, at, h % C::kParts, f & 1);
+                };
+                if (p.n > 0) ask(0);
+                for (int f = 0; f < p.n * kFills && alive; ++f) {
+                    const int h = f % kFills;
+                    const uint32_t byte = h < C::kParts ? kb : vb, there = __ballot_sync(0xffffffffu, at >= 0);
+                    if (h == 0 && lane == 0) sm.flags.there[tile % kFlags][warp] = there;
+                    if (h == kFills - 1) ++tile;
+                    if (f + 1 < p.n * kFills) {
+                        ask(f + 1);
+                        cp_wait<1>();
+                    } else {
+                        cp_wait<0>();
+                    }
+                    widen(byte, f & 1);
+                    if (f == kFills - 1 && !asked && alive) {
+                        queries(w, p, piece);
+                        asked = true;
+                    }
+                }
+            } else {
             for (int j = 0; j < p.n && alive; ++j, ++tile) {
                 const int next = page_of(j + 1);
                 const int pos = (w.t0 + j) * kTile;
@@ -354,6 +469,7 @@ struct Gather {
                 }
                 page = next;
             }
+            }
             if (p.n > 0) ++piece;
             w.next(a);
         }
@@ -370,18 +486,18 @@ using Const = std::integral_constant<int, N>;
 // One warp, one lane of which issues.  Lanes (of barriers) are constants, so that counters and addresses stay in registers: the
 // tensor cores take a product of 16 columns in 64 clocks, and one must not take longer to issue.  What is issued next goes by what is
 // ready: a stream's weights (P V), else its next scores, so that a stream never waits behind the other's softmax.
-template <int DP>
+template <int DP, bool EIGHT>
 struct Issue {
-    using C = Cfg<DP>;
+    using C = Cfg<DP, EIGHT>;
     const Args& a;
-    Smem<DP>& sm;
+    Smem<DP, EIGHT>& sm;
     Bars& bars;
     int* abort;
     const uint32_t lead, tmem, q0, ring, idesc_s;
     uint32_t first_fill = 0, use0 = 0, use1 = 0, use2 = 0;      // stages of the pieces before; tiles of each lane so far
     int last = 1;                                               // lane that the second buffer was used in last
 
-    __device__ __forceinline__ Issue(const Args& a_, Smem<DP>& sm_)
+    __device__ __forceinline__ Issue(const Args& a_, Smem<DP, EIGHT>& sm_)
         : a(a_), sm(sm_), bars(sm_.bars), abort(&sm_.bars.abort), lead(elect()), tmem(sm_.bars.tmem), q0(smem_u32(sm_.q) >> 4),
           ring(smem_u32(sm_.ring) >> 4),
           // a negative scale: -Q instead, so that the largest score stays the largest product
@@ -615,8 +731,8 @@ __device__ __forceinline__ void turn_words(uint4 (&w)[4], int lane) {
     }
 }
 
-template <int DP>
-__device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, kTile, kOver> w, long long total) {
+template <int DP, bool EIGHT>
+__device__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm, Walk<Cfg<DP>::kRows, kTile, kOver> w, long long total) {
     using C = Cfg<DP>;
     constexpr float kSlack = 8.0f;            // powers of two that a reference may lag behind where it is looked at
     constexpr float kSum = 1048576.0f;        // what a tile's weights may sum to before it is
@@ -649,55 +765,60 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
                 uint32_t there[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) there[c] = *const_cast<volatile const uint32_t*>(&sm.flags.there[(tile + j) % kFlags][c]);
-                uint32_t sc[4][32], pk[4][16];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld_32x32(s_addr + c * 32, sc[c]);
-                tmem_ld_wait();
                 const bool masked = p0 + kTile > all_see || (there[0] & there[1] & there[2] & there[3]) != 0xffffffffu;
-                Pair sum[2];
-                const auto weights = [&]() {
-                    const Pair times = twice(scale), minus = twice(m == -INFINITY ? 0.0f : -m * scale);
-                    sum[0] = sum[1] = 0;
+                uint32_t pk[4][16];
+                // 32 scores at a time, the next on their way; mask: what the row does not see as -infinity
+                const auto each = [&](auto mask, auto use) {
+                    uint32_t sc[2][32];
+                    tmem_ld_32x32(s_addr, sc[0]);
+                    tmem_ld_wait_for(sc[0]);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
+                    for (int c = 0; c < 4; ++c) {
+                        if (c < 3) tmem_ld_32x32(s_addr + (c + 1) * 32, sc[(c + 1) & 1]);
+                        if (decltype(mask)::value) {
+                            const int left = row.sees - p0 - c * 32;
+                            const uint32_t in = left >= 32 ? there[c] : left <= 0 ? 0u : there[c] & ((1u << left) - 1u);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!(in >> e & 1u)) sc[c & 1][e] = 0xff800000u;
+                        }
+                        use(c, sc[c & 1]);
+                        if (c < 3) tmem_ld_wait_for(sc[(c + 1) & 1]);
+                    }
+                };
+                const auto weights = [&](auto mask) {
+                    const Pair times = twice(scale), minus = twice(m == -INFINITY ? 0.0f : -m * scale);
+                    Pair sum[2] = {0, 0};
+                    each(mask, [&](int c, const uint32_t (&sc)[32]) {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            const Pair x = fma2(pair_of(__uint_as_float(sc[c][2 * e]), __uint_as_float(sc[c][2 * e + 1])), times, minus);
+                            const Pair x = fma2(pair_of(__uint_as_float(sc[2 * e]), __uint_as_float(sc[2 * e + 1])), times, minus);
                             float2 y = both(x);
                             y = make_float2(pow2(y.x), pow2(y.y));
                             sum[e & 1] = add2(sum[e & 1], pair_of(y.x, y.y));
                             pk[c][e] = pack_bf16(y.x, y.y);
                         }
+                    });
                     const float2 s0 = both(sum[0]), s1 = both(sum[1]);
                     return (s0.x + s0.y) + (s1.x + s1.y);
                 };
                 float more = INFINITY;
-                if (!masked && __all_sync(0xffffffffu, m > -INFINITY)) more = weights();
+                if (!masked && __all_sync(0xffffffffu, m > -INFINITY)) more = weights(Const<0>());
                 if (__any_sync(0xffffffffu, !(more < kSum))) {
-                    // masks, a new reference, or something infinite or NaN: from the scores again, exactly
+                    // masks, the first tile, a new reference, or something infinite or NaN: from the scores again
+                    float mx = -INFINITY;
+                    each(Const<1>(), [&](int, const uint32_t (&sc)[32]) {
+                        float most[4];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld_32x32(s_addr + c * 32, sc[c]);
-                    tmem_ld_wait();
-                    if (masked) {
+                        for (int q = 0; q < 4; ++q) most[q] = max3(__uint_as_float(sc[q]), __uint_as_float(sc[q + 4]), __uint_as_float(sc[q + 8]));
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const int left = row.sees - p0 - c * 32;
-                            const uint32_t in = left >= 32 ? there[c] : left <= 0 ? 0u : there[c] & ((1u << left) - 1u);
+                        for (int e = 12; e < 28; e += 8)
 #pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                if (!(in >> e & 1u)) sc[c][e] = 0xff800000u;
-                        }
-                    }
-                    float most[4];
+                            for (int q = 0; q < 4; ++q) most[q] = max3(most[q], __uint_as_float(sc[e + q]), __uint_as_float(sc[e + 4 + q]));
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) most[c] = max3(__uint_as_float(sc[c][0]), __uint_as_float(sc[c][1]), __uint_as_float(sc[c][2]));
-#pragma unroll
-                    for (int e = 3; e < 31; e += 2)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) most[c] = max3(most[c], __uint_as_float(sc[c][e]), __uint_as_float(sc[c][e + 1]));
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) most[c] = max2(most[c], __uint_as_float(sc[c][31]));
-                    const float mx = max2(max3(most[0], most[1], most[2]), most[3]);
+                        for (int q = 0; q < 4; ++q) most[q] = max2(most[q], __uint_as_float(sc[28 + q]));
+                        mx = max3(max3(most[0], most[1], most[2]), most[3], mx);
+                    });
                     if (__any_sync(0xffffffffu, (mx - m) * scale > kSlack)) {      // not where it is NaN: all weights of the row are
                         const float to = fmaxf(m, mx), f = m == -INFINITY ? 0.0f : pow2((m - to) * scale);
                         if (j > 0) {
@@ -706,7 +827,7 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
                             for (int c = 0; c < a.dh; c += 16) {
                                 uint32_t o[16];
                                 tmem_ld_32x16(o_addr + c, o);
-                                tmem_ld_wait();
+                                tmem_ld_wait_for(o);
 #pragma unroll
                                 for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
                                 tmem_st_32x16(o_addr + c, o);
@@ -715,7 +836,7 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
                         l *= f;
                         m = to;
                     }
-                    more = weights();
+                    more = weights(Const<1>());
                 }
                 l += more;
                 if (C::kApart && j > (p.streams == 2 ? 0 : 1)) {      // the P before it in its place has been read
@@ -750,7 +871,8 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
                     if (n > 0) {
                         tmem_ld_32x16(o_addr + c, o[0]);
                         if (c + 16 < a.dh) tmem_ld_32x16(o_addr + c + 16, o[1]);
-                        tmem_ld_wait();
+                        tmem_ld_wait_for(o[0]);
+                        tmem_ld_wait_for(o[1]);
                     }
                     uint4 y[4];
 #pragma unroll
@@ -780,7 +902,7 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
                     uint32_t o[16] = {};
                     if (n > 0) {
                         tmem_ld_32x16(o_addr + c, o);
-                        tmem_ld_wait();
+                        tmem_ld_wait_for(o);
                     }
 #pragma unroll
                     for (int e = 0; e < 16; ++e) odd |= !(fabsf(__uint_as_float(o[e])) < INFINITY);
@@ -810,11 +932,11 @@ __device__ void softmax_rows(const Args& a, Smem<DP>& sm, Walk<Cfg<DP>::kRows, k
     }
 }
 
-template <int DP>
+template <int DP, bool EIGHT>
 __global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
-    using C = Cfg<DP>;
+    using C = Cfg<DP, EIGHT>;
     extern __shared__ __align__(1024) unsigned char raw[];
-    Smem<DP>& sm = *reinterpret_cast<Smem<DP>*>(raw);
+    Smem<DP, EIGHT>& sm = *reinterpret_cast<Smem<DP, EIGHT>*>(raw);
     Bars& bars = sm.bars;
     const int tid = threadIdx.x, warp = tid >> 5;
     chain_wait();
@@ -845,13 +967,13 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __g
     tcgen05_fence_after_sync();
     if (warp < 8) {
         more_registers<kRowRegs>();
-        softmax_rows<DP>(a, sm, f.walk, f.total);
+        softmax_rows<DP, EIGHT>(a, sm, f.walk, f.total);
     } else if (warp < 12) {
         fewer_registers<kCopyRegs>();
-        Gather<DP>(a, maps, sm).run(f.walk);
+        Gather<DP, EIGHT>(a, maps, sm).run(f.walk);
     } else {
         fewer_registers<kIssueRegs>();
-        if (warp == 12) Issue<DP>(a, sm).run(f.walk);
+        if (warp == 12) Issue<DP, EIGHT>(a, sm).run(f.walk);
     }
     __syncwarp();
     tcgen05_fence_before_sync();
@@ -873,8 +995,6 @@ auto by_width(const halo_paged_shape& sh, F f) {
            : sh.head_dim <= 128 ? f(std::integral_constant<int, 128>())
                                 : f(std::integral_constant<int, 256>());
 }
-bool tensor_cores(const halo_paged_shape& sh, bool eight) { return sh.dtype == HALO_BF16 && !eight; }
-
 size_t workspace(const halo_paged_shape& sh, int n_tok, int n_seq) {
     return by_width(sh, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
@@ -885,8 +1005,6 @@ size_t workspace(const halo_paged_shape& sh, int n_tok, int n_seq) {
 halo_status launch(const Args& args, const halo_paged_shape& sh, void* ws, cudaStream_t st) {
     return by_width(sh, [&](auto dp) -> halo_status {
         constexpr int DP = decltype(dp)::value;
-        static bool done[64];
-        if (!ensure_dynamic_smem(paged_prompt_mha_kernel<DP>, sizeof(Smem<DP>), done)) return HALO_ERR_CUDA;
         Args a = args;
         a.blocks = blocks_of<DP>(sh, a.n_tok, a.n_seq);
         a.rows = slot_rows(Cfg<DP>::kRows, a.n_tok, sh);
@@ -896,7 +1014,7 @@ halo_status launch(const Args& args, const halo_paged_shape& sh, void* ws, cudaS
         Maps maps = {};
         const uint64_t wide = sh.head_dim, row = wide * 2;
         const int page_bits = sh.page_size & -sh.page_size;
-        if (wide >= 64 && page_bits >= 8) {
+        if (wide >= 64 && page_bits >= 8 && !a.K_scale) {
             maps.box_rows = page_bits < 32 ? page_bits : 32;
             const uint64_t dims[4] = {wide, static_cast<uint64_t>(sh.page_size), static_cast<uint64_t>(a.Hk), static_cast<uint64_t>(sh.n_pages)};
             const uint64_t strides[3] = {row, row * sh.page_size, static_cast<uint64_t>(a.page_stride) * 2};
@@ -910,7 +1028,13 @@ halo_status launch(const Args& args, const halo_paged_shape& sh, void* ws, cudaS
             const uint32_t box[3] = {64, static_cast<uint32_t>(a.G), static_cast<uint32_t>(128 / a.G)};
             if (!make_bf16_map_nd(&maps.q, a.q, 3, dims, strides, box)) return HALO_ERR_CUDA;
         }
-        const halo_status rc = launch_chained(paged_prompt_mha_kernel<DP>, a.blocks, kThreads, sizeof(Smem<DP>), st, a, maps);
+        const auto run = [&](auto eight) -> halo_status {
+            constexpr bool E = decltype(eight)::value;
+            static bool done[64];
+            if (!ensure_dynamic_smem(paged_prompt_mha_kernel<DP, E>, sizeof(Smem<DP, E>), done)) return HALO_ERR_CUDA;
+            return launch_chained(paged_prompt_mha_kernel<DP, E>, a.blocks, kThreads, sizeof(Smem<DP, E>), st, a, maps);
+        };
+        const halo_status rc = a.K_scale ? run(std::true_type()) : run(std::false_type());
         return rc != HALO_OK ? rc : launch_join<__nv_bfloat16, Cfg<DP>::kRows>(a, st);
     });
 }
@@ -923,10 +1047,7 @@ using namespace halo;
 
 extern "C" size_t halo_paged_prompt_mha_workspace_bytes(const halo_paged_shape* shape, int n_tok, int n_seq) {
     if (check_paged_shape(shape) != HALO_OK || n_seq <= 0 || n_seq > HALO_MAX_SEQUENCES || n_tok <= 0 || n_tok > HALO_MAX_PROMPT_ROWS) return 0;
-    const size_t rows = prompt::f32_workspace(*shape, n_tok, n_seq);
-    if (shape->dtype == HALO_F32) return rows;
-    const size_t ts = prompt::workspace(*shape, n_tok, n_seq);
-    return rows > ts ? rows : ts;
+    return shape->dtype == HALO_F32 ? prompt::f32_workspace(*shape, n_tok, n_seq) : prompt::workspace(*shape, n_tok, n_seq);
 }
 
 extern "C" halo_status halo_paged_prompt_mha(const halo_paged_shape* shape, int n_tok, int n_seq, const void* q, long long q_stride,
@@ -977,5 +1098,5 @@ extern "C" halo_status halo_paged_prompt_mha(const halo_paged_shape* shape, int 
     a.lse = lse;
     a.status = dev_status;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return prompt::tensor_cores(*shape, K_scale != nullptr) ? prompt::launch(a, *shape, workspace, st) : prompt::f32_launch(a, *shape, workspace, st);
+    return shape->dtype == HALO_F32 ? prompt::f32_launch(a, *shape, workspace, st) : prompt::launch(a, *shape, workspace, st);
 }
