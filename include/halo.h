@@ -505,7 +505,7 @@ halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, const void*
  *
  * halo_paged_mha_f8: halo_paged_mha over an 8-bit cache; its own workspace size.  A query enters the scores with the bits of
  *   fp16 relative to its row's largest element (8 bits of bf16 fit; what is below 2^-39 of the largest loses some); a weight
- *   meets the values rounded to fp16 (off by at most 2^-11 of itself, or by 2^-40 of what the largest can be).
+ *   meets the values rounded to fp16 (off by at most 2^-11 of itself, or by 2^-34 of what the largest can be).
  *
  * halo_paged_prompt_mha: causal attention of packed chunks of new tokens.  Rows q_start[s] .. q_start[s + 1] - 1 of q are the n_s
  *   newest tokens of sequence s, whose keys and values are in the cache already: row i of them is at position

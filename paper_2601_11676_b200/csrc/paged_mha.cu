@@ -20,13 +20,14 @@
 //     4096 positions 92.7 us with one number, 93.1 with two; 128 of up to 300 positions, 32 / 32 heads, 96 and 99; 16 heads on
 //     one, a sequence of 131071 29.0 and 29.8).
 //   fp32: fused multiply-adds, two lanes per position for the scores, a column per lane for the weighted sums.
-//   8-bit rows (halo_paged_mha_f8): as bf16, through mma.sync on fp16.  A code's bits, shifted by one, are an fp16 number 2^-8
-//     of its value, so three instructions bring two codes to the tensor cores and no product is rounded; which two codes
-//     share a register decides the order of the elements, and the queries' registers follow it.  Queries come as fp16, a row times
-//     the power of two that brings its largest element to 2^14 (their 8 bits fit; elements below 2^-39 of the largest lose
-//     some).  A position's power of two of the keys multiplies its scores; that of the values its weights, relative to
-//     the largest so far.  Weights are rounded to fp16 once, times 2^15 (off by at most 2^-11 of themselves, an
-//     eighth of what the output's own rounding is; those below 2^-29 of the largest lose bits, 2^-40 of it at most).
+//   8-bit rows (halo_paged_mha_f8): mma.sync on fp16, keys and values as the 16 rows of A, heads as the 8 columns of B; codes are fp16
+//     numbers exactly (one conversion for two of them), so no product is rounded, and a lane's codes decide the order of the
+//     elements, which the queries' registers follow.
+//     Queries come as fp16, a row times the power of two that brings its largest element to 2^14 (their 8 bits fit; elements
+//     below 2^-39 of the largest lose some).  A position's power of two of the keys multiplies its scores; that of the values its
+//     weights, relative to the largest so far.  Weights are relative to a reference that a score may pass by 2^6 before it
+//     moves, and rounded to fp16 once, times 2^9 (off by at most 2^-11 of themselves, an eighth of what the output's own
+//     rounding is; those below 2^-23 lose bits, 2^-34 at most).
 //
 // bf16, 32 / 8 heads of 128, both kernels: one sequence of 131071 positions 91 us (537 MB: 5.9 TB/s; HBM, and the join
 // behind it), 64 sequences of up to 4096 positions 93 to 95 us (besides, a piece's start and meeting); one sequence of 700
@@ -122,12 +123,26 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], u
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Codes 1 and 3 of a word, and 0 and 2, as fp16 numbers 2^-8 of their values.
-__device__ __forceinline__ uint32_t odd_codes(uint32_t w) { return ((w >> 1) & 0x3f803f80u) | (w & 0x80008000u); }
-__device__ __forceinline__ uint32_t even_codes(uint32_t w) { return odd_codes(w << 8); }
+// Codes 0 and 1 of a word, and 2 and 3, as fp16 numbers: exactly
+__device__ __forceinline__ uint32_t low_codes(uint32_t w) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(r) : "r"(w));
+    return r;
+}
+__device__ __forceinline__ uint32_t high_codes(uint32_t w) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, hi;\n\t}" : "=r"(r) : "r"(w));
+    return r;
+}
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
+}
+// An 8 x 8 matrix of 16-bit numbers, a row to four lanes, turned
+__device__ __forceinline__ uint32_t turn8(uint32_t a) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a));
     return r;
 }
 // 2^n for n <= 127, exactly; 0 below 2^-126
@@ -162,8 +177,10 @@ struct Cfg {
     // fp32: two stages, so that two thread blocks of four warps fit an SM at head sizes up to 64, or of three at 128 with
     // one query head per K/V head.  64 sequences of up to 2000 positions, 32 / 8 heads of 64: 77 us with three stages and
     // one thread block, 59 so; 5 of up to 900, 8 / 8 heads of 128: 13.1 us with one thread block of four warps, 10.4 so.
-    // 8-bit rows: half the bytes a stage, one more of them where that leaves several thread blocks per SM.
-    static constexpr int kStages = kF32 ? 2 : kEight && DP < 256 ? 4 : 3;
+    // 8-bit rows: the widening of codes bounds them, and more warps help more than more stages: with two and 8 heads, five thread
+    // blocks of 128 columns fit an SM (128 sequences of up to 600 positions, 32 heads of 128: 117 us with two, 131 with three; 16
+    // heads on one have registers for two thread blocks only: 64 sequences of 4000 108 us with two, 84 with three).
+    static constexpr int kStages = kF32 ? 2 : kEight && GR <= 8 ? 2 : 3;
     static constexpr int kTile = kWarps * kRun;
     static constexpr int kRowBytes = kF32 ? (DP + 8) * 4 : kEight ? DP : DP * 2;   // fp32: rows padded against bank conflicts; else swizzled
     static constexpr int kHalf = kRun * kRowBytes;                   // keys (or values) of one stage
@@ -458,39 +475,9 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
         const bool complete = con.t0 == 0 && con.t1 == con.nt;
         float* slot = a.ws + (static_cast<long long>(blockIdx.x) * 2 + (con.left == range ? 0 : 1)) * a.slot;
 
-        if constexpr (!kF32) {
+        if constexpr (!kF32 && !kEight) {
             constexpr int kK = GR > 8 ? 2 : 1;    // rows of a lane: g, and g + 8 where an item has more than 8 heads
             uint32_t qf[DP / 16][4];
-            [[maybe_unused]] float unit[kK];   // 8-bit rows: what a row's products are multiplied with
-            if constexpr (kEight) {
-                // elements 4 t4 to 4 t4 + 3 of every 16, in the order of the codes' registers
-#pragma unroll
-                for (int j = 0; j < kK; ++j) {
-                    const int r = g + j * 8;
-                    uint2 w[DP / 16];
-                    uint32_t top = 0;
-#pragma unroll
-                    for (int k = 0; k < DP / 16; ++k) {
-                        const unsigned long long v = r < rows && k * 16 < a.dh   // dh % 16 == 0
-                            ? ldg_waited(reinterpret_cast<const unsigned long long*>(qrow + static_cast<long long>(r) * a.dh + k * 16 + t4 * 4)) : 0ull;
-                        w[k] = make_uint2(static_cast<uint32_t>(v), static_cast<uint32_t>(v >> 32));
-                        top = max(max(top, w[k].x & 0x7fffu), (w[k].x >> 16) & 0x7fffu);
-                        top = max(max(top, w[k].y & 0x7fffu), (w[k].y >> 16) & 0x7fffu);
-                    }
-                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    // 2^up brings the largest element below 2^15; at least 2^-113, at most 2^120 (tiny rows stay smaller)
-                    const int up = min(14 + 127 - static_cast<int>(top >> 7), 120);
-                    const float n = eight_power(up);
-                    unit[j] = a.scale_log2 * eight_power(8 - up);
-#pragma unroll
-                    for (int k = 0; k < DP / 16; ++k) {
-                        qf[k][j] = pack_f16(bf16_lo(w[k].x) * n, bf16_lo(w[k].y) * n);
-                        qf[k][2 + j] = pack_f16(bf16_hi(w[k].x) * n, bf16_hi(w[k].y) * n);
-                        if (kK == 1) qf[k][1] = qf[k][3] = 0u;
-                    }
-                }
-            } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int r = g + (j & 1) * 8;
@@ -500,8 +487,6 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                 for (int k = 0; k < DP / 16; ++k)
                     qf[k][j] = there && k * 16 < a.dh ? ldg_waited(reinterpret_cast<const uint32_t*>(q + k * 16)) : 0u;   // dh % 16 == 0
             }
-            }
-            [[maybe_unused]] int top_byte = 0;   // 8-bit rows: the largest scale byte of the values so far; o is relative to it
             float o[NT][4];
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -519,50 +504,14 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                 cp_wait<S - 1>();
                 __syncwarp();
                 const uint32_t mask = masks[0];
-                [[maybe_unused]] uint32_t byte = 0;
-                if constexpr (kEight) byte = bytes[0];
 #pragma unroll
-                for (int i = 0; i + 1 < S; ++i) {
-                    masks[i] = masks[i + 1];
-                    if constexpr (kEight) bytes[i] = bytes[i + 1];
-                }
+                for (int i = 0; i + 1 < S; ++i) masks[i] = masks[i + 1];
                 const uint32_t st = ring_a + slot_out * C_::kStage;
                 if (++slot_out == S) slot_out = 0;
                 if (mask == 0) continue;
                 // scores of 16 heads x 16 positions, even and odd steps in two chains
                 float sc[2][4] = {}, sc2[2][4] = {};
-                [[maybe_unused]] float vf[2][2];   // 8-bit rows: what the weights of this lane's positions are multiplied with
-                [[maybe_unused]] float down = 1.0f;
-                if constexpr (kEight) {
-                    const int key = ((lane >> 3) & 1) * 8 + (lane & 7), second = lane >> 4;
-#pragma unroll
-                    for (int k = 0; k < DP / 16; k += 2) {
-                        uint32_t b[4];
-                        ldsm4(b, st + key * C_::kRowBytes + eight_chunk<DP>(key, k + second));
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            mma_f16(e ? sc2[0] : sc[0], qf[k + e], even_codes(b[2 * e]), odd_codes(b[2 * e]));
-                            mma_f16(e ? sc2[1] : sc[1], qf[k + e], even_codes(b[2 * e + 1]), odd_codes(b[2 * e + 1]));
-                        }
-                    }
-                    // lanes 0 to 15: the keys' powers of two; 16 to 31: the values', relative to the largest
-                    const int most = __reduce_max_sync(0xffffffffu, lane < 16 || byte == kEightNan ? 0 : static_cast<int>(byte));
-                    float own = eight_unit(byte);
-                    if (most > top_byte) {
-                        down = power(top_byte - most);
-                        top_byte = most;
-                    }
-                    if (lane >= 16 && byte != kEightNan) own = power(static_cast<int>(byte) - top_byte + 15);
-#pragma unroll
-                    for (int n = 0; n < 2; ++n)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const float kf = __shfl_sync(0xffffffffu, own, n * 8 + t4 * 2 + e);
-                            vf[n][e] = __shfl_sync(0xffffffffu, own, 16 + n * 8 + t4 * 2 + e);
-#pragma unroll
-                            for (int j = 0; j < kK; ++j) sc[n][2 * j + e] = (sc[n][2 * j + e] + sc2[n][2 * j + e]) * unit[j] * kf;
-                        }
-                } else {
+                {
                     const int key = (lane >> 4) * 8 + (lane & 7), half = (lane >> 3) & 1;
 #pragma unroll
                     for (int k = 0; k < DP / 16; ++k) {
@@ -574,12 +523,10 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                     }
                 }
                 // running softmax; a lane holds rows g (and g + 8), positions 2 * t4 + {0, 1} and 8 more
-                if constexpr (!kEight) {
 #pragma unroll
-                    for (int n = 0; n < 2; ++n)
+                for (int n = 0; n < 2; ++n)
 #pragma unroll
-                        for (int j = 0; j < 2 * kK; ++j) sc[n][j] = (sc[n][j] + sc2[n][j]) * a.scale_log2;
-                }
+                    for (int j = 0; j < 2 * kK; ++j) sc[n][j] = (sc[n][j] + sc2[n][j]) * a.scale_log2;
                 if (mask != 0xffffu) {
 #pragma unroll
                     for (int n = 0; n < 2; ++n)
@@ -604,9 +551,7 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
 #pragma unroll
                         for (int j = 2 * k; j < 2 * k + 2; ++j) sc[n][j] = pow2(sc[n][j] - base);
                     l[k] = fmaf(l[k], f[k], (sc[0][2 * k] + sc[0][2 * k + 1]) + (sc[1][2 * k] + sc[1][2 * k + 1]));
-                    if constexpr (kEight) f[k] *= down;
                 }
-                if constexpr (kEight) moved |= down != 1.0f;
                 if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
@@ -616,22 +561,6 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                 // weighted sum of the values: the weights' upper bits and their rests, these in the rows 8 to 15 of the
                 // same product (up to 8 heads; o[n][2], o[n][3] are their sums) or in one of their own
                 uint32_t pa[4], pr[4];
-                if constexpr (kEight) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        pa[j] = kK == 2 || !(j & 1) ? pack_f16(sc[j >> 1][(j & 1) * 2] * vf[j >> 1][0], sc[j >> 1][(j & 1) * 2 + 1] * vf[j >> 1][1]) : 0u;
-                    const int key = ((lane >> 3) & 1) * 8 + (lane & 7), second = lane >> 4;
-#pragma unroll
-                    for (int n = 0; n < NT; n += 4) {   // 32 columns; o[n], o[n + 1]: the even and the odd ones of 16
-                        uint32_t b[4];
-                        ldsm4t(b, st + C_::kHalf + key * C_::kRowBytes + eight_chunk<DP>(key, n / 2 + second));
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            mma_f16(o[n + 2 * e], pa, even_codes(b[2 * e]), even_codes(b[2 * e + 1]));
-                            mma_f16(o[n + 2 * e + 1], pa, odd_codes(b[2 * e]), odd_codes(b[2 * e + 1]));
-                        }
-                    }
-                } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float* w = &sc[j >> 1][kK == 2 ? (j & 1) * 2 : 0];
@@ -651,23 +580,9 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                         mma_bf16(o[n + 1], pr, b[2], b[3]);
                     }
                 }
-                }
                 __syncwarp();   // the stage is free for the copies that the next round starts
             }
-            // columns of o[n][0], o[n][1] (and 2, 3)
-            const auto col = [&](int n) { return kEight ? (n >> 1) * 16 + t4 * 4 + (n & 1) * 2 : n * 8 + t4 * 2; };
-            if constexpr (kEight) {   // neighbours side by side, and the values' own size: codes are 2^-8 of it, weights 2^15
-                const float size = eight_unit(static_cast<uint32_t>(top_byte));
-#pragma unroll
-                for (int n = 0; n < NT; n += 2)
-#pragma unroll
-                    for (int k = 0; k < kK; ++k) {
-                        const float x[4] = {o[n][2 * k], o[n + 1][2 * k], o[n][2 * k + 1], o[n + 1][2 * k + 1]};
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[n + (e >> 1)][2 * k + (e & 1)] = x[e] * 0x1p-7f * size;
-                    }
-            }
-            if constexpr (kK == 1 && !kEight) {
+            if constexpr (kK == 1) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n) { o[n][0] += o[n][2]; o[n][1] += o[n][3]; }
             }
@@ -700,7 +615,7 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                     if (g + k * 8 < rows) {
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
-                            *reinterpret_cast<float2*>(mg + (b * rows + g + k * 8) * C_::kMergeRow + col(n)) =
+                            *reinterpret_cast<float2*>(mg + (b * rows + g + k * 8) * C_::kMergeRow + n * 8 + t4 * 2) =
                                 make_float2(o[n][2 * k], o[n][2 * k + 1]);
                     }
             };
@@ -710,7 +625,7 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                     if (g + k * 8 < rows) {
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            const float2 v = *reinterpret_cast<const float2*>(mg + (b * rows + g + k * 8) * C_::kMergeRow + col(n));
+                            const float2 v = *reinterpret_cast<const float2*>(mg + (b * rows + g + k * 8) * C_::kMergeRow + n * 8 + t4 * 2);
                             o[n][2 * k] += v.x;
                             o[n][2 * k + 1] += v.y;
                         }
@@ -740,15 +655,243 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                         uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<Io*>(a.out) + row * a.dh);
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
-                            if (col(n) < a.dh) out[col(n) / 2] = some ? pack_bf16(o[n][2 * k] * f, o[n][2 * k + 1] * f) : 0u;
+                            if (n * 8 + t4 * 2 < a.dh) out[n * 4 + t4] = some ? pack_bf16(o[n][2 * k] * f, o[n][2 * k + 1] * f) : 0u;
                         if (t4 == 0 && a.lse) a.lse[row] = some ? (M[k] + log2f(L[k])) * kLn2 : -INFINITY;
                     } else {
                         if (t4 == 0) { slot[r] = M[k]; slot[16 + r] = L[k]; }
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
-                            *reinterpret_cast<float2*>(slot + kSlotHead + r * DP + col(n)) = make_float2(o[n][2 * k], o[n][2 * k + 1]);
+                            *reinterpret_cast<float2*>(slot + kSlotHead + r * DP + n * 8 + t4 * 2) = make_float2(o[n][2 * k], o[n][2 * k + 1]);
                     }
                 }
+            }
+        } else if constexpr (kEight) {
+            // Keys and values are the rows of A and the query heads the eight columns of B, so that no part of a product is
+            // empty: S^T = K Q^T, O^T = V^T P^T.  A lane has scores of keys g and g + 8, heads 2 t4 and 2 t4 + 1 (of eight).
+            constexpr int NB = GR / 8, NC = DP / 16;
+            constexpr float kLag = 6.0f;      // powers of two that a reference may lag behind: weights up to 2^6, times 2^9, fit fp16
+            uint32_t qf[NC][NB][2];
+            float unit[NB][2];                // what a head's products are multiplied with
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                // head g: elements 4 t4 to 4 t4 + 3 of every 16, where a lane has the keys' codes
+                const int r = b * 8 + g;
+                uint2 w[NC];
+                uint32_t top = 0;
+#pragma unroll
+                for (int k = 0; k < NC; ++k) {
+                    const unsigned long long v = r < rows && k * 16 < a.dh   // dh % 16 == 0
+                        ? ldg_waited(reinterpret_cast<const unsigned long long*>(qrow + static_cast<long long>(r) * a.dh + k * 16 + t4 * 4)) : 0ull;
+                    w[k] = make_uint2(static_cast<uint32_t>(v), static_cast<uint32_t>(v >> 32));
+                    top = max(max(top, w[k].x & 0x7fffu), (w[k].x >> 16) & 0x7fffu);
+                    top = max(max(top, w[k].y & 0x7fffu), (w[k].y >> 16) & 0x7fffu);
+                }
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                // 2^up brings the largest element below 2^15; at least 2^-114, at most 2^120 (tiny rows stay smaller)
+                const int up = min(14 + 127 - static_cast<int>(top >> 7), 120);
+                const float n = eight_power(up), own = a.scale_log2 * eight_power(-up);
+                unit[b][0] = __shfl_sync(0xffffffffu, own, t4 * 8);
+                unit[b][1] = __shfl_sync(0xffffffffu, own, t4 * 8 + 4);
+#pragma unroll
+                for (int k = 0; k < NC; ++k) {
+                    qf[k][b][0] = pack_f16(bf16_lo(w[k].x) * n, bf16_hi(w[k].x) * n);
+                    qf[k][b][1] = pack_f16(bf16_lo(w[k].y) * n, bf16_hi(w[k].y) * n);
+                }
+            }
+            float o[NC][NB][4], m[NB][2], l[NB][2];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                m[b][0] = m[b][1] = -INFINITY;
+                l[b][0] = l[b][1] = 0.0f;
+#pragma unroll
+                for (int n = 0; n < NC; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[n][b][j] = 0.0f;
+            }
+            int top_byte = 0;      // the largest scale byte of the values so far; o is relative to it
+
+            for (int t = con.t0; t < con.t1; ++t) {
+                masks[S - 1] = issue();
+                cp_wait<S - 1>();
+                __syncwarp();
+                const uint32_t mask = masks[0], byte = bytes[0];
+#pragma unroll
+                for (int i = 0; i + 1 < S; ++i) {
+                    masks[i] = masks[i + 1];
+                    bytes[i] = bytes[i + 1];
+                }
+                const uint32_t st = ring_a + slot_out * C_::kStage;
+                if (++slot_out == S) slot_out = 0;
+                if (mask == 0) continue;
+                const int key = ((lane >> 3) & 1) * 8 + (lane & 7), second = lane >> 4;
+                float sc[NB][4] = {}, sc2[NB][4] = {};      // even and odd steps in two chains
+#pragma unroll
+                for (int k = 0; k < NC; k += 2) {
+                    uint32_t c[4];
+                    ldsm4(c, st + key * C_::kRowBytes + eight_chunk<DP>(key, k + second));
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t x[4] = {low_codes(c[2 * e]), low_codes(c[2 * e + 1]), high_codes(c[2 * e]), high_codes(c[2 * e + 1])};
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) mma_f16(e ? sc2[b] : sc[b], x, qf[k + e][b][0], qf[k + e][b][1]);
+                    }
+                }
+                // lanes 0 to 15: the keys' powers of two; 16 to 31: the values', relative to the largest
+                const int most = __reduce_max_sync(0xffffffffu, lane < 16 || byte == kEightNan ? 0 : static_cast<int>(byte));
+                float down = 1.0f, own = eight_unit(byte);
+                if (most > top_byte) {
+                    down = power(top_byte - most);
+                    top_byte = most;
+                }
+                if (lane >= 16 && byte != kEightNan) own = power(static_cast<int>(byte) - top_byte + 9);
+                bool ahead = false;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float kf = __shfl_sync(0xffffffffu, own, k * 8 + g);
+                    const bool there = mask >> (k * 8 + g) & 1u;
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float& x = sc[b][2 * k + e];
+                            x = there ? (x + sc2[b][2 * k + e]) * unit[b][e] * kf : -INFINITY;
+                            ahead |= x - m[b][e] > kLag;
+                        }
+                }
+                if (__any_sync(0xffffffffu, ahead || down != 1.0f)) {      // new references
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float mx = fmaxf(fmaxf(sc[b][e], sc[b][2 + e]), m[b][e]);
+#pragma unroll
+                            for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+                            const float f = mx == -INFINITY ? 1.0f : pow2(m[b][e] - mx);
+                            m[b][e] = mx;
+                            l[b][e] *= f;
+#pragma unroll
+                            for (int n = 0; n < NC; ++n) {
+                                o[n][b][e] *= f * down;
+                                o[n][b][2 + e] *= f * down;
+                            }
+                        }
+                }
+                const float v0 = __shfl_sync(0xffffffffu, own, 16 + g), v1 = __shfl_sync(0xffffffffu, own, 24 + g);
+                uint32_t pt[NB][2];      // weights, turned: head g, keys 2 t4 and 2 t4 + 1 (and 8 more)
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    float w[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = pow2(sc[b][j] - (m[b][j & 1] == -INFINITY ? 0.0f : m[b][j & 1]));
+                    l[b][0] += w[0] + w[2];
+                    l[b][1] += w[1] + w[3];
+                    pt[b][0] = turn8(pack_f16(w[0] * v0, w[1] * v0));
+                    pt[b][1] = turn8(pack_f16(w[2] * v1, w[3] * v1));
+                }
+#pragma unroll
+                for (int n = 0; n < NC; n += 2) {      // rows g of a product: columns 2 g of 16; rows g + 8: the odd ones
+                    uint32_t c[4];
+                    ldsm4t(c, st + C_::kHalf + key * C_::kRowBytes + eight_chunk<DP>(key, n + second));
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        // a word has two columns of two keys
+                        const uint32_t k0 = low_codes(c[2 * e]), k1 = high_codes(c[2 * e]), k8 = low_codes(c[2 * e + 1]), k9 = high_codes(c[2 * e + 1]);
+                        const uint32_t x[4] = {__byte_perm(k0, k1, 0x5410), __byte_perm(k0, k1, 0x7632), __byte_perm(k8, k9, 0x5410), __byte_perm(k8, k9, 0x7632)};
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) mma_f16(o[n + e][b], x, pt[b][0], pt[b][1]);
+                    }
+                }
+                __syncwarp();   // the stage is free for the copies that the next round starts
+            }
+            // the values' own size; then the warps meet, as above
+            const float size = 0x1p-9f * eight_unit(static_cast<uint32_t>(top_byte));
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) l[b][e] += __shfl_xor_sync(0xffffffffu, l[b][e], d);
+                    const int r = b * 8 + t4 * 2 + e;
+                    if (g == 0) { wm[warp][r] = m[b][e]; wl[warp][r] = l[b][e]; }
+                }
+            __syncthreads();
+            float M[NB][2], L[NB][2];
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int r = b * 8 + t4 * 2 + e;
+                    M[b][e] = wm[0][r];
+#pragma unroll
+                    for (int w = 1; w < C_::kWarps; ++w) M[b][e] = fmaxf(M[b][e], wm[w][r]);
+                    const float base = M[b][e] == -INFINITY ? 0.0f : M[b][e];
+                    L[b][e] = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < C_::kWarps; ++w) L[b][e] = fmaf(wl[w][r], pow2(wm[w][r] - base), L[b][e]);
+                    const float f = pow2(m[b][e] - base);
+#pragma unroll
+                    for (int n = 0; n < NC; ++n) {
+                        o[n][b][e] = o[n][b][e] * size * f;
+                        o[n][b][2 + e] = o[n][b][2 + e] * size * f;
+                    }
+                }
+            const auto each = [&](auto use) {      // of this lane's heads and pairs of columns
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int r = b * 8 + t4 * 2 + e;
+                        if (r < rows) {
+#pragma unroll
+                            for (int n = 0; n < NC; ++n) use(r, n * 16 + g * 2, o[n][b][e], o[n][b][2 + e]);
+                        }
+                    }
+            };
+            const auto put = [&](int at) {
+                each([&](int r, int c, float x, float y) { *reinterpret_cast<float2*>(mg + (at * rows + r) * C_::kMergeRow + c) = make_float2(x, y); });
+            };
+            const auto add = [&](int at) {
+                each([&](int r, int c, float& x, float& y) {
+                    const float2 v = *reinterpret_cast<const float2*>(mg + (at * rows + r) * C_::kMergeRow + c);
+                    x += v.x;
+                    y += v.y;
+                });
+            };
+            if (warp >= 2) put(warp - 2);
+            __syncthreads();
+            if (warp < 2) add(warp);
+            if (warp == 1) put(1);
+            __syncthreads();
+            if (warp == 0) {
+                add(1);
+                if (a.split > 1) put(0);
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int r = b * 8 + t4 * 2 + e;
+                        if (a.split > 1) {
+                            if (g == 0) { wm[0][r] = M[b][e]; wl[0][r] = L[b][e]; }
+                            continue;
+                        }
+                        if (r >= rows) continue;
+                        if (complete) {
+                            const bool some = L[b][e] != 0.0f && head_kept(a, h0 + r);
+                            const long long row = static_cast<long long>(con.s) * a.H + h0 + r;
+                            const float f = some ? 1.0f / L[b][e] : 0.0f;
+                            uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<Io*>(a.out) + row * a.dh);
+#pragma unroll
+                            for (int n = 0; n < NC; ++n)
+                                if (n * 16 < a.dh) out[n * 8 + g] = some ? pack_bf16(o[n][b][e] * f, o[n][b][2 + e] * f) : 0u;
+                            if (g == 0 && a.lse) a.lse[row] = some ? (M[b][e] + log2f(L[b][e])) * kLn2 : -INFINITY;
+                        } else {
+                            if (g == 0) { slot[r] = M[b][e]; slot[16 + r] = L[b][e]; }
+#pragma unroll
+                            for (int n = 0; n < NC; ++n)
+                                *reinterpret_cast<float2*>(slot + kSlotHead + r * DP + n * 16 + g * 2) = make_float2(o[n][b][e], o[n][b][2 + e]);
+                        }
+                    }
             }
         } else {
             float* q = reinterpret_cast<float*>(ring + C_::kRing);

@@ -7,7 +7,9 @@ length.  d = (dh 2^-24 + 2^-20) (|a| + |b|) turn_scale for the pair (a, b), norm
 8-bit rows: the nearest code is off by 2^-4 of the value, or by half the smallest step, 2^-10 of the row's power of two; that power is
 the double where d carries the largest element past 448.
 
-Attention: as test_gpu_paged_attention, a weight rounded to fp16: 2^-11 of itself, or 2^-40 of the largest, for each of n positions.
+Attention: as test_gpu_paged_attention, a weight rounded to fp16 after it was multiplied with 2^9 and its position's power of two
+relative to the largest: off by 2^-11 of itself or, below fp16's normal numbers, by half its smallest step, 2^-25 / 2^9 = 2^-34 relative
+to a weight of 1 at the largest power, for each of n positions.
 """
 import numpy as np
 import pytest
@@ -226,7 +228,7 @@ def check_tokens(c):
     ref, ref_lse, size, reach, _, ref_bad = c.expected()
     e = (2.0 ** -21 + c.q.shape[2] * 2.0 ** -24 + 2.0 ** -20) * reach
     top = 448 * torch.exp2(c.Vs[c.Vs != 255].double().max() - 127)
-    rough = (2 * e + 1e-5 + 2.0 ** -11)[..., None] * size + (c.lens.clamp(min=0).double() * 2.0 ** -40 * top)[:, None, None]
+    rough = (2 * e + 1e-5 + 2.0 ** -11)[..., None] * size + (c.lens.clamp(min=0).double() * 2.0 ** -34 * top)[:, None, None]
     assert ((out.double() - ref).abs() <= rough + 2.0 ** -8 * ref.abs()).all()
     fine = torch.isfinite(ref_lse)
     assert torch.equal(lse[~fine].double(), ref_lse[~fine])
