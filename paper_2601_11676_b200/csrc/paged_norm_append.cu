@@ -7,10 +7,12 @@
 //   fp64, cosine and sine in fp32, once per token, through shared memory.  Everything between the load and the one rounding
 //   of the store is fp32.
 //
-// A lane keeps eight elements of the head (16 bytes of bf16) and walks over the heads of q, k and v alike, so gains, cosines and
-// sines stay in registers; LANES lanes hold a head, a power of two, and sum its squares and find its largest element by
-// shuffles.  The other half of a pair (i, i + rotary / 2) is in another lane: normed elements pass through a row of shared memory
-// that only the warp's own lanes touch.
+// A lane has two 16-byte words' worth of elements (eight of each) of a head: those of its pairs (i, i + rotary / 2), or two
+// neighbours; it walks over the heads of q, k and v alike, so cosines and sines stay in registers, and no element of a pair has to
+// be fetched from another lane.  LANES lanes hold a head, a power of two, and sum its squares and find its largest element by
+// shuffles.  An element costs about ten instructions; with one word to a lane (and its partners' from another) it was twice that,
+// and the instructions were what bounded it.  Pairs whose distance is no whole number of eight elements go by that form
+// (paged_norm_append_any_kernel): through a row of shared memory that only the warp's own lanes touch.
 #include <math.h>
 
 #include "eight.cuh"
@@ -86,7 +88,7 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
 // Thread block (token, part): heads part * groups + group, ... in steps of groups * parts.
 template <typename T, int LANES, bool EIGHT>
 __global__ void __launch_bounds__(kThreads)
-paged_norm_append_kernel(const __grid_constant__ NormAppendArgs a, int parts, int interleaved) {
+paged_norm_append_any_kernel(const __grid_constant__ NormAppendArgs a, int parts) {
     constexpr int kGroups = kThreads / LANES;
     constexpr int kRow = LANES * kOwn + 4;     // floats; rows of neighbouring groups start in other banks
     __shared__ float2 turn[128];               // [rotary / 2] cosine, sine
@@ -148,14 +150,13 @@ paged_norm_append_kernel(const __grid_constant__ NormAppendArgs a, int parts, in
         co[e] = 1.0f;
         si[e] = 0.0f;
         if (at < a.rotary) {
-            const bool second = interleaved ? at & 1 : at >= half;
-            const float2 t = turn[interleaved ? at >> 1 : second ? at - half : at];
+            const bool second = at >= half;
+            const float2 t = turn[second ? at - half : at];
             co[e] = t.x;
             si[e] = second ? t.y : -t.y;
         }
     }
     const bool turned = el < a.rotary;                 // elements behind the last pair are left as they are (infinity * 0 would not be)
-    const bool whole = half % kOwn == 0;               // the other halves of a lane's pairs are eight neighbours
     const long long row = static_cast<long long>(page) * a.Hk * a.page_size + pos % a.page_size;   // of the scales
     const long long base = static_cast<long long>(page) * a.page_stride + static_cast<long long>(pos % a.page_size) * a.dh + el;
     const long long plane = static_cast<long long>(a.page_size) * a.dh;
@@ -181,38 +182,22 @@ paged_norm_append_kernel(const __grid_constant__ NormAppendArgs a, int parts, in
                 for (int e = 0; e < kOwn; ++e) sum = fmaf(f[e], f[e], sum);
                 sum = lanes_sum<LANES>(sum);
                 if (there && normed) {
-                    const float n = 1.0f / sqrtf(sum / static_cast<float>(a.dh) + a.eps);
+                    const float n = rsqrtf(sum / static_cast<float>(a.dh) + a.eps);
 #pragma unroll
                     for (int e = 0; e < kOwn; ++e) f[e] = f[e] * n * (is_q ? wq[e] : wk[e]);
                 }
             }
-            if (interleaved) {
-                if (turned && !is_v) {
-#pragma unroll
-                    for (int e = 0; e < kOwn; e += 2) {
-                        if (el + e >= a.rotary) continue;
-                        const float p = f[e], o = f[e + 1];
-                        f[e] = p * co[e] + o * si[e];
-                        f[e + 1] = o * co[e + 1] + p * si[e + 1];
-                    }
-                }
-            } else if (a.rotary > 0) {
+            {
                 __syncwarp();
                 *reinterpret_cast<float4*>(mine + el) = make_float4(f[0], f[1], f[2], f[3]);
                 *reinterpret_cast<float4*>(mine + el + 4) = make_float4(f[4], f[5], f[6], f[7]);
                 __syncwarp();
                 if (turned && !is_v) {
                     float o[kOwn];
-                    if (whole) {
-                        const float* from = mine + (el < half ? el + half : el - half);
-                        *reinterpret_cast<float4*>(o) = *reinterpret_cast<const float4*>(from);
-                        *reinterpret_cast<float4*>(o + 4) = *reinterpret_cast<const float4*>(from + 4);
-                    } else {
 #pragma unroll
-                        for (int e = 0; e < kOwn; ++e) {
-                            const int at = el + e;
-                            o[e] = at < a.rotary ? mine[at < half ? at + half : at - half] : 0.0f;
-                        }
+                    for (int e = 0; e < kOwn; ++e) {
+                        const int at = el + e;
+                        o[e] = at < a.rotary ? mine[at < half ? at + half : at - half] : 0.0f;
                     }
 #pragma unroll
                     for (int e = 0; e < kOwn; ++e)
@@ -249,20 +234,193 @@ paged_norm_append_kernel(const __grid_constant__ NormAppendArgs a, int parts, in
     }
 }
 
-template <typename T, int LANES, bool EIGHT>
-halo_status launch(const NormAppendArgs& a, int n_tok, int interleaved, cudaStream_t st) {
+// Thread block (token, part): heads part * groups + group, ... in steps of groups * parts.  Units of 16 elements, LANES a head.
+template <typename T, int LANES, bool EIGHT, bool INTERLEAVED>
+__global__ void __launch_bounds__(kThreads)
+paged_norm_append_kernel(const __grid_constant__ NormAppendArgs a, int parts) {
+    constexpr int kGroups = kThreads / LANES;
+    __shared__ float2 turn[128];                         // [rotary / 2] cosine, sine
+    __shared__ __align__(16) float gain[2][LANES * 16];  // of queries, of keys; 1 where there is no norm
+    const int tid = threadIdx.x, group = tid / LANES, u = tid % LANES;
+    const int tok = blockIdx.x / parts, part = blockIdx.x % parts;
+    chain_wait();
+    // everything that depends on the token alone is requested at once
+    const int pos = ldg_waited(a.pos + tok);
+    const int s = a.seq ? ldg_waited(a.seq + tok) : tok;
+    const int half = a.rotary / 2, heads = a.H + 2 * a.Hk, step = kGroups * parts;
+    const bool in = u * 16 < a.dh;                       // lanes behind the head's end hold zeros
+    // the unit's two words: eight pairs' first and second elements, or sixteen neighbours
+    const int hu = half / 8;
+    const bool across = !INTERLEAVED && u < hu;
+    const int el0 = across || INTERLEAVED ? u * (INTERLEAVED ? 16 : 8) : a.rotary + (u - hu) * 16, el1 = across ? el0 + half : el0 + 8;
+    const T* q = static_cast<const T*>(a.q) + static_cast<long long>(tok) * a.q_stride;
+    const T* k = static_cast<const T*>(a.k) + static_cast<long long>(tok) * a.k_stride - a.H * a.dh;
+    const T* v = static_cast<const T*>(a.v) + static_cast<long long>(tok) * a.v_stride - (a.H + a.Hk) * a.dh;
+    Own<T> x[kHeads][2];
+    const auto fetch = [&](int h0) {
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) {
+            const int h = h0 + i * step;
+            if (in && h < heads) {
+                const T* src = (h < a.H ? q : h < a.H + a.Hk ? k : v) + h * a.dh;
+                x[i][0].load(src + el0);
+                x[i][1].load(src + el1);
+            }
+        }
+    };
+    const int first = part * kGroups + group;
+    const double freq = tid < half ? ldg_waited(a.inv_freq + tid) : 0.0;   // half <= 128 threads
+    fetch(first);
+    for (int i = tid; i < 2 * a.dh; i += kThreads) {
+        const bool key = i >= a.dh;
+        const T* w = static_cast<const T*>(key ? a.w_k : a.w_q);
+        gain[key][key ? i - a.dh : i] = w ? to_float(w[key ? i - a.dh : i]) : 1.0f;
+    }
+
+    if (pos < 0) return;               // a padding row: nothing is written for it
+    const int pi = pos / a.page_size, in_page = pos - pi * a.page_size;
+    int page = -1;
+    if (s >= 0 && s < a.n_seq && pi < a.max_pages) page = ldg_waited(a.table + static_cast<long long>(s) * a.max_pages + pi);
+    if (tid < half) {
+        const double turns = static_cast<double>(pos) * freq * 0.15915494309189533577;
+        float co, si;
+        sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &si, &co);
+        turn[tid] = make_float2(co * a.turn_scale, si * a.turn_scale);
+    }
+    if (page < 0 || page >= a.n_pages) {   // the same in every thread
+        if (tid == 0 && part == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
+        return;
+    }
+    __syncthreads();
+    float co[kOwn], si[kOwn];          // of pairs 8 u to 8 u + 7; those that are not turned are left as they are (infinity * 0 would not be)
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) {
+        const float2 t = u * 8 + e < half ? turn[u * 8 + e] : make_float2(1.0f, 0.0f);
+        co[e] = t.x;
+        si[e] = t.y;
+    }
+    const long long row = static_cast<long long>(page) * a.Hk * a.page_size + in_page;   // of the scales
+    const long long base = static_cast<long long>(page) * a.page_stride + static_cast<long long>(in_page) * a.dh;
+    const long long plane = static_cast<long long>(a.page_size) * a.dh;
+    T* qo = static_cast<T*>(a.q_out) + static_cast<long long>(tok) * a.qo_stride;
+
+    // every lane of a warp takes every step: lanes meet in the shuffles
+    for (int h0 = first, b0 = part * kGroups; b0 < heads; h0 += step * kHeads, b0 += step * kHeads) {
+        if (h0 != first) fetch(h0);
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) {
+            if (b0 + i * step >= heads) break;         // the same in every lane of the block
+            const int h = h0 + i * step;
+            const bool there = in && h < heads, is_q = h < a.H, is_v = h >= a.H + a.Hk;
+            float f[2][kOwn];
+            if (there) {
+                x[i][0].widen(f[0]);
+                x[i][1].widen(f[1]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kOwn; ++e) f[0][e] = f[1][e] = 0.0f;
+            }
+            float n = 1.0f;
+            if (__any_sync(0xffffffffu, there && !is_v)) {       // queries or keys among the warp's heads
+                const bool normed = !is_v && (is_q ? a.w_q : a.w_k) != nullptr;
+                if (a.w_q || a.w_k) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < kOwn; ++e) sum = fmaf(f[0][e], f[0][e], fmaf(f[1][e], f[1][e], sum));
+                    sum = lanes_sum<LANES>(sum);
+                    if (normed) n = rsqrtf(sum / static_cast<float>(a.dh) + a.eps);
+                }
+                if (!is_v && there) {
+                    if (normed) {
+                        const float* g = gain[is_q ? 0 : 1];
+#pragma unroll
+                        for (int w = 0; w < 2; ++w)
+#pragma unroll
+                            for (int e = 0; e < kOwn; e += 4) {
+                                const float4 by = *reinterpret_cast<const float4*>(g + (w ? el1 : el0) + e);
+                                f[w][e] *= by.x;
+                                f[w][e + 1] *= by.y;
+                                f[w][e + 2] *= by.z;
+                                f[w][e + 3] *= by.w;
+                            }
+                    }
+#pragma unroll
+                    for (int e = 0; e < kOwn; ++e) {
+                        // pair e: its elements lie in the two words, or side by side
+                        float& one = INTERLEAVED ? f[e >> 2][(e & 3) * 2] : f[0][e];
+                        float& two = INTERLEAVED ? f[e >> 2][(e & 3) * 2 + 1] : f[1][e];
+                        if (INTERLEAVED ? u * 8 + e < half : across) {
+                            const float p = one, o = two;
+                            one = p * co[e] - o * si[e];
+                            two = p * si[e] + o * co[e];
+                        }
+                    }
+                }
+            }
+            if (EIGHT && __any_sync(0xffffffffu, there && !is_q)) {
+                uint32_t top = 0;                               // sizes of finite numbers, ordered as their bits are
+#pragma unroll
+                for (int e = 0; e < kOwn; ++e)
+                    top = max(top, max(__float_as_uint(f[0][e] * n) & 0x7fffffffu, __float_as_uint(f[1][e] * n) & 0x7fffffffu));
+                top = lanes_max<LANES>(top);
+                if (there && !is_q) {
+                    const bool sound = top < 0x7f800000u;
+                    const int ex = eight_exponent(__uint_as_float(top));
+                    const float by = eight_power(-ex);
+                    const int kv = is_v ? h - a.H - a.Hk : h - a.H;
+                    uint8_t* to = static_cast<uint8_t*>(is_v ? a.V : a.K) + base + kv * plane;
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        uint32_t c[2];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            c[j] = sound ? eight_pair(f[w][4 * j] * n * by, f[w][4 * j + 1] * n * by) |
+                                               eight_pair(f[w][4 * j + 2] * n * by, f[w][4 * j + 3] * n * by) << 16 : 0u;
+                        *reinterpret_cast<uint2*>(to + (w ? el1 : el0)) = make_uint2(c[0], c[1]);
+                    }
+                    if (u == 0)
+                        (is_v ? a.V_scale : a.K_scale)[row + static_cast<long long>(kv) * a.page_size] =
+                            static_cast<uint8_t>(sound ? ex + 127 : kEightNan);
+                }
+            }
+            if (there && (is_q || !EIGHT)) {
+                T* to = is_q ? qo + h * a.dh : is_v ? static_cast<T*>(a.V) + base + (h - a.H - a.Hk) * plane : static_cast<T*>(a.K) + base + (h - a.H) * plane;
+                if (!is_v) {
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+#pragma unroll
+                        for (int e = 0; e < kOwn; ++e) f[w][e] *= n;
+                        x[i][w].narrow(f[w]);
+                    }
+                }
+                x[i][0].store(to + el0);
+                x[i][1].store(to + el1);
+            }
+        }
+    }
+}
+
+template <int LANES, typename K>
+halo_status launch(K kernel, const NormAppendArgs& a, int n_tok, cudaStream_t st) {
     const int groups = kThreads / LANES, heads = a.H + 2 * a.Hk, most = (heads + groups - 1) / groups;
     // few tokens: their heads are spread over thread blocks until the GPU is covered four times
     int parts = (4 * kSmCount + n_tok - 1) / n_tok;
     parts = parts < 1 ? 1 : parts > most ? most : parts;
-    return launch_chained(paged_norm_append_kernel<T, LANES, EIGHT>, static_cast<unsigned>(n_tok) * parts, kThreads, 0, st, a, parts,
-                          interleaved);
+    return launch_chained(kernel, static_cast<unsigned>(n_tok) * parts, kThreads, 0, st, a, parts);
+}
+template <typename T, bool EIGHT, bool INTERLEAVED>
+halo_status by_width(const NormAppendArgs& a, int n_tok, cudaStream_t st) {
+    return a.dh <= 64    ? launch<4>(paged_norm_append_kernel<T, 4, EIGHT, INTERLEAVED>, a, n_tok, st)
+           : a.dh <= 128 ? launch<8>(paged_norm_append_kernel<T, 8, EIGHT, INTERLEAVED>, a, n_tok, st)
+                         : launch<16>(paged_norm_append_kernel<T, 16, EIGHT, INTERLEAVED>, a, n_tok, st);
 }
 template <typename T, bool EIGHT>
-halo_status by_width(const NormAppendArgs& a, int n_tok, int interleaved, cudaStream_t st) {
-    return a.dh <= 64    ? launch<T, 8, EIGHT>(a, n_tok, interleaved, st)
-           : a.dh <= 128 ? launch<T, 16, EIGHT>(a, n_tok, interleaved, st)
-                         : launch<T, 32, EIGHT>(a, n_tok, interleaved, st);
+halo_status by_pairs(const NormAppendArgs& a, int n_tok, int interleaved, cudaStream_t st) {
+    if (interleaved) return by_width<T, EIGHT, true>(a, n_tok, st);
+    if (a.rotary / 2 % kOwn == 0) return by_width<T, EIGHT, false>(a, n_tok, st);
+    return a.dh <= 64    ? launch<8>(paged_norm_append_any_kernel<T, 8, EIGHT>, a, n_tok, st)
+           : a.dh <= 128 ? launch<16>(paged_norm_append_any_kernel<T, 16, EIGHT>, a, n_tok, st)
+                         : launch<32>(paged_norm_append_any_kernel<T, 32, EIGHT>, a, n_tok, st);
 }
 
 struct ReadArgs {
@@ -280,47 +438,76 @@ struct ReadArgs {
     uint32_t* status;
 };
 
-// Thread block: a token.  A unit is 16 bytes of the cache: of 8-bit rows 16 codes, which leave as 32 bytes of bf16.
-template <typename T, bool EIGHT>
-__global__ void __launch_bounds__(kThreads) paged_kv_read_kernel(const __grid_constant__ ReadArgs a) {
+// Thread block: TOKENS tokens, whose chains of loads (position, page, rows) run side by side.  A unit is 16 bytes of the cache: of
+// 8-bit rows 16 codes, which leave as 32 bytes of bf16.
+template <typename T, bool EIGHT, int TOKENS>
+__global__ void __launch_bounds__(kThreads) paged_kv_read_kernel(const __grid_constant__ ReadArgs a, int n_tok) {
     constexpr int E = EIGHT ? 16 : Elem<T>::kPerChunk;
-    const int tok = blockIdx.x;
+    const int tok0 = blockIdx.x * TOKENS;
     chain_wait();
-    const int pos = ldg_waited(a.pos + tok), s = a.seq ? ldg_waited(a.seq + tok) : tok;
-    if (pos < 0) return;
-    const int pi = pos / a.page_size, at = pos % a.page_size;
-    int page = -1;
-    if (s >= 0 && s < a.n_seq && pi < a.max_pages) page = ldg_waited(a.table + static_cast<long long>(s) * a.max_pages + pi);
-    if (page < 0 || page >= a.n_pages) {
-        if (threadIdx.x == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
-        return;
+    int pos[TOKENS], page[TOKENS];
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t) pos[t] = tok0 + t < n_tok ? ldg_waited(a.pos + tok0 + t) : -1;
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t) {
+        page[t] = -1;
+        if (pos[t] < 0) continue;
+        const int s = a.seq ? ldg_waited(a.seq + tok0 + t) : tok0 + t, pi = pos[t] / a.page_size;
+        pos[t] -= pi * a.page_size;      // from here on the row in its page
+        if (s >= 0 && s < a.n_seq && pi < a.max_pages) page[t] = ldg_waited(a.table + static_cast<long long>(s) * a.max_pages + pi);
     }
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t)
+        if (pos[t] >= 0 && (page[t] < 0 || page[t] >= a.n_pages)) {
+            if (threadIdx.x == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
+            pos[t] = -1;
+        }
     const int per_head = a.dh / E, per_row = a.Hk * per_head;
-    const long long base = static_cast<long long>(page) * a.page_stride;
     for (int u = threadIdx.x; u < 2 * per_row; u += kThreads) {
         const bool is_v = u >= per_row;
         const int w = is_v ? u - per_row : u, h = w / per_head, el = (w - h * per_head) * E;
-        const long long from = base + (static_cast<long long>(h) * a.page_size + at) * a.dh + el;
-        T* to = (is_v ? static_cast<T*>(a.v_out) + static_cast<long long>(tok) * a.v_stride
-                      : static_cast<T*>(a.k_out) + static_cast<long long>(tok) * a.k_stride) + h * a.dh + el;
-        if constexpr (EIGHT) {
-            const uint4 codes = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(is_v ? a.V : a.K) + from);
-            const float unit = eight_unit((is_v ? a.V_scale : a.K_scale)[(static_cast<long long>(page) * a.Hk + h) * a.page_size + at]);
-            const uint32_t in[4] = {codes.x, codes.y, codes.z, codes.w};
-            __align__(16) T out[16];
+        uint4 x[TOKENS];
+        uint32_t byte[TOKENS];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float f[4];
-                eight_widen(in[j], f);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) out[4 * j + e] = from_float<T>(f[e] * unit);   // exact
+        for (int t = 0; t < TOKENS; ++t) {
+            if (pos[t] < 0) continue;
+            const long long row = static_cast<long long>(h) * a.page_size + pos[t], from = page[t] * a.page_stride + row * a.dh + el;
+            if constexpr (EIGHT) {
+                x[t] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(is_v ? a.V : a.K) + from);
+                byte[t] = (is_v ? a.V_scale : a.K_scale)[static_cast<long long>(page[t]) * a.Hk * a.page_size + row];
+            } else {
+                x[t] = *reinterpret_cast<const uint4*>(static_cast<const T*>(is_v ? a.V : a.K) + from);
             }
-            reinterpret_cast<uint4*>(to)[0] = reinterpret_cast<const uint4*>(out)[0];
-            reinterpret_cast<uint4*>(to)[1] = reinterpret_cast<const uint4*>(out)[1];
-        } else {
-            *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(static_cast<const T*>(is_v ? a.V : a.K) + from);
+        }
+#pragma unroll
+        for (int t = 0; t < TOKENS; ++t) {
+            if (pos[t] < 0) continue;
+            T* to = (is_v ? static_cast<T*>(a.v_out) + static_cast<long long>(tok0 + t) * a.v_stride
+                          : static_cast<T*>(a.k_out) + static_cast<long long>(tok0 + t) * a.k_stride) + h * a.dh + el;
+            if constexpr (EIGHT) {
+                const float unit = eight_unit(byte[t]);
+                const uint32_t in[4] = {x[t].x, x[t].y, x[t].z, x[t].w};
+                __align__(16) T out[16];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float f[4];
+                    eight_widen(in[j], f);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) out[4 * j + e] = from_float<T>(f[e] * unit);   // exact
+                }
+                reinterpret_cast<uint4*>(to)[0] = reinterpret_cast<const uint4*>(out)[0];
+                reinterpret_cast<uint4*>(to)[1] = reinterpret_cast<const uint4*>(out)[1];
+            } else {
+                *reinterpret_cast<uint4*>(to) = x[t];
+            }
         }
     }
+}
+template <typename T, bool EIGHT>
+halo_status launch_read(const ReadArgs& a, int n_tok, cudaStream_t st) {
+    // four tokens to a thread block where that still fills the GPU (8297 tokens, 8 heads of 128 in 8 bits: 15 us with one)
+    if (n_tok >= 4 * 8 * kSmCount) return launch_chained(paged_kv_read_kernel<T, EIGHT, 4>, static_cast<unsigned>((n_tok + 3) / 4), kThreads, 0, st, a, n_tok);
+    return launch_chained(paged_kv_read_kernel<T, EIGHT, 1>, static_cast<unsigned>(n_tok), kThreads, 0, st, a, n_tok);
 }
 
 }  // namespace
@@ -395,9 +582,9 @@ extern "C" halo_status halo_paged_norm_append(const halo_paged_shape* shape, int
     a.V_scale = V_scale;
     a.status = dev_status;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (shape->dtype == HALO_F32) return by_width<float, false>(a, n_tok, interleaved != 0, st);
-    return K_scale ? by_width<__nv_bfloat16, true>(a, n_tok, interleaved != 0, st)
-                   : by_width<__nv_bfloat16, false>(a, n_tok, interleaved != 0, st);
+    if (shape->dtype == HALO_F32) return by_pairs<float, false>(a, n_tok, interleaved != 0, st);
+    return K_scale ? by_pairs<__nv_bfloat16, true>(a, n_tok, interleaved != 0, st)
+                   : by_pairs<__nv_bfloat16, false>(a, n_tok, interleaved != 0, st);
 }
 
 extern "C" halo_status halo_paged_kv_read(const halo_paged_shape* shape, int n_tok, int n_seq, const int32_t* pos,
@@ -437,8 +624,6 @@ extern "C" halo_status halo_paged_kv_read(const halo_paged_shape* shape, int n_t
     a.v_out = v_out;
     a.status = dev_status;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const auto kernel = shape->dtype == HALO_F32 ? paged_kv_read_kernel<float, false>
-                        : K_scale                ? paged_kv_read_kernel<__nv_bfloat16, true>
-                                                 : paged_kv_read_kernel<__nv_bfloat16, false>;
-    return launch_chained(kernel, static_cast<unsigned>(n_tok), kThreads, 0, st, a);
+    if (shape->dtype == HALO_F32) return launch_read<float, false>(a, n_tok, st);
+    return K_scale ? launch_read<__nv_bfloat16, true>(a, n_tok, st) : launch_read<__nv_bfloat16, false>(a, n_tok, st);
 }
