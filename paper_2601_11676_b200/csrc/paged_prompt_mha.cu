@@ -485,7 +485,7 @@ using Const = std::integral_constant<int, N>;
 
 // One warp, one lane of which issues.  Lanes (of barriers) are constants, so that counters and addresses stay in registers: the
 // tensor cores take a product of 16 columns in 64 clocks, and one must not take longer to issue.  What is issued next goes by what is
-// ready: a stream's weights (P V), else its next scores, so that a stream never waits behind the other's softmax.
+// ready, so that a stream never waits behind the other's softmax.
 template <int DP, bool EIGHT>
 struct Issue {
     using C = Cfg<DP, EIGHT>;
@@ -564,32 +564,46 @@ struct Issue {
         }
         commit(lead, &bars.pv_done[b]);
     }
-    // One step of a stream that has had q scores and s sums of its n tiles: true if something was issued.  o: the other stream's.
-    template <int t, int b, int b2>
+    // One step of one of two streams (lane b is its own) that has had q scores and s sums of its n tiles: true if something was issued.
+    // oq, os, on: the other stream's.  A tile's sums and the next tile's scores go together: were the other stream's sums put in
+    // between, both streams' scores would come one after the other and both be in the softmax at the same time, in each other's
+    // way, while the tensor cores wait.
+    template <int t, int b>
     __device__ __forceinline__ bool step(int& q, int& s, int n, int oq, int os, int on) {
-        // lane of tile j: b, or b and b2 in turn
-        const bool odd = b != b2;
-        if (s < q) {
-            const bool second = odd && (s & 1);
-            const uint32_t phase = second ? use<b2>() - 1 : use<b>() - (odd ? 1 : q - s);
-            if (done(second ? &bars.p_full[b2] : &bars.p_full[b], phase) && there(s, 1)) {
-                const bool end = os > s || s >= on;
-                if (second) sums<t, b2>(s, end);
-                else sums<t, b>(s, end);
-                ++s;
-                return true;
-            }
-        }
-        // scores in every buffer of S that the stream has; two ahead of the sums where P lies apart
-        if (q < n && q - s < (odd || C::kApart ? 2 : 1)) {
-            const bool second = odd && (q & 1);
-            if ((second ? free_scores<b2>() : free_scores<b>()) && there(q, 0)) {
-                const bool end = oq > q || q >= on;
-                if (second) scores<t, b2>(q, end);
-                else scores<t, b>(q, end);
+        if (s < q && done(&bars.p_full[b], use<b>() - 1) && there(s, 1)) {
+            if (C::kApart && q < n && there(q, 0)) {      // S has been read: its place is free
+                scores<t, b>(q, oq > q || q >= on);
                 ++q;
-                return true;
             }
+            sums<t, b>(s, os > s || s >= on);
+            ++s;
+            // keys that are not there yet are not waited for: their stage may be one that the other stream has to free
+            if (!C::kApart && q < n && there(q, 0) && warp_wait(&bars.pv_done[b], use<b>() - 1, abort)) {
+                scores<t, b>(q, oq > q || q >= on);
+                ++q;
+            }
+            return true;
+        }
+        if (q == s && q < n && free_scores<b>() && there(q, 0)) {
+            scores<t, b>(q, oq > q || q >= on);
+            ++q;
+            return true;
+        }
+        return false;
+    }
+    // One step of a stream on its own, lanes 0 and 2 in turn
+    __device__ __forceinline__ bool step_alone(int& q, int& s, int n) {
+        if (s < q && done(s & 1 ? &bars.p_full[2] : &bars.p_full[0], (s & 1 ? use2 : use0) - 1) && there(s, 1)) {
+            if (s & 1) sums<0, 2>(s, true);
+            else sums<0, 0>(s, true);
+            ++s;
+            return true;
+        }
+        if (q < n && q - s < 2 && (q & 1 ? free_scores<2>() : free_scores<0>()) && there(q, 0)) {
+            if (q & 1) scores<0, 2>(q, true);
+            else scores<0, 0>(q, true);
+            ++q;
+            return true;
         }
         return false;
     }
@@ -606,10 +620,10 @@ struct Issue {
                 while (s0_ < p.tiles[0] || s1_ < p.tiles[1]) {
                     bool any;
                     if (C::kStreams == 2 && p.streams == 2) {
-                        any = step<0, 0, 0>(q0_, s0_, p.tiles[0], q1_, s1_, p.tiles[1]);
-                        any |= step<C::kStreams - 1, 1, 1>(q1_, s1_, p.tiles[1], q0_, s0_, p.tiles[0]);
+                        any = step<0, 0>(q0_, s0_, p.tiles[0], q1_, s1_, p.tiles[1]);
+                        any |= step<C::kStreams - 1, 1>(q1_, s1_, p.tiles[1], q0_, s0_, p.tiles[0]);
                     } else {
-                        any = step<0, 0, 2>(q0_, s0_, p.tiles[0], 0, 0, 0);
+                        any = step_alone(q0_, s0_, p.tiles[0]);
                     }
                     if (!asked && q0_ == p.tiles[0] && q1_ == p.tiles[1]) {
                         commit(lead, &bars.q_empty);
