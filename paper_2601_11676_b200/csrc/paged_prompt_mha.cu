@@ -10,9 +10,9 @@
 // An item has 256 rows in two streams of 128: while one stream's rows are in the softmax, the other's products run.  Head sizes
 // above 128 (whose O fills half of tensor memory) and items of up to 128 rows have one stream with two S buffers instead.
 //
-// Weights are powers of two relative to a reference that is a row's maximum when it is set, and set again only when a tile's
-// weights sum to more than 2^20: O and the sum are in fp32, so weights above 1 lose nothing, O, which would have to be read,
-// multiplied and written back for every new reference, is left alone after the first tiles, and a tile needs no maximum.
+// Weights are powers of two relative to a reference: the row's score of the first key, until a tile's weights sum to more than
+// 2^20, then its maximum so far.  O and the sum are in fp32, so weights above 1 lose nothing, O, which would have to be read,
+// multiplied and written back for every new reference, is hardly ever touched, and a tile needs no maximum.
 //
 // What a row does not see must not reach it.  Weights of 0 see to that but for values that are infinite or NaN; a row whose
 // sums come out as neither although its weights are finite is summed again, key by key (resum).
@@ -145,6 +145,12 @@ __device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&v)[16]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
                  : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
                    "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
+}
+__device__ __forceinline__ uint32_t tmem_ld_word(uint32_t taddr) {
+    uint32_t v;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(v) : "r"(taddr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(v)::"memory");
+    return v;
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 template <int N>
@@ -781,7 +787,8 @@ __device__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm, Walk<Cfg<DP>::k
                 for (int c = 0; c < 4; ++c) there[c] = *const_cast<volatile const uint32_t*>(&sm.flags.there[(tile + j) % kFlags][c]);
                 const bool masked = p0 + kTile > all_see || (there[0] & there[1] & there[2] & there[3]) != 0xffffffffu;
                 uint32_t pk[4][16];
-                // 32 scores at a time, the next on their way; mask: what the row does not see as -infinity
+                // 32 scores at a time, the next on their way; mask: what the row does not see as -infinity (none: no row of the warp sees
+                // any of them)
                 const auto each = [&](auto mask, auto use) {
                     uint32_t sc[2][32];
                     tmem_ld_32x32(s_addr, sc[0]);
@@ -789,21 +796,30 @@ __device__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm, Walk<Cfg<DP>::k
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         if (c < 3) tmem_ld_32x32(s_addr + (c + 1) * 32, sc[(c + 1) & 1]);
+                        bool none = false;
                         if (decltype(mask)::value) {
                             const int left = row.sees - p0 - c * 32;
                             const uint32_t in = left >= 32 ? there[c] : left <= 0 ? 0u : there[c] & ((1u << left) - 1u);
+                            none = __all_sync(0xffffffffu, in == 0u);
+                            if (!none && !__all_sync(0xffffffffu, in == 0xffffffffu)) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                if (!(in >> e & 1u)) sc[c & 1][e] = 0xff800000u;
+                                for (int e = 0; e < 32; ++e)
+                                    if (!(in >> e & 1u)) sc[c & 1][e] = 0xff800000u;
+                            }
                         }
-                        use(c, sc[c & 1]);
+                        use(c, sc[c & 1], none);
                         if (c < 3) tmem_ld_wait_for(sc[(c + 1) & 1]);
                     }
                 };
                 const auto weights = [&](auto mask) {
                     const Pair times = twice(scale), minus = twice(m == -INFINITY ? 0.0f : -m * scale);
                     Pair sum[2] = {0, 0};
-                    each(mask, [&](int c, const uint32_t (&sc)[32]) {
+                    each(mask, [&](int c, const uint32_t (&sc)[32], bool none) {
+                        if (decltype(mask)::value && none) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) pk[c][e] = 0u;
+                            return;
+                        }
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             const Pair x = fma2(pair_of(__uint_as_float(sc[2 * e]), __uint_as_float(sc[2 * e + 1])), times, minus);
@@ -816,12 +832,18 @@ __device__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm, Walk<Cfg<DP>::k
                     const float2 s0 = both(sum[0]), s1 = both(sum[1]);
                     return (s0.x + s0.y) + (s1.x + s1.y);
                 };
+                // the first tile: relative to the score of its first key, which every row of it sees that sees anything
+                if (j == 0) {
+                    const float first_score = __uint_as_float(tmem_ld_word(s_addr));
+                    if (row.sees > p0 && (there[0] & 1u) && fabsf(first_score) < INFINITY) m = first_score;
+                }
                 float more = INFINITY;
-                if (!masked && __all_sync(0xffffffffu, m > -INFINITY)) more = weights(Const<0>());
+                if (__all_sync(0xffffffffu, m > -INFINITY || row.sees <= p0)) more = masked ? weights(Const<1>()) : weights(Const<0>());
                 if (__any_sync(0xffffffffu, !(more < kSum))) {
-                    // masks, the first tile, a new reference, or something infinite or NaN: from the scores again
+                    // a new reference, or something infinite or NaN: from the scores again
                     float mx = -INFINITY;
-                    each(Const<1>(), [&](int, const uint32_t (&sc)[32]) {
+                    each(Const<1>(), [&](int, const uint32_t (&sc)[32], bool none) {
+                        if (none) return;
                         float most[4];
 #pragma unroll
                         for (int q = 0; q < 4; ++q) most[q] = max3(__uint_as_float(sc[q]), __uint_as_float(sc[q + 4]), __uint_as_float(sc[q + 8]));
