@@ -361,6 +361,39 @@ struct Gather {
         }
         cp_commit();
     }
+    // Words of a stage to bf16, four loads ahead of their conversions: one behind the other, a load's and its conversion's latencies
+    // add up.
+    template <bool FAR>
+    __device__ __forceinline__ void spread(uint32_t dst, uint32_t steps, int slot) {
+        constexpr int kAhead = 4;
+        const int c = lane % kCodes;
+#pragma unroll
+        for (int i0 = 0; i0 < 32 / kCodeRows; i0 += kAhead) {
+            uint32_t w[kAhead][4], by[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int r = (i0 + i) * kCodeRows + lane / kCodes;
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3]) : "r"(code_place(slot, r)));
+                by[i] = __shfl_sync(0xffffffffu, steps, r);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int r = (i0 + i) * kCodeRows + lane / kCodes;
+                const uint32_t by_one = __byte_perm(by[i], by[i], 0x1010), by_two = __byte_perm(by[i], by[i], 0x3232);
+                uint32_t o[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint32_t t = __byte_perm(w[i][k >> 1], 0, k & 1 ? 0x3424 : 0x1404);      // a code in the upper byte of each half
+                    o[k] = times_bf16(((t >> 4) & 0x07f007f0u) | (t & 0x80008000u), by_one);
+                    if (FAR) o[k] = times_bf16(o[k], by_two);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(place(dst, r, 2 * c + h)), "r"(o[4 * h]), "r"(o[4 * h + 1]),
+                                 "r"(o[4 * h + 2]), "r"(o[4 * h + 3]) : "memory");
+            }
+        }
+    }
     // ... and on to a stage as bf16.  A code's bits are a bf16 number's exponent and significand, of 2^-120 of its value; the row's power
     // of two puts that right: without rounding, as every value of a row is a bf16 number.  byte: of this lane's key's row.
     __device__ __forceinline__ void widen(uint32_t byte, int slot) {
@@ -374,27 +407,8 @@ struct Gather {
         const float one = byte == 0 ? 0.0f : byte == kEightNan ? __uint_as_float(0x7fc00000u) : eight_power(120 + min(e, 7));
         const float two = byte == kEightNan ? 1.0f : eight_power(max(e, 7) - 7);
         const uint32_t steps = pack_bf16(one, two);
-        const bool far = __any_sync(0xffffffffu, two != 1.0f);
-#pragma unroll
-        for (int i = 0; i < 32 / kCodeRows; ++i) {
-            const int r = i * kCodeRows + lane / kCodes, c = lane % kCodes;
-            const uint32_t by = __shfl_sync(0xffffffffu, steps, r);
-            const uint32_t by_one = __byte_perm(by, by, 0x1010), by_two = __byte_perm(by, by, 0x3232);
-            uint4 v;
-            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(code_place(slot, r)));
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-            uint32_t o[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const uint32_t t = __byte_perm(w[k >> 1], 0, k & 1 ? 0x3424 : 0x1404);      // a code in the upper byte of each half
-                o[k] = times_bf16(((t >> 4) & 0x07f007f0u) | (t & 0x80008000u), by_one);
-                if (far) o[k] = times_bf16(o[k], by_two);
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(place(dst, r, 2 * c + h)), "r"(o[4 * h]), "r"(o[4 * h + 1]), "r"(o[4 * h + 2]),
-                             "r"(o[4 * h + 3]) : "memory");
-        }
+        if (__any_sync(0xffffffffu, two != 1.0f)) spread<true>(dst, steps, slot);
+        else spread<false>(dst, steps, slot);
         signal(smem_u32(&sm.bars.full[s]));
     }
     __device__ void run(Walk<C::kRows, kTile, kOver> w) {
