@@ -504,8 +504,9 @@ template <int N>
 using Const = std::integral_constant<int, N>;
 
 // One warp, one lane of which issues.  Lanes (of barriers) are constants, so that counters and addresses stay in registers: the
-// tensor cores take a product of 16 columns in 64 clocks, and one must not take longer to issue.  What is issued next goes by what is
-// ready, so that a stream never waits behind the other's softmax.
+// tensor cores take a product of 16 columns in 64 clocks, and one must not take longer to issue.  Two streams take fixed turns:
+// with tests of what is ready instead, 8192 tokens of 16 heads of 128 took 330 us and not 325, 4096 of 32 heads of 64 took 187 and
+// not 173; with a warp for each stream, whose products then share the tensor cores, 393 and 198.
 template <int DP, bool EIGHT>
 struct Issue {
     using C = Cfg<DP, EIGHT>;
@@ -584,32 +585,43 @@ struct Issue {
         }
         commit(lead, &bars.pv_done[b]);
     }
-    // One step of one of two streams (lane b is its own) that has had q scores and s sums of its n tiles: true if something was issued.
-    // oq, os, on: the other stream's.  A tile's sums and the next tile's scores go together: were the other stream's sums put in
-    // between, both streams' scores would come one after the other and both be in the softmax at the same time, in each other's
-    // way, while the tensor cores wait.
-    template <int t, int b>
-    __device__ __forceinline__ bool step(int& q, int& s, int n, int oq, int os, int on) {
-        if (s < q && done(&bars.p_full[b], use<b>() - 1) && there(s, 1)) {
-            if (C::kApart && q < n && there(q, 0)) {      // S has been read: its place is free
-                scores<t, b>(q, oq > q || q >= on);
-                ++q;
-            }
-            sums<t, b>(s, os > s || s >= on);
-            ++s;
-            // keys that are not there yet are not waited for: their stage may be one that the other stream has to free
-            if (!C::kApart && q < n && there(q, 0) && warp_wait(&bars.pv_done[b], use<b>() - 1, abort)) {
-                scores<t, b>(q, oq > q || q >= on);
-                ++q;
-            }
-            return true;
+    __device__ __forceinline__ bool await_stage(int j, int v) {      // items of two streams have a stage to a tile
+        const uint32_t f = first_fill + j * 2 + v;
+        return warp_wait(&bars.full[f % C::kStages], f / C::kStages, abort);
+    }
+    // The next turn of stream t of two, whose lane t is: sums of tile j and the scores of the one behind it.
+    template <int t>
+    __device__ __forceinline__ bool turn(int j, int n, int on) {
+        if (j >= n) return true;
+        if (!warp_wait(&bars.p_full[t], use<t>() - 1, abort)) return false;
+        const bool more = j + 1 < n;
+        if (C::kApart && more) {      // S has been read: its place is free
+            if (!await_stage(j + 1, 0)) return false;
+            scores<t, t>(j + 1, t == 1 || j + 1 >= on);
         }
-        if (q == s && q < n && free_scores<b>() && there(q, 0)) {
-            scores<t, b>(q, oq > q || q >= on);
-            ++q;
-            return true;
+        if (!await_stage(j, 1)) return false;
+        sums<t, t>(j, t == 1 || j >= on);
+        if (!C::kApart && more) {
+            if (!await_stage(j + 1, 0) || !warp_wait(&bars.pv_done[t], use<t>() - 1, abort)) return false;
+            scores<t, t>(j + 1, t == 1 || j + 1 >= on);
         }
-        return false;
+        return true;
+    }
+    // An item of two streams, which take turns: while the tensor cores have one's products, the other is in its softmax.
+    __device__ __forceinline__ bool turns(int n0, int n1) {
+        if (use0 > 0 && !warp_wait(&bars.pv_done[0], use0 - 1, abort)) return false;
+        const uint32_t used = last == 1 ? use1 : use2;
+        if (used > 0 && !warp_wait(last == 1 ? &bars.pv_done[1] : &bars.pv_done[2], used - 1, abort)) return false;
+        if (!await_stage(0, 0)) return false;
+        if (n0 > 0) scores<0, 0>(0, false);
+        scores<C::kStreams - 1, 1>(0, true);
+        if (n1 == 1) commit(lead, &bars.q_empty);
+        for (int j = 0; j < n1; ++j) {
+            if (!turn<0>(j, n0, n1)) return false;
+            if (!turn<C::kStreams - 1>(j, n1, n0)) return false;
+            if (j + 2 == n1) commit(lead, &bars.q_empty);      // the last scores: n0 <= n1
+        }
+        return true;
     }
     // One step of a stream on its own, lanes 0 and 2 in turn
     __device__ __forceinline__ bool step_alone(int& q, int& s, int n) {
@@ -627,39 +639,42 @@ struct Issue {
         }
         return false;
     }
+    // An item of one stream
+    __device__ __forceinline__ bool alone(int n) {
+        int q = 0, s = 0;      // scores and sums issued
+        bool asked = false;
+        long long since = 0;
+        uint32_t idle = 0;
+        while (s < n) {
+            const bool any = step_alone(q, s, n);
+            if (!asked && q == n) {
+                commit(lead, &bars.q_empty);
+                asked = true;
+            }
+            if (any) {
+                idle = 0;
+            } else if ((++idle & 255u) == 0u) {      // bounded, as every wait
+                const long long now = clock64();
+                if (idle == 256u) since = now;
+                const bool stop = *reinterpret_cast<volatile int*>(abort) || now - since > kWaitLimitCycles;
+                if (__any_sync(0xffffffffu, stop)) {
+                    *reinterpret_cast<volatile int*>(abort) = 1;
+                    return false;
+                }
+            }
+        }
+        return true;
+    }
     __device__ void run(Walk<C::kRows, kTile, kOver> w) {
         uint32_t piece = 0;
         while (w.left > 0) {
             const Piece<DP> p(a, w);
             if (p.n > 0) {
                 if (!warp_wait(&bars.q_full, piece++, abort)) return;
-                int q0_ = 0, s0_ = 0, q1_ = 0, s1_ = 0;      // scores and sums issued, per stream
-                bool asked = false;
-                long long since = clock64();
-                uint32_t idle = 0;
-                while (s0_ < p.tiles[0] || s1_ < p.tiles[1]) {
-                    bool any;
-                    if (C::kStreams == 2 && p.streams == 2) {
-                        any = step<0, 0>(q0_, s0_, p.tiles[0], q1_, s1_, p.tiles[1]);
-                        any |= step<C::kStreams - 1, 1>(q1_, s1_, p.tiles[1], q0_, s0_, p.tiles[0]);
-                    } else {
-                        any = step_alone(q0_, s0_, p.tiles[0]);
-                    }
-                    if (!asked && q0_ == p.tiles[0] && q1_ == p.tiles[1]) {
-                        commit(lead, &bars.q_empty);
-                        asked = true;
-                    }
-                    if (any) {
-                        idle = 0;
-                    } else if ((++idle & 255u) == 0u) {      // bounded, as every wait
-                        const long long now = clock64();
-                        if (idle == 256u) since = now;
-                        const bool stop = *reinterpret_cast<volatile int*>(abort) || now - since > kWaitLimitCycles;
-                        if (__any_sync(0xffffffffu, stop)) {
-                            *reinterpret_cast<volatile int*>(abort) = 1;
-                            return;
-                        }
-                    }
+                if (C::kStreams == 2 && p.streams == 2) {
+                    if (!turns(p.tiles[0], p.tiles[1])) return;
+                } else if (!alone(p.n)) {
+                    return;
                 }
                 first_fill += p.n * 2 * C::kParts;
             }
