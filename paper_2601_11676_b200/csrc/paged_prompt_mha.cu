@@ -64,21 +64,11 @@ struct Flags {
 constexpr int kLanes = 3;
 struct Bars {
     uint64_t full[8], empty[8], q_full, q_empty, s_full[kLanes], p_full[kLanes], pv_done[kLanes];
+    uint64_t piece_full[4], piece_empty[4];
     uint64_t raw[4];                 // a gathering warp's own: values of which it hands on a part
     uint32_t tmem;
     int abort;
 };
-template <int DP, bool EIGHT>
-struct Smem {
-    unsigned char q[Cfg<DP, EIGHT>::kQ];
-    unsigned char ring[Cfg<DP, EIGHT>::kStages * Cfg<DP>::kStage];
-    unsigned char raw[2 * Cfg<DP, EIGHT>::kRaw + 16];
-    long long q_row[Cfg<DP>::kRows];     // where the item's rows of q are, -1: none
-    Flags flags;
-    Bars bars;
-    long long sh[kThreads / 32 + 3];
-};
-
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t phase, int* abort) {
     if (mbar_wait_bounded(bar, phase & 1u, abort)) return true;
     *reinterpret_cast<volatile int*>(abort) = 1;
@@ -176,26 +166,83 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-// A piece as every role sees it: its tiles, its streams and how many of the tiles each of them takes part in.
-template <int DP>
-struct Piece {
-    using C = Cfg<DP>;
-    int n, streams, tiles[2];
-    __device__ __forceinline__ Piece(const Args& a, const Walk<C::kRows, kTile, kOver>& w) {
-        const int base = w.rb * C::kRows, all = w.r.n * a.G, first = w.r.len - w.r.n + 1;
-        n = w.reach > 0 ? w.t1 - w.t0 : 0;
-        streams = C::kStreams == 2 && base + 128 < all ? 2 : 1;
-        tiles[0] = tiles[1] = n;
-        if (C::kStreams == 2 && streams == 2) {      // the first stream's last row may not see the last tiles
-            const int sees = first + (base + 127) / a.G;
-            tiles[0] = min(n, max((sees + kTile - 1) / kTile - w.t0, 0));
-        }
-        if (streams == 1) tiles[1] = 0;
-    }
+// A piece of an item as every role sees it.  One warp walks along the line and hands the pieces to the others through shared memory: the
+// walk's state and its divisions, kept by every warp, went to local memory (7 prompts of up to 1500 tokens: 230 us and not 217; 4096
+// tokens of 32 heads of 64: 172 and not 160).
+struct __align__(16) Piece {
+    int n, streams;      // tiles, -1: no more pieces; blocks of 128 rows
+    int first_tiles;     // tiles that the first stream takes part in; the second one takes part in all
+    int complete;        // all of the item's tiles
+    int t0, s, kvh, rb;
+    Rows r;
+    int reach;           // positions that take part
+    __device__ __forceinline__ int tiles(int stream) const { return stream == 0 ? first_tiles : n; }
     // lane of tile j of a stream; its buffer of S and P
     __device__ __forceinline__ int lane(int stream, int j) const { return streams == 2 ? stream : (j & 1) * 2; }
     static __device__ __forceinline__ int buffer(int lane) { return lane != 0; }
+    __device__ __forceinline__ float* slot(const Args& a) const { return slot_of(a, t0); }
 };
+static_assert(sizeof(Piece) == 48, "three 16-byte words");
+constexpr int kPieces = 4;         // that a role can be ahead of another
+constexpr int kReaders = 13;       // warps
+
+template <int DP, bool EIGHT>
+struct Smem {
+    unsigned char q[Cfg<DP, EIGHT>::kQ];
+    unsigned char ring[Cfg<DP, EIGHT>::kStages * Cfg<DP>::kStage];
+    unsigned char raw[2 * Cfg<DP, EIGHT>::kRaw + 16];
+    long long q_row[Cfg<DP>::kRows];     // where the item's rows of q are, -1: none
+    Flags flags;
+    Piece pieces[kPieces];
+    Bars bars;
+    long long sh[kThreads / 32 + 3];
+};
+
+// The next piece, by a whole warp; false: there is none.
+template <int DP, bool EIGHT>
+__device__ __forceinline__ bool next_piece(Smem<DP, EIGHT>& sm, uint32_t& k, Piece& p) {
+    const uint32_t at = k % kPieces;
+    if (!warp_wait(&sm.bars.piece_full[at], k / kPieces, &sm.bars.abort)) return false;
+    ++k;
+    p = sm.pieces[at];
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(&sm.bars.piece_empty[at]);
+    return p.n >= 0;
+}
+template <int DP, bool EIGHT>
+__device__ void walk_line(const Args& a, Smem<DP, EIGHT>& sm, Walk<Cfg<DP>::kRows, kTile, kOver> w, long long total) {
+    using C = Cfg<DP>;
+    for (uint32_t k = 0;; ++k) {
+        Piece p = {};
+        p.n = -1;
+        if (w.left > 0) {
+            const int base = w.rb * C::kRows, all = w.r.n * a.G;
+            p.n = w.reach > 0 ? w.t1 - w.t0 : 0;
+            p.streams = C::kStreams == 2 && base + 128 < all ? 2 : 1;
+            p.first_tiles = p.n;
+            if (p.streams == 2) {      // the first stream's last row may not see the last tiles
+                const int sees = w.r.len - w.r.n + 1 + (base + 127) / a.G;
+                p.first_tiles = min(p.n, max((sees + kTile - 1) / kTile - w.t0, 0));
+            }
+            p.complete = w.complete();
+            p.t0 = w.t0;
+            p.s = w.s;
+            p.kvh = w.kvh;
+            p.rb = w.rb;
+            p.r = w.r;
+            p.reach = w.reach;
+        }
+        const uint32_t at = k % kPieces;
+        if (!warp_wait(&sm.bars.piece_empty[at], k / kPieces + 1, &sm.bars.abort)) return;      // the phase before
+        if ((threadIdx.x & 31) == 0) {
+            sm.pieces[at] = p;
+            mbar_arrive(&sm.bars.piece_full[at]);
+            if (w.left > 0 && w.opens()) a.openings[blockIdx.x] = w.opening(total);
+        }
+        if (p.n < 0) return;
+        w.next(a);
+    }
+}
 
 // ---- gathering ------------------------------------------------------------------------------------------------------------------
 
@@ -305,7 +352,7 @@ struct Gather {
         }
         issued(full);
     }
-    __device__ __forceinline__ void queries(const Walk<C::kRows, kTile, kOver>& w, const Piece<DP>& p, uint32_t piece) {
+    __device__ __forceinline__ void queries(const Piece& p, uint32_t piece) {
         await(&sm.bars.q_empty, piece + 1);
         if (!alive) return;
         const uint32_t q = smem_u32(sm.q), full = smem_u32(&sm.bars.q_full);
@@ -318,15 +365,15 @@ struct Gather {
             __syncwarp();
             if (lane < mine) {
                 const int box = lane * 4 + warp, t = box / blocks, block = box - t * blocks;
-                const int token = w.r.first + (w.rb * C::kRows + t * 128) / a.G;
-                tma_load_3d(q + t * C::kQTile + block * (128 * 128), &maps.q, block * 64, w.kvh * a.G, token, full);
+                const int token = p.r.first + (p.rb * C::kRows + t * 128) / a.G;
+                tma_load_3d(q + t * C::kQTile + block * (128 * 128), &maps.q, block * 64, p.kvh * a.G, token, full);
             }
             return;
         }
         constexpr int kOwn = C::kRows / 4, kWide = DP / 8, kRowsAtOnce = 32 / kWide;      // rows of a warp
 #pragma unroll
         for (int i = lane; i < kOwn; i += 32) {
-            const Row r = row_at<C::kRows>(a, w.r, w.kvh, w.rb, warp * kOwn + i);
+            const Row r = row_at<C::kRows>(a, p.r, p.kvh, p.rb, warp * kOwn + i);
             sm.q_row[warp * kOwn + i] = r.there ? static_cast<long long>(r.token) * a.q_stride + static_cast<long long>(r.head) * a.dh : -1;
         }
         __syncwarp();
@@ -411,21 +458,20 @@ struct Gather {
         else spread<false>(dst, steps, slot);
         signal(smem_u32(&sm.bars.full[s]));
     }
-    __device__ void run(Walk<C::kRows, kTile, kOver> w) {
+    __device__ void run() {
         bool bad = false;
-        uint32_t tile = 0, piece = 0;
-        while (w.left > 0 && alive) {
-            const Piece<DP> p(a, w);
+        uint32_t tile = 0, piece = 0, k = 0;
+        for (Piece p; alive && next_piece(sm, k, p);) {
             const auto page_of = [&](int j) {     // of this lane's key of the j-th tile
-                const int at = (w.t0 + j) * kTile + warp * 32 + lane;
-                if (j >= p.n || at >= w.reach) return -1;
-                return ldg_waited(a.table + static_cast<long long>(w.s) * a.max_pages + (a.page_shift >= 0 ? at >> a.page_shift : at / a.page_size));
+                const int at = (p.t0 + j) * kTile + warp * 32 + lane;
+                if (j >= p.n || at >= p.reach) return -1;
+                return ldg_waited(a.table + static_cast<long long>(p.s) * a.max_pages + (a.page_shift >= 0 ? at >> a.page_shift : at / a.page_size));
             };
             int page = page_of(0);
             // ahead of the keys where the item before is through with its own, else behind the first keys and values
             bool asked = p.n == 0;
             if (!asked && ready(&sm.bars.q_empty, piece + 1)) {
-                queries(w, p, piece);
+                queries(p, piece);
                 asked = true;
             }
             if constexpr (EIGHT) {
@@ -436,11 +482,11 @@ struct Gather {
                 const auto ask = [&](int f) {    // the codes of the f-th stage of the piece
                     const int j = f / kFills, h = f % kFills;
                     if (h == 0) {
-                        const int pos = (w.t0 + j) * kTile + warp * 32 + lane;
-                        const bool in = pos < w.reach, ok = in && page >= 0 && page < a.n_pages;
+                        const int pos = (p.t0 + j) * kTile + warp * 32 + lane;
+                        const bool in = pos < p.reach, ok = in && page >= 0 && page < a.n_pages;
                         bad |= in && !ok;
                         const int in_page = a.page_shift >= 0 ? pos & (a.page_size - 1) : pos % a.page_size;
-                        const long long row = static_cast<long long>(w.kvh) * a.page_size + in_page;
+                        const long long row = static_cast<long long>(p.kvh) * a.page_size + in_page;
                         at = ok ? page * a.page_stride + row * a.dh : -1;
                         kb = vb = 0;
                         if (ok) {
@@ -465,33 +511,32 @@ struct Gather {
                     }
                     widen(byte, f & 1);
                     if (f == kFills - 1 && !asked && alive) {
-                        queries(w, p, piece);
+                        queries(p, piece);
                         asked = true;
                     }
                 }
             } else {
             for (int j = 0; j < p.n && alive; ++j, ++tile) {
                 const int next = page_of(j + 1);
-                const int pos = (w.t0 + j) * kTile;
-                const bool in = pos + warp * 32 + lane < w.reach, ok = in && page >= 0 && page < a.n_pages;
+                const int pos = (p.t0 + j) * kTile;
+                const bool in = pos + warp * 32 + lane < p.reach, ok = in && page >= 0 && page < a.n_pages;
                 bad |= in && !ok;
                 const uint32_t there = __ballot_sync(0xffffffffu, ok);
                 // the slot's last readers are done: their P went into a product behind which stages were freed for this tile
                 if (lane == 0) sm.flags.there[tile % kFlags][warp] = there;
                 const int from = ok ? page : a.n_pages;
 #pragma unroll
-                for (int h = 0; h < C::kParts; ++h) stage(&maps.K, a.K, from, pos, w.kvh, h, 0xffffffffu);      // scores of absent keys are masked
+                for (int h = 0; h < C::kParts; ++h) stage(&maps.K, a.K, from, pos, p.kvh, h, 0xffffffffu);      // scores of absent keys are masked
 #pragma unroll
-                for (int h = 0; h < C::kParts; ++h) stage(&maps.V, a.V, from, pos, w.kvh, h, there);
+                for (int h = 0; h < C::kParts; ++h) stage(&maps.V, a.V, from, pos, p.kvh, h, there);
                 if (!asked && alive) {
-                    queries(w, p, piece);
+                    queries(p, piece);
                     asked = true;
                 }
                 page = next;
             }
             }
             if (p.n > 0) ++piece;
-            w.next(a);
         }
         flush();
         if (__any_sync(0xffffffffu, bad) && lane == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
@@ -593,16 +638,12 @@ struct Issue {
     template <int t>
     __device__ __forceinline__ bool turn(int j, int n, int on) {
         if (j >= n) return true;
-        if (!warp_wait(&bars.p_full[t], use<t>() - 1, abort)) return false;
         const bool more = j + 1 < n;
-        if (C::kApart && more) {      // S has been read: its place is free
-            if (!await_stage(j + 1, 0)) return false;
-            scores<t, t>(j + 1, t == 1 || j + 1 >= on);
-        }
-        if (!await_stage(j, 1)) return false;
+        if (!await_stage(j, 1) || (more && !await_stage(j + 1, 0)) || !warp_wait(&bars.p_full[t], use<t>() - 1, abort)) return false;
+        if (C::kApart && more) scores<t, t>(j + 1, t == 1 || j + 1 >= on);      // S has been read: its place is free
         sums<t, t>(j, t == 1 || j >= on);
         if (!C::kApart && more) {
-            if (!await_stage(j + 1, 0) || !warp_wait(&bars.pv_done[t], use<t>() - 1, abort)) return false;
+            if (!warp_wait(&bars.pv_done[t], use<t>() - 1, abort)) return false;
             scores<t, t>(j + 1, t == 1 || j + 1 >= on);
         }
         return true;
@@ -665,20 +706,13 @@ struct Issue {
         }
         return true;
     }
-    __device__ void run(Walk<C::kRows, kTile, kOver> w) {
-        uint32_t piece = 0;
-        while (w.left > 0) {
-            const Piece<DP> p(a, w);
-            if (p.n > 0) {
-                if (!warp_wait(&bars.q_full, piece++, abort)) return;
-                if (C::kStreams == 2 && p.streams == 2) {
-                    if (!turns(p.tiles[0], p.tiles[1])) return;
-                } else if (!alone(p.n)) {
-                    return;
-                }
-                first_fill += p.n * 2 * C::kParts;
-            }
-            w.next(a);
+    __device__ void run() {
+        uint32_t piece = 0, k = 0;
+        for (Piece p; next_piece(sm, k, p);) {
+            if (p.n == 0) continue;
+            if (!warp_wait(&bars.q_full, piece++, abort)) return;
+            if (!(C::kStreams == 2 && p.streams == 2 ? turns(p.first_tiles, p.n) : alone(p.n))) return;
+            first_fill += p.n * 2 * C::kParts;
         }
     }
 };
@@ -781,7 +815,7 @@ __device__ __forceinline__ void turn_words(uint4 (&w)[4], int lane) {
 }
 
 template <int DP, bool EIGHT>
-__device__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm, Walk<Cfg<DP>::kRows, kTile, kOver> w, long long total) {
+__device__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm) {
     using C = Cfg<DP>;
     constexpr float kSlack = 8.0f;            // powers of two that a reference may lag behind where it is looked at
     constexpr float kSum = 1048576.0f;        // what a tile's weights may sum to before it is
@@ -793,12 +827,12 @@ __device__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm, Walk<Cfg<DP>::k
     const float scale = fabsf(a.scale_log2);
     uint32_t tile = 0, used[kLanes] = {0, 0, 0};      // tiles so far; of the lanes of this stream
     bool alive = true;
-    while (w.left > 0 && alive) {
-        const Piece<DP> p(a, w);
+    uint32_t k = 0;
+    for (Piece p; alive && next_piece(sm, k, p);) {
         if (t < p.streams) {
-            const Row row = row_at<C::kRows>(a, w.r, w.kvh, w.rb, item_row);
-            const int n = p.tiles[t];
-            const int all_see = w.r.len - w.r.n + 1 + (w.rb * C::kRows + t * 128) / a.G;
+            const Row row = row_at<C::kRows>(a, p.r, p.kvh, p.rb, item_row);
+            const int n = p.tiles(t);
+            const int all_see = p.r.len - p.r.n + 1 + (p.rb * C::kRows + t * 128) / a.G;
             float m = -INFINITY, l = 0.0f;
             const auto await_sums = [&](int j) {      // of tile j, the last one that was counted in its lane
                 const int b = p.lane(t, j);
@@ -806,7 +840,7 @@ __device__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm, Walk<Cfg<DP>::k
                 tcgen05_fence_after_sync();
             };
             for (int j = 0; j < n && alive; ++j) {
-                const int b = p.lane(t, j), p0 = (w.t0 + j) * kTile;
+                const int b = p.lane(t, j), p0 = (p.t0 + j) * kTile;
                 alive = warp_wait(&bars.s_full[b], used[b], abort);
                 if (!alive) break;
                 tcgen05_fence_after_sync();
@@ -923,8 +957,8 @@ __device__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm, Walk<Cfg<DP>::k
             const long long at = static_cast<long long>(row.token) * a.H + row.head;
             const float f = some ? 1.0f / l : 0.0f, base = m == -INFINITY ? 0.0f : m * scale;
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + at * a.dh;
-            float* slot = w.slot(a) + 2ll * a.rows + static_cast<long long>(item_row) * 4;
-            const bool complete = w.complete();
+            float* slot = p.slot(a) + 2ll * a.rows + static_cast<long long>(item_row) * 4;
+            const bool complete = p.complete;
             bool odd = false;
             if (complete) {
                 const long long mine = row.there ? at * a.dh : -1;
@@ -960,8 +994,8 @@ __device__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm, Walk<Cfg<DP>::k
                 if (row.there && a.lse) a.lse[at] = some ? (m * scale + log2f(l)) * kLn2 : -INFINITY;
             } else {
                 if (row.there) {
-                    w.slot(a)[item_row] = m * scale;
-                    w.slot(a)[a.rows + item_row] = l;
+                    p.slot(a)[item_row] = m * scale;
+                    p.slot(a)[a.rows + item_row] = l;
                 }
                 for (int c = 0; c < a.dh; c += 16) {
                     uint32_t o[16] = {};
@@ -979,21 +1013,19 @@ __device__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm, Walk<Cfg<DP>::k
                 }
             }
             // a value that is infinite or NaN, in a tile that the row does not see all of: what it does see, on its own
-            uint32_t again = __ballot_sync(0xffffffffu, odd && some && fabsf(l) < INFINITY && (w.t0 + n) * kTile > all_see);
+            uint32_t again = __ballot_sync(0xffffffffu, odd && some && fabsf(l) < INFINITY && (p.t0 + n) * kTile > all_see);
             while (again) {
                 const int q = __ffs(again) - 1;
                 again &= again - 1;
-                const int p1 = min((w.t0 + n) * kTile, row.sees);
+                const int p1 = min((p.t0 + n) * kTile, row.sees);
                 const unsigned long long to = reinterpret_cast<unsigned long long>(complete ? static_cast<void*>(out) : static_cast<void*>(slot));
-                resum(a, w.s, w.kvh, __shfl_sync(0xffffffffu, row.token, q), __shfl_sync(0xffffffffu, row.head, q), w.t0 * kTile,
+                resum(a, p.s, p.kvh, __shfl_sync(0xffffffffu, row.token, q), __shfl_sync(0xffffffffu, row.head, q), p.t0 * kTile,
                       __shfl_sync(0xffffffffu, p1, q), __shfl_sync(0xffffffffu, base, q), __shfl_sync(0xffffffffu, f, q),
                       reinterpret_cast<void*>(__shfl_sync(0xffffffffu, to, q)), complete ? 0 : 4ll * a.rows);
                 __syncwarp();
             }
         }
-        if (threadIdx.x == 0 && w.opens()) a.openings[blockIdx.x] = w.opening(total);
         tile += p.n;
-        w.next(a);
     }
 }
 
@@ -1005,8 +1037,6 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __g
     Bars& bars = sm.bars;
     const int tid = threadIdx.x, warp = tid >> 5;
     chain_wait();
-    const Found<C::kRows, kTile, kOver> f = locate<C::kRows, kTile, kOver, kThreads>(a, sm.sh);
-    if (f.walk.left <= 0) return;      // the same in every thread
     if (tid == 0) {
         for (int i = 0; i < C::kStages; ++i) {
             mbar_init(&bars.full[i], 4);      // the gathering warps
@@ -1020,6 +1050,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __g
             mbar_init(&bars.pv_done[b], 1);
         }
         for (int i = 0; i < 4; ++i) mbar_init(&bars.raw[i], 1);
+        for (int i = 0; i < kPieces; ++i) {
+            mbar_init(&bars.piece_full[i], 1);
+            mbar_init(&bars.piece_empty[i], kReaders);
+        }
         bars.abort = 0;
         mbar_fence_init();
     }
@@ -1028,17 +1062,22 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __g
         tmem_relinquish_alloc_permit();
     }
     tcgen05_fence_before_sync();
-    __syncthreads();
+    const Found<C::kRows, kTile, kOver> f = locate<C::kRows, kTile, kOver, kThreads>(a, sm.sh);      // threads meet in it
     tcgen05_fence_after_sync();
+    if (f.walk.left <= 0) {      // the same in every thread
+        if (warp == 12) tmem_dealloc(bars.tmem, 512);
+        return;
+    }
     if (warp < 8) {
         more_registers<kRowRegs>();
-        softmax_rows<DP, EIGHT>(a, sm, f.walk, f.total);
+        softmax_rows<DP, EIGHT>(a, sm);
     } else if (warp < 12) {
         fewer_registers<kCopyRegs>();
-        Gather<DP, EIGHT>(a, maps, sm).run(f.walk);
+        Gather<DP, EIGHT>(a, maps, sm).run();
     } else {
         fewer_registers<kIssueRegs>();
-        if (warp == 12) Issue<DP, EIGHT>(a, sm).run(f.walk);
+        if (warp == 12) Issue<DP, EIGHT>(a, sm).run();
+        if (warp == 13) walk_line<DP, EIGHT>(a, sm, f.walk, f.total);
     }
     __syncwarp();
     tcgen05_fence_before_sync();

@@ -125,13 +125,20 @@ struct Line {
 // Thread blocks that have a range, and where the c-th range begins.  A range has at least kMinUnits unless there are fewer: a
 // cut costs two slots of traffic and a join.
 constexpr int kMinUnits = 4;
+// Most lines are short: a division of 32 bits takes a fifth of the time
+__device__ __forceinline__ long long quotient(long long x, long long by) {      // of numbers that are not negative
+    return (x | by) >> 32 ? x / by : static_cast<uint32_t>(x) / static_cast<uint32_t>(by);
+}
 __device__ __forceinline__ int ranges(long long T, int blocks) {
     const long long n = T / kMinUnits;
     return n < 1 ? 1 : n < blocks ? static_cast<int>(n) : blocks;
 }
-__device__ __forceinline__ long long cut(long long T, int c, int C) { return T * c / C; }
+__device__ __forceinline__ long long cut(long long T, int c, int C) { return quotient(T * c, C); }
 // the range that holds line position x: the last c with T * c / C <= x
-__device__ __forceinline__ int range_of(long long T, long long x, int C) { return static_cast<int>(((x + 1) * C - 1) / T); }
+__device__ __forceinline__ int range_of(long long T, long long x, int C) { return static_cast<int>(quotient((x + 1) * C - 1, T)); }
+
+// where the sums of a piece that is not complete go: a range's first piece has no first tile, its last one has
+__device__ __forceinline__ float* slot_of(const Args& a, int t0) { return a.ws + (static_cast<long long>(blockIdx.x) * 2 + (t0 > 0 ? 0 : 1)) * a.slot; }
 
 // The way along a range: piece after piece.
 template <int ROWS, int TILE, int OVER>
@@ -174,8 +181,7 @@ struct Walk {
             item(a);
         } while (t1 <= t0);      // a piece of the units in front alone: its tiles are the next range's
     }
-    // where the sums of a piece that is not complete go: a range's first piece has no first tile, its last one has
-    __device__ __forceinline__ float* slot(const Args& a) const { return a.ws + (static_cast<long long>(blockIdx.x) * 2 + (t0 > 0 ? 0 : 1)) * a.slot; }
+    __device__ __forceinline__ float* slot(const Args& a) const { return slot_of(a, t0); }
     __device__ __forceinline__ Opening opening(long long total) const { return {opens(), kvh, rb, r.first, r.n, nt + OVER - u1, total}; }
 };
 
@@ -240,7 +246,7 @@ __device__ __forceinline__ Found<ROWS, TILE, OVER> locate(const Args& a, long lo
     w.left = cut(f.total, blockIdx.x + 1, C) - x;
     w.r = rows_of(a, w.s, false);
     w.nb = L::blocks_of(a, w.r);
-    w.kvh = static_cast<int>(inside / per_head);
+    w.kvh = static_cast<int>(quotient(inside, per_head));
     // the item: 32 at a time
     long long rem = inside - w.kvh * per_head;
     for (int b = 0;; b += 32) {
