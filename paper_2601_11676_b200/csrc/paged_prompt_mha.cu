@@ -597,6 +597,10 @@ struct Issue {
         const uint32_t d = tmem + (b != 0) * 128;
         if (b != 0) last = b;
         ++use<b>();
+        // what this thread has seen of the gathering warps, the tile's flags among it; in front of the products, as what follows
+        // them waits until the tensor cores have taken them
+        if (lead) mbar_arrive(&bars.s_full[b]);
+        __syncwarp();
 #pragma unroll
         for (int h = 0; h < C::kParts; ++h) {
             const uint32_t s = (first_fill + j * 2 * C::kParts + h) % C::kStages;
@@ -613,7 +617,6 @@ struct Issue {
             if (end) commit(lead, &bars.empty[s]);
         }
         commit(lead, &bars.s_full[b]);
-        if (lead) mbar_arrive(&bars.s_full[b]);      // what this thread has seen of the gathering warps, the tile's flags among it
     }
     template <int t, int b>
     __device__ __forceinline__ void sums(int j, bool end) {
@@ -639,7 +642,10 @@ struct Issue {
     __device__ __forceinline__ bool turn(int j, int n, int on) {
         if (j >= n) return true;
         const bool more = j + 1 < n;
-        if (!await_stage(j, 1) || (more && !await_stage(j + 1, 0)) || !warp_wait(&bars.p_full[t], use<t>() - 1, abort)) return false;
+        // the second stream's stages are the first one's, where that had them
+        if (!(t == 1 && j < on) && !await_stage(j, 1)) return false;
+        if (more && !(t == 1 && j + 1 < on) && !await_stage(j + 1, 0)) return false;
+        if (!warp_wait(&bars.p_full[t], use<t>() - 1, abort)) return false;
         if (C::kApart && more) scores<t, t>(j + 1, t == 1 || j + 1 >= on);      // S has been read: its place is free
         sums<t, t>(j, t == 1 || j >= on);
         if (!C::kApart && more) {
