@@ -34,7 +34,9 @@ namespace {
 
 constexpr int kTile = 128;         // keys
 constexpr int kThreads = 512;
-constexpr int kOver = 4;           // an item's rows, first scores and outputs cost about as much as four tiles
+// An item's rows, first scores and outputs cost 6000 to 9000 clocks, a tile 4500 (thread blocks of many short items against ones of
+// two long items).  With 1 here, 4096 tokens of 32 heads of 64 took 165 us and not 151; with 4, of heads of 128 197 and not 192.
+constexpr int kOver = 2;
 constexpr int kFlags = 8;          // tiles whose flags are kept
 
 // DP: head size padded to 64, 128 or 256.  EIGHT: 8-bit rows.
