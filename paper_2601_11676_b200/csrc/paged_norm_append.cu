@@ -10,7 +10,8 @@
 // A lane has two 16-byte words' worth of elements (eight of each) of a head: those of its pairs (i, i + rotary / 2), or two
 // neighbours; it walks over the heads of q, k and v alike, so cosines and sines stay in registers, and no element of a pair has to
 // be fetched from another lane.  LANES lanes hold a head, a power of two, and sum its squares and find its largest element by
-// shuffles.  An element costs about ten instructions; with one word to a lane (and its partners' from another) it was twice that,
+// shuffles.  One head of a lane is in flight at a time: three took more registers, and 8297 tokens into 8-bit rows 64 us and not 59.
+// An element costs about ten instructions; with one word to a lane (and its partners' from another) it was twice that,
 // and the instructions were what bounded it.  Pairs whose distance is no whole number of eight elements go by that form
 // (paged_norm_append_any_kernel): through a row of shared memory that only the warp's own lanes touch.
 #include <math.h>
@@ -26,7 +27,6 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kOwn = 8;      // elements per lane
-constexpr int kHeads = 3;    // heads in flight per lane
 
 struct NormAppendArgs {
     int H, Hk, dh, page_size, n_pages, max_pages, n_seq, rotary;
@@ -104,14 +104,9 @@ paged_norm_append_any_kernel(const __grid_constant__ NormAppendArgs a, int parts
     const T* q = static_cast<const T*>(a.q) + static_cast<long long>(tok) * a.q_stride + el;
     const T* k = static_cast<const T*>(a.k) + static_cast<long long>(tok) * a.k_stride + el;
     const T* v = static_cast<const T*>(a.v) + static_cast<long long>(tok) * a.v_stride + el;
-    Own<T> x[kHeads];
-    const auto fetch = [&](int h0) {
-#pragma unroll
-        for (int i = 0; i < kHeads; ++i) {
-            const int h = h0 + i * step;
-            if (in && h < heads)
-                x[i].load(h < a.H ? q + h * a.dh : h < a.H + a.Hk ? k + (h - a.H) * a.dh : v + (h - a.H - a.Hk) * a.dh);
-        }
+    Own<T> x;
+    const auto fetch = [&](int h) {
+        if (in && h < heads) x.load(h < a.H ? q + h * a.dh : h < a.H + a.Hk ? k + (h - a.H) * a.dh : v + (h - a.H - a.Hk) * a.dh);
     };
     const int first = part * kGroups + group;
     const double freq = tid < half ? ldg_waited(a.inv_freq + tid) : 0.0;   // half <= 128 threads
@@ -164,72 +159,67 @@ paged_norm_append_any_kernel(const __grid_constant__ NormAppendArgs a, int parts
     float* mine = rows[group];
 
     // every lane of a warp takes every step: lanes meet in the shuffles
-    for (int h0 = first, b0 = part * kGroups; b0 < heads; h0 += step * kHeads, b0 += step * kHeads) {
-        if (h0 != first) fetch(h0);
+    for (int h = first, b0 = part * kGroups; b0 < heads; h += step, b0 += step) {      // b0: the same in every lane of the block
+        if (h != first) fetch(h);
+        const bool there = in && h < heads, is_q = h < a.H, is_v = h >= a.H + a.Hk;
+        float f[kOwn];
 #pragma unroll
-        for (int i = 0; i < kHeads; ++i) {
-            if (b0 + i * step >= heads) break;         // the same in every lane of the block
-            const int h = h0 + i * step;
-            const bool there = in && h < heads, is_q = h < a.H, is_v = h >= a.H + a.Hk;
-            float f[kOwn];
+        for (int e = 0; e < kOwn; ++e) f[e] = 0.0f;
+        if (there) x.widen(f);
+        const bool normed = !is_v && (is_q ? a.w_q : a.w_k) != nullptr;
+        if (a.w_q || a.w_k) {
+            float sum = 0.0f;
 #pragma unroll
-            for (int e = 0; e < kOwn; ++e) f[e] = 0.0f;
-            if (there) x[i].widen(f);
-            const bool normed = !is_v && (is_q ? a.w_q : a.w_k) != nullptr;
-            if (a.w_q || a.w_k) {
-                float sum = 0.0f;
+            for (int e = 0; e < kOwn; ++e) sum = fmaf(f[e], f[e], sum);
+            sum = lanes_sum<LANES>(sum);
+            if (there && normed) {
+                const float n = rsqrtf(sum / static_cast<float>(a.dh) + a.eps);
 #pragma unroll
-                for (int e = 0; e < kOwn; ++e) sum = fmaf(f[e], f[e], sum);
-                sum = lanes_sum<LANES>(sum);
-                if (there && normed) {
-                    const float n = rsqrtf(sum / static_cast<float>(a.dh) + a.eps);
+                for (int e = 0; e < kOwn; ++e) f[e] = f[e] * n * (is_q ? wq[e] : wk[e]);
+            }
+        }
+        {
+            __syncwarp();
+            *reinterpret_cast<float4*>(mine + el) = make_float4(f[0], f[1], f[2], f[3]);
+            *reinterpret_cast<float4*>(mine + el + 4) = make_float4(f[4], f[5], f[6], f[7]);
+            __syncwarp();
+            if (turned && !is_v) {
+                float o[kOwn];
 #pragma unroll
-                    for (int e = 0; e < kOwn; ++e) f[e] = f[e] * n * (is_q ? wq[e] : wk[e]);
+                for (int e = 0; e < kOwn; ++e) {
+                    const int at = el + e;
+                    o[e] = at < a.rotary ? mine[at < half ? at + half : at - half] : 0.0f;
                 }
-            }
-            {
-                __syncwarp();
-                *reinterpret_cast<float4*>(mine + el) = make_float4(f[0], f[1], f[2], f[3]);
-                *reinterpret_cast<float4*>(mine + el + 4) = make_float4(f[4], f[5], f[6], f[7]);
-                __syncwarp();
-                if (turned && !is_v) {
-                    float o[kOwn];
 #pragma unroll
-                    for (int e = 0; e < kOwn; ++e) {
-                        const int at = el + e;
-                        o[e] = at < a.rotary ? mine[at < half ? at + half : at - half] : 0.0f;
-                    }
-#pragma unroll
-                    for (int e = 0; e < kOwn; ++e)
-                        if (el + e < a.rotary) f[e] = f[e] * co[e] + o[e] * si[e];
-                }
+                for (int e = 0; e < kOwn; ++e)
+                    if (el + e < a.rotary) f[e] = f[e] * co[e] + o[e] * si[e];
             }
-            if (EIGHT && b0 + i * step + kGroups > a.H) {      // a head of this pass is a key or a value
-                uint32_t top = 0;                               // sizes of finite numbers, ordered as their bits are
+        }
+        if (EIGHT && b0 + kGroups > a.H) {      // a head of this pass is a key or a value
+            uint32_t top = 0;                               // sizes of finite numbers, ordered as their bits are
 #pragma unroll
-                for (int e = 0; e < kOwn; ++e) top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
-                top = lanes_max<LANES>(top);
-                if (there && !is_q) {
-                    const bool sound = top < 0x7f800000u;
-                    const int ex = eight_exponent(__uint_as_float(top));
-                    const float n = eight_power(-ex);
-                    uint32_t w[2];
+            for (int e = 0; e < kOwn; ++e) top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
+            top = lanes_max<LANES>(top);
+            if (there && !is_q) {
+                const bool sound = top < 0x7f800000u;
+                const int ex = eight_exponent(__uint_as_float(top));
+                const float n = eight_power(-ex);
+                uint32_t w[2];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        w[j] = sound ? eight_pair(f[4 * j] * n, f[4 * j + 1] * n) | eight_pair(f[4 * j + 2] * n, f[4 * j + 3] * n) << 16 : 0u;
-                    const int kv = is_v ? h - a.H - a.Hk : h - a.H;
-                    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(is_v ? a.V : a.K) + base + kv * plane) = make_uint2(w[0], w[1]);
-                    if (c == 0)
-                        (is_v ? a.V_scale : a.K_scale)[row + static_cast<long long>(kv) * a.page_size] =
-                            static_cast<uint8_t>(sound ? ex + 127 : kEightNan);
-                }
+                for (int j = 0; j < 2; ++j)
+                    w[j] = sound ? eight_pair(f[4 * j] * n, f[4 * j + 1] * n) | eight_pair(f[4 * j + 2] * n, f[4 * j + 3] * n) << 16 : 0u;
+                const int kv = is_v ? h - a.H - a.Hk : h - a.H;
+                *reinterpret_cast<uint2*>(static_cast<uint8_t*>(is_v ? a.V : a.K) + base + kv * plane) = make_uint2(w[0], w[1]);
+                if (c == 0)
+                    (is_v ? a.V_scale : a.K_scale)[row + static_cast<long long>(kv) * a.page_size] =
+                        static_cast<uint8_t>(sound ? ex + 127 : kEightNan);
             }
-            if (there && (is_q || !EIGHT)) {
-                x[i].narrow(f);
-                x[i].store(is_q ? qo + h * a.dh
-                           : is_v ? static_cast<T*>(a.V) + base + (h - a.H - a.Hk) * plane
-                                  : static_cast<T*>(a.K) + base + (h - a.H) * plane);
-            }
+        }
+        if (there && (is_q || !EIGHT)) {
+            x.narrow(f);
+            x.store(is_q ? qo + h * a.dh
+                       : is_v ? static_cast<T*>(a.V) + base + (h - a.H - a.Hk) * plane
+                              : static_cast<T*>(a.K) + base + (h - a.H) * plane);
         }
     }
 }
@@ -256,16 +246,12 @@ paged_norm_append_kernel(const __grid_constant__ NormAppendArgs a, int parts) {
     const T* q = static_cast<const T*>(a.q) + static_cast<long long>(tok) * a.q_stride;
     const T* k = static_cast<const T*>(a.k) + static_cast<long long>(tok) * a.k_stride - a.H * a.dh;
     const T* v = static_cast<const T*>(a.v) + static_cast<long long>(tok) * a.v_stride - (a.H + a.Hk) * a.dh;
-    Own<T> x[kHeads][2];
-    const auto fetch = [&](int h0) {
-#pragma unroll
-        for (int i = 0; i < kHeads; ++i) {
-            const int h = h0 + i * step;
-            if (in && h < heads) {
-                const T* src = (h < a.H ? q : h < a.H + a.Hk ? k : v) + h * a.dh;
-                x[i][0].load(src + el0);
-                x[i][1].load(src + el1);
-            }
+    Own<T> x[2];
+    const auto fetch = [&](int h) {
+        if (in && h < heads) {
+            const T* src = (h < a.H ? q : h < a.H + a.Hk ? k : v) + h * a.dh;
+            x[0].load(src + el0);
+            x[1].load(src + el1);
         }
     };
     const int first = part * kGroups + group;
@@ -305,97 +291,92 @@ paged_norm_append_kernel(const __grid_constant__ NormAppendArgs a, int parts) {
     T* qo = static_cast<T*>(a.q_out) + static_cast<long long>(tok) * a.qo_stride;
 
     // every lane of a warp takes every step: lanes meet in the shuffles
-    for (int h0 = first, b0 = part * kGroups; b0 < heads; h0 += step * kHeads, b0 += step * kHeads) {
-        if (h0 != first) fetch(h0);
+    for (int h = first, b0 = part * kGroups; b0 < heads; h += step, b0 += step) {      // b0: the same in every lane of the block
+        if (h != first) fetch(h);
+        const bool there = in && h < heads, is_q = h < a.H, is_v = h >= a.H + a.Hk;
+        float f[2][kOwn];
+        if (there) {
+            x[0].widen(f[0]);
+            x[1].widen(f[1]);
+        } else {
 #pragma unroll
-        for (int i = 0; i < kHeads; ++i) {
-            if (b0 + i * step >= heads) break;         // the same in every lane of the block
-            const int h = h0 + i * step;
-            const bool there = in && h < heads, is_q = h < a.H, is_v = h >= a.H + a.Hk;
-            float f[2][kOwn];
-            if (there) {
-                x[i][0].widen(f[0]);
-                x[i][1].widen(f[1]);
-            } else {
+            for (int e = 0; e < kOwn; ++e) f[0][e] = f[1][e] = 0.0f;
+        }
+        float n = 1.0f;
+        if (__any_sync(0xffffffffu, there && !is_v)) {       // queries or keys among the warp's heads
+            const bool normed = !is_v && (is_q ? a.w_q : a.w_k) != nullptr;
+            if (a.w_q || a.w_k) {
+                float sum = 0.0f;
 #pragma unroll
-                for (int e = 0; e < kOwn; ++e) f[0][e] = f[1][e] = 0.0f;
+                for (int e = 0; e < kOwn; ++e) sum = fmaf(f[0][e], f[0][e], fmaf(f[1][e], f[1][e], sum));
+                sum = lanes_sum<LANES>(sum);
+                if (normed) n = rsqrtf(sum / static_cast<float>(a.dh) + a.eps);
             }
-            float n = 1.0f;
-            if (__any_sync(0xffffffffu, there && !is_v)) {       // queries or keys among the warp's heads
-                const bool normed = !is_v && (is_q ? a.w_q : a.w_k) != nullptr;
-                if (a.w_q || a.w_k) {
-                    float sum = 0.0f;
+            if (!is_v && there) {
+                if (normed) {
+                    const float* g = gain[is_q ? 0 : 1];
 #pragma unroll
-                    for (int e = 0; e < kOwn; ++e) sum = fmaf(f[0][e], f[0][e], fmaf(f[1][e], f[1][e], sum));
-                    sum = lanes_sum<LANES>(sum);
-                    if (normed) n = rsqrtf(sum / static_cast<float>(a.dh) + a.eps);
-                }
-                if (!is_v && there) {
-                    if (normed) {
-                        const float* g = gain[is_q ? 0 : 1];
+                    for (int w = 0; w < 2; ++w)
 #pragma unroll
-                        for (int w = 0; w < 2; ++w)
-#pragma unroll
-                            for (int e = 0; e < kOwn; e += 4) {
-                                const float4 by = *reinterpret_cast<const float4*>(g + (w ? el1 : el0) + e);
-                                f[w][e] *= by.x;
-                                f[w][e + 1] *= by.y;
-                                f[w][e + 2] *= by.z;
-                                f[w][e + 3] *= by.w;
-                            }
-                    }
-#pragma unroll
-                    for (int e = 0; e < kOwn; ++e) {
-                        // pair e: its elements lie in the two words, or side by side
-                        float& one = INTERLEAVED ? f[e >> 2][(e & 3) * 2] : f[0][e];
-                        float& two = INTERLEAVED ? f[e >> 2][(e & 3) * 2 + 1] : f[1][e];
-                        if (INTERLEAVED ? u * 8 + e < half : across) {
-                            const float p = one, o = two;
-                            one = p * co[e] - o * si[e];
-                            two = p * si[e] + o * co[e];
+                        for (int e = 0; e < kOwn; e += 4) {
+                            const float4 by = *reinterpret_cast<const float4*>(g + (w ? el1 : el0) + e);
+                            f[w][e] *= by.x;
+                            f[w][e + 1] *= by.y;
+                            f[w][e + 2] *= by.z;
+                            f[w][e + 3] *= by.w;
                         }
+                }
+#pragma unroll
+                for (int e = 0; e < kOwn; ++e) {
+                    // pair e: its elements lie in the two words, or side by side
+                    float& one = INTERLEAVED ? f[e >> 2][(e & 3) * 2] : f[0][e];
+                    float& two = INTERLEAVED ? f[e >> 2][(e & 3) * 2 + 1] : f[1][e];
+                    if (INTERLEAVED ? u * 8 + e < half : across) {
+                        const float p = one, o = two;
+                        one = p * co[e] - o * si[e];
+                        two = p * si[e] + o * co[e];
                     }
                 }
             }
-            if (EIGHT && __any_sync(0xffffffffu, there && !is_q)) {
-                uint32_t top = 0;                               // sizes of finite numbers, ordered as their bits are
+        }
+        if (EIGHT && __any_sync(0xffffffffu, there && !is_q)) {
+            uint32_t top = 0;                               // sizes of finite numbers, ordered as their bits are
 #pragma unroll
-                for (int e = 0; e < kOwn; ++e)
-                    top = max(top, max(__float_as_uint(f[0][e] * n) & 0x7fffffffu, __float_as_uint(f[1][e] * n) & 0x7fffffffu));
-                top = lanes_max<LANES>(top);
-                if (there && !is_q) {
-                    const bool sound = top < 0x7f800000u;
-                    const int ex = eight_exponent(__uint_as_float(top));
-                    const float by = eight_power(-ex);
-                    const int kv = is_v ? h - a.H - a.Hk : h - a.H;
-                    uint8_t* to = static_cast<uint8_t*>(is_v ? a.V : a.K) + base + kv * plane;
+            for (int e = 0; e < kOwn; ++e)
+                top = max(top, max(__float_as_uint(f[0][e] * n) & 0x7fffffffu, __float_as_uint(f[1][e] * n) & 0x7fffffffu));
+            top = lanes_max<LANES>(top);
+            if (there && !is_q) {
+                const bool sound = top < 0x7f800000u;
+                const int ex = eight_exponent(__uint_as_float(top));
+                const float by = eight_power(-ex);
+                const int kv = is_v ? h - a.H - a.Hk : h - a.H;
+                uint8_t* to = static_cast<uint8_t*>(is_v ? a.V : a.K) + base + kv * plane;
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        uint32_t c[2];
+                for (int w = 0; w < 2; ++w) {
+                    uint32_t c[2];
 #pragma unroll
-                        for (int j = 0; j < 2; ++j)
-                            c[j] = sound ? eight_pair(f[w][4 * j] * n * by, f[w][4 * j + 1] * n * by) |
-                                               eight_pair(f[w][4 * j + 2] * n * by, f[w][4 * j + 3] * n * by) << 16 : 0u;
-                        *reinterpret_cast<uint2*>(to + (w ? el1 : el0)) = make_uint2(c[0], c[1]);
-                    }
-                    if (u == 0)
-                        (is_v ? a.V_scale : a.K_scale)[row + static_cast<long long>(kv) * a.page_size] =
-                            static_cast<uint8_t>(sound ? ex + 127 : kEightNan);
+                    for (int j = 0; j < 2; ++j)
+                        c[j] = sound ? eight_pair(f[w][4 * j] * n * by, f[w][4 * j + 1] * n * by) |
+                                           eight_pair(f[w][4 * j + 2] * n * by, f[w][4 * j + 3] * n * by) << 16 : 0u;
+                    *reinterpret_cast<uint2*>(to + (w ? el1 : el0)) = make_uint2(c[0], c[1]);
+                }
+                if (u == 0)
+                    (is_v ? a.V_scale : a.K_scale)[row + static_cast<long long>(kv) * a.page_size] =
+                        static_cast<uint8_t>(sound ? ex + 127 : kEightNan);
+            }
+        }
+        if (there && (is_q || !EIGHT)) {
+            T* to = is_q ? qo + h * a.dh : is_v ? static_cast<T*>(a.V) + base + (h - a.H - a.Hk) * plane : static_cast<T*>(a.K) + base + (h - a.H) * plane;
+            if (!is_v) {
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+#pragma unroll
+                    for (int e = 0; e < kOwn; ++e) f[w][e] *= n;
+                    x[w].narrow(f[w]);
                 }
             }
-            if (there && (is_q || !EIGHT)) {
-                T* to = is_q ? qo + h * a.dh : is_v ? static_cast<T*>(a.V) + base + (h - a.H - a.Hk) * plane : static_cast<T*>(a.K) + base + (h - a.H) * plane;
-                if (!is_v) {
-#pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-#pragma unroll
-                        for (int e = 0; e < kOwn; ++e) f[w][e] *= n;
-                        x[i][w].narrow(f[w]);
-                    }
-                }
-                x[i][0].store(to + el0);
-                x[i][1].store(to + el1);
-            }
+            x[0].store(to + el0);
+            x[1].store(to + el1);
         }
     }
 }
@@ -438,76 +419,52 @@ struct ReadArgs {
     uint32_t* status;
 };
 
-// Thread block: TOKENS tokens, whose chains of loads (position, page, rows) run side by side.  A unit is 16 bytes of the cache: of
-// 8-bit rows 16 codes, which leave as 32 bytes of bf16.
-template <typename T, bool EIGHT, int TOKENS>
-__global__ void __launch_bounds__(kThreads) paged_kv_read_kernel(const __grid_constant__ ReadArgs a, int n_tok) {
+// Thread block: a token (four, with their chains of loads side by side, took 15.1 us and not 13.7 for 8297 tokens, 8 heads of 128 in 8
+// bits).  A unit is 16 bytes of the cache: of 8-bit rows 16 codes, which leave as 32 bytes of bf16.
+template <typename T, bool EIGHT>
+__global__ void __launch_bounds__(kThreads) paged_kv_read_kernel(const __grid_constant__ ReadArgs a) {
     constexpr int E = EIGHT ? 16 : Elem<T>::kPerChunk;
-    const int tok0 = blockIdx.x * TOKENS;
+    const int tok = blockIdx.x;
     chain_wait();
-    int pos[TOKENS], page[TOKENS];
-#pragma unroll
-    for (int t = 0; t < TOKENS; ++t) pos[t] = tok0 + t < n_tok ? ldg_waited(a.pos + tok0 + t) : -1;
-#pragma unroll
-    for (int t = 0; t < TOKENS; ++t) {
-        page[t] = -1;
-        if (pos[t] < 0) continue;
-        const int s = a.seq ? ldg_waited(a.seq + tok0 + t) : tok0 + t, pi = pos[t] / a.page_size;
-        pos[t] -= pi * a.page_size;      // from here on the row in its page
-        if (s >= 0 && s < a.n_seq && pi < a.max_pages) page[t] = ldg_waited(a.table + static_cast<long long>(s) * a.max_pages + pi);
+    const int pos = ldg_waited(a.pos + tok);
+    const int s = a.seq ? ldg_waited(a.seq + tok) : tok;
+    if (pos < 0) return;               // a padding row
+    const int pi = pos / a.page_size, in_page = pos - pi * a.page_size;
+    int page = -1;
+    if (s >= 0 && s < a.n_seq && pi < a.max_pages) page = ldg_waited(a.table + static_cast<long long>(s) * a.max_pages + pi);
+    if (page < 0 || page >= a.n_pages) {
+        if (threadIdx.x == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
+        return;
     }
-#pragma unroll
-    for (int t = 0; t < TOKENS; ++t)
-        if (pos[t] >= 0 && (page[t] < 0 || page[t] >= a.n_pages)) {
-            if (threadIdx.x == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
-            pos[t] = -1;
-        }
     const int per_head = a.dh / E, per_row = a.Hk * per_head;
     for (int u = threadIdx.x; u < 2 * per_row; u += kThreads) {
         const bool is_v = u >= per_row;
         const int w = is_v ? u - per_row : u, h = w / per_head, el = (w - h * per_head) * E;
-        uint4 x[TOKENS];
-        uint32_t byte[TOKENS];
+        const long long row = static_cast<long long>(h) * a.page_size + in_page, from = page * a.page_stride + row * a.dh + el;
+        T* to = (is_v ? static_cast<T*>(a.v_out) + static_cast<long long>(tok) * a.v_stride
+                      : static_cast<T*>(a.k_out) + static_cast<long long>(tok) * a.k_stride) + h * a.dh + el;
+        if constexpr (EIGHT) {
+            const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(is_v ? a.V : a.K) + from);
+            const float unit = eight_unit((is_v ? a.V_scale : a.K_scale)[static_cast<long long>(page) * a.Hk * a.page_size + row]);
+            const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+            __align__(16) T out[16];
 #pragma unroll
-        for (int t = 0; t < TOKENS; ++t) {
-            if (pos[t] < 0) continue;
-            const long long row = static_cast<long long>(h) * a.page_size + pos[t], from = page[t] * a.page_stride + row * a.dh + el;
-            if constexpr (EIGHT) {
-                x[t] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(is_v ? a.V : a.K) + from);
-                byte[t] = (is_v ? a.V_scale : a.K_scale)[static_cast<long long>(page[t]) * a.Hk * a.page_size + row];
-            } else {
-                x[t] = *reinterpret_cast<const uint4*>(static_cast<const T*>(is_v ? a.V : a.K) + from);
+            for (int j = 0; j < 4; ++j) {
+                float f[4];
+                eight_widen(in[j], f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) out[4 * j + e] = from_float<T>(f[e] * unit);   // exact
             }
-        }
-#pragma unroll
-        for (int t = 0; t < TOKENS; ++t) {
-            if (pos[t] < 0) continue;
-            T* to = (is_v ? static_cast<T*>(a.v_out) + static_cast<long long>(tok0 + t) * a.v_stride
-                          : static_cast<T*>(a.k_out) + static_cast<long long>(tok0 + t) * a.k_stride) + h * a.dh + el;
-            if constexpr (EIGHT) {
-                const float unit = eight_unit(byte[t]);
-                const uint32_t in[4] = {x[t].x, x[t].y, x[t].z, x[t].w};
-                __align__(16) T out[16];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float f[4];
-                    eight_widen(in[j], f);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) out[4 * j + e] = from_float<T>(f[e] * unit);   // exact
-                }
-                reinterpret_cast<uint4*>(to)[0] = reinterpret_cast<const uint4*>(out)[0];
-                reinterpret_cast<uint4*>(to)[1] = reinterpret_cast<const uint4*>(out)[1];
-            } else {
-                *reinterpret_cast<uint4*>(to) = x[t];
-            }
+            reinterpret_cast<uint4*>(to)[0] = reinterpret_cast<const uint4*>(out)[0];
+            reinterpret_cast<uint4*>(to)[1] = reinterpret_cast<const uint4*>(out)[1];
+        } else {
+            *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(static_cast<const T*>(is_v ? a.V : a.K) + from);
         }
     }
 }
 template <typename T, bool EIGHT>
 halo_status launch_read(const ReadArgs& a, int n_tok, cudaStream_t st) {
-    // four tokens to a thread block where that still fills the GPU (8297 tokens, 8 heads of 128 in 8 bits: 15 us with one)
-    if (n_tok >= 4 * 8 * kSmCount) return launch_chained(paged_kv_read_kernel<T, EIGHT, 4>, static_cast<unsigned>((n_tok + 3) / 4), kThreads, 0, st, a, n_tok);
-    return launch_chained(paged_kv_read_kernel<T, EIGHT, 1>, static_cast<unsigned>(n_tok), kThreads, 0, st, a, n_tok);
+    return launch_chained(paged_kv_read_kernel<T, EIGHT>, static_cast<unsigned>(n_tok), kThreads, 0, st, a);
 }
 
 }  // namespace
