@@ -325,6 +325,7 @@ __global__ void __launch_bounds__(256) paged_prompt_join_kernel(const __grid_con
         }
 #pragma unroll
         for (int e = 0; e < kAhead; ++e) {
+            if (l[e] == 0.0f) continue;      // the row sees nothing of the piece, whose sums may be 0 * infinity
             const float mx = fmaxf(M, m[e]), base = mx == -INFINITY ? 0.0f : mx;
             const float f = pow2(M - base), g = pow2(m[e] - base);
             M = mx;

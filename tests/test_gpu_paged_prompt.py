@@ -393,3 +393,28 @@ def test_the_bound_itself_follows_the_oracle():
     kept = c.keep.cpu().numpy() != 0
     assert np.allclose(got[3].cpu().numpy()[:, kept], want[3][:, kept], rtol=1e-12)
     assert (got[4].cpu().numpy() == want[4]).all() and got[5] == want[5]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("what", [INF, NAN])
+@pytest.mark.parametrize("chunks", [[(60, 100), (9, 300), (50, 90)], [(60, 100), (60, 220), (60, 340)], [(60, 100)], [(1, 127), (300, 500)]])
+def test_pieces_of_an_item_that_some_rows_do_not_see(kind, what, chunks):
+    """Rows in front of a tile that a thread block has on its own: their weights there are zero, whatever its values are."""
+    c = Case(kind, 8, 2, 64, 16, chunks)
+    for s, (new, past) in enumerate(chunks):
+        p = past + new - 1                       # of the last key, which the sequence's last row alone sees
+        page = c.table[s, p // 16].long()
+        if kind == "8bit":
+            c.Vs[page, :, p % 16] = 255          # a row of NaN
+            c.Vv[page, :, p % 16] = NAN
+        else:
+            c.V[page, :, p % 16, 7] = what
+            c.V[page, 1, p % 16, 8] = -what
+    if kind != "8bit":
+        c.refresh()
+    out, lse, _ = c.run()
+    c.compare(out, lse)
+    last = c.start[1:].long() - 1
+    seen = torch.ones(out.shape[0], dtype=torch.bool, device=DEV)
+    seen[last], seen[int(c.start[-1]):] = False, False
+    assert torch.isfinite(out[seen]).all() and not torch.isfinite(out[last]).all()
