@@ -17,7 +17,7 @@ import torch
 
 from oracle import paged_prompt_ref as P
 from paper_2601_11676_b200 import binding as B
-from tests.test_gpu_paged_prompt import BF16, DEV, F32, INF, NAN, Case, block_table, eight, gen, randn
+from tests.test_gpu_paged_prompt import BF16, DEV, F32, INF, NAN, Case, block_table, eight, far, gen, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -362,3 +362,29 @@ def test_a_prompt_in_chunks_then_tokens(kind):
     where = (table[0, pos.long() // page].long(), slice(None), pos.long() % page)
     c.Kv[where], c.Vv[where], c.q = k.double(), v.double(), q
     c.compare(out, lse)
+
+
+@pytest.mark.parametrize("factor", [-1.0, 0.0, -8.0])
+def test_one_token_under_scales_that_are_negative_or_zero(factor):
+    c = one_token_case(8, 2, 64, 16, [200, 31, 1, 900])
+    c.scale *= factor
+    check_tokens(c)
+
+
+def test_one_token_and_rows_in_pages_behind_31_bits():
+    c = one_token_case(4, 2, 64, 16, [50, 15])
+    far(c)
+    check_tokens(c)
+    pos = torch.arange(50, dtype=torch.int32, device=DEV)
+    k, v = (torch.empty((50, 2, 64), dtype=BF16, device=DEV) for _ in range(2))
+    B.halo_paged_kv_read(c.shape(), pos, torch.zeros_like(pos), c.table, c.K, c.V, k, v, c.Ks, c.Vs)
+    where = (c.table[0, pos.long() // 16].long(), slice(None), pos.long() % 16)
+    assert torch.equal(k.double(), c.Kv[where]) and torch.equal(v.double(), c.Vv[where])
+    # and written there: the same rows again, which come back as they are
+    q = torch.zeros((50, 4, 64), dtype=BF16, device=DEV)
+    c.K[where], c.Ks[where], c.V[where], c.Vs[where] = 1, 1, 1, 1
+    B.halo_paged_norm_append(c.shape(), q, k, v, None, None, 1e-6, pos, torch.zeros_like(pos), c.table, None, False, 1.0, q.clone(), c.K, c.V,
+                             c.Ks, c.Vs)
+    k2, v2 = torch.empty_like(k), torch.empty_like(v)
+    B.halo_paged_kv_read(c.shape(), pos, torch.zeros_like(pos), c.table, c.K, c.V, k2, v2, c.Ks, c.Vs)
+    assert torch.equal(k, k2) and torch.equal(v, v2)

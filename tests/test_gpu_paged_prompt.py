@@ -418,3 +418,45 @@ def test_pieces_of_an_item_that_some_rows_do_not_see(kind, what, chunks):
     seen = torch.ones(out.shape[0], dtype=torch.bool, device=DEV)
     seen[last], seen[int(c.start[-1]):] = False, False
     assert torch.isfinite(out[seen]).all() and not torch.isfinite(out[last]).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("factor", [-1.0, 0.0, -8.0])
+def test_scales_that_are_negative_or_zero(kind, factor):
+    """The largest score is then the smallest product; under zero every key has the same weight."""
+    c = Case(kind, 8, 2, 64, 16, [(150, 400), (20, 0)])
+    c.scale *= factor
+    c.check()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dh,page", [(128, 8), (64, 40), (128, 2), (256, 8)])
+def test_page_sizes(kind, dh, page):
+    Case(kind, 8, 2, dh, page, [(150, 300), (1, 7), (33, 0)]).check()
+
+
+def far(c):
+    """The caches with their pages so far apart that elements of the last one, which is in use, lie more than 2^31 behind the first."""
+    n_pages = c.K.shape[0]
+    stride = 2 ** 31 // (n_pages - 2) // 64 * 64
+    assert (n_pages - 1) * stride > 2 ** 31
+    last = c.table == c.table.max()
+    for x in (c.Ks, c.Vs, c.Kv, c.Vv, c.K, c.V):
+        if x is not None:
+            x[n_pages - 1] = x[int(c.table.max())]
+    c.table[last] = n_pages - 1
+    for name in ("K", "V"):
+        x = getattr(c, name)
+        store = torch.empty((n_pages - 1) * stride + x[0].numel(), dtype=x.dtype, device=DEV)
+        y = store.as_strided(x.shape, (stride, *x.stride()[1:]))
+        y.copy_(x)
+        setattr(c, name, y)
+    shape = c.shape
+    c.shape = lambda: shape(stride)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_pages_behind_31_bits(kind):
+    c = Case(kind, 4, 2, 64, 16, [(20, 30), (3, 12)])
+    far(c)
+    c.check()
