@@ -513,7 +513,7 @@ halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, const void*
  *     w = softmax(scale * <q, K_p>),  out = sum_p w_p V_p,  lse = log sum_p exp(scale * <q, K_p>)    per row and head.
  *   q device, n_tok rows of n_heads * head_dim every q_stride elements; q_start device int32 [n_seq + 1], not decreasing,
  *   q_start[n_seq] <= n_tok; out device [n_tok][n_heads][head_dim], must not overlap q; lse device fp32 [n_tok][n_heads] or
- *   NULL.  Rows of no sequence are neither read nor written.  keep as in halo_paged_mha.
+ *   NULL.  Rows of no sequence have no influence and are not written.  keep as in halo_paged_mha.
  *   A row that sees nothing (P < 0, a lost head, scores that are all -infinity) gives zeros and lse = -infinity.  What a row does
  *   not see has no influence on it, NaN and infinities included (which may change the order of its sums).
  *   fp32 sums and softmax; bf16 and 8-bit caches: a weight meets the values rounded to bf16 (2^-8 of itself).

@@ -80,6 +80,13 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t phase, int* abort) 
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t phase, int* abort) {
     return __all_sync(0xffffffffu, wait(bar, phase, abort));
 }
+// For a piece of work, which another role may take any time over: until it is there or another role has given up.  Who holds a piece
+// up is in a wait with a limit, so this one ends too.
+__device__ __forceinline__ bool piece_wait(uint64_t* bar, uint32_t phase, volatile int* abort) {
+    while (!__all_sync(0xffffffffu, mbar_wait_bounded(bar, phase & 1u, abort)))
+        if (__any_sync(0xffffffffu, *abort)) return false;
+    return true;
+}
 // Products issued by one lane of a warp that runs together: D[tmem] (+)= A * B, A in shared memory or (ts) in tensor memory, B in shared memory.  Descriptors by
 // their lower words (address, distance of 64-column blocks); the upper word is the same for every tile here.
 constexpr uint32_t kDescHigh = (1024u >> 4) | 1u << 14 | 2u << 29;      // eight rows 1024 bytes, descriptor version, 128-byte swizzle
@@ -204,7 +211,7 @@ struct Smem {
 template <int DP, bool EIGHT>
 __device__ __forceinline__ bool next_piece(Smem<DP, EIGHT>& sm, uint32_t& k, Piece& p) {
     const uint32_t at = k % kPieces;
-    if (!warp_wait(&sm.bars.piece_full[at], k / kPieces, &sm.bars.abort)) return false;
+    if (!piece_wait(&sm.bars.piece_full[at], k / kPieces, &sm.bars.abort)) return false;
     ++k;
     p = sm.pieces[at];
     __syncwarp();
@@ -235,7 +242,7 @@ __device__ void walk_line(const Args& a, Smem<DP, EIGHT>& sm, Walk<Cfg<DP>::kRow
             p.reach = w.reach;
         }
         const uint32_t at = k % kPieces;
-        if (!warp_wait(&sm.bars.piece_empty[at], k / kPieces + 1, &sm.bars.abort)) return;      // the phase before
+        if (!piece_wait(&sm.bars.piece_empty[at], k / kPieces + 1, &sm.bars.abort)) return;      // the phase before
         if ((threadIdx.x & 31) == 0) {
             sm.pieces[at] = p;
             mbar_arrive(&sm.bars.piece_full[at]);
