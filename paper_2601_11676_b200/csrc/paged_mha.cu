@@ -34,6 +34,8 @@
 // positions, 32 / 4 heads of 64: 6.3 us (launch, one chain of loads, a cluster's meeting), 8.5 under a table of 131072
 // positions (the line: the plan goes by the table's width); fp32, 7 sequences of up to 1500 positions, 8 / 8 heads of 64:
 // 9.3 us (the same chain, 18 MB).
+// 8-bit rows: the one of 131071 55 to 57 us (271 MB: 4.9 TB/s), the 64 sequences 63, the one of 700 6.5.  The conversions keep them off
+// HBM's rate: 436 instructions of a warp to 16 positions, two a clock and SM.
 #include <cooperative_groups.h>
 #include <math.h>
 

@@ -6,9 +6,12 @@
 //     128-byte swizzle that the tensor cores read) and an item's rows of Q: boxes of a page's rows by the copy engine, or, where
 //     pages are no whole number of eight rows, row by row; 8-bit rows row by row as codes, widened to bf16 on the way to a stage;
 //   - one thread of warp 12 issues the products: S = Q K^T into tensor memory, O += P V with P in tensor memory;
+//   - warp 13 walks along the thread block's part of the work line and tells the others the pieces;
 //   - warps 0 to 3 and 4 to 7 take a row per thread: running maximum and sum, P = 2^(S scale - maximum) as bf16 in place of S.
 // An item has 256 rows in two streams of 128: while one stream's rows are in the softmax, the other's products run.  Head sizes
 // above 128 (whose O fills half of tensor memory) and items of up to 128 rows have one stream with two S buffers instead.
+// 128 keys to a tile: with two halves of 64 in flight per stream, so that a stream's own products and softmax overlap, 8192 tokens of
+// 16 heads of 128 took 379 us and not 330, a handover costing the same for half the work.
 //
 // Weights are powers of two relative to a reference: the row's score of the first key, until a tile's weights sum to more than
 // 2^20, then its maximum so far.  O and the sum are in fp32, so weights above 1 lose nothing, O, which would have to be read,
@@ -16,6 +19,15 @@
 //
 // What a row does not see must not reach it.  Weights of 0 see to that but for values that are infinite or NaN; a row whose
 // sums come out as neither although its weights are finite is summed again, key by key (resum).
+//
+// A weight meets the values as one bf16 number: as two, the sums, half of the products, would be twice as many.  Outputs are then
+// 0.0023 (relative) from 64 bits where their own rounding alone is 0.0017.
+//
+// Measured, both kernels: 4096 tokens, 32 / 8 heads of 128, 188 to 191 us (0.73 PFLOP/s); 8192 tokens, 16 / 4 heads of 128, 320 us
+// (0.86); 512 tokens over 32000 positions in 8 bits, 32 / 8 heads, 360 us (0.75); 7 packed prompts of up to 1500 tokens, 32 / 32
+// heads, 209 to 212 us (0.43); 1 to 8 tokens for each of 16 sequences of up to 4000 positions, 32 / 8 heads, 44 us (3.3 TB/s).
+// The tensor pipe is active 34 to 42 % of the time and the unit of the powers of two as much: a tile of a stream is 1800 clocks in its
+// softmax and then 1900 until its next scores (its sums, their completion, its scores: 1300 if nothing else asked shared memory).
 #include <math.h>
 
 #include <type_traits>
@@ -418,7 +430,7 @@ struct Gather {
         cp_commit();
     }
     // Words of a stage to bf16, four loads ahead of their conversions: one behind the other, a load's and its conversion's latencies
-    // add up.
+    // add up (512 tokens over 32000 positions 496 us and not 362; all eight ahead 359).
     template <bool FAR>
     __device__ __forceinline__ void spread(uint32_t dst, uint32_t steps, int slot) {
         constexpr int kAhead = 4;
