@@ -1,7 +1,7 @@
 // halo_paged_norm_append: the keys and values of new tokens go to their pages in the caches' type or as 8-bit rows, queries
 // and keys normed per head and turned by their position on the way; halo_paged_kv_read: rows back out of the pages.
-// Every element is read once and written once.  8297 tokens, 32 + 2 * 8 heads of 128, into 8-bit rows: 59 us where HBM would
-// take (187 MB; the instructions bound it), read back in 12.7 (52 MB: 8).
+// Every element is read once and written once.  8297 tokens, 32 + 2 * 8 heads of 128, into 8-bit rows: 50 us where HBM would
+// take 28 (187 MB; the instructions bound it), read back in 11 (52 MB: 8).
 //
 //   y = x / sqrt(mean(x^2) + eps) * w over a head's elements (queries and keys that have a gain), then pair i of the first
 //   rotary elements by the angle pos * inv_freq[i], times turn_scale.  Angles as in halo_paged_kv_append: reduced to one turn in
@@ -26,7 +26,7 @@ long long paged_stride(const halo_paged_shape& s);
 
 namespace {
 
-constexpr int kThreads = 128;
+constexpr int kThreads = 64;     // each warp sees to its token's page and angles: with 128, 8297 tokens 59 us and not 50, 32 tokens 4.0 and not 3.6
 constexpr int kOwn = 8;      // elements per lane
 
 struct NormAppendArgs {
@@ -110,7 +110,7 @@ paged_norm_append_any_kernel(const __grid_constant__ NormAppendArgs a, int parts
         if (in && h < heads) x.load(h < a.H ? q + h * a.dh : h < a.H + a.Hk ? k + (h - a.H) * a.dh : v + (h - a.H - a.Hk) * a.dh);
     };
     const int first = part * kGroups + group;
-    const double freq = tid < half ? ldg_waited(a.inv_freq + tid) : 0.0;   // half <= 128 threads
+    double freq = tid < half ? ldg_waited(a.inv_freq + tid) : 0.0;
     fetch(first);
     float wq[kOwn], wk[kOwn];
     const auto gain = [&](const void* w, float (&out)[kOwn]) {
@@ -127,11 +127,12 @@ paged_norm_append_any_kernel(const __grid_constant__ NormAppendArgs a, int parts
     const int pi = pos / a.page_size;
     int page = -1;
     if (s >= 0 && s < a.n_seq && pi < a.max_pages) page = ldg_waited(a.table + static_cast<long long>(s) * a.max_pages + pi);
-    if (tid < half) {
+    for (int i = tid; i < half; i += kThreads) {
+        if (i != tid) freq = ldg_waited(a.inv_freq + i);
         const double turns = static_cast<double>(pos) * freq * 0.15915494309189533577;
         float co, si;
         sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &si, &co);
-        turn[tid] = make_float2(co * a.turn_scale, si * a.turn_scale);
+        turn[i] = make_float2(co * a.turn_scale, si * a.turn_scale);
     }
     if (page < 0 || page >= a.n_pages) {   // the same in every thread
         if (tid == 0 && part == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
@@ -256,7 +257,7 @@ paged_norm_append_kernel(const __grid_constant__ NormAppendArgs a, int parts) {
         }
     };
     const int first = part * kGroups + group;
-    const double freq = tid < half ? ldg_waited(a.inv_freq + tid) : 0.0;   // half <= 128 threads
+    double freq = tid < half ? ldg_waited(a.inv_freq + tid) : 0.0;
     fetch(first);
     for (int i = tid; i < 2 * a.dh; i += kThreads) {
         const bool key = i >= a.dh;
@@ -268,11 +269,12 @@ paged_norm_append_kernel(const __grid_constant__ NormAppendArgs a, int parts) {
     const int pi = pos / a.page_size, in_page = pos - pi * a.page_size;
     int page = -1;
     if (s >= 0 && s < a.n_seq && pi < a.max_pages) page = ldg_waited(a.table + static_cast<long long>(s) * a.max_pages + pi);
-    if (tid < half) {
+    for (int i = tid; i < half; i += kThreads) {
+        if (i != tid) freq = ldg_waited(a.inv_freq + i);
         const double turns = static_cast<double>(pos) * freq * 0.15915494309189533577;
         float co, si;
         sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &si, &co);
-        turn[tid] = make_float2(co * a.turn_scale, si * a.turn_scale);
+        turn[i] = make_float2(co * a.turn_scale, si * a.turn_scale);
     }
     if (page < 0 || page >= a.n_pages) {   // the same in every thread
         if (tid == 0 && part == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
@@ -344,7 +346,8 @@ paged_norm_append_kernel(const __grid_constant__ NormAppendArgs a, int parts) {
             uint32_t top = 0;                               // sizes of finite numbers, ordered as their bits are
 #pragma unroll
             for (int e = 0; e < kOwn; ++e)
-                top = max(top, max(__float_as_uint(f[0][e] * n) & 0x7fffffffu, __float_as_uint(f[1][e] * n) & 0x7fffffffu));
+                top = max(top, max(__float_as_uint(f[0][e]) & 0x7fffffffu, __float_as_uint(f[1][e]) & 0x7fffffffu));
+            top = __float_as_uint(__uint_as_float(top) * n) & 0x7fffffffu;      // the largest stays it: products round in order
             top = lanes_max<LANES>(top);
             if (there && !is_q) {
                 const bool sound = top < 0x7f800000u;
