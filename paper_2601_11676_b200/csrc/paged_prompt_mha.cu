@@ -17,8 +17,13 @@
 // 2^20, then its maximum so far.  O and the sum are in fp32, so weights above 1 lose nothing, O, which would have to be read,
 // multiplied and written back for every new reference, is hardly ever touched, and a tile needs no maximum.
 //
-// What a row does not see must not reach it.  Weights of 0 see to that but for values that are infinite or NaN; a row whose
-// sums come out as neither although its weights are finite is summed again, key by key (resum).
+// What a row does not see must not reach it.  Weights of 0 see to that but for values that are infinite or NaN.  Where sums come out as
+// such over tiles that a row does not see all of, the thread block takes its whole part of the line a second time, with care: such
+// values of those tiles (at most three of an item) are taken out of the stages on their way in, and rows that see them
+// get their part behind the sums (add_odd).  One NaN at the third position takes 4096 tokens of 32 / 8 heads of 128 from 185 us to 690;
+// only values of an item's last tiles are gone through key by key, so a sequence's length adds nothing.  With care in the first place (two warps
+// of their own look through those tiles) every call paid: 4096 tokens of 32 heads of 64 took 180 us and not 144, packed prompts 238
+// and not 212.
 //
 // A weight meets the values as one bf16 number: as two, the sums, half of the products, would be twice as many.  Outputs are then
 // 0.0023 (relative) from 64 bits where their own rounding alone is 0.0017.
@@ -72,16 +77,21 @@ struct Cfg {
 struct Flags {
     uint32_t there[kFlags][4];       // which of a tile's keys are there
 };
+// Tiles of an item that not every row of it sees all of: its rows see up to 255 positions more than its first one.
+constexpr int kEdge = 3;
+static_assert(kEdge <= 8, "a bit of a byte each");
 // S, P and O of a tile hand over through barriers of the lane that it is in: a stream's own in items of two streams, 0 and 2 in
 // turn in items of one.  Lanes 1 and 2 share the buffer behind 0, but not the warps that wait: 1 belongs to the second stream's,
 // 0 and 2 to the first's, so that nobody waits for a phase of a barrier without having seen the one before it.
 constexpr int kLanes = 3;
+constexpr int kPieces = 4;         // that a role can be ahead of another
 struct Bars {
     uint64_t full[8], empty[8], q_full, q_empty, s_full[kLanes], p_full[kLanes], pv_done[kLanes];
     uint64_t piece_full[4], piece_empty[4];
     uint64_t raw[4];                 // a gathering warp's own: values of which it hands on a part
+    uint64_t looked[2 * kPieces];    // with care: all values of a piece have been looked at, odd is there
     uint32_t tmem;
-    int abort;
+    int abort, again;                // again: a row's sums ask for care
 };
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t phase, int* abort) {
     if (mbar_wait_bounded(bar, phase & 1u, abort)) return true;
@@ -202,9 +212,12 @@ struct __align__(16) Piece {
     __device__ __forceinline__ int lane(int stream, int j) const { return streams == 2 ? stream : (j & 1) * 2; }
     static __device__ __forceinline__ int buffer(int lane) { return lane != 0; }
     __device__ __forceinline__ float* slot(const Args& a) const { return slot_of(a, t0); }
+    // the first of this piece's tiles that the item's first row does not see all of
+    __device__ __forceinline__ int edge(const Args& a, int rows) const {
+        return max(max(r.len - r.n + 1 + rb * rows / a.G, 0) / kTile - t0, 0);
+    }
 };
 static_assert(sizeof(Piece) == 48, "three 16-byte words");
-constexpr int kPieces = 4;         // that a role can be ahead of another
 constexpr int kReaders = 13;       // warps
 
 template <int DP, bool EIGHT>
@@ -215,6 +228,10 @@ struct Smem {
     long long q_row[Cfg<DP>::kRows];     // where the item's rows of q are, -1: none
     Flags flags;
     Piece pieces[kPieces];
+    // With care, per piece and gathering warp: bit j, an infinite or NaN value among the warp's 32 keys of tile edge + j.  A gathering warp
+    // is at most kPieces pieces ahead of who reads this, and the phases of `looked` of the pieces before are over: the walk waits for
+    // every reader before it writes over a piece.
+    alignas(4) unsigned char odd[2 * kPieces][4];
     Bars bars;
     long long sh[kThreads / 32 + 3];
 };
@@ -274,7 +291,29 @@ struct Maps {
     int box_rows, whole_q;      // 0: rows are gathered one by one (pages of odd sizes, head sizes below 64, head counts that do not divide 128)
 };
 
-template <int DP, bool EIGHT>
+// Infinite and NaN values of `rows` rows of a stage, 16 bytes of a row to a lane and eight rows 1024 bytes apart, become zeros; true: there were
+// some of this lane's.  at: of row r of the first ones; step: rows that a warp has at once.
+__device__ __forceinline__ bool purge(uint32_t at, int r, int chunk, int rows, int step) {
+    bool some = false;
+    for (; r < rows; r += step) {
+        const uint32_t word = at + r * 128 + ((chunk ^ (r & 7)) << 4);
+        uint32_t w[4], top = 0;
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(word) : "memory");
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top |= (w[e] & 0x7f807f80u) + 0x00800080u;      // an exponent of ones carries into the sign
+        if (!(top & 0x80008000u)) continue;
+        some = true;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u;
+            if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0x0000ffffu;
+        }
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(word), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    }
+    return some;
+}
+
+template <int DP, bool EIGHT, bool CARE>
 struct Gather {
     using C = Cfg<DP, EIGHT>;
     [[maybe_unused]] static constexpr int kChunks = C::kCols / 8;           // 16-byte chunks of a stage's row
@@ -284,7 +323,8 @@ struct Gather {
     Smem<DP, EIGHT>& sm;
     int* abort;
     const int warp, lane;
-    uint32_t fill = 0, cleared = 0;      // stages filled so far, and stages of values that rows were taken out of
+    uint32_t fill = 0, cleared = 0;      // stages filled so far, and stages of values that something was taken out of
+    uint32_t odd = 0;                    // this lane's part of sm.odd of the piece
     uint32_t waiting0 = 0, waiting1 = 0;      // barriers of row copies that are on their way
     int n_waiting = 0;
     bool alive = true;
@@ -334,9 +374,14 @@ struct Gather {
             if (!(there >> r & 1u)) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(place(stage, r, c)), "r"(0) : "memory");
         }
     }
+    // values of the edge-th tile that not every row sees all of
+    __device__ __forceinline__ void look(uint32_t stage, int part, int edge) {
+        const int c = lane % kChunks;
+        if (part * C::kCols + c * 8 < a.dh && purge(stage + (c >> 3) * (kTile * 128) + warp * (32 * 128), lane / kChunks, c & 7, 32, kAtOnce)) odd |= 1u << edge;
+    }
     // 128 keys x kCols columns.  page: of this lane's key, n_pages: none, which reads as zeros; pos: of the tile; there: which of
-    // this warp's rows are, the others have to be zeros.
-    __device__ __forceinline__ void stage(const CUtensorMap* map, const void* cache, int page, int pos, int kvh, int part, uint32_t there) {
+    // this warp's rows are, the others have to be zeros; edge: as in look, -1: none.
+    __device__ __forceinline__ void stage(const CUtensorMap* map, const void* cache, int page, int pos, int kvh, int part, uint32_t there, int edge) {
         const uint32_t s = fill % C::kStages, phase = fill / C::kStages;
         await(&sm.bars.empty[s], phase + 1);     // the phase before: passes at once the first time
         if (!alive) return;
@@ -347,15 +392,17 @@ struct Gather {
             const int boxes = 32 / maps.box_rows, blocks = min(C::kCols / 64, (a.dh - part * C::kCols + 63) / 64);
             const int box = lane % boxes, block = lane / boxes, row = box * maps.box_rows;
             const int from = __shfl_sync(0xffffffffu, page, row), at = first + row;
-            uint64_t* bar = there != 0xffffffffu ? &sm.bars.raw[warp] : &sm.bars.full[s];
+            const bool own = there != 0xffffffffu || edge >= 0;
+            uint64_t* bar = own ? &sm.bars.raw[warp] : &sm.bars.full[s];
             if (lane == 0) mbar_arrive_expect_tx(bar, blocks * 32 * 128);
             __syncwarp();
             if (block < blocks)
                 tma_load_4d(dst + block * (kTile * 128) + (warp * 32 + row) * 128, map, part * C::kCols + block * 64,
                             a.page_shift >= 0 ? at & (a.page_size - 1) : at % a.page_size, kvh, from, smem_u32(bar));
-            if (there != 0xffffffffu) {
+            if (own) {
                 alive = warp_wait(bar, cleared++, abort) && alive;
                 clear(dst, there);
+                if (edge >= 0) look(dst, part, edge);      // a lane has the words that it has cleared
                 signal(full);
             }
             return;
@@ -371,7 +418,15 @@ struct Gather {
             const long long from = __shfl_sync(0xffffffffu, at, r);
             if (in) cp_async16(place(dst, r, c), from >= 0 ? src + from : src, from >= 0);
         }
-        issued(full);
+        if (edge < 0) {
+            issued(full);
+            return;
+        }
+        cp_commit();
+        cp_wait<0>();
+        flush();
+        look(dst, part, edge);      // a lane has the words that it has copied
+        signal(full);
     }
     __device__ __forceinline__ void queries(const Piece& p, uint32_t piece) {
         await(&sm.bars.q_empty, piece + 1);
@@ -489,6 +544,8 @@ struct Gather {
                 return ldg_waited(a.table + static_cast<long long>(p.s) * a.max_pages + (a.page_shift >= 0 ? at >> a.page_shift : at / a.page_size));
             };
             int page = page_of(0);
+            [[maybe_unused]] const int first_edge = CARE ? p.edge(a, C::kRows) : 0;
+            odd = 0;
             // ahead of the keys where the item before is through with its own, else behind the first keys and values
             bool asked = p.n == 0;
             if (!asked && ready(&sm.bars.q_empty, piece + 1)) {
@@ -530,7 +587,9 @@ struct Gather {
                     } else {
                         cp_wait<0>();
                     }
-                    widen(byte, f & 1);
+                    const bool out = CARE && h >= C::kParts && f / kFills >= first_edge && byte == kEightNan;      // a row of NaN
+                    if (out) odd |= 1u << (f / kFills - first_edge);
+                    widen(out ? 0u : byte, f & 1);
                     if (f == kFills - 1 && !asked && alive) {
                         queries(p, piece);
                         asked = true;
@@ -547,9 +606,9 @@ struct Gather {
                 if (lane == 0) sm.flags.there[tile % kFlags][warp] = there;
                 const int from = ok ? page : a.n_pages;
 #pragma unroll
-                for (int h = 0; h < C::kParts; ++h) stage(&maps.K, a.K, from, pos, p.kvh, h, 0xffffffffu);      // scores of absent keys are masked
+                for (int h = 0; h < C::kParts; ++h) stage(&maps.K, a.K, from, pos, p.kvh, h, 0xffffffffu, -1);      // scores of absent keys are masked
 #pragma unroll
-                for (int h = 0; h < C::kParts; ++h) stage(&maps.V, a.V, from, pos, p.kvh, h, there);
+                for (int h = 0; h < C::kParts; ++h) stage(&maps.V, a.V, from, pos, p.kvh, h, there, CARE ? j - first_edge : -1);
                 if (!asked && alive) {
                     queries(p, piece);
                     asked = true;
@@ -558,6 +617,13 @@ struct Gather {
             }
             }
             if (p.n > 0) ++piece;
+            if (CARE) {
+                const uint32_t at = (k - 1) % (2 * kPieces), all = __reduce_or_sync(0xffffffffu, odd);
+                if (lane == 0) {
+                    sm.odd[at][warp] = static_cast<unsigned char>(all);
+                    mbar_arrive(&sm.bars.looked[at]);
+                }
+            }
         }
         flush();
         if (__any_sync(0xffffffffu, bad) && lane == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
@@ -742,6 +808,13 @@ struct Issue {
             if (!(C::kStreams == 2 && p.streams == 2 ? turns(p.first_tiles, p.n) : alone(p.n))) return;
             first_fill += p.n * 2 * C::kParts;
         }
+        // every stage is free again: no arrival is on its way
+        for (uint32_t f = first_fill > C::kStages ? first_fill - C::kStages : 0; f < first_fill; ++f)
+            if (!warp_wait(&bars.empty[f % C::kStages], f / C::kStages, abort)) return;
+        if (piece > 0 && !warp_wait(&bars.q_empty, piece - 1, abort)) return;
+        if (use0 > 0 && !warp_wait(&bars.pv_done[0], use0 - 1, abort)) return;
+        if (use1 > 0 && !warp_wait(&bars.pv_done[1], use1 - 1, abort)) return;
+        if (use2 > 0) warp_wait(&bars.pv_done[2], use2 - 1, abort);
     }
 };
 
@@ -790,36 +863,49 @@ __device__ __forceinline__ float cache_at(const Args& a, const void* cache, cons
     return f[0] * eight_unit(scale[static_cast<long long>(page) * a.Hk * a.page_size + row]);
 }
 
-// A row's weighted sum of values over the positions p0 to p1 - 1 of sequence s, key by key: a lane has a key for its score, and columns
-// lane, lane + 32, ... for the sums.  By a whole warp; to: fp32, every `step` floats four columns, or bf16 (step 0) times f.
-__device__ __forceinline__ void resum(const Args& a, int s, int kvh, int token, int head, int p0, int p1, float base, float f, void* to, long long step) {
+// Infinite and NaN values of a piece's last tiles, which the gathering warps have taken out: their parts are added to O in tensor memory where a
+// row sees them.  By a whole warp, a row per lane, which sees `own` positions (0: no row); bounded by kEdge tiles.  k: number of the piece; n:
+// tiles of the row's stream.
+template <int DP, bool EIGHT>
+__device__ __forceinline__ bool add_odd(const Args& a, Smem<DP, EIGHT>& sm, const Piece& p, uint32_t k, int n, int token, int head, int own, float base,
+                                     uint32_t o_addr) {
+    const uint32_t slot = k % (2 * kPieces);
+    if (!warp_wait(&sm.bars.looked[slot], k / (2 * kPieces), &sm.bars.abort)) return false;
+    const int edge = p.edge(a, Cfg<DP>::kRows);
+    const uint32_t odd = *reinterpret_cast<const volatile uint32_t*>(sm.odd[slot]);
+    if (odd == 0) return true;
     const int lane = threadIdx.x & 31;
     const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + static_cast<long long>(token) * a.q_stride + static_cast<long long>(head) * a.dh;
-    float o[8] = {};
-    for (int p = p0; p < p1; p += 32) {
-        const int at = p + lane, pi = at / a.page_size, in_page = at - pi * a.page_size;
-        int page = at < p1 ? ldg_waited(a.table + static_cast<long long>(s) * a.max_pages + pi) : -1;
-        if (page < 0 || page >= a.n_pages) page = -1;
+    for (int at = edge * kTile; at < n * kTile; ++at) {
+        const int j = at / kTile, of = at % kTile, pos = p.t0 * kTile + at;
+        if (!(odd >> (of / 32 * 8 + j - edge) & 1u) || pos >= p.reach) continue;
+        const int pi = pos / a.page_size, in_page = pos - pi * a.page_size;
+        const int page = ldg_waited(a.table + static_cast<long long>(p.s) * a.max_pages + pi);
+        if (page < 0 || page >= a.n_pages) continue;
+        bool here = false;
+        for (int c = lane; c < a.dh; c += 32) here |= !(fabsf(cache_at(a, a.V, a.V_scale, page, p.kvh, in_page, c)) < INFINITY);
+        const bool sees = pos < own;
+        if (!__any_sync(0xffffffffu, here) || !__any_sync(0xffffffffu, sees)) continue;
         float score = 0.0f;
-        if (page >= 0)
-            for (int c = 0; c < a.dh; ++c) score = fmaf(__bfloat162float(q[c]), cache_at(a, a.K, a.K_scale, page, kvh, in_page, c), score);
-        const float w = page >= 0 ? __bfloat162float(__float2bfloat16_rn(pow2(fmaf(score, a.scale_log2, -base)))) : 0.0f;
-        for (int k = 0; k < 32; ++k) {
-            const int from = __shfl_sync(0xffffffffu, page, k), in = __shfl_sync(0xffffffffu, in_page, k);
-            const float x = __shfl_sync(0xffffffffu, w, k);
-            if (from < 0) continue;
+        if (sees)
+            for (int c = 0; c < a.dh; ++c) score = fmaf(__bfloat162float(q[c]), cache_at(a, a.K, a.K_scale, page, p.kvh, in_page, c), score);
+        const float w = __bfloat162float(__float2bfloat16_rn(pow2(fmaf(score, a.scale_log2, -base))));
+        for (int c = 0; c < a.dh; c += 16) {
+            uint32_t o[16];
+            __syncwarp();
+            tmem_ld_32x16(o_addr + c, o);
+            tmem_ld_wait_for(o);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (lane + e * 32 < a.dh) o[e] = fmaf(x, cache_at(a, a.V, a.V_scale, from, kvh, in, lane + e * 32), o[e]);
+            for (int e = 0; e < 16; ++e) {
+                const float v = cache_at(a, a.V, a.V_scale, page, p.kvh, in_page, c + e);
+                if (sees && !(fabsf(v) < INFINITY)) o[e] = __float_as_uint(fmaf(w, v, __uint_as_float(o[e])));
+            }
+            __syncwarp();
+            tmem_st_32x16(o_addr + c, o);
+            tmem_st_wait();
         }
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int c = lane + e * 32;
-        if (c >= a.dh) continue;
-        if (step) static_cast<float*>(to)[c / 4 * step + c % 4] = o[e];
-        else static_cast<__nv_bfloat16*>(to)[c] = __float2bfloat16_rn(o[e] * f);
-    }
+    return true;
 }
 
 // Four lanes with four 16-byte words each, of the rows l, to a word each of four rows: 2 x 2 blocks, then halves of them.  Stores of
@@ -842,8 +928,8 @@ __device__ __forceinline__ void turn_words(uint4 (&w)[4], int lane) {
     }
 }
 
-template <int DP, bool EIGHT>
-__device__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm) {
+template <int DP, bool EIGHT, bool CARE>
+__device__ __forceinline__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm) {
     using C = Cfg<DP>;
     constexpr float kSlack = 8.0f;            // powers of two that a reference may lag behind where it is looked at
     constexpr float kSum = 1048576.0f;        // what a tile's weights may sum to before it is
@@ -980,15 +1066,15 @@ __device__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm) {
                 if (lane == 0) mbar_arrive(&bars.p_full[b]);
             }
             if (n > 0 && alive) await_sums(n - 1);
+            if (CARE && alive)
+                alive = add_odd<DP, EIGHT>(a, sm, p, k - 1, n, row.token, row.head, row.there ? row.sees : 0, m == -INFINITY ? 0.0f : m * scale, o_addr);
             if (!alive) break;
             const bool some = l != 0.0f && row.kept;
             const long long at = static_cast<long long>(row.token) * a.H + row.head;
-            const float f = some ? 1.0f / l : 0.0f, base = m == -INFINITY ? 0.0f : m * scale;
-            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + at * a.dh;
+            const float f = some ? 1.0f / l : 0.0f;
             float* slot = p.slot(a) + 2ll * a.rows + static_cast<long long>(item_row) * 4;
-            const bool complete = p.complete;
-            bool odd = false;
-            if (complete) {
+            Pair zeros = 0;      // the sums times 0: NaN where one is infinite or NaN
+            if (p.complete) {
                 const long long mine = row.there ? at * a.dh : -1;
                 long long rows[4];      // of the four lanes' rows of the output
 #pragma unroll
@@ -1008,7 +1094,7 @@ __device__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const float x = __uint_as_float(o[q >> 1][(q & 1) * 8 + 2 * e]), z = __uint_as_float(o[q >> 1][(q & 1) * 8 + 2 * e + 1]);
-                            odd |= !(fabsf(x) < INFINITY) || !(fabsf(z) < INFINITY);
+                            zeros = fma2(pair_of(x, z), 0, zeros);
                             v[e] = some ? pack_bf16(x * f, z * f) : 0u;
                         }
                         y[q] = make_uint4(v[0], v[1], v[2], v[3]);
@@ -1032,7 +1118,7 @@ __device__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm) {
                         tmem_ld_wait_for(o);
                     }
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) odd |= !(fabsf(__uint_as_float(o[e])) < INFINITY);
+                    for (int e = 0; e < 16; e += 2) zeros = fma2(pair_of(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), 0, zeros);
                     if (row.there) {
 #pragma unroll
                         for (int q = 0; q < 4; ++q)
@@ -1040,80 +1126,94 @@ __device__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm) {
                     }
                 }
             }
-            // a value that is infinite or NaN, in a tile that the row does not see all of: what it does see, on its own
-            uint32_t again = __ballot_sync(0xffffffffu, odd && some && fabsf(l) < INFINITY && (p.t0 + n) * kTile > all_see);
-            while (again) {
-                const int q = __ffs(again) - 1;
-                again &= again - 1;
-                const int p1 = min((p.t0 + n) * kTile, row.sees);
-                const unsigned long long to = reinterpret_cast<unsigned long long>(complete ? static_cast<void*>(out) : static_cast<void*>(slot));
-                resum(a, p.s, p.kvh, __shfl_sync(0xffffffffu, row.token, q), __shfl_sync(0xffffffffu, row.head, q), p.t0 * kTile,
-                      __shfl_sync(0xffffffffu, p1, q), __shfl_sync(0xffffffffu, base, q), __shfl_sync(0xffffffffu, f, q),
-                      reinterpret_cast<void*>(__shfl_sync(0xffffffffu, to, q)), complete ? 0 : 4ll * a.rows);
-                __syncwarp();
-            }
+            // a value that is infinite or NaN, and a tile that the row does not see all of
+            const float2 z = both(zeros);
+            if (!CARE && z.x + z.y != 0.0f && some && fabsf(l) < INFINITY && (p.t0 + n) * kTile > all_see) *const_cast<volatile int*>(&bars.again) = 1;
         }
         tile += p.n;
     }
 }
 
 template <int DP, bool EIGHT>
-__global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
+__device__ __forceinline__ void init_barriers(Bars& bars) {
+    for (int i = 0; i < Cfg<DP, EIGHT>::kStages; ++i) {
+        mbar_init(&bars.full[i], 4);      // the gathering warps
+        mbar_init(&bars.empty[i], 1);
+    }
+    mbar_init(&bars.q_full, 4);
+    mbar_init(&bars.q_empty, 1);
+    for (int b = 0; b < kLanes; ++b) {
+        mbar_init(&bars.s_full[b], 2);    // the products, and the thread that issues them
+        mbar_init(&bars.p_full[b], 4);    // a stream's warps
+        mbar_init(&bars.pv_done[b], 1);
+    }
+    for (int i = 0; i < 4; ++i) mbar_init(&bars.raw[i], 1);
+    for (int i = 0; i < 2 * kPieces; ++i) mbar_init(&bars.looked[i], 4);
+    for (int i = 0; i < kPieces; ++i) {
+        mbar_init(&bars.piece_full[i], 1);
+        mbar_init(&bars.piece_empty[i], kReaders);
+    }
+    bars.again = 0;
+    mbar_fence_init();
+}
+// The thread block's part of the line, by all its threads; the first time they share registers out anew.
+template <int DP, bool EIGHT, bool CARE>
+__device__ __forceinline__ void take_part(const Args& a, const Maps& maps, Smem<DP, EIGHT>& sm) {
     using C = Cfg<DP, EIGHT>;
-    extern __shared__ __align__(1024) unsigned char raw[];
-    Smem<DP, EIGHT>& sm = *reinterpret_cast<Smem<DP, EIGHT>*>(raw);
-    Bars& bars = sm.bars;
-    const int tid = threadIdx.x, warp = tid >> 5;
-    chain_wait();
-    if (tid == 0) {
-        for (int i = 0; i < C::kStages; ++i) {
-            mbar_init(&bars.full[i], 4);      // the gathering warps
-            mbar_init(&bars.empty[i], 1);
-        }
-        mbar_init(&bars.q_full, 4);
-        mbar_init(&bars.q_empty, 1);
-        for (int b = 0; b < kLanes; ++b) {
-            mbar_init(&bars.s_full[b], 2);    // the products, and the thread that issues them
-            mbar_init(&bars.p_full[b], 4);    // a stream's warps
-            mbar_init(&bars.pv_done[b], 1);
-        }
-        for (int i = 0; i < 4; ++i) mbar_init(&bars.raw[i], 1);
-        for (int i = 0; i < kPieces; ++i) {
-            mbar_init(&bars.piece_full[i], 1);
-            mbar_init(&bars.piece_empty[i], kReaders);
-        }
-        bars.abort = 0;
-        mbar_fence_init();
-    }
-    if (warp == 12) {
-        tmem_alloc(&bars.tmem, 512);
-        tmem_relinquish_alloc_permit();
-    }
-    tcgen05_fence_before_sync();
+    const int warp = threadIdx.x >> 5;
     const Found<C::kRows, kTile, kOver> f = locate<C::kRows, kTile, kOver, kThreads>(a, sm.sh);      // threads meet in it
     tcgen05_fence_after_sync();
-    if (f.walk.left <= 0) {      // the same in every thread
-        if (warp == 12) tmem_dealloc(bars.tmem, 512);
-        return;
-    }
+    if (f.walk.left <= 0) return;      // the same in every thread
     if (warp < 8) {
-        more_registers<kRowRegs>();
-        softmax_rows<DP, EIGHT>(a, sm);
+        if (!CARE) more_registers<kRowRegs>();
+        softmax_rows<DP, EIGHT, CARE>(a, sm);
     } else if (warp < 12) {
-        fewer_registers<kCopyRegs>();
-        Gather<DP, EIGHT>(a, maps, sm).run();
+        if (!CARE) fewer_registers<kCopyRegs>();
+        Gather<DP, EIGHT, CARE>(a, maps, sm).run();
     } else {
-        fewer_registers<kIssueRegs>();
+        if (!CARE) fewer_registers<kIssueRegs>();
         if (warp == 12) Issue<DP, EIGHT>(a, sm).run();
         if (warp == 13) walk_line<DP, EIGHT>(a, sm, f.walk, f.total);
     }
     __syncwarp();
     tcgen05_fence_before_sync();
     __syncthreads();
-    if (warp == 12) {
-        tcgen05_fence_after_sync();
-        tmem_dealloc(bars.tmem, 512);
+    tcgen05_fence_after_sync();
+}
+// A second time, with the registers of the launch.  A function of its own, so that none of it is in the first time's way.
+template <int DP, bool EIGHT>
+__device__ __noinline__ void take_part_with_care(const Args& a, const Maps& maps, Smem<DP, EIGHT>& sm) {
+    if (threadIdx.x == 0) {
+        for (uint64_t* b = reinterpret_cast<uint64_t*>(&sm.bars); b < reinterpret_cast<uint64_t*>(&sm.bars.tmem); ++b) mbar_inval(b);
+        init_barriers<DP, EIGHT>(sm.bars);
     }
+    take_part<DP, EIGHT, true>(a, maps, sm);
+}
+
+template <int DP, bool EIGHT>
+__global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
+    extern __shared__ __align__(1024) unsigned char raw[];
+    Smem<DP, EIGHT>& sm = *reinterpret_cast<Smem<DP, EIGHT>*>(raw);
+    Bars& bars = sm.bars;
+    const int tid = threadIdx.x, warp = tid >> 5;
+    chain_wait();
+    if (tid == 0) {
+        init_barriers<DP, EIGHT>(bars);
+        bars.abort = 0;
+    }
+    if (warp == 12) {
+        tmem_alloc(&bars.tmem, 512);
+        tmem_relinquish_alloc_permit();
+    }
+    tcgen05_fence_before_sync();
+    take_part<DP, EIGHT, false>(a, maps, sm);
+    if (bars.again && !bars.abort) {      // the same in every thread
+        if (warp < 8) fewer_registers<128>();
+        __syncthreads();
+        if (warp >= 8) more_registers<128>();
+        take_part_with_care<DP, EIGHT>(a, maps, sm);
+    }
+    if (warp == 12) tmem_dealloc(bars.tmem, 512);
     if (tid == 0 && bars.abort) flag_status(a.status, HALO_DEV_TIMEOUT);
 }
 
@@ -1162,6 +1262,7 @@ halo_status launch(const Args& args, const halo_paged_shape& sh, void* ws, cudaS
         }
         const auto run = [&](auto eight) -> halo_status {
             constexpr bool E = decltype(eight)::value;
+            static_assert(sizeof(Smem<DP, E>) <= 227 * 1024, "shared memory of a thread block");
             static bool done[64];
             if (!ensure_dynamic_smem(paged_prompt_mha_kernel<DP, E>, sizeof(Smem<DP, E>), done)) return HALO_ERR_CUDA;
             return launch_chained(paged_prompt_mha_kernel<DP, E>, a.blocks, kThreads, sizeof(Smem<DP, E>), st, a, maps);

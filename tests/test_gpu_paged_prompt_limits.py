@@ -1,0 +1,51 @@
+"""halo_paged_prompt_mha and halo_paged_mha_f8 where contents are extreme: values that are infinite or NaN over long sequences and in all of
+an item's last tiles.  Against the definition in 64 bits, with the bounds of test_gpu_paged_prompt and test_gpu_eight_bit_cache."""
+import pytest
+import torch
+
+from tests.test_gpu_paged_prompt import DEV, INF, KINDS, NAN, Case, gen
+
+pytestmark = pytest.mark.gpu
+
+
+def spoil(c, s, p, col, what, heads=slice(None)):
+    """An infinite or NaN value at position p of sequence s; of an 8-bit cache the whole row is NaN."""
+    page, at = c.table[s, p // c.K.shape[2]].long(), p % c.K.shape[2]
+    if c.kind == "8bit":
+        c.Vs[page, heads, at], c.Vv[page, heads, at] = 255, NAN
+    else:
+        c.V[page, heads, at, col] = what
+        c.Vv[page, heads, at, col] = what
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dh", [64, 128])
+def test_values_that_are_not_finite_over_a_long_sequence(kind, dh):
+    """One that every row sees, far in front, and one that some of the last tile's rows see; the sequence behind is untouched by both, and
+    nothing runs out of time."""
+    c = Case(kind, 4, 2, dh, 16, [(200, 40000), (150, 60)])
+    spoil(c, 0, 5, 3, NAN, 0)
+    spoil(c, 0, 40120, 7, INF, 1)
+    out, lse, bad = c.run()
+    assert bad == 0
+    c.compare(out, lse)
+    assert torch.isfinite(out[200:350]).all() and torch.isnan(out[:200, :2, 3]).all() and torch.isfinite(out[:120, 2:]).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("H,Hk,dh,page", [(2, 2, 64, 16), (2, 2, 128, 16), (2, 2, 256, 64), (2, 2, 144, 32), (8, 2, 128, 5), (5, 1, 80, 48), (12, 1, 64, 24)])
+@pytest.mark.parametrize("chunks", [[(256, 300), (300, 5), (130, 0)], [(255, 129), (1, 400), (40, 990)]])
+def test_last_tiles_full_of_values_that_are_not_finite(kind, H, Hk, dh, page, chunks):
+    """Every row sees another part of them, in up to three tiles of an item, whole and cut."""
+    c = Case(kind, H, Hk, dh, page, chunks)
+    g = gen(11)
+    kinds = [INF, -INF, NAN]
+    for s, (new, past) in enumerate(chunks):
+        for p in range(past + 1, past + new, 9):
+            pick = torch.randint(0, 1 << 20, (3,), generator=g, device=DEV).tolist()
+            spoil(c, s, p, pick[0] % dh, kinds[pick[1] % 3], pick[2] % Hk)
+    out, lse, bad = c.run()
+    assert bad == 0
+    c.compare(out, lse)
+    first = c.start[:-1].long()
+    assert torch.isfinite(out[first]).all()
