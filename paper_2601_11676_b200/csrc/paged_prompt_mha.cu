@@ -89,6 +89,7 @@ struct Bars {
     uint64_t full[8], empty[8], q_full, q_empty, s_full[kLanes], p_full[kLanes], pv_done[kLanes];
     uint64_t piece_full[4], piece_empty[4];
     uint64_t raw[4];                 // a gathering warp's own: values of which it hands on a part
+    uint64_t drained;                // products that were issued before a wait ran out
     uint64_t looked[2 * kPieces];    // with care: all values of a piece have been looked at, odd is there
     uint32_t tmem;
     int abort, again;                // again: a row's sums ask for care
@@ -325,6 +326,7 @@ struct Gather {
     const int warp, lane;
     uint32_t fill = 0, cleared = 0;      // stages filled so far, and stages of values that something was taken out of
     uint32_t odd = 0;                    // this lane's part of sm.odd of the piece
+    uint32_t piece_asked = 0;            // pieces whose rows of q were asked for
     uint32_t waiting0 = 0, waiting1 = 0;      // barriers of row copies that are on their way
     int n_waiting = 0;
     bool alive = true;
@@ -431,6 +433,7 @@ struct Gather {
     __device__ __forceinline__ void queries(const Piece& p, uint32_t piece) {
         await(&sm.bars.q_empty, piece + 1);
         if (!alive) return;
+        ++piece_asked;
         const uint32_t q = smem_u32(sm.q), full = smem_u32(&sm.bars.q_full);
         if (maps.whole_q) {      // tokens behind the sequence's last come along, and go nowhere
             const int blocks = (a.dh + 63) / 64, boxes = p.streams * blocks, mine = (boxes - warp + 3) / 4;
@@ -626,6 +629,12 @@ struct Gather {
             }
         }
         flush();
+        cp_wait<0>();
+        if (lane == 0) {     // for land()
+            sm.sh[warp] = fill;
+            sm.sh[4 + warp] = piece_asked;
+            sm.sh[8 + warp] = cleared;
+        }
         if (__any_sync(0xffffffffu, bad) && lane == 0) flag_status(a.status, HALO_DEV_BAD_INDEX);
     }
 };
@@ -801,20 +810,29 @@ struct Issue {
         return true;
     }
     __device__ void run() {
+        if (all()) return;
+        int never = 0;       // products that are on their way read shared memory and write tensor memory
+        commit(lead, &bars.drained);
+        mbar_wait_bounded(&bars.drained, 0, &never);
+        __syncwarp();
+    }
+    __device__ __forceinline__ bool all() {
         uint32_t piece = 0, k = 0;
         for (Piece p; next_piece(sm, k, p);) {
             if (p.n == 0) continue;
-            if (!warp_wait(&bars.q_full, piece++, abort)) return;
-            if (!(C::kStreams == 2 && p.streams == 2 ? turns(p.first_tiles, p.n) : alone(p.n))) return;
+            if (!warp_wait(&bars.q_full, piece++, abort)) return false;
+            if (!(C::kStreams == 2 && p.streams == 2 ? turns(p.first_tiles, p.n) : alone(p.n))) return false;
             first_fill += p.n * 2 * C::kParts;
         }
         // every stage is free again: no arrival is on its way
-        for (uint32_t f = first_fill > C::kStages ? first_fill - C::kStages : 0; f < first_fill; ++f)
-            if (!warp_wait(&bars.empty[f % C::kStages], f / C::kStages, abort)) return;
-        if (piece > 0 && !warp_wait(&bars.q_empty, piece - 1, abort)) return;
-        if (use0 > 0 && !warp_wait(&bars.pv_done[0], use0 - 1, abort)) return;
-        if (use1 > 0 && !warp_wait(&bars.pv_done[1], use1 - 1, abort)) return;
-        if (use2 > 0) warp_wait(&bars.pv_done[2], use2 - 1, abort);
+        bool ok = !*reinterpret_cast<volatile int*>(abort);      // next_piece may have given up
+        for (uint32_t f = first_fill > C::kStages ? first_fill - C::kStages : 0; ok && f < first_fill; ++f)
+            ok = warp_wait(&bars.empty[f % C::kStages], f / C::kStages, abort);
+        if (ok && piece > 0) ok = warp_wait(&bars.q_empty, piece - 1, abort);
+        if (ok && use0 > 0) ok = warp_wait(&bars.pv_done[0], use0 - 1, abort);
+        if (ok && use1 > 0) ok = warp_wait(&bars.pv_done[1], use1 - 1, abort);
+        if (ok && use2 > 0) ok = warp_wait(&bars.pv_done[2], use2 - 1, abort);
+        return __all_sync(0xffffffffu, ok);
     }
 };
 
@@ -1148,6 +1166,7 @@ __device__ __forceinline__ void init_barriers(Bars& bars) {
         mbar_init(&bars.pv_done[b], 1);
     }
     for (int i = 0; i < 4; ++i) mbar_init(&bars.raw[i], 1);
+    mbar_init(&bars.drained, 1);
     for (int i = 0; i < 2 * kPieces; ++i) mbar_init(&bars.looked[i], 4);
     for (int i = 0; i < kPieces; ++i) {
         mbar_init(&bars.piece_full[i], 1);
@@ -1179,6 +1198,28 @@ __device__ __forceinline__ void take_part(const Args& a, const Maps& maps, Smem<
     tcgen05_fence_before_sync();
     __syncthreads();
     tcgen05_fence_after_sync();
+}
+// Behind a wait that ran out: every copy that the gathering warps have asked for lands before the thread block goes away.  Warps got to different
+// stages; who lags arrives at the others' without copies, so that their phases end.  No warp lags a whole ring.
+template <int DP, bool EIGHT>
+__device__ __noinline__ void land(Smem<DP, EIGHT>& sm) {
+    constexpr uint32_t S = Cfg<DP, EIGHT>::kStages;
+    const int warp = static_cast<int>(threadIdx.x >> 5) - 8;
+    if (warp >= 0 && warp < 4 && (threadIdx.x & 31) == 0) {
+        uint32_t fills = 0, asked = 0;
+        for (int w = 0; w < 4; ++w) {
+            fills = max(fills, static_cast<uint32_t>(sm.sh[w]));
+            asked = max(asked, static_cast<uint32_t>(sm.sh[4 + w]));
+        }
+        const uint32_t cleared = static_cast<uint32_t>(sm.sh[8 + warp]);
+        int never = 0;
+        for (uint32_t f = static_cast<uint32_t>(sm.sh[warp]); f < fills; ++f) mbar_arrive(&sm.bars.full[f % S]);
+        for (uint32_t p = static_cast<uint32_t>(sm.sh[4 + warp]); p < asked; ++p) mbar_arrive(&sm.bars.q_full);
+        if (cleared > 0) mbar_wait_bounded(&sm.bars.raw[warp], (cleared - 1) & 1u, &never);
+        for (uint32_t f = fills > S ? fills - S : 0; f < fills; ++f) mbar_wait_bounded(&sm.bars.full[f % S], f / S & 1u, &never);
+        if (asked > 0) mbar_wait_bounded(&sm.bars.q_full, (asked - 1) & 1u, &never);
+    }
+    __syncthreads();
 }
 // A second time, with the registers of the launch.  A function of its own, so that none of it is in the first time's way.
 template <int DP, bool EIGHT>
@@ -1213,6 +1254,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prompt_mha_kernel(const __g
         if (warp >= 8) more_registers<128>();
         take_part_with_care<DP, EIGHT>(a, maps, sm);
     }
+    if (bars.abort) land<DP, EIGHT>(sm);
     if (warp == 12) tmem_dealloc(bars.tmem, 512);
     if (tid == 0 && bars.abort) flag_status(a.status, HALO_DEV_TIMEOUT);
 }
