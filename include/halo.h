@@ -516,7 +516,8 @@ halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, const void*
  *   NULL.  Rows of no sequence have no influence and are not written.  keep as in halo_paged_mha.
  *   A row that sees nothing (P < 0, a lost head, scores that are all -infinity) gives zeros and lse = -infinity.  What a row does
  *   not see has no influence on it, NaN and infinities included (which may change the order of its sums).
- *   fp32 sums and softmax; bf16 and 8-bit caches: a weight meets the values rounded to bf16 (2^-8 of itself).
+ *   fp32 sums and softmax; bf16 and 8-bit caches: a weight meets the values rounded to bf16 (2^-8 of itself), and sums are scaled so that
+ *   finite values do not overflow in them (values below 2^-60 in size may be lost).
  *   A sequence whose rows are out of range or decrease is left out, one whose length is negative or behind the table
  *   counts as empty, positions on a page out of range are left out; each sets HALO_DEV_BAD_INDEX.
  *   workspace: halo_paged_prompt_mha_workspace_bytes(shape, n_tok, n_seq) bytes, as for halo_paged_mha.  The result does not depend

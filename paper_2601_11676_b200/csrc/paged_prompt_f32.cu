@@ -256,6 +256,8 @@ halo_status f32_launch(const Args& args, const halo_paged_shape& sh, void* works
         a.blocks = blocks_of<DP>(sh, a.n_tok, a.n_seq);
         a.rows = slot_rows(kRows, a.n_tok, sh);
         a.slot = slot_floats(a.rows, a.dh);
+        a.lower = 0.0f;
+        a.raise = 1.0f;
         a.openings = static_cast<Opening*>(workspace);
         a.ws = reinterpret_cast<float*>(a.openings + a.blocks);
         const halo_status rc = launch_chained(paged_prompt_rows_kernel<DP>, a.blocks, kThreads, sizeof(Smem<DP>), st, a);

@@ -14,8 +14,10 @@
 // 16 heads of 128 took 379 us and not 330, a handover costing the same for half the work.
 //
 // Weights are powers of two relative to a reference: the row's score of the first key, until a tile's weights sum to more than
-// 2^20, then its maximum so far.  O and the sum are in fp32, so weights above 1 lose nothing, O, which would have to be read,
-// multiplied and written back for every new reference, is hardly ever touched, and a tile needs no maximum.
+// 2^20, then its maximum so far.  So O, which would have to be read, multiplied and written back for every new reference, is hardly
+// ever touched, and a tile needs no maximum.  All weights are 2^-lower of that (Args), which costs nothing, as it joins the
+// reference: 2^20 for each of the most tiles that the table holds, so that a row's weights never sum to more than 1/2 and O overflows for no
+// finite values.  What a weight times a value then leaves below 2^-126 can be lost: 2^-80 of the output's own scale at most.
 //
 // What a row does not see must not reach it.  Weights of 0 see to that but for values that are infinite or NaN.  Where sums come out as
 // such over tiles that a row does not see all of, the thread block takes its whole part of the line a second time, with care: such
@@ -54,6 +56,7 @@ constexpr int kThreads = 512;
 // An item's rows, first scores and outputs cost 6000 to 9000 clocks, a tile 4500 (thread blocks of many short items against ones of
 // two long items).  With 1 here, 4096 tokens of 32 heads of 64 took 165 us and not 151; with 4, of heads of 128 197 and not 192.
 constexpr int kOver = 2;
+constexpr float kSum = 1048576.0f;      // 2^20: a tile's weights relative to the reference, together
 constexpr int kFlags = 8;          // tiles whose flags are kept
 
 // DP: head size padded to 64, 128 or 256.  EIGHT: 8-bit rows.
@@ -950,7 +953,7 @@ template <int DP, bool EIGHT, bool CARE>
 __device__ __forceinline__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm) {
     using C = Cfg<DP>;
     constexpr float kSlack = 8.0f;            // powers of two that a reference may lag behind where it is looked at
-    constexpr float kSum = 1048576.0f;        // what a tile's weights may sum to before it is
+    const float most_sum = kSum * exp2f(-a.lower);      // what a tile's weights may sum to before it is
     Bars& bars = sm.bars;
     int* abort = &bars.abort;
     const int t = threadIdx.x >> 7, i = threadIdx.x & 127, lane = threadIdx.x & 31, item_row = t * 128 + i;
@@ -1007,7 +1010,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm)
                     }
                 };
                 const auto weights = [&](auto mask) {
-                    const Pair times = twice(scale), minus = twice(m == -INFINITY ? 0.0f : -m * scale);
+                    const Pair times = twice(scale), minus = twice(fmaf(m == -INFINITY ? 0.0f : -m, scale, -a.lower));
                     Pair sum[2] = {0, 0};
                     each(mask, [&](int c, const uint32_t (&sc)[32], bool none) {
                         if (decltype(mask)::value && none) {
@@ -1032,10 +1035,10 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm)
                     const float first_score = __uint_as_float(tmem_ld_word(s_addr));
                     if (row.sees > p0 && (there[0] & 1u) && fabsf(first_score) < INFINITY) m = first_score;
                 }
-                float more = INFINITY;
-                if (__all_sync(0xffffffffu, m > -INFINITY || row.sees <= p0)) more = masked ? weights(Const<1>()) : weights(Const<0>());
-                if (__any_sync(0xffffffffu, !(more < kSum))) {
-                    // a new reference, or something infinite or NaN: from the scores again
+                float more = masked ? weights(Const<1>()) : weights(Const<0>());
+                // a new reference, or something infinite or NaN: from the scores again.  A row moves by what it sees alone, not by its neighbours.
+                const bool anew = !(more < most_sum) || !(m > -INFINITY || row.sees <= p0);
+                if (__any_sync(0xffffffffu, anew)) {
                     float mx = -INFINITY;
                     each(Const<1>(), [&](int, const uint32_t (&sc)[32], bool none) {
                         if (none) return;
@@ -1050,8 +1053,9 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm)
                         for (int q = 0; q < 4; ++q) most[q] = max2(most[q], __uint_as_float(sc[28 + q]));
                         mx = max3(max3(most[0], most[1], most[2]), most[3], mx);
                     });
-                    if (__any_sync(0xffffffffu, (mx - m) * scale > kSlack)) {      // not where it is NaN: all weights of the row are
-                        const float to = fmaxf(m, mx), f = m == -INFINITY ? 0.0f : pow2((m - to) * scale);
+                    const bool moves = anew && (mx - m) * scale > kSlack;      // not where it is NaN: all weights of the row are
+                    if (__any_sync(0xffffffffu, moves)) {
+                        const float to = moves ? fmaxf(m, mx) : m, f = !moves ? 1.0f : m == -INFINITY ? 0.0f : pow2((m - to) * scale);
                         if (j > 0) {
                             await_sums(j - 1);
                             if (!alive) break;
@@ -1085,7 +1089,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm)
             }
             if (n > 0 && alive) await_sums(n - 1);
             if (CARE && alive)
-                alive = add_odd<DP, EIGHT>(a, sm, p, k - 1, n, row.token, row.head, row.there ? row.sees : 0, m == -INFINITY ? 0.0f : m * scale, o_addr);
+                alive = add_odd<DP, EIGHT>(a, sm, p, k - 1, n, row.token, row.head, row.there ? row.sees : 0, (m == -INFINITY ? 0.0f : m * scale) + a.lower, o_addr);
             if (!alive) break;
             const bool some = l != 0.0f && row.kept;
             const long long at = static_cast<long long>(row.token) * a.H + row.head;
@@ -1123,7 +1127,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm)
                     for (int q = 0; q < 4; ++q)
                         if (rows[q] >= 0 && col < a.dh) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + rows[q] + col) = y[q];
                 }
-                if (row.there && a.lse) a.lse[at] = some ? (m * scale + log2f(l)) * kLn2 : -INFINITY;
+                if (row.there && a.lse) a.lse[at] = some ? fmaf(m, scale, log2f(l * a.raise)) * kLn2 : -INFINITY;
             } else {
                 if (row.there) {
                     p.slot(a)[item_row] = m * scale;
@@ -1285,6 +1289,11 @@ halo_status launch(const Args& args, const halo_paged_shape& sh, void* ws, cudaS
         a.slot = slot_floats(a.rows, a.dh);
         a.openings = static_cast<Opening*>(ws);
         a.ws = reinterpret_cast<float*>(a.openings + a.blocks);
+        const long long tiles = (static_cast<long long>(sh.max_pages) * sh.page_size + kTile - 1) / kTile;
+        int lower = 21;
+        while (1ll << (lower - 21) < tiles) ++lower;
+        a.lower = static_cast<float>(lower);
+        a.raise = ldexpf(1.0f, lower);
         Maps maps = {};
         const uint64_t wide = sh.head_dim, row = wide * 2;
         const int page_bits = sh.page_size & -sh.page_size;

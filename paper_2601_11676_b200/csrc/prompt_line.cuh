@@ -31,6 +31,7 @@ struct Args {
     long long slot;          // floats of it
     long long page_stride, q_stride;
     float scale_log2;
+    float lower, raise;      // weights are times 2^-lower; 2^lower
     const void* q;
     const void* K;
     const void* V;
@@ -344,7 +345,7 @@ __global__ void __launch_bounds__(256) paged_prompt_join_kernel(const __grid_con
     for (int e = 0; e < 8; ++e) y[e] = from_float<Io>(some ? v[e] * n : 0.0f);
 #pragma unroll
     for (int e = 0; e < static_cast<int>(sizeof(Io) / 2); ++e) reinterpret_cast<uint4*>(out)[e] = reinterpret_cast<const uint4*>(y)[e];
-    if (c4 == 0 && a.lse) a.lse[at] = some ? (M + log2f(L)) * kLn2 : -INFINITY;
+    if (c4 == 0 && a.lse) a.lse[at] = some ? (M + log2f(L * a.raise)) * kLn2 : -INFINITY;
 }
 
 template <typename Io, int ROWS>

@@ -3,7 +3,7 @@ an item's last tiles.  Against the definition in 64 bits, with the bounds of tes
 import pytest
 import torch
 
-from tests.test_gpu_paged_prompt import DEV, INF, KINDS, NAN, Case, gen
+from tests.test_gpu_paged_prompt import DEV, INF, KINDS, NAN, Case, eight, gen
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +49,41 @@ def test_last_tiles_full_of_values_that_are_not_finite(kind, H, Hk, dh, page, ch
     c.compare(out, lse)
     first = c.start[:-1].long()
     assert torch.isfinite(out[first]).all()
+
+
+def rising(c, size):
+    """Scores that rise by 18 powers of two from a sequence's first position to its last, over values of about `size` of one sign."""
+    page, dh = c.K.shape[2], c.K.shape[3]
+    c.q = torch.zeros_like(c.q)
+    c.q[..., 0] = 1.0
+    K, V = torch.zeros(c.K.shape, device=DEV), torch.full(c.V.shape, 0.0, device=DEV)
+    g = gen(21)
+    for s, n in enumerate(c.lens.tolist()):
+        p = torch.arange(n, device=DEV)
+        at = (c.table[s].long()[p // page], slice(None), p % page)
+        K[at] = torch.nn.functional.pad((p * (18 * 0.6931 / c.scale) / max(n - 1, 1))[:, None, None], (0, dh - 1)).expand(-1, K.shape[1], -1)
+        V[at] = (0.5 + 0.5 * torch.rand((n, K.shape[1], dh), generator=g, device=DEV)) * size
+    if c.kind == "8bit":
+        c.K, c.Ks, c.Kv = eight(K)
+        c.V, c.Vs, c.Vv = eight(V)
+    else:
+        c.K, c.V = K.to(c.t), V.to(c.t)
+        c.refresh()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dh,chunks", [(64, [(150, 400), (1, 0)]), (128, [(20, 3000), (300, 0)]), (256, [(9, 700)]), (128, [(5, 20000)])])
+def test_values_near_the_largest_under_rising_scores(kind, dh, chunks):
+    """fp32 caches: a plain sum of the values has to be finite."""
+    c = Case(kind, 4, 2, dh, 16, chunks)
+    rising(c, 1e34 if kind == "f32" else 3e38)
+    out, _ = c.check()
+    assert torch.isfinite(out[: int(c.start[-1])]).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "8bit"])
+@pytest.mark.parametrize("size", [1e-15, 1e15])
+def test_values_of_other_sizes(kind, size):
+    c = Case(kind, 4, 2, 128, 16, [(150, 400), (3, 5000)])
+    rising(c, size)
+    c.check()
