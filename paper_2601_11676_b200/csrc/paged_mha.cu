@@ -82,6 +82,7 @@ struct PagedArgs {
     int merge;   // bytes in front of the rings where the warps meet
     long long page_stride, q_stride;
     float scale_log2;
+    float raise;   // a part's sum of weights is times 1 / raise: 8-bit rows
     const void* q;
     const void* K;
     const void* V;
@@ -806,7 +807,8 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                 }
                 __syncwarp();   // the stage is free for the copies that the next round starts
             }
-            // the values' own size; then the warps meet, as above
+            // The values' own size last, behind the division by the sum: weights are up to 2^6, and a sum of values times them could
+            // overflow.  Then the warps meet, as above.
             const float size = 0x1p-9f * eight_unit(static_cast<uint32_t>(top_byte));
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -831,11 +833,11 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                     L[b][e] = 0.0f;
 #pragma unroll
                     for (int w = 0; w < C_::kWarps; ++w) L[b][e] = fmaf(wl[w][r], pow2(wm[w][r] - base), L[b][e]);
-                    const float f = pow2(m[b][e] - base);
+                    const float f = L[b][e] == 0.0f ? 0.0f : __fdividef(pow2(m[b][e] - base), L[b][e]);
 #pragma unroll
                     for (int n = 0; n < NC; ++n) {
-                        o[n][b][e] = o[n][b][e] * size * f;
-                        o[n][b][2 + e] = o[n][b][2 + e] * size * f;
+                        o[n][b][e] = o[n][b][e] * f * size;
+                        o[n][b][2 + e] = o[n][b][2 + e] * f * size;
                     }
                 }
             const auto each = [&](auto use) {      // of this lane's heads and pairs of columns
@@ -867,31 +869,37 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
             __syncthreads();
             if (warp == 0) {
                 add(1);
-                if (a.split > 1) put(0);
+                // a part's sum of weights as its reference; parts are 2^-10 each, so that hundreds of them do not overflow
+                const float part = 1.0f / a.raise;
+                if (a.split > 1) {
+                    each([&](int, int, float& x, float& y) { x *= part; y *= part; });
+                    put(0);
+                }
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int r = b * 8 + t4 * 2 + e;
+                        const bool none = L[b][e] == 0.0f;
+                        const auto whole = [&] { return none ? -INFINITY : M[b][e] + log2f(L[b][e]); };
                         if (a.split > 1) {
-                            if (g == 0) { wm[0][r] = M[b][e]; wl[0][r] = L[b][e]; }
+                            if (g == 0) { wm[0][r] = whole(); wl[0][r] = none ? 0.0f : part; }
                             continue;
                         }
                         if (r >= rows) continue;
                         if (complete) {
                             const bool some = L[b][e] != 0.0f && head_kept(a, h0 + r);
                             const long long row = static_cast<long long>(con.s) * a.H + h0 + r;
-                            const float f = some ? 1.0f / L[b][e] : 0.0f;
                             uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<Io*>(a.out) + row * a.dh);
 #pragma unroll
                             for (int n = 0; n < NC; ++n)
-                                if (n * 16 < a.dh) out[n * 8 + g] = some ? pack_bf16(o[n][b][e] * f, o[n][b][2 + e] * f) : 0u;
-                            if (g == 0 && a.lse) a.lse[row] = some ? (M[b][e] + log2f(L[b][e])) * kLn2 : -INFINITY;
+                                if (n * 16 < a.dh) out[n * 8 + g] = some ? pack_bf16(o[n][b][e], o[n][b][2 + e]) : 0u;
+                            if (g == 0 && a.lse) a.lse[row] = some ? whole() * kLn2 : -INFINITY;
                         } else {
-                            if (g == 0) { slot[r] = M[b][e]; slot[16 + r] = L[b][e]; }
+                            if (g == 0) { slot[r] = whole(); slot[16 + r] = none ? 0.0f : part; }
 #pragma unroll
                             for (int n = 0; n < NC; ++n)
-                                *reinterpret_cast<float2*>(slot + kSlotHead + r * DP + n * 16 + g * 2) = make_float2(o[n][b][e], o[n][b][2 + e]);
+                                *reinterpret_cast<float2*>(slot + kSlotHead + r * DP + n * 16 + g * 2) = make_float2(o[n][b][e] * part, o[n][b][2 + e] * part);
                         }
                     }
             }
@@ -1079,7 +1087,7 @@ paged_mha_kernel(const __grid_constant__ PagedArgs a) {
                 const bool some = L != 0.0f && head_kept(a, h0 + r);
                 write_head<T>(a, con.s, h0 + r, j, some ? v / L : 0.0f);
                 if (j == 0 && a.lse)
-                    a.lse[static_cast<long long>(con.s) * a.H + h0 + r] = some ? (M + log2f(L)) * kLn2 : -INFINITY;
+                    a.lse[static_cast<long long>(con.s) * a.H + h0 + r] = some ? (M + log2f(L * a.raise)) * kLn2 : -INFINITY;
             }
             cl.sync();       // nobody leaves while its sums may still be read
         }
@@ -1152,7 +1160,7 @@ __global__ void __launch_bounds__(kRangeJoin) paged_mha_join_range_kernel(const 
     const int h = o.kvh * a.G + o.r0 + r;
     const bool some = L != 0.0f && head_kept(a, h);
     if (j < a.dh) write_head<T>(a, o.s, h, j, some ? v / L : 0.0f);
-    if (j == 0 && a.lse) a.lse[static_cast<long long>(o.s) * a.H + h] = some ? (M + log2f(L)) * kLn2 : -INFINITY;
+    if (j == 0 && a.lse) a.lse[static_cast<long long>(o.s) * a.H + h] = some ? (M + log2f(L * a.raise)) * kLn2 : -INFINITY;
 }
 
 // Few items of many pieces.  blockIdx.x = item, blockIdx.y = query head of it; the thread block looks for the item among the
@@ -1250,7 +1258,7 @@ __global__ void __launch_bounds__(kItemJoin) paged_mha_join_item_kernel(const __
         for (int e = 1; e < kGroups; ++e) v += part[tid + e * DP];
     }
     if (grp == 0 && j < a.dh) write_head<T>(a, s, h, j, some ? v / L : 0.0f);
-    if (tid == 0 && a.lse) a.lse[static_cast<long long>(s) * a.H + h] = some ? (M + log2f(L)) * kLn2 : -INFINITY;
+    if (tid == 0 && a.lse) a.lse[static_cast<long long>(s) * a.H + h] = some ? (M + log2f(L * a.raise)) * kLn2 : -INFINITY;
 }
 
 struct LaunchPlan {
@@ -1403,6 +1411,7 @@ halo_status attend(const halo_paged_shape* shape, int n_seq, const void* q, long
     a.page_stride = paged_stride(*shape);
     a.q_stride = q_stride;
     a.scale_log2 = scale * 1.44269504088896340736f;
+    a.raise = eight ? 1024.0f : 1.0f;
     a.q = q;
     a.K = K_cache;
     a.V = V_cache;

@@ -3,6 +3,7 @@ an item's last tiles.  Against the definition in 64 bits, with the bounds of tes
 import pytest
 import torch
 
+from tests.test_gpu_eight_bit_cache import check_tokens, one_token_case
 from tests.test_gpu_paged_prompt import DEV, INF, KINDS, NAN, Case, eight, gen
 
 pytestmark = pytest.mark.gpu
@@ -87,3 +88,12 @@ def test_values_of_other_sizes(kind, size):
     c = Case(kind, 4, 2, 128, 16, [(150, 400), (3, 5000)])
     rising(c, size)
     c.check()
+
+
+@pytest.mark.parametrize("H,Hk,dh,lens", [(8, 2, 64, [700]), (32, 8, 128, [9, 40, 300, 1, 2500]), (8, 2, 128, [30000]), (16, 1, 256, [64, 1000]), (8, 8, 64, [300] * 150)])
+@pytest.mark.parametrize("size", [3e38, 1e-30])
+def test_one_token_over_values_near_the_largest_and_small_ones(H, Hk, dh, lens, size):
+    c = one_token_case(H, Hk, dh, 16, lens)
+    rising(c, size)
+    out, _ = check_tokens(c)
+    assert torch.isfinite(out).all()
