@@ -503,8 +503,8 @@ halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, const void*
  *   v_out, device, n_kv_heads * head_dim elements of dtype every *_stride elements.  Rows with a negative position, and those
  *   out of range (HALO_DEV_BAD_INDEX), are left as they are.
  *
- * halo_paged_mha_f8: halo_paged_mha over an 8-bit cache; its own workspace size.  A query enters the scores with the bits of
- *   fp16 relative to its row's largest element (8 bits of bf16 fit; what is below 2^-39 of the largest loses some); a weight
+ * halo_paged_mha_f8: halo_paged_mha over an 8-bit cache; its own workspace size.  A query enters the scores as fp16 relative
+ *   to its row's largest element: exactly from 2^-31 of that on, what is smaller off by at most 2^-39 of it; a weight
  *   meets the values rounded to fp16 (off by at most 2^-11 of itself, or by 2^-34 of what the largest can be).
  *
  * halo_paged_prompt_mha: causal attention of packed chunks of new tokens.  Rows q_start[s] .. q_start[s + 1] - 1 of q are the n_s

@@ -23,9 +23,9 @@
 //   8-bit rows (halo_paged_mha_f8): mma.sync on fp16, keys and values as the 16 rows of A, heads as the 8 columns of B; codes are fp16
 //     numbers exactly (one conversion for two of them), so no product is rounded, and a lane's codes decide the order of the
 //     elements, which the queries' registers follow.
-//     Queries come as fp16, a row times the power of two that brings its largest element to 2^14 (their 8 bits fit; elements
-//     below 2^-39 of the largest lose some).  A position's power of two of the keys multiplies its scores; that of the values its
-//     weights, relative to the largest so far.  Weights are relative to a reference that a score may pass by 2^6 before it
+//     Queries come as fp16, a row times the power of two that brings its largest element to 2^14: its smallest step is 2^-24 there, so
+//     that their 8 bits fit from 2^-17, 2^-31 of the largest, on, and smaller elements are off by 2^-25, 2^-39 of the largest, at most.
+//     A position's power of two of the keys multiplies its scores; that of the values its weights, relative to the largest so far.  Weights are relative to a reference that a score may pass by 2^6 before it
 //     moves, and rounded to fp16 once, times 2^9 (off by at most 2^-11 of themselves, an eighth of what the output's own
 //     rounding is; those below 2^-23 lose bits, 2^-34 at most).
 //

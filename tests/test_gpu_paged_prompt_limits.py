@@ -3,8 +3,8 @@ an item's last tiles.  Against the definition in 64 bits, with the bounds of tes
 import pytest
 import torch
 
-from tests.test_gpu_eight_bit_cache import check_tokens, one_token_case
-from tests.test_gpu_paged_prompt import DEV, INF, KINDS, NAN, Case, eight, gen
+from tests.test_gpu_eight_bit_cache import attend, check_tokens, one_token_case
+from tests.test_gpu_paged_prompt import BF16, DEV, INF, KINDS, NAN, Case, eight, gen
 
 pytestmark = pytest.mark.gpu
 
@@ -97,3 +97,23 @@ def test_one_token_over_values_near_the_largest_and_small_ones(H, Hk, dh, lens, 
     rising(c, size)
     out, _ = check_tokens(c)
     assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("bits", [0, 30, 38, 45])
+def test_queries_whose_elements_spread_over_many_powers_of_two(bits):
+    """Small elements of a query meet large ones of the keys, so that all count.  An element is exact from 2^-31 of its row's largest on, and off
+    by at most 2^-39 of that below."""
+    c = one_token_case(8, 2, 64, 16, [200, 31])
+    by = torch.exp2(-(torch.arange(64, device=DEV) * bits // 63).float())
+    c.q = (c.q.float() * by).to(BF16)
+    c.K, c.Ks, c.Kv = eight(torch.randn(c.K.shape, generator=gen(5), device=DEV) / by)
+    out, lse, bad = attend(c, c.q)
+    ref, ref_lse, size, reach, _, _ = c.expected()
+    e = (2.0 ** -21 + 64 * 2.0 ** -24 + 2.0 ** -20) * reach
+    # the largest lies in [2^14, 2^15) and fp16's smallest step is 2^-24: an element is off by 2^-25 at most, 2^-39 of the largest.  Elements
+    # are 2^-bits times a normal number, so that with 30 bits too a few lie below 2^-31 of the largest
+    e = e + 2.0 ** -39 * c.q.double().abs().amax(-1) * c.Kv.abs().sum(-1).max() * c.scale
+    top = 448 * torch.exp2(c.Vs.double().max() - 127)
+    rough = (2 * e + 1e-5 + 2.0 ** -11)[..., None] * size + (c.lens.double() * 2.0 ** -34 * top)[:, None, None]
+    assert bad == 0 and ((out.double() - ref).abs() <= rough + 2.0 ** -8 * ref.abs()).all()
+    assert ((lse.double() - ref_lse).abs() <= e + 1e-6 * (1 + ref_lse.abs())).all()
