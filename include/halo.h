@@ -518,7 +518,8 @@ halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, const void*
  *   not see has no influence on it, NaN and infinities included (which may change the order of its sums).
  *   fp32 sums and softmax; bf16 and 8-bit caches: a weight meets the values rounded to bf16 (2^-8 of itself), and sums are scaled so that
  *   finite values do not overflow in them (values below 2^-60 in size may be lost).
- *   A sequence whose rows are out of range or decrease is left out, one whose length is negative or behind the table
+ *   A sequence whose rows are out of range, decrease, or begin in front of the end of an earlier one's that are in range is left
+ *   out, one whose length is negative or behind the table
  *   counts as empty, positions on a page out of range are left out; each sets HALO_DEV_BAD_INDEX.
  *   workspace: halo_paged_prompt_mha_workspace_bytes(shape, n_tok, n_seq) bytes, as for halo_paged_mha.  The result does not depend
  *   on timing.  n_seq <= HALO_MAX_SEQUENCES, n_tok <= HALO_MAX_PROMPT_ROWS.

@@ -47,14 +47,15 @@ def prompt_mha(q, q_start, K, V, table, lens, scale, keep=None):
     Hk, page_size, cap = K.shape[1], K.shape[2], table.shape[1] * K.shape[2]
     out, size = np.zeros((n_tok, H, dh)), np.zeros((n_tok, H, dh))
     lse, reach = np.full((n_tok, H), -np.inf), np.zeros((n_tok, H))
-    mine, bad = np.zeros(n_tok, bool), False
+    mine, bad, end = np.zeros(n_tok, bool), False, 0
     for s in range(len(lens)):
         a, b, length = int(q_start[s]), int(q_start[s + 1]), int(lens[s])
         if not 0 <= length <= cap:
             bad, length = True, 0
-        if not 0 <= a <= b <= n_tok:
-            bad = True
+        if not 0 <= a <= b <= n_tok or a < end:      # rows of two sequences belong to the first one
+            bad, end = True, max(end, b) if 0 <= a <= b <= n_tok else end
             continue
+        end = b
         mine[a:b] = True
         for t in range(a, b):
             for p_end in [length - (b - t) + 1]:

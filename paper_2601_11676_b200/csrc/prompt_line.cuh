@@ -69,11 +69,17 @@ __device__ __forceinline__ bool head_kept(const Args& a, int h) { return !a.keep
 struct Rows {      // of a sequence
     int first, n, len;
 };
-__device__ __forceinline__ Rows rows_of(const Args& a, int s, bool flag) {
+struct Order {     // of sequences in front
+    int end;         // the largest end of those whose rows are in range
+    bool falls;      // a start was behind its end
+};
+__device__ __forceinline__ Rows rows_of(const Args& a, int s, Order& o, bool flag) {
     const int q0 = ldg_waited(a.q_start + s), q1 = ldg_waited(a.q_start + s + 1), len = ldg_waited(a.seq_len + s);
-    const bool rows = q0 >= 0 && q1 >= q0 && q1 <= a.n_tok;
+    const bool in = q0 >= 0 && q1 >= q0 && q1 <= a.n_tok, rows = in && q0 >= o.end;      // rows of two sequences belong to the first one
     const bool fits = len >= 0 && len <= static_cast<long long>(a.max_pages) * a.page_size;
     if (flag && !(rows && fits)) flag_status(a.status, HALO_DEV_BAD_INDEX);
+    o.falls |= q1 < q0;
+    if (in) o.end = max(o.end, q1);
     return {q0, rows ? q1 - q0 : 0, fits ? len : 0};
 }
 
@@ -143,6 +149,7 @@ struct Walk {
     using L = Line<ROWS, TILE, OVER>;
     long long left;      // units from u0 of this item to the end of the range
     Rows r;
+    Order order;         // of the sequences up to this one
     int s, kvh, rb, nb;
     int u0, u1;          // units of the item that the range has
     int nt, t0, t1;      // tiles of the item, and of them this piece's
@@ -170,7 +177,7 @@ struct Walk {
                 rb = 0;
                 if (++kvh == a.Hk) {
                     kvh = 0;
-                    do r = rows_of(a, ++s, false);
+                    do r = rows_of(a, ++s, order, false);
                     while (r.n == 0);      // a range ends with the last item: there is one
                     nb = L::blocks_of(a, r);
                 }
@@ -195,20 +202,45 @@ __device__ __forceinline__ Found<ROWS, TILE, OVER> locate(const Args& a, long lo
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (a.n_seq + THREADS - 1) / THREADS;
     const int s0 = min(tid * per, a.n_seq), s1 = min(s0 + per, a.n_seq);
-    long long own = 0, first = 0;      // units of one K/V head: of all this thread's sequences, of its first
-    for (int s = s0; s < s1; ++s) {
-        const long long n = L::per_head(a, rows_of(a, s, blockIdx.x == 0));
-        if (s == s0) first = n;
-        own += n;
-    }
-    long long incl = own;
+    long long own, first, incl;             // units of one K/V head: of all this thread's sequences, of its first; of all up to it
+    Order front = {0, false}, behind;       // of the sequences in front of this thread's, and behind its first one
+    const auto count = [&] {
+        Order o = front;
+        own = first = 0;
+        for (int s = s0; s < s1; ++s) {
+            const long long n = L::per_head(a, rows_of(a, s, o, blockIdx.x == 0));
+            if (s == s0) {
+                first = n;
+                behind = o;
+            }
+            own += n;
+        }
+        incl = own;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += v;
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, incl, d);
+            if (lane >= d) incl += v;
+        }
+        if (lane == 31) sh[warp] = incl;
+        return o;
+    };
+    const Order upto = count();
+    if (__syncthreads_or(upto.falls)) {     // starts that fall: rows may belong to two sequences; the ends in front of this thread's
+        int end = upto.end;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, end, d);
+            if (lane >= d) end = max(end, v);
+        }
+        if (lane == 31) sh[warp] = end;
+        __syncthreads();
+        end = __shfl_up_sync(0xffffffffu, end, 1);
+        if (lane > 0) front.end = end;
+        for (int w = 0; w < warp; ++w) front.end = max(front.end, static_cast<int>(sh[w]));
+        __syncthreads();
+        count();
+        __syncthreads();
     }
-    if (lane == 31) sh[warp] = incl;
-    __syncthreads();
     long long before = 0, total = 0;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
@@ -226,11 +258,14 @@ __device__ __forceinline__ Found<ROWS, TILE, OVER> locate(const Args& a, long lo
     const long long x = cut(f.total, blockIdx.x, C);
     long long at = (before + incl - own) * a.Hk;
     if (x >= at && x < at + own * a.Hk) {
+        Order o = front;
         for (int s = s0; s < s1; ++s) {
-            const long long n = s == s0 ? first : L::per_head(a, rows_of(a, s, false));
+            const int end = o.end;
+            const long long n = s == s0 ? first : L::per_head(a, rows_of(a, s, o, false));
+            if (s == s0) o = behind;
             if (x < at + n * a.Hk) {
                 sh[W] = x - at;
-                sh[W + 1] = s;
+                sh[W + 1] = static_cast<long long>(end) << 32 | s;
                 sh[W + 2] = n;
                 break;
             }
@@ -240,8 +275,9 @@ __device__ __forceinline__ Found<ROWS, TILE, OVER> locate(const Args& a, long lo
     __syncthreads();
     const long long inside = sh[W], per_head = sh[W + 2];
     w.s = static_cast<int>(sh[W + 1]);
+    w.order = {static_cast<int>(sh[W + 1] >> 32), false};
     w.left = cut(f.total, blockIdx.x + 1, C) - x;
-    w.r = rows_of(a, w.s, false);
+    w.r = rows_of(a, w.s, w.order, false);
     w.nb = L::blocks_of(a, w.r);
     w.kvh = static_cast<int>(quotient(inside, per_head));
     // the item: 32 at a time

@@ -1,8 +1,10 @@
 """halo_paged_prompt_mha and halo_paged_mha_f8 where contents are extreme: values that are infinite or NaN over long sequences and in all of
 an item's last tiles.  Against the definition in 64 bits, with the bounds of test_gpu_paged_prompt and test_gpu_eight_bit_cache."""
+import numpy as np
 import pytest
 import torch
 
+from oracle import paged_prompt_ref as P
 from tests.test_gpu_eight_bit_cache import attend, check_tokens, one_token_case
 from tests.test_gpu_paged_prompt import BF16, DEV, INF, KINDS, NAN, Case, eight, gen
 
@@ -117,3 +119,53 @@ def test_queries_whose_elements_spread_over_many_powers_of_two(bits):
     rough = (2 * e + 1e-5 + 2.0 ** -11)[..., None] * size + (c.lens.double() * 2.0 ** -34 * top)[:, None, None]
     assert bad == 0 and ((out.double() - ref).abs() <= rough + 2.0 ** -8 * ref.abs()).all()
     assert ((lse.double() - ref_lse).abs() <= e + 1e-6 * (1 + ref_lse.abs())).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("start,mine", [
+    ([0, 20, 10, 30], [20, 0, 0]),                      # the third begins inside the first
+    ([0, 20, 10, 30, 25, 40], [20, 0, 0, 0, 0]),        # the fifth inside the third, which is left out
+    ([5, 3, 9, 9, 30, 12, 40, 40], [0, 6, 0, 21, 0, 0, 0]),
+    ([0, 10, 10 ** 6, 10, 25], [10, 0, 0, 15]),         # what is out of range holds nothing
+    ([30, 40, 0, 12, 8, 20, 39, 40], [10, 0, 0, 0, 0, 0, 0]),
+])
+def test_rows_that_two_sequences_claim(kind, start, mine):
+    """They belong to the first one; the other is left out as a whole."""
+    n = len(mine)
+    c = Case(kind, 4, 2, 64, 16, [(40, 100 + 30 * s) for s in range(n)])
+    c.q = c.q[:40].contiguous()
+    for s in range(n):
+        c.lens[s] -= 40 - max(start[s + 1] - start[s], 0) if start[s + 1] <= 40 else 0
+    c.start = torch.tensor(start, dtype=torch.int32, device=DEV)
+    out, lse, bad = c.run()
+    assert bad != 0
+    # the same calls with the others' rows taken away
+    want, want_lse = c.buffers()
+    for s, k in enumerate(mine):
+        if k:
+            one = Case(kind, 4, 2, 64, 16, [(40, 100 + 30 * i) for i in range(n)])
+            one.q, one.table, one.lens = c.q[start[s]:start[s] + k].contiguous(), c.table[s:s + 1].contiguous(), c.lens[s:s + 1].contiguous()
+            one.start = torch.tensor([0, k], dtype=torch.int32, device=DEV)
+            one.compare(out[start[s]:start[s] + k], lse[start[s]:start[s] + k])
+            want[start[s]:start[s] + k], want_lse[start[s]:start[s] + k] = out[start[s]:start[s] + k], lse[start[s]:start[s] + k]
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)          # the other rows stay as they were
+
+
+def test_many_sequences_that_claim_rows_twice():
+    """More of them than a thread block has threads."""
+    starts, n = [0], 700
+    g = np.random.default_rng(8)
+    for i in range(n):
+        starts.append(max(starts[-1] - 3, 0) if i % 50 == 20 else starts[-1] + int(g.integers(0, 3)))
+    c = Case("bf16", 4, 2, 64, 16, [(2, int(g.integers(2, 60))) for _ in range(n)])
+    c.q = c.q[: max(starts)].contiguous()
+    c.start = torch.tensor(starts, dtype=torch.int32, device=DEV)
+    out, lse, bad = c.run()
+    ref, ref_lse, size, reach, mine, ref_bad = P.prompt_mha(c.q.double().cpu().numpy(), np.array(starts), c.Kv.cpu().numpy(), c.Vv.cpu().numpy(),
+                                                            c.table.cpu().numpy(), c.lens.cpu().numpy(), c.scale)
+    assert bad != 0 and ref_bad and not mine.all()
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    assert (out[~mine] == 7).all() and (lse[~mine] == 7).all()
+    e = (2.0 ** -21 + 64 * 2.0 ** -24 + 2.0 ** -20) * reach
+    assert (np.abs(lse - ref_lse) <= e + 1e-5 + 1e-6 * (1 + np.abs(ref_lse)))[mine].all()
+    assert (np.abs(out - ref) <= (2 * e + 1e-5 + 2.0 ** -8)[..., None] * size + 2.0 ** -8 * np.abs(ref))[mine].all()
