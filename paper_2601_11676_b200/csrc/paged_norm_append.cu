@@ -86,6 +86,32 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
     return v;
 }
 
+// 1 / sqrt(mean(x^2) + eps) of rows of dh elements, N of which a lane has; by whole warps.  Rows whose squares pass the largest number become
+// 2^-70 of themselves where they are normed (eps is nothing beside them), and so does their factor's reference.
+template <int LANES, int N>
+__device__ __forceinline__ float norm_factor(float (&f)[N], bool normed, int dh, float eps) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) sum = fmaf(f[e], f[e], sum);
+    sum = lanes_sum<LANES>(sum);
+    const bool past = !(sum < INFINITY);
+    if (__any_sync(0xffffffffu, past)) {
+        float less = 0.0f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float x = f[e] * 0x1p-70f;
+            less = fmaf(x, x, less);
+            if (past && normed) f[e] = x;
+        }
+        less = lanes_sum<LANES>(less);
+        if (past) {
+            sum = less;
+            eps = 0.0f;
+        }
+    }
+    return rsqrtf(sum / static_cast<float>(dh) + eps);
+}
+
 // Thread block (token, part): heads part * groups + group, ... in steps of groups * parts.
 template <typename T, int LANES, bool EIGHT>
 __global__ void __launch_bounds__(kThreads)
@@ -170,12 +196,8 @@ paged_norm_append_any_kernel(const __grid_constant__ NormAppendArgs a, int parts
         if (there) x.widen(f);
         const bool normed = !is_v && (is_q ? a.w_q : a.w_k) != nullptr;
         if (a.w_q || a.w_k) {
-            float sum = 0.0f;
-#pragma unroll
-            for (int e = 0; e < kOwn; ++e) sum = fmaf(f[e], f[e], sum);
-            sum = lanes_sum<LANES>(sum);
+            const float n = norm_factor<LANES>(f, normed, a.dh, a.eps);
             if (there && normed) {
-                const float n = rsqrtf(sum / static_cast<float>(a.dh) + a.eps);
 #pragma unroll
                 for (int e = 0; e < kOwn; ++e) f[e] = f[e] * n * (is_q ? wq[e] : wk[e]);
             }
@@ -305,28 +327,22 @@ paged_norm_append_kernel(const __grid_constant__ NormAppendArgs a, int parts) {
 #pragma unroll
             for (int e = 0; e < kOwn; ++e) f[0][e] = f[1][e] = 0.0f;
         }
-        float n = 1.0f;
         if (__any_sync(0xffffffffu, there && !is_v)) {       // queries or keys among the warp's heads
             const bool normed = !is_v && (is_q ? a.w_q : a.w_k) != nullptr;
-            if (a.w_q || a.w_k) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int e = 0; e < kOwn; ++e) sum = fmaf(f[0][e], f[0][e], fmaf(f[1][e], f[1][e], sum));
-                sum = lanes_sum<LANES>(sum);
-                if (normed) n = rsqrtf(sum / static_cast<float>(a.dh) + a.eps);
-            }
+            float n = 1.0f;
+            if (a.w_q || a.w_k) n = norm_factor<LANES>(reinterpret_cast<float(&)[2 * kOwn]>(f), normed, a.dh, a.eps);
             if (!is_v && there) {
-                if (normed) {
+                if (normed) {      // first of all: a gain or a turn could carry the elements themselves out of range
                     const float* g = gain[is_q ? 0 : 1];
 #pragma unroll
                     for (int w = 0; w < 2; ++w)
 #pragma unroll
                         for (int e = 0; e < kOwn; e += 4) {
                             const float4 by = *reinterpret_cast<const float4*>(g + (w ? el1 : el0) + e);
-                            f[w][e] *= by.x;
-                            f[w][e + 1] *= by.y;
-                            f[w][e + 2] *= by.z;
-                            f[w][e + 3] *= by.w;
+                            f[w][e] = f[w][e] * n * by.x;
+                            f[w][e + 1] = f[w][e + 1] * n * by.y;
+                            f[w][e + 2] = f[w][e + 2] * n * by.z;
+                            f[w][e + 3] = f[w][e + 3] * n * by.w;
                         }
                 }
 #pragma unroll
@@ -347,7 +363,6 @@ paged_norm_append_kernel(const __grid_constant__ NormAppendArgs a, int parts) {
 #pragma unroll
             for (int e = 0; e < kOwn; ++e)
                 top = max(top, max(__float_as_uint(f[0][e]) & 0x7fffffffu, __float_as_uint(f[1][e]) & 0x7fffffffu));
-            top = __float_as_uint(__uint_as_float(top) * n) & 0x7fffffffu;      // the largest stays it: products round in order
             top = lanes_max<LANES>(top);
             if (there && !is_q) {
                 const bool sound = top < 0x7f800000u;
@@ -360,8 +375,7 @@ paged_norm_append_kernel(const __grid_constant__ NormAppendArgs a, int parts) {
                     uint32_t c[2];
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
-                        c[j] = sound ? eight_pair(f[w][4 * j] * n * by, f[w][4 * j + 1] * n * by) |
-                                           eight_pair(f[w][4 * j + 2] * n * by, f[w][4 * j + 3] * n * by) << 16 : 0u;
+                        c[j] = sound ? eight_pair(f[w][4 * j] * by, f[w][4 * j + 1] * by) | eight_pair(f[w][4 * j + 2] * by, f[w][4 * j + 3] * by) << 16 : 0u;
                     *reinterpret_cast<uint2*>(to + (w ? el1 : el0)) = make_uint2(c[0], c[1]);
                 }
                 if (u == 0)
@@ -372,12 +386,8 @@ paged_norm_append_kernel(const __grid_constant__ NormAppendArgs a, int parts) {
         if (there && (is_q || !EIGHT)) {
             T* to = is_q ? qo + h * a.dh : is_v ? static_cast<T*>(a.V) + base + (h - a.H - a.Hk) * plane : static_cast<T*>(a.K) + base + (h - a.H) * plane;
             if (!is_v) {
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-#pragma unroll
-                    for (int e = 0; e < kOwn; ++e) f[w][e] *= n;
-                    x[w].narrow(f[w]);
-                }
+                x[0].narrow(f[0]);
+                x[1].narrow(f[1]);
             }
             x[0].store(to + el0);
             x[1].store(to + el1);
