@@ -34,3 +34,22 @@ def test_infinite_elements_leave_the_other_rows_alone(kind, dh, rotary):
     assert torch.equal(k[rest], b.read()[0][rest]) and torch.equal(a.q_out, b.q_out)
     row = k[7, 1]
     assert torch.isnan(row[dh - 1]) and int(torch.isnan(row).sum()) == (2 if rotary == dh else 1) and (row[~torch.isnan(row)] == 0).all()
+
+
+@pytest.mark.parametrize("dh,rotary,inter", [(64, 64, False), (128, 64, True), (96, 24, False)])
+@pytest.mark.parametrize("turn_scale", [1.0, 1.1386])
+def test_cosines_and_sines_are_the_nearest(dh, rotary, inter, turn_scale):
+    """Of pairs (1, 0) the turned ones are the cosine and the sine times turn_scale: rounded once, so equal to the 64-bit ones rounded but where
+    the angle's own error (1e-10 for positions up to 10^5) meets a tie."""
+    a = Append("f32", 4, 2, dh, 16, 200, rotary, inter, "none", turn_scale)
+    a.q.zero_()
+    first = slice(0, rotary, 2) if inter else slice(0, rotary // 2)
+    second = slice(1, rotary, 2) if inter else slice(rotary // 2, rotary)
+    a.q[..., first] = 1.0
+    a.call()
+    angle = a.pos.double()[:, None] * a.inv
+    scale = torch.tensor(turn_scale, dtype=torch.float32).double().item()
+    for part, want in ((first, torch.cos(angle) * scale), (second, torch.sin(angle) * scale)):
+        got, want = a.q_out[..., part], want[:, None].expand(-1, 4, -1)
+        assert ((got.double() - want).abs() <= 2.0 ** -24 * want.abs() + 1e-10).all()
+        assert (got == want.float()).float().mean() > 0.99
