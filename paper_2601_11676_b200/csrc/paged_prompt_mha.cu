@@ -965,7 +965,9 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm)
     uint32_t k = 0;
     for (Piece p; alive && next_piece(sm, k, p);) {
         if (t < p.streams) {
-            const Row row = row_at<C::kRows>(a, p.r, p.kvh, p.rb, item_row);
+            Row row = row_at<C::kRows>(a, p.r, p.kvh, p.rb, item_row);
+            if (!row.there) row.sees = 0;
+            const float limit = row.there ? most_sum : INFINITY - INFINITY;      // NaN: nothing is as large
             const int n = p.tiles(t);
             const int all_see = p.r.len - p.r.n + 1 + (p.rb * C::kRows + t * 128) / a.G;
             float m = -INFINITY, l = 0.0f;
@@ -1036,8 +1038,9 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm)
                     if (row.sees > p0 && (there[0] & 1u) && fabsf(first_score) < INFINITY) m = first_score;
                 }
                 float more = masked ? weights(Const<1>()) : weights(Const<0>());
-                // a new reference, or something infinite or NaN: from the scores again.  A row moves by what it sees alone, not by its neighbours.
-                const bool anew = !(more < most_sum) || !(m > -INFINITY || row.sees <= p0);
+                // a new reference: from the scores again.  A row moves by what it sees alone, not by its neighbours, and not where its weights
+                // are NaN, which no reference mends; what lies in rows of no sequence moves nothing.
+                const bool anew = more >= limit || !(m > -INFINITY || row.sees <= p0);
                 if (__any_sync(0xffffffffu, anew)) {
                     float mx = -INFINITY;
                     each(Const<1>(), [&](int, const uint32_t (&sc)[32], bool none) {
@@ -1089,7 +1092,7 @@ __device__ __forceinline__ void softmax_rows(const Args& a, Smem<DP, EIGHT>& sm)
             }
             if (n > 0 && alive) await_sums(n - 1);
             if (CARE && alive)
-                alive = add_odd<DP, EIGHT>(a, sm, p, k - 1, n, row.token, row.head, row.there ? row.sees : 0, (m == -INFINITY ? 0.0f : m * scale) + a.lower, o_addr);
+                alive = add_odd<DP, EIGHT>(a, sm, p, k - 1, n, row.token, row.head, row.sees, (m == -INFINITY ? 0.0f : m * scale) + a.lower, o_addr);
             if (!alive) break;
             const bool some = l != 0.0f && row.kept;
             const long long at = static_cast<long long>(row.token) * a.H + row.head;

@@ -1,5 +1,6 @@
 """halo_paged_prompt_mha and halo_paged_mha_f8 where contents are extreme: values that are infinite or NaN over long sequences and in all of
-an item's last tiles.  Against the definition in 64 bits, with the bounds of test_gpu_paged_prompt and test_gpu_eight_bit_cache."""
+an item's last tiles, values near the largest number, queries of many powers of two, rows of two sequences or of none.  Against the
+definition in 64 bits, with the bounds of test_gpu_paged_prompt and test_gpu_eight_bit_cache."""
 import numpy as np
 import pytest
 import torch
@@ -169,3 +170,18 @@ def test_many_sequences_that_claim_rows_twice():
     e = (2.0 ** -21 + 64 * 2.0 ** -24 + 2.0 ** -20) * reach
     assert (np.abs(lse - ref_lse) <= e + 1e-5 + 1e-6 * (1 + np.abs(ref_lse)))[mine].all()
     assert (np.abs(out - ref) <= (2 * e + 1e-5 + 2.0 ** -8)[..., None] * size + 2.0 ** -8 * np.abs(ref))[mine].all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("H,Hk,dh", [(32, 8, 128), (8, 2, 64), (6, 2, 256)])
+@pytest.mark.parametrize("what", [NAN, INF, 3e38])
+def test_rows_of_no_sequence_have_no_influence(kind, H, Hk, dh, what):
+    """A padded batch: whatever lies behind the last sequence's rows changes no bit of the others."""
+    c = Case(kind, H, Hk, dh, 16, [(5, 300), (1, 900), (140, 200), (3, 40)], rows_behind=200)
+    c.start = torch.tensor([0, 5, 6, 146, 149], dtype=torch.int32, device=DEV)
+    got = []
+    for fill in (0.0, what):
+        c.q[149:] = fill
+        out, lse = c.check()
+        got.append((out, lse))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
