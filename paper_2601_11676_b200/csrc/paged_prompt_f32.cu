@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(kThreads) paged_prompt_rows_kernel(const __gri
             }
             cp_wait<1>();
             __syncthreads();
-            const bool whole = p0 + kTile <= all_see;   // else: a weight of zero meets nothing, so that a value behind a row's last cannot reach it
+            const bool whole = p0 + kTile <= all_see;   // else: what a row does not see meets nothing, as its value may be infinite or NaN
 #pragma unroll 1
             for (int k0 = 0; k0 < kTile; k0 += 4) {
                 float4 v[4][V];
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(kThreads) paged_prompt_rows_kernel(const __gri
                     const float e[4] = {e4.x, e4.y, e4.z, e4.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        if (!whole && e[i] == 0.0f) continue;
+                        if (!whole && p0 + k0 + i >= sees[r]) continue;
 #pragma unroll
                         for (int g = 0; g < V; ++g) {
                             o[r][4 * g] = fmaf(e[i], v[i][g].x, o[r][4 * g]);

@@ -185,3 +185,17 @@ def test_rows_of_no_sequence_have_no_influence(kind, H, Hk, dh, what):
         out, lse = c.check()
         got.append((out, lse))
     assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("past", [0, 300])
+def test_a_value_of_nan_counts_however_small_its_weight(kind, past):
+    """Weights that underflow: of the first keys, in tiles that every row sees and in an item's last ones."""
+    c = Case(kind, 4, 2, 64, 16, [(100, past)])
+    rising(c, 1.0)
+    c.q[..., 0] = 40.0                                   # 720 powers of two from the first key to the last
+    spoil(c, 0, past, 5, NAN)
+    out, _, bad = c.run()
+    assert bad == 0
+    assert torch.isnan(out[:100, :, 5]).all()            # every row sees that position
+    assert kind == "8bit" or torch.isfinite(out[:100, :, 6]).all()
