@@ -34,7 +34,7 @@
 // positions, 32 / 4 heads of 64: 6.3 us (launch, one chain of loads, a cluster's meeting), 8.5 under a table of 131072
 // positions (the line: the plan goes by the table's width); fp32, 7 sequences of up to 1500 positions, 8 / 8 heads of 64:
 // 9.3 us (the same chain, 18 MB).
-// 8-bit rows: the one of 131071 55 to 57 us (271 MB: 4.9 TB/s), the 64 sequences 63, the one of 700 6.5.  The conversions keep them off
+// 8-bit rows: the one of 131071 56 to 58 us (271 MB: 4.8 TB/s), the 64 sequences 64, the one of 700 6.8.  The conversions keep them off
 // HBM's rate: 436 instructions of a warp to 16 positions, two a clock and SM.
 #include <cooperative_groups.h>
 #include <math.h>
@@ -180,8 +180,8 @@ struct Cfg {
     // fp32: two stages, so that two thread blocks of four warps fit an SM at head sizes up to 64, or of three at 128 with
     // one query head per K/V head.  64 sequences of up to 2000 positions, 32 / 8 heads of 64: 77 us with three stages and
     // one thread block, 59 so; 5 of up to 900, 8 / 8 heads of 128: 13.1 us with one thread block of four warps, 10.4 so.
-    // 8-bit rows: the widening of codes bounds them, and more warps help more than more stages: with two and 8 heads, five thread
-    // blocks of 128 columns fit an SM (128 sequences of up to 600 positions, 32 heads of 128: 117 us with two, 131 with three; 16
+    // 8-bit rows: the widening of codes bounds them, and more warps help more than more stages: with two and 8 heads, four thread
+    // blocks of 128 columns fit an SM, with three stages three (128 sequences of up to 600 positions, 32 heads of 128: 117 us with two, 131 with three; 16
     // heads on one have registers for two thread blocks only: 64 sequences of 4000 108 us with two, 84 with three).
     static constexpr int kStages = kF32 ? 2 : kEight && GR <= 8 ? 2 : 3;
     static constexpr int kTile = kWarps * kRun;

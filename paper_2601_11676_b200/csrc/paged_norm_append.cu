@@ -1,7 +1,7 @@
 // halo_paged_norm_append: the keys and values of new tokens go to their pages in the caches' type or as 8-bit rows, queries
 // and keys normed per head and turned by their position on the way; halo_paged_kv_read: rows back out of the pages.
-// Every element is read once and written once.  8297 tokens, 32 + 2 * 8 heads of 128, into 8-bit rows: 50 us where HBM would
-// take 28 (187 MB; the instructions bound it), read back in 11 (52 MB: 8).
+// Every element is read once and written once.  8297 tokens, 32 + 2 * 8 heads of 128, into 8-bit rows: 47 us where HBM would
+// take 28 (187 MB; the instructions bound it), read back in 9 to 11 (52 MB: 8).  Into bf16 rows 44 (204 MB: 31), fp32 69 (408 MB: 62).
 //
 //   y = x / sqrt(mean(x^2) + eps) * w over a head's elements (queries and keys that have a gain), then pair i of the first
 //   rotary elements by the angle pos * inv_freq[i], times turn_scale.  Angles are reduced to one turn in fp64 as in
@@ -15,7 +15,8 @@
 // shuffles.  One head of a lane is in flight at a time: three took more registers, and 8297 tokens into 8-bit rows 64 us and not 59.
 // An element costs about ten instructions; with one word to a lane (and its partners' from another) it was twice that,
 // and the instructions were what bounded it.  Pairs whose distance is no whole number of eight elements go by that form
-// (paged_norm_append_any_kernel): through a row of shared memory that only the warp's own lanes touch.
+// (paged_norm_append_any_kernel): through a row of shared memory that only the warp's own lanes touch.  8297 tokens of 32 + 2 * 8 heads of 80, of
+// which 40 are turned: 107 us into 8-bit rows, 87 into bf16.
 #include <math.h>
 
 #include "eight.cuh"
@@ -434,8 +435,8 @@ struct ReadArgs {
     uint32_t* status;
 };
 
-// Thread block: a token (four, with their chains of loads side by side, took 15.1 us and not 13.7 for 8297 tokens, 8 heads of 128 in 8
-// bits).  A unit is 16 bytes of the cache: of 8-bit rows 16 codes, which leave as 32 bytes of bf16.
+// Thread block: a token (four, with their chains of loads side by side, took 15.1 us and not 12.7 for 8297 tokens, 8 heads of 128 in 8
+// bits, in thread blocks of four warps).  A unit is 16 bytes of the cache: of 8-bit rows 16 codes, which leave as 32 bytes of bf16.
 template <typename T, bool EIGHT>
 __global__ void __launch_bounds__(kThreads) paged_kv_read_kernel(const __grid_constant__ ReadArgs a) {
     constexpr int E = EIGHT ? 16 : Elem<T>::kPerChunk;

@@ -30,10 +30,11 @@
 // A weight meets the values as one bf16 number: as two, the sums, half of the products, would be twice as many.  Outputs are then
 // 0.0023 (relative) from 64 bits where their own rounding alone is 0.0017.
 //
-// Measured, both kernels: 4096 tokens, 32 / 8 heads of 128, 188 to 191 us (0.73 PFLOP/s); 8192 tokens, 16 / 4 heads of 128, 320 us
-// (0.86); 512 tokens over 32000 positions in 8 bits, 32 / 8 heads, 360 us (0.75); 7 packed prompts of up to 1500 tokens, 32 / 32
-// heads, 209 to 212 us (0.43); 1 to 8 tokens for each of 16 sequences of up to 4000 positions, 32 / 8 heads, 44 us (3.3 TB/s).
-// The tensor pipe is active 34 to 42 % of the time and the unit of the powers of two as much: a tile of a stream is 1800 clocks in its
+// Measured, both kernels, on different GPUs: 4096 tokens, 32 / 8 heads of 128, 180 to 186 us (0.74 to 0.76 PFLOP/s), of 64 143 to 147;
+// 8192 tokens, 16 / 4 heads of 128, 310 to 316 (0.88); 512 tokens over 32000 positions in 8 bits, 32 / 8 heads, 347 to 357 (0.77); 7 packed
+// prompts of up to 1500 tokens, 32 / 32 heads, 204 to 212 (0.44); 1 to 8 tokens for each of 16 sequences of up to 4000 positions, 32 / 8
+// heads, 45 (3.2 TB/s).
+// The tensor pipe is active 35 to 39 % of the time and the unit of the powers of two as much: a tile of a stream is 1800 clocks in its
 // softmax and then 1900 until its next scores (its sums, their completion, its scores: 1300 if nothing else asked shared memory).
 #include <math.h>
 
