@@ -515,7 +515,8 @@ halo_status halo_paged_mha(const halo_paged_shape* shape, int n_seq, const void*
  *   q_start[n_seq] <= n_tok; out device [n_tok][n_heads][head_dim], must not overlap q; lse device fp32 [n_tok][n_heads] or
  *   NULL.  Rows of no sequence have no influence and are not written.  keep as in halo_paged_mha.
  *   A row that sees nothing (P < 0, a lost head, scores that are all -infinity) gives zeros and lse = -infinity.  What a row does
- *   not see has no influence on it, NaN and infinities included (which may change the order of its sums).
+ *   not see has no influence on it, NaN and infinities included (values that hold some may change the order of its sums, and make the
+ *   call several times as long).
  *   fp32 sums and softmax; bf16 and 8-bit caches: a weight meets the values rounded to bf16 (2^-8 of itself), and sums are scaled so that
  *   finite values do not overflow in them (values below 2^-60 in size may be lost).
  *   A sequence whose rows are out of range, decrease, or begin in front of the end of an earlier one's that are in range is left
